@@ -669,6 +669,148 @@ typedef struct gemel_kernel_stat {
 gemel_status gemel_profile(gemel_ctx *ctx, gemel_kernel_stat *stats,
                            int32_t *rounds);
 
+/*
+ * ---- Serving and retraining merged layers ----
+ *
+ * A merged FC layer, or a merged 1x1 convolution over NHWC pixels, is one
+ * projection y = x W^T + bias that the rows (frames, pixels) of many models
+ * go through. Where one weight copy costs a model accuracy, the method
+ * retrains the shared layers jointly; a low-rank adapter per model keeps the
+ * single copy and lets the models differ. The calls below run such a
+ * projection for many requests at once, give its gradients, and update
+ * matrices with orthogonalised steps.
+ *
+ * Conventions of these calls:
+ *  - All data are device pointers to row-major matrices whose rows are
+ *    contiguous; a stride is the distance between rows in elements. The
+ *    element type is the context's (GEMEL_F32: float; GEMEL_BF16: bf16)
+ *    unless a call says float32. Pointers are aligned to their element.
+ *    Any sizes and strides are taken; 16-byte aligned rows whose length is
+ *    a multiple of 8 are read in place, others are first copied.
+ *  - Outputs must not overlap inputs or each other.
+ *  - The calls enqueue on hip_stream (NULL = the null stream) and return.
+ *    Calls on one stream share a workspace of the context, which grows to
+ *    the largest call (growing synchronises the device) and is kept until
+ *    gemel_destroy; calls on different streams do not wait for each other.
+ *  - While hip_stream is being captured into a graph a call is enqueued if
+ *    an earlier call of the same sizes on that stream has grown the
+ *    workspace, else it returns ESTATE. Replays of the graph use that
+ *    workspace, so they are ordered after other work on the stream, and the
+ *    graph is not replayed once a larger call on that stream has grown it.
+ *  - Sums are float32 (norms float64), in an order that the sizes alone
+ *    fix: the same call on the same data gives the same bits. float32
+ *    contexts multiply float32 values as pairs of float16 (22 bits, each
+ *    row scaled by a power of two); a row holding a value that is not
+ *    finite gives results that are not finite.
+ */
+
+/*
+ * Put together a batch of requests: request i brings n_rows[i] rows (>= 0;
+ * the rows of all requests follow each other) and uses adapter
+ * adapter_ids[i], or none where that is -1.
+ *  n_adapters, max_rank   sizes of the bank the adapters lie in
+ *                         (max_rank 1..256).
+ *  ranks   NULL (all max_rank), or per adapter its rank in 1..max_rank: the
+ *          bank's entries from that rank index on are not used, whatever
+ *          they hold.
+ *  scales  NULL (all 1), or per adapter the finite factor on its product.
+ * The tables are on the device when the call returns (it waits for its own
+ * copy, not for other work), so the batch serves calls on any stream, for
+ * every projection that its requests go through. Not during capture.
+ * *out_batch receives the batch's id.
+ * Errors: EINVAL, ENOMEM, EDEVICE.
+ */
+gemel_status gemel_adapter_batch(gemel_ctx *ctx, const int32_t *adapter_ids,
+                                 const int32_t *n_rows, int32_t n_requests,
+                                 int32_t n_adapters, int32_t max_rank,
+                                 const int32_t *ranks, const float *scales,
+                                 int32_t *out_batch);
+
+/* Give a batch's tables back. Work already enqueued with it still runs
+ * (the memory is used again only after the device has been waited for);
+ * graphs that hold its calls must not be replayed. Errors: EINVAL. */
+gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch);
+
+/*
+ * A shared projection and the bank of adapters beside it.
+ *  weight  [n_out][n_in], rows weight_stride apart.
+ *  bias    float32 [n_out] or NULL.
+ *  a, b    the bank: a [n_adapters][max_rank][n_in] and
+ *          b [n_adapters][n_out][max_rank], contiguous; both may be NULL
+ *          for a batch none of whose rows uses an adapter.
+ */
+typedef struct gemel_projection {
+    int32_t n_in, n_out;
+    const void *weight;
+    int64_t weight_stride;
+    const float *bias;
+    const void *a, *b;
+} gemel_projection;
+
+/*
+ * y = x W^T + bias + scale * (x A^T) B^T, each row with the adapter of its
+ * request: x [rows][n_in] and y [rows][n_out], rows those of the batch.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_adapt(gemel_ctx *ctx, int32_t batch,
+                         const gemel_projection *proj, const void *x,
+                         int64_t x_stride, void *y, int64_t y_stride,
+                         void *hip_stream);
+
+/*
+ * Gradients of gemel_adapt for dy [rows][n_out]. Each output may be NULL
+ * (not computed):
+ *  dx      [rows][n_in], rows dx_stride apart, the context's type:
+ *          dy W + scale * (dy B) A
+ *  dweight float32 [n_out][n_in]: dy^T x over all rows
+ *  dbias   float32 [n_out]: the sum of dy over all rows
+ *  da, db  float32, laid out as the bank: sums over each adapter's rows;
+ *          zeros for adapters without rows and from an adapter's rank on.
+ * Outputs are written, not added to. proj->bias is not read.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_adapt_backward(gemel_ctx *ctx, int32_t batch,
+                                  const gemel_projection *proj, const void *x,
+                                  int64_t x_stride, const void *dy,
+                                  int64_t dy_stride, void *dx,
+                                  int64_t dx_stride, float *dweight,
+                                  float *dbias, float *da, float *db,
+                                  void *hip_stream);
+
+/*
+ * Orthogonalise `count` matrices [rows][cols] (contiguous, one after the
+ * other): out = X_steps with X_0 = g / (|g|_F + 1e-7) and
+ *   X <- a X + b (X X^T) X + c (X X^T)^2 X,  (a, b, c) = (3.4445, -4.7750,
+ * 2.0315), the odd polynomial that drives every singular value from (0, 1]
+ * towards 1 (to about 0.7 .. 1.2 within 5 steps). out has g's type and
+ * shape. steps in 1..16. Products take float16 operands (GEMEL_BF16; the
+ * first step reads the bf16 values unrounded) or float16 pairs (GEMEL_F32).
+ * A matrix of zeros gives zeros; one holding a value that is not finite
+ * gives values that are not finite, in that matrix alone.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_orthogonalize(gemel_ctx *ctx, int32_t count, int32_t rows,
+                                 int32_t cols, const void *g, void *out,
+                                 int32_t steps, void *hip_stream);
+
+/*
+ * One optimiser step of `count` float32 matrices [rows][cols] (contiguous)
+ * with momentum and an orthogonalised update:
+ *   momentum = beta * momentum + g
+ *   u = g + beta * momentum (nesterov), else momentum
+ *   w = (1 - lr * weight_decay) * w
+ *       - lr * sqrt(max(1, rows / cols)) * orthogonalised(u)
+ * w, momentum and g are float32 in every context, and so is the precision
+ * of the update (float16 pairs). copy: NULL, or in GEMEL_BF16 contexts bf16
+ * that receives the new w rounded (the weights gemel_adapt reads).
+ * lr, beta, weight_decay are finite. Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows,
+                             int32_t cols, float *w, float *momentum,
+                             const float *g, void *copy, float lr, float beta,
+                             float weight_decay, int32_t nesterov,
+                             int32_t steps, void *hip_stream);
+
 /* Description of the last error (see general conventions). */
 const char *gemel_last_error(const gemel_ctx *ctx);
 

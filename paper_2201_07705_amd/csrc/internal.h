@@ -229,6 +229,14 @@ struct Options {
     int prefetch = 1;         // conv launches read the next conv's weights into the caches (2: in any round)
 };
 
+// Device state of the operators that serve and retrain merged layers
+// (operators.cpp); freed with the context.
+struct OperatorState {
+    virtual ~OperatorState() {}
+    // waits for the device and frees; false where a fault was found
+    virtual bool release() = 0;
+};
+
 }  // namespace gemel
 
 struct gemel_ctx {
@@ -303,6 +311,7 @@ struct gemel_ctx {
     size_t tune_ctr_bytes = 0;
     void *tune_w = nullptr;   // stand-in weights while the weight cache is on
     size_t tune_w_bytes = 0;
+    std::unique_ptr<gemel::OperatorState> operators;
 };
 
 namespace gemel {

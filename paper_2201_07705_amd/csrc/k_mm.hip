@@ -1,0 +1,570 @@
+// Products of 16-bit matrices with float32 sums: C[m][n] = sum over k of
+// A[m][k] * B[n][k], both operands rows of contiguous elements.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <climits>
+#include <type_traits>
+
+#include "op_args.h"
+
+namespace gemel {
+
+namespace {
+
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+constexpr int BK = 64;   // depth of a step: a 128-byte line of each row
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+
+__device__ __forceinline__ void wait_lgkm0() { __builtin_amdgcn_s_waitcnt(0xF | (0x3 << 14) | (0x7 << 4)); }
+
+__device__ __forceinline__ u16 to_bf16(float f) { return __builtin_bit_cast(u16, (__bf16)f); }
+__device__ __forceinline__ float half_up(u16 h) { return (float)__builtin_bit_cast(_Float16, h); }
+__device__ __forceinline__ u16 to_half(float f) { return __builtin_bit_cast(u16, (_Float16)f); }
+
+__device__ __forceinline__ f32x4 half_up4(ushort4 h) {
+    return f32x4{half_up(h.x), half_up(h.y), half_up(h.z), half_up(h.w)};
+}
+// Four values of a matrix kept as float16 planes: the nearest halves, and
+// the rest of each value in a second half (22 bits together).
+__device__ __forceinline__ void put4(const Planes &p, int64_t at, f32x4 v) {
+    const ushort4 h = make_ushort4(to_half(v[0]), to_half(v[1]), to_half(v[2]), to_half(v[3]));
+    *(ushort4 *)(p.hi + at) = h;
+    if (p.lo) {
+        const f32x4 r = v - half_up4(h);
+        *(ushort4 *)(p.lo + at) = make_ushort4(to_half(r[0]), to_half(r[1]), to_half(r[2]), to_half(r[3]));
+    }
+}
+
+// Elements (m, n .. n + 3) of a matrix in planes; rows are padded to 64, so
+// 4 elements stay in a row, and rows beyond the last one read the last one.
+__device__ __forceinline__ void at4(const Planes &p, int z, int m, int n, int rows, f32x4 &hi, f32x4 &lo) {
+    const int64_t at = (int64_t)z * p.z + (int64_t)min(m, rows - 1) * p.ld + min(n, (int)p.ld - 4);
+    hi = half_up4(*(const ushort4 *)(p.hi + at));
+    lo = p.lo ? half_up4(*(const ushort4 *)(p.lo + at)) : f32x4{0.f, 0.f, 0.f, 0.f};
+}
+__device__ __forceinline__ f32x4 rest4(f32x4 v) {
+    return f32x4{v[0] - half_up(to_half(v[0])), v[1] - half_up(to_half(v[1])), v[2] - half_up(to_half(v[2])),
+                 v[3] - half_up(to_half(v[3]))};
+}
+
+// a X + M X at (m, n .. n + 3) in X's plane units, v being the product of
+// the planes. Where M is a single plane, what its diagonal (most of M once X
+// is nearly orthogonal) and X have lost to rounding is put back.
+__device__ __forceinline__ f32x4 next4(const MmArgs &a, int z, int m, int n, f32x4 v) {
+    const MmOut &o = a.o;
+    f32x4 hi, lo;
+    at4(o.s, z, m, n, a.M, hi, lo);
+    f32x4 x = (float)COEF_A * (hi + lo) + v * 0x1p-14f;
+    if (o.mdiag) {
+        const float *d = o.mdiag + z * o.diag_z;
+        f32x4 md;
+        if (o.diag_rows) {
+            const float r = d[min(m, a.M - 1)];
+            md = f32x4{r, r, r, r};
+        } else {
+            md = *(const f32x4 *)(d + min(n, (int)o.diag_z - 4));
+        }
+        x += 0x1p-14f * (rest4(md) * hi + md * lo);
+    }
+    return x;
+}
+
+// One operand's loads of a step: 16 bytes at base + off[i] + depth into the
+// wave's slots. A buffer resource keeps the base in scalar registers; every
+// offset is in bounds, so its own check is not used.
+template <int LOADS, int NW>
+__device__ __forceinline__ void fetch(const u16 *base, const uint32_t (&off)[LOADS], int depth, unsigned char *stage,
+                                      int wave) {
+    const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<u16 *>(base), 0, -1, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i)
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8 *)(stage + (i * NW + wave) * 1024), 16, (int)off[i], depth, 0, 0);
+}
+
+// The kernel's argument block where the hardware keeps it.
+__device__ __forceinline__ const MmArgs *late_args(const MmArgs &) {
+    auto *p = __builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return (const MmArgs *)p;
+}
+
+// Tile of a workgroup: consecutive tiles on one XCD, and among them groups
+// of 8 tile rows, whose operand rows then stay in its L2.
+template <int T>
+__device__ __forceinline__ void mm_place(const MmArgs &a, int &tm, int &tn) {
+    const int tiles_m = (a.M + T - 1) / T, tiles_n = (a.N + T - 1) / T;
+    const int G = gridDim.x;
+    const int t = (G & 7) == 0 ? (int)(blockIdx.x & 7) * (G >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+    const int group = t / (8 * tiles_n), first = group * 8, rows = min(8, tiles_m - first);
+    const int in = t - group * 8 * tiles_n;
+    tn = in / rows;
+    tm = first + in - tn * rows;
+}
+
+// The epilogue of elements (m, n .. n + 3) of batch entry z. M and N are the
+// product's; planes are written up to their padded row lengths, with zeros
+// beyond M and N, because later products read them in steps of 64.
+template <int EPI>
+__device__ __forceinline__ f32x4 finish(const MmArgs &a, int z, int m, int n, f32x4 v) {
+    const MmOut &o = a.o;
+    if constexpr (EPI == EPI_ROWS || EPI == EPI_SCALED) {
+        if (m >= a.M || n >= a.N) return v;
+        const int64_t at = (int64_t)(o.perm ? o.perm[m] : m) * o.ld + n;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int j = min(n + i, a.N - 1);
+            if constexpr (EPI == EPI_SCALED) v[i] = ldexpf(v[i], -(o.ea[m] + o.eb[j]));
+            if (o.bias) v[i] += o.bias[j];
+        }
+        if constexpr (EPI == EPI_SCALED) {
+            if (a.runs > 0 && m >= a.run_start[0]) {
+                int u = a.first_run[m >> 6];
+                while (a.run_start[u + 1] <= m) ++u;
+                const float *t = o.t + (int64_t)m * o.rp, *bx = o.bx + (int64_t)u * o.rp * o.ldbx + n;
+                for (int r = 0; r < o.rp; ++r) v += t[r] * *(const f32x4 *)(bx + r * o.ldbx);
+            }
+        }
+        if (o.out_f32) {
+            float *p = (float *)o.out + at;
+            if (o.vec && n + 3 < a.N) {
+                *(f32x4 *)p = v;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n + i < a.N) p[i] = v[i];
+            }
+        } else {
+            u16 *p = (u16 *)o.out + at;
+            if (o.vec && n + 3 < a.N) {
+                const ushort4 h = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
+                *(ushort4 *)p = h;
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n + i < a.N) p[i] = to_bf16(v[i]);
+            }
+        }
+    } else if constexpr (EPI == EPI_ORTH || EPI == EPI_STEP) {
+        if (m >= a.M || n >= a.N) return v;
+        const int64_t at = (int64_t)z * o.z + (int64_t)m * o.ld + n;
+        f32x4 x = o.lambda[z * ORTH_LAMBDAS] * 0x1p-13f * next4(a, z, m, n, v);
+        if (o.vec && n + 3 < a.N) {
+            if constexpr (EPI == EPI_STEP) x = (1.f - o.decay) * *(const f32x4 *)((float *)o.out + at) - o.rate * x;
+            if (EPI == EPI_STEP || o.out_f32) *(f32x4 *)((float *)o.out + at) = x;
+            u16 *h = EPI == EPI_STEP ? o.copy : o.out_f32 ? nullptr : (u16 *)o.out;
+            if (h) *(ushort4 *)(h + at) = make_ushort4(to_bf16(x[0]), to_bf16(x[1]), to_bf16(x[2]), to_bf16(x[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (n + i >= a.N) continue;
+                if constexpr (EPI == EPI_STEP) x[i] = (1.f - o.decay) * ((float *)o.out)[at + i] - o.rate * x[i];
+                if (EPI == EPI_STEP || o.out_f32) ((float *)o.out)[at + i] = x[i];
+                u16 *h = EPI == EPI_STEP ? o.copy : o.out_f32 ? nullptr : (u16 *)o.out;
+                if (h) h[at + i] = to_bf16(x[i]);
+            }
+        }
+    } else {
+        const Planes &p = o.p;
+        f32x4 x;
+        if constexpr (EPI == EPI_GRAM) {
+            x = v * 0x1p-15f;
+        } else if constexpr (EPI == EPI_POLY) {
+            const float l = o.lambda[z * ORTH_LAMBDAS], l2 = l * l;
+            f32x4 s, lo;
+            at4(o.s, z, m, n, a.M, s, lo);
+            if (o.sdiag) {
+                // S is its plane but for the diagonal
+                const float *d = o.sdiag + z * o.diag_z;
+                const f32x4 dn = *(const f32x4 *)(d + min(n, (int)o.diag_z - 4));
+                const float dm = d[min(m, a.M - 1)];
+                v += (dm - half_up(to_half(dm)) + rest4(dn)) * s;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) s[i] = m == n + i ? dm : s[i];
+            } else {
+                s += lo;
+            }
+            x = 0x1p14f * ((float)COEF_B * 0x1p-11f * l2 * s + (float)COEF_C * 0x1p-22f * l2 * l2 * v);
+        } else {
+            const float *l = o.lambda + z * ORTH_LAMBDAS;
+            x = l[0] / l[1] * next4(a, z, m, n, v);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = m < a.M && n + i < a.N ? x[i] : 0.f;
+        if constexpr (EPI == EPI_GRAM || EPI == EPI_POLY) {
+            float *const d = EPI == EPI_GRAM ? o.sdiag : o.mdiag;
+            if (d && m >= n && m < n + 4 && m < a.M) d[z * o.diag_z + m] = m == n ? x[0] : m == n + 1 ? x[1] : m == n + 2 ? x[2] : x[3];
+        }
+        if (m < a.M && n < p.ld) put4(p, (int64_t)z * p.z + (int64_t)m * p.ld + n, x);
+        return x;
+    }
+    return v;
+}
+
+// One T x T output tile per workgroup: 8 waves of 128 x 64 (T = 256) or 4 of
+// T/2 x T/2. A step of depth 64 is fetched by global_load_lds into one of two
+// LDS buffers (separate arrays, so that the compiler sees which buffer a load
+// in flight writes), the step after next being requested as soon as the
+// current buffer's last fragments are in registers. Slot p of a buffer holds
+// row p / 8, 16-byte chunk (p % 8) ^ (row / 2 % 8): the fragment reads of 16
+// rows then fall on distinct banks. A step is four phases of (depth half, row
+// half) fragments; each phase reads the next one's fragments, so that the
+// matrix cores wait for LDS only across the one barrier of a step, and there
+// the fragments read before it cover the others.
+//
+// At 8192^3 (bf16) T = 256 runs at 1354 TFLOP/s and T = 128 (two workgroups
+// on a CU) at 1144; at 4096^3 1312 and 1166.
+template <int T>
+constexpr int mm_threads() { return T == 256 ? 512 : 256; }
+
+template <int T, bool F16, int EPI>
+__global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(const MmArgs a) {
+    constexpr int NT = mm_threads<T>(), NW = NT / 64, WN = T == 256 ? 4 : 2;
+    constexpr int TM = T / 2, TN = T / WN, FM = TM / 16, FN = TN / 16, HM = FM / 2;
+    constexpr int LOADS = T * 8 / NT, ROW = BK * 2;
+    __shared__ __attribute__((aligned(1024))) unsigned char st0[2 * T * ROW], st1[2 * T * ROW];
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / WN, wn = wave - wm * WN, g = lane >> 4, l16 = lane & 15;
+    int tm, tn;
+    mm_place<T>(a, tm, tn);
+    if (a.sym && tn < tm) return;
+    const int split = blockIdx.y, z = blockIdx.z;
+    const int m0 = tm * T, n0 = tn * T;
+    const int nk = (a.K + BK - 1) / BK;
+    const int s0 = split * a.steps, mains = min(nk * a.nseg - s0, a.steps);
+    // extension steps: the runs that overlap the tile's rows, in the last split
+    int u = 0, ek = 0, exts = 0;
+    if (EPI == EPI_ROWS && a.ext && split == a.splits - 1) {
+        u = a.first_run[m0 >> 6];
+        int e = u;
+        while (e < a.runs && a.run_start[e] < min(m0 + T, a.M)) ++e;
+        exts = (e - u) * (a.ext / BK);
+    }
+    const int total = mains + exts;
+
+    // load i of a thread fills slot i * NT + tid; byte offsets from the
+    // tile's first row (or, with a row table, from the matrix)
+    uint32_t oa[LOADS], ob[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int row = (i * NT + tid) >> 3, ch = ((tid & 7) ^ ((row >> 1) & 7)) * 8;
+        const int m = min(m0 + row, a.M - 1), n = min(n0 + row, a.N - 1);
+        oa[i] = (uint32_t)((a.perm ? a.perm[m] : m - m0) * (uint32_t)a.lda + ch) * 2u;
+        ob[i] = (uint32_t)((n - n0) * (uint32_t)a.ldb + ch) * 2u;
+    }
+    int seg = s0 / nk, kk = (s0 - seg * nk) * BK, iss = 0;
+    const int64_t za = (int64_t)z * a.za + (a.perm ? 0 : (int64_t)m0 * a.lda), zb = (int64_t)z * a.zb + (int64_t)n0 * a.ldb;
+    // Requests the next step; past the last one, the last one again (into a
+    // buffer whose reads are over), so that every step waits alike.
+    auto issue = [&](unsigned char *stage) __attribute__((always_inline)) {
+        const bool ext = EPI == EPI_ROWS && exts > 0 && iss >= mains;
+        if (EPI == EPI_ROWS && (ext || kk + BK > a.K)) {
+            // rows of other runs, and chunks beyond a depth that is no
+            // multiple of 64, are zeros
+            const char *pa, *pb;
+            int lo = 0, hi = INT_MAX;
+            if (ext) {
+                pa = (const char *)(a.t + (int64_t)m0 * a.ext + ek);
+                pb = (const char *)(a.bx + ((int64_t)u * a.N + n0) * a.ext + ek);
+                lo = a.run_start[u];
+                hi = a.run_start[u + 1];
+            } else {
+                pa = (const char *)(a.a[0] + za + kk);
+                pb = (const char *)(a.b[0] + zb + kk);
+            }
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int row = (i * NT + tid) >> 3, ch = ((tid & 7) ^ ((row >> 1) & 7)) * 8;
+                const bool in = ext ? m0 + row >= lo && m0 + row < hi : kk + ch < a.K;
+                const uint32_t xa = ext ? (uint32_t)(row * a.ext + ch) * 2u : oa[i];
+                const uint32_t xb = ext ? (uint32_t)((min(n0 + row, a.N - 1) - n0) * a.ext + ch) * 2u : ob[i];
+                __builtin_amdgcn_global_load_lds(in ? (const void *)(pa + xa) : (const void *)a.zero,
+                                                 (lds_u8 *)(stage + (i * NW + wave) * 1024), 16, 0, 0);
+                __builtin_amdgcn_global_load_lds(ext || in ? (const void *)(pb + xb) : (const void *)a.zero,
+                                                 (lds_u8 *)(stage + T * ROW + (i * NW + wave) * 1024), 16, 0, 0);
+                __builtin_amdgcn_sched_barrier(0);
+            }
+            if (ext && iss + 1 < total) {
+                ek += BK;
+                if (ek >= a.ext) {
+                    ek = 0;
+                    ++u;
+                }
+            }
+        } else {
+            const u16 *pa = a.a[0], *pb = a.b[0];
+            if (EPI != EPI_ROWS && seg) {
+                pa = seg == 1 ? a.a[1] : a.a[2];
+                pb = seg == 1 ? a.b[1] : a.b[2];
+            }
+            fetch<LOADS, NW>(pa + za, oa, kk * 2, stage, wave);
+            fetch<LOADS, NW>(pb + zb, ob, kk * 2, stage + T * ROW, wave);
+        }
+        iss = min(iss + 1, total);
+        if (iss < mains) {
+            kk += BK;
+            if (kk >= nk * BK) {
+                kk = 0;
+                ++seg;
+            }
+        }
+    };
+    f32x4 acc[FM][FN];
+#pragma unroll
+    for (int i = 0; i < FM; ++i)
+#pragma unroll
+        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    using H8 = std::conditional_t<F16, f16x8, bf16x8>;
+    H8 fa0[HM], fa1[HM], fb0[FN], fb1[FN];
+    // rows 16 apart share their swizzle: one address per depth half
+    const int ra = (wm * TM + l16) * ROW, rb = T * ROW + (wn * TN + l16) * ROW;
+    const int h0 = (g ^ ((l16 >> 1) & 7)) * 16, h1 = ((4 + g) ^ ((l16 >> 1) & 7)) * 16;
+    auto read_a = [&](H8(&f)[HM], const unsigned char *s, int h, int half) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < HM; ++i) f[i] = *(const H8 *)(s + ra + h + (half * HM + i) * 16 * ROW);
+    };
+    auto read_b = [&](H8(&f)[FN], const unsigned char *s, int h) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) f[j] = *(const H8 *)(s + rb + h + j * 16 * ROW);
+    };
+    auto mul = [&](H8(&f)[HM], H8(&b)[FN], int half) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < HM; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                f32x4 &c = acc[half * HM + i][j];
+                if constexpr (F16)
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], f[i], c, 0, 0, 0);
+                else
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], f[i], c, 0, 0, 0);
+            }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // the loads of the step after `cur`'s have landed in every wave, and
+    // every wave has read the last of `cur`
+    auto turn = [&]() __attribute__((always_inline)) {
+        wait_lgkm0();
+        wait_vm<0>();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto step = [&](unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
+        read_a(fa1, cur, h0, 1);
+        mul(fa0, fb0, 0);
+        read_a(fa0, cur, h1, 0);
+        read_b(fb1, cur, h1);
+        mul(fa1, fb0, 1);
+        read_a(fa1, cur, h1, 1);
+        mul(fa0, fb1, 0);
+        turn();
+        issue(cur);
+        read_a(fa0, next, h0, 0);
+        read_b(fb0, next, h0);
+        mul(fa1, fb1, 1);
+    };
+    issue(st0);
+    issue(st1);
+    wait_vm<2 * LOADS>();
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    read_a(fa0, st0, h0, 0);
+    read_b(fb0, st0, h0);
+    // no way out of the loop but its end: with one the compiler spills the sums
+    for (int s = 0; s + 2 <= total; s += 2) {
+        step(st0, st1);
+        step(st1, st0);
+    }
+    if (total & 1) {
+        read_a(fa1, st0, h0, 1);
+        mul(fa0, fb0, 0);
+        read_a(fa0, st0, h1, 0);
+        read_b(fb1, st0, h1);
+        mul(fa1, fb0, 1);
+        read_a(fa1, st0, h1, 1);
+        mul(fa0, fb1, 0);
+        mul(fa1, fb1, 1);
+    }
+    wait_vm<0>();
+    __builtin_amdgcn_sched_barrier(0);
+    __syncthreads();
+    // the argument block is read again from here on: its epilogue part would
+    // otherwise sit in scalar registers through the loop
+    const MmArgs &e = *late_args(a);
+    // Each wave's sums pass through its own part of LDS, 64 rows at a time,
+    // so that one rolled loop finishes whole rows of contiguous columns (and
+    // another, for transposed outputs, whole columns). 16-byte chunk c of row
+    // m sits at chunk c ^ swz(m): writes in the MFMA's layout, reads of rows
+    // and reads of columns all spread over the banks.
+    constexpr int RP = TM < 64 ? TM : 64, C = TN / 4, SZ = RP * TN * 4;
+    static_assert(NW * SZ <= 4 * T * ROW && 2 * T * ROW % SZ == 0, "staging");
+    unsigned char *const mine = wave * SZ < 2 * T * ROW ? st0 + wave * SZ : st1 + (wave * SZ - 2 * T * ROW);
+    auto swz = [](int m) __attribute__((always_inline)) { return ((m & 3) * 4 + (m >> 2)) & (C - 1); };
+#pragma unroll
+    for (int pass = 0; pass < TM / RP; ++pass) {
+        const int mb = m0 + wm * TM + pass * RP, nb = n0 + wn * TN;
+        if (pass) wait_lgkm0();
+#pragma unroll
+        for (int i = 0; i < RP / 16; ++i)
+#pragma unroll
+            for (int j = 0; j < FN; ++j) {
+                const int m = i * 16 + l16;
+                *(f32x4 *)(mine + m * TN * 4 + ((j * 4 + g) ^ swz(m)) * 16) = acc[pass * (RP / 16) + i][j];
+            }
+        wait_lgkm0();
+        asm volatile("" ::: "memory");
+        const bool turned = (EPI == EPI_NEXT || ((EPI == EPI_GRAM || EPI == EPI_POLY) && e.sym && tn > tm)) && e.splits == 1;
+        for (int it = lane; it < RP * C; it += 64) {
+            const int m = it / C, c = it & (C - 1);
+            f32x4 *const slot = (f32x4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16);
+            f32x4 v = *slot;
+            if (e.splits > 1) {
+                if (mb + m < e.M && nb + c * 4 < e.N)
+                    *(f32x4 *)(e.partial + (((int64_t)split * e.batch + z) * e.M + mb + m) * e.ldp + nb + c * 4) = v;
+            } else {
+                v = finish<EPI>(e, z, mb + m, nb + c * 4, v);
+                if (turned) *slot = v;
+            }
+        }
+        if (!turned) continue;
+        wait_lgkm0();
+        asm volatile("" ::: "memory");
+        const Planes &q = EPI == EPI_NEXT ? e.o.q : e.o.p;
+        for (int it = lane; it < TN * RP / 4; it += 64) {
+            const int n = it / (RP / 4), m = (it % (RP / 4)) * 4;
+            f32x4 v;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                v[i] = *(const float *)(mine + (m + i) * TN * 4 + ((n >> 2) ^ swz(m + i)) * 16 + (n & 3) * 4);
+            if (nb + n < e.N && mb + m < q.ld) put4(q, (int64_t)z * q.z + (int64_t)(nb + n) * q.ld + mb + m, v);
+        }
+    }
+}
+
+// Sums the splits of each element in order and applies the epilogue.
+// One thread per 4 columns of the padded width, rows up to the padded
+// height where planes need their zeros.
+template <int EPI>
+__global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a, int rows, int quads, int T) {
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int m = (int)(i / quads), n = (int)(i - (int64_t)m * quads) * 4, z = blockIdx.z;
+    if (m >= rows) return;
+    const int tm = m / T, tn = n / T;
+    if (a.sym && tn < tm) return;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (m < a.M && n < a.N)
+        for (int s = 0; s < a.splits; ++s)
+            v += *(const f32x4 *)(a.partial + (((int64_t)s * a.batch + z) * a.M + m) * a.ldp + n);
+    v = finish<EPI>(a, z, m, n, v);
+    if constexpr (EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT) {
+        const Planes &q = EPI == EPI_NEXT ? a.o.q : a.o.p;
+        if ((EPI == EPI_NEXT || (a.sym && tn > tm)) && m < q.ld) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (n + i >= a.N) continue;
+                const int64_t at = (int64_t)z * q.z + (int64_t)(n + i) * q.ld + m;
+                const u16 h = to_half(v[i]);
+                q.hi[at] = h;
+                if (q.lo) q.lo[at] = to_half(v[i] - half_up(h));
+            }
+        }
+    }
+}
+
+template <int T, bool F16, int EPI>
+hipError_t go(const MmArgs &a, hipStream_t s) {
+    const int tm = (a.M + T - 1) / T, tn = (a.N + T - 1) / T;
+    const dim3 grid((unsigned)(tm * tn), (unsigned)a.splits, (unsigned)a.batch);
+    void *p[] = {const_cast<MmArgs *>(&a)};
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, F16, EPI>), grid,
+                                   dim3(mm_threads<T>()), p, 0, s);
+    if (e != hipSuccess || a.splits == 1) return e;
+    int rows = tm * T, quads = tn * T / 4, tt = T;
+    const int64_t blocks = ((int64_t)rows * quads + 255) / 256;
+    void *q[] = {const_cast<MmArgs *>(&a), &rows, &quads, &tt};
+    return hipLaunchKernel(reinterpret_cast<const void *>(&mm_reduce_kernel<EPI>),
+                           dim3((unsigned)blocks, 1, (unsigned)a.batch), dim3(256), q, 0, s);
+}
+
+template <int EPI, bool F16>
+hipError_t pick(const MmArgs &a, hipStream_t s) {
+    return a.tile == 256 ? go<256, F16, EPI>(a, s) : a.tile == 128 ? go<128, F16, EPI>(a, s) : go<64, F16, EPI>(a, s);
+}
+
+}  // namespace
+
+// Tile and depth splits: the estimated time of the launch is the turns that
+// the compute units take, each a step's time for every step and a fixed part
+// for the pipeline's start and the epilogue, plus writing and reading the
+// partial sums and the second launch where the depth is split.
+void mm_plan(MmArgs &a) {
+    struct Form {
+        int tile, slots;      // workgroups that run at once
+        double step, fixed;   // microseconds
+    };
+    static const Form forms[] = {{256, 256, 1.62, 6.0}, {128, 512, 0.92, 4.0}, {64, 1024, 0.75, 2.5}};
+    const int steps = (a.K + BK - 1) / BK * a.nseg;
+    double best = 1e30;
+    for (const Form &f : forms) {
+        const int64_t tm = (a.M + f.tile - 1) / f.tile, tn = (a.N + f.tile - 1) / f.tile;
+        const int64_t tiles = (a.sym ? tm * (tm + 1) / 2 : tm * tn) * a.batch;
+        for (int want = 1; want <= 32 && want <= std::max(1, steps / 4); ++want) {
+            const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
+            if (splits != want) continue;
+            const double turns = (double)((tiles * splits + f.slots - 1) / f.slots);
+            double us = turns * (per * f.step + f.fixed);
+            const double bytes = (double)splits * a.batch * a.M * op_round_up(a.N, 4) * (a.sym ? 2 : 4);
+            if (splits > 1) us += 4.0 + 2 * bytes / 4e6;
+            if (splits > 1 && bytes > 1e9) continue;
+            if (us < best) {
+                best = us;
+                a.tile = f.tile;
+                a.steps = per;
+                a.splits = splits;
+            }
+        }
+    }
+    a.ldp = op_round_up(a.N, 4);
+}
+
+hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
+    const int nk = (a.K + BK - 1) / BK;
+    if (a.M <= 0 || a.N <= 0 || a.K <= 0 || a.K % 8 || a.batch <= 0 || a.batch > 65535 || a.nseg < 1 || a.nseg > 3 ||
+        a.lda % 8 || a.ldb % 8 || a.lda > MM_MAX_LD || a.ldb > MM_MAX_LD ||
+        (a.perm && a.perm_rows * a.lda > (1ll << 30)) || (a.tile != 64 && a.tile != 128 && a.tile != 256) || a.za % 8 || a.zb % 8 || a.lda < a.K || a.ldb < a.K || !a.zero || a.splits < 1 ||
+        a.steps < 1 || a.ext % BK || (int64_t)a.splits * a.steps < (int64_t)nk * a.nseg ||
+        (int64_t)(a.splits - 1) * a.steps >= (int64_t)nk * a.nseg)
+        return hipErrorInvalidValue;
+    for (int i = 0; i < a.nseg; ++i)
+        if (!a.a[i] || !a.b[i] || (uintptr_t)a.a[i] % 16 || (uintptr_t)a.b[i] % 16) return hipErrorInvalidValue;
+    if (a.splits > 1 && (!a.partial || a.ldp % 4 || a.ldp < a.N)) return hipErrorInvalidValue;
+    if (a.ext && (!a.t || !a.bx || a.runs < 1 || !a.run_start || !a.first_run || a.batch != 1 || a.nseg != 1 || a.f16))
+        return hipErrorInvalidValue;
+    if (a.sym && a.M != a.N) return hipErrorInvalidValue;
+    if (a.epi != EPI_ROWS && (a.K % BK || a.ext)) return hipErrorInvalidValue;
+    if ((int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64) > INT32_MAX / 256) return hipErrorInvalidValue;
+    switch (a.epi) {
+        case EPI_ROWS: return a.f16 ? hipErrorInvalidValue : pick<EPI_ROWS, false>(a, s);
+        case EPI_SCALED: return pick<EPI_SCALED, true>(a, s);
+        case EPI_GRAM: return pick<EPI_GRAM, true>(a, s);
+        case EPI_POLY: return pick<EPI_POLY, true>(a, s);
+        case EPI_NEXT: return pick<EPI_NEXT, true>(a, s);
+        case EPI_ORTH: return pick<EPI_ORTH, true>(a, s);
+        case EPI_STEP: return pick<EPI_STEP, true>(a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace gemel

@@ -1,0 +1,213 @@
+// Argument blocks and launchers of the operators that serve and retrain
+// merged layers: adapted projections, their gradients, and orthogonalised
+// matrix updates. Each launcher checks on the host that its block matches
+// what the kernel and grid assume and returns hipErrorInvalidValue instead
+// of launching otherwise.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace gemel {
+
+typedef unsigned short u16;
+
+constexpr int64_t op_round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
+
+// What a product does with its sums v (float32) of element (m, n).
+enum MmEpi {
+    EPI_ROWS = 0,   // out[perm[m]][n] = v + bias[n], in the context's type
+    EPI_SCALED = 1, // out[perm[m]][n] = v * 2^-(ea[m] + eb[n]) + low-rank part + bias[n], float32
+    EPI_GRAM = 2,   // S = v * 2^-26, stored * 2^11 as planes, with its mirror image
+    EPI_POLY = 3,   // M = b l^2 S + c l^4 v 2^-22, stored * 2^14 as planes, with its mirror image
+    EPI_NEXT = 4,   // X = f (a X + v * 2^-27), stored * 2^13 as planes, in both layouts
+    EPI_ORTH = 5,   // out[m][n] = l (a X + v * 2^-27), in the context's type
+    EPI_STEP = 6    // w = (1 - decay) w - rate * l (a X + v * 2^-27), and its copy
+};
+
+// 16-bit planes of a matrix: hi, and lo (the rest; null = not kept). Rows of
+// ld elements, z elements between the matrices of a batch.
+struct Planes {
+    u16 *hi, *lo;
+    int64_t ld, z;
+};
+
+struct MmOut {
+    void *out;            // ROWS, SCALED, ORTH, STEP (w)
+    int64_t ld, z;
+    int out_f32;          // ROWS, ORTH: float32 instead of bf16
+    int vec;              // 4 consecutive outputs may be stored at once
+    const float *bias;    // [N] or null
+    const int *perm;      // output row of product row m, or null
+    const int *ea, *eb;   // SCALED
+    // SCALED: low-rank part, sum over r of t[m][r] * bx[run][r][n], rows of
+    // ldbx (a multiple of 4)
+    const float *t, *bx;
+    int rp;
+    int64_t ldbx;
+    Planes p, q;          // GRAM, POLY: p; NEXT: p = [m][n], q = [n][m]
+    Planes s;             // POLY: S; NEXT, ORTH, STEP: X as the product's rows lie
+    // diagonals of S and M, kept unrounded where these are single planes
+    // ([batch][diag_z]): GRAM and POLY write theirs, POLY reads S's, NEXT,
+    // ORTH and STEP read M's, by output row or column
+    float *sdiag, *mdiag;
+    int64_t diag_z;
+    int diag_rows;
+    const float *lambda;  // l of each matrix, ORTH_LAMBDAS apart; f = lambda[0] / lambda[1]
+    u16 *copy;            // STEP: bf16 copy of w or null
+    float rate, decay;    // STEP
+};
+
+// C[m][n] = sum over segments and k of a[seg][row m][k] * b[seg][n][k].
+// Operands are rows of contiguous 16-bit elements; 16-byte aligned, ld a
+// multiple of 8; where K is not a multiple of 64 chunks of 8 beyond K
+// are read as zeros (K a multiple of 8).
+struct MmArgs {
+    const u16 *a[3], *b[3];
+    int64_t lda, ldb, za, zb;
+    int nseg, M, N, K, batch;
+    int f16;              // 1: float16 operands, 0: bf16
+    int epi;
+    int sym;              // only tiles on and above the diagonal
+    int tile;             // 64, 128 or 256 (mm_plan)
+    int splits, steps;    // depth splits, and steps of 64 in each
+    float *partial;       // [splits][batch][M][ldp] with splits > 1
+    int64_t ldp;
+    const u16 *zero;      // 16 zero bytes or more
+    const int *perm;      // row of a[seg] behind product row m, or null
+    int64_t perm_rows;    // rows that it points into
+    // low-rank extension of the depth (bf16): t [M][ext] rows against
+    // bx [run][N][ext], where the row's run is the one holding m
+    const u16 *t, *bx;
+    int ext, runs;        // ext a multiple of 64, 0 = none
+    const int *run_start; // [runs + 1]; rows before run_start[0] have none
+    const int *first_run; // [ceil(M / 64) + 1] first run ending after row 64 i
+    MmOut o;
+};
+// Longest rows: a tile's byte offsets fit 32 bits (and with a row table the
+// whole matrix's: perm_rows * lda up to 2^30 elements).
+constexpr int64_t MM_MAX_LD = 1 << 22;
+void mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape
+hipError_t launch_mm(const MmArgs &a, hipStream_t s);
+
+// Requests grouped by adapter, as tables in device memory.
+struct BatchTables {
+    const int *perm;       // [rows] row behind position p
+    const int *run_start;  // [runs + 1] positions
+    const int *run_id;     // [runs] adapter
+    const int *run_rank;   // [runs]
+    const float *run_scale;// [runs]
+    const int *first_run;  // [ceil(rows / 64) + 1]
+    const int *items;      // [n_items][3]: run, first position, positions (<= 16)
+    const int *chunks;     // [n_chunks][3]: run, first position, positions
+    const int *chunk_first;// [runs + 1] chunks of a run
+    const int *run_of;     // [adapters] run or -1
+    int rows, runs, adapters, rank, n_items, n_chunks;
+};
+
+// t[p][r] = scale * sum over k of x[perm[p]][k] * a[run][r][k]
+struct ShrinkArgs {
+    const void *x;
+    const void *a;         // rows of K (by_run: packed, [runs][rp][lda]; else [adapters][rank][K])
+    int64_t ldx, lda;
+    int by_run, f32, K, rp;
+    int vx, va;            // 16-byte loads of whole chunks of 8 (bf16) or 4 (f32) are safe
+    u16 *planes;           // [rows][2 rp] hi | lo, or null
+    float *t;              // [rows][rp]
+    BatchTables b;
+};
+hipError_t launch_shrink(const ShrinkArgs &a, hipStream_t s);
+
+// Adapter halves per run, in [adapters][C][R] (or [R][C]): out[run][C][2 rp]
+// with each row's ranks twice (bf16), or by_rank: out[run][rp][ldc]. Rank
+// indices from the run's rank on are zeros, and so are columns beyond C.
+struct PackRankArgs {
+    const void *in;
+    void *out;
+    int in_rc, by_rank, f32, C, R, rp;
+    int64_t ldc;
+    BatchTables b;
+};
+hipError_t launch_pack_rank(const PackRankArgs &a, hipStream_t s);
+
+// part[chunk][r][c] = sum over the chunk's positions of p[pos][r] * q[perm[pos]][c]
+// and out[adapter] = sum over its chunks ([R][C], or [C][R] transposed)
+struct OuterArgs {
+    const float *p;        // [rows][rp]
+    const void *q;
+    int64_t ldq;
+    int f32, C, rp, transposed;
+    float *part;           // [n_chunks][rp][C]
+    float *out;
+    BatchTables b;
+};
+hipError_t launch_outer(const OuterArgs &a, hipStream_t s);
+
+// Column sums of [rows][cols].
+struct ColsumArgs {
+    const void *in;
+    int64_t ld;
+    int f32, rows, cols, parts;
+    float *part;           // [parts][cols]
+    float *out;
+};
+hipError_t launch_colsum(const ColsumArgs &a, hipStream_t s);
+
+// Copies into zero-padded rows: out[r][c] for c < ldo (transposed:
+// out[c][r] for r < ldo).
+struct PadArgs {
+    const u16 *in;
+    u16 *out;
+    int64_t ldi, ldo;
+    int rows, cols, transposed;
+    const int *perm;       // not transposed: input row of output row, or null
+};
+hipError_t launch_pad(const PadArgs &a, hipStream_t s);
+
+// float32 rows as two float16 planes of in * 2^e, one exponent per row of
+// the output (the row's largest value lands in [2^14, 2^15)).
+struct SplitArgs {
+    const float *in;
+    u16 *hi, *lo;
+    int *e;                // [output rows]
+    unsigned *colmax;      // transposed: [cols] scratch
+    int64_t ldi, ldo;
+    int rows, cols, transposed;
+    const int *perm;       // not transposed: input row of output row, or null
+};
+hipError_t launch_split(const SplitArgs &a, hipStream_t s);
+
+// ---- orthogonalised updates ----
+constexpr double COEF_A = 3.4445, COEF_B = -4.7750, COEF_C = 2.0315;
+constexpr int ORTH_MAX_STEPS = 16, ORTH_LAMBDAS = ORTH_MAX_STEPS + 1;
+constexpr int THIN_MAX = 64;
+
+// One batch of `count` row-major [rows][cols] matrices.
+struct OrthArgs {
+    const void *g;         // update, or the gradient of a step
+    float *m;              // step: momentum (null otherwise)
+    int f32;               // type of g and of `out`
+    int step, nesterov;
+    float beta;
+    int rows, cols, count, steps;
+    int parts;             // partial sums per matrix
+    // planes of X_k / lambda[k], X_k the k-th iterate
+    double *sums;          // [count][parts] squared sums
+    float *lambda;         // [count][ORTH_LAMBDAS]
+    Planes x;              // [n][ld >= m]: the wide orientation
+    Planes xt;             // [m][ld >= n]
+    // thin matrices: n = min(rows, cols) <= THIN_MAX
+    int vec;               // 4 consecutive elements may be moved at once
+    double *gram;          // [count][parts][np * np], np = n rounded up to 16
+    float *q;              // [count][np * np]: out = q * (2^e u)
+    int *e;                // [count]
+    void *out;             // result, or the weights of a step
+    u16 *copy;
+    float rate, decay;
+};
+hipError_t launch_norm(const OrthArgs &a, hipStream_t s);   // momentum and squared sums
+hipError_t launch_seed(const OrthArgs &a, hipStream_t s);   // planes of the scaled update, lambda
+hipError_t launch_thin_gram(const OrthArgs &a, hipStream_t s);   // momentum and partial Gram matrices
+hipError_t launch_thin_poly(const OrthArgs &a, hipStream_t s);   // q, e
+hipError_t launch_thin_apply(const OrthArgs &a, hipStream_t s);  // out
+
+}  // namespace gemel

@@ -1,0 +1,1059 @@
+// The operators that serve and retrain merged layers: argument checks,
+// request tables, workspaces, and the order of their kernels.
+#include <algorithm>
+#include <climits>
+#include <cmath>
+#include <cstring>
+#include <map>
+#include <memory>
+#include <new>
+#include <string>
+#include <utility>
+#include <vector>
+
+#include "internal.h"
+#include "op_args.h"
+
+using namespace gemel;
+
+namespace {
+
+constexpr int64_t MAX_ROWS = 1 << 22, MAX_DIM = 1 << 20, MAX_COUNT = 65535;
+constexpr int MAX_RANK = 256, MAX_STEPS = ORTH_MAX_STEPS;
+
+struct DeviceScope {
+    int prev = -1;
+    explicit DeviceScope(int d) {
+        if (hipGetDevice(&prev) != hipSuccess) prev = -1;
+        if (prev != d)
+            (void)hipSetDevice(d);
+        else
+            prev = -1;
+    }
+    ~DeviceScope() {
+        if (prev >= 0) (void)hipSetDevice(prev);
+    }
+};
+
+gemel_status hip_fail(gemel_ctx *ctx, hipError_t e, const char *what) {
+    return fail(ctx, e == hipErrorOutOfMemory ? GEMEL_ENOMEM : GEMEL_EDEVICE,
+                std::string(what) + ": " + hipGetErrorString(e));
+}
+#define OPCHK(call, what)                                   \
+    do {                                                    \
+        const hipError_t e_ = (call);                       \
+        if (e_ != hipSuccess) return hip_fail(ctx, e_, what); \
+    } while (0)
+
+// Requests grouped by adapter. Positions are rows sorted by adapter (rows
+// without one first), in row order within one, so that a tile of positions
+// meets few adapters whatever the order of the requests.
+struct Batch {
+    BatchTables t{};
+    void *dev = nullptr;
+    size_t bytes = 0;
+};
+
+// A stretch of device memory that the kernels of one stream share.
+struct Workspace {
+    char *p = nullptr;
+    size_t bytes = 0;
+};
+
+struct State : OperatorState {
+    int device;
+    void *zero = nullptr;        // 256 zero bytes
+    hipStream_t side = nullptr;  // uploads of tables
+    void *pinned = nullptr;
+    size_t pinned_bytes = 0;
+    std::map<hipStream_t, Workspace> ws;
+    std::vector<std::unique_ptr<Batch>> batches;
+    // tables given back: `retired` ones may still be read by enqueued work
+    std::vector<std::pair<void *, size_t>> spare, retired;
+
+    explicit State(int d) : device(d) {}
+    bool release() override {
+        DeviceScope scope(device);
+        const bool ok = hipDeviceSynchronize() == hipSuccess;
+        for (auto &w : ws)
+            if (w.second.p) (void)hipFree(w.second.p);
+        for (auto &b : batches)
+            if (b && b->dev) (void)hipFree(b->dev);
+        for (auto *v : {&spare, &retired})
+            for (auto &b : *v) (void)hipFree(b.first);
+        if (zero) (void)hipFree(zero);
+        if (pinned) (void)hipHostFree(pinned);
+        if (side) (void)hipStreamDestroy(side);
+        ws.clear();
+        batches.clear();
+        spare.clear();
+        retired.clear();
+        zero = pinned = nullptr;
+        side = nullptr;
+        return ok;
+    }
+};
+
+gemel_status ready(gemel_ctx *ctx, State **out) {
+    if (ctx->operators) {
+        *out = static_cast<State *>(ctx->operators.get());
+        return GEMEL_OK;
+    }
+    int n = 0;
+    OPCHK(hipGetDeviceCount(&n), "hipGetDeviceCount");
+    if (ctx->device >= n) return fail(ctx, GEMEL_EINVAL, "device index beyond the visible devices");
+    hipDeviceProp_t prop;
+    OPCHK(hipGetDeviceProperties(&prop, ctx->device), "hipGetDeviceProperties");
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0)
+        return fail(ctx, GEMEL_EDEVICE, std::string("libgemel is built for gfx950; device is ") + prop.gcnArchName);
+    auto st = std::make_unique<State>(ctx->device);
+    hipError_t e = hipMalloc(&st->zero, 256);
+    if (e == hipSuccess) e = hipStreamCreateWithFlags(&st->side, hipStreamNonBlocking);
+    if (e == hipSuccess) e = launch_fill_u32((uint32_t *)st->zero, 64, 0, Sink{st->side});
+    if (e == hipSuccess) e = hipStreamSynchronize(st->side);
+    if (e != hipSuccess) {
+        st->release();
+        return hip_fail(ctx, e, "operator state");
+    }
+    *out = st.get();
+    ctx->operators = std::move(st);
+    return GEMEL_OK;
+}
+
+// Offsets of a call's buffers in its stream's workspace.
+struct Layout {
+    size_t bytes = 0;
+    size_t take(int64_t n, size_t elem) {
+        const size_t at = bytes;
+        bytes += (size_t)op_round_up(n * (int64_t)elem, 256);
+        return at;
+    }
+};
+
+gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, size_t bytes, char **out) {
+    Workspace &w = st.ws[stream];
+    if (w.bytes < bytes) {
+        if (stream) {
+            hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+            OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
+            if (cs != hipStreamCaptureStatusNone)
+                return fail(ctx, GEMEL_ESTATE, "the stream's workspace is too small to be captured: make the call once before");
+        }
+        bytes = (size_t)op_round_up((int64_t)bytes, 2 << 20);
+        if (w.p) {
+            OPCHK(hipDeviceSynchronize(), "hipDeviceSynchronize");
+            (void)hipFree(w.p);
+            w = Workspace();
+        }
+        void *p = nullptr;
+        OPCHK(hipMalloc(&p, bytes), "workspace");
+        w.p = (char *)p;
+        w.bytes = bytes;
+    }
+    *out = w.p;
+    return GEMEL_OK;
+}
+
+// Ranges of device memory that a call reads or writes.
+struct Range {
+    const char *what;
+    uintptr_t lo, hi;
+    bool out;
+};
+Range range(const char *what, const void *p, int64_t bytes, bool out) {
+    return {what, (uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)bytes : 0), out};
+}
+int64_t span(int64_t rows, int64_t cols, int64_t stride, int64_t elem) {
+    return rows > 0 ? ((rows - 1) * stride + cols) * elem : 0;
+}
+gemel_status apart(gemel_ctx *ctx, const std::vector<Range> &r) {
+    for (size_t i = 0; i < r.size(); ++i)
+        for (size_t j = 0; j < r.size(); ++j)
+            if (r[i].out && i != j && r[i].lo < r[j].hi && r[j].lo < r[i].hi)
+                return fail(ctx, GEMEL_EINVAL, std::string(r[i].what) + " overlaps " + r[j].what);
+    return GEMEL_OK;
+}
+
+gemel_status upload(gemel_ctx *ctx, State &st, const std::vector<int32_t> &words, Batch &b) {
+    size_t want = 64 << 10;
+    while (want < words.size() * 4) want *= 2;
+    auto fits = [&]() {
+        for (size_t i = 0; i < st.spare.size(); ++i)
+            if (st.spare[i].second == want) return (int)i;
+        return -1;
+    };
+    int at = fits();
+    if (at < 0 && st.retired.size() >= 32) {
+        OPCHK(hipDeviceSynchronize(), "hipDeviceSynchronize");
+        st.spare.insert(st.spare.end(), st.retired.begin(), st.retired.end());
+        st.retired.clear();
+        at = fits();
+    }
+    if (at >= 0) {
+        b.dev = st.spare[(size_t)at].first;
+        st.spare.erase(st.spare.begin() + at);
+    } else {
+        OPCHK(hipMalloc(&b.dev, want), "request tables");
+    }
+    b.bytes = want;
+    hipError_t e = hipSuccess;
+    if (st.pinned_bytes < want) {
+        if (st.pinned) (void)hipHostFree(st.pinned);
+        st.pinned = nullptr;
+        st.pinned_bytes = 0;
+        e = hipHostMalloc(&st.pinned, want, hipHostMallocDefault);
+        if (e == hipSuccess) st.pinned_bytes = want;
+    }
+    if (e == hipSuccess) {
+        std::memcpy(st.pinned, words.data(), words.size() * 4);
+        e = hipMemcpyAsync(b.dev, st.pinned, words.size() * 4, hipMemcpyHostToDevice, st.side);
+    }
+    if (e == hipSuccess) e = hipStreamSynchronize(st.side);
+    if (e != hipSuccess) {
+        (void)hipFree(b.dev);
+        b.dev = nullptr;
+        return hip_fail(ctx, e, "request tables");
+    }
+    return GEMEL_OK;
+}
+
+gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_rows, int n_req, int n_ad, int max_rank,
+                        const int32_t *ranks, const float *scales, int32_t *out_id) {
+    int64_t rows = 0;
+    for (int i = 0; i < n_req; ++i) rows += n_rows[i];
+    // rows by adapter: slot 0 none, slot 1 + a adapter a
+    std::vector<int> start((size_t)n_ad + 2, 0);
+    for (int i = 0; i < n_req; ++i) start[(size_t)(ids[i] + 1)] += n_rows[i];
+    std::vector<int> at((size_t)n_ad + 1);
+    int sum = 0;
+    for (int s = 0; s <= n_ad; ++s) {
+        at[(size_t)s] = sum;
+        sum += start[(size_t)s];
+    }
+    std::vector<int> perm((size_t)rows);
+    for (int i = 0, row = 0; i < n_req; ++i)
+        for (int k = 0; k < n_rows[i]; ++k) perm[(size_t)at[(size_t)(ids[i] + 1)]++] = row++;
+    std::vector<int> run_start, run_id, run_rank, run_of((size_t)n_ad, -1), items, chunks, chunk_first;
+    std::vector<float> run_scale;
+    // chunks of rows whose gradient sums are kept apart and then added in
+    // order: about 32 over the batch, so that few adapters still fill the card
+    const int per_chunk = (int)std::max<int64_t>(64, op_round_up((rows + 31) / 32, 16));
+    for (int a = 0; a < n_ad; ++a) {
+        const int n = start[(size_t)a + 1];
+        if (!n) continue;
+        const int u = (int)run_id.size(), p0 = at[(size_t)a + 1] - n;
+        run_of[(size_t)a] = u;
+        run_start.push_back(p0);
+        run_id.push_back(a);
+        run_rank.push_back(ranks ? ranks[a] : max_rank);
+        run_scale.push_back(scales ? scales[a] : 1.f);
+        for (int p = 0; p < n; p += 16)
+            for (int v : {u, p0 + p, std::min(16, n - p)}) items.push_back(v);
+        chunk_first.push_back((int)chunks.size() / 3);
+        for (int p = 0; p < n; p += per_chunk)
+            for (int v : {u, p0 + p, std::min(per_chunk, n - p)}) chunks.push_back(v);
+    }
+    run_start.push_back((int)rows);
+    chunk_first.push_back((int)chunks.size() / 3);
+    const int runs = (int)run_id.size();
+    std::vector<int> first_run;
+    for (int64_t p = 0, u = 0; p <= rows + 63; p += 64) {
+        while (u < runs && run_start[(size_t)u + 1] <= p) ++u;
+        first_run.push_back((int)u);
+    }
+    std::vector<int32_t> words;
+    auto add = [&](const void *p, size_t n) {
+        const size_t o = words.size();
+        words.resize(o + (size_t)op_round_up((int64_t)std::max<size_t>(n, 1), 4));
+        if (n) std::memcpy(words.data() + o, p, n * 4);
+        return o;
+    };
+    const size_t o_perm = add(perm.data(), perm.size()), o_start = add(run_start.data(), run_start.size()),
+                 o_id = add(run_id.data(), run_id.size()), o_rank = add(run_rank.data(), run_rank.size()),
+                 o_scale = add(run_scale.data(), run_scale.size()), o_first = add(first_run.data(), first_run.size()),
+                 o_items = add(items.data(), items.size()), o_chunks = add(chunks.data(), chunks.size()),
+                 o_cf = add(chunk_first.data(), chunk_first.size()), o_of = add(run_of.data(), run_of.size());
+    DeviceScope scope(ctx->device);
+    State *st = nullptr;
+    if (gemel_status s = ready(ctx, &st)) return s;
+    auto b = std::make_unique<Batch>();
+    size_t id = 0;
+    while (id < st->batches.size() && st->batches[id]) ++id;
+    if (id == st->batches.size()) st->batches.emplace_back();
+    st->retired.reserve(st->retired.size() + st->batches.size());
+    if (gemel_status s = upload(ctx, *st, words, *b)) return s;
+    const int *d = (const int *)b->dev;
+    BatchTables &t = b->t;
+    t.perm = d + o_perm;
+    t.run_start = d + o_start;
+    t.run_id = d + o_id;
+    t.run_rank = d + o_rank;
+    t.run_scale = (const float *)(d + o_scale);
+    t.first_run = d + o_first;
+    t.items = d + o_items;
+    t.chunks = d + o_chunks;
+    t.chunk_first = d + o_cf;
+    t.run_of = d + o_of;
+    t.rows = (int)rows;
+    t.runs = runs;
+    t.adapters = n_ad;
+    t.rank = max_rank;
+    t.n_items = (int)items.size() / 3;
+    t.n_chunks = (int)chunks.size() / 3;
+    st->batches[id] = std::move(b);
+    *out_id = (int32_t)id;
+    return GEMEL_OK;
+}
+
+// ---- products ----
+
+int64_t partial_floats(const MmArgs &a) {
+    return a.splits > 1 ? (int64_t)a.splits * a.batch * a.M * a.ldp : 0;
+}
+int vec_ok(const void *p, int64_t ld, int f32) {
+    return (uintptr_t)p % (f32 ? 16 : 8) == 0 && ld % 4 == 0;
+}
+// Rows that a product reads where they are; others are copied first.
+bool in_place(const void *p, int64_t rows, int64_t ld, int64_t cols) {
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= MM_MAX_LD && rows * ld <= 1ll << 30;
+}
+
+struct Call {
+    gemel_ctx *ctx;
+    State *st;
+    hipStream_t stream;
+    Layout lay;
+    char *base = nullptr;
+    template <typename T>
+    T *at(size_t off) const {
+        return (T *)(base + off);
+    }
+};
+
+gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_projection *p) {
+    if (!p) return fail(ctx, GEMEL_EINVAL, "proj is null");
+    if (p->n_in < 1 || p->n_out < 1 || p->n_in > MAX_DIM || p->n_out > MAX_DIM)
+        return fail(ctx, GEMEL_EINVAL, "n_in and n_out must be in 1.." + std::to_string(MAX_DIM));
+    if (!p->weight) return fail(ctx, GEMEL_EINVAL, "weight is null");
+    if (p->weight_stride < p->n_in) return fail(ctx, GEMEL_EINVAL, "weight_stride is smaller than n_in");
+    if (t.runs > 0 && (!p->a || !p->b)) return fail(ctx, GEMEL_EINVAL, "the batch uses adapters: a and b must be given");
+    return GEMEL_OK;
+}
+gemel_status check_rows(gemel_ctx *ctx, const char *what, const void *p, int64_t stride, int64_t cols, int64_t elem) {
+    if (!p) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is null");
+    if (stride < cols || stride > INT32_MAX) return fail(ctx, GEMEL_EINVAL, std::string(what) + " has a bad row stride");
+    if ((uintptr_t)p % (uintptr_t)elem) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is not aligned to its type");
+    return GEMEL_OK;
+}
+
+// The adapted product out[row] = in[row] * Wrows^T + low-rank part, where
+// `in` has K columns and the N rows of the other operand are at w (for
+// gradients its transposed copy).
+struct Adapted {
+    const void *in;
+    int64_t ld_in;
+    int K, N;
+    const void *w;       // [N][K] rows ld_w apart, or (w_t) [K][N]
+    int64_t ld_w;
+    bool w_t;
+    const void *bank;    // adapter halves with N, for the extension
+    int bank_rc;         // the half lies [rank][N], not [N][rank]
+    const float *bias;
+    void *out;
+    int64_t ld_out;
+    // the thin product, if it has been laid out
+    u16 *planes = nullptr;
+    float *t = nullptr;
+    // layout
+    size_t o_in = 0, o_in_lo = 0, o_ein = 0, o_w = 0, o_w_lo = 0, o_ew = 0, o_bank = 0, o_part = 0, o_max = 0;
+    bool pad_in = false, pad_w = false;
+    int64_t Kp = 0;
+    MmArgs mm{};
+};
+
+void plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
+    const int rp = (int)op_round_up(b.rank, 32);
+    p.Kp = op_round_up(p.K, 64);
+    MmArgs &m = p.mm;
+    m.M = b.rows;
+    m.N = p.N;
+    m.batch = 1;
+    m.nseg = f32 ? 3 : 1;
+    m.f16 = f32;
+    m.epi = f32 ? EPI_SCALED : EPI_ROWS;
+    p.pad_in = f32 || !in_place(p.in, b.rows, p.ld_in, p.K);
+    p.pad_w = f32 || p.w_t || !in_place(p.w, p.N, p.ld_w, p.K);
+    m.K = !f32 && p.K % 8 == 0 ? p.K : (int)p.Kp;
+    mm_plan(m);
+    if (p.pad_in) p.o_in = c.lay.take(b.rows * p.Kp, 2);
+    if (p.pad_w) p.o_w = c.lay.take(p.N * p.Kp, 2);
+    if (f32) {
+        p.o_in_lo = c.lay.take(b.rows * p.Kp, 2);
+        p.o_w_lo = c.lay.take(p.N * p.Kp, 2);
+        p.o_ein = c.lay.take(b.rows, 4);
+        p.o_ew = c.lay.take(p.N, 4);
+        if (p.w_t) p.o_max = c.lay.take(p.N, 4);
+    }
+    if (b.runs) p.o_bank = c.lay.take((int64_t)b.runs * op_round_up(p.N, 4) * rp, 4);
+    p.o_part = c.lay.take(partial_floats(m), 4);
+}
+
+gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
+    gemel_ctx *ctx = c.ctx;
+    const int rp = (int)op_round_up(b.rank, 32);
+    MmArgs &m = p.mm;
+    const u16 *in = (const u16 *)p.in, *w = (const u16 *)p.w;
+    m.lda = p.ld_in;
+    m.ldb = p.ld_w;
+    m.perm = b.perm;
+    m.perm_rows = b.rows;
+    m.o.perm = b.perm;
+    if (f32) {
+        SplitArgs s{};
+        s.in = (const float *)p.in;
+        s.ldi = p.ld_in;
+        s.hi = c.at<u16>(p.o_in);
+        s.lo = c.at<u16>(p.o_in_lo);
+        s.e = c.at<int>(p.o_ein);
+        s.ldo = p.Kp;
+        s.rows = b.rows;
+        s.cols = p.K;
+        s.perm = b.perm;
+        OPCHK(launch_split(s, c.stream), "split");
+        s.in = (const float *)p.w;
+        s.ldi = p.ld_w;
+        s.hi = c.at<u16>(p.o_w);
+        s.lo = c.at<u16>(p.o_w_lo);
+        s.e = c.at<int>(p.o_ew);
+        s.perm = nullptr;
+        s.transposed = p.w_t;
+        s.rows = p.w_t ? p.K : p.N;
+        s.cols = p.w_t ? p.N : p.K;
+        s.colmax = c.at<unsigned>(p.o_max);
+        OPCHK(launch_split(s, c.stream), "split");
+        const u16 *ah = c.at<u16>(p.o_in), *al = c.at<u16>(p.o_in_lo), *bh = c.at<u16>(p.o_w), *bl = c.at<u16>(p.o_w_lo);
+        m.a[0] = ah;
+        m.b[0] = bl;
+        m.a[1] = al;
+        m.b[1] = bh;
+        m.a[2] = ah;
+        m.b[2] = bh;
+        m.lda = m.ldb = p.Kp;
+        m.perm = nullptr;
+        m.o.ea = c.at<int>(p.o_ein);
+        m.o.eb = c.at<int>(p.o_ew);
+        m.o.t = p.t;
+        m.o.bx = c.at<float>(p.o_bank);
+        m.o.rp = rp;
+        m.o.ldbx = op_round_up(p.N, 4);
+        m.o.out_f32 = 1;
+    } else {
+        if (p.pad_in) {
+            OPCHK(launch_pad({in, c.at<u16>(p.o_in), p.ld_in, p.Kp, b.rows, p.K, 0, b.perm}, c.stream), "pad");
+            in = c.at<u16>(p.o_in);
+            m.lda = p.Kp;
+            m.perm = nullptr;
+        }
+        if (p.pad_w) {
+            OPCHK(launch_pad({w, c.at<u16>(p.o_w), p.ld_w, p.Kp, p.w_t ? p.K : p.N, p.w_t ? p.N : p.K, p.w_t, nullptr}, c.stream),
+                  "pad");
+            w = c.at<u16>(p.o_w);
+            m.ldb = p.Kp;
+        }
+        m.a[0] = in;
+        m.b[0] = w;
+        if (b.runs) {
+            m.ext = 2 * rp;
+            m.t = p.planes;
+            m.bx = c.at<u16>(p.o_bank);
+        }
+    }
+    m.runs = b.runs;
+    m.run_start = b.run_start;
+    m.first_run = b.first_run;
+    if (b.runs) {
+        PackRankArgs k{p.bank, c.at<char>(p.o_bank), p.bank_rc, f32, f32, p.N, b.rank, rp, op_round_up(p.N, 4), b};
+        OPCHK(launch_pack_rank(k, c.stream), "pack");
+    }
+    m.zero = (const u16 *)c.st->zero;
+    m.partial = c.at<float>(p.o_part);
+    m.o.out = p.out;
+    m.o.ld = p.ld_out;
+    m.o.vec = vec_ok(p.out, p.ld_out, f32);
+    m.o.bias = p.bias;
+    OPCHK(launch_mm(m, c.stream), "product");
+    return GEMEL_OK;
+}
+
+gemel_status get_batch(gemel_ctx *ctx, int32_t id, State **st, Batch **b) {
+    State *s = static_cast<State *>(ctx->operators.get());
+    if (!s || id < 0 || (size_t)id >= s->batches.size() || !s->batches[(size_t)id])
+        return fail(ctx, GEMEL_EINVAL, "unknown batch id " + std::to_string(id));
+    *st = s;
+    *b = s->batches[(size_t)id].get();
+    return GEMEL_OK;
+}
+
+gemel_status shrink(Call &c, const BatchTables &b, bool f32, const void *x, int64_t ldx, int K, const void *a, int64_t lda,
+                    bool by_run, u16 *planes, float *t) {
+    gemel_ctx *ctx = c.ctx;
+    ShrinkArgs s{};
+    s.x = x;
+    s.a = a;
+    s.ldx = ldx;
+    s.lda = lda;
+    s.by_run = by_run;
+    s.f32 = f32;
+    s.K = K;
+    s.rp = (int)op_round_up(b.rank, 32);
+    const int64_t q = f32 ? 4 : 8;
+    s.vx = (uintptr_t)x % 16 == 0 && ldx % q == 0;
+    s.va = (uintptr_t)a % 16 == 0 && lda % q == 0;
+    s.planes = planes;
+    s.t = t;
+    s.b = b;
+    OPCHK(launch_shrink(s, c.stream), "thin product");
+    return GEMEL_OK;
+}
+
+gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, const void *x, int64_t ldx, void *y,
+                   int64_t ldy, hipStream_t stream) {
+    State *st;
+    Batch *bt;
+    if (gemel_status s = get_batch(ctx, id, &st, &bt)) return s;
+    const BatchTables &b = bt->t;
+    if (gemel_status s = check_projection(ctx, b, proj)) return s;
+    if (b.rows == 0) return GEMEL_OK;
+    const bool f32 = ctx->dtype == GEMEL_F32;
+    const int64_t e = f32 ? 4 : 2, K = proj->n_in, N = proj->n_out, bank = (int64_t)b.adapters * b.rank;
+    if (gemel_status s = check_rows(ctx, "x", x, ldx, K, e)) return s;
+    if (gemel_status s = check_rows(ctx, "y", y, ldy, N, e)) return s;
+    if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
+    if (gemel_status s = apart(ctx, {range("y", y, span(b.rows, N, ldy, e), true),
+                                     range("x", x, span(b.rows, K, ldx, e), false),
+                                     range("weight", proj->weight, span(N, K, proj->weight_stride, e), false),
+                                     range("bias", proj->bias, N * 4, false), range("a", proj->a, bank * K * e, false),
+                                     range("b", proj->b, bank * N * e, false)}))
+        return s;
+    DeviceScope scope(ctx->device);
+    Call c{ctx, st, stream, {}, nullptr};
+    const int rp = (int)op_round_up(b.rank, 32);
+    Adapted p{};
+    p.in = x;
+    p.ld_in = ldx;
+    p.K = (int)K;
+    p.N = (int)N;
+    p.w = proj->weight;
+    p.ld_w = proj->weight_stride;
+    p.w_t = false;
+    p.bank = proj->b;
+    p.bank_rc = 0;
+    p.bias = proj->bias;
+    p.out = y;
+    p.ld_out = ldy;
+    const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4);
+    plan_adapted(c, b, f32, p);
+    if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
+    if (b.runs) {
+        p.planes = f32 ? nullptr : c.at<u16>(o_t);
+        p.t = f32 ? c.at<float>(o_t) : nullptr;
+        if (gemel_status s = shrink(c, b, f32, x, ldx, (int)K, proj->a, K, false, p.planes, p.t)) return s;
+    }
+    return run_adapted(c, b, f32, p);
+}
+
+gemel_status zero_out(Call &c, float *p, int64_t n) {
+    gemel_ctx *ctx = c.ctx;
+    for (int64_t at = 0; p && at < n; at += 1 << 30)
+        OPCHK(launch_fill_u32((uint32_t *)p + at, (size_t)std::min<int64_t>(n - at, 1 << 30), 0, Sink{c.stream}), "fill");
+    return GEMEL_OK;
+}
+
+gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, const void *x, int64_t ldx, const void *dy,
+                      int64_t lddy, void *dx, int64_t lddx, float *dw, float *dbias, float *da, float *db,
+                      hipStream_t stream) {
+    State *st;
+    Batch *bt;
+    if (gemel_status s = get_batch(ctx, id, &st, &bt)) return s;
+    const BatchTables &b = bt->t;
+    if (gemel_status s = check_projection(ctx, b, proj)) return s;
+    const bool f32 = ctx->dtype == GEMEL_F32;
+    const int64_t e = f32 ? 4 : 2, K = proj->n_in, N = proj->n_out, M = b.rows, bank = (int64_t)b.adapters * b.rank;
+    if (M > 0) {
+        if (gemel_status s = check_rows(ctx, "x", x, ldx, K, e)) return s;
+        if (gemel_status s = check_rows(ctx, "dy", dy, lddy, N, e)) return s;
+        if (dx)
+            if (gemel_status s = check_rows(ctx, "dx", dx, lddx, K, e)) return s;
+        if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
+    }
+    if (gemel_status s = apart(ctx, {range("dx", dx, span(M, K, lddx, e), true), range("dweight", dw, N * K * 4, true),
+                                     range("dbias", dbias, N * 4, true), range("da", da, bank * K * 4, true),
+                                     range("db", db, bank * N * 4, true), range("x", x, span(M, K, ldx, e), false),
+                                     range("dy", dy, span(M, N, lddy, e), false),
+                                     range("weight", proj->weight, span(N, K, proj->weight_stride, e), false),
+                                     range("a", proj->a, bank * K * e, false), range("b", proj->b, bank * N * e, false)}))
+        return s;
+    if (!dx && !dw && !dbias && !da && !db) return GEMEL_OK;
+    DeviceScope scope(ctx->device);
+    Call c{ctx, st, stream, {}, nullptr};
+    if (M == 0 || b.runs == 0) {
+        if (gemel_status s = zero_out(c, da, bank * K)) return s;
+        if (gemel_status s = zero_out(c, db, bank * N)) return s;
+        da = db = nullptr;
+    }
+    if (M == 0) {
+        if (gemel_status s = zero_out(c, dw, N * K)) return s;
+        return zero_out(c, dbias, N);
+    }
+    const int rp = (int)op_round_up(b.rank, 32);
+    const int64_t Mp = op_round_up(M, 64), Np = op_round_up(N, 64);
+    const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
+    const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u ? M * rp : 0, 4),
+                 o_t = c.lay.take(need_t ? M * rp : 0, 4), o_bt = c.lay.take(need_u ? b.runs * rp * Np : 0, e);
+    // the parts below run one after the other in the same stretch
+    const size_t shared = c.lay.bytes;
+    size_t most = shared;
+    Adapted p{};
+    if (dx) {
+        p.in = dy;
+        p.ld_in = lddy;
+        p.K = (int)N;
+        p.N = (int)K;
+        p.w = proj->weight;
+        p.ld_w = proj->weight_stride;
+        p.w_t = true;
+        p.bank = proj->a;
+        p.bank_rc = 1;
+        p.out = dx;
+        p.ld_out = lddx;
+        plan_adapted(c, b, f32, p);
+        most = std::max(most, c.lay.bytes);
+        c.lay.bytes = shared;
+    }
+    MmArgs w{};
+    size_t o_x = 0, o_xl = 0, o_ex = 0, o_d = 0, o_dl = 0, o_ed = 0, o_max = 0, o_wp = 0;
+    if (dw) {
+        w.M = (int)N;
+        w.N = (int)K;
+        w.K = (int)Mp;
+        w.batch = 1;
+        w.nseg = f32 ? 3 : 1;
+        w.f16 = f32;
+        w.epi = f32 ? EPI_SCALED : EPI_ROWS;
+        w.lda = w.ldb = Mp;
+        mm_plan(w);
+        o_x = c.lay.take(K * Mp, 2);
+        o_d = c.lay.take(N * Mp, 2);
+        if (f32) {
+            o_xl = c.lay.take(K * Mp, 2);
+            o_dl = c.lay.take(N * Mp, 2);
+            o_ex = c.lay.take(K, 4);
+            o_ed = c.lay.take(N, 4);
+            o_max = c.lay.take(std::max(K, N), 4);
+        }
+        o_wp = c.lay.take(partial_floats(w), 4);
+        most = std::max(most, c.lay.bytes);
+        c.lay.bytes = shared;
+    }
+    ColsumArgs cs{dy, lddy, f32, (int)M, (int)N, (int)std::min<int64_t>(256, (M + 31) / 32), nullptr, dbias};
+    const size_t o_cs = c.lay.take(dbias ? cs.parts * N : 0, 4);
+    const size_t o_op = c.lay.take(da || db ? (int64_t)b.n_chunks * rp * std::max(K, N) : 0, 4);
+    c.lay.bytes = std::max(most, c.lay.bytes);
+    if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
+
+    float *t = need_t ? c.at<float>(o_t) : nullptr, *u = need_u ? c.at<float>(o_u) : nullptr;
+    if (need_t)
+        if (gemel_status s = shrink(c, b, f32, x, ldx, (int)K, proj->a, K, false, nullptr, t)) return s;
+    if (need_u) {
+        PackRankArgs k{proj->b, c.at<char>(o_bt), 0, 1, f32, (int)N, b.rank, rp, Np, b};
+        OPCHK(launch_pack_rank(k, stream), "pack");
+        p.planes = f32 ? nullptr : c.at<u16>(o_up);
+        p.t = f32 ? u : nullptr;
+        if (gemel_status s = shrink(c, b, f32, dy, lddy, (int)N, c.at<char>(o_bt), Np, true, p.planes, u)) return s;
+    }
+    if (dx)
+        if (gemel_status s = run_adapted(c, b, f32, p)) return s;
+    if (dw) {
+        if (f32) {
+            SplitArgs s{};
+            s.transposed = 1;
+            s.rows = (int)M;
+            s.ldo = Mp;
+            s.colmax = c.at<unsigned>(o_max);
+            s.in = (const float *)dy;
+            s.ldi = lddy;
+            s.cols = (int)N;
+            s.hi = c.at<u16>(o_d);
+            s.lo = c.at<u16>(o_dl);
+            s.e = c.at<int>(o_ed);
+            OPCHK(launch_split(s, stream), "split");
+            s.in = (const float *)x;
+            s.ldi = ldx;
+            s.cols = (int)K;
+            s.hi = c.at<u16>(o_x);
+            s.lo = c.at<u16>(o_xl);
+            s.e = c.at<int>(o_ex);
+            OPCHK(launch_split(s, stream), "split");
+            w.a[0] = c.at<u16>(o_d);
+            w.b[0] = c.at<u16>(o_xl);
+            w.a[1] = c.at<u16>(o_dl);
+            w.b[1] = c.at<u16>(o_x);
+            w.a[2] = c.at<u16>(o_d);
+            w.b[2] = c.at<u16>(o_x);
+            w.o.ea = c.at<int>(o_ed);
+            w.o.eb = c.at<int>(o_ex);
+        } else {
+            OPCHK(launch_pad({(const u16 *)dy, c.at<u16>(o_d), lddy, Mp, (int)M, (int)N, 1, nullptr}, stream), "pad");
+            OPCHK(launch_pad({(const u16 *)x, c.at<u16>(o_x), ldx, Mp, (int)M, (int)K, 1, nullptr}, stream), "pad");
+            w.a[0] = c.at<u16>(o_d);
+            w.b[0] = c.at<u16>(o_x);
+        }
+        w.zero = (const u16 *)st->zero;
+        w.partial = c.at<float>(o_wp);
+        w.o.out = dw;
+        w.o.ld = K;
+        w.o.out_f32 = 1;
+        w.o.vec = vec_ok(dw, K, 1);
+        OPCHK(launch_mm(w, stream), "product");
+    }
+    if (dbias) {
+        cs.part = c.at<float>(o_cs);
+        OPCHK(launch_colsum(cs, stream), "column sums");
+    }
+    OuterArgs o{};
+    o.f32 = f32;
+    o.rp = rp;
+    o.part = c.at<float>(o_op);
+    o.b = b;
+    if (da) {
+        o.p = u;
+        o.q = x;
+        o.ldq = ldx;
+        o.C = (int)K;
+        o.out = da;
+        OPCHK(launch_outer(o, stream), "adapter gradient");
+    }
+    if (db) {
+        o.p = t;
+        o.q = dy;
+        o.ldq = lddy;
+        o.C = (int)N;
+        o.transposed = 1;
+        o.out = db;
+        OPCHK(launch_outer(o, stream), "adapter gradient");
+    }
+    return GEMEL_OK;
+}
+
+// ---- orthogonalised updates ----
+
+// Thin matrices: their Gram matrix, its polynomials, and the result.
+gemel_status orthogonal_thin(Call &c, OrthArgs o) {
+    gemel_ctx *ctx = c.ctx;
+    const int n = std::min(o.rows, o.cols), m = std::max(o.rows, o.cols), np = (int)op_round_up(n, 16);
+    const int64_t e = o.f32 ? 16 : 8;
+    o.vec = o.cols % 4 == 0 && (uintptr_t)o.g % e == 0 && (uintptr_t)o.m % 16 == 0 &&
+            (uintptr_t)o.out % (o.step ? 16 : e) == 0 && (uintptr_t)o.copy % 8 == 0;
+    // stretches of 64 positions for each workgroup: enough workgroups for
+    // two on each compute unit, few enough that one adds their sums
+    o.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(m + 63) / 64, 64, (1024 + o.count - 1) / o.count}));
+    const size_t og = c.lay.take((int64_t)o.count * o.parts * np * np, 8), oq = c.lay.take((int64_t)o.count * np * np, 4),
+                 oe = c.lay.take(o.count, 4);
+    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return s;
+    o.gram = c.at<double>(og);
+    o.q = c.at<float>(oq);
+    o.e = c.at<int>(oe);
+    OPCHK(launch_thin_gram(o, c.stream), "Gram matrix");
+    OPCHK(launch_thin_poly(o, c.stream), "polynomials");
+    OPCHK(launch_thin_apply(o, c.stream), "result");
+    return GEMEL_OK;
+}
+
+// Newton-Schulz on the wide orientation X [n][m], n <= m: S = X X^T,
+// M = b S + c S^2, X <- a X + M X. All operands are read along their rows,
+// so X is kept in both layouts and S and M, being symmetric, in one.
+//
+// bf16 updates take one float16 product where float32 ones take three (hi hi,
+// hi lo, lo hi). What rounding would cost them is in a X: noise of 2^-12 of
+// X's large directions, spread over all small ones, would grow with these up
+// to 485 times. So X keeps its rest (lo) for that term, while M, S and X in M
+// X, whose rounding lands in the directions that are large already or is
+// averaged over a whole row, do without, except for their diagonals: once X
+// is nearly orthogonal these are most of S and M.
+gemel_status orthogonal(Call &c, OrthArgs o) {
+    gemel_ctx *ctx = c.ctx;
+    if (std::min(o.rows, o.cols) <= THIN_MAX) return orthogonal_thin(c, o);
+    const int steps = o.steps;
+    const bool step = o.step;
+    const int n = std::min(o.rows, o.cols), m = std::max(o.rows, o.cols);
+    const int64_t np = op_round_up(n, 64), mp = op_round_up(m, 64), size = (int64_t)o.rows * o.cols;
+    const bool lo = step || o.f32, wide = o.rows <= o.cols;
+    const int all = o.count;
+    // matrices at a time: planes of at most 4 GiB
+    const int64_t each = 12 * np * mp + 4 * np * (np + 64);
+    const int group = (int)std::max<int64_t>(1, std::min<int64_t>(all, (int64_t)(4ll << 30) / each));
+    auto planes = [&](int64_t rows, int64_t ld, bool rest) {
+        Planes p{nullptr, nullptr, ld, rows * ld};
+        const size_t a = c.lay.take(group * rows * ld, 2), b = rest ? c.lay.take(group * rows * ld, 2) : 0;
+        p.hi = (u16 *)a;
+        p.lo = (u16 *)b;
+        return p;
+    };
+    Planes x = planes(n, mp, true), t0 = planes(m, np, true), t1 = planes(m, np, true), s = planes(n, np, lo),
+           p = planes(n, np, lo);
+    o.parts = (int)std::min<int64_t>(256, (size + 4095) / 4096);
+    const size_t o_sums = c.lay.take((int64_t)group * o.parts, 8), o_lambda = c.lay.take(group * ORTH_LAMBDAS, 4),
+                 o_sd = c.lay.take(lo ? 0 : group * np, 4), o_md = c.lay.take(lo ? 0 : group * np, 4);
+    MmArgs gram{}, poly{}, next{}, last{};
+    auto shape = [&](MmArgs &a, int M, int N, int64_t K, int epi, bool sym) {
+        a.M = M;
+        a.N = N;
+        a.K = (int)K;
+        a.batch = group;
+        a.nseg = lo ? 3 : 1;
+        a.f16 = 1;
+        a.epi = epi;
+        a.sym = sym;
+        mm_plan(a);
+        return partial_floats(a);
+    };
+    int64_t part = shape(gram, n, n, mp, EPI_GRAM, true);
+    part = std::max(part, shape(poly, n, n, np, EPI_POLY, true));
+    part = std::max(part, shape(next, m, n, np, EPI_NEXT, false));
+    part = std::max(part, wide ? shape(last, n, m, np, step ? EPI_STEP : EPI_ORTH, false)
+                               : shape(last, m, n, np, step ? EPI_STEP : EPI_ORTH, false));
+    const size_t o_part = c.lay.take(part, 4);
+    if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return e;
+    for (Planes *q : {&x, &t0, &t1, &s, &p}) {
+        q->hi = c.at<u16>((size_t)q->hi);
+        q->lo = q->lo ? c.at<u16>((size_t)q->lo) : nullptr;
+    }
+    o.sums = c.at<double>(o_sums);
+    o.lambda = c.at<float>(o_lambda);
+    const int64_t ge = o.f32 ? 4 : 2;
+    const char *g0 = (const char *)o.g;
+    float *m0 = o.m;
+    for (int at = 0; at < all; at += group) {
+        const int count = std::min(group, all - at);
+        o.count = count;
+        o.g = g0 + at * size * ge;
+        o.m = m0 ? m0 + at * size : nullptr;
+        // a bf16 update is its own float16 plane
+        o.x = x;
+        o.xt = t0;
+        if (!lo) o.x.lo = o.xt.lo = nullptr;
+        OPCHK(launch_norm(o, c.stream), "norm");
+        OPCHK(launch_seed(o, c.stream), "scaled update");
+        auto operands = [&](MmArgs &a, const Planes &l, const Planes &r) {
+            const u16 *al[3] = {l.hi, lo ? l.lo : nullptr, l.hi}, *bl[3] = {lo ? r.lo : r.hi, r.hi, r.hi};
+            for (int i = 0; i < 3; ++i) {
+                a.a[i] = al[i];
+                a.b[i] = bl[i];
+            }
+            a.lda = l.ld;
+            a.ldb = r.ld;
+            a.za = l.z;
+            a.zb = r.z;
+            a.batch = count;
+            a.zero = (const u16 *)c.st->zero;
+            a.partial = c.at<float>(o_part);
+            a.o.sdiag = lo ? nullptr : c.at<float>(o_sd);
+            a.o.mdiag = lo ? nullptr : c.at<float>(o_md);
+            a.o.diag_z = np;
+        };
+        Planes from = o.xt, to = t1, now = o.x;
+        for (int k = 0; k < steps; ++k) {
+            operands(gram, now, now);
+            gram.o.p = s;
+            OPCHK(launch_mm(gram, c.stream), "product");
+            operands(poly, s, s);
+            poly.o.s = s;
+            poly.o.p = p;
+            poly.o.lambda = o.lambda + k;
+            OPCHK(launch_mm(poly, c.stream), "product");
+            if (k + 1 < steps) {
+                operands(next, from, p);
+                next.o.s = from;
+                next.o.p = to;
+                now = x;
+                if (!lo && (!wide || k + 2 < steps)) now.lo = nullptr;   // nobody reads it
+                next.o.q = now;
+                next.o.lambda = o.lambda + k;
+                OPCHK(launch_mm(next, c.stream), "product");
+                const Planes read = from.lo ? from : t0;
+                from = to;
+                to = read;
+            } else {
+                if (wide)
+                    operands(last, p, from);
+                else
+                    operands(last, from, p);
+                last.o.s = wide ? now : from;
+                last.o.diag_rows = wide;
+                last.o.ld = o.cols;
+                last.o.z = size;
+                last.o.out_f32 = o.f32;
+                last.o.out = (char *)o.out + at * size * (step ? 4 : ge);
+                last.o.copy = o.copy ? o.copy + at * size : nullptr;
+                last.o.rate = o.rate;
+                last.o.decay = o.decay;
+                last.o.lambda = o.lambda + k;
+                last.o.vec = o.cols % 4 == 0 && (uintptr_t)last.o.out % 16 == 0 && (uintptr_t)last.o.copy % 8 == 0;
+                OPCHK(launch_mm(last, c.stream), "product");
+            }
+        }
+    }
+    return GEMEL_OK;
+}
+
+gemel_status check_matrices(gemel_ctx *ctx, int count, int rows, int cols, int steps) {
+    if (count < 0 || count > MAX_COUNT) return fail(ctx, GEMEL_EINVAL, "count must be in 0.." + std::to_string(MAX_COUNT));
+    if (rows < 1 || cols < 1 || rows > MAX_DIM || cols > MAX_DIM)
+        return fail(ctx, GEMEL_EINVAL, "rows and cols must be in 1.." + std::to_string(MAX_DIM));
+    if (steps < 1 || steps > MAX_STEPS) return fail(ctx, GEMEL_EINVAL, "steps must be in 1.." + std::to_string(MAX_STEPS));
+    return GEMEL_OK;
+}
+
+// Runs f, with host allocation failures as a status.
+template <typename F>
+gemel_status guarded(gemel_ctx *ctx, F &&f) {
+    try {
+        return f();
+    } catch (const std::bad_alloc &) {
+        return fail(ctx, GEMEL_ENOMEM, "out of host memory");
+    } catch (const std::exception &e) {
+        return fail(ctx, GEMEL_EDEVICE, e.what());
+    }
+}
+
+}  // namespace
+
+extern "C" {
+
+gemel_status gemel_adapter_batch(gemel_ctx *ctx, const int32_t *adapter_ids, const int32_t *n_rows, int32_t n_requests,
+                                 int32_t n_adapters, int32_t max_rank, const int32_t *ranks, const float *scales,
+                                 int32_t *out_batch) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        if (!out_batch) return fail(ctx, GEMEL_EINVAL, "out_batch is null");
+        if (n_requests < 0 || (n_requests > 0 && (!adapter_ids || !n_rows)))
+            return fail(ctx, GEMEL_EINVAL, "bad request arrays");
+        if (n_adapters < 1 || n_adapters > MAX_COUNT)
+            return fail(ctx, GEMEL_EINVAL, "n_adapters must be in 1.." + std::to_string(MAX_COUNT));
+        if (max_rank < 1 || max_rank > MAX_RANK)
+            return fail(ctx, GEMEL_EINVAL, "max_rank must be in 1.." + std::to_string(MAX_RANK));
+        int64_t rows = 0;
+        for (int i = 0; i < n_requests; ++i) {
+            if (adapter_ids[i] < -1 || adapter_ids[i] >= n_adapters)
+                return fail(ctx, GEMEL_EINVAL, "request " + std::to_string(i) + ": unknown adapter " + std::to_string(adapter_ids[i]));
+            if (n_rows[i] < 0) return fail(ctx, GEMEL_EINVAL, "request " + std::to_string(i) + ": negative row count");
+            rows += n_rows[i];
+        }
+        if (rows > MAX_ROWS) return fail(ctx, GEMEL_EINVAL, "a batch holds at most " + std::to_string(MAX_ROWS) + " rows");
+        for (int a = 0; a < n_adapters; ++a) {
+            if (ranks && (ranks[a] < 1 || ranks[a] > max_rank))
+                return fail(ctx, GEMEL_EINVAL, "adapter " + std::to_string(a) + ": rank must be in 1..max_rank");
+            if (scales && !std::isfinite(scales[a]))
+                return fail(ctx, GEMEL_EINVAL, "adapter " + std::to_string(a) + ": scale is not finite");
+        }
+        return make_batch(ctx, adapter_ids, n_rows, n_requests, n_adapters, max_rank, ranks, scales, out_batch);
+    });
+}
+
+gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        State *st;
+        Batch *b;
+        if (gemel_status s = get_batch(ctx, batch, &st, &b)) return s;
+        st->retired.push_back({b->dev, b->bytes});
+        st->batches[(size_t)batch].reset();
+        return GEMEL_OK;
+    });
+}
+
+gemel_status gemel_adapt(gemel_ctx *ctx, int32_t batch, const gemel_projection *proj, const void *x, int64_t x_stride,
+                         void *y, int64_t y_stride, void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() { return adapt(ctx, batch, proj, x, x_stride, y, y_stride, (hipStream_t)hip_stream); });
+}
+
+gemel_status gemel_adapt_backward(gemel_ctx *ctx, int32_t batch, const gemel_projection *proj, const void *x,
+                                  int64_t x_stride, const void *dy, int64_t dy_stride, void *dx, int64_t dx_stride,
+                                  float *dweight, float *dbias, float *da, float *db, void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() {
+        return backward(ctx, batch, proj, x, x_stride, dy, dy_stride, dx, dx_stride, dweight, dbias, da, db,
+                        (hipStream_t)hip_stream);
+    });
+}
+
+gemel_status gemel_orthogonalize(gemel_ctx *ctx, int32_t count, int32_t rows, int32_t cols, const void *g, void *out,
+                                 int32_t steps, void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        if (gemel_status s = check_matrices(ctx, count, rows, cols, steps)) return s;
+        if (count == 0) return GEMEL_OK;
+        const int64_t e = ctx->dtype == GEMEL_F32 ? 4 : 2, bytes = (int64_t)count * rows * cols * e;
+        if (gemel_status s = check_rows(ctx, "g", g, cols, cols, e)) return s;
+        if (gemel_status s = check_rows(ctx, "out", out, cols, cols, e)) return s;
+        if (gemel_status s = apart(ctx, {range("out", out, bytes, true), range("g", g, bytes, false)})) return s;
+        DeviceScope scope(ctx->device);
+        State *st;
+        if (gemel_status s = ready(ctx, &st)) return s;
+        Call c{ctx, st, (hipStream_t)hip_stream, {}, nullptr};
+        OrthArgs o{};
+        o.g = g;
+        o.f32 = ctx->dtype == GEMEL_F32;
+        o.rows = rows;
+        o.cols = cols;
+        o.count = count;
+        o.steps = steps;
+        o.out = out;
+        return orthogonal(c, o);
+    });
+}
+
+gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows, int32_t cols, float *w, float *momentum,
+                             const float *g, void *copy, float lr, float beta, float weight_decay, int32_t nesterov,
+                             int32_t steps, void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        if (gemel_status s = check_matrices(ctx, count, rows, cols, steps)) return s;
+        if (!std::isfinite(lr) || !std::isfinite(beta) || !std::isfinite(weight_decay))
+            return fail(ctx, GEMEL_EINVAL, "lr, beta and weight_decay must be finite");
+        if (count == 0) return GEMEL_OK;
+        const int64_t n = (int64_t)count * rows * cols;
+        if (gemel_status s = check_rows(ctx, "w", w, cols, cols, 4)) return s;
+        if (gemel_status s = check_rows(ctx, "momentum", momentum, cols, cols, 4)) return s;
+        if (gemel_status s = check_rows(ctx, "g", g, cols, cols, 4)) return s;
+        if (copy && ctx->dtype != GEMEL_BF16) return fail(ctx, GEMEL_EINVAL, "copy is for bf16 contexts: w is float32 already");
+        if (copy)
+            if (gemel_status s = check_rows(ctx, "copy", copy, cols, cols, 2)) return s;
+        if (gemel_status s = apart(ctx, {range("w", w, n * 4, true), range("momentum", momentum, n * 4, true),
+                                         range("copy", copy, n * 2, true), range("g", g, n * 4, false)}))
+            return s;
+        DeviceScope scope(ctx->device);
+        State *st;
+        if (gemel_status s = ready(ctx, &st)) return s;
+        Call c{ctx, st, (hipStream_t)hip_stream, {}, nullptr};
+        OrthArgs o{};
+        o.g = g;
+        o.m = momentum;
+        o.f32 = 1;
+        o.step = 1;
+        o.nesterov = nesterov != 0;
+        o.beta = beta;
+        o.rows = rows;
+        o.cols = cols;
+        o.count = count;
+        o.steps = steps;
+        o.out = w;
+        o.copy = (u16 *)copy;
+        o.rate = (float)((double)lr * std::sqrt(std::max(1., (double)rows / cols)));
+        o.decay = (float)((double)lr * weight_decay);
+        return orthogonal(c, o);
+    });
+}
+
+}  // extern "C"

@@ -741,6 +741,7 @@ gemel_status gemel_destroy(gemel_ctx *ctx) {
         release_device(ctx);
         (void)hipSetDevice(prev);
     }
+    if (ctx->operators && !ctx->operators->release()) st = GEMEL_EDEVICE;
     delete ctx;
     return st;
 }

@@ -53,7 +53,13 @@ EXPORTED = ("gemel_create", "gemel_register_model", "gemel_merge",
             "gemel_sla_batches", "gemel_profile_batches",
             "gemel_model_outputs", "gemel_output_shape",
             "gemel_query", "gemel_set_option", "gemel_profile",
-            "gemel_last_error", "gemel_destroy")
+            "gemel_last_error", "gemel_destroy",
+            "gemel_adapter_batch", "gemel_adapter_batch_free",
+            "gemel_adapt", "gemel_adapt_backward", "gemel_orthogonalize",
+            "gemel_muon_step")
+# Operators that serve and retrain merged layers: not part of CPU builds of
+# the planner alone.
+OPERATORS = EXPORTED[-6:]
 
 _fp = ctypes.POINTER(ctypes.c_float)
 
@@ -78,6 +84,14 @@ class Member(ctypes.Structure):
 class Group(ctypes.Structure):
     _fields_ = [("n_members", ctypes.c_int32),
                 ("members", ctypes.POINTER(Member))]
+
+
+class Projection(ctypes.Structure):
+    _fields_ = [("n_in", ctypes.c_int32), ("n_out", ctypes.c_int32),
+                ("weight", ctypes.c_void_p),
+                ("weight_stride", ctypes.c_int64),
+                ("bias", ctypes.c_void_p), ("a", ctypes.c_void_p),
+                ("b", ctypes.c_void_p)]
 
 
 class KernelStat(ctypes.Structure):
@@ -110,7 +124,8 @@ def _hip_runtimes():
 
 def load(path):
     """Load another build of the same ABI (e.g. a CPU build of the host
-    code used by the tests) with its C signatures declared."""
+    code used by the tests) with its C signatures declared. Such a build may
+    lack the operators of OPERATORS."""
     return _configure(ctypes.CDLL(path))
 
 
@@ -151,9 +166,28 @@ def _configure(L):
     L.gemel_last_error.restype = ctypes.c_char_p
     L.gemel_destroy.argtypes = [vp]
     for name in EXPORTED:
-        if name != "gemel_last_error":
+        if name != "gemel_last_error" and name not in OPERATORS:
             getattr(L, name).restype = ctypes.c_int32
+    if hasattr(L, OPERATORS[0]):
+        _configure_operators(L)
     return L
+
+
+def _configure_operators(L):
+    vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    f32, pi32 = ctypes.c_float, ctypes.POINTER(ctypes.c_int32)
+    proj = ctypes.POINTER(Projection)
+    L.gemel_adapter_batch.argtypes = [vp, pi32, pi32, i32, i32, i32, pi32,
+                                      _fp, pi32]
+    L.gemel_adapter_batch_free.argtypes = [vp, i32]
+    L.gemel_adapt.argtypes = [vp, i32, proj, vp, i64, vp, i64, vp]
+    L.gemel_adapt_backward.argtypes = [vp, i32, proj, vp, i64, vp, i64, vp,
+                                       i64, vp, vp, vp, vp, vp]
+    L.gemel_orthogonalize.argtypes = [vp, i32, i32, i32, vp, vp, i32, vp]
+    L.gemel_muon_step.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, f32,
+                                  f32, f32, i32, i32, vp]
+    for name in OPERATORS:
+        getattr(L, name).restype = i32
 
 
 def lib():
@@ -237,6 +271,27 @@ def sla_batches(cost_ms, sla_ms, fps, swap_ms=None, pipelined=True,
     if st != OK:
         raise GemelError(st, "gemel_sla_batches: " + STATUS_NAMES.get(st, "?"))
     return list(b), v.value, t.value
+
+
+class AdapterBatch:
+    """The requests of Context.adapter_batch: rows of the batch, the bank's
+    sizes and the library's id. Give it back with close(), or drop it."""
+
+    def __init__(self, ctx, batch_id, rows, n_adapters, rank):
+        self._ctx, self.id = ctx, batch_id
+        self.rows, self.n_adapters, self.rank = rows, n_adapters, rank
+
+    def close(self):
+        if self._ctx is not None and self._ctx._h:
+            self._ctx._check(self._ctx._lib.gemel_adapter_batch_free(
+                self._ctx._h, self.id))
+        self._ctx = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
 
 
 class Context:
@@ -419,3 +474,182 @@ class Context:
                                    n_frames, out_ptrs, s.cuda_stream,
                                    noalloc=noalloc))
         return outputs
+
+    # -- serving and retraining merged layers --
+    def adapter_batch(self, adapter_ids, n_rows, n_adapters, rank, ranks=None,
+                      scales=None):
+        """Requests of n_rows[i] rows with adapter adapter_ids[i] (-1: none)
+        of a bank of n_adapters adapters of up to `rank`; per adapter its
+        rank (None: all `rank`) and scale (None: 1)."""
+        n = len(adapter_ids)
+        if len(n_rows) != n:
+            raise ValueError("adapter_ids and n_rows differ in length")
+        for what, v in (("ranks", ranks), ("scales", scales)):
+            if v is not None and len(v) != n_adapters:
+                raise ValueError(f"{what} must have one entry per adapter")
+        i32 = ctypes.c_int32
+        out = i32(-1)
+        self._check(self._lib.gemel_adapter_batch(
+            self._h, (i32 * max(n, 1))(*adapter_ids),
+            (i32 * max(n, 1))(*n_rows), n, n_adapters, rank,
+            None if ranks is None else (i32 * max(n_adapters, 1))(*ranks),
+            None if scales is None else
+            (ctypes.c_float * max(n_adapters, 1))(*scales),
+            ctypes.byref(out)))
+        return AdapterBatch(self, out.value, sum(n_rows), n_adapters, rank)
+
+    def _torch_dtype(self):
+        import torch
+        return torch.bfloat16 if self.dtype == "bf16" else torch.float32
+
+    def _tensor(self, name, t, shape, dtype, contiguous=True):
+        """Checks one operand: a tensor of the context's device with the
+        given shape and type whose rows are contiguous."""
+        if not t.is_cuda or t.device.index != self.device:
+            raise ValueError(f"{name} is not on cuda:{self.device}")
+        if t.dtype != dtype:
+            raise ValueError(f"{name} must be {dtype}, is {t.dtype}")
+        if t.shape != shape:
+            raise ValueError(f"{name} must have shape {tuple(shape)}, has "
+                             f"{tuple(t.shape)}")
+        if contiguous:
+            if not t.is_contiguous():
+                raise ValueError(f"{name} must be contiguous")
+        elif t.numel() and (t.shape[1] > 1 and t.stride(1) != 1 or
+                            t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name} must have contiguous rows")
+
+    @staticmethod
+    def _stride(t):
+        return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+    def _stream(self, stream):
+        if stream is not None:
+            return stream.cuda_stream
+        import torch
+        return torch.cuda.current_stream(self.device).cuda_stream
+
+    def _projection(self, batch, weight, a, b, bias):
+        if batch._ctx is not self:
+            raise ValueError("the batch is closed or of another context")
+        if weight.dim() != 2:
+            raise ValueError("weight must be [n_out, n_in]")
+        import torch
+        dt = self._torch_dtype()
+        n, k = weight.shape
+        self._tensor("weight", weight, (n, k), dt, contiguous=False)
+        if (a is None) != (b is None):
+            raise ValueError("a and b come together")
+        if a is not None:
+            self._tensor("a", a, (batch.n_adapters, batch.rank, k), dt)
+            self._tensor("b", b, (batch.n_adapters, n, batch.rank), dt)
+        if bias is not None:
+            self._tensor("bias", bias, (n,), torch.float32)
+        return Projection(k, n, weight.data_ptr(), self._stride(weight),
+                          None if bias is None else bias.data_ptr(),
+                          None if a is None else a.data_ptr(),
+                          None if b is None else b.data_ptr())
+
+    def adapt(self, batch, x, weight, a=None, b=None, bias=None, out=None,
+              stream=None):
+        """y = x W^T + bias + scale * (x A^T) B^T, each row with its
+        request's adapter: x [rows, n_in], weight [n_out, n_in], a
+        [adapters, rank, n_in], b [adapters, n_out, rank] of the context's
+        type, bias float32. x, weight and out may have a row stride."""
+        import torch
+        p = self._projection(batch, weight, a, b, bias)
+        dt = weight.dtype
+        self._tensor("x", x, (batch.rows, p.n_in), dt, contiguous=False)
+        if out is None:
+            out = torch.empty((batch.rows, p.n_out), dtype=dt,
+                              device=x.device)
+        else:
+            self._tensor("out", out, (batch.rows, p.n_out), dt,
+                         contiguous=False)
+        self._check(self._lib.gemel_adapt(
+            self._h, batch.id, ctypes.byref(p), x.data_ptr(),
+            self._stride(x), out.data_ptr(), self._stride(out),
+            self._stream(stream)))
+        return out
+
+    def adapt_backward(self, batch, dy, x, weight, a=None, b=None,
+                       needs=("x", "weight", "bias", "a", "b"), outputs=None,
+                       stream=None):
+        """Gradients of adapt for dy [rows, n_out], as a dict of those in
+        `needs`: "x" in the context's type; "weight", "bias", "a" and "b"
+        in float32. outputs: tensors to write, by name (others are made)."""
+        import torch
+        p = self._projection(batch, weight, a, b, None)
+        dt, f32 = weight.dtype, torch.float32
+        self._tensor("x", x, (batch.rows, p.n_in), dt, contiguous=False)
+        self._tensor("dy", dy, (batch.rows, p.n_out), dt, contiguous=False)
+        shapes = {"x": (batch.rows, p.n_in), "weight": (p.n_out, p.n_in),
+                  "bias": (p.n_out,),
+                  "a": (batch.n_adapters, batch.rank, p.n_in),
+                  "b": (batch.n_adapters, p.n_out, batch.rank)}
+        res = {}
+        for name in needs:
+            if name not in shapes:
+                raise ValueError(f"unknown gradient {name!r}")
+            if a is None and name in ("a", "b"):
+                if needs != ("x", "weight", "bias", "a", "b"):
+                    raise ValueError(f"gradient {name!r} without adapters")
+                continue
+            want = dt if name == "x" else f32
+            t = (outputs or {}).get(name)
+            if t is None:
+                t = torch.empty(shapes[name], dtype=want, device=x.device)
+            else:
+                self._tensor(f"outputs[{name!r}]", t, shapes[name], want,
+                             contiguous=name != "x")
+            res[name] = t
+        ptr = {k: t.data_ptr() for k, t in res.items()}
+        self._check(self._lib.gemel_adapt_backward(
+            self._h, batch.id, ctypes.byref(p), x.data_ptr(),
+            self._stride(x), dy.data_ptr(), self._stride(dy), ptr.get("x"),
+            self._stride(res["x"]) if "x" in res else 0, ptr.get("weight"),
+            ptr.get("bias"), ptr.get("a"), ptr.get("b"),
+            self._stream(stream)))
+        return res
+
+    @staticmethod
+    def _matrices(t):
+        if t.dim() not in (2, 3):
+            raise ValueError("expected [rows, cols] or [count, rows, cols]")
+        return (1,) * (3 - t.dim()) + tuple(t.shape)
+
+    def orthogonalize(self, g, steps=5, out=None, stream=None):
+        """Newton-Schulz orthogonalisation of [rows, cols] or [count, rows,
+        cols] contiguous matrices of the context's type."""
+        import torch
+        count, rows, cols = self._matrices(g)
+        dt = self._torch_dtype()
+        self._tensor("g", g, g.shape, dt)
+        if out is None:
+            out = torch.empty_like(g)
+        else:
+            self._tensor("out", out, g.shape, dt)
+        self._check(self._lib.gemel_orthogonalize(
+            self._h, count, rows, cols, g.data_ptr(), out.data_ptr(), steps,
+            self._stream(stream)))
+        return out
+
+    def muon_step(self, w, momentum_buffer, g, lr, momentum=0.95,
+                  weight_decay=0.0, nesterov=True, steps=5, copy=None,
+                  stream=None):
+        """One optimiser step, in place, of float32 matrices w [rows, cols]
+        or [count, rows, cols] with their momentum buffer and gradient; copy
+        (bf16 contexts) receives the new w in bf16."""
+        import torch
+        count, rows, cols = self._matrices(w)
+        for name, t in (("w", w), ("momentum_buffer", momentum_buffer),
+                        ("g", g)):
+            self._tensor(name, t, w.shape, torch.float32)
+        if copy is not None:
+            self._tensor("copy", copy, w.shape, torch.bfloat16)
+        self._check(self._lib.gemel_muon_step(
+            self._h, count, rows, cols, w.data_ptr(),
+            momentum_buffer.data_ptr(), g.data_ptr(),
+            None if copy is None else copy.data_ptr(), lr, momentum,
+            weight_decay, 1 if nesterov else 0, steps, self._stream(stream)))
+        return w
