@@ -193,23 +193,26 @@ __global__ __launch_bounds__(256) void colsum_sum_kernel(const ColsumArgs a) {
     a.out[c] = v;
 }
 
+template <typename E>
 __global__ __launch_bounds__(256) void pad_kernel(const PadArgs a) {
     const int64_t n = (int64_t)a.rows * a.ldo;
     for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
         const int64_t r = i / a.ldo, c = i - r * a.ldo;
-        a.out[i] = c < a.cols ? a.in[(a.perm ? a.perm[r] : r) * a.ldi + c] : (u16)0;
+        ((E *)a.out)[i] = c < a.cols ? ((const E *)a.in)[(a.perm ? a.perm[r] : r) * a.ldi + c] : (E)0;
     }
 }
 
 // 64 x 64 tiles through LDS; out[c][r], zeros for r in [rows, ldo).
 __global__ __launch_bounds__(256) void pad_t_kernel(const PadArgs a) {
     __shared__ u16 tile[64][66];
+    const u16 *in = (const u16 *)a.in;
+    u16 *out = (u16 *)a.out;
     const int r0 = blockIdx.x * 64, c0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
     for (int i = y; i < 64; i += 4)
-        tile[i][x] = r0 + i < a.rows && c0 + x < a.cols ? a.in[(int64_t)(r0 + i) * a.ldi + c0 + x] : (u16)0;
+        tile[i][x] = r0 + i < a.rows && c0 + x < a.cols ? in[(int64_t)(r0 + i) * a.ldi + c0 + x] : (u16)0;
     __syncthreads();
     for (int i = y; i < 64; i += 4)
-        if (c0 + i < a.cols && r0 + x < a.ldo) a.out[(int64_t)(c0 + i) * a.ldo + r0 + x] = tile[x][i];
+        if (c0 + i < a.cols && r0 + x < a.ldo) out[(int64_t)(c0 + i) * a.ldo + r0 + x] = tile[x][i];
 }
 
 // The exponent that brings a largest magnitude `mx` into [2^14, 2^15); 0
@@ -332,10 +335,10 @@ hipError_t launch_colsum(const ColsumArgs &a, hipStream_t s) {
 hipError_t launch_pad(const PadArgs &a, hipStream_t s) {
     if (!a.in || !a.out || a.rows <= 0 || a.cols <= 0 || a.ldo < (a.transposed ? a.rows : a.cols)) return hipErrorInvalidValue;
     if (!a.transposed)
-        return launch(reinterpret_cast<const void *>(&pad_kernel), dim3(blocks(((int64_t)a.rows * a.ldo + 255) / 256, 8192)),
-                      256, a, s);
+        return launch(a.f32 ? reinterpret_cast<const void *>(&pad_kernel<uint32_t>) : reinterpret_cast<const void *>(&pad_kernel<u16>),
+                      dim3(blocks(((int64_t)a.rows * a.ldo + 255) / 256, 8192)), 256, a, s);
     const int64_t by = (a.cols + 63) / 64;
-    if (by > 65535) return hipErrorInvalidValue;
+    if (by > 65535 || a.f32) return hipErrorInvalidValue;
     return launch(reinterpret_cast<const void *>(&pad_t_kernel), dim3((unsigned)((a.ldo + 63) / 64), (unsigned)by), 256, a, s);
 }
 

@@ -1,0 +1,310 @@
+// Adapted projections of few rows (up to 64): every request its own adapter,
+// one row each, is the usual load of a server.
+//
+// Reading the weights is what bounds them, and after that the launches. Two
+// launches do the work. The first holds workgroups of two kinds that do not
+// wait for each other: 64 outputs by a slice of the depth (the weights, by
+// direct global-to-LDS loads four steps ahead, on the matrix cores), and the
+// thin products x A^T of 16 rows of one adapter by a slice of the depth. The
+// second adds the slices in order, multiplies the thin sums with the rows of
+// B that each output needs, and adds the bias. All sums are float32; float32
+// operands stay float32.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <type_traits>
+
+#include "op_args.h"
+
+namespace gemel {
+
+namespace {
+
+typedef __attribute__((address_space(3))) unsigned char lds_u8;
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf_up(u16 h) { return __uint_as_float((uint32_t)h << 16); }
+__device__ __forceinline__ u16 bf_down(float f) { return __builtin_bit_cast(u16, (__bf16)f); }
+
+template <int N>
+__device__ __forceinline__ void wait_vm() {
+    static_assert(N >= 0 && N < 64, "vmcnt range");
+    __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
+}
+__device__ __forceinline__ void barrier() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+}
+
+// The matrix-core product of two 16-byte chunks a lane holds: 8 bf16 (32
+// depths over the 4 lane groups) or 4 float32 (16 depths; element e of every
+// chunk is one product of 4 depths, in an order that both operands share).
+template <bool F32>
+__device__ __forceinline__ f32x4 mul(const uint4 &a, const uint4 &b, f32x4 c) {
+    if constexpr (F32) {
+        const f32x4 x = __builtin_bit_cast(f32x4, a), y = __builtin_bit_cast(f32x4, b);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) c = __builtin_amdgcn_mfma_f32_16x16x4f32(x[e], y[e], c, 0, 0, 0);
+        return c;
+    } else {
+        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                       0);
+    }
+}
+
+// Bytes [at, at + 16) of a row of `end` bytes; what lies beyond is zero.
+// Elements are 2 or 4 bytes; `whole`: full chunks may be loaded at once.
+template <bool F32>
+__device__ __forceinline__ uint4 chunk(const char *row, int at, int end, int whole) {
+    if (whole && at + 16 <= end) return *(const uint4 *)(row + at);
+    union {
+        uint4 v;
+        u16 h[8];
+        uint32_t w[4];
+    } r;
+    if constexpr (F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = at + 4 * i < end ? *(const uint32_t *)(row + at + 4 * i) : 0u;
+    } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) r.h[i] = at + 2 * i < end ? *(const u16 *)(row + at + 2 * i) : (u16)0;
+    }
+    return r.v;
+}
+
+constexpr int ROW = 128;   // bytes of a row in a step
+constexpr int RING = 4;
+
+// Thin sums of item blockIdx / (rank blocks * slices): 4 waves share the slice.
+template <bool F32>
+__device__ __forceinline__ void thin(const RowsArgs &a, int block, f32x4 *part) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+    const int slice = block % a.thin_slices, rest = block / a.thin_slices;
+    const int rb = rest % a.rank_blocks, item = rest / a.rank_blocks;
+    const int *it = a.b.items + 3 * item;
+    const int u = it[0], p0 = it[1], n = it[2], rank = a.b.run_rank[u];
+    const int elem = F32 ? 4 : 2, end = a.k_bank * elem;
+    const char *x = (const char *)a.x + (int64_t)a.b.perm[p0 + min(l16, n - 1)] * a.ldx * elem;
+    const int r = rb * 16 + l16;
+    const bool used = r < rank;
+    const char *w = (const char *)a.a + ((int64_t)a.b.run_id[u] * a.b.rank + (used ? r : 0)) * a.k_bank * elem;
+    const int k0 = slice * a.thin_bytes, k1 = min(end, k0 + a.thin_bytes);
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    if (rb * 16 < rank) {
+#pragma unroll 4
+        for (int k = k0 + wave * 64 + g * 16; k - g * 16 < k1; k += 256) {
+            const uint4 xv = chunk<F32>(x, k, k1, 1);
+            const uint4 wv = chunk<F32>(w, k, used ? k1 : 0, a.va);
+            acc = mul<F32>(wv, xv, acc);
+        }
+    }
+    part[wave * 64 + lane] = acc;
+    __syncthreads();
+    if (wave) return;
+    for (int i = 1; i < 4; ++i) acc += part[i * 64 + lane];
+    if (l16 < n)
+        *(f32x4 *)(a.t + ((int64_t)slice * a.b.rows + p0 + l16) * a.rank_blocks * 16 + rb * 16 + 4 * g) =
+            acc * a.b.run_scale[u];
+}
+
+// MB blocks of 16 rows.
+template <bool F32, int MB>
+__global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a) {
+    constexpr int STAGE = (64 + 16 * MB) * ROW, LOADS = 2 + (MB + 1) / 2;
+    __shared__ __attribute__((aligned(1024))) unsigned char r0[STAGE + (MB & 1) * 16 * ROW], r1[STAGE + (MB & 1) * 16 * ROW],
+        r2[STAGE + (MB & 1) * 16 * ROW], r3[STAGE + (MB & 1) * 16 * ROW];
+    if ((int)blockIdx.x < a.thin_blocks) {
+        thin<F32>(a, blockIdx.x, (f32x4 *)r0);
+        return;
+    }
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int g = lane >> 4, l16 = lane & 15;
+    const int block = blockIdx.x - a.thin_blocks, tiles = (a.N + 63) / 64;
+    const int slice = block / tiles, n0 = (block - slice * tiles) * 64;
+    const int elem = F32 ? 4 : 2;
+    const int s0 = slice * a.steps, s1 = min(a.all_steps, s0 + a.steps);
+    // load i of a thread fills slot i * 256 + tid of a buffer: row slot / 8
+    // (64 weight rows, then the inputs; rows beyond the last repeat it),
+    // whose position slot % 8 holds chunk (slot % 8) ^ (row / 2 % 8)
+    const char *src[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) {
+        const int row = (i * 256 + tid) >> 3, ch = ((tid & 7) ^ ((row >> 1) & 7)) * 16;
+        const int m = min(max(row - 64, 0), a.b.rows - 1);
+        src[i] = i < 2 ? (const char *)a.w + (int64_t)min(n0 + row, a.N - 1) * a.ldw * elem + ch
+                       : (const char *)a.x + (int64_t)m * a.ldx * elem + ch;
+    }
+    const int end = a.K * elem;
+    int at = s0;
+    auto issue = [&](unsigned char *buf) __attribute__((always_inline)) {
+        // past the last step its chunks again, so that every step waits alike
+        const int k = min(at, s1 - 1) * ROW;
+        ++at;
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int row = (i * 256 + tid) >> 3, ch = ((tid & 7) ^ ((row >> 1) & 7)) * 16;
+            __builtin_amdgcn_global_load_lds(k + ch < end ? (const void *)(src[i] + k) : (const void *)a.zero,
+                                             (lds_u8 *)(buf + (i * 4 + wave) * 1024), 16, 0, 0);
+        }
+    };
+    f32x4 acc[MB];
+#pragma unroll
+    for (int i = 0; i < MB; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+    unsigned char *const ring[RING] = {r0, r1, r2, r3};
+#pragma unroll
+    for (int i = 0; i < RING - 1; ++i) issue(ring[i]);
+    const int sw = (l16 >> 1) & 7;
+    auto step = [&](const unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
+        wait_vm<(RING - 2) * LOADS>();
+        barrier();
+        issue(next);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int c = ((h * 4 + g) ^ sw) * 16;
+            const uint4 wv = *(const uint4 *)(cur + (wave * 16 + l16) * ROW + c);
+#pragma unroll
+            for (int i = 0; i < MB; ++i) acc[i] = mul<F32>(wv, *(const uint4 *)(cur + (64 + i * 16 + l16) * ROW + c), acc[i]);
+        }
+    };
+    // the slices are whole rings of steps (the last may run past its end,
+    // whose weights are then not multiplied)
+    int s = s0;
+    for (; s + RING <= s1; s += RING) {
+        step(r0, r3);
+        step(r1, r0);
+        step(r2, r1);
+        step(r3, r2);
+    }
+    if (s < s1) step(r0, r3);
+    if (s + 1 < s1) step(r1, r0);
+    if (s + 2 < s1) step(r2, r1);
+    wait_vm<0>();
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+        const int m = i * 16 + l16, n = n0 + wave * 16 + g * 4;
+        if (m < a.b.rows && n < a.ldp) *(f32x4 *)(a.partial + ((int64_t)slice * a.b.rows + m) * a.ldp + n) = acc[i];
+    }
+}
+
+// One row and 512 columns per workgroup. A chain of dependent loads is all
+// that a short launch takes, so what a row needs of the tables lies together,
+// and the slices are requested before it arrives.
+template <bool F32>
+__global__ __launch_bounds__(128) void rows_sum_kernel(const RowsArgs a) {
+    __shared__ float ts[256];
+    const int row = blockIdx.y, tid = threadIdx.x;
+    const int4 info = a.b.row_info[row];   // position, run or -1, adapter, rank
+    const int n = (blockIdx.x * 128 + tid) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (n < a.N) {
+        const float *part = a.partial + (int64_t)row * a.ldp + n;
+#pragma unroll 8
+        for (int k = 0; k < a.slices; ++k) v += *(const f32x4 *)(part + (int64_t)k * a.b.rows * a.ldp);
+    }
+    const int u = info.y, rank = u < 0 ? 0 : info.w;
+    for (int r = tid; r < rank; r += 128) {
+        const float *t = a.t + (int64_t)info.x * a.rank_blocks * 16 + r;
+        float x = 0.f;
+#pragma unroll 4
+        for (int k = 0; k < a.thin_slices; ++k) x += t[(int64_t)k * a.b.rows * a.rank_blocks * 16];
+        ts[r] = x;
+    }
+    __syncthreads();
+    if (n >= a.N) return;
+    if (u >= 0) {
+        const int R = a.b.rank, elem = F32 ? 4 : 2;
+        const char *b = (const char *)a.bank_b + ((int64_t)info.z * a.N + n) * R * elem;
+        const int left = min(4, a.N - n);
+        constexpr int Q = F32 ? 4 : 8;
+        for (int r = 0; r < rank; r += Q) {
+            uint4 q[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                q[i] = i < left ? chunk<F32>(b + (int64_t)i * R * elem, r * elem, rank * elem, a.vb) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+            for (int j = 0; j < Q; ++j) {
+                const float t = r + j < rank ? ts[r + j] : 0.f;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const uint32_t w = (&q[i].x)[F32 ? j : j / 2];
+                    v[i] += t * (F32 ? __uint_as_float(w) : bf_up((u16)(j % 2 ? w >> 16 : w & 0xffff)));
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (a.bias && n + i < a.N) v[i] += a.bias[n + i];
+    const int64_t at = (int64_t)row * a.ldy + n;
+    if constexpr (F32) {
+        float *y = (float *)a.y + at;
+        if (a.vy && n + 3 < a.N) {
+            *(f32x4 *)y = v;
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n + i < a.N) y[i] = v[i];
+        }
+    } else {
+        u16 *y = (u16 *)a.y + at;
+        if (a.vy && n + 3 < a.N) {
+            *(ushort4 *)y = make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3]));
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (n + i < a.N) y[i] = bf_down(v[i]);
+        }
+    }
+}
+
+template <bool F32>
+hipError_t go(const RowsArgs &a, hipStream_t s) {
+    const dim3 grid((unsigned)(a.thin_blocks + (a.N + 63) / 64 * a.slices));
+    void *p[] = {const_cast<RowsArgs *>(&a)};
+    const void *fn = nullptr;
+    switch ((a.b.rows + 15) / 16) {
+        case 1: fn = reinterpret_cast<const void *>(&rows_kernel<F32, 1>); break;
+        case 2: fn = reinterpret_cast<const void *>(&rows_kernel<F32, 2>); break;
+        case 3: fn = reinterpret_cast<const void *>(&rows_kernel<F32, 3>); break;
+        case 4: fn = reinterpret_cast<const void *>(&rows_kernel<F32, 4>); break;
+        default: return hipErrorInvalidValue;
+    }
+    const hipError_t e = hipLaunchKernel(fn, grid, dim3(256), p, 0, s);
+    if (e != hipSuccess) return e;
+    return hipLaunchKernel(reinterpret_cast<const void *>(&rows_sum_kernel<F32>),
+                           dim3((unsigned)((a.N + 511) / 512), (unsigned)a.b.rows), dim3(128), p, 0, s);
+}
+
+}  // namespace
+
+// Slices of the depth: as many workgroups as run at once (three on a compute
+// unit with up to 32 rows, else two), and at least four steps in each; thin
+// products 2 KB of each row in a slice.
+void rows_plan(RowsArgs &a) {
+    const int elem = a.f32 ? 4 : 2;
+    a.all_steps = (int)(((int64_t)a.K * elem + ROW - 1) / ROW);
+    a.rank_blocks = (a.b.rank + 15) / 16;
+    a.thin_bytes = 2048;
+    a.thin_slices = (int)(((int64_t)a.K * elem + a.thin_bytes - 1) / a.thin_bytes);
+    a.thin_blocks = a.b.runs ? a.b.n_items * a.rank_blocks * a.thin_slices : 0;
+    const int tiles = (a.N + 63) / 64, slots = a.b.rows <= 32 ? 768 : 512;
+    const int want = std::max(1, std::min({(slots - a.thin_blocks) / tiles, (a.all_steps + 3) / 4, 64}));
+    a.steps = (a.all_steps + want - 1) / want;
+    a.slices = (a.all_steps + a.steps - 1) / a.steps;
+    a.ldp = op_round_up(a.N, 4);
+}
+
+hipError_t launch_rows(const RowsArgs &a, hipStream_t s) {
+    const int q = a.f32 ? 4 : 8;
+    if (!a.x || !a.w || !a.y || !a.partial || !a.zero || a.b.rows < 1 || a.b.rows > ROWS_MAX || a.N < 1 || a.K < 1 ||
+        a.slices < 1 || a.steps < 1 || (int64_t)(a.slices - 1) * a.steps >= a.all_steps ||
+        (int64_t)a.slices * a.steps < a.all_steps || (uintptr_t)a.x % 16 || (uintptr_t)a.w % 16 || a.ldx % q || a.ldw % q ||
+        a.K % q || a.ldx < a.K || a.ldw < a.K || a.k_bank > a.K || a.k_bank < 1 || a.ldp < a.N || a.ldp % 4 || (int64_t)a.K * (a.f32 ? 4 : 2) > (1 << 30) ||
+        (a.thin_blocks && (!a.a || !a.bank_b || !a.t || a.b.rank > 256)))
+        return hipErrorInvalidValue;
+    return a.f32 ? go<true>(a, s) : go<false>(a, s);
+}
+
+}  // namespace gemel

@@ -89,6 +89,8 @@ constexpr int64_t MM_MAX_LD = 1 << 22;
 void mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape
 hipError_t launch_mm(const MmArgs &a, hipStream_t s);
 
+constexpr int ROWS_MAX = 64;   // rows that launch_rows takes
+
 // Requests grouped by adapter, as tables in device memory.
 struct BatchTables {
     const int *perm;       // [rows] row behind position p
@@ -101,8 +103,31 @@ struct BatchTables {
     const int *chunks;     // [n_chunks][3]: run, first position, positions
     const int *chunk_first;// [runs + 1] chunks of a run
     const int *run_of;     // [adapters] run or -1
+    const int4 *row_info;  // [rows], batches of up to ROWS_MAX rows: position, run or -1, adapter, rank
     int rows, runs, adapters, rank, n_items, n_chunks;
 };
+
+// y of up to ROWS_MAX rows. x and w in place: 16-byte aligned rows, K a
+// multiple of 8 (bf16) or 4 (f32).
+struct RowsArgs {
+    const void *x, *w, *a, *bank_b;
+    const float *bias;
+    void *y;
+    int64_t ldx, ldw, ldy;
+    int f32, K, N;
+    int k_bank;            // row length of a (K of x and w may be padded)
+    int va, vb, vy;        // whole 16-byte chunks (y: 4 elements) may be moved at once
+    const void *zero;      // 16 zero bytes or more
+    // rows_plan: slices of the depth in steps of 128 bytes, and of the thin
+    // products in bytes
+    int all_steps, steps, slices, rank_blocks, thin_bytes, thin_slices, thin_blocks;
+    int64_t ldp;
+    float *partial;        // [slices][rows][ldp]
+    float *t;              // [thin_slices][rows][rank_blocks * 16]
+    BatchTables b;
+};
+void rows_plan(RowsArgs &a);
+hipError_t launch_rows(const RowsArgs &a, hipStream_t s);
 
 // t[p][r] = scale * sum over k of x[perm[p]][k] * a[run][r][k]
 struct ShrinkArgs {
@@ -155,10 +180,10 @@ hipError_t launch_colsum(const ColsumArgs &a, hipStream_t s);
 // Copies into zero-padded rows: out[r][c] for c < ldo (transposed:
 // out[c][r] for r < ldo).
 struct PadArgs {
-    const u16 *in;
-    u16 *out;
+    const void *in;
+    void *out;
     int64_t ldi, ldo;
-    int rows, cols, transposed;
+    int rows, cols, transposed, f32;
     const int *perm;       // not transposed: input row of output row, or null
 };
 hipError_t launch_pad(const PadArgs &a, hipStream_t s);

@@ -261,6 +261,13 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
         while (u < runs && run_start[(size_t)u + 1] <= p) ++u;
         first_run.push_back((int)u);
     }
+    std::vector<int> info;
+    for (int i = 0, row = 0; rows <= ROWS_MAX && i < n_req; ++i)
+        for (int k = 0; k < n_rows[i]; ++k, ++row) {
+            const int pos = (int)(std::find(perm.begin(), perm.end(), row) - perm.begin());
+            const int u = ids[i] < 0 ? -1 : run_of[(size_t)ids[i]];
+            for (int v : {pos, u, ids[i], u < 0 ? 0 : run_rank[(size_t)u]}) info.push_back(v);
+        }
     std::vector<int32_t> words;
     auto add = [&](const void *p, size_t n) {
         const size_t o = words.size();
@@ -272,7 +279,8 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
                  o_id = add(run_id.data(), run_id.size()), o_rank = add(run_rank.data(), run_rank.size()),
                  o_scale = add(run_scale.data(), run_scale.size()), o_first = add(first_run.data(), first_run.size()),
                  o_items = add(items.data(), items.size()), o_chunks = add(chunks.data(), chunks.size()),
-                 o_cf = add(chunk_first.data(), chunk_first.size()), o_of = add(run_of.data(), run_of.size());
+                 o_cf = add(chunk_first.data(), chunk_first.size()), o_of = add(run_of.data(), run_of.size()),
+                 o_info = add(info.data(), info.size());
     DeviceScope scope(ctx->device);
     State *st = nullptr;
     if (gemel_status s = ready(ctx, &st)) return s;
@@ -294,6 +302,7 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
     t.chunks = d + o_chunks;
     t.chunk_first = d + o_cf;
     t.run_of = d + o_of;
+    t.row_info = (const int4 *)(d + o_info);
     t.rows = (int)rows;
     t.runs = runs;
     t.adapters = n_ad;
@@ -449,13 +458,13 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
         m.o.out_f32 = 1;
     } else {
         if (p.pad_in) {
-            OPCHK(launch_pad({in, c.at<u16>(p.o_in), p.ld_in, p.Kp, b.rows, p.K, 0, b.perm}, c.stream), "pad");
+            OPCHK(launch_pad({in, c.at<u16>(p.o_in), p.ld_in, p.Kp, b.rows, p.K, 0, 0, b.perm}, c.stream), "pad");
             in = c.at<u16>(p.o_in);
             m.lda = p.Kp;
             m.perm = nullptr;
         }
         if (p.pad_w) {
-            OPCHK(launch_pad({w, c.at<u16>(p.o_w), p.ld_w, p.Kp, p.w_t ? p.K : p.N, p.w_t ? p.N : p.K, p.w_t, nullptr}, c.stream),
+            OPCHK(launch_pad({w, c.at<u16>(p.o_w), p.ld_w, p.Kp, p.w_t ? p.K : p.N, p.w_t ? p.N : p.K, p.w_t, 0, nullptr}, c.stream),
                   "pad");
             w = c.at<u16>(p.o_w);
             m.ldb = p.Kp;
@@ -516,6 +525,55 @@ gemel_status shrink(Call &c, const BatchTables &b, bool f32, const void *x, int6
     return GEMEL_OK;
 }
 
+// Few rows: k_rows.hip, on copies of the operands that it cannot read in
+// place.
+gemel_status adapt_rows(Call &c, const BatchTables &b, bool f32, const gemel_projection *proj, const void *x, int64_t ldx,
+                        void *y, int64_t ldy) {
+    gemel_ctx *ctx = c.ctx;
+    const int64_t e = f32 ? 4 : 2, q = 16 / e, K = proj->n_in, N = proj->n_out, Kp = op_round_up(K, q);
+    auto fits = [&](const void *p, int64_t ld) { return (uintptr_t)p % 16 == 0 && ld % q == 0 && K % q == 0; };
+    const bool copy_x = !fits(x, ldx), copy_w = !fits(proj->weight, proj->weight_stride);
+    RowsArgs a{};
+    a.f32 = f32;
+    a.K = (int)Kp;
+    a.N = (int)N;
+    a.b = b;
+    rows_plan(a);
+    const size_t o_x = c.lay.take(copy_x ? b.rows * Kp : 0, e), o_w = c.lay.take(copy_w ? N * Kp : 0, e),
+                 o_p = c.lay.take((int64_t)a.slices * b.rows * a.ldp, 4),
+                 o_t = c.lay.take(a.thin_blocks ? (int64_t)a.thin_slices * b.rows * a.rank_blocks * 16 : 0, 4);
+    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return s;
+    a.x = x;
+    a.ldx = ldx;
+    a.w = proj->weight;
+    a.ldw = proj->weight_stride;
+    if (copy_x) {
+        OPCHK(launch_pad({x, c.at<char>(o_x), ldx, Kp, b.rows, (int)K, 0, f32, nullptr}, c.stream), "pad");
+        a.x = c.at<char>(o_x);
+        a.ldx = Kp;
+    }
+    if (copy_w) {
+        OPCHK(launch_pad({proj->weight, c.at<char>(o_w), proj->weight_stride, Kp, (int)N, (int)K, 0, f32, nullptr}, c.stream),
+              "pad");
+        a.w = c.at<char>(o_w);
+        a.ldw = Kp;
+    }
+    a.a = proj->a;
+    a.bank_b = proj->b;
+    a.bias = proj->bias;
+    a.y = y;
+    a.ldy = ldy;
+    a.k_bank = (int)K;
+    a.va = (uintptr_t)proj->a % 16 == 0 && K % q == 0;
+    a.vb = (uintptr_t)proj->b % 16 == 0 && b.rank % q == 0;
+    a.vy = vec_ok(y, ldy, f32);
+    a.zero = c.st->zero;
+    a.partial = c.at<float>(o_p);
+    a.t = c.at<float>(o_t);
+    OPCHK(launch_rows(a, c.stream), "product");
+    return GEMEL_OK;
+}
+
 gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, const void *x, int64_t ldx, void *y,
                    int64_t ldy, hipStream_t stream) {
     State *st;
@@ -537,6 +595,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
         return s;
     DeviceScope scope(ctx->device);
     Call c{ctx, st, stream, {}, nullptr};
+    if (b.rows <= ROWS_MAX) return adapt_rows(c, b, f32, proj, x, ldx, y, ldy);
     const int rp = (int)op_round_up(b.rank, 32);
     Adapted p{};
     p.in = x;
@@ -703,8 +762,8 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
             w.o.ea = c.at<int>(o_ed);
             w.o.eb = c.at<int>(o_ex);
         } else {
-            OPCHK(launch_pad({(const u16 *)dy, c.at<u16>(o_d), lddy, Mp, (int)M, (int)N, 1, nullptr}, stream), "pad");
-            OPCHK(launch_pad({(const u16 *)x, c.at<u16>(o_x), ldx, Mp, (int)M, (int)K, 1, nullptr}, stream), "pad");
+            OPCHK(launch_pad({(const u16 *)dy, c.at<u16>(o_d), lddy, Mp, (int)M, (int)N, 1, 0, nullptr}, stream), "pad");
+            OPCHK(launch_pad({(const u16 *)x, c.at<u16>(o_x), ldx, Mp, (int)M, (int)K, 1, 0, nullptr}, stream), "pad");
             w.a[0] = c.at<u16>(o_d);
             w.b[0] = c.at<u16>(o_x);
         }

@@ -273,6 +273,18 @@ def sla_batches(cost_ms, sla_ms, fps, swap_ms=None, pipelined=True,
     return list(b), v.value, t.value
 
 
+_torch_module = None
+
+
+def _torch():
+    """The torch module, imported at the first use."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
+
+
 class AdapterBatch:
     """The requests of Context.adapter_batch: rows of the batch, the bank's
     sizes and the library's id. Give it back with close(), or drop it."""
@@ -499,56 +511,55 @@ class Context:
         return AdapterBatch(self, out.value, sum(n_rows), n_adapters, rank)
 
     def _torch_dtype(self):
-        import torch
-        return torch.bfloat16 if self.dtype == "bf16" else torch.float32
+        return _torch().bfloat16 if self.dtype == "bf16" else _torch().float32
 
     def _tensor(self, name, t, shape, dtype, contiguous=True):
         """Checks one operand: a tensor of the context's device with the
         given shape and type whose rows are contiguous."""
-        if not t.is_cuda or t.device.index != self.device:
+        if t.get_device() != self.device:
             raise ValueError(f"{name} is not on cuda:{self.device}")
         if t.dtype != dtype:
             raise ValueError(f"{name} must be {dtype}, is {t.dtype}")
         if t.shape != shape:
             raise ValueError(f"{name} must have shape {tuple(shape)}, has "
                              f"{tuple(t.shape)}")
+        if t.is_contiguous():
+            return
         if contiguous:
-            if not t.is_contiguous():
-                raise ValueError(f"{name} must be contiguous")
-        elif t.numel() and (t.shape[1] > 1 and t.stride(1) != 1 or
-                            t.shape[0] > 1 and t.stride(0) < t.shape[1]):
+            raise ValueError(f"{name} must be contiguous")
+        if t.numel() and (t.shape[1] > 1 and t.stride(1) != 1 or
+                          t.shape[0] > 1 and t.stride(0) < t.shape[1]):
             raise ValueError(f"{name} must have contiguous rows")
 
     @staticmethod
     def _stride(t):
-        return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+        rows, cols = t.shape
+        return max(t.stride(0), cols) if rows > 1 else cols
 
     def _stream(self, stream):
-        if stream is not None:
-            return stream.cuda_stream
-        import torch
-        return torch.cuda.current_stream(self.device).cuda_stream
+        if stream is None:
+            stream = _torch().cuda.current_stream(self.device)
+        return stream.cuda_stream
 
     def _projection(self, batch, weight, a, b, bias):
         if batch._ctx is not self:
             raise ValueError("the batch is closed or of another context")
         if weight.dim() != 2:
             raise ValueError("weight must be [n_out, n_in]")
-        import torch
         dt = self._torch_dtype()
         n, k = weight.shape
         self._tensor("weight", weight, (n, k), dt, contiguous=False)
         if (a is None) != (b is None):
             raise ValueError("a and b come together")
+        p = Projection(k, n, weight.data_ptr(), self._stride(weight))
         if a is not None:
             self._tensor("a", a, (batch.n_adapters, batch.rank, k), dt)
             self._tensor("b", b, (batch.n_adapters, n, batch.rank), dt)
+            p.a, p.b = a.data_ptr(), b.data_ptr()
         if bias is not None:
-            self._tensor("bias", bias, (n,), torch.float32)
-        return Projection(k, n, weight.data_ptr(), self._stride(weight),
-                          None if bias is None else bias.data_ptr(),
-                          None if a is None else a.data_ptr(),
-                          None if b is None else b.data_ptr())
+            self._tensor("bias", bias, (n,), _torch().float32)
+            p.bias = bias.data_ptr()
+        return p, n, k, dt
 
     def adapt(self, batch, x, weight, a=None, b=None, bias=None, out=None,
               stream=None):
@@ -556,20 +567,16 @@ class Context:
         request's adapter: x [rows, n_in], weight [n_out, n_in], a
         [adapters, rank, n_in], b [adapters, n_out, rank] of the context's
         type, bias float32. x, weight and out may have a row stride."""
-        import torch
-        p = self._projection(batch, weight, a, b, bias)
-        dt = weight.dtype
-        self._tensor("x", x, (batch.rows, p.n_in), dt, contiguous=False)
+        p, n, k, dt = self._projection(batch, weight, a, b, bias)
+        rows = batch.rows
+        self._tensor("x", x, (rows, k), dt, contiguous=False)
         if out is None:
-            out = torch.empty((batch.rows, p.n_out), dtype=dt,
-                              device=x.device)
+            out = x.new_empty((rows, n))
         else:
-            self._tensor("out", out, (batch.rows, p.n_out), dt,
-                         contiguous=False)
+            self._tensor("out", out, (rows, n), dt, contiguous=False)
         self._check(self._lib.gemel_adapt(
-            self._h, batch.id, ctypes.byref(p), x.data_ptr(),
-            self._stride(x), out.data_ptr(), self._stride(out),
-            self._stream(stream)))
+            self._h, batch.id, p, x.data_ptr(), self._stride(x),
+            out.data_ptr(), self._stride(out), self._stream(stream)))
         return out
 
     def adapt_backward(self, batch, dy, x, weight, a=None, b=None,
@@ -578,16 +585,14 @@ class Context:
         """Gradients of adapt for dy [rows, n_out], as a dict of those in
         `needs`: "x" in the context's type; "weight", "bias", "a" and "b"
         in float32. outputs: tensors to write, by name (others are made)."""
-        import torch
-        p = self._projection(batch, weight, a, b, None)
-        dt, f32 = weight.dtype, torch.float32
-        self._tensor("x", x, (batch.rows, p.n_in), dt, contiguous=False)
-        self._tensor("dy", dy, (batch.rows, p.n_out), dt, contiguous=False)
-        shapes = {"x": (batch.rows, p.n_in), "weight": (p.n_out, p.n_in),
-                  "bias": (p.n_out,),
-                  "a": (batch.n_adapters, batch.rank, p.n_in),
-                  "b": (batch.n_adapters, p.n_out, batch.rank)}
-        res = {}
+        p, n, k, dt = self._projection(batch, weight, a, b, None)
+        f32, rows = _torch().float32, batch.rows
+        self._tensor("x", x, (rows, k), dt, contiguous=False)
+        self._tensor("dy", dy, (rows, n), dt, contiguous=False)
+        shapes = {"x": (rows, k), "weight": (n, k), "bias": (n,),
+                  "a": (batch.n_adapters, batch.rank, k),
+                  "b": (batch.n_adapters, n, batch.rank)}
+        res, ptr = {}, {}
         for name in needs:
             if name not in shapes:
                 raise ValueError(f"unknown gradient {name!r}")
@@ -596,17 +601,16 @@ class Context:
                     raise ValueError(f"gradient {name!r} without adapters")
                 continue
             want = dt if name == "x" else f32
-            t = (outputs or {}).get(name)
+            t = outputs.get(name) if outputs else None
             if t is None:
-                t = torch.empty(shapes[name], dtype=want, device=x.device)
+                t = x.new_empty(shapes[name], dtype=want)
             else:
                 self._tensor(f"outputs[{name!r}]", t, shapes[name], want,
                              contiguous=name != "x")
-            res[name] = t
-        ptr = {k: t.data_ptr() for k, t in res.items()}
+            res[name], ptr[name] = t, t.data_ptr()
         self._check(self._lib.gemel_adapt_backward(
-            self._h, batch.id, ctypes.byref(p), x.data_ptr(),
-            self._stride(x), dy.data_ptr(), self._stride(dy), ptr.get("x"),
+            self._h, batch.id, p, x.data_ptr(), self._stride(x),
+            dy.data_ptr(), self._stride(dy), ptr.get("x"),
             self._stride(res["x"]) if "x" in res else 0, ptr.get("weight"),
             ptr.get("bias"), ptr.get("a"), ptr.get("b"),
             self._stream(stream)))
@@ -621,12 +625,11 @@ class Context:
     def orthogonalize(self, g, steps=5, out=None, stream=None):
         """Newton-Schulz orthogonalisation of [rows, cols] or [count, rows,
         cols] contiguous matrices of the context's type."""
-        import torch
         count, rows, cols = self._matrices(g)
         dt = self._torch_dtype()
         self._tensor("g", g, g.shape, dt)
         if out is None:
-            out = torch.empty_like(g)
+            out = g.new_empty(g.shape)
         else:
             self._tensor("out", out, g.shape, dt)
         self._check(self._lib.gemel_orthogonalize(
@@ -640,13 +643,12 @@ class Context:
         """One optimiser step, in place, of float32 matrices w [rows, cols]
         or [count, rows, cols] with their momentum buffer and gradient; copy
         (bf16 contexts) receives the new w in bf16."""
-        import torch
         count, rows, cols = self._matrices(w)
         for name, t in (("w", w), ("momentum_buffer", momentum_buffer),
                         ("g", g)):
-            self._tensor(name, t, w.shape, torch.float32)
+            self._tensor(name, t, w.shape, _torch().float32)
         if copy is not None:
-            self._tensor("copy", copy, w.shape, torch.bfloat16)
+            self._tensor("copy", copy, w.shape, _torch().bfloat16)
         self._check(self._lib.gemel_muon_step(
             self._h, count, rows, cols, w.data_ptr(),
             momentum_buffer.data_ptr(), g.data_ptr(),
