@@ -1,0 +1,349 @@
+// Layouts and sums around the products of the operators: small pieces of
+// work, several of which share a launch (alone each would cost the launch
+// more than its work).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "op_args.h"
+
+namespace gemel {
+
+namespace {
+
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ float bf_up(u16 h) { return __uint_as_float((uint32_t)h << 16); }
+__device__ __forceinline__ u16 half_down(float f) { return __builtin_bit_cast(u16, (_Float16)f); }
+__device__ __forceinline__ float half_up(u16 h) { return (float)__builtin_bit_cast(_Float16, h); }
+
+// The exponent that brings a largest magnitude, given as bits, into
+// [2^14, 2^15); 0 where it is zero or not finite.
+__device__ __forceinline__ int plane_exp(unsigned bits) {
+    const float mx = __uint_as_float(bits);
+    if (bits == 0u || bits >= 0x7f800000u) return 0;
+    return 14 - ilogbf(mx);
+}
+__device__ __forceinline__ void split_put(u16 *hi, u16 *lo, int64_t at, float v, int e) {
+    const float s = ldexpf(v, e);
+    const u16 h = half_down(s);
+    hi[at] = h;
+    // the rest of a value that is not finite would be NaN; the sum has it already
+    lo[at] = isfinite(s) ? half_down(s - half_up(h)) : (u16)0;
+}
+__device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
+
+// 4 consecutive float32 (`left` of them there; others zero)
+__device__ __forceinline__ f32x4 load4(const float *p, int left, int vec) {
+    if (vec && left >= 4) return *(const f32x4 *)p;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) v[i] = p[i];
+    return v;
+}
+
+constexpr int PAD_ITEMS = 2048;    // elements of a block of JOB_PAD
+constexpr int CHUNK_COLS = 64;     // columns of a block of JOB_CHUNKS
+
+template <typename E>
+__device__ __forceinline__ void pad(const Job &j, int block) {
+    const int64_t n = (int64_t)j.rows * j.ldo, end = min(n, (int64_t)(block + 1) * PAD_ITEMS);
+    for (int64_t i = (int64_t)block * PAD_ITEMS + threadIdx.x; i < end; i += 256) {
+        const int64_t r = i / j.ldo, c = i - r * j.ldo;
+        ((E *)j.out)[i] = c < j.cols ? ((const E *)j.in)[(j.perm ? j.perm[r] : r) * j.ldi + c] : (E)0;
+    }
+}
+
+// a wave per row
+__device__ __forceinline__ void split(const Job &j, int block) {
+    const int r = block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+    if (r >= j.rows) return;
+    const float *in = (const float *)j.in + (int64_t)(j.perm ? j.perm[r] : r) * j.ldi;
+    unsigned m = 0;
+#pragma unroll 4
+    for (int c = lane * 4; c < j.cols; c += 256) {
+        const f32x4 v = load4(in + c, j.cols - c, j.vec);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) m = max(m, magnitude(v[i]));
+    }
+    for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    const int e = plane_exp(m);
+    if (lane == 0) j.e[r] = e;
+    u16 *hi = (u16 *)j.out + r * j.ldo, *lo = j.lo + r * j.ldo;
+#pragma unroll 4
+    for (int c = lane * 4; c < j.ldo; c += 256) {
+        const f32x4 v = load4(in + c, j.cols - c, j.vec);
+        u16 h[4], l[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) split_put(h, l, i, v[i], e);
+        *(ushort4 *)(hi + c) = make_ushort4(h[0], h[1], h[2], h[3]);
+        *(ushort4 *)(lo + c) = make_ushort4(l[0], l[1], l[2], l[3]);
+    }
+}
+
+// 64 x 64 tiles through LDS, which holds the tile transposed. E: u16 (copied)
+// or float (split).
+template <typename E>
+__device__ __forceinline__ void turn(const Job &j, int block, unsigned char *lds) {
+    constexpr bool F = sizeof(E) == 4;
+    constexpr int Q = 16 / sizeof(E), PITCH = F ? 65 : 66;
+    E *const tile = (E *)lds;                             // [column][row]
+    float *const part = (float *)(lds + 64 * PITCH * sizeof(E) + 8);   // [4][64]
+    const int tid = threadIdx.x, across = (j.cols + 63) / 64;
+    const int r0 = block / across * 64, c0 = block % across * 64;
+    for (int i = tid; i < 64 * 64 / Q; i += 256) {
+        const int r = i / (64 / Q), c = i % (64 / Q) * Q;
+        union {
+            uint4 v;
+            E e[Q];
+        } x;
+        const E *in = (const E *)j.in + (int64_t)(r0 + r) * j.ldi + c0 + c;
+        if (r0 + r < j.rows && j.vec && c0 + c + Q <= j.cols) {
+            x.v = *(const uint4 *)in;
+        } else {
+#pragma unroll
+            for (int k = 0; k < Q; ++k) x.e[k] = r0 + r < j.rows && c0 + c + k < j.cols ? in[k] : (E)0;
+        }
+#pragma unroll
+        for (int k = 0; k < Q; ++k) tile[(c + k) * PITCH + r] = x.e[k];
+    }
+    int *const es = (int *)(part + 256);
+    if (F && tid < 64 && c0 + tid < j.cols) {
+        unsigned m = 0;
+        for (int p = 0; p < j.parts; ++p) m = max(m, j.max[(int64_t)p * j.cols + c0 + tid]);
+        es[tid] = plane_exp(m);
+        if (r0 == 0) j.e[c0 + tid] = es[tid];
+    }
+    __syncthreads();
+    for (int i = tid; i < 64 * 16; i += 256) {
+        const int c = i >> 4, r = (i & 15) * 4;
+        if (c0 + c >= j.cols || r0 + r >= j.ldo) continue;
+        const E *t = tile + c * PITCH + r;
+        const int64_t at = (int64_t)(c0 + c) * j.ldo + r0 + r;
+        if constexpr (F) {
+            u16 h[4], l[4];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) split_put(h, l, k, t[k], es[c]);
+            *(ushort4 *)((u16 *)j.out + at) = make_ushort4(h[0], h[1], h[2], h[3]);
+            *(ushort4 *)(j.lo + at) = make_ushort4(l[0], l[1], l[2], l[3]);
+        } else {
+            *(ushort4 *)((u16 *)j.out + at) = make_ushort4(t[0], t[1], t[2], t[3]);
+        }
+    }
+    if (j.sum) {
+        const int c = tid & 63, q = tid >> 6;
+        float v = 0.f;
+        for (int r = q * 16; r < q * 16 + 16; ++r) v += F ? (float)tile[c * PITCH + r] : bf_up((u16)tile[c * PITCH + r]);
+        part[q * 64 + c] = v;
+        __syncthreads();
+        if (q == 0 && c0 + c < j.cols)
+            j.sum[(int64_t)(block / across) * j.cols + c0 + c] = part[c] + part[64 + c] + part[128 + c] + part[192 + c];
+    }
+}
+
+// [parts][cols] of column maxima (float32) or sums: 64 columns per block, 16
+// threads across, 16 groups of rows.
+template <bool MAX>
+__device__ __forceinline__ void columns(const Job &j, int block, unsigned char *lds) {
+    f32x4 *const part = (f32x4 *)lds;   // [16][16]
+    const int across = (j.cols + 63) / 64, p = block / across, c = block % across * 64 + (threadIdx.x & 15) * 4;
+    const int g = threadIdx.x >> 4, left = j.cols - c;
+    const int r0 = (int)((int64_t)j.rows * p / j.parts), r1 = (int)((int64_t)j.rows * (p + 1) / j.parts);
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int r = r0 + g; r < r1; r += 16) {
+        f32x4 x = {0.f, 0.f, 0.f, 0.f};
+        if (left > 0) {
+            if (j.f32) {
+                x = load4((const float *)j.in + r * j.ldi + c, left, j.vec);
+            } else {
+                const u16 *in = (const u16 *)j.in + r * j.ldi + c;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (i < left) x[i] = bf_up(in[i]);
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            v[i] = MAX ? __uint_as_float(max(__float_as_uint(v[i]), magnitude(x[i]))) : v[i] + x[i];
+    }
+    part[g * 16 + (threadIdx.x & 15)] = v;
+    __syncthreads();
+    if (g) return;
+    for (int k = 1; k < 16; ++k) {
+        const f32x4 x = part[k * 16 + threadIdx.x];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = MAX ? __uint_as_float(max(__float_as_uint(v[i]), __float_as_uint(x[i]))) : v[i] + x[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) {
+            if (MAX)
+                j.max[(int64_t)p * j.cols + c + i] = __float_as_uint(v[i]);
+            else
+                j.sum[(int64_t)p * j.cols + c + i] = v[i];
+        }
+}
+
+// 64 columns per block, 4 groups of parts
+__device__ __forceinline__ void coladd(const Job &j, int block, unsigned char *lds) {
+    float *const part = (float *)lds;
+    const int c = block * 64 + (threadIdx.x & 63), g = threadIdx.x >> 6;
+    float v = 0.f;
+    if (c < j.cols) {
+#pragma unroll 8
+        for (int p = g; p < j.parts; p += 4) v += j.sum[(int64_t)p * j.cols + c];
+    }
+    part[threadIdx.x] = v;
+    __syncthreads();
+    if (g == 0 && c < j.cols)
+        ((float *)j.out)[c] = part[threadIdx.x] + part[64 + threadIdx.x] + part[128 + threadIdx.x] + part[192 + threadIdx.x];
+}
+
+// 64 columns of a run per block
+__device__ __forceinline__ void pack(const Job &j, int block) {
+    const int across = ((int)(j.by_rank ? j.ldo : j.cols) + 63) / 64, u = block / across, c0 = block % across * 64;
+    const int rank = j.run_rank[u];
+    const int64_t in = (int64_t)j.run_id[u] * j.cols * j.R;
+    for (int i = threadIdx.x; i < 64 * j.rp; i += 256) {
+        // neighbours along the input's rows
+        const int r = j.in_rc ? i >> 6 : i % j.rp, c = c0 + (j.in_rc ? i & 63 : i / j.rp);
+        const bool there = r < rank && c < j.cols;
+        const int64_t at = in + (j.in_rc ? (int64_t)r * j.cols + c : (int64_t)c * j.R + r);
+        if (j.by_rank) {
+            if (c >= j.ldo) continue;
+            const int64_t to = ((int64_t)u * j.rp + r) * j.ldo + c;
+            if (j.f32)
+                ((float *)j.out)[to] = there ? ((const float *)j.in)[at] : 0.f;
+            else
+                ((u16 *)j.out)[to] = there ? ((const u16 *)j.in)[at] : (u16)0;
+        } else if (c < j.cols) {
+            u16 *out = (u16 *)j.out + ((int64_t)u * j.cols + c) * 2 * j.rp + r;
+            out[0] = out[j.rp] = there ? ((const u16 *)j.in)[at] : (u16)0;
+        }
+    }
+}
+
+// 64 columns of an adapter per block, 32 rank indices at a time
+__device__ __forceinline__ void chunks(const Job &j, int block, unsigned char *lds) {
+    float *const tile = (float *)lds;   // [32][65]
+    const int across = (j.cols + CHUNK_COLS - 1) / CHUNK_COLS, ad = block / across, c0 = block % across * CHUNK_COLS;
+    const int u = j.run_of[ad], rank = u < 0 ? 0 : j.run_rank[u];
+    const int k0 = u < 0 ? 0 : j.chunk_first[u], k1 = u < 0 ? 0 : j.chunk_first[u + 1];
+    float *out = (float *)j.out + (int64_t)ad * j.R * j.cols;
+    for (int r0 = 0; r0 < j.R; r0 += 32) {
+        for (int i = threadIdx.x; i < 32 * 64; i += 256) {
+            const int r = r0 + (i >> 6), c = c0 + (i & 63);
+            float v = 0.f;
+            if (r < rank && c < j.cols) {
+#pragma unroll 4
+                for (int k = k0; k < k1; ++k) v += j.sum[((int64_t)k * j.rp + r) * j.cols + c];
+            }
+            if (j.turned)
+                tile[(i >> 6) * 65 + (i & 63)] = v;
+            else if (r < j.R && c < j.cols)
+                out[(int64_t)r * j.cols + c] = v;
+        }
+        if (!j.turned) continue;
+        __syncthreads();
+        for (int i = threadIdx.x; i < 64 * 32; i += 256) {
+            const int c = i >> 5, r = i & 31;
+            if (c0 + c < j.cols && r0 + r < j.R) out[(int64_t)(c0 + c) * j.R + r0 + r] = tile[r * 65 + c];
+        }
+        __syncthreads();
+    }
+}
+
+__global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
+    __shared__ __attribute__((aligned(16))) unsigned char lds[64 * 65 * 4 + 16 + 1024 + 256];
+    // (a uniform index into the argument block where it lies)
+    const Jobs &all = *(const Jobs *)__builtin_amdgcn_kernarg_segment_ptr();
+    int i = 0;
+    while (i + 1 < all.n && (int)blockIdx.x >= all.first[i + 1]) ++i;
+    const Job &j = all.job[i];
+    const int block = (int)blockIdx.x - all.first[i];
+    switch (j.kind) {
+        case JOB_PAD:
+            if (j.f32)
+                pad<uint32_t>(j, block);
+            else
+                pad<u16>(j, block);
+            break;
+        case JOB_SPLIT: split(j, block); break;
+        case JOB_TURN:
+            if (j.f32)
+                turn<float>(j, block, lds);
+            else
+                turn<u16>(j, block, lds);
+            break;
+        case JOB_COLMAX: columns<true>(j, block, lds); break;
+        case JOB_COLSUM: columns<false>(j, block, lds); break;
+        case JOB_COLADD: coladd(j, block, lds); break;
+        case JOB_PACK: pack(j, block); break;
+        case JOB_CHUNKS: chunks(j, block, lds); break;
+    }
+}
+
+}  // namespace
+
+bool add_job(Jobs &all, const Job &in) {
+    if (all.n >= MAX_JOBS) return false;
+    Job &j = all.job[all.n];
+    j = in;
+    const int64_t across = ((int64_t)j.cols + 63) / 64;
+    int64_t blocks = 0;
+    bool ok = j.cols > 0;
+    switch (j.kind) {
+        case JOB_PAD:
+            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.cols;
+            blocks = ((int64_t)j.rows * j.ldo + PAD_ITEMS - 1) / PAD_ITEMS;
+            break;
+        case JOB_SPLIT:
+            ok = ok && j.in && j.out && j.lo && j.e && j.rows > 0 && j.ldo >= j.cols && j.ldo % 4 == 0;
+            blocks = ((int64_t)j.rows + 3) / 4;
+            break;
+        case JOB_TURN:
+            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.rows && j.ldo % 4 == 0 &&
+                 (!j.f32 || (j.lo && j.e && j.max && j.parts > 0));
+            blocks = across * ((j.ldo + 63) / 64);
+            ok = ok && (!j.sum || (j.ldo + 63) / 64 == (j.rows + 63) / 64);
+            break;
+        case JOB_COLMAX:
+            ok = ok && j.in && j.max && j.rows > 0 && j.parts > 0 && j.f32;
+            blocks = across * j.parts;
+            break;
+        case JOB_COLSUM:
+            ok = ok && j.in && j.sum && j.rows > 0 && j.parts > 0;
+            blocks = across * j.parts;
+            break;
+        case JOB_COLADD:
+            ok = ok && j.sum && j.out && j.parts > 0;
+            blocks = across;
+            break;
+        case JOB_PACK:
+            ok = ok && j.in && j.out && j.run_id && j.run_rank && j.R > 0 && j.rp >= j.R && j.n > 0 &&
+                 (j.by_rank ? j.ldo >= j.cols : !j.f32);
+            blocks = (j.by_rank ? (j.ldo + 63) / 64 : across) * j.n;
+            break;
+        case JOB_CHUNKS:
+            ok = ok && j.sum && j.out && j.run_of && j.run_rank && j.chunk_first && j.R > 0 && j.rp >= j.R && j.n > 0;
+            blocks = across * j.n;
+            break;
+        default: ok = false;
+    }
+    if (!ok || blocks < 1 || blocks + all.blocks > 0x7fffff00) return false;
+    j.blocks = (int)blocks;
+    all.first[all.n] = all.blocks;
+    all.blocks += j.blocks;
+    all.first[++all.n] = all.blocks;
+    return true;
+}
+
+hipError_t launch_jobs(const Jobs &j, hipStream_t s) {
+    if (j.n == 0) return hipSuccess;
+    void *p[] = {const_cast<Jobs *>(&j)};
+    return hipLaunchKernel(reinterpret_cast<const void *>(&jobs_kernel), dim3((unsigned)j.blocks), dim3(256), p, 0, s);
+}
+
+}  // namespace gemel

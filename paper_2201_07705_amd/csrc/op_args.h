@@ -99,7 +99,7 @@ struct BatchTables {
     const int *run_rank;   // [runs]
     const float *run_scale;// [runs]
     const int *first_run;  // [ceil(rows / 64) + 1]
-    const int *items;      // [n_items][3]: run, first position, positions (<= 16)
+    const int *items;      // [n_items][3]: run, first position, positions (<= 16, or 32 with more than ROWS_MAX rows)
     const int *chunks;     // [n_chunks][3]: run, first position, positions
     const int *chunk_first;// [runs + 1] chunks of a run
     const int *run_of;     // [adapters] run or -1
@@ -140,66 +140,67 @@ struct ShrinkArgs {
     float *t;              // [rows][rp]
     BatchTables b;
 };
-hipError_t launch_shrink(const ShrinkArgs &a, hipStream_t s);
-
-// Adapter halves per run, in [adapters][C][R] (or [R][C]): out[run][C][2 rp]
-// with each row's ranks twice (bf16), or by_rank: out[run][rp][ldc]. Rank
-// indices from the run's rank on are zeros, and so are columns beyond C.
-struct PackRankArgs {
-    const void *in;
-    void *out;
-    int in_rc, by_rank, f32, C, R, rp;
-    int64_t ldc;
-    BatchTables b;
-};
-hipError_t launch_pack_rank(const PackRankArgs &a, hipStream_t s);
+// One or two thin products (of one batch) in a launch.
+hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s);
 
 // part[chunk][r][c] = sum over the chunk's positions of p[pos][r] * q[perm[pos]][c]
-// and out[adapter] = sum over its chunks ([R][C], or [C][R] transposed)
 struct OuterArgs {
     const float *p;        // [rows][rp]
     const void *q;
     int64_t ldq;
-    int f32, C, rp, transposed;
+    int f32, C, rp, vq;    // vq: whole 16-byte chunks of q's rows may be loaded at once
     float *part;           // [n_chunks][rp][C]
-    float *out;
     BatchTables b;
 };
-hipError_t launch_outer(const OuterArgs &a, hipStream_t s);
+hipError_t launch_outer(const OuterArgs *a, int n, hipStream_t s);
 
-// Column sums of [rows][cols].
-struct ColsumArgs {
-    const void *in;
-    int64_t ld;
-    int f32, rows, cols, parts;
-    float *part;           // [parts][cols]
-    float *out;
+// Small pieces of work around the products, several in one launch. Blocks of
+// one job do not depend on those of another.
+enum JobKind {
+    // out[r][c], c < ldo: rows (perm[r]) of `in` copied, zeros from cols on
+    JOB_PAD,
+    // float32 rows (perm[r]) as two float16 planes of in * 2^e, one exponent
+    // per row (its largest value lands in [2^14, 2^15)): out, lo, e
+    JOB_SPLIT,
+    // out[c][r], r < ldo: the transpose, zeros from rows on; float32 as
+    // planes with one exponent per output row, from the maxima of
+    // JOB_COLMAX. sum: NULL, or [ceil(rows / 64)][cols] sums of 64 rows
+    JOB_TURN,
+    JOB_COLMAX,            // max [parts][cols]: largest magnitudes (as bits)
+    JOB_COLSUM,            // sum [parts][cols]
+    JOB_COLADD,            // out[c] = sum over parts of sum[part][c]
+    // adapter halves per run, in [adapters][C][R] (or in_rc [R][C]):
+    // out[run][C][2 rp] with each row's ranks twice (bf16), or by_rank:
+    // out[run][rp][ldo]. Rank indices from the run's rank on are zeros, and
+    // so are columns beyond C
+    JOB_PACK,
+    // out[adapter] = sum over its chunks of part [chunk][rp][C], as [R][C] or
+    // (turned) [C][R]; zeros for adapters without rows, and from an
+    // adapter's rank on
+    JOB_CHUNKS
 };
-hipError_t launch_colsum(const ColsumArgs &a, hipStream_t s);
-
-// Copies into zero-padded rows: out[r][c] for c < ldo (transposed:
-// out[c][r] for r < ldo).
-struct PadArgs {
+struct Job {
+    int kind, blocks, f32, rows, cols, parts;
     const void *in;
     void *out;
+    u16 *lo;
+    int *e;
+    unsigned *max;
+    float *sum;
     int64_t ldi, ldo;
-    int rows, cols, transposed, f32;
-    const int *perm;       // not transposed: input row of output row, or null
+    const int *perm;
+    int vec;               // whole 16-byte chunks of the input may be loaded at once
+    int in_rc, by_rank, turned, R, rp, n;   // PACK: n runs, CHUNKS: n adapters; columns in cols
+    const int *run_id, *run_rank, *run_of, *chunk_first;
 };
-hipError_t launch_pad(const PadArgs &a, hipStream_t s);
-
-// float32 rows as two float16 planes of in * 2^e, one exponent per row of
-// the output (the row's largest value lands in [2^14, 2^15)).
-struct SplitArgs {
-    const float *in;
-    u16 *hi, *lo;
-    int *e;                // [output rows]
-    unsigned *colmax;      // transposed: [cols] scratch
-    int64_t ldi, ldo;
-    int rows, cols, transposed;
-    const int *perm;       // not transposed: input row of output row, or null
+constexpr int MAX_JOBS = 6;
+struct Jobs {
+    int n = 0, blocks = 0;
+    int first[MAX_JOBS + 1] = {};
+    Job job[MAX_JOBS];
 };
-hipError_t launch_split(const SplitArgs &a, hipStream_t s);
+bool add_job(Jobs &j, const Job &job);   // sets its blocks; false: not valid
+hipError_t launch_jobs(const Jobs &j, hipStream_t s);
 
 // ---- orthogonalised updates ----
 constexpr double COEF_A = 3.4445, COEF_B = -4.7750, COEF_C = 2.0315;

@@ -247,8 +247,9 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
         run_id.push_back(a);
         run_rank.push_back(ranks ? ranks[a] : max_rank);
         run_scale.push_back(scales ? scales[a] : 1.f);
-        for (int p = 0; p < n; p += 16)
-            for (int v : {u, p0 + p, std::min(16, n - p)}) items.push_back(v);
+        const int per_item = rows > ROWS_MAX ? 32 : 16;
+        for (int p = 0; p < n; p += per_item)
+            for (int v : {u, p0 + p, std::min(per_item, n - p)}) items.push_back(v);
         chunk_first.push_back((int)chunks.size() / 3);
         for (int p = 0; p < n; p += per_chunk)
             for (int v : {u, p0 + p, std::min(per_chunk, n - p)}) chunks.push_back(v);
@@ -355,9 +356,79 @@ gemel_status check_rows(gemel_ctx *ctx, const char *what, const void *p, int64_t
     return GEMEL_OK;
 }
 
-// The adapted product out[row] = in[row] * Wrows^T + low-rank part, where
-// `in` has K columns and the N rows of the other operand are at w (for
-// gradients its transposed copy).
+// ---- jobs around the products ----
+
+Job job(int kind, const void *in, int64_t ldi, int rows, int cols, bool f32) {
+    Job j{};
+    j.kind = kind;
+    j.in = in;
+    j.ldi = ldi;
+    j.rows = rows;
+    j.cols = cols;
+    j.f32 = f32;
+    j.vec = (uintptr_t)in % 16 == 0 && ldi % (f32 ? 4 : 8) == 0;
+    return j;
+}
+
+// A 16-bit copy of an operand: bf16 rows padded, float32 as planes.
+struct Copy {
+    size_t o = 0, o_lo = 0, o_e = 0, o_max = 0;
+    int64_t ld = 0;
+    int parts = 0;
+};
+// `rows` rows of `cols` in the copy
+Copy plan_copy(Call &c, int64_t rows, int64_t cols, bool f32, bool turned) {
+    Copy p;
+    p.ld = op_round_up(cols, 64);
+    p.o = c.lay.take(rows * p.ld, 2);
+    if (f32) {
+        p.o_lo = c.lay.take(rows * p.ld, 2);
+        p.o_e = c.lay.take(rows, 4);
+        // column maxima by stretches of the input's rows
+        p.parts = (int)std::min<int64_t>(32, (cols + 63) / 64);
+        if (turned) p.o_max = c.lay.take(p.parts * rows, 4);
+    }
+    return p;
+}
+// The jobs that fill it from `in` (rows ldi apart; turned: the copy is its
+// transpose).
+bool add_copy(Call &c, const Copy &p, const void *in, int64_t ldi, int rows, int cols, bool f32, bool turned, const int *perm,
+              float *sum, Jobs &first, Jobs &second) {
+    Job j = job(turned ? JOB_TURN : f32 ? JOB_SPLIT : JOB_PAD, in, ldi, turned ? cols : rows, turned ? rows : cols, f32);
+    j.out = c.at<u16>(p.o);
+    j.lo = c.at<u16>(p.o_lo);
+    j.e = c.at<int>(p.o_e);
+    j.max = c.at<unsigned>(p.o_max);
+    j.ldo = p.ld;
+    j.parts = p.parts;
+    j.perm = perm;
+    j.sum = sum;
+    if (turned && f32) {
+        Job m = j;
+        m.kind = JOB_COLMAX;
+        if (!add_job(first, m)) return false;
+    }
+    return add_job(second, j);
+}
+
+// The operands of a product: bf16 one, float32 the three pairs of planes.
+void operands(Call &c, MmArgs &m, const Copy &a, const Copy &b) {
+    const u16 *ah = c.at<u16>(a.o), *al = c.at<u16>(a.o_lo), *bh = c.at<u16>(b.o), *bl = c.at<u16>(b.o_lo);
+    // the small products first
+    const u16 *as[3] = {ah, al, ah}, *bs[3] = {bl, bh, bh};
+    for (int i = 0; i < 3; ++i) {
+        m.a[i] = as[i];
+        m.b[i] = bs[i];
+    }
+    m.lda = a.ld;
+    m.ldb = b.ld;
+    m.o.ea = c.at<int>(a.o_e);
+    m.o.eb = c.at<int>(b.o_e);
+    m.o.out_f32 = 1;
+}
+
+// The adapted product out[row] = in[row] * w^T + low-rank part, where `in`
+// has K columns and the N rows of the other operand are at w.
 struct Adapted {
     const void *in;
     int64_t ld_in;
@@ -365,24 +436,23 @@ struct Adapted {
     const void *w;       // [N][K] rows ld_w apart, or (w_t) [K][N]
     int64_t ld_w;
     bool w_t;
-    const void *bank;    // adapter halves with N, for the extension
-    int bank_rc;         // the half lies [rank][N], not [N][rank]
+    const void *bank;    // the adapter half with N
+    int bank_rc;         // it lies [rank][N], not [N][rank]
     const float *bias;
     void *out;
     int64_t ld_out;
-    // the thin product, if it has been laid out
-    u16 *planes = nullptr;
-    float *t = nullptr;
+    u16 *planes = nullptr;   // the thin product (bf16)
+    float *t = nullptr;      // (float32)
     // layout
-    size_t o_in = 0, o_in_lo = 0, o_ein = 0, o_w = 0, o_w_lo = 0, o_ew = 0, o_bank = 0, o_part = 0, o_max = 0;
     bool pad_in = false, pad_w = false;
-    int64_t Kp = 0;
+    Copy c_in, c_w;
+    size_t o_bank = 0;
     MmArgs mm{};
 };
 
-void plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
+// Sizes; returns the floats of partial sums that the product wants.
+int64_t plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
     const int rp = (int)op_round_up(b.rank, 32);
-    p.Kp = op_round_up(p.K, 64);
     MmArgs &m = p.mm;
     m.M = b.rows;
     m.N = p.N;
@@ -392,85 +462,49 @@ void plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
     m.epi = f32 ? EPI_SCALED : EPI_ROWS;
     p.pad_in = f32 || !in_place(p.in, b.rows, p.ld_in, p.K);
     p.pad_w = f32 || p.w_t || !in_place(p.w, p.N, p.ld_w, p.K);
-    m.K = !f32 && p.K % 8 == 0 ? p.K : (int)p.Kp;
+    m.K = !f32 && p.K % 8 == 0 ? p.K : (int)op_round_up(p.K, 64);
     mm_plan(m);
-    if (p.pad_in) p.o_in = c.lay.take(b.rows * p.Kp, 2);
-    if (p.pad_w) p.o_w = c.lay.take(p.N * p.Kp, 2);
-    if (f32) {
-        p.o_in_lo = c.lay.take(b.rows * p.Kp, 2);
-        p.o_w_lo = c.lay.take(p.N * p.Kp, 2);
-        p.o_ein = c.lay.take(b.rows, 4);
-        p.o_ew = c.lay.take(p.N, 4);
-        if (p.w_t) p.o_max = c.lay.take(p.N, 4);
-    }
+    if (p.pad_in) p.c_in = plan_copy(c, b.rows, p.K, f32, false);
+    if (p.pad_w) p.c_w = plan_copy(c, p.N, p.K, f32, p.w_t);
     if (b.runs) p.o_bank = c.lay.take((int64_t)b.runs * op_round_up(p.N, 4) * rp, 4);
-    p.o_part = c.lay.take(partial_floats(m), 4);
+    return partial_floats(m);
 }
 
-gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
+bool add_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, Jobs &first, Jobs &second) {
+    const int rp = (int)op_round_up(b.rank, 32);
+    if (p.pad_in && !add_copy(c, p.c_in, p.in, p.ld_in, b.rows, p.K, f32, false, b.perm, nullptr, first, second)) return false;
+    if (p.pad_w && !add_copy(c, p.c_w, p.w, p.ld_w, p.N, p.K, f32, p.w_t, nullptr, nullptr, first, second)) return false;
+    if (!b.runs) return true;
+    Job k = job(JOB_PACK, p.bank, 0, 0, p.N, f32);
+    k.out = c.at<char>(p.o_bank);
+    k.in_rc = p.bank_rc;
+    k.by_rank = f32;
+    k.R = b.rank;
+    k.rp = rp;
+    k.n = b.runs;
+    k.ldo = op_round_up(p.N, 4);
+    k.run_id = b.run_id;
+    k.run_rank = b.run_rank;
+    return add_job(second, k);
+}
+
+gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, float *partial) {
     gemel_ctx *ctx = c.ctx;
     const int rp = (int)op_round_up(b.rank, 32);
     MmArgs &m = p.mm;
-    const u16 *in = (const u16 *)p.in, *w = (const u16 *)p.w;
-    m.lda = p.ld_in;
-    m.ldb = p.ld_w;
-    m.perm = b.perm;
-    m.perm_rows = b.rows;
-    m.o.perm = b.perm;
     if (f32) {
-        SplitArgs s{};
-        s.in = (const float *)p.in;
-        s.ldi = p.ld_in;
-        s.hi = c.at<u16>(p.o_in);
-        s.lo = c.at<u16>(p.o_in_lo);
-        s.e = c.at<int>(p.o_ein);
-        s.ldo = p.Kp;
-        s.rows = b.rows;
-        s.cols = p.K;
-        s.perm = b.perm;
-        OPCHK(launch_split(s, c.stream), "split");
-        s.in = (const float *)p.w;
-        s.ldi = p.ld_w;
-        s.hi = c.at<u16>(p.o_w);
-        s.lo = c.at<u16>(p.o_w_lo);
-        s.e = c.at<int>(p.o_ew);
-        s.perm = nullptr;
-        s.transposed = p.w_t;
-        s.rows = p.w_t ? p.K : p.N;
-        s.cols = p.w_t ? p.N : p.K;
-        s.colmax = c.at<unsigned>(p.o_max);
-        OPCHK(launch_split(s, c.stream), "split");
-        const u16 *ah = c.at<u16>(p.o_in), *al = c.at<u16>(p.o_in_lo), *bh = c.at<u16>(p.o_w), *bl = c.at<u16>(p.o_w_lo);
-        m.a[0] = ah;
-        m.b[0] = bl;
-        m.a[1] = al;
-        m.b[1] = bh;
-        m.a[2] = ah;
-        m.b[2] = bh;
-        m.lda = m.ldb = p.Kp;
-        m.perm = nullptr;
-        m.o.ea = c.at<int>(p.o_ein);
-        m.o.eb = c.at<int>(p.o_ew);
+        operands(c, m, p.c_in, p.c_w);
         m.o.t = p.t;
         m.o.bx = c.at<float>(p.o_bank);
         m.o.rp = rp;
         m.o.ldbx = op_round_up(p.N, 4);
-        m.o.out_f32 = 1;
     } else {
-        if (p.pad_in) {
-            OPCHK(launch_pad({in, c.at<u16>(p.o_in), p.ld_in, p.Kp, b.rows, p.K, 0, 0, b.perm}, c.stream), "pad");
-            in = c.at<u16>(p.o_in);
-            m.lda = p.Kp;
-            m.perm = nullptr;
-        }
-        if (p.pad_w) {
-            OPCHK(launch_pad({w, c.at<u16>(p.o_w), p.ld_w, p.Kp, p.w_t ? p.K : p.N, p.w_t ? p.N : p.K, p.w_t, 0, nullptr}, c.stream),
-                  "pad");
-            w = c.at<u16>(p.o_w);
-            m.ldb = p.Kp;
-        }
-        m.a[0] = in;
-        m.b[0] = w;
+        m.a[0] = p.pad_in ? c.at<u16>(p.c_in.o) : (const u16 *)p.in;
+        m.b[0] = p.pad_w ? c.at<u16>(p.c_w.o) : (const u16 *)p.w;
+        m.lda = p.pad_in ? p.c_in.ld : p.ld_in;
+        m.ldb = p.pad_w ? p.c_w.ld : p.ld_w;
+        m.perm = p.pad_in ? nullptr : b.perm;   // copies are in the order of positions
+        m.perm_rows = b.rows;
         if (b.runs) {
             m.ext = 2 * rp;
             m.t = p.planes;
@@ -480,12 +514,9 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
     m.runs = b.runs;
     m.run_start = b.run_start;
     m.first_run = b.first_run;
-    if (b.runs) {
-        PackRankArgs k{p.bank, c.at<char>(p.o_bank), p.bank_rc, f32, f32, p.N, b.rank, rp, op_round_up(p.N, 4), b};
-        OPCHK(launch_pack_rank(k, c.stream), "pack");
-    }
     m.zero = (const u16 *)c.st->zero;
-    m.partial = c.at<float>(p.o_part);
+    m.partial = partial;
+    m.o.perm = b.perm;
     m.o.out = p.out;
     m.o.ld = p.ld_out;
     m.o.vec = vec_ok(p.out, p.ld_out, f32);
@@ -503,9 +534,8 @@ gemel_status get_batch(gemel_ctx *ctx, int32_t id, State **st, Batch **b) {
     return GEMEL_OK;
 }
 
-gemel_status shrink(Call &c, const BatchTables &b, bool f32, const void *x, int64_t ldx, int K, const void *a, int64_t lda,
-                    bool by_run, u16 *planes, float *t) {
-    gemel_ctx *ctx = c.ctx;
+ShrinkArgs shrink(const BatchTables &b, bool f32, const void *x, int64_t ldx, int K, const void *a, int64_t lda, bool by_run,
+                  u16 *planes, float *t) {
     ShrinkArgs s{};
     s.x = x;
     s.a = a;
@@ -521,8 +551,7 @@ gemel_status shrink(Call &c, const BatchTables &b, bool f32, const void *x, int6
     s.planes = planes;
     s.t = t;
     s.b = b;
-    OPCHK(launch_shrink(s, c.stream), "thin product");
-    return GEMEL_OK;
+    return s;
 }
 
 // Few rows: k_rows.hip, on copies of the operands that it cannot read in
@@ -547,17 +576,20 @@ gemel_status adapt_rows(Call &c, const BatchTables &b, bool f32, const gemel_pro
     a.ldx = ldx;
     a.w = proj->weight;
     a.ldw = proj->weight_stride;
+    Jobs jobs;
     if (copy_x) {
-        OPCHK(launch_pad({x, c.at<char>(o_x), ldx, Kp, b.rows, (int)K, 0, f32, nullptr}, c.stream), "pad");
-        a.x = c.at<char>(o_x);
-        a.ldx = Kp;
+        Job j = job(JOB_PAD, x, ldx, b.rows, (int)K, f32);
+        a.x = j.out = c.at<char>(o_x);
+        a.ldx = j.ldo = Kp;
+        if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
     }
     if (copy_w) {
-        OPCHK(launch_pad({proj->weight, c.at<char>(o_w), proj->weight_stride, Kp, (int)N, (int)K, 0, f32, nullptr}, c.stream),
-              "pad");
-        a.w = c.at<char>(o_w);
-        a.ldw = Kp;
+        Job j = job(JOB_PAD, proj->weight, proj->weight_stride, (int)N, (int)K, f32);
+        a.w = j.out = c.at<char>(o_w);
+        a.ldw = j.ldo = Kp;
+        if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "weight is too large");
     }
+    OPCHK(launch_jobs(jobs, c.stream), "copies");
     a.a = proj->a;
     a.bank_b = proj->b;
     a.bias = proj->bias;
@@ -611,14 +643,17 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     p.out = y;
     p.ld_out = ldy;
     const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4);
-    plan_adapted(c, b, f32, p);
+    const size_t o_part = c.lay.take(plan_adapted(c, b, f32, p), 4);
     if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
+    Jobs first, second;
+    if (!add_adapted(c, b, f32, p, first, second)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
+    OPCHK(launch_jobs(second, stream), "copies");
     if (b.runs) {
-        p.planes = f32 ? nullptr : c.at<u16>(o_t);
-        p.t = f32 ? c.at<float>(o_t) : nullptr;
-        if (gemel_status s = shrink(c, b, f32, x, ldx, (int)K, proj->a, K, false, p.planes, p.t)) return s;
+        (f32 ? (void *&)p.t : (void *&)p.planes) = c.at<void>(o_t);
+        const ShrinkArgs t = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, p.planes, p.t);
+        OPCHK(launch_shrink(&t, 1, stream), "thin product");
     }
-    return run_adapted(c, b, f32, p);
+    return run_adapted(c, b, f32, p, c.at<float>(o_part));
 }
 
 gemel_status zero_out(Call &c, float *p, int64_t n) {
@@ -665,13 +700,11 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         return zero_out(c, dbias, N);
     }
     const int rp = (int)op_round_up(b.rank, 32);
-    const int64_t Mp = op_round_up(M, 64), Np = op_round_up(N, 64);
+    const int64_t Np = op_round_up(N, 64);
     const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
-    const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u ? M * rp : 0, 4),
+    const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u && !f32 ? M * rp : 0, 4),
                  o_t = c.lay.take(need_t ? M * rp : 0, 4), o_bt = c.lay.take(need_u ? b.runs * rp * Np : 0, e);
-    // the parts below run one after the other in the same stretch
-    const size_t shared = c.lay.bytes;
-    size_t most = shared;
+    int64_t part = 0;
     Adapted p{};
     if (dx) {
         p.in = dy;
@@ -685,122 +718,121 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         p.bank_rc = 1;
         p.out = dx;
         p.ld_out = lddx;
-        plan_adapted(c, b, f32, p);
-        most = std::max(most, c.lay.bytes);
-        c.lay.bytes = shared;
+        part = plan_adapted(c, b, f32, p);
     }
+    // dW = dy^T x, on transposed copies of both
     MmArgs w{};
-    size_t o_x = 0, o_xl = 0, o_ex = 0, o_d = 0, o_dl = 0, o_ed = 0, o_max = 0, o_wp = 0;
+    Copy c_dy, c_x;
     if (dw) {
         w.M = (int)N;
         w.N = (int)K;
-        w.K = (int)Mp;
+        w.K = (int)op_round_up(M, 64);
         w.batch = 1;
         w.nseg = f32 ? 3 : 1;
         w.f16 = f32;
         w.epi = f32 ? EPI_SCALED : EPI_ROWS;
-        w.lda = w.ldb = Mp;
         mm_plan(w);
-        o_x = c.lay.take(K * Mp, 2);
-        o_d = c.lay.take(N * Mp, 2);
-        if (f32) {
-            o_xl = c.lay.take(K * Mp, 2);
-            o_dl = c.lay.take(N * Mp, 2);
-            o_ex = c.lay.take(K, 4);
-            o_ed = c.lay.take(N, 4);
-            o_max = c.lay.take(std::max(K, N), 4);
-        }
-        o_wp = c.lay.take(partial_floats(w), 4);
-        most = std::max(most, c.lay.bytes);
-        c.lay.bytes = shared;
+        c_dy = plan_copy(c, N, M, f32, true);
+        c_x = plan_copy(c, K, M, f32, true);
+        part = std::max(part, partial_floats(w));
     }
-    ColsumArgs cs{dy, lddy, f32, (int)M, (int)N, (int)std::min<int64_t>(256, (M + 31) / 32), nullptr, dbias};
-    const size_t o_cs = c.lay.take(dbias ? cs.parts * N : 0, 4);
-    const size_t o_op = c.lay.take(da || db ? (int64_t)b.n_chunks * rp * std::max(K, N) : 0, 4);
-    c.lay.bytes = std::max(most, c.lay.bytes);
+    // column sums of dy: of 64 rows each where dy is transposed anyway
+    const int sums = (int)(dw ? (M + 63) / 64 : std::min<int64_t>(128, (M + 63) / 64));
+    const size_t o_sum = c.lay.take(dbias ? sums * N : 0, 4);
+    const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * rp * K : 0, 4),
+                 o_db = c.lay.take(db ? (int64_t)b.n_chunks * rp * N : 0, 4), o_part = c.lay.take(part, 4);
     if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
 
-    float *t = need_t ? c.at<float>(o_t) : nullptr, *u = need_u ? c.at<float>(o_u) : nullptr;
-    if (need_t)
-        if (gemel_status s = shrink(c, b, f32, x, ldx, (int)K, proj->a, K, false, nullptr, t)) return s;
-    if (need_u) {
-        PackRankArgs k{proj->b, c.at<char>(o_bt), 0, 1, f32, (int)N, b.rank, rp, Np, b};
-        OPCHK(launch_pack_rank(k, stream), "pack");
-        p.planes = f32 ? nullptr : c.at<u16>(o_up);
-        p.t = f32 ? u : nullptr;
-        if (gemel_status s = shrink(c, b, f32, dy, lddy, (int)N, c.at<char>(o_bt), Np, true, p.planes, u)) return s;
-    }
-    if (dx)
-        if (gemel_status s = run_adapted(c, b, f32, p)) return s;
+    Jobs first, second, last;
+    bool ok = !dx || add_adapted(c, b, f32, p, first, second);
+    float *const sum = dbias ? c.at<float>(o_sum) : nullptr;
     if (dw) {
-        if (f32) {
-            SplitArgs s{};
-            s.transposed = 1;
-            s.rows = (int)M;
-            s.ldo = Mp;
-            s.colmax = c.at<unsigned>(o_max);
-            s.in = (const float *)dy;
-            s.ldi = lddy;
-            s.cols = (int)N;
-            s.hi = c.at<u16>(o_d);
-            s.lo = c.at<u16>(o_dl);
-            s.e = c.at<int>(o_ed);
-            OPCHK(launch_split(s, stream), "split");
-            s.in = (const float *)x;
-            s.ldi = ldx;
-            s.cols = (int)K;
-            s.hi = c.at<u16>(o_x);
-            s.lo = c.at<u16>(o_xl);
-            s.e = c.at<int>(o_ex);
-            OPCHK(launch_split(s, stream), "split");
-            w.a[0] = c.at<u16>(o_d);
-            w.b[0] = c.at<u16>(o_xl);
-            w.a[1] = c.at<u16>(o_dl);
-            w.b[1] = c.at<u16>(o_x);
-            w.a[2] = c.at<u16>(o_d);
-            w.b[2] = c.at<u16>(o_x);
-            w.o.ea = c.at<int>(o_ed);
-            w.o.eb = c.at<int>(o_ex);
-        } else {
-            OPCHK(launch_pad({(const u16 *)dy, c.at<u16>(o_d), lddy, Mp, (int)M, (int)N, 1, 0, nullptr}, stream), "pad");
-            OPCHK(launch_pad({(const u16 *)x, c.at<u16>(o_x), ldx, Mp, (int)M, (int)K, 1, 0, nullptr}, stream), "pad");
-            w.a[0] = c.at<u16>(o_d);
-            w.b[0] = c.at<u16>(o_x);
+        ok = ok && add_copy(c, c_dy, dy, lddy, (int)N, (int)M, f32, true, nullptr, sum, first, second);
+        ok = ok && add_copy(c, c_x, x, ldx, (int)K, (int)M, f32, true, nullptr, nullptr, first, second);
+    } else if (dbias) {
+        Job j = job(JOB_COLSUM, dy, lddy, (int)M, (int)N, f32);
+        j.sum = sum;
+        j.parts = sums;
+        ok = ok && add_job(second, j);
+    }
+    if (need_u) {
+        Job j = job(JOB_PACK, proj->b, 0, 0, (int)N, f32);
+        j.out = c.at<char>(o_bt);
+        j.by_rank = 1;
+        j.R = b.rank;
+        j.rp = rp;
+        j.n = b.runs;
+        j.ldo = Np;
+        j.run_id = b.run_id;
+        j.run_rank = b.run_rank;
+        ok = ok && add_job(second, j);
+    }
+    if (dbias) {
+        Job j = job(JOB_COLADD, nullptr, 0, 0, (int)N, true);
+        j.sum = sum;
+        j.parts = sums;
+        j.out = dbias;
+        ok = ok && add_job(last, j);
+    }
+    float *const t = need_t ? c.at<float>(o_t) : nullptr, *const u = need_u ? c.at<float>(o_u) : nullptr;
+    OuterArgs outer[2];
+    int n_outer = 0;
+    auto adapter_gradient = [&](const float *left, const void *right, int64_t ld, int64_t C, size_t o_sums, float *out, int turned) {
+        OuterArgs o{};
+        o.p = left;
+        o.q = right;
+        o.ldq = ld;
+        o.f32 = f32;
+        o.C = (int)C;
+        o.rp = rp;
+        o.vq = (uintptr_t)right % 16 == 0 && ld % (f32 ? 4 : 8) == 0;
+        o.part = c.at<float>(o_sums);
+        o.b = b;
+        outer[n_outer++] = o;
+        Job j = job(JOB_CHUNKS, nullptr, 0, 0, (int)C, true);
+        j.sum = o.part;
+        j.out = out;
+        j.turned = turned;
+        j.R = b.rank;
+        j.rp = rp;
+        j.n = b.adapters;
+        j.run_of = b.run_of;
+        j.run_rank = b.run_rank;
+        j.chunk_first = b.chunk_first;
+        ok = ok && add_job(last, j);
+    };
+    if (da) adapter_gradient(u, x, ldx, K, o_da, da, 0);
+    if (db) adapter_gradient(t, dy, lddy, N, o_db, db, 1);
+    if (!ok) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
+
+    OPCHK(launch_jobs(first, stream), "column maxima");
+    OPCHK(launch_jobs(second, stream), "copies");
+    ShrinkArgs thin[2];
+    int n_thin = 0;
+    if (need_u) {
+        p.planes = f32 ? nullptr : c.at<u16>(o_up);
+        p.t = u;
+        thin[n_thin++] = shrink(b, f32, dy, lddy, (int)N, c.at<char>(o_bt), Np, true, dx ? p.planes : nullptr, u);
+    }
+    if (need_t) thin[n_thin++] = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, nullptr, t);
+    if (n_thin) OPCHK(launch_shrink(thin, n_thin, stream), "thin products");
+    if (dx)
+        if (gemel_status s = run_adapted(c, b, f32, p, c.at<float>(o_part))) return s;
+    if (dw) {
+        operands(c, w, c_dy, c_x);
+        if (!f32) {
+            w.a[0] = c.at<u16>(c_dy.o);
+            w.b[0] = c.at<u16>(c_x.o);
         }
         w.zero = (const u16 *)st->zero;
-        w.partial = c.at<float>(o_wp);
+        w.partial = c.at<float>(o_part);
         w.o.out = dw;
         w.o.ld = K;
-        w.o.out_f32 = 1;
         w.o.vec = vec_ok(dw, K, 1);
         OPCHK(launch_mm(w, stream), "product");
     }
-    if (dbias) {
-        cs.part = c.at<float>(o_cs);
-        OPCHK(launch_colsum(cs, stream), "column sums");
-    }
-    OuterArgs o{};
-    o.f32 = f32;
-    o.rp = rp;
-    o.part = c.at<float>(o_op);
-    o.b = b;
-    if (da) {
-        o.p = u;
-        o.q = x;
-        o.ldq = ldx;
-        o.C = (int)K;
-        o.out = da;
-        OPCHK(launch_outer(o, stream), "adapter gradient");
-    }
-    if (db) {
-        o.p = t;
-        o.q = dy;
-        o.ldq = lddy;
-        o.C = (int)N;
-        o.transposed = 1;
-        o.out = db;
-        OPCHK(launch_outer(o, stream), "adapter gradient");
-    }
+    if (n_outer) OPCHK(launch_outer(outer, n_outer, stream), "adapter gradients");
+    OPCHK(launch_jobs(last, stream), "sums");
     return GEMEL_OK;
 }
 
@@ -903,7 +935,7 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         if (!lo) o.x.lo = o.xt.lo = nullptr;
         OPCHK(launch_norm(o, c.stream), "norm");
         OPCHK(launch_seed(o, c.stream), "scaled update");
-        auto operands = [&](MmArgs &a, const Planes &l, const Planes &r) {
+        auto planes_of = [&](MmArgs &a, const Planes &l, const Planes &r) {
             const u16 *al[3] = {l.hi, lo ? l.lo : nullptr, l.hi}, *bl[3] = {lo ? r.lo : r.hi, r.hi, r.hi};
             for (int i = 0; i < 3; ++i) {
                 a.a[i] = al[i];
@@ -922,16 +954,16 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         };
         Planes from = o.xt, to = t1, now = o.x;
         for (int k = 0; k < steps; ++k) {
-            operands(gram, now, now);
+            planes_of(gram, now, now);
             gram.o.p = s;
             OPCHK(launch_mm(gram, c.stream), "product");
-            operands(poly, s, s);
+            planes_of(poly, s, s);
             poly.o.s = s;
             poly.o.p = p;
             poly.o.lambda = o.lambda + k;
             OPCHK(launch_mm(poly, c.stream), "product");
             if (k + 1 < steps) {
-                operands(next, from, p);
+                planes_of(next, from, p);
                 next.o.s = from;
                 next.o.p = to;
                 now = x;
@@ -944,9 +976,9 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
                 to = read;
             } else {
                 if (wide)
-                    operands(last, p, from);
+                    planes_of(last, p, from);
                 else
-                    operands(last, from, p);
+                    planes_of(last, from, p);
                 last.o.s = wide ? now : from;
                 last.o.diag_rows = wide;
                 last.o.ld = o.cols;
