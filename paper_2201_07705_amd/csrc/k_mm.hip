@@ -79,16 +79,15 @@ __device__ __forceinline__ f32x4 next4(const MmArgs &a, int z, int m, int n, f32
     return x;
 }
 
-// One operand's loads of a step: 16 bytes at base + off[i] + depth into the
-// wave's slots. A buffer resource keeps the base in scalar registers; every
+// One operand's loads of a step: 16 bytes at base + off[i] into the wave's
+// slots. A buffer resource keeps the base in scalar registers; every
 // offset is in bounds, so its own check is not used.
 template <int LOADS, int NW>
-__device__ __forceinline__ void fetch(const u16 *base, const uint32_t (&off)[LOADS], int depth, unsigned char *stage,
-                                      int wave) {
+__device__ __forceinline__ void fetch(const u16 *base, const uint32_t (&off)[LOADS], unsigned char *stage, int wave) {
     const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<u16 *>(base), 0, -1, 0x00020000);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8 *)(stage + (i * NW + wave) * 1024), 16, (int)off[i], depth, 0, 0);
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8 *)(stage + (i * NW + wave) * 1024), 16, (int)off[i], 0, 0, 0);
 }
 
 // The kernel's argument block where the hardware keeps it.
@@ -98,13 +97,33 @@ __device__ __forceinline__ const MmArgs *late_args(const MmArgs &) {
     return (const MmArgs *)p;
 }
 
+// Brings the argument block into the scalar cache with the first loads of the
+// kernel: its later part would otherwise be fetched, from host memory, only
+// when the epilogue asks for it.
+__device__ __forceinline__ void touch_args() {
+    typedef const __attribute__((address_space(4))) int *args_t;
+    const args_t p = (args_t)__builtin_amdgcn_kernarg_segment_ptr();
+    int x = 0;
+#pragma unroll
+    for (int i = 0; i < (int)(sizeof(MmArgs) / 4); i += 16) x |= p[i];
+    asm volatile("" ::"s"(x));
+}
+
 // Tile of a workgroup: consecutive tiles on one XCD, and among them groups
-// of 8 tile rows, whose operand rows then stay in its L2.
+// of 8 tile rows, whose operand rows then stay in its L2. Symmetric results:
+// only tiles on and above the diagonal exist, row i of them paired with row
+// last - i, so that each pair has as many.
 template <int T>
 __device__ __forceinline__ void mm_place(const MmArgs &a, int &tm, int &tn) {
     const int tiles_m = (a.M + T - 1) / T, tiles_n = (a.N + T - 1) / T;
     const int G = gridDim.x;
     const int t = (G & 7) == 0 ? (int)(blockIdx.x & 7) * (G >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
+    if (a.sym) {
+        const int pair = t / (tiles_n + 1), c = t - pair * (tiles_n + 1), first = tiles_n - pair;
+        tm = c < first ? pair : tiles_n - 1 - pair;
+        tn = tm + (c < first ? c : c - first);
+        return;
+    }
     const int group = t / (8 * tiles_n), first = group * 8, rows = min(8, tiles_m - first);
     const int in = t - group * 8 * tiles_n;
     tn = in / rows;
@@ -210,34 +229,39 @@ __device__ __forceinline__ f32x4 finish(const MmArgs &a, int z, int m, int n, f3
     return v;
 }
 
-// One T x T output tile per workgroup: 8 waves of 128 x 64 (T = 256) or 4 of
-// T/2 x T/2. A step of depth 64 is fetched by global_load_lds into one of two
-// LDS buffers (separate arrays, so that the compiler sees which buffer a load
-// in flight writes), the step after next being requested as soon as the
-// current buffer's last fragments are in registers. Slot p of a buffer holds
-// row p / 8, 16-byte chunk (p % 8) ^ (row / 2 % 8): the fragment reads of 16
-// rows then fall on distinct banks. A step is four phases of (depth half, row
-// half) fragments; each phase reads the next one's fragments, so that the
-// matrix cores wait for LDS only across the one barrier of a step, and there
-// the fragments read before it cover the others.
+// One T x T output tile per workgroup: 8 waves of 128 x 64 (T = 256) or 32 x
+// 64 (T = 128, two workgroups on a compute unit), or 4 of 32 x 32 (T = 64).
+// A step of depth 64 is fetched by direct global-to-LDS loads into one of
+// STAGES buffers (separate arrays, so that the compiler sees which buffer a
+// load in flight writes), a buffer being asked for again as soon as its last
+// fragments are in registers. Slot p of a buffer holds row p / 8, 16-byte
+// chunk (p % 8) ^ (row / 2 % 8): the fragment reads of 16 rows then fall on
+// distinct banks. A step is PHASES pieces, each reading the next one's
+// fragments, so that the matrix cores wait for LDS only across the one
+// barrier of a step, and there the fragments read before it cover the others.
+// Large tiles have no registers for more than a quarter step (256) or half a
+// step (128) in hand; small ones take a whole one and four buffers, which is
+// what latency wants.
 //
-// At 8192^3 (bf16) T = 256 runs at 1354 TFLOP/s and T = 128 (two workgroups
-// on a CU) at 1144; at 4096^3 1312 and 1166.
+// What bounds it: the matrix cores at T = 256 (25088 x 4096 x 12288, float16:
+// 1262 TFLOP/s), the CU's 64 bytes a cycle from the L2 at T = 64 (half the
+// peak). 4096 x 4096 x 4096: T = 128 1243, T = 256 1190, T = 64 715 TFLOP/s.
 template <int T>
-constexpr int mm_threads() { return T == 256 ? 512 : 256; }
+constexpr int mm_threads() { return T == 64 ? 256 : 512; }
 
-template <int T, bool F16, int EPI>
-__global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(const MmArgs a) {
+template <int T, int STAGES, int PHASES, bool F16, int EPI>
+__global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2) void mm_kernel(const MmArgs a) {
     constexpr int NT = mm_threads<T>(), NW = NT / 64, WN = T == 256 ? 4 : 2;
-    constexpr int TM = T / 2, TN = T / WN, FM = TM / 16, FN = TN / 16, HM = FM / 2;
+    constexpr int TM = T * WN / NW, TN = T / WN, FM = TM / 16, FN = TN / 16;
     constexpr int LOADS = T * 8 / NT, ROW = BK * 2;
-    __shared__ __attribute__((aligned(1024))) unsigned char st0[2 * T * ROW], st1[2 * T * ROW];
+    __shared__ __attribute__((aligned(1024))) unsigned char st0[2 * T * ROW], st1[2 * T * ROW],
+        st2[STAGES > 2 ? 2 * T * ROW : 16], st3[STAGES > 3 ? 2 * T * ROW : 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave - wm * WN, g = lane >> 4, l16 = lane & 15;
+    touch_args();
     int tm, tn;
     mm_place<T>(a, tm, tn);
-    if (a.sym && tn < tm) return;
     const int split = blockIdx.y, z = blockIdx.z;
     const int m0 = tm * T, n0 = tn * T;
     const int nk = (a.K + BK - 1) / BK;
@@ -262,25 +286,27 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
         oa[i] = (uint32_t)((a.perm ? a.perm[m] : m - m0) * (uint32_t)a.lda + ch) * 2u;
         ob[i] = (uint32_t)((n - n0) * (uint32_t)a.ldb + ch) * 2u;
     }
-    int seg = s0 / nk, kk = (s0 - seg * nk) * BK, iss = 0;
     const int64_t za = (int64_t)z * a.za + (a.perm ? 0 : (int64_t)m0 * a.lda), zb = (int64_t)z * a.zb + (int64_t)n0 * a.ldb;
+    // the next step's operands: kept as running pointers, since a load of a
+    // segment's pointers in every step would hold it up
+    int seg = s0 / nk, seg_left = nk - (s0 - seg * nk), iss = 0;
+    const u16 *pa = (seg == 0 ? a.a[0] : seg == 1 ? a.a[1] : a.a[2]) + za + (s0 - seg * nk) * BK;
+    const u16 *pb = (seg == 0 ? a.b[0] : seg == 1 ? a.b[1] : a.b[2]) + zb + (s0 - seg * nk) * BK;
     // Requests the next step; past the last one, the last one again (into a
     // buffer whose reads are over), so that every step waits alike.
     auto issue = [&](unsigned char *stage) __attribute__((always_inline)) {
         const bool ext = EPI == EPI_ROWS && exts > 0 && iss >= mains;
+        const int kk = (s0 + min(iss, mains - 1)) * BK;   // (of one segment, where it is used)
         if (EPI == EPI_ROWS && (ext || kk + BK > a.K)) {
             // rows of other runs, and chunks beyond a depth that is no
             // multiple of 64, are zeros
-            const char *pa, *pb;
+            const u16 *qa = pa, *qb = pb;
             int lo = 0, hi = INT_MAX;
             if (ext) {
-                pa = (const char *)(a.t + (int64_t)m0 * a.ext + ek);
-                pb = (const char *)(a.bx + ((int64_t)u * a.N + n0) * a.ext + ek);
+                qa = a.t + (int64_t)m0 * a.ext + ek;
+                qb = a.bx + ((int64_t)u * a.N + n0) * a.ext + ek;
                 lo = a.run_start[u];
                 hi = a.run_start[u + 1];
-            } else {
-                pa = (const char *)(a.a[0] + za + kk);
-                pb = (const char *)(a.b[0] + zb + kk);
             }
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) {
@@ -288,9 +314,9 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
                 const bool in = ext ? m0 + row >= lo && m0 + row < hi : kk + ch < a.K;
                 const uint32_t xa = ext ? (uint32_t)(row * a.ext + ch) * 2u : oa[i];
                 const uint32_t xb = ext ? (uint32_t)((min(n0 + row, a.N - 1) - n0) * a.ext + ch) * 2u : ob[i];
-                __builtin_amdgcn_global_load_lds(in ? (const void *)(pa + xa) : (const void *)a.zero,
+                __builtin_amdgcn_global_load_lds(in ? (const void *)((const char *)qa + xa) : (const void *)a.zero,
                                                  (lds_u8 *)(stage + (i * NW + wave) * 1024), 16, 0, 0);
-                __builtin_amdgcn_global_load_lds(ext || in ? (const void *)(pb + xb) : (const void *)a.zero,
+                __builtin_amdgcn_global_load_lds(ext || in ? (const void *)((const char *)qb + xb) : (const void *)a.zero,
                                                  (lds_u8 *)(stage + T * ROW + (i * NW + wave) * 1024), 16, 0, 0);
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -302,20 +328,18 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
                 }
             }
         } else {
-            const u16 *pa = a.a[0], *pb = a.b[0];
-            if (EPI != EPI_ROWS && seg) {
-                pa = seg == 1 ? a.a[1] : a.a[2];
-                pb = seg == 1 ? a.b[1] : a.b[2];
-            }
-            fetch<LOADS, NW>(pa + za, oa, kk * 2, stage, wave);
-            fetch<LOADS, NW>(pb + zb, ob, kk * 2, stage + T * ROW, wave);
+            fetch<LOADS, NW>(pa, oa, stage, wave);
+            fetch<LOADS, NW>(pb, ob, stage + T * ROW, wave);
         }
         iss = min(iss + 1, total);
         if (iss < mains) {
-            kk += BK;
-            if (kk >= nk * BK) {
-                kk = 0;
+            pa += BK;
+            pb += BK;
+            if (EPI != EPI_ROWS && --seg_left == 0) {
                 ++seg;
+                seg_left = nk;
+                pa = (seg == 1 ? a.a[1] : a.a[2]) + za;
+                pb = (seg == 1 ? a.b[1] : a.b[2]) + zb;
             }
         }
     };
@@ -325,28 +349,33 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
     using H8 = std::conditional_t<F16, f16x8, bf16x8>;
-    H8 fa0[HM], fa1[HM], fb0[FN], fb1[FN];
+    // fragments: of a quarter (depth half, row half), a half or a whole step,
+    // and the next one's
+    constexpr int NA = PHASES == 4 ? FM / 2 : PHASES == 2 ? FM : 2 * FM, NB = PHASES == 1 ? 2 * FN : FN;
+    H8 fa0[NA], fa1[NA], fb0[NB], fb1[NB];
     // rows 16 apart share their swizzle: one address per depth half
     const int ra = (wm * TM + l16) * ROW, rb = T * ROW + (wn * TN + l16) * ROW;
     const int h0 = (g ^ ((l16 >> 1) & 7)) * 16, h1 = ((4 + g) ^ ((l16 >> 1) & 7)) * 16;
-    auto read_a = [&](H8(&f)[HM], const unsigned char *s, int h, int half) __attribute__((always_inline)) {
+    auto read_a = [&](H8(&f)[NA], const unsigned char *s, int h, int row) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < HM; ++i) f[i] = *(const H8 *)(s + ra + h + (half * HM + i) * 16 * ROW);
+        for (int i = 0; i < NA; ++i)
+            f[i] = *(const H8 *)(s + ra + (PHASES == 1 && i >= FM ? h1 : h) + (row + i % FM) * 16 * ROW);
     };
-    auto read_b = [&](H8(&f)[FN], const unsigned char *s, int h) __attribute__((always_inline)) {
+    auto read_b = [&](H8(&f)[NB], const unsigned char *s, int h) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < FN; ++j) f[j] = *(const H8 *)(s + rb + h + j * 16 * ROW);
+        for (int j = 0; j < NB; ++j) f[j] = *(const H8 *)(s + rb + (PHASES == 1 && j >= FN ? h1 : h) + j % FN * 16 * ROW);
     };
-    auto mul = [&](H8(&f)[HM], H8(&b)[FN], int half) __attribute__((always_inline)) {
+    auto mul = [&](H8(&f)[NA], H8(&b)[NB], int row) __attribute__((always_inline)) {
 #pragma unroll
-        for (int i = 0; i < HM; ++i)
+        for (int i = 0; i < NA; ++i)
 #pragma unroll
             for (int j = 0; j < FN; ++j) {
-                f32x4 &c = acc[half * HM + i][j];
+                f32x4 &c = acc[row + i % FM][j];
+                const H8 &bj = b[PHASES == 1 && i >= FM ? FN + j : j];
                 if constexpr (F16)
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(b[j], f[i], c, 0, 0, 0);
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bj, f[i], c, 0, 0, 0);
                 else
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[j], f[i], c, 0, 0, 0);
+                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bj, f[i], c, 0, 0, 0);
             }
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -354,49 +383,69 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
     // every wave has read the last of `cur`
     auto turn = [&]() __attribute__((always_inline)) {
         wait_lgkm0();
-        wait_vm<0>();
+        wait_vm<(STAGES - 2) * 2 * LOADS>();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto step = [&](unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
-        read_a(fa1, cur, h0, 1);
-        mul(fa0, fb0, 0);
-        read_a(fa0, cur, h1, 0);
-        read_b(fb1, cur, h1);
-        mul(fa1, fb0, 1);
-        read_a(fa1, cur, h1, 1);
-        mul(fa0, fb1, 0);
-        turn();
-        issue(cur);
-        read_a(fa0, next, h0, 0);
-        read_b(fb0, next, h0);
-        mul(fa1, fb1, 1);
+    // one step; set: which fragments hold the whole step (PHASES == 1)
+    auto step = [&](unsigned char *cur, unsigned char *next, int set) __attribute__((always_inline)) {
+        if constexpr (PHASES == 4) {
+            read_a(fa1, cur, h0, NA);
+            mul(fa0, fb0, 0);
+            read_a(fa0, cur, h1, 0);
+            read_b(fb1, cur, h1);
+            mul(fa1, fb0, NA);
+            read_a(fa1, cur, h1, NA);
+            mul(fa0, fb1, 0);
+            turn();
+            issue(cur);
+            read_a(fa0, next, h0, 0);
+            read_b(fb0, next, h0);
+            mul(fa1, fb1, NA);
+        } else if constexpr (PHASES == 2) {
+            read_a(fa1, cur, h1, 0);
+            read_b(fb1, cur, h1);
+            mul(fa0, fb0, 0);
+            turn();
+            issue(cur);
+            read_a(fa0, next, h0, 0);
+            read_b(fb0, next, h0);
+            mul(fa1, fb1, 0);
+        } else {
+            turn();
+            issue(cur);
+            if (set) {
+                read_a(fa0, next, h0, 0);
+                read_b(fb0, next, h0);
+                mul(fa1, fb1, 0);
+            } else {
+                read_a(fa1, next, h0, 0);
+                read_b(fb1, next, h0);
+                mul(fa0, fb0, 0);
+            }
+        }
     };
-    issue(st0);
-    issue(st1);
-    wait_vm<2 * LOADS>();
+    static_assert(PHASES != 1 || STAGES % 2 == 0, "a turn of the ring is a turn of the fragments");
+    unsigned char *const ring[4] = {st0, st1, st2, st3};
+#pragma unroll
+    for (int i = 0; i < STAGES; ++i) issue(ring[i]);
+    wait_vm<(STAGES - 1) * 2 * LOADS>();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
     read_a(fa0, st0, h0, 0);
     read_b(fb0, st0, h0);
     // no way out of the loop but its end: with one the compiler spills the sums
-    for (int s = 0; s + 2 <= total; s += 2) {
-        step(st0, st1);
-        step(st1, st0);
+    int left = total;
+    for (; left >= STAGES; left -= STAGES) {
+#pragma unroll
+        for (int i = 0; i < STAGES; ++i) step(ring[i], ring[(i + 1) % STAGES], i & 1);
     }
-    if (total & 1) {
-        read_a(fa1, st0, h0, 1);
-        mul(fa0, fb0, 0);
-        read_a(fa0, st0, h1, 0);
-        read_b(fb1, st0, h1);
-        mul(fa1, fb0, 1);
-        read_a(fa1, st0, h1, 1);
-        mul(fa0, fb1, 0);
-        mul(fa1, fb1, 1);
-    }
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (left > i) step(ring[i], ring[i + 1], i & 1);
     wait_vm<0>();
     __builtin_amdgcn_sched_barrier(0);
     __syncthreads();
@@ -453,80 +502,101 @@ __global__ __launch_bounds__(mm_threads<T>(), T == 256 ? 1 : 2) void mm_kernel(c
     }
 }
 
-// Sums the splits of each element in order and applies the epilogue.
-// One thread per 4 columns of the padded width, rows up to the padded
-// height where planes need their zeros.
+// Sums the splits of each element in order and applies the epilogue, one
+// 64 x 64 tile per workgroup; transposed planes go through LDS.
 template <int EPI>
-__global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a, int rows, int quads, int T) {
-    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int m = (int)(i / quads), n = (int)(i - (int64_t)m * quads) * 4, z = blockIdx.z;
-    if (m >= rows) return;
-    const int tm = m / T, tn = n / T;
-    if (a.sym && tn < tm) return;
-    f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    if (m < a.M && n < a.N)
-        for (int s = 0; s < a.splits; ++s)
-            v += *(const f32x4 *)(a.partial + (((int64_t)s * a.batch + z) * a.M + m) * a.ldp + n);
-    v = finish<EPI>(a, z, m, n, v);
-    if constexpr (EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT) {
-        const Planes &q = EPI == EPI_NEXT ? a.o.q : a.o.p;
-        if ((EPI == EPI_NEXT || (a.sym && tn > tm)) && m < q.ld) {
+__global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
+    constexpr bool PLANES = EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT;
+    __shared__ float tile[PLANES ? 64 : 1][65];
+    int tm, tn;
+    mm_place<64>(a, tm, tn);
+    const int z = blockIdx.z, m0 = tm * 64, n0 = tn * 64;
+    const bool turned = EPI == EPI_NEXT || (PLANES && a.sym && tn > tm);
+    f32x4 v[4];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                if (n + i >= a.N) continue;
-                const int64_t at = (int64_t)z * q.z + (int64_t)(n + i) * q.ld + m;
-                const u16 h = to_half(v[i]);
-                q.hi[at] = h;
-                if (q.lo) q.lo[at] = to_half(v[i] - half_up(h));
-            }
+    for (int i = 0; i < 4; ++i) {
+        const int m = m0 + i * 16 + (threadIdx.x >> 4), n = n0 + (threadIdx.x & 15) * 4;
+        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (m < a.M && n < a.N) {
+            const float *p = a.partial + ((int64_t)z * a.M + m) * a.ldp + n;
+#pragma unroll 4
+            for (int s = 0; s < a.splits; ++s) v[i] += *(const f32x4 *)(p + (int64_t)s * a.batch * a.M * a.ldp);
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int m = i * 16 + (threadIdx.x >> 4), n = (threadIdx.x & 15) * 4;
+        v[i] = finish<EPI>(a, z, m0 + m, n0 + n, v[i]);
+        if constexpr (PLANES)
+            if (turned)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) tile[m][n + e] = v[i][e];
+    }
+    if constexpr (PLANES) {
+        if (!turned) return;
+        __syncthreads();
+        const Planes &q = EPI == EPI_NEXT ? a.o.q : a.o.p;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int n = i * 16 + (threadIdx.x >> 4), m = (threadIdx.x & 15) * 4;
+            const f32x4 x = {tile[m][n], tile[m + 1][n], tile[m + 2][n], tile[m + 3][n]};
+            if (n0 + n < a.N && m0 + m < q.ld) put4(q, (int64_t)z * q.z + (int64_t)(n0 + n) * q.ld + m0 + m, x);
         }
     }
 }
 
-template <int T, bool F16, int EPI>
+int64_t tiles_of(const MmArgs &a, int T) {
+    const int64_t tm = (a.M + T - 1) / T, tn = (a.N + T - 1) / T;
+    return a.sym ? tm * (tm + 1) / 2 : tm * tn;
+}
+
+template <int T, int STAGES, int PHASES, bool F16, int EPI>
 hipError_t go(const MmArgs &a, hipStream_t s) {
-    const int tm = (a.M + T - 1) / T, tn = (a.N + T - 1) / T;
-    const dim3 grid((unsigned)(tm * tn), (unsigned)a.splits, (unsigned)a.batch);
+    const dim3 grid((unsigned)tiles_of(a, T), (unsigned)a.splits, (unsigned)a.batch);
     void *p[] = {const_cast<MmArgs *>(&a)};
-    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, F16, EPI>), grid,
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, STAGES, PHASES, F16, EPI>), grid,
                                    dim3(mm_threads<T>()), p, 0, s);
     if (e != hipSuccess || a.splits == 1) return e;
-    int rows = tm * T, quads = tn * T / 4, tt = T;
-    const int64_t blocks = ((int64_t)rows * quads + 255) / 256;
-    void *q[] = {const_cast<MmArgs *>(&a), &rows, &quads, &tt};
     return hipLaunchKernel(reinterpret_cast<const void *>(&mm_reduce_kernel<EPI>),
-                           dim3((unsigned)blocks, 1, (unsigned)a.batch), dim3(256), q, 0, s);
+                           dim3((unsigned)tiles_of(a, 64), 1, (unsigned)a.batch), dim3(256), p, 0, s);
 }
 
 template <int EPI, bool F16>
 hipError_t pick(const MmArgs &a, hipStream_t s) {
-    return a.tile == 256 ? go<256, F16, EPI>(a, s) : a.tile == 128 ? go<128, F16, EPI>(a, s) : go<64, F16, EPI>(a, s);
+        return a.tile == 256   ? go<256, 2, 4, F16, EPI>(a, s)
+           : a.tile == 128 ? go<128, 2, 2, F16, EPI>(a, s)
+                           : go<64, 4, 1, F16, EPI>(a, s);
 }
 
 }  // namespace
 
-// Tile and depth splits: the estimated time of the launch is the turns that
+// Tile and depth splits, by the estimated time of the launch: the turns that
 // the compute units take, each a step's time for every step and a fixed part
-// for the pipeline's start and the epilogue, plus writing and reading the
-// partial sums and the second launch where the depth is split.
+// for the pipeline's start and the epilogue; and, where the depth is split,
+// writing and reading the partial sums and the second launch. Measured steps
+// (microseconds, float16, workgroups on every compute unit): 64 x 64 tiles
+// 0.18 alone on a compute unit and 0.33 two at once, 128 x 128 0.6 and 0.8,
+// 256 x 256 1.65. A 512 x 512 result of depth 4608 takes 18.5 us unsplit and
+// 13.6 in 4 splits, a symmetric 4096 x 4096 one of depth 75264 1704 and 1117
+// us in 7 (its 136 tiles of 256 leave half of the 256 compute units idle).
 void mm_plan(MmArgs &a) {
     struct Form {
-        int tile, slots;      // workgroups that run at once
-        double step, fixed;   // microseconds
+        int tile, slots;                 // workgroups that run at once
+        double alone, full, fixed;       // microseconds
     };
-    static const Form forms[] = {{256, 256, 1.62, 6.0}, {128, 512, 0.92, 4.0}, {64, 1024, 0.75, 2.5}};
+    static const Form forms[] = {{256, 256, 1.65, 1.65, 8.0}, {128, 512, 0.6, 0.8, 6.5}, {64, 512, 0.18, 0.33, 5.5}};
     const int steps = (a.K + BK - 1) / BK * a.nseg;
     double best = 1e30;
     for (const Form &f : forms) {
-        const int64_t tm = (a.M + f.tile - 1) / f.tile, tn = (a.N + f.tile - 1) / f.tile;
-        const int64_t tiles = (a.sym ? tm * (tm + 1) / 2 : tm * tn) * a.batch;
+        const int64_t tiles = tiles_of(a, f.tile) * a.batch;
         for (int want = 1; want <= 32 && want <= std::max(1, steps / 4); ++want) {
             const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
             if (splits != want) continue;
-            const double turns = (double)((tiles * splits + f.slots - 1) / f.slots);
-            double us = turns * (per * f.step + f.fixed);
+            const int64_t groups = tiles * splits, whole = groups / f.slots, rest = groups % f.slots;
+            double us = (double)whole * (per * f.full + f.fixed);
+            if (rest) us += per * (rest > 256 ? f.full : f.alone) + f.fixed;
             const double bytes = (double)splits * a.batch * a.M * op_round_up(a.N, 4) * (a.sym ? 2 : 4);
-            if (splits > 1) us += 4.0 + 2 * bytes / 4e6;
+            if (splits > 1) us += 5.0 + 2 * bytes / 5.5e6;
             if (splits > 1 && bytes > 1e9) continue;
             if (us < best) {
                 best = us;
