@@ -57,14 +57,14 @@ __device__ __forceinline__ f32x4 rest4(f32x4 v) {
                  v[3] - half_up(to_half(v[3]))};
 }
 
-// a X + M X at (m, n .. n + 3) in X's plane units, v being the product of
-// the planes. Where M is a single plane, what its diagonal (most of M once X
+// cs X + cv v at (m, n .. n + 3) in X's plane units (a X + M X, v being the
+// product of the planes). Where M is a single plane, what its diagonal (most of M once X
 // is nearly orthogonal) and X have lost to rounding is put back.
 __device__ __forceinline__ f32x4 next4(const MmArgs &a, int z, int m, int n, f32x4 v) {
     const MmOut &o = a.o;
     f32x4 hi, lo;
     at4(o.s, z, m, n, a.M, hi, lo);
-    f32x4 x = (float)COEF_A * (hi + lo) + v * 0x1p-14f;
+    f32x4 x = o.cs * (hi + lo) + o.cv * v;
     if (o.mdiag) {
         const float *d = o.mdiag + z * o.diag_z;
         f32x4 md;
@@ -150,7 +150,12 @@ __device__ __forceinline__ f32x4 finish(const MmArgs &a, int z, int m, int n, f3
                 int u = a.first_run[m >> 6];
                 while (a.run_start[u + 1] <= m) ++u;
                 const float *t = o.t + (int64_t)m * o.rp, *bx = o.bx + (int64_t)u * o.rp * o.ldbx + n;
-                for (int r = 0; r < o.rp; ++r) v += t[r] * *(const f32x4 *)(bx + r * o.ldbx);
+                // (zeros from the run's rank on, up to a multiple of 32)
+                for (int r = 0; r < o.run_rank[u]; r += 4) {
+                    const f32x4 t4 = *(const f32x4 *)(t + r);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) v += t4[i] * *(const f32x4 *)(bx + (r + i) * o.ldbx);
+                }
             }
         }
         if (o.out_f32) {
@@ -213,9 +218,18 @@ __device__ __forceinline__ f32x4 finish(const MmArgs &a, int z, int m, int n, f3
                 s += lo;
             }
             x = 0x1p14f * ((float)COEF_B * 0x1p-11f * l2 * s + (float)COEF_C * 0x1p-22f * l2 * l2 * v);
+        } else if constexpr (EPI == EPI_MIX) {
+            f32x4 hi, lo, hi2, lo2;
+            at4(o.s, z, m, n, a.M, hi, lo);
+            at4(o.s2, z, m, n, a.M, hi2, lo2);
+            x = o.cs * (hi + lo) + o.cs2 * (hi2 + lo2) + o.cv * v;
+            if (o.lambdas) {
+                const float *l = o.lambda + z * ORTH_LAMBDAS, f = l[0] / l[o.lambdas];
+                x *= f * f;
+            }
         } else {
             const float *l = o.lambda + z * ORTH_LAMBDAS;
-            x = l[0] / l[1] * next4(a, z, m, n, v);
+            x = l[0] / l[o.lambdas] * next4(a, z, m, n, v);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) x[i] = m < a.M && n + i < a.N ? x[i] : 0.f;
@@ -474,7 +488,8 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
             }
         wait_lgkm0();
         asm volatile("" ::: "memory");
-        const bool turned = (EPI == EPI_NEXT || ((EPI == EPI_GRAM || EPI == EPI_POLY) && e.sym && tn > tm)) && e.splits == 1;
+        const bool turned = (EPI == EPI_NEXT || ((EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_MIX) && e.sym && tn > tm)) &&
+                            e.splits == 1;
         for (int it = lane; it < RP * C; it += 64) {
             const int m = it / C, c = it & (C - 1);
             f32x4 *const slot = (f32x4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16);
@@ -506,7 +521,7 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
 // 64 x 64 tile per workgroup; transposed planes go through LDS.
 template <int EPI>
 __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
-    constexpr bool PLANES = EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT;
+    constexpr bool PLANES = EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT || EPI == EPI_MIX;
     __shared__ float tile[PLANES ? 64 : 1][65];
     int tm, tn;
     mm_place<64>(a, tm, tn);
@@ -579,7 +594,7 @@ hipError_t pick(const MmArgs &a, hipStream_t s) {
 // 256 x 256 1.65. A 512 x 512 result of depth 4608 takes 18.5 us unsplit and
 // 13.6 in 4 splits, a symmetric 4096 x 4096 one of depth 75264 1704 and 1117
 // us in 7 (its 136 tiles of 256 leave half of the 256 compute units idle).
-void mm_plan(MmArgs &a) {
+double mm_plan(MmArgs &a) {
     struct Form {
         int tile, slots;                 // workgroups that run at once
         double alone, full, fixed;       // microseconds
@@ -607,6 +622,7 @@ void mm_plan(MmArgs &a) {
         }
     }
     a.ldp = op_round_up(a.N, 4);
+    return best;
 }
 
 hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
@@ -633,6 +649,7 @@ hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
         case EPI_NEXT: return pick<EPI_NEXT, true>(a, s);
         case EPI_ORTH: return pick<EPI_ORTH, true>(a, s);
         case EPI_STEP: return pick<EPI_STEP, true>(a, s);
+        case EPI_MIX: return pick<EPI_MIX, true>(a, s);
     }
     return hipErrorInvalidValue;
 }

@@ -11,6 +11,9 @@ namespace gemel {
 
 namespace {
 
+typedef double f64x4 __attribute__((ext_vector_type(4)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+
 __device__ __forceinline__ float bf_up(u16 h) { return __uint_as_float((uint32_t)h << 16); }
 __device__ __forceinline__ u16 half_down(float f) { return __builtin_bit_cast(u16, (_Float16)f); }
 __device__ __forceinline__ float half_up(u16 h) { return (float)__builtin_bit_cast(_Float16, h); }
@@ -31,13 +34,46 @@ __device__ __forceinline__ double block_sum(double v) {
     return part[0] + part[1] + part[2] + part[3];
 }
 
+// 4 consecutive elements of the update from element `at` on; those from
+// `left` on are zeros. With a step, momentum is brought up to date first
+// (FIRST) and read back later.
+template <bool FIRST>
+__device__ __forceinline__ f32x4 update4(const OrthArgs &a, int64_t at, int left) {
+    f32x4 u = {0.f, 0.f, 0.f, 0.f};
+    if (left >= 4 && a.vec) {
+        f32x4 g;
+        if (a.f32) {
+            g = *(const f32x4 *)((const float *)a.g + at);
+        } else {
+            const ushort4 h = *(const ushort4 *)((const u16 *)a.g + at);
+            g = f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
+        }
+        if (!a.step) return g;
+        f32x4 m = *(const f32x4 *)(a.m + at);
+        if (FIRST) {
+            m = a.beta * m + g;
+            *(f32x4 *)(a.m + at) = m;
+        }
+        return a.nesterov ? g + a.beta * m : m;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= left) continue;
+        if (FIRST && a.step) a.m[at + i] = a.beta * a.m[at + i] + ((const float *)a.g)[at + i];
+        u[i] = update_at(a, at + i);
+    }
+    return u;
+}
+
+// Momentum and squared sums, 4 elements at a time; reading and writing bounds it.
 __global__ __launch_bounds__(256) void norm_kernel(const OrthArgs a) {
     const int64_t size = (int64_t)a.rows * a.cols, base = blockIdx.y * size;
     double s = 0.;
-    for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < size; i += (int64_t)a.parts * 256) {
-        if (a.step) a.m[base + i] = a.beta * a.m[base + i] + ((const float *)a.g)[base + i];
-        const double v = update_at(a, base + i);
-        s += v * v;
+#pragma unroll 4
+    for (int64_t i = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4; i < size; i += (int64_t)a.parts * 1024) {
+        const f32x4 u = update4<true>(a, base + i, (int)min((int64_t)4, size - i));
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s += (double)u[e] * u[e];
     }
     s = block_sum(s);
     if (threadIdx.x == 0) a.sums[(int64_t)blockIdx.y * a.parts + blockIdx.x] = s;
@@ -70,32 +106,35 @@ __global__ __launch_bounds__(256) void seed_kernel(const OrthArgs a) {
     }
     __syncthreads();
     const int e = es + 13;
-    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    const int c0 = blockIdx.x * 64, r0 = blockIdx.y * 64, x = (threadIdx.x & 15) * 4, y = threadIdx.x >> 4;
     const bool wide = a.rows <= a.cols;
     const Planes &p = wide ? a.x : a.xt, &q = wide ? a.xt : a.x;   // as the input lies, and transposed
     const int64_t base = (int64_t)z * a.rows * a.cols;
-    for (int i = y; i < 64; i += 4) {
-        const int r = r0 + i, c = c0 + x;
-        float v = 0.f;
-        if (r < a.rows && c < a.cols) v = ldexpf(update_at(a, base + (int64_t)r * a.cols + c), e);
-        tile[i][x] = v;
-        if (r < a.rows && c < p.ld) {
-            const int64_t at = z * p.z + r * p.ld + c;
-            const u16 h = half_down(v);
-            p.hi[at] = h;
-            if (p.lo) p.lo[at] = half_down(v - half_up(h));
+    auto put4 = [](const Planes &p, int64_t at, f32x4 v) __attribute__((always_inline)) {
+        const ushort4 h = make_ushort4(half_down(v[0]), half_down(v[1]), half_down(v[2]), half_down(v[3]));
+        *(ushort4 *)(p.hi + at) = h;
+        if (p.lo)
+            *(ushort4 *)(p.lo + at) = make_ushort4(half_down(v[0] - half_up(h.x)), half_down(v[1] - half_up(h.y)),
+                                                   half_down(v[2] - half_up(h.z)), half_down(v[3] - half_up(h.w)));
+    };
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = r0 + y + 16 * i, c = c0 + x;
+        f32x4 v = {0.f, 0.f, 0.f, 0.f};
+        if (r < a.rows && c < a.cols) v = update4<false>(a, base + (int64_t)r * a.cols + c, min(4, a.cols - c));
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            v[k] = ldexpf(v[k], e);
+            tile[y + 16 * i][x + k] = v[k];
         }
+        if (r < a.rows && c < p.ld) put4(p, z * p.z + r * p.ld + c, v);
     }
     __syncthreads();
-    for (int i = y; i < 64; i += 4) {
-        const int c = c0 + i, r = r0 + x;
-        if (c < a.cols && r < q.ld) {
-            const float v = tile[x][i];
-            const int64_t at = z * q.z + c * q.ld + r;
-            const u16 h = half_down(v);
-            q.hi[at] = h;
-            if (q.lo) q.lo[at] = half_down(v - half_up(h));
-        }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int c = c0 + y + 16 * i, r = r0 + x;
+        const f32x4 v = {tile[x][y + 16 * i], tile[x + 1][y + 16 * i], tile[x + 2][y + 16 * i], tile[x + 3][y + 16 * i]};
+        if (c < a.cols && r < q.ld) put4(q, z * q.z + c * q.ld + r, v);
     }
 }
 
@@ -109,40 +148,6 @@ __global__ __launch_bounds__(256) void seed_kernel(const OrthArgs a) {
 // float32 sums 1e-7 of S_0 became up to 3e-3 of the result, so S_0 and the
 // polynomials are float64 (the f64 matrix cores are idle otherwise, and the
 // work is n^2 m + 19 n^3).
-
-typedef double f64x4 __attribute__((ext_vector_type(4)));
-typedef float f32x4 __attribute__((ext_vector_type(4)));
-
-// 4 consecutive elements of the update from element `at` on; those from
-// `left` on are zeros. With a step, momentum is brought up to date first
-// (FIRST) and read back later.
-template <bool FIRST>
-__device__ __forceinline__ f32x4 update4(const OrthArgs &a, int64_t at, int left) {
-    f32x4 u = {0.f, 0.f, 0.f, 0.f};
-    if (left >= 4 && a.vec) {
-        f32x4 g;
-        if (a.f32) {
-            g = *(const f32x4 *)((const float *)a.g + at);
-        } else {
-            const ushort4 h = *(const ushort4 *)((const u16 *)a.g + at);
-            g = f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
-        }
-        if (!a.step) return g;
-        f32x4 m = *(const f32x4 *)(a.m + at);
-        if (FIRST) {
-            m = a.beta * m + g;
-            *(f32x4 *)(a.m + at) = m;
-        }
-        return a.nesterov ? g + a.beta * m : m;
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if (i >= left) continue;
-        if (FIRST && a.step) a.m[at + i] = a.beta * a.m[at + i] + ((const float *)a.g)[at + i];
-        u[i] = update_at(a, at + i);
-    }
-    return u;
-}
 
 // Partial Gram matrices. A workgroup takes stretches of 64 positions of the
 // long axis through LDS ([n][64], row pitch 66 doubles' worth of banks), its

@@ -19,9 +19,10 @@ enum MmEpi {
     EPI_SCALED = 1, // out[perm[m]][n] = v * 2^-(ea[m] + eb[n]) + low-rank part + bias[n], float32
     EPI_GRAM = 2,   // S = v * 2^-26, stored * 2^11 as planes, with its mirror image
     EPI_POLY = 3,   // M = b l^2 S + c l^4 v 2^-22, stored * 2^14 as planes, with its mirror image
-    EPI_NEXT = 4,   // X = f (a X + v * 2^-27), stored * 2^13 as planes, in both layouts
-    EPI_ORTH = 5,   // out[m][n] = l (a X + v * 2^-27), in the context's type
-    EPI_STEP = 6    // w = (1 - decay) w - rate * l (a X + v * 2^-27), and its copy
+    EPI_NEXT = 4,   // X = f (cs X + cv v), in plane units (2^13), in both layouts
+    EPI_ORTH = 5,   // out[m][n] = l 2^-13 (cs X + cv v), in the context's type
+    EPI_STEP = 6,   // w = (1 - decay) w - rate * l 2^-13 (cs X + cv v), and its copy
+    EPI_MIX = 7     // f (cs S + cs2 S2 + cv v), in plane units, with its mirror image
 };
 
 // 16-bit planes of a matrix: hi, and lo (the rest; null = not kept). Rows of
@@ -42,17 +43,20 @@ struct MmOut {
     // SCALED: low-rank part, sum over r of t[m][r] * bx[run][r][n], rows of
     // ldbx (a multiple of 4)
     const float *t, *bx;
+    const int *run_rank;
     int rp;
     int64_t ldbx;
-    Planes p, q;          // GRAM, POLY: p; NEXT: p = [m][n], q = [n][m]
-    Planes s;             // POLY: S; NEXT, ORTH, STEP: X as the product's rows lie
+    Planes p, q;          // GRAM, POLY, MIX: p; NEXT: p = [m][n], q = [n][m]
+    Planes s, s2;         // POLY, MIX: S; NEXT, ORTH, STEP: X as the product's rows lie
+    float cs, cs2, cv;
+    int lambdas;          // f = lambda[0] / lambda[lambdas], MIX: squared (0: 1)
     // diagonals of S and M, kept unrounded where these are single planes
     // ([batch][diag_z]): GRAM and POLY write theirs, POLY reads S's, NEXT,
     // ORTH and STEP read M's, by output row or column
     float *sdiag, *mdiag;
     int64_t diag_z;
     int diag_rows;
-    const float *lambda;  // l of each matrix, ORTH_LAMBDAS apart; f = lambda[0] / lambda[1]
+    const float *lambda;  // l of each matrix, ORTH_LAMBDAS apart
     u16 *copy;            // STEP: bf16 copy of w or null
     float rate, decay;    // STEP
 };
@@ -86,7 +90,7 @@ struct MmArgs {
 // Longest rows: a tile's byte offsets fit 32 bits (and with a row table the
 // whole matrix's: perm_rows * lda up to 2^30 elements).
 constexpr int64_t MM_MAX_LD = 1 << 22;
-void mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape
+double mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape; the microseconds expected
 hipError_t launch_mm(const MmArgs &a, hipStream_t s);
 
 constexpr int ROWS_MAX = 64;   // rows that launch_rows takes

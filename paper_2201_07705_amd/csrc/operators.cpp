@@ -496,6 +496,7 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, fl
         operands(c, m, p.c_in, p.c_w);
         m.o.t = p.t;
         m.o.bx = c.at<float>(p.o_bank);
+        m.o.run_rank = b.run_rank;
         m.o.rp = rp;
         m.o.ldbx = op_round_up(p.N, 4);
     } else {
@@ -842,9 +843,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
 gemel_status orthogonal_thin(Call &c, OrthArgs o) {
     gemel_ctx *ctx = c.ctx;
     const int n = std::min(o.rows, o.cols), m = std::max(o.rows, o.cols), np = (int)op_round_up(n, 16);
-    const int64_t e = o.f32 ? 16 : 8;
-    o.vec = o.cols % 4 == 0 && (uintptr_t)o.g % e == 0 && (uintptr_t)o.m % 16 == 0 &&
-            (uintptr_t)o.out % (o.step ? 16 : e) == 0 && (uintptr_t)o.copy % 8 == 0;
     // stretches of 64 positions for each workgroup: enough workgroups for
     // two on each compute unit, few enough that one adds their sums
     o.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(m + 63) / 64, 64, (1024 + o.count - 1) / o.count}));
@@ -864,6 +862,12 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
 // M = b S + c S^2, X <- a X + M X. All operands are read along their rows,
 // so X is kept in both layouts and S and M, being symmetric, in one.
 //
+// Where it costs less, two steps share S: with P = a I + M, S' = P S P
+// follows from S alone, and X moves on by P' P = a^2 I + Mq at once. What S
+// has lost to rounding then grows by one more polynomial, up to 12 times,
+// which pairs can afford (2^-22 of S, spread over a whole row) and longer
+// chains could not (485 times after five).
+//
 // bf16 updates take one float16 product where float32 ones take three (hi hi,
 // hi lo, lo hi). What rounding would cost them is in a X: noise of 2^-12 of
 // X's large directions, spread over all small ones, would grow with these up
@@ -873,6 +877,9 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
 // is nearly orthogonal these are most of S and M.
 gemel_status orthogonal(Call &c, OrthArgs o) {
     gemel_ctx *ctx = c.ctx;
+    const int64_t bytes4 = o.f32 ? 16 : 8;
+    o.vec = o.cols % 4 == 0 && (uintptr_t)o.g % bytes4 == 0 && (uintptr_t)o.m % 16 == 0 &&
+            (uintptr_t)o.out % (o.step ? 16 : bytes4) == 0 && (uintptr_t)o.copy % 8 == 0;
     if (std::min(o.rows, o.cols) <= THIN_MAX) return orthogonal_thin(c, o);
     const int steps = o.steps;
     const bool step = o.step;
@@ -881,7 +888,7 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     const bool lo = step || o.f32, wide = o.rows <= o.cols;
     const int all = o.count;
     // matrices at a time: planes of at most 4 GiB
-    const int64_t each = 12 * np * mp + 4 * np * (np + 64);
+    const int64_t each = 12 * np * mp + 20 * np * np;
     const int group = (int)std::max<int64_t>(1, std::min<int64_t>(all, (int64_t)(4ll << 30) / each));
     auto planes = [&](int64_t rows, int64_t ld, bool rest) {
         Planes p{nullptr, nullptr, ld, rows * ld};
@@ -892,10 +899,11 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     };
     Planes x = planes(n, mp, true), t0 = planes(m, np, true), t1 = planes(m, np, true), s = planes(n, np, lo),
            p = planes(n, np, lo);
-    o.parts = (int)std::min<int64_t>(256, (size + 4095) / 4096);
+    o.parts = (int)std::min<int64_t>(1024, (size + 4095) / 4096);
     const size_t o_sums = c.lay.take((int64_t)group * o.parts, 8), o_lambda = c.lay.take(group * ORTH_LAMBDAS, 4),
                  o_sd = c.lay.take(lo ? 0 : group * np, 4), o_md = c.lay.take(lo ? 0 : group * np, 4);
-    MmArgs gram{}, poly{}, next{}, last{};
+    MmArgs gram{}, poly{}, next{}, last{}, mix{};
+    int64_t part = 0;
     auto shape = [&](MmArgs &a, int M, int N, int64_t K, int epi, bool sym) {
         a.M = M;
         a.N = N;
@@ -905,36 +913,49 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         a.f16 = 1;
         a.epi = epi;
         a.sym = sym;
-        mm_plan(a);
-        return partial_floats(a);
+        const double us = mm_plan(a);
+        part = std::max(part, partial_floats(a));
+        return us;
     };
-    int64_t part = shape(gram, n, n, mp, EPI_GRAM, true);
-    part = std::max(part, shape(poly, n, n, np, EPI_POLY, true));
-    part = std::max(part, shape(next, m, n, np, EPI_NEXT, false));
-    part = std::max(part, wide ? shape(last, n, m, np, step ? EPI_STEP : EPI_ORTH, false)
-                               : shape(last, m, n, np, step ? EPI_STEP : EPI_ORTH, false));
+    const int final = step ? EPI_STEP : EPI_ORTH;
+    const double us_gram = shape(gram, n, n, mp, EPI_GRAM, true), us_poly = shape(poly, n, n, np, EPI_POLY, true),
+                 us_next = shape(next, m, n, np, EPI_NEXT, false);
+    (void)(wide ? shape(last, n, m, np, final, false) : shape(last, m, n, np, final, false));
+    // two steps at once: a Gram matrix and an update of X less, three
+    // products of n x n matrices more
+    const bool paired = lo && steps > 1 && 3 * us_poly < us_gram + us_next;
+    Planes t{}, m0{}, q{};
+    if (paired) {
+        (void)shape(mix, n, n, np, EPI_MIX, true);
+        t = planes(n, np, true);
+        m0 = planes(n, np, true);
+        q = planes(n, np, true);
+    }
     const size_t o_part = c.lay.take(part, 4);
     if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return e;
-    for (Planes *q : {&x, &t0, &t1, &s, &p}) {
-        q->hi = c.at<u16>((size_t)q->hi);
-        q->lo = q->lo ? c.at<u16>((size_t)q->lo) : nullptr;
+    for (Planes *b : {&x, &t0, &t1, &s, &p, &t, &m0, &q}) {
+        if (!b->ld) continue;
+        b->hi = c.at<u16>((size_t)b->hi);
+        b->lo = b->lo ? c.at<u16>((size_t)b->lo) : nullptr;
     }
     o.sums = c.at<double>(o_sums);
     o.lambda = c.at<float>(o_lambda);
     const int64_t ge = o.f32 ? 4 : 2;
     const char *g0 = (const char *)o.g;
-    float *m0 = o.m;
+    float *mom0 = o.m;
+    const float A = (float)COEF_A;
     for (int at = 0; at < all; at += group) {
         const int count = std::min(group, all - at);
         o.count = count;
         o.g = g0 + at * size * ge;
-        o.m = m0 ? m0 + at * size : nullptr;
+        o.m = mom0 ? mom0 + at * size : nullptr;
         // a bf16 update is its own float16 plane
         o.x = x;
         o.xt = t0;
         if (!lo) o.x.lo = o.xt.lo = nullptr;
         OPCHK(launch_norm(o, c.stream), "norm");
         OPCHK(launch_seed(o, c.stream), "scaled update");
+        // l * r of one batch, into a
         auto planes_of = [&](MmArgs &a, const Planes &l, const Planes &r) {
             const u16 *al[3] = {l.hi, lo ? l.lo : nullptr, l.hi}, *bl[3] = {lo ? r.lo : r.hi, r.hi, r.hi};
             for (int i = 0; i < 3; ++i) {
@@ -952,33 +973,65 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
             a.o.mdiag = lo ? nullptr : c.at<float>(o_md);
             a.o.diag_z = np;
         };
+        auto polynomial = [&](int k, const Planes &to) {
+            planes_of(poly, s, s);
+            poly.o.s = s;
+            poly.o.p = to;
+            poly.o.lambda = o.lambda + k;
+            return launch_mm(poly, c.stream);
+        };
+        // to = f^2 (cs u + cs2 v + cv l r)
+        auto mixed = [&](const Planes &to, const Planes &l, const Planes &r, const Planes &u, float cs, const Planes &v, float cs2,
+                         float cv, int lambdas, int k) {
+            planes_of(mix, l, r);
+            mix.o.p = to;
+            mix.o.s = u;
+            mix.o.s2 = v;
+            mix.o.cs = cs;
+            mix.o.cs2 = cs2;
+            mix.o.cv = cv;
+            mix.o.lambdas = lambdas;
+            mix.o.lambda = o.lambda + k;
+            return launch_mm(mix, c.stream);
+        };
         Planes from = o.xt, to = t1, now = o.x;
-        for (int k = 0; k < steps; ++k) {
+        for (int k = 0; k < steps;) {
+            const int by = paired && k + 2 <= steps ? 2 : 1;
             planes_of(gram, now, now);
             gram.o.p = s;
             OPCHK(launch_mm(gram, c.stream), "product");
-            planes_of(poly, s, s);
-            poly.o.s = s;
-            poly.o.p = p;
-            poly.o.lambda = o.lambda + k;
-            OPCHK(launch_mm(poly, c.stream), "product");
-            if (k + 1 < steps) {
-                planes_of(next, from, p);
+            const Planes *mul = &p;
+            if (by == 2) {
+                OPCHK(polynomial(k, m0), "product");
+                OPCHK(mixed(t, m0, s, s, A, s, 0.f, 0x1p-14f, 0, k), "product");            // P S
+                OPCHK(mixed(s, t, m0, t, A, t, 0.f, 0x1p-14f, 1, k), "product");            // f^2 P S P
+                OPCHK(polynomial(k + 1, p), "product");
+                OPCHK(mixed(q, p, m0, p, A * 0.25f, m0, A * 0.25f, 0x1p-16f, 0, k), "product");    // P' P - a^2 I, * 2^12
+                mul = &q;
+            } else {
+                OPCHK(polynomial(k, p), "product");
+            }
+            const float cs = by == 2 ? A * A : A, cv = by == 2 ? 0x1p-12f : 0x1p-14f;
+            if (k + by < steps) {
+                planes_of(next, from, *mul);
                 next.o.s = from;
                 next.o.p = to;
                 now = x;
                 if (!lo && (!wide || k + 2 < steps)) now.lo = nullptr;   // nobody reads it
                 next.o.q = now;
                 next.o.lambda = o.lambda + k;
+                next.o.lambdas = by;
+                next.o.cs = cs;
+                next.o.cv = cv;
                 OPCHK(launch_mm(next, c.stream), "product");
                 const Planes read = from.lo ? from : t0;
                 from = to;
                 to = read;
             } else {
                 if (wide)
-                    planes_of(last, p, from);
+                    planes_of(last, *mul, from);
                 else
-                    planes_of(last, from, p);
+                    planes_of(last, from, *mul);
                 last.o.s = wide ? now : from;
                 last.o.diag_rows = wide;
                 last.o.ld = o.cols;
@@ -989,9 +1042,12 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
                 last.o.rate = o.rate;
                 last.o.decay = o.decay;
                 last.o.lambda = o.lambda + k;
+                last.o.cs = cs;
+                last.o.cv = cv;
                 last.o.vec = o.cols % 4 == 0 && (uintptr_t)last.o.out % 16 == 0 && (uintptr_t)last.o.copy % 8 == 0;
                 OPCHK(launch_mm(last, c.stream), "product");
             }
+            k += by;
         }
     }
     return GEMEL_OK;
