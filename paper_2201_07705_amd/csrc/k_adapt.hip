@@ -127,39 +127,46 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
     }
 }
 
-// part[r][c] = sum over a chunk's positions of p[pos][r] q[row][c] for RB
-// blocks of 16 rank indices and 4 * CT columns, 32 positions at a time. The
-// matrix cores want 8 positions of a column (or rank index) in a lane, so
-// both operands are turned on the way out of LDS. p is float32: beside bf16
-// q it is multiplied as three bf16 pieces, which hold all of its bits;
-// beside float32 q on the float32 MFMA. The next 32 positions are in
-// registers while the present ones are multiplied; reading q bounds it.
-template <bool F32, int RB>
-__global__ __launch_bounds__(256) void outer_kernel(const Two<OuterArgs> args) {
-    const OuterArgs &a = arg_of<OuterArgs>(blockIdx.y & 1);
-    constexpr int E = F32 ? 4 : 2, CT = F32 ? 32 : 64, COLS = 4 * CT, FC = CT / 16;
+// out[r][c] = sum over a chunk's positions of p(pos, r) q[row][c] for 32 r
+// and 4 * CT columns, 32 positions at a time. The matrix cores want 8
+// positions of a column (or of an r) in a lane, so both operands are turned
+// on the way out of LDS. A float32 p beside bf16 q is multiplied as three
+// bf16 pieces, which hold all of its bits; float32 q goes to the float32
+// MFMA. The next 32 positions are in registers while the present ones are
+// multiplied; reading q (or writing out) bounds it.
+template <bool F32, bool P32>
+__device__ __forceinline__ void outer(const OuterArgs &a, int block, unsigned char *qs, float *ps) {
+    constexpr int RB = 2, E = F32 ? 4 : 2, CT = F32 ? 32 : 64, COLS = 4 * CT, FC = CT / 16, PIECES = P32 ? 3 : 1;
     constexpr int PITCH = COLS * E + 16, PP = RB * 16 + 1;   // bytes; floats
-    __shared__ __attribute__((aligned(16))) unsigned char qs[32 * PITCH];
-    __shared__ float ps[32 * PP];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l16 = lane & 15;
-    const int c0 = blockIdx.x * COLS, r0 = (blockIdx.y >> 1) * 16 * RB;
-    if (c0 >= a.C || r0 >= a.rp) return;
-    const int *ch = a.b.chunks + 3 * blockIdx.z;
-    const int p0 = ch[1], n = ch[2];
+    const int across = (a.C + COLS - 1) / COLS, down = (a.R + 31) / 32;
+    const int bx = block % across, by = block / across % down, bz = block / (across * down);
+    const int c0 = bx * COLS, r0 = by * 32;
+    const int p0 = a.chunks ? a.chunks[3 * bz + 1] : bz * a.per;
+    const int n = a.chunks ? a.chunks[3 * bz + 2] : min(a.per, a.positions - p0);
     constexpr int Q = 16 / E, LR = COLS / Q, NQ = 32 * LR / 256, NP = 32 * RB * 16 / 256;
     uint4 q[NQ];
     float p[NP];
+    // items of p along whichever of its indices is contiguous
+    const bool along = a.sr == 1;
+    auto p_row = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) / 32 : (i * 256 + tid) % 32; };
+    auto p_col = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) % 32 : (i * 256 + tid) / 32; };
     auto load = [&](int s) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i) {
             const int row = (i * 256 + tid) / LR, c = c0 + (tid % LR) * Q;
             const bool in = s + row < n;
-            q[i] = chunk<F32>(a.q, in ? (int64_t)a.b.perm[p0 + s + row] * a.ldq : 0, c, in ? a.C : 0, a.vq);
+            const int pos = p0 + s + row;
+            q[i] = chunk<F32>(a.q, in ? (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq : 0, c, in ? a.C : 0, a.vq);
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {
-            const int row = (i * 256 + tid) / (RB * 16), r = (i * 256 + tid) % (RB * 16);
-            p[i] = s + row < n && r0 + r < a.rp ? a.p[(int64_t)(p0 + s + row) * a.rp + r0 + r] : 0.f;
+            const int row = p_row(i), r = r0 + p_col(i);
+            p[i] = 0.f;
+            if (s + row < n && r < a.R) {
+                const int64_t at = (int64_t)(p0 + s + row) * a.sp + r * a.sr;
+                p[i] = P32 ? ((const float *)a.p)[at] : bf_up(((const u16 *)a.p)[at]);
+            }
         }
     };
     f32x4 acc[RB][FC];
@@ -173,7 +180,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const Two<OuterArgs> args) {
 #pragma unroll
         for (int i = 0; i < NQ; ++i) *(uint4 *)(qs + ((i * 256 + tid) / LR) * PITCH + (tid % LR) * 16) = q[i];
 #pragma unroll
-        for (int i = 0; i < NP; ++i) ps[((i * 256 + tid) / (RB * 16)) * PP + (i * 256 + tid) % (RB * 16)] = p[i];
+        for (int i = 0; i < NP; ++i) ps[p_row(i) * PP + p_col(i)] = p[i];
         __syncthreads();
         if (s + 32 < n) load(s + 32);
         if constexpr (F32) {
@@ -190,14 +197,14 @@ __global__ __launch_bounds__(256) void outer_kernel(const Two<OuterArgs> args) {
                     for (int j = 0; j < FC; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(x[i], y[j], acc[i][j], 0, 0, 0);
             }
         } else {
-            bf16x8 x[RB][3];
+            bf16x8 x[RB][PIECES];
 #pragma unroll
             for (int i = 0; i < RB; ++i)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
                     float v = ps[(8 * g + e) * PP + i * 16 + l16];
 #pragma unroll
-                    for (int w = 0; w < 3; ++w) {
+                    for (int w = 0; w < PIECES; ++w) {
                         x[i][w][e] = (__bf16)v;
                         v -= (float)x[i][w][e];
                     }
@@ -211,10 +218,12 @@ __global__ __launch_bounds__(256) void outer_kernel(const Two<OuterArgs> args) {
 #pragma unroll
                 for (int i = 0; i < RB; ++i)
 #pragma unroll
-                    for (int w = 2; w >= 0; --w) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][w], y, acc[i][j], 0, 0, 0);
+                    for (int w = PIECES - 1; w >= 0; --w)
+                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[i][w], y, acc[i][j], 0, 0, 0);
             }
         }
     }
+    float *out = a.out + bz * a.chunk;
 #pragma unroll
     for (int j = 0; j < FC; ++j) {
         const int c = c0 + wave * CT + j * 16 + l16;
@@ -224,9 +233,25 @@ __global__ __launch_bounds__(256) void outer_kernel(const Two<OuterArgs> args) {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int r = r0 + i * 16 + 4 * g + e;
-                if (r < a.rp) a.part[((int64_t)blockIdx.z * a.rp + r) * a.C + c] = acc[i][j][e];
+                if (r < a.R) out[r * a.ld + c] = acc[i][j][e];
             }
     }
+}
+
+// Several such products in one launch.
+template <bool F32>
+__global__ __launch_bounds__(256) void outer_kernel(const Outers args) {
+    __shared__ __attribute__((aligned(16))) unsigned char qs[32 * (512 + 16)];
+    __shared__ float ps[32 * 33];
+    const Outers &all = *(const Outers *)__builtin_amdgcn_kernarg_segment_ptr();
+    int i = 0;
+    while (i + 1 < all.n && (int)blockIdx.x >= all.first[i + 1]) ++i;
+    const OuterArgs &a = all.a[i];
+    const int block = (int)blockIdx.x - all.first[i];
+    if (F32 || a.p_f32)
+        outer<F32, true>(a, block, qs, ps);
+    else
+        outer<F32, F32>(a, block, qs, ps);
 }
 
 bool tables(const BatchTables &b) {
@@ -254,23 +279,28 @@ hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
                     : launch(reinterpret_cast<const void *>(&shrink_kernel<false, 2>), grid, 512, a, n, s);
 }
 
-hipError_t launch_outer(const OuterArgs *a, int n, hipStream_t s) {
-    if (n < 1 || n > 2) return hipErrorInvalidValue;
-    int C = 0;
-    for (int i = 0; i < n; ++i) {
-        if (!tables(a[i].b) || !a[i].p || !a[i].q || !a[i].part || a[i].C <= 0 || a[i].rp % 32 || a[i].rp < a[i].b.rank ||
-            a[i].b.n_chunks > 65535 || a[i].b.n_chunks < 1 || a[i].rp != a[0].rp || a[i].f32 != a[0].f32 ||
-            a[i].b.chunks != a[0].b.chunks)
-            return hipErrorInvalidValue;
-        C = std::max(C, a[i].C);
-    }
-    const int cols = a[0].f32 ? 128 : 256;
-    // (grid.y: which of the two, then the rank blocks)
-    OuterArgs two[2] = {a[0], a[n - 1]};
-    if (n == 1) two[1].C = 0;
-    const dim3 grid((unsigned)((C + cols - 1) / cols), (unsigned)(2 * (a[0].rp / 32)), (unsigned)a[0].b.n_chunks);
-    return a[0].f32 ? launch(reinterpret_cast<const void *>(&outer_kernel<true, 2>), grid, 256, two, 2, s)
-                    : launch(reinterpret_cast<const void *>(&outer_kernel<false, 2>), grid, 256, two, 2, s);
+bool add_outer(Outers &o, const OuterArgs &a) {
+    if (o.n >= MAX_OUTER || !a.p || !a.q || !a.out || a.R < 1 || a.C < 1 || a.n_chunks < 1 || (a.sp != 1 && a.sr != 1) ||
+        a.ld < a.C || (a.q_f32 && !a.p_f32) || (o.n && a.q_f32 != o.a[0].q_f32) ||
+        (!a.chunks && (a.per < 1 || a.positions < 1 || (int64_t)a.n_chunks * a.per < a.positions ||
+                       (int64_t)(a.n_chunks - 1) * a.per >= a.positions)))
+        return false;
+    const int cols = a.q_f32 ? 128 : 256;
+    const int64_t blocks = (int64_t)((a.C + cols - 1) / cols) * ((a.R + 31) / 32) * a.n_chunks;
+    if (blocks + o.blocks > 0x7fffff00) return false;
+    o.a[o.n] = a;
+    o.first[o.n] = o.blocks;
+    o.blocks += (int)blocks;
+    o.first[++o.n] = o.blocks;
+    return true;
+}
+
+hipError_t launch_outer(const Outers &o, hipStream_t s) {
+    if (o.n == 0) return hipSuccess;
+    void *p[] = {const_cast<Outers *>(&o)};
+    return hipLaunchKernel(o.a[0].q_f32 ? reinterpret_cast<const void *>(&outer_kernel<true>)
+                                        : reinterpret_cast<const void *>(&outer_kernel<false>),
+                           dim3((unsigned)o.blocks), dim3(256), p, 0, s);
 }
 
 }  // namespace gemel

@@ -255,6 +255,46 @@ __device__ __forceinline__ void chunks(const Job &j, int block, unsigned char *l
     }
 }
 
+// 1024 columns of a row per block
+__device__ __forceinline__ void rows(const Job &j, int block, unsigned char *lds) {
+    float *const ts = (float *)lds;   // [256]
+    const int across = (j.cols + 1023) / 1024, row = block / across, c = (block % across * 256 + threadIdx.x) * 4;
+    const int4 info = j.row_info[row];   // position, run or -1, adapter, rank
+    const int rank = j.t && info.y >= 0 ? info.w : 0, left = j.cols - c;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0) {
+#pragma unroll 8
+        for (int p = 0; p < j.parts; ++p) v += *(const f32x4 *)(j.sum + ((int64_t)p * j.rows + row) * j.ldi + c);
+    }
+    if ((int)threadIdx.x < rank) ts[threadIdx.x] = j.t[(int64_t)info.x * j.rp + threadIdx.x];
+    __syncthreads();
+    if (left <= 0) return;
+#pragma unroll 4
+    for (int r = 0; r < rank; ++r) {
+        const int64_t at = ((int64_t)info.z * j.R + r) * j.cols + c;
+        f32x4 x;
+        if (j.f32) {
+            x = load4((const float *)j.in + at, left, j.vec);
+        } else if (j.vec && left >= 4) {
+            const ushort4 h = *(const ushort4 *)((const u16 *)j.in + at);
+            x = f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = i < left ? bf_up(((const u16 *)j.in)[at + i]) : 0.f;
+        }
+        v += ts[r] * x;
+    }
+    const int64_t to = row * j.ldo + c;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if (i >= left) continue;
+        if (j.f32)
+            ((float *)j.out)[to + i] = v[i];
+        else
+            ((u16 *)j.out)[to + i] = __builtin_bit_cast(u16, (__bf16)v[i]);
+    }
+}
+
 __global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
     __shared__ __attribute__((aligned(16))) unsigned char lds[64 * 65 * 4 + 16 + 1024 + 256];
     // (a uniform index into the argument block where it lies)
@@ -282,6 +322,7 @@ __global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
         case JOB_COLADD: coladd(j, block, lds); break;
         case JOB_PACK: pack(j, block); break;
         case JOB_CHUNKS: chunks(j, block, lds); break;
+        case JOB_ROWS: rows(j, block, lds); break;
     }
 }
 
@@ -329,6 +370,11 @@ bool add_job(Jobs &all, const Job &in) {
         case JOB_CHUNKS:
             ok = ok && j.sum && j.out && j.run_of && j.run_rank && j.chunk_first && j.R > 0 && j.rp >= j.R && j.n > 0;
             blocks = across * j.n;
+            break;
+        case JOB_ROWS:
+            ok = ok && j.sum && j.out && j.row_info && j.rows > 0 && j.rows <= ROWS_MAX && j.parts > 0 && j.ldi >= j.cols &&
+                 j.ldi % 4 == 0 && j.ldo >= j.cols && (!j.t || (j.in && j.R > 0 && j.R <= 256 && j.rp >= j.R));
+            blocks = (((int64_t)j.cols + 1023) / 1024) * j.rows;
             break;
         default: ok = false;
     }

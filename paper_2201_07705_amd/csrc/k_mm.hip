@@ -34,49 +34,64 @@ __device__ __forceinline__ u16 to_half(float f) { return __builtin_bit_cast(u16,
 __device__ __forceinline__ f32x4 half_up4(ushort4 h) {
     return f32x4{half_up(h.x), half_up(h.y), half_up(h.z), half_up(h.w)};
 }
-// Four values of a matrix kept as float16 planes: the nearest halves, and
-// the rest of each value in a second half (22 bits together).
-__device__ __forceinline__ void put4(const Planes &p, int64_t at, f32x4 v) {
-    const ushort4 h = make_ushort4(to_half(v[0]), to_half(v[1]), to_half(v[2]), to_half(v[3]));
-    *(ushort4 *)(p.hi + at) = h;
-    if (p.lo) {
-        const f32x4 r = v - half_up4(h);
-        *(ushort4 *)(p.lo + at) = make_ushort4(to_half(r[0]), to_half(r[1]), to_half(r[2]), to_half(r[3]));
-    }
-}
-
-// Elements (m, n .. n + 3) of a matrix in planes; rows are padded to 64, so
-// 4 elements stay in a row, and rows beyond the last one read the last one.
-__device__ __forceinline__ void at4(const Planes &p, int z, int m, int n, int rows, f32x4 &hi, f32x4 &lo) {
-    const int64_t at = (int64_t)z * p.z + (int64_t)min(m, rows - 1) * p.ld + min(n, (int)p.ld - 4);
-    hi = half_up4(*(const ushort4 *)(p.hi + at));
-    lo = p.lo ? half_up4(*(const ushort4 *)(p.lo + at)) : f32x4{0.f, 0.f, 0.f, 0.f};
-}
 __device__ __forceinline__ f32x4 rest4(f32x4 v) {
     return f32x4{v[0] - half_up(to_half(v[0])), v[1] - half_up(to_half(v[1])), v[2] - half_up(to_half(v[2])),
                  v[3] - half_up(to_half(v[3]))};
 }
 
-// cs X + cv v at (m, n .. n + 3) in X's plane units (a X + M X, v being the
-// product of the planes). Where M is a single plane, what its diagonal (most of M once X
-// is nearly orthogonal) and X have lost to rounding is put back.
-__device__ __forceinline__ f32x4 next4(const MmArgs &a, int z, int m, int n, f32x4 v) {
-    const MmOut &o = a.o;
-    f32x4 hi, lo;
-    at4(o.s, z, m, n, a.M, hi, lo);
-    f32x4 x = o.cs * (hi + lo) + o.cv * v;
-    if (o.mdiag) {
-        const float *d = o.mdiag + z * o.diag_z;
-        f32x4 md;
-        if (o.diag_rows) {
-            const float r = d[min(m, a.M - 1)];
-            md = f32x4{r, r, r, r};
-        } else {
-            md = *(const f32x4 *)(d + min(n, (int)o.diag_z - 4));
-        }
-        x += 0x1p-14f * (rest4(md) * hi + md * lo);
+// Where an epilogue works: the first element of the tile, and whether the
+// whole tile lies inside the result: then addresses are a uniform base and a
+// 32-bit offset, and nothing is clamped or masked.
+struct Tile {
+    int z, m0, n0;
+    bool inside;
+};
+// The byte offset of element (m, n) of the tile in a matrix of `bytes` each.
+__device__ __forceinline__ uint32_t offset_of(int m, int n, int64_t ld, int bytes) {
+    return ((uint32_t)m * (uint32_t)ld + (uint32_t)n) * (uint32_t)bytes;
+}
+template <typename P>
+__device__ __forceinline__ P *at_tile(P *p, const Tile &t, int64_t z, int64_t ld) {
+    return p + (int64_t)t.z * z + (int64_t)t.m0 * ld + t.n0;
+}
+template <typename V>
+__device__ __forceinline__ V load_at(const void *base, uint32_t off) {
+    return *(const V *)((const char *)base + off);
+}
+template <typename V>
+__device__ __forceinline__ void store_at(void *base, uint32_t off, V v) {
+    *(V *)((char *)base + off) = v;
+}
+// Elements (m, n .. n + 3) of the tile of a matrix in planes; rows are padded
+// to 64, so 4 elements stay in a row, and rows beyond the last one read it.
+__device__ __forceinline__ void at4(const Planes &p, const Tile &t, int m, int n, int rows, f32x4 &hi, f32x4 &lo) {
+    lo = f32x4{0.f, 0.f, 0.f, 0.f};
+    if (t.inside) {
+        const uint32_t off = offset_of(m, n, p.ld, 2);
+        hi = half_up4(load_at<ushort4>(at_tile(p.hi, t, p.z, p.ld), off));
+        if (p.lo) lo = half_up4(load_at<ushort4>(at_tile(p.lo, t, p.z, p.ld), off));
+    } else {
+        const int64_t at = (int64_t)t.z * p.z + (int64_t)min(t.m0 + m, rows - 1) * p.ld + min(t.n0 + n, (int)p.ld - 4);
+        hi = half_up4(*(const ushort4 *)(p.hi + at));
+        if (p.lo) lo = half_up4(*(const ushort4 *)(p.lo + at));
     }
-    return x;
+}
+
+// Values of a matrix kept as float16 planes, as pairs: the nearest half, and
+// above it the rest of the value in a second half (22 bits together).
+__device__ __forceinline__ uint4 pairs(f32x4 v) {
+    uint4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const u16 h = to_half(v[i]);
+        (&r.x)[i] = h | (uint32_t)to_half(v[i] - half_up(h)) << 16;
+    }
+    return r;
+}
+__device__ __forceinline__ void put_pairs(u16 *hi, u16 *lo, uint32_t off, uint4 v) {
+    store_at(hi, off, make_uint2(__builtin_amdgcn_perm(v.y, v.x, 0x05040100), __builtin_amdgcn_perm(v.w, v.z, 0x05040100)));
+    if (lo)
+        store_at(lo, off, make_uint2(__builtin_amdgcn_perm(v.y, v.x, 0x07060302), __builtin_amdgcn_perm(v.w, v.z, 0x07060302)));
 }
 
 // One operand's loads of a step: 16 bytes at base + off[i] into the wave's
@@ -130,117 +145,181 @@ __device__ __forceinline__ void mm_place(const MmArgs &a, int &tm, int &tn) {
     tm = first + in - tn * rows;
 }
 
-// The epilogue of elements (m, n .. n + 3) of batch entry z. M and N are the
-// product's; planes are written up to their padded row lengths, with zeros
-// beyond M and N, because later products read them in steps of 64.
+// What the epilogue of elements (m, n .. n + 3) of the tile reads, gathered
+// before any of a group's results are stored.
+struct Near {
+    f32x4 hi, lo;   // a matrix in planes (MIX: lo is the second matrix)
+    f32x4 w;        // a diagonal, the weights, or the bias
+    float d;        // POLY: the diagonal at m
+    int row, e;     // ROWS, SCALED: output row; SCALED: its exponent
+};
 template <int EPI>
-__device__ __forceinline__ f32x4 finish(const MmArgs &a, int z, int m, int n, f32x4 v) {
+__device__ __forceinline__ Near gather(const MmArgs &a, const Tile &t, int m, int n) {
     const MmOut &o = a.o;
+    Near r;
     if constexpr (EPI == EPI_ROWS || EPI == EPI_SCALED) {
-        if (m >= a.M || n >= a.N) return v;
-        const int64_t at = (int64_t)(o.perm ? o.perm[m] : m) * o.ld + n;
+        const int mc = min(t.m0 + m, a.M - 1);
+        r.row = o.perm ? o.perm[mc] : mc;
+        if constexpr (EPI == EPI_SCALED) r.e = o.ea[mc];
+        r.w = f32x4{0.f, 0.f, 0.f, 0.f};
+        if (o.bias)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int j = min(n + i, a.N - 1);
-            if constexpr (EPI == EPI_SCALED) v[i] = ldexpf(v[i], -(o.ea[m] + o.eb[j]));
-            if (o.bias) v[i] += o.bias[j];
+            for (int i = 0; i < 4; ++i) r.w[i] = o.bias[min(t.n0 + n + i, a.N - 1)];
+    } else if constexpr (EPI == EPI_POLY) {
+        at4(o.s, t, m, n, a.M, r.hi, r.lo);
+        if (o.sdiag) {
+            const float *d = o.sdiag + t.z * o.diag_z;
+            r.w = *(const f32x4 *)(d + min(t.n0 + n, (int)o.diag_z - 4));
+            r.d = d[min(t.m0 + m, a.M - 1)];
         }
+    } else if constexpr (EPI == EPI_MIX) {
+        f32x4 lo;
+        at4(o.s2, t, m, n, a.M, r.lo, lo);
+        r.lo += lo;
+        at4(o.s, t, m, n, a.M, r.hi, lo);
+        r.hi += lo;
+    } else if constexpr (EPI != EPI_GRAM) {
+        at4(o.s, t, m, n, a.M, r.hi, r.lo);
+        if constexpr (EPI == EPI_STEP) {
+            if (o.vec && t.inside) {
+                r.w = load_at<f32x4>(at_tile((const float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4));
+            } else {
+                const float *w = (const float *)o.out + (int64_t)t.z * o.z + (int64_t)min(t.m0 + m, a.M - 1) * o.ld;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.w[i] = w[min(t.n0 + n + i, a.N - 1)];
+            }
+        } else if (o.mdiag) {
+            const float *d = o.mdiag + t.z * o.diag_z;
+            if (o.diag_rows) {
+                const float x = d[min(t.m0 + m, a.M - 1)];
+                r.w = f32x4{x, x, x, x};
+            } else {
+                r.w = *(const f32x4 *)(d + min(t.n0 + n, (int)o.diag_z - 4));
+            }
+        }
+    }
+    return r;
+}
+
+// The epilogue of elements (m, n .. n + 3) of the tile. M and N are the
+// product's; planes are written up to their padded row lengths, with zeros
+// beyond M and N, because later products read them in steps of 64. Returns
+// the plane pairs.
+template <int EPI>
+__device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, int n, f32x4 v, const Near &in) {
+    const MmOut &o = a.o;
+    const int left = a.N - t.n0 - n;                   // elements of the row from n on
+    const bool there = t.inside || (t.m0 + m < a.M && left > 0);
+    // cs X + cv v in X's plane units (a X + M X, v being the product of the
+    // planes). Where M is a single plane, what its diagonal (most of M once X
+    // is nearly orthogonal) and X have lost to rounding is put back.
+    if constexpr (EPI == EPI_NEXT || EPI == EPI_ORTH || EPI == EPI_STEP) {
+        v = o.cs * (in.hi + in.lo) + o.cv * v;
+        if constexpr (EPI != EPI_STEP)
+            if (o.mdiag) v += 0x1p-14f * (rest4(in.w) * in.hi + in.w * in.lo);
+    }
+    if constexpr (EPI == EPI_ROWS || EPI == EPI_SCALED) {
+        if (!there) return uint4{};
+        const int64_t at = (int64_t)in.row * o.ld + t.n0 + n;
         if constexpr (EPI == EPI_SCALED) {
-            if (a.runs > 0 && m >= a.run_start[0]) {
-                int u = a.first_run[m >> 6];
-                while (a.run_start[u + 1] <= m) ++u;
-                const float *t = o.t + (int64_t)m * o.rp, *bx = o.bx + (int64_t)u * o.rp * o.ldbx + n;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -(in.e + o.eb[min(t.n0 + n + i, a.N - 1)]));
+        }
+        v += in.w;
+        if constexpr (EPI == EPI_SCALED) {
+            const int p = t.m0 + m;
+            if (a.runs > 0 && p >= a.run_start[0]) {
+                int u = a.first_run[p >> 6];
+                while (a.run_start[u + 1] <= p) ++u;
+                const float *x = o.t + (int64_t)p * o.rp, *bx = o.bx + (int64_t)u * o.rp * o.ldbx + t.n0 + n;
                 // (zeros from the run's rank on, up to a multiple of 32)
                 for (int r = 0; r < o.run_rank[u]; r += 4) {
-                    const f32x4 t4 = *(const f32x4 *)(t + r);
+                    const f32x4 x4 = *(const f32x4 *)(x + r);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) v += t4[i] * *(const f32x4 *)(bx + (r + i) * o.ldbx);
+                    for (int i = 0; i < 4; ++i) v += x4[i] * *(const f32x4 *)(bx + (r + i) * o.ldbx);
                 }
             }
         }
         if (o.out_f32) {
             float *p = (float *)o.out + at;
-            if (o.vec && n + 3 < a.N) {
+            if (o.vec && left > 3) {
                 *(f32x4 *)p = v;
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (n + i < a.N) p[i] = v[i];
+                    if (i < left) p[i] = v[i];
             }
         } else {
             u16 *p = (u16 *)o.out + at;
-            if (o.vec && n + 3 < a.N) {
-                const ushort4 h = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
-                *(ushort4 *)p = h;
+            if (o.vec && left > 3) {
+                *(ushort4 *)p = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    if (n + i < a.N) p[i] = to_bf16(v[i]);
+                    if (i < left) p[i] = to_bf16(v[i]);
             }
         }
+        return uint4{};
     } else if constexpr (EPI == EPI_ORTH || EPI == EPI_STEP) {
-        if (m >= a.M || n >= a.N) return v;
-        const int64_t at = (int64_t)z * o.z + (int64_t)m * o.ld + n;
-        f32x4 x = o.lambda[z * ORTH_LAMBDAS] * 0x1p-13f * next4(a, z, m, n, v);
-        if (o.vec && n + 3 < a.N) {
-            if constexpr (EPI == EPI_STEP) x = (1.f - o.decay) * *(const f32x4 *)((float *)o.out + at) - o.rate * x;
-            if (EPI == EPI_STEP || o.out_f32) *(f32x4 *)((float *)o.out + at) = x;
-            u16 *h = EPI == EPI_STEP ? o.copy : o.out_f32 ? nullptr : (u16 *)o.out;
-            if (h) *(ushort4 *)(h + at) = make_ushort4(to_bf16(x[0]), to_bf16(x[1]), to_bf16(x[2]), to_bf16(x[3]));
+        if (!there) return uint4{};
+        f32x4 x = o.lambda[t.z * ORTH_LAMBDAS] * 0x1p-13f * v;
+        if constexpr (EPI == EPI_STEP) x = (1.f - o.decay) * in.w - o.rate * x;
+        const bool wide = EPI == EPI_STEP || o.out_f32;
+        u16 *const h = EPI == EPI_STEP ? o.copy : wide ? nullptr : (u16 *)o.out;
+        if (o.vec && left > 3) {
+            if (wide) store_at(at_tile((float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4), x);
+            if (h)
+                store_at(at_tile(h, t, o.z, o.ld), offset_of(m, n, o.ld, 2),
+                         make_ushort4(to_bf16(x[0]), to_bf16(x[1]), to_bf16(x[2]), to_bf16(x[3])));
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                if (n + i >= a.N) continue;
-                if constexpr (EPI == EPI_STEP) x[i] = (1.f - o.decay) * ((float *)o.out)[at + i] - o.rate * x[i];
-                if (EPI == EPI_STEP || o.out_f32) ((float *)o.out)[at + i] = x[i];
-                u16 *h = EPI == EPI_STEP ? o.copy : o.out_f32 ? nullptr : (u16 *)o.out;
-                if (h) h[at + i] = to_bf16(x[i]);
+                if (i >= left) continue;
+                if (wide) store_at(at_tile((float *)o.out, t, o.z, o.ld), offset_of(m, n + i, o.ld, 4), x[i]);
+                if (h) store_at(at_tile(h, t, o.z, o.ld), offset_of(m, n + i, o.ld, 2), to_bf16(x[i]));
             }
         }
+        return uint4{};
     } else {
         const Planes &p = o.p;
         f32x4 x;
         if constexpr (EPI == EPI_GRAM) {
             x = v * 0x1p-15f;
         } else if constexpr (EPI == EPI_POLY) {
-            const float l = o.lambda[z * ORTH_LAMBDAS], l2 = l * l;
-            f32x4 s, lo;
-            at4(o.s, z, m, n, a.M, s, lo);
+            const float l = o.lambda[t.z * ORTH_LAMBDAS], l2 = l * l;
+            f32x4 s = in.hi;
             if (o.sdiag) {
                 // S is its plane but for the diagonal
-                const float *d = o.sdiag + z * o.diag_z;
-                const f32x4 dn = *(const f32x4 *)(d + min(n, (int)o.diag_z - 4));
-                const float dm = d[min(m, a.M - 1)];
-                v += (dm - half_up(to_half(dm)) + rest4(dn)) * s;
+                v += (in.d - half_up(to_half(in.d)) + rest4(in.w)) * s;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) s[i] = m == n + i ? dm : s[i];
+                for (int i = 0; i < 4; ++i) s[i] = t.m0 + m == t.n0 + n + i ? in.d : s[i];
             } else {
-                s += lo;
+                s += in.lo;
             }
-            x = 0x1p14f * ((float)COEF_B * 0x1p-11f * l2 * s + (float)COEF_C * 0x1p-22f * l2 * l2 * v);
+            x = 0x1p14f * (float)COEF_B * 0x1p-11f * l2 * s + 0x1p14f * (float)COEF_C * 0x1p-22f * l2 * l2 * v;
         } else if constexpr (EPI == EPI_MIX) {
-            f32x4 hi, lo, hi2, lo2;
-            at4(o.s, z, m, n, a.M, hi, lo);
-            at4(o.s2, z, m, n, a.M, hi2, lo2);
-            x = o.cs * (hi + lo) + o.cs2 * (hi2 + lo2) + o.cv * v;
+            x = o.cs * in.hi + o.cs2 * in.lo + o.cv * v;
             if (o.lambdas) {
-                const float *l = o.lambda + z * ORTH_LAMBDAS, f = l[0] / l[o.lambdas];
+                const float *l = o.lambda + t.z * ORTH_LAMBDAS, f = l[0] / l[o.lambdas];
                 x *= f * f;
             }
         } else {
-            const float *l = o.lambda + z * ORTH_LAMBDAS;
-            x = l[0] / l[o.lambdas] * next4(a, z, m, n, v);
+            const float *l = o.lambda + t.z * ORTH_LAMBDAS;
+            x = l[0] / l[o.lambdas] * v;
         }
+        if (!t.inside)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[i] = m < a.M && n + i < a.N ? x[i] : 0.f;
+            for (int i = 0; i < 4; ++i) x[i] = t.m0 + m < a.M && i < left ? x[i] : 0.f;
         if constexpr (EPI == EPI_GRAM || EPI == EPI_POLY) {
             float *const d = EPI == EPI_GRAM ? o.sdiag : o.mdiag;
-            if (d && m >= n && m < n + 4 && m < a.M) d[z * o.diag_z + m] = m == n ? x[0] : m == n + 1 ? x[1] : m == n + 2 ? x[2] : x[3];
+            const int i = t.m0 + m - t.n0 - n;
+            if (d && i >= 0 && i < 4 && t.m0 + m < a.M) d[t.z * o.diag_z + t.m0 + m] = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
         }
-        if (m < a.M && n < p.ld) put4(p, (int64_t)z * p.z + (int64_t)m * p.ld + n, x);
-        return x;
+        const uint4 q = pairs(x);
+        if (t.inside || (t.m0 + m < a.M && t.n0 + n < p.ld))
+            put_pairs(at_tile(p.hi, t, p.z, p.ld), p.lo ? at_tile(p.lo, t, p.z, p.ld) : nullptr, offset_of(m, n, p.ld, 2), q);
+        return q;
     }
-    return v;
 }
 
 // One T x T output tile per workgroup: 8 waves of 128 x 64 (T = 256) or 32 x
@@ -490,29 +569,47 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         asm volatile("" ::: "memory");
         const bool turned = (EPI == EPI_NEXT || ((EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_MIX) && e.sym && tn > tm)) &&
                             e.splits == 1;
-        for (int it = lane; it < RP * C; it += 64) {
-            const int m = it / C, c = it & (C - 1);
-            f32x4 *const slot = (f32x4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16);
-            f32x4 v = *slot;
-            if (e.splits > 1) {
-                if (mb + m < e.M && nb + c * 4 < e.N)
-                    *(f32x4 *)(e.partial + (((int64_t)split * e.batch + z) * e.M + mb + m) * e.ldp + nb + c * 4) = v;
-            } else {
-                v = finish<EPI>(e, z, mb + m, nb + c * 4, v);
-                if (turned) *slot = v;
+        const Tile tile{z, mb, nb, mb + RP <= e.M && nb + TN <= e.N};
+        constexpr int ITEMS = RP * C / 64, GROUP = T == 256 ? (EPI == EPI_ROWS ? 1 : 2) : 4;   // (registers)
+        static_assert(ITEMS % GROUP == 0, "whole groups");
+#pragma unroll 1
+        for (int i0 = 0; i0 < ITEMS; i0 += GROUP) {
+            f32x4 v[GROUP];
+            Near near[GROUP];
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const int it = (i0 + i) * 64 + lane, m = it / C, c = it & (C - 1);
+                v[i] = *(const f32x4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16);
+                if (e.splits == 1) near[i] = gather<EPI>(e, tile, m, c * 4);
+            }
+#pragma unroll
+            for (int i = 0; i < GROUP; ++i) {
+                const int it = (i0 + i) * 64 + lane, m = it / C, c = it & (C - 1);
+                if (e.splits > 1) {
+                    if (mb + m < e.M && nb + c * 4 < e.N)
+                        store_at(e.partial + (((int64_t)split * e.batch + z) * e.M + mb) * e.ldp + nb,
+                                 offset_of(m, c * 4, e.ldp, 4), v[i]);
+                } else {
+                    const uint4 q = finish<EPI>(e, tile, m, c * 4, v[i], near[i]);
+                    if (turned) *(uint4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16) = q;
+                }
             }
         }
         if (!turned) continue;
         wait_lgkm0();
         asm volatile("" ::: "memory");
         const Planes &q = EPI == EPI_NEXT ? e.o.q : e.o.p;
-        for (int it = lane; it < TN * RP / 4; it += 64) {
+        u16 *const hi = q.hi + (int64_t)z * q.z + (int64_t)nb * q.ld + mb;
+        u16 *const lo = q.lo ? q.lo + (int64_t)z * q.z + (int64_t)nb * q.ld + mb : nullptr;
+#pragma unroll 1
+        for (int i = 0; i < TN * RP / 256; ++i) {
+            const int it = i * 64 + lane;
             const int n = it / (RP / 4), m = (it % (RP / 4)) * 4;
-            f32x4 v;
+            uint4 v;
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                v[i] = *(const float *)(mine + (m + i) * TN * 4 + ((n >> 2) ^ swz(m + i)) * 16 + (n & 3) * 4);
-            if (nb + n < e.N && mb + m < q.ld) put4(q, (int64_t)z * q.z + (int64_t)(nb + n) * q.ld + mb + m, v);
+            for (int k = 0; k < 4; ++k)
+                (&v.x)[k] = *(const uint32_t *)(mine + (m + k) * TN * 4 + ((n >> 2) ^ swz(m + k)) * 16 + (n & 3) * 4);
+            if (tile.inside || (nb + n < e.N && mb + m < q.ld)) put_pairs(hi, lo, offset_of(n, m, q.ld, 2), v);
         }
     }
 }
@@ -522,18 +619,21 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
 template <int EPI>
 __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
     constexpr bool PLANES = EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT || EPI == EPI_MIX;
-    __shared__ float tile[PLANES ? 64 : 1][65];
+    __shared__ uint32_t turn[PLANES ? 64 : 1][65];
     int tm, tn;
     mm_place<64>(a, tm, tn);
     const int z = blockIdx.z, m0 = tm * 64, n0 = tn * 64;
+    const Tile tile{z, m0, n0, m0 + 64 <= a.M && n0 + 64 <= a.N};
     const bool turned = EPI == EPI_NEXT || (PLANES && a.sym && tn > tm);
     f32x4 v[4];
+    Near near[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int m = m0 + i * 16 + (threadIdx.x >> 4), n = n0 + (threadIdx.x & 15) * 4;
+        const int m = i * 16 + (threadIdx.x >> 4), n = (threadIdx.x & 15) * 4;
+        near[i] = gather<EPI>(a, tile, m, n);
         v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (m < a.M && n < a.N) {
-            const float *p = a.partial + ((int64_t)z * a.M + m) * a.ldp + n;
+        if (m0 + m < a.M && n0 + n < a.N) {
+            const float *p = a.partial + ((int64_t)z * a.M + m0 + m) * a.ldp + n0 + n;
 #pragma unroll 4
             for (int s = 0; s < a.splits; ++s) v[i] += *(const f32x4 *)(p + (int64_t)s * a.batch * a.M * a.ldp);
         }
@@ -541,21 +641,23 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int m = i * 16 + (threadIdx.x >> 4), n = (threadIdx.x & 15) * 4;
-        v[i] = finish<EPI>(a, z, m0 + m, n0 + n, v[i]);
+        const uint4 q = finish<EPI>(a, tile, m, n, v[i], near[i]);
         if constexpr (PLANES)
             if (turned)
 #pragma unroll
-                for (int e = 0; e < 4; ++e) tile[m][n + e] = v[i][e];
+                for (int e = 0; e < 4; ++e) turn[m][n + e] = (&q.x)[e];
     }
     if constexpr (PLANES) {
         if (!turned) return;
         __syncthreads();
         const Planes &q = EPI == EPI_NEXT ? a.o.q : a.o.p;
+        u16 *const hi = q.hi + (int64_t)z * q.z + (int64_t)n0 * q.ld + m0;
+        u16 *const lo = q.lo ? q.lo + (int64_t)z * q.z + (int64_t)n0 * q.ld + m0 : nullptr;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int n = i * 16 + (threadIdx.x >> 4), m = (threadIdx.x & 15) * 4;
-            const f32x4 x = {tile[m][n], tile[m + 1][n], tile[m + 2][n], tile[m + 3][n]};
-            if (n0 + n < a.N && m0 + m < q.ld) put4(q, (int64_t)z * q.z + (int64_t)(n0 + n) * q.ld + m0 + m, x);
+            const uint4 x = make_uint4(turn[m][n], turn[m + 1][n], turn[m + 2][n], turn[m + 3][n]);
+            if (n0 + n < a.N && m0 + m < q.ld) put_pairs(hi, lo, offset_of(n, m, q.ld, 2), x);
         }
     }
 }
@@ -590,16 +692,17 @@ hipError_t pick(const MmArgs &a, hipStream_t s) {
 // for the pipeline's start and the epilogue; and, where the depth is split,
 // writing and reading the partial sums and the second launch. Measured steps
 // (microseconds, float16, workgroups on every compute unit): 64 x 64 tiles
-// 0.18 alone on a compute unit and 0.33 two at once, 128 x 128 0.6 and 0.8,
-// 256 x 256 1.65. A 512 x 512 result of depth 4608 takes 18.5 us unsplit and
-// 13.6 in 4 splits, a symmetric 4096 x 4096 one of depth 75264 1704 and 1117
+// 0.21 alone on a compute unit and 0.36 two at once, 128 x 128 0.62 and 0.95,
+// 256 x 256 1.65. A 512 x 512 result of depth 4608 takes 18.6 us unsplit and
+// 13.3 in 4 splits, a symmetric 4096 x 4096 one of depth 75264 1690 and 1210
 // us in 7 (its 136 tiles of 256 leave half of the 256 compute units idle).
 double mm_plan(MmArgs &a) {
     struct Form {
-        int tile, slots;                 // workgroups that run at once
-        double alone, full, fixed;       // microseconds
+        int tile, slots;                        // workgroups that run at once
+        double alone, full, fixed, fixed_part;  // microseconds; with partial sums out
     };
-    static const Form forms[] = {{256, 256, 1.65, 1.65, 8.0}, {128, 512, 0.6, 0.8, 6.5}, {64, 512, 0.18, 0.33, 5.5}};
+    static const Form forms[] = {
+        {256, 256, 1.65, 1.65, 28.0, 12.0}, {128, 512, 0.62, 0.95, 9.0, 7.0}, {64, 512, 0.21, 0.36, 5.5, 5.0}};
     const int steps = (a.K + BK - 1) / BK * a.nseg;
     double best = 1e30;
     for (const Form &f : forms) {
@@ -608,8 +711,9 @@ double mm_plan(MmArgs &a) {
             const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
             if (splits != want) continue;
             const int64_t groups = tiles * splits, whole = groups / f.slots, rest = groups % f.slots;
-            double us = (double)whole * (per * f.full + f.fixed);
-            if (rest) us += per * (rest > 256 ? f.full : f.alone) + f.fixed;
+            const double fixed = splits > 1 ? f.fixed_part : f.fixed;
+            double us = (double)whole * (per * f.full + fixed);
+            if (rest) us += per * (rest > 256 ? f.full : f.alone) + fixed;
             const double bytes = (double)splits * a.batch * a.M * op_round_up(a.N, 4) * (a.sym ? 2 : 4);
             if (splits > 1) us += 5.0 + 2 * bytes / 5.5e6;
             if (splits > 1 && bytes > 1e9) continue;

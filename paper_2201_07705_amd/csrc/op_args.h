@@ -147,16 +147,28 @@ struct ShrinkArgs {
 // One or two thin products (of one batch) in a launch.
 hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s);
 
-// part[chunk][r][c] = sum over the chunk's positions of p[pos][r] * q[perm[pos]][c]
+// out[chunk][r][c] = sum over the chunk's positions of p(pos, r) * q[perm[pos]][c],
+// p(pos, r) = p[pos * sp + r * sr], r < R, c < C.
 struct OuterArgs {
-    const float *p;        // [rows][rp]
+    const void *p;
     const void *q;
-    int64_t ldq;
-    int f32, C, rp, vq;    // vq: whole 16-byte chunks of q's rows may be loaded at once
-    float *part;           // [n_chunks][rp][C]
-    BatchTables b;
+    int64_t sp, sr, ldq;
+    int p_f32, q_f32;      // types (a float32 q goes with a float32 p)
+    int R, C, vq;          // vq: whole 16-byte chunks of q's rows may be loaded at once
+    const int *perm;       // or null
+    float *out;
+    int64_t ld, chunk;     // distance of rows, and of chunks
+    const int *chunks;     // [n_chunks][3]: .., first position, positions; null: `per` positions in each
+    int n_chunks, positions, per;
 };
-hipError_t launch_outer(const OuterArgs *a, int n, hipStream_t s);
+constexpr int MAX_OUTER = 4;
+struct Outers {
+    int n = 0, blocks = 0;
+    int first[MAX_OUTER + 1] = {};
+    OuterArgs a[MAX_OUTER];
+};
+bool add_outer(Outers &o, const OuterArgs &a);   // false: not valid
+hipError_t launch_outer(const Outers &o, hipStream_t s);
 
 // Small pieces of work around the products, several in one launch. Blocks of
 // one job do not depend on those of another.
@@ -181,7 +193,11 @@ enum JobKind {
     // out[adapter] = sum over its chunks of part [chunk][rp][C], as [R][C] or
     // (turned) [C][R]; zeros for adapters without rows, and from an
     // adapter's rank on
-    JOB_CHUNKS
+    JOB_CHUNKS,
+    // up to ROWS_MAX rows: out[r][c], rows ldo apart, = sum over parts of
+    // sum [part][rows][ldi] + sum over rank of t[position][rank] *
+    // in[adapter][rank][c], in the type f32 says
+    JOB_ROWS
 };
 struct Job {
     int kind, blocks, f32, rows, cols, parts;
@@ -196,6 +212,8 @@ struct Job {
     int vec;               // whole 16-byte chunks of the input may be loaded at once
     int in_rc, by_rank, turned, R, rp, n;   // PACK: n runs, CHUNKS: n adapters; columns in cols
     const int *run_id, *run_rank, *run_of, *chunk_first;
+    const int4 *row_info;
+    const float *t;
 };
 constexpr int MAX_JOBS = 6;
 struct Jobs {

@@ -703,11 +703,35 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     const int rp = (int)op_round_up(b.rank, 32);
     const int64_t Np = op_round_up(N, 64);
     const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
-    const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u && !f32 ? M * rp : 0, 4),
+    // few rows: W is read as it lies for dx, and dW written as the product
+    // of a few columns of dy and rows of x, without copies of either
+    const bool few = M <= ROWS_MAX;
+    const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u && !f32 && !few ? M * rp : 0, 4),
                  o_t = c.lay.take(need_t ? M * rp : 0, 4), o_bt = c.lay.take(need_u ? b.runs * rp * Np : 0, e);
     int64_t part = 0;
     Adapted p{};
-    if (dx) {
+    OuterArgs rows_dx{};
+    if (dx && few) {
+        OuterArgs &o = rows_dx;
+        o.p = dy;
+        o.sp = 1;
+        o.sr = lddy;
+        o.q = proj->weight;
+        o.ldq = proj->weight_stride;
+        o.p_f32 = o.q_f32 = f32;
+        o.R = (int)M;
+        o.C = (int)K;
+        o.vq = (uintptr_t)o.q % 16 == 0 && o.ldq % (f32 ? 4 : 8) == 0;
+        o.ld = op_round_up(K, 4);
+        o.chunk = M * o.ld;
+        o.positions = (int)N;
+        // stretches of W's rows: about three workgroups on each compute unit
+        const int64_t across = (K + (f32 ? 127 : 255)) / (f32 ? 128 : 256) * ((M + 31) / 32);
+        const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(768 + across - 1) / across, (N + 63) / 64, 64}));
+        o.per = (int)op_round_up((N + want - 1) / want, 32);
+        o.n_chunks = (int)((N + o.per - 1) / o.per);
+        part = o.n_chunks * o.chunk;
+    } else if (dx) {
         p.in = dy;
         p.ld_in = lddy;
         p.K = (int)N;
@@ -724,7 +748,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // dW = dy^T x, on transposed copies of both
     MmArgs w{};
     Copy c_dy, c_x;
-    if (dw) {
+    if (dw && !few) {
         w.M = (int)N;
         w.N = (int)K;
         w.K = (int)op_round_up(M, 64);
@@ -739,21 +763,43 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     }
     // column sums of dy: of 64 rows each where dy is transposed anyway
     const int sums = (int)(dw ? (M + 63) / 64 : std::min<int64_t>(128, (M + 63) / 64));
-    const size_t o_sum = c.lay.take(dbias ? sums * N : 0, 4);
+    const size_t o_sum = c.lay.take(dbias && !few ? sums * N : 0, 4);
     const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * rp * K : 0, 4),
                  o_db = c.lay.take(db ? (int64_t)b.n_chunks * rp * N : 0, 4), o_part = c.lay.take(part, 4);
     if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
 
     Jobs first, second, last;
-    bool ok = !dx || add_adapted(c, b, f32, p, first, second);
-    float *const sum = dbias ? c.at<float>(o_sum) : nullptr;
-    if (dw) {
+    Outers outers;
+    bool ok = !dx || few || add_adapted(c, b, f32, p, first, second);
+    float *const sum = dbias && !few ? c.at<float>(o_sum) : dbias;
+    if (dw && few) {
+        OuterArgs o{};
+        o.p = dy;
+        o.sp = lddy;
+        o.sr = 1;
+        o.q = x;
+        o.ldq = ldx;
+        o.p_f32 = o.q_f32 = f32;
+        o.R = (int)N;
+        o.C = (int)K;
+        o.vq = (uintptr_t)x % 16 == 0 && ldx % (f32 ? 4 : 8) == 0;
+        o.out = dw;
+        o.ld = K;
+        o.positions = o.per = (int)M;
+        o.n_chunks = 1;
+        ok = ok && add_outer(outers, o);
+    }
+    if (dx && few) {
+        rows_dx.out = c.at<float>(o_part);
+        ok = ok && add_outer(outers, rows_dx);
+    }
+    if (dw && !few) {
         ok = ok && add_copy(c, c_dy, dy, lddy, (int)N, (int)M, f32, true, nullptr, sum, first, second);
         ok = ok && add_copy(c, c_x, x, ldx, (int)K, (int)M, f32, true, nullptr, nullptr, first, second);
     } else if (dbias) {
         Job j = job(JOB_COLSUM, dy, lddy, (int)M, (int)N, f32);
         j.sum = sum;
-        j.parts = sums;
+        j.parts = few ? 1 : sums;
         ok = ok && add_job(second, j);
     }
     if (need_u) {
@@ -768,7 +814,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         j.run_rank = b.run_rank;
         ok = ok && add_job(second, j);
     }
-    if (dbias) {
+    if (dbias && !few) {
         Job j = job(JOB_COLADD, nullptr, 0, 0, (int)N, true);
         j.sum = sum;
         j.parts = sums;
@@ -776,22 +822,27 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         ok = ok && add_job(last, j);
     }
     float *const t = need_t ? c.at<float>(o_t) : nullptr, *const u = need_u ? c.at<float>(o_u) : nullptr;
-    OuterArgs outer[2];
-    int n_outer = 0;
     auto adapter_gradient = [&](const float *left, const void *right, int64_t ld, int64_t C, size_t o_sums, float *out, int turned) {
         OuterArgs o{};
         o.p = left;
+        o.sp = rp;
+        o.sr = 1;
         o.q = right;
         o.ldq = ld;
-        o.f32 = f32;
+        o.p_f32 = 1;
+        o.q_f32 = f32;
+        o.R = rp;
         o.C = (int)C;
-        o.rp = rp;
         o.vq = (uintptr_t)right % 16 == 0 && ld % (f32 ? 4 : 8) == 0;
-        o.part = c.at<float>(o_sums);
-        o.b = b;
-        outer[n_outer++] = o;
+        o.perm = b.perm;
+        o.out = c.at<float>(o_sums);
+        o.ld = C;
+        o.chunk = rp * C;
+        o.chunks = b.chunks;
+        o.n_chunks = b.n_chunks;
+        ok = ok && add_outer(outers, o);
         Job j = job(JOB_CHUNKS, nullptr, 0, 0, (int)C, true);
-        j.sum = o.part;
+        j.sum = o.out;
         j.out = out;
         j.turned = turned;
         j.R = b.rank;
@@ -804,6 +855,19 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     };
     if (da) adapter_gradient(u, x, ldx, K, o_da, da, 0);
     if (db) adapter_gradient(t, dy, lddy, N, o_db, db, 1);
+    if (dx && few) {
+        Job j = job(JOB_ROWS, proj->a, rows_dx.ld, (int)M, (int)K, f32);
+        j.vec = (uintptr_t)proj->a % 16 == 0 && K % 4 == 0;
+        j.sum = rows_dx.out;
+        j.parts = rows_dx.n_chunks;
+        j.out = dx;
+        j.ldo = lddx;
+        j.row_info = b.row_info;
+        j.t = u;
+        j.R = b.rank;
+        j.rp = rp;
+        ok = ok && add_job(last, j);
+    }
     if (!ok) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
 
     OPCHK(launch_jobs(first, stream), "column maxima");
@@ -811,15 +875,15 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     ShrinkArgs thin[2];
     int n_thin = 0;
     if (need_u) {
-        p.planes = f32 ? nullptr : c.at<u16>(o_up);
+        p.planes = f32 || few ? nullptr : c.at<u16>(o_up);
         p.t = u;
         thin[n_thin++] = shrink(b, f32, dy, lddy, (int)N, c.at<char>(o_bt), Np, true, dx ? p.planes : nullptr, u);
     }
     if (need_t) thin[n_thin++] = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, nullptr, t);
     if (n_thin) OPCHK(launch_shrink(thin, n_thin, stream), "thin products");
-    if (dx)
+    if (dx && !few)
         if (gemel_status s = run_adapted(c, b, f32, p, c.at<float>(o_part))) return s;
-    if (dw) {
+    if (dw && !few) {
         operands(c, w, c_dy, c_x);
         if (!f32) {
             w.a[0] = c.at<u16>(c_dy.o);
@@ -832,7 +896,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         w.o.vec = vec_ok(dw, K, 1);
         OPCHK(launch_mm(w, stream), "product");
     }
-    if (n_outer) OPCHK(launch_outer(outer, n_outer, stream), "adapter gradients");
+    OPCHK(launch_outer(outers, stream), "gradients");
     OPCHK(launch_jobs(last, stream), "sums");
     return GEMEL_OK;
 }
