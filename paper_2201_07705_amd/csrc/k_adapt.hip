@@ -57,7 +57,7 @@ template <bool F32, int RB>
 __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args) {
     const ShrinkArgs &a = arg_of<ShrinkArgs>(blockIdx.z);
     __shared__ f32x4 part[8][2 * RB][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, l16 = lane & 15;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, l16 = lane & 15;
     const int *it = a.b.items + 3 * blockIdx.x;
     const int u = it[0], p0 = it[1], n = it[2];
     const int rank = a.b.run_rank[u], r0 = blockIdx.y * 16 * RB;
@@ -77,27 +77,64 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < RB; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto add = [&](const uint4 (&xv)[2], const uint4 (&av)[RB]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int j = 0; j < RB; ++j) {
+                if constexpr (F32) {
+                    const f32x4 x = __builtin_bit_cast(f32x4, xv[i]), w = __builtin_bit_cast(f32x4, av[j]);
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[i][j], 0, 0, 0);
+                } else {
+                    acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[j]),
+                                                                        __builtin_bit_cast(bf16x8, xv[i]), acc[i][j], 0, 0, 0);
+                }
+            }
+    };
     if (r0 < rank) {
-#pragma unroll 4
-        for (int k = (wave * 4 + g) * Q; k - g * Q < a.K; k += 32 * Q) {
+        int k = wave * 4 * Q;   // (the wave's; its lane groups take Q each)
+        if (a.vx && a.va) {
+            // whole chunks, four rounds of them in flight: no branch may
+            // stand between the loads
+            const char *const xb = (const char *)a.x, *const ab = (const char *)a.a;
+            constexpr int E = F32 ? 4 : 2, ROUNDS = 4;
+            for (; k + (ROUNDS - 1) * 32 * Q + 4 * Q <= a.K; k += ROUNDS * 32 * Q) {
+                uint4 xv[ROUNDS][2], av[ROUNDS][RB];
+#pragma unroll
+                for (int q = 0; q < ROUNDS; ++q) {
+                    const int kk = k + q * 32 * Q + g * Q;
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) xv[q][i] = *(const uint4 *)(xb + (xrow[i] + kk) * E);
+#pragma unroll
+                    for (int j = 0; j < RB; ++j) av[q][j] = *(const uint4 *)(ab + (arow[j] + kk) * E);
+                }
+#pragma unroll
+                for (int q = 0; q < ROUNDS; ++q) {
+#pragma unroll
+                    for (int j = 0; j < RB; ++j) av[q][j] = used[j] ? av[q][j] : uint4{};
+                    add(xv[q], av[q]);
+                }
+            }
+            for (; k + 4 * Q <= a.K; k += 32 * Q) {
+                const int kk = k + g * Q;
+                uint4 xv[2], av[RB];
+#pragma unroll
+                for (int i = 0; i < 2; ++i) xv[i] = *(const uint4 *)(xb + (xrow[i] + kk) * E);
+#pragma unroll
+                for (int j = 0; j < RB; ++j) av[j] = *(const uint4 *)(ab + (arow[j] + kk) * E);
+#pragma unroll
+                for (int j = 0; j < RB; ++j) av[j] = used[j] ? av[j] : uint4{};
+                add(xv, av);
+            }
+        }
+        for (; k < a.K; k += 32 * Q) {
             uint4 xv[2], av[RB];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k, a.K, a.vx);
+            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k + g * Q, a.K, a.vx);
 #pragma unroll
-            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k, used[j] ? a.K : 0, a.va);
-#pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < RB; ++j) {
-                    if constexpr (F32) {
-                        const f32x4 x = __builtin_bit_cast(f32x4, xv[i]), w = __builtin_bit_cast(f32x4, av[j]);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(w[e], x[e], acc[i][j], 0, 0, 0);
-                    } else {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, av[j]),
-                                                                            __builtin_bit_cast(bf16x8, xv[i]), acc[i][j], 0, 0, 0);
-                    }
-                }
+            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k + g * Q, used[j] ? a.K : 0, a.va);
+            add(xv, av);
         }
     }
 #pragma unroll
@@ -151,13 +188,26 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int block, unsigned ch
     const bool along = a.sr == 1;
     auto p_row = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) / 32 : (i * 256 + tid) % 32; };
     auto p_col = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) % 32 : (i * 256 + tid) / 32; };
+    const bool whole = a.vq && c0 + COLS <= a.C;
     auto load = [&](int s) __attribute__((always_inline)) {
+        if (whole && s + 32 <= n) {
+            // (no branch between the loads)
+            int64_t at[NQ];
 #pragma unroll
-        for (int i = 0; i < NQ; ++i) {
-            const int row = (i * 256 + tid) / LR, c = c0 + (tid % LR) * Q;
-            const bool in = s + row < n;
-            const int pos = p0 + s + row;
-            q[i] = chunk<F32>(a.q, in ? (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq : 0, c, in ? a.C : 0, a.vq);
+            for (int i = 0; i < NQ; ++i) {
+                const int pos = p0 + s + (i * 256 + tid) / LR;
+                at[i] = (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq + c0 + (tid % LR) * Q;
+            }
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) q[i] = *(const uint4 *)((const char *)a.q + at[i] * E);
+        } else {
+#pragma unroll
+            for (int i = 0; i < NQ; ++i) {
+                const int row = (i * 256 + tid) / LR, c = c0 + (tid % LR) * Q;
+                const bool in = s + row < n;
+                const int pos = p0 + s + row;
+                q[i] = chunk<F32>(a.q, in ? (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq : 0, c, in ? a.C : 0, a.vq);
+            }
         }
 #pragma unroll
         for (int i = 0; i < NP; ++i) {

@@ -130,7 +130,9 @@ __device__ __forceinline__ void touch_args() {
 // last - i, so that each pair has as many.
 template <int T>
 __device__ __forceinline__ void mm_place(const MmArgs &a, int &tm, int &tn) {
-    const int tiles_m = (a.M + T - 1) / T, tiles_n = (a.N + T - 1) / T;
+    // (32: the reduction's, which covers the planes' padding to 64)
+    const int tiles_m = T < 64 ? (a.M + 63) / 64 * (64 / T) : (a.M + T - 1) / T;
+    const int tiles_n = T < 64 ? (a.N + 63) / 64 * (64 / T) : (a.N + T - 1) / T;
     const int G = gridDim.x;
     const int t = (G & 7) == 0 ? (int)(blockIdx.x & 7) * (G >> 3) + (int)(blockIdx.x >> 3) : (int)blockIdx.x;
     if (a.sym) {
@@ -615,55 +617,51 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
 }
 
 // Sums the splits of each element in order and applies the epilogue, one
-// 64 x 64 tile per workgroup; transposed planes go through LDS.
+// 32 x 32 tile per workgroup (4 elements to a thread: what takes time is the
+// latency of a few loads); transposed planes go through LDS.
 template <int EPI>
 __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
     constexpr bool PLANES = EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_NEXT || EPI == EPI_MIX;
-    __shared__ uint32_t turn[PLANES ? 64 : 1][65];
+    __shared__ uint32_t turn[PLANES ? 32 : 1][33];
     int tm, tn;
-    mm_place<64>(a, tm, tn);
-    const int z = blockIdx.z, m0 = tm * 64, n0 = tn * 64;
-    const Tile tile{z, m0, n0, m0 + 64 <= a.M && n0 + 64 <= a.N};
+    mm_place<32>(a, tm, tn);
+    const int z = blockIdx.z, m0 = tm * 32, n0 = tn * 32;
+    const Tile tile{z, m0, n0, m0 + 32 <= a.M && n0 + 32 <= a.N};
     const bool turned = EPI == EPI_NEXT || (PLANES && a.sym && tn > tm);
-    f32x4 v[4];
-    Near near[4];
+    const int m = threadIdx.x >> 3, n = (threadIdx.x & 7) * 4;
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+    const Near near = gather<EPI>(a, tile, m, n);
+    if (m0 + m < a.M && n0 + n < a.N) {
+        const float *p = a.partial + ((int64_t)z * a.M + m0 + m) * a.ldp + n0 + n;
+        const int64_t step = (int64_t)a.batch * a.M * a.ldp;
+        int s = 0;
+        for (; s + 4 <= a.splits; s += 4) {
+            f32x4 x[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = i * 16 + (threadIdx.x >> 4), n = (threadIdx.x & 15) * 4;
-        near[i] = gather<EPI>(a, tile, m, n);
-        v[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (m0 + m < a.M && n0 + n < a.N) {
-            const float *p = a.partial + ((int64_t)z * a.M + m0 + m) * a.ldp + n0 + n;
-#pragma unroll 4
-            for (int s = 0; s < a.splits; ++s) v[i] += *(const f32x4 *)(p + (int64_t)s * a.batch * a.M * a.ldp);
+            for (int i = 0; i < 4; ++i) x[i] = *(const f32x4 *)(p + (s + i) * step);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) v += x[i];
         }
+        for (; s < a.splits; ++s) v += *(const f32x4 *)(p + s * step);
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int m = i * 16 + (threadIdx.x >> 4), n = (threadIdx.x & 15) * 4;
-        const uint4 q = finish<EPI>(a, tile, m, n, v[i], near[i]);
-        if constexpr (PLANES)
-            if (turned)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) turn[m][n + e] = (&q.x)[e];
-    }
+    const uint4 q = finish<EPI>(a, tile, m, n, v, near);
     if constexpr (PLANES) {
         if (!turned) return;
-        __syncthreads();
-        const Planes &q = EPI == EPI_NEXT ? a.o.q : a.o.p;
-        u16 *const hi = q.hi + (int64_t)z * q.z + (int64_t)n0 * q.ld + m0;
-        u16 *const lo = q.lo ? q.lo + (int64_t)z * q.z + (int64_t)n0 * q.ld + m0 : nullptr;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int n = i * 16 + (threadIdx.x >> 4), m = (threadIdx.x & 15) * 4;
-            const uint4 x = make_uint4(turn[m][n], turn[m + 1][n], turn[m + 2][n], turn[m + 3][n]);
-            if (n0 + n < a.N && m0 + m < q.ld) put_pairs(hi, lo, offset_of(n, m, q.ld, 2), x);
-        }
+        for (int e = 0; e < 4; ++e) turn[m][n + e] = (&q.x)[e];
+        __syncthreads();
+        const Planes &t = EPI == EPI_NEXT ? a.o.q : a.o.p;
+        u16 *const hi = t.hi + (int64_t)z * t.z + (int64_t)n0 * t.ld + m0;
+        u16 *const lo = t.lo ? t.lo + (int64_t)z * t.z + (int64_t)n0 * t.ld + m0 : nullptr;
+        // (thread: row m of the transpose, 4 of its columns from n on)
+        const uint4 x = make_uint4(turn[n][m], turn[n + 1][m], turn[n + 2][m], turn[n + 3][m]);
+        if (n0 + m < a.N && m0 + n < t.ld) put_pairs(hi, lo, offset_of(m, n, t.ld, 2), x);
     }
 }
 
 int64_t tiles_of(const MmArgs &a, int T) {
-    const int64_t tm = (a.M + T - 1) / T, tn = (a.N + T - 1) / T;
+    const int64_t tm = T < 64 ? (a.M + 63) / 64 * (64 / T) : (a.M + T - 1) / T;
+    const int64_t tn = T < 64 ? (a.N + 63) / 64 * (64 / T) : (a.N + T - 1) / T;
     return a.sym ? tm * (tm + 1) / 2 : tm * tn;
 }
 
@@ -675,7 +673,7 @@ hipError_t go(const MmArgs &a, hipStream_t s) {
                                    dim3(mm_threads<T>()), p, 0, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&mm_reduce_kernel<EPI>),
-                           dim3((unsigned)tiles_of(a, 64), 1, (unsigned)a.batch), dim3(256), p, 0, s);
+                           dim3((unsigned)tiles_of(a, 32), 1, (unsigned)a.batch), dim3(256), p, 0, s);
 }
 
 template <int EPI, bool F16>

@@ -93,10 +93,24 @@ __device__ __forceinline__ void thin(const RowsArgs &a, int block, f32x4 *part) 
     const int k0 = slice * a.thin_bytes, k1 = min(end, k0 + a.thin_bytes);
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (rb * 16 < rank) {
-#pragma unroll 4
-        for (int k = k0 + wave * 64 + g * 16; k - g * 16 < k1; k += 256) {
-            const uint4 xv = chunk<F32>(x, k, k1, 1);
-            const uint4 wv = chunk<F32>(w, k, used ? k1 : 0, a.va);
+        int k = k0 + wave * 64;   // (the wave's; its lane groups take 16 bytes each)
+        if (a.va) {
+            // whole chunks, eight of each operand in flight: no branch may
+            // stand between the loads
+            for (; k + 7 * 256 + 64 <= min(k1, end & ~15); k += 8 * 256) {
+                uint4 xv[8], wv[8];
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    xv[q] = *(const uint4 *)(x + k + q * 256 + g * 16);
+                    wv[q] = *(const uint4 *)(w + k + q * 256 + g * 16);
+                }
+#pragma unroll
+                for (int q = 0; q < 8; ++q) acc = mul<F32>(used ? wv[q] : uint4{}, xv[q], acc);
+            }
+        }
+        for (; k < k1; k += 256) {
+            const uint4 xv = chunk<F32>(x, k + g * 16, k1, 1);
+            const uint4 wv = chunk<F32>(w, k + g * 16, used ? k1 : 0, a.va);
             acc = mul<F32>(wv, xv, acc);
         }
     }
@@ -218,11 +232,18 @@ __global__ __launch_bounds__(128) void rows_sum_kernel(const RowsArgs a) {
         const char *b = (const char *)a.bank_b + ((int64_t)info.z * a.N + n) * R * elem;
         const int left = min(4, a.N - n);
         constexpr int Q = F32 ? 4 : 8;
+        const bool whole = a.vb && left == 4 && rank % Q == 0;
+#pragma unroll 2
         for (int r = 0; r < rank; r += Q) {
             uint4 q[4];
+            if (whole) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                q[i] = i < left ? chunk<F32>(b + (int64_t)i * R * elem, r * elem, rank * elem, a.vb) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 4; ++i) q[i] = *(const uint4 *)(b + ((int64_t)i * R + r) * elem);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    q[i] = i < left ? chunk<F32>(b + (int64_t)i * R * elem, r * elem, rank * elem, a.vb) : make_uint4(0, 0, 0, 0);
+            }
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
                 const float t = r + j < rank ? ts[r + j] : 0.f;
