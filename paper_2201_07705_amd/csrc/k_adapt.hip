@@ -5,6 +5,7 @@
 #include <algorithm>
 
 #include "op_args.h"
+#include "op_moves.h"
 
 namespace gemel {
 
@@ -18,10 +19,9 @@ __device__ __forceinline__ u16 bf_down(float f) { return __builtin_bit_cast(u16,
 
 // 16 bytes of a row from element k on; elements at k_end and beyond are zeros.
 template <bool F32>
-__device__ __forceinline__ uint4 chunk(const void *base, int64_t row, int k, int k_end, int whole) {
+__device__ __forceinline__ uint4 chunk(const void *base, int64_t row, int k, int k_end) {
     constexpr int Q = F32 ? 4 : 8;
-    if (whole && k + Q <= k_end)
-        return F32 ? *(const uint4 *)((const float *)base + row + k) : *(const uint4 *)((const u16 *)base + row + k);
+    if (k + Q <= k_end) return get_16b((const char *)base + (row + k) * (F32 ? 4 : 2));
     union {
         uint4 v;
         u16 h[8];
@@ -94,46 +94,33 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
     };
     if (r0 < rank) {
         int k = wave * 4 * Q;   // (the wave's; its lane groups take Q each)
-        if (a.vx && a.va) {
-            // whole chunks, four rounds of them in flight: no branch may
-            // stand between the loads
-            const char *const xb = (const char *)a.x, *const ab = (const char *)a.a;
-            constexpr int E = F32 ? 4 : 2, ROUNDS = 4;
-            for (; k + (ROUNDS - 1) * 32 * Q + 4 * Q <= a.K; k += ROUNDS * 32 * Q) {
-                uint4 xv[ROUNDS][2], av[ROUNDS][RB];
+        // whole chunks, four rounds of them in flight: no branch may stand
+        // between the loads
+        const char *const xb = (const char *)a.x, *const ab = (const char *)a.a;
+        constexpr int E = F32 ? 4 : 2, ROUNDS = 4;
+        for (; k + (ROUNDS - 1) * 32 * Q + 4 * Q <= a.K; k += ROUNDS * 32 * Q) {
+            uint4 xv[ROUNDS][2], av[ROUNDS][RB];
 #pragma unroll
-                for (int q = 0; q < ROUNDS; ++q) {
-                    const int kk = k + q * 32 * Q + g * Q;
+            for (int q = 0; q < ROUNDS; ++q) {
+                const int kk = k + q * 32 * Q + g * Q;
 #pragma unroll
-                    for (int i = 0; i < 2; ++i) xv[q][i] = *(const uint4 *)(xb + (xrow[i] + kk) * E);
+                for (int i = 0; i < 2; ++i) xv[q][i] = get_16b(xb + (xrow[i] + kk) * E);
 #pragma unroll
-                    for (int j = 0; j < RB; ++j) av[q][j] = *(const uint4 *)(ab + (arow[j] + kk) * E);
-                }
-#pragma unroll
-                for (int q = 0; q < ROUNDS; ++q) {
-#pragma unroll
-                    for (int j = 0; j < RB; ++j) av[q][j] = used[j] ? av[q][j] : uint4{};
-                    add(xv[q], av[q]);
-                }
+                for (int j = 0; j < RB; ++j) av[q][j] = get_16b(ab + (arow[j] + kk) * E);
             }
-            for (; k + 4 * Q <= a.K; k += 32 * Q) {
-                const int kk = k + g * Q;
-                uint4 xv[2], av[RB];
 #pragma unroll
-                for (int i = 0; i < 2; ++i) xv[i] = *(const uint4 *)(xb + (xrow[i] + kk) * E);
+            for (int q = 0; q < ROUNDS; ++q) {
 #pragma unroll
-                for (int j = 0; j < RB; ++j) av[j] = *(const uint4 *)(ab + (arow[j] + kk) * E);
-#pragma unroll
-                for (int j = 0; j < RB; ++j) av[j] = used[j] ? av[j] : uint4{};
-                add(xv, av);
+                for (int j = 0; j < RB; ++j) av[q][j] = used[j] ? av[q][j] : uint4{};
+                add(xv[q], av[q]);
             }
         }
         for (; k < a.K; k += 32 * Q) {
             uint4 xv[2], av[RB];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k + g * Q, a.K, a.vx);
+            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k + g * Q, a.K);
 #pragma unroll
-            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k + g * Q, used[j] ? a.K : 0, a.va);
+            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k + g * Q, used[j] ? a.K : 0);
             add(xv, av);
         }
     }
@@ -188,7 +175,7 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int block, unsigned ch
     const bool along = a.sr == 1;
     auto p_row = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) / 32 : (i * 256 + tid) % 32; };
     auto p_col = [&](int i) __attribute__((always_inline)) { return along ? (i * 256 + tid) % 32 : (i * 256 + tid) / 32; };
-    const bool whole = a.vq && c0 + COLS <= a.C;
+    const bool whole = c0 + COLS <= a.C;
     auto load = [&](int s) __attribute__((always_inline)) {
         if (whole && s + 32 <= n) {
             // (no branch between the loads)
@@ -199,14 +186,14 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int block, unsigned ch
                 at[i] = (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq + c0 + (tid % LR) * Q;
             }
 #pragma unroll
-            for (int i = 0; i < NQ; ++i) q[i] = *(const uint4 *)((const char *)a.q + at[i] * E);
+            for (int i = 0; i < NQ; ++i) q[i] = get_16b((const char *)a.q + at[i] * E);
         } else {
 #pragma unroll
             for (int i = 0; i < NQ; ++i) {
                 const int row = (i * 256 + tid) / LR, c = c0 + (tid % LR) * Q;
                 const bool in = s + row < n;
                 const int pos = p0 + s + row;
-                q[i] = chunk<F32>(a.q, in ? (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq : 0, c, in ? a.C : 0, a.vq);
+                q[i] = chunk<F32>(a.q, in ? (int64_t)(a.perm ? a.perm[pos] : pos) * a.ldq : 0, c, in ? a.C : 0);
             }
         }
 #pragma unroll

@@ -6,6 +6,7 @@
 #include <algorithm>
 
 #include "op_args.h"
+#include "op_moves.h"
 
 namespace gemel {
 
@@ -14,6 +15,7 @@ namespace {
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 __device__ __forceinline__ float bf_up(u16 h) { return __uint_as_float((uint32_t)h << 16); }
+__device__ __forceinline__ u16 bf_down(float f) { return __builtin_bit_cast(u16, (__bf16)f); }
 __device__ __forceinline__ u16 half_down(float f) { return __builtin_bit_cast(u16, (_Float16)f); }
 __device__ __forceinline__ float half_up(u16 h) { return (float)__builtin_bit_cast(_Float16, h); }
 
@@ -34,8 +36,8 @@ __device__ __forceinline__ void split_put(u16 *hi, u16 *lo, int64_t at, float v,
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
 // 4 consecutive float32 (`left` of them there; others zero)
-__device__ __forceinline__ f32x4 load4(const float *p, int left, int vec) {
-    if (vec && left >= 4) return *(const f32x4 *)p;
+__device__ __forceinline__ f32x4 load4(const float *p, int left) {
+    if (left >= 4) return get_f32x4<f32x4>(p);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int i = 0; i < 4; ++i)
@@ -43,15 +45,45 @@ __device__ __forceinline__ f32x4 load4(const float *p, int left, int vec) {
     return v;
 }
 
-constexpr int PAD_ITEMS = 2048;    // elements of a block of JOB_PAD
+// the same of bf16
+__device__ __forceinline__ f32x4 up4(const u16 *p, int left) {
+    if (left >= 4) {
+        const ushort4 h = get_u16x4(p);
+        return f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
+    }
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        if (i < left) v[i] = bf_up(p[i]);
+    return v;
+}
+
+constexpr int PAD_ITEMS = 1024;    // 16-byte chunks of a block of JOB_PAD
 constexpr int CHUNK_COLS = 64;     // columns of a block of JOB_CHUNKS
 
+// 16 bytes at a time; output rows are whole chunks of that
 template <typename E>
 __device__ __forceinline__ void pad(const Job &j, int block) {
-    const int64_t n = (int64_t)j.rows * j.ldo, end = min(n, (int64_t)(block + 1) * PAD_ITEMS);
-    for (int64_t i = (int64_t)block * PAD_ITEMS + threadIdx.x; i < end; i += 256) {
-        const int64_t r = i / j.ldo, c = i - r * j.ldo;
-        ((E *)j.out)[i] = c < j.cols ? ((const E *)j.in)[(j.perm ? j.perm[r] : r) * j.ldi + c] : (E)0;
+    constexpr int Q = 16 / sizeof(E);
+    const int across = (int)(j.ldo / Q);   // chunks of a row
+    const int64_t first = (int64_t)block * PAD_ITEMS;
+    const int row = (int)(first / across), at = (int)(first - (int64_t)row * across) + threadIdx.x;
+#pragma unroll
+    for (int i = 0; i < PAD_ITEMS / 256; ++i) {
+        const int down = (at + i * 256) / across, r = row + down, c = (at + i * 256 - down * across) * Q;
+        if (r >= j.rows) continue;
+        const E *in = (const E *)j.in + (int64_t)(j.perm ? j.perm[r] : r) * j.ldi + c;
+        union {
+            uint4 v;
+            E e[Q];
+        } x;
+        if (c + Q <= j.cols) {
+            x.v = get_16b(in);
+        } else {
+#pragma unroll
+            for (int k = 0; k < Q; ++k) x.e[k] = c + k < j.cols ? in[k] : (E)0;
+        }
+        *(uint4 *)((E *)j.out + (int64_t)r * j.ldo + c) = x.v;
     }
 }
 
@@ -63,7 +95,7 @@ __device__ __forceinline__ void split(const Job &j, int block) {
     unsigned m = 0;
 #pragma unroll 4
     for (int c = lane * 4; c < j.cols; c += 256) {
-        const f32x4 v = load4(in + c, j.cols - c, j.vec);
+        const f32x4 v = load4(in + c, j.cols - c);
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = max(m, magnitude(v[i]));
     }
@@ -73,7 +105,7 @@ __device__ __forceinline__ void split(const Job &j, int block) {
     u16 *hi = (u16 *)j.out + r * j.ldo, *lo = j.lo + r * j.ldo;
 #pragma unroll 4
     for (int c = lane * 4; c < j.ldo; c += 256) {
-        const f32x4 v = load4(in + c, j.cols - c, j.vec);
+        const f32x4 v = load4(in + c, j.cols - c);
         u16 h[4], l[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) split_put(h, l, i, v[i], e);
@@ -99,8 +131,8 @@ __device__ __forceinline__ void turn(const Job &j, int block, unsigned char *lds
             E e[Q];
         } x;
         const E *in = (const E *)j.in + (int64_t)(r0 + r) * j.ldi + c0 + c;
-        if (r0 + r < j.rows && j.vec && c0 + c + Q <= j.cols) {
-            x.v = *(const uint4 *)in;
+        if (r0 + r < j.rows && c0 + c + Q <= j.cols) {
+            x.v = get_16b(in);
         } else {
 #pragma unroll
             for (int k = 0; k < Q; ++k) x.e[k] = r0 + r < j.rows && c0 + c + k < j.cols ? in[k] : (E)0;
@@ -155,14 +187,7 @@ __device__ __forceinline__ void columns(const Job &j, int block, unsigned char *
     for (int r = r0 + g; r < r1; r += 16) {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         if (left > 0) {
-            if (j.f32) {
-                x = load4((const float *)j.in + r * j.ldi + c, left, j.vec);
-            } else {
-                const u16 *in = (const u16 *)j.in + r * j.ldi + c;
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (i < left) x[i] = bf_up(in[i]);
-            }
+            x = j.f32 ? load4((const float *)j.in + r * j.ldi + c, left) : up4((const u16 *)j.in + r * j.ldi + c, left);
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
@@ -272,26 +297,23 @@ __device__ __forceinline__ void rows(const Job &j, int block, unsigned char *lds
 #pragma unroll 4
     for (int r = 0; r < rank; ++r) {
         const int64_t at = ((int64_t)info.z * j.R + r) * j.cols + c;
-        f32x4 x;
-        if (j.f32) {
-            x = load4((const float *)j.in + at, left, j.vec);
-        } else if (j.vec && left >= 4) {
-            const ushort4 h = *(const ushort4 *)((const u16 *)j.in + at);
-            x = f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
-        } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = i < left ? bf_up(((const u16 *)j.in)[at + i]) : 0.f;
-        }
-        v += ts[r] * x;
+        v += ts[r] * (j.f32 ? load4((const float *)j.in + at, left) : up4((const u16 *)j.in + at, left));
     }
     const int64_t to = row * j.ldo + c;
+    if (left >= 4) {
+        if (j.f32)
+            put_f32x4((float *)j.out + to, v);
+        else
+            put_u16x4((u16 *)j.out + to, make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3])));
+        return;
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         if (i >= left) continue;
         if (j.f32)
             ((float *)j.out)[to + i] = v[i];
         else
-            ((u16 *)j.out)[to + i] = __builtin_bit_cast(u16, (__bf16)v[i]);
+            ((u16 *)j.out)[to + i] = bf_down(v[i]);
     }
 }
 
@@ -337,8 +359,8 @@ bool add_job(Jobs &all, const Job &in) {
     bool ok = j.cols > 0;
     switch (j.kind) {
         case JOB_PAD:
-            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.cols;
-            blocks = ((int64_t)j.rows * j.ldo + PAD_ITEMS - 1) / PAD_ITEMS;
+            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.cols && j.ldo % (j.f32 ? 4 : 8) == 0;
+            blocks = ((int64_t)j.rows * (j.ldo / (j.f32 ? 4 : 8)) + PAD_ITEMS - 1) / PAD_ITEMS;
             break;
         case JOB_SPLIT:
             ok = ok && j.in && j.out && j.lo && j.e && j.rows > 0 && j.ldo >= j.cols && j.ldo % 4 == 0;

@@ -7,6 +7,7 @@
 #include <type_traits>
 
 #include "op_args.h"
+#include "op_moves.h"
 
 namespace gemel {
 
@@ -183,8 +184,8 @@ __device__ __forceinline__ Near gather(const MmArgs &a, const Tile &t, int m, in
     } else if constexpr (EPI != EPI_GRAM) {
         at4(o.s, t, m, n, a.M, r.hi, r.lo);
         if constexpr (EPI == EPI_STEP) {
-            if (o.vec && t.inside) {
-                r.w = load_at<f32x4>(at_tile((const float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4));
+            if (t.inside) {
+                r.w = load_at<f32x4_any>(at_tile((const float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4));
             } else {
                 const float *w = (const float *)o.out + (int64_t)t.z * o.z + (int64_t)min(t.m0 + m, a.M - 1) * o.ld;
 #pragma unroll
@@ -244,8 +245,8 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
         }
         if (o.out_f32) {
             float *p = (float *)o.out + at;
-            if (o.vec && left > 3) {
-                *(f32x4 *)p = v;
+            if (left > 3) {
+                put_f32x4(p, v);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -253,8 +254,8 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
             }
         } else {
             u16 *p = (u16 *)o.out + at;
-            if (o.vec && left > 3) {
-                *(ushort4 *)p = make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3]));
+            if (left > 3) {
+                put_u16x4(p, make_ushort4(to_bf16(v[0]), to_bf16(v[1]), to_bf16(v[2]), to_bf16(v[3])));
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
@@ -268,11 +269,11 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
         if constexpr (EPI == EPI_STEP) x = (1.f - o.decay) * in.w - o.rate * x;
         const bool wide = EPI == EPI_STEP || o.out_f32;
         u16 *const h = EPI == EPI_STEP ? o.copy : wide ? nullptr : (u16 *)o.out;
-        if (o.vec && left > 3) {
-            if (wide) store_at(at_tile((float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4), x);
+        if (left > 3) {
+            if (wide) store_at(at_tile((float *)o.out, t, o.z, o.ld), offset_of(m, n, o.ld, 4), (f32x4_any)x);
             if (h)
                 store_at(at_tile(h, t, o.z, o.ld), offset_of(m, n, o.ld, 2),
-                         make_ushort4(to_bf16(x[0]), to_bf16(x[1]), to_bf16(x[2]), to_bf16(x[3])));
+                         u16x4_any{to_bf16(x[0]), to_bf16(x[1]), to_bf16(x[2]), to_bf16(x[3])});
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i) {

@@ -6,6 +6,7 @@
 #include <type_traits>
 
 #include "op_args.h"
+#include "op_moves.h"
 
 namespace gemel {
 
@@ -40,19 +41,19 @@ __device__ __forceinline__ double block_sum(double v) {
 template <bool FIRST>
 __device__ __forceinline__ f32x4 update4(const OrthArgs &a, int64_t at, int left) {
     f32x4 u = {0.f, 0.f, 0.f, 0.f};
-    if (left >= 4 && a.vec) {
+    if (left >= 4) {
         f32x4 g;
         if (a.f32) {
-            g = *(const f32x4 *)((const float *)a.g + at);
+            g = get_f32x4<f32x4>((const float *)a.g + at);
         } else {
-            const ushort4 h = *(const ushort4 *)((const u16 *)a.g + at);
+            const ushort4 h = get_u16x4((const u16 *)a.g + at);
             g = f32x4{bf_up(h.x), bf_up(h.y), bf_up(h.z), bf_up(h.w)};
         }
         if (!a.step) return g;
-        f32x4 m = *(const f32x4 *)(a.m + at);
+        f32x4 m = get_f32x4<f32x4>(a.m + at);
         if (FIRST) {
             m = a.beta * m + g;
-            *(f32x4 *)(a.m + at) = m;
+            put_f32x4(a.m + at, m);
         }
         return a.nesterov ? g + a.beta * m : m;
     }
@@ -345,10 +346,10 @@ __global__ __launch_bounds__(256) void thin_apply_kernel(const OrthArgs a) {
         for (int e = 0; e < 4; ++e) v[e] = WIDE ? os[r][c + e] : os[c + e][r];
         float *const f = a.step || a.f32 ? (float *)a.out + at : nullptr;
         u16 *const h = a.step ? (a.copy ? a.copy + at : nullptr) : a.f32 ? nullptr : (u16 *)a.out + at;
-        if (left >= 4 && a.vec) {
-            if (a.step) v = (1.f - a.decay) * *(const f32x4 *)f - a.rate * v;
-            if (f) *(f32x4 *)f = v;
-            if (h) *(ushort4 *)h = make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3]));
+        if (left >= 4) {
+            if (a.step) v = (1.f - a.decay) * get_f32x4<f32x4>(f) - a.rate * v;
+            if (f) put_f32x4(f, v);
+            if (h) put_u16x4(h, make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3])));
         } else {
 #pragma unroll
             for (int e = 0; e < 4; ++e) {

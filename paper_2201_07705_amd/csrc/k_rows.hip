@@ -15,6 +15,7 @@
 #include <type_traits>
 
 #include "op_args.h"
+#include "op_moves.h"
 
 namespace gemel {
 
@@ -55,10 +56,9 @@ __device__ __forceinline__ f32x4 mul(const uint4 &a, const uint4 &b, f32x4 c) {
 }
 
 // Bytes [at, at + 16) of a row of `end` bytes; what lies beyond is zero.
-// Elements are 2 or 4 bytes; `whole`: full chunks may be loaded at once.
 template <bool F32>
-__device__ __forceinline__ uint4 chunk(const char *row, int at, int end, int whole) {
-    if (whole && at + 16 <= end) return *(const uint4 *)(row + at);
+__device__ __forceinline__ uint4 chunk(const char *row, int at, int end) {
+    if (at + 16 <= end) return get_16b(row + at);
     union {
         uint4 v;
         u16 h[8];
@@ -94,23 +94,21 @@ __device__ __forceinline__ void thin(const RowsArgs &a, int block, f32x4 *part) 
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     if (rb * 16 < rank) {
         int k = k0 + wave * 64;   // (the wave's; its lane groups take 16 bytes each)
-        if (a.va) {
-            // whole chunks, eight of each operand in flight: no branch may
-            // stand between the loads
-            for (; k + 7 * 256 + 64 <= min(k1, end & ~15); k += 8 * 256) {
-                uint4 xv[8], wv[8];
+        // whole chunks, eight of each operand in flight: no branch may stand
+        // between the loads
+        for (; k + 7 * 256 + 64 <= k1; k += 8 * 256) {
+            uint4 xv[8], wv[8];
 #pragma unroll
-                for (int q = 0; q < 8; ++q) {
-                    xv[q] = *(const uint4 *)(x + k + q * 256 + g * 16);
-                    wv[q] = *(const uint4 *)(w + k + q * 256 + g * 16);
-                }
-#pragma unroll
-                for (int q = 0; q < 8; ++q) acc = mul<F32>(used ? wv[q] : uint4{}, xv[q], acc);
+            for (int q = 0; q < 8; ++q) {
+                xv[q] = get_16b(x + k + q * 256 + g * 16);
+                wv[q] = get_16b(w + k + q * 256 + g * 16);
             }
+#pragma unroll
+            for (int q = 0; q < 8; ++q) acc = mul<F32>(used ? wv[q] : uint4{}, xv[q], acc);
         }
         for (; k < k1; k += 256) {
-            const uint4 xv = chunk<F32>(x, k + g * 16, k1, 1);
-            const uint4 wv = chunk<F32>(w, k + g * 16, used ? k1 : 0, a.va);
+            const uint4 xv = chunk<F32>(x, k + g * 16, k1);
+            const uint4 wv = chunk<F32>(w, k + g * 16, used ? k1 : 0);
             acc = mul<F32>(wv, xv, acc);
         }
     }
@@ -232,17 +230,17 @@ __global__ __launch_bounds__(128) void rows_sum_kernel(const RowsArgs a) {
         const char *b = (const char *)a.bank_b + ((int64_t)info.z * a.N + n) * R * elem;
         const int left = min(4, a.N - n);
         constexpr int Q = F32 ? 4 : 8;
-        const bool whole = a.vb && left == 4 && rank % Q == 0;
+        const bool whole = left == 4 && rank % Q == 0;
 #pragma unroll 2
         for (int r = 0; r < rank; r += Q) {
             uint4 q[4];
             if (whole) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) q[i] = *(const uint4 *)(b + ((int64_t)i * R + r) * elem);
+                for (int i = 0; i < 4; ++i) q[i] = get_16b(b + ((int64_t)i * R + r) * elem);
             } else {
 #pragma unroll
                 for (int i = 0; i < 4; ++i)
-                    q[i] = i < left ? chunk<F32>(b + (int64_t)i * R * elem, r * elem, rank * elem, a.vb) : make_uint4(0, 0, 0, 0);
+                    q[i] = i < left ? chunk<F32>(b + (int64_t)i * R * elem, r * elem, rank * elem) : make_uint4(0, 0, 0, 0);
             }
 #pragma unroll
             for (int j = 0; j < Q; ++j) {
@@ -261,8 +259,8 @@ __global__ __launch_bounds__(128) void rows_sum_kernel(const RowsArgs a) {
     const int64_t at = (int64_t)row * a.ldy + n;
     if constexpr (F32) {
         float *y = (float *)a.y + at;
-        if (a.vy && n + 3 < a.N) {
-            *(f32x4 *)y = v;
+        if (n + 3 < a.N) {
+            put_f32x4(y, v);
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)
@@ -270,8 +268,8 @@ __global__ __launch_bounds__(128) void rows_sum_kernel(const RowsArgs a) {
         }
     } else {
         u16 *y = (u16 *)a.y + at;
-        if (a.vy && n + 3 < a.N) {
-            *(ushort4 *)y = make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3]));
+        if (n + 3 < a.N) {
+            put_u16x4(y, make_ushort4(bf_down(v[0]), bf_down(v[1]), bf_down(v[2]), bf_down(v[3])));
         } else {
 #pragma unroll
             for (int i = 0; i < 4; ++i)

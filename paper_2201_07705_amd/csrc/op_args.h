@@ -36,7 +36,6 @@ struct MmOut {
     void *out;            // ROWS, SCALED, ORTH, STEP (w)
     int64_t ld, z;
     int out_f32;          // ROWS, ORTH: float32 instead of bf16
-    int vec;              // 4 consecutive outputs may be stored at once
     const float *bias;    // [N] or null
     const int *perm;      // output row of product row m, or null
     const int *ea, *eb;   // SCALED
@@ -120,7 +119,6 @@ struct RowsArgs {
     int64_t ldx, ldw, ldy;
     int f32, K, N;
     int k_bank;            // row length of a (K of x and w may be padded)
-    int va, vb, vy;        // whole 16-byte chunks (y: 4 elements) may be moved at once
     const void *zero;      // 16 zero bytes or more
     // rows_plan: slices of the depth in steps of 128 bytes, and of the thin
     // products in bytes
@@ -139,7 +137,6 @@ struct ShrinkArgs {
     const void *a;         // rows of K (by_run: packed, [runs][rp][lda]; else [adapters][rank][K])
     int64_t ldx, lda;
     int by_run, f32, K, rp;
-    int vx, va;            // 16-byte loads of whole chunks of 8 (bf16) or 4 (f32) are safe
     u16 *planes;           // [rows][2 rp] hi | lo, or null
     float *t;              // [rows][rp]
     BatchTables b;
@@ -154,7 +151,7 @@ struct OuterArgs {
     const void *q;
     int64_t sp, sr, ldq;
     int p_f32, q_f32;      // types (a float32 q goes with a float32 p)
-    int R, C, vq;          // vq: whole 16-byte chunks of q's rows may be loaded at once
+    int R, C;
     const int *perm;       // or null
     float *out;
     int64_t ld, chunk;     // distance of rows, and of chunks
@@ -173,7 +170,8 @@ hipError_t launch_outer(const Outers &o, hipStream_t s);
 // Small pieces of work around the products, several in one launch. Blocks of
 // one job do not depend on those of another.
 enum JobKind {
-    // out[r][c], c < ldo: rows (perm[r]) of `in` copied, zeros from cols on
+    // out[r][c], c < ldo: rows (perm[r]) of `in` copied, zeros from cols on;
+    // ldo whole 16-byte chunks
     JOB_PAD,
     // float32 rows (perm[r]) as two float16 planes of in * 2^e, one exponent
     // per row (its largest value lands in [2^14, 2^15)): out, lo, e
@@ -209,7 +207,6 @@ struct Job {
     float *sum;
     int64_t ldi, ldo;
     const int *perm;
-    int vec;               // whole 16-byte chunks of the input may be loaded at once
     int in_rc, by_rank, turned, R, rp, n;   // PACK: n runs, CHUNKS: n adapters; columns in cols
     const int *run_id, *run_rank, *run_of, *chunk_first;
     const int4 *row_info;
@@ -244,7 +241,6 @@ struct OrthArgs {
     Planes x;              // [n][ld >= m]: the wide orientation
     Planes xt;             // [m][ld >= n]
     // thin matrices: n = min(rows, cols) <= THIN_MAX
-    int vec;               // 4 consecutive elements may be moved at once
     double *gram;          // [count][parts][np * np], np = n rounded up to 16
     float *q;              // [count][np * np]: out = q * (2^e u)
     int *e;                // [count]

@@ -320,9 +320,6 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
 int64_t partial_floats(const MmArgs &a) {
     return a.splits > 1 ? (int64_t)a.splits * a.batch * a.M * a.ldp : 0;
 }
-int vec_ok(const void *p, int64_t ld, int f32) {
-    return (uintptr_t)p % (f32 ? 16 : 8) == 0 && ld % 4 == 0;
-}
 // Rows that a product reads where they are; others are copied first.
 bool in_place(const void *p, int64_t rows, int64_t ld, int64_t cols) {
     return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= MM_MAX_LD && rows * ld <= 1ll << 30;
@@ -366,7 +363,6 @@ Job job(int kind, const void *in, int64_t ldi, int rows, int cols, bool f32) {
     j.rows = rows;
     j.cols = cols;
     j.f32 = f32;
-    j.vec = (uintptr_t)in % 16 == 0 && ldi % (f32 ? 4 : 8) == 0;
     return j;
 }
 
@@ -520,7 +516,6 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, fl
     m.o.perm = b.perm;
     m.o.out = p.out;
     m.o.ld = p.ld_out;
-    m.o.vec = vec_ok(p.out, p.ld_out, f32);
     m.o.bias = p.bias;
     OPCHK(launch_mm(m, c.stream), "product");
     return GEMEL_OK;
@@ -546,9 +541,6 @@ ShrinkArgs shrink(const BatchTables &b, bool f32, const void *x, int64_t ldx, in
     s.f32 = f32;
     s.K = K;
     s.rp = (int)op_round_up(b.rank, 32);
-    const int64_t q = f32 ? 4 : 8;
-    s.vx = (uintptr_t)x % 16 == 0 && ldx % q == 0;
-    s.va = (uintptr_t)a % 16 == 0 && lda % q == 0;
     s.planes = planes;
     s.t = t;
     s.b = b;
@@ -597,9 +589,6 @@ gemel_status adapt_rows(Call &c, const BatchTables &b, bool f32, const gemel_pro
     a.y = y;
     a.ldy = ldy;
     a.k_bank = (int)K;
-    a.va = (uintptr_t)proj->a % 16 == 0 && K % q == 0;
-    a.vb = (uintptr_t)proj->b % 16 == 0 && b.rank % q == 0;
-    a.vy = vec_ok(y, ldy, f32);
     a.zero = c.st->zero;
     a.partial = c.at<float>(o_p);
     a.t = c.at<float>(o_t);
@@ -721,7 +710,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         o.p_f32 = o.q_f32 = f32;
         o.R = (int)M;
         o.C = (int)K;
-        o.vq = (uintptr_t)o.q % 16 == 0 && o.ldq % (f32 ? 4 : 8) == 0;
         o.ld = op_round_up(K, 4);
         o.chunk = M * o.ld;
         o.positions = (int)N;
@@ -782,7 +770,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         o.p_f32 = o.q_f32 = f32;
         o.R = (int)N;
         o.C = (int)K;
-        o.vq = (uintptr_t)x % 16 == 0 && ldx % (f32 ? 4 : 8) == 0;
         o.out = dw;
         o.ld = K;
         o.positions = o.per = (int)M;
@@ -833,7 +820,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         o.q_f32 = f32;
         o.R = rp;
         o.C = (int)C;
-        o.vq = (uintptr_t)right % 16 == 0 && ld % (f32 ? 4 : 8) == 0;
         o.perm = b.perm;
         o.out = c.at<float>(o_sums);
         o.ld = C;
@@ -857,7 +843,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     if (db) adapter_gradient(t, dy, lddy, N, o_db, db, 1);
     if (dx && few) {
         Job j = job(JOB_ROWS, proj->a, rows_dx.ld, (int)M, (int)K, f32);
-        j.vec = (uintptr_t)proj->a % 16 == 0 && K % 4 == 0;
         j.sum = rows_dx.out;
         j.parts = rows_dx.n_chunks;
         j.out = dx;
@@ -893,7 +878,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         w.partial = c.at<float>(o_part);
         w.o.out = dw;
         w.o.ld = K;
-        w.o.vec = vec_ok(dw, K, 1);
         OPCHK(launch_mm(w, stream), "product");
     }
     OPCHK(launch_outer(outers, stream), "gradients");
@@ -941,9 +925,6 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
 // is nearly orthogonal these are most of S and M.
 gemel_status orthogonal(Call &c, OrthArgs o) {
     gemel_ctx *ctx = c.ctx;
-    const int64_t bytes4 = o.f32 ? 16 : 8;
-    o.vec = o.cols % 4 == 0 && (uintptr_t)o.g % bytes4 == 0 && (uintptr_t)o.m % 16 == 0 &&
-            (uintptr_t)o.out % (o.step ? 16 : bytes4) == 0 && (uintptr_t)o.copy % 8 == 0;
     if (std::min(o.rows, o.cols) <= THIN_MAX) return orthogonal_thin(c, o);
     const int steps = o.steps;
     const bool step = o.step;
@@ -1108,7 +1089,6 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
                 last.o.lambda = o.lambda + k;
                 last.o.cs = cs;
                 last.o.cv = cv;
-                last.o.vec = o.cols % 4 == 0 && (uintptr_t)last.o.out % 16 == 0 && (uintptr_t)last.o.copy % 8 == 0;
                 OPCHK(launch_mm(last, c.stream), "product");
             }
             k += by;
