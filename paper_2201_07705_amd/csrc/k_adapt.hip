@@ -48,14 +48,28 @@ __device__ __forceinline__ const A &arg_of(int i) {
     return ((const Two<A> *)__builtin_amdgcn_kernarg_segment_ptr())->a[i];
 }
 
+// What becomes of a sum t (scaled) of position p and rank index q.
+__device__ __forceinline__ void put_thin(const ShrinkArgs &a, int64_t p, int q, float t) {
+    if (a.t) a.t[p * a.rp + q] = t;
+    if (a.planes) {
+        // bf16 pair: t to 16 bits, so that its product with B is as exact as
+        // the main product's sums
+        const u16 h = bf_down(t);
+        a.planes[p * 2 * a.rp + q] = h;
+        a.planes[p * 2 * a.rp + a.rp + q] = bf_down(t - bf_up(h));
+    }
+}
+
 // t[p][r] = scale * sum_k x[row p][k] a[r][k] for up to 32 positions of one
-// run and RB blocks of 16 rank indices. 8 waves share the depth, chunk by
-// chunk, and add their sums in LDS in wave order. Reading x bounds it, once
+// run and RB blocks of 16 rank indices. 8 waves share the depth (or a slice of
+// it), chunk by chunk, and add their sums in LDS in wave order. Reading x bounds it, once
 // each wave has four chunks of every operand in flight. Sums are float32;
 // float32 operands go through the float32 MFMA unrounded.
 template <bool F32, int RB>
 __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args) {
-    const ShrinkArgs &a = arg_of<ShrinkArgs>(blockIdx.z);
+    const int first = arg_of<ShrinkArgs>(0).slices, second = (int)blockIdx.z >= first;
+    const ShrinkArgs &a = arg_of<ShrinkArgs>(second);
+    const int slice = (int)blockIdx.z - (second ? first : 0);
     __shared__ f32x4 part[8][2 * RB][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), g = lane >> 4, l16 = lane & 15;
     const int *it = a.b.items + 3 * blockIdx.x;
@@ -93,12 +107,13 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
             }
     };
     if (r0 < rank) {
-        int k = wave * 4 * Q;   // (the wave's; its lane groups take Q each)
+        int k = slice * a.per + wave * 4 * Q;   // (the wave's; its lane groups take Q each)
+        const int end = min(a.K, (slice + 1) * a.per);
         // whole chunks, four rounds of them in flight: no branch may stand
         // between the loads
         const char *const xb = (const char *)a.x, *const ab = (const char *)a.a;
         constexpr int E = F32 ? 4 : 2, ROUNDS = 4;
-        for (; k + (ROUNDS - 1) * 32 * Q + 4 * Q <= a.K; k += ROUNDS * 32 * Q) {
+        for (; k + (ROUNDS - 1) * 32 * Q + 4 * Q <= end; k += ROUNDS * 32 * Q) {
             uint4 xv[ROUNDS][2], av[ROUNDS][RB];
 #pragma unroll
             for (int q = 0; q < ROUNDS; ++q) {
@@ -115,12 +130,12 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
                 add(xv[q], av[q]);
             }
         }
-        for (; k < a.K; k += 32 * Q) {
+        for (; k < end; k += 32 * Q) {
             uint4 xv[2], av[RB];
 #pragma unroll
-            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k + g * Q, a.K);
+            for (int i = 0; i < 2; ++i) xv[i] = chunk<F32>(a.x, xrow[i], k + g * Q, end);
 #pragma unroll
-            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k + g * Q, used[j] ? a.K : 0);
+            for (int j = 0; j < RB; ++j) av[j] = chunk<F32>(a.a, arow[j], k + g * Q, used[j] ? end : 0);
             add(xv, av);
         }
     }
@@ -139,16 +154,25 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
         const int q = r0 + 16 * j + 4 * g + e;
-        const float t = q < rank ? sum[e] * scale : 0.f;
-        if (a.t) a.t[p * a.rp + q] = t;
-        if (a.planes) {
-            // bf16 pair: t to 16 bits, so that its product with B is as
-            // exact as the main product's sums
-            const u16 h = bf_down(t);
-            a.planes[p * 2 * a.rp + q] = h;
-            a.planes[p * 2 * a.rp + a.rp + q] = bf_down(t - bf_up(h));
-        }
+        if (a.slices > 1)
+            a.part[((int64_t)slice * a.b.rows + p) * a.rp + q] = sum[e];
+        else
+            put_thin(a, p, q, q < rank ? sum[e] * scale : 0.f);
     }
+}
+
+// The slices' sums, added in order.
+__global__ __launch_bounds__(256) void shrink_sum_kernel(const Two<ShrinkArgs> args) {
+    const ShrinkArgs &a = arg_of<ShrinkArgs>(blockIdx.y);
+    const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.b.rows * a.rp;
+    const int p = (int)(i / a.rp), q = (int)(i - (int64_t)p * a.rp);
+    if (a.slices < 2 || i >= n || p < a.b.run_start[0]) return;
+    int u = a.b.first_run[p >> 6];
+    while (a.b.run_start[u + 1] <= p) ++u;
+    float t = 0.f;
+#pragma unroll 8
+    for (int k = 0; k < a.slices; ++k) t += a.part[k * n + i];
+    put_thin(a, p, q, q < a.b.run_rank[u] ? t * a.b.run_scale[u] : 0.f);
 }
 
 // out[r][c] = sum over a chunk's positions of p(pos, r) q[row][c] for 32 r
@@ -304,16 +328,36 @@ hipError_t launch(const void *fn, dim3 grid, int block, const A *a, int n, hipSt
 
 }  // namespace
 
+// A workgroup takes 2 us for every 512 (float32) or 1024 columns, and adding
+// slices a launch of 5 us: the depth is cut where few workgroups would have
+// more than 8 us of it, into as many as the card holds at once.
+void shrink_plan(ShrinkArgs &a, int n) {
+    const int turn = a.f32 ? 512 : 1024, turns = (a.K + turn - 1) / turn;
+    const int64_t groups = (int64_t)a.b.n_items * (a.rp / 32) * n;
+    a.slices = 1;
+    a.per = a.K;
+    if (turns <= 4 || groups > 256) return;
+    const int want = (int)std::min<int64_t>(turns, 512 / std::max<int64_t>(1, groups));
+    a.per = (turns + want - 1) / want * turn;
+    a.slices = (a.K + a.per - 1) / a.per;
+}
+
 hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
     if (n < 1 || n > 2) return hipErrorInvalidValue;
     for (int i = 0; i < n; ++i)
         if (!tables(a[i].b) || !a[i].x || !a[i].a || a[i].K <= 0 || a[i].rp % 32 || a[i].rp < a[i].b.rank ||
             a[i].b.n_items <= 0 || !(a[i].t || a[i].planes) || a[i].rp != a[0].rp || a[i].f32 != a[0].f32 ||
-            a[i].b.items != a[0].b.items)
+            a[i].b.items != a[0].b.items || a[i].slices < 1 || a[i].per < 1 || (int64_t)a[i].slices * a[i].per < a[i].K ||
+            (int64_t)(a[i].slices - 1) * a[i].per >= a[i].K || (a[i].slices > 1 && !a[i].part))
             return hipErrorInvalidValue;
-    const dim3 grid((unsigned)a[0].b.n_items, (unsigned)(a[0].rp / 32), (unsigned)n);
-    return a[0].f32 ? launch(reinterpret_cast<const void *>(&shrink_kernel<true, 2>), grid, 512, a, n, s)
-                    : launch(reinterpret_cast<const void *>(&shrink_kernel<false, 2>), grid, 512, a, n, s);
+    const int slices = a[0].slices + (n > 1 ? a[1].slices : 0);
+    const dim3 grid((unsigned)a[0].b.n_items, (unsigned)(a[0].rp / 32), (unsigned)slices);
+    const void *fn = a[0].f32 ? reinterpret_cast<const void *>(&shrink_kernel<true, 2>)
+                              : reinterpret_cast<const void *>(&shrink_kernel<false, 2>);
+    const hipError_t e = launch(fn, grid, 512, a, n, s);
+    if (e != hipSuccess || slices == n) return e;
+    const dim3 all((unsigned)(((int64_t)a[0].b.rows * a[0].rp + 255) / 256), (unsigned)n);
+    return launch(reinterpret_cast<const void *>(&shrink_sum_kernel), all, 256, a, n, s);
 }
 
 bool add_outer(Outers &o, const OuterArgs &a) {

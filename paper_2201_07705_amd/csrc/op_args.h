@@ -137,11 +137,14 @@ struct ShrinkArgs {
     const void *a;         // rows of K (by_run: packed, [runs][rp][lda]; else [adapters][rank][K])
     int64_t ldx, lda;
     int by_run, f32, K, rp;
+    int slices, per;       // shrink_plan: the depth in slices of `per`
+    float *part;           // [slices][rows][rp] with slices > 1
     u16 *planes;           // [rows][2 rp] hi | lo, or null
     float *t;              // [rows][rp]
     BatchTables b;
 };
-// One or two thin products (of one batch) in a launch.
+void shrink_plan(ShrinkArgs &a, int n);   // slices, per; n products go in one launch
+// One or two thin products (of one batch) in a launch (two, where the depth is cut).
 hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s);
 
 // out[chunk][r][c] = sum over the chunk's positions of p(pos, r) * q[perm[pos]][c],

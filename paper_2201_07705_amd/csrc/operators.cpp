@@ -531,7 +531,7 @@ gemel_status get_batch(gemel_ctx *ctx, int32_t id, State **st, Batch **b) {
 }
 
 ShrinkArgs shrink(const BatchTables &b, bool f32, const void *x, int64_t ldx, int K, const void *a, int64_t lda, bool by_run,
-                  u16 *planes, float *t) {
+                  int n) {
     ShrinkArgs s{};
     s.x = x;
     s.a = a;
@@ -541,11 +541,12 @@ ShrinkArgs shrink(const BatchTables &b, bool f32, const void *x, int64_t ldx, in
     s.f32 = f32;
     s.K = K;
     s.rp = (int)op_round_up(b.rank, 32);
-    s.planes = planes;
-    s.t = t;
     s.b = b;
+    shrink_plan(s, n);
     return s;
 }
+
+int64_t part_floats(const ShrinkArgs &s) { return s.slices > 1 ? (int64_t)s.slices * s.b.rows * s.rp : 0; }
 
 // Few rows: k_rows.hip, on copies of the operands that it cannot read in
 // place.
@@ -632,7 +633,9 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     p.bias = proj->bias;
     p.out = y;
     p.ld_out = ldy;
-    const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4);
+    ShrinkArgs t = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, 1);
+    const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4),
+                 o_tp = c.lay.take(b.runs ? part_floats(t) : 0, 4);
     const size_t o_part = c.lay.take(plan_adapted(c, b, f32, p), 4);
     if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
     Jobs first, second;
@@ -640,7 +643,9 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     OPCHK(launch_jobs(second, stream), "copies");
     if (b.runs) {
         (f32 ? (void *&)p.t : (void *&)p.planes) = c.at<void>(o_t);
-        const ShrinkArgs t = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, p.planes, p.t);
+        t.planes = p.planes;
+        t.t = p.t;
+        t.part = c.at<float>(o_tp);
         OPCHK(launch_shrink(&t, 1, stream), "thin product");
     }
     return run_adapted(c, b, f32, p, c.at<float>(o_part));
@@ -695,6 +700,13 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // few rows: W is read as it lies for dx, and dW written as the product
     // of a few columns of dy and rows of x, without copies of either
     const bool few = M <= ROWS_MAX;
+    // U = scale dy B and T = scale x A^T
+    ShrinkArgs thin[2];
+    const int n_thin = need_u + need_t;
+    if (need_u) thin[0] = shrink(b, f32, dy, lddy, (int)N, nullptr, Np, true, n_thin);
+    if (need_t) thin[need_u] = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, n_thin);
+    size_t o_thin[2] = {};
+    for (int i = 0; i < n_thin; ++i) o_thin[i] = c.lay.take(part_floats(thin[i]), 4);
     const size_t o_u = c.lay.take(need_u ? M * rp : 0, 4), o_up = c.lay.take(need_u && !f32 && !few ? M * rp : 0, 4),
                  o_t = c.lay.take(need_t ? M * rp : 0, 4), o_bt = c.lay.take(need_u ? b.runs * rp * Np : 0, e);
     int64_t part = 0;
@@ -857,14 +869,15 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
 
     OPCHK(launch_jobs(first, stream), "column maxima");
     OPCHK(launch_jobs(second, stream), "copies");
-    ShrinkArgs thin[2];
-    int n_thin = 0;
+    for (int i = 0; i < n_thin; ++i) thin[i].part = c.at<float>(o_thin[i]);
     if (need_u) {
         p.planes = f32 || few ? nullptr : c.at<u16>(o_up);
         p.t = u;
-        thin[n_thin++] = shrink(b, f32, dy, lddy, (int)N, c.at<char>(o_bt), Np, true, dx ? p.planes : nullptr, u);
+        thin[0].a = c.at<char>(o_bt);
+        thin[0].planes = dx ? p.planes : nullptr;
+        thin[0].t = u;
     }
-    if (need_t) thin[n_thin++] = shrink(b, f32, x, ldx, (int)K, proj->a, K, false, nullptr, t);
+    if (need_t) thin[need_u].t = t;
     if (n_thin) OPCHK(launch_shrink(thin, n_thin, stream), "thin products");
     if (dx && !few)
         if (gemel_status s = run_adapted(c, b, f32, p, c.at<float>(o_part))) return s;

@@ -1,0 +1,76 @@
+"""The operators at sizes where they change how they work: long depths that
+are cut and joined, tiles of every size with ragged edges, results wider than
+one tile, and Newton-Schulz steps taken in pairs. Definitions and tolerances
+are those of the small cases."""
+
+import pytest
+
+from test_gpu_operators import (check, close, ctxs, near, orthogonal, problem,  # noqa: F401
+                                rand, reference, batch_of, DT)
+
+pytestmark = pytest.mark.gpu
+
+SHAPES = [
+    # rows per request, adapters, bank, rank, n_in, n_out
+    ([80], [0], 1, 20, 5003, 70),                   # thin sums in slices
+    ([1, 0, 9], [1, 0, 1], 3, 4, 9001, 5501),       # the same, few rows
+    ([70, 3], [0, -1], 2, 40, 70, 9000),            # only one of the two
+    ([100, 30, 10], [1, 0, 1], 2, 8, 20001, 140),   # split depth
+    ([19000, 33], [0, 1], 2, 8, 120, 100),          # split over the rows
+    ([2000, 65, 2034], [2, -1, 0], 3, 24, 520, 4100),
+    ([4200], [0], 1, 48, 4104, 136),
+    ([520, 1], [0, 1], 2, 16, 1, 3000),
+    ([60], [0], 1, 7, 4999, 3),
+]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("case", range(len(SHAPES)))
+def test_adapt_and_gradients(ctxs, dtype, case):  # noqa: F811
+    n_rows, ids, bank, rank, k, n = SHAPES[case]
+    check(ctxs[dtype], problem(dtype, n_rows, ids, bank, rank, k, n, 100 + case))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_some_gradients_alone(ctxs, dtype):  # noqa: F811
+    """Each gradient asked for by itself, with cut depths and without."""
+    ctx = ctxs[dtype]
+    for rows in ([12, 4], [90, 40]):
+        s = problem(dtype, rows, [1, 0], 2, 12, 5200, 2600, 7)
+        b = batch_of(ctx, s)
+        want = reference(s)
+        for name in ("x", "weight", "bias", "a", "b"):
+            got = ctx.adapt_backward(b, s["dy"], s["x"], s["w"], s["a"], s["b"],
+                                     needs=(name,))
+            assert set(got) == {name}
+            close(name, got[name], want[name])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows,cols", [(2050, 6200), (6200, 2050), (1030, 1025),
+                                       (700, 9000), (3001, 90)])
+def test_orthogonalize(ctxs, dtype, rows, cols):  # noqa: F811
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(rows)
+    g = rand(gen, rows, cols, dtype=DT[dtype])
+    near(ctxs[dtype].orthogonalize(g), orthogonal(g),
+         2.0 ** -8 if dtype == "bf16" else 2.0 ** -17)
+
+
+@pytest.mark.parametrize("rows,cols", [(2050, 6201), (6201, 2050)])
+def test_muon_step(ctxs, rows, cols):  # noqa: F811
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(cols)
+    f64 = torch.float64
+    w, m, g = (rand(gen, rows, cols, std=s, dtype=torch.float32)
+               for s in (1.0, 1e-2, 1e-2))
+    w0, m1 = w.clone(), 0.95 * m.to(f64) + g.to(f64)
+    o = orthogonal(g.to(f64) + 0.95 * m1)
+    rate = 0.3 * max(1.0, rows / cols) ** 0.5
+    copy = torch.empty_like(w, dtype=torch.bfloat16)
+    ctxs["bf16"].muon_step(w, m, g, lr=0.3, momentum=0.95, weight_decay=0.1,
+                           copy=copy)
+    want = (1 - 0.3 * 0.1) * w0.to(f64) - rate * o
+    assert ((m.to(f64) - m1).abs() <= 2.0 ** -22 * (1.95 * m1.abs() + g.abs())).all()
+    assert (w.to(f64) - want).norm() <= rate * 2.0 ** -17 * o.norm() + 2.0 ** -22 * w0.norm()
+    assert torch.equal(copy, w.bfloat16())
