@@ -26,12 +26,19 @@ __device__ __forceinline__ int plane_exp(unsigned bits) {
     if (bits == 0u || bits >= 0x7f800000u) return 0;
     return 14 - ilogbf(mx);
 }
-__device__ __forceinline__ void split_put(u16 *hi, u16 *lo, int64_t at, float v, int e) {
-    const float s = ldexpf(v, e);
-    const u16 h = half_down(s);
-    hi[at] = h;
-    // the rest of a value that is not finite would be NaN; the sum has it already
-    lo[at] = isfinite(s) ? half_down(s - half_up(h)) : (u16)0;
+// 4 values from column c (a multiple of 4) of a row of pairs on
+__device__ __forceinline__ void split_put(u16 *row, int c, f32x4 v, int e) {
+    u16 h[4], l[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float s = ldexpf(v[i], e);
+        h[i] = half_down(s);
+        // the rest of a value that is not finite would be NaN; the sum has it already
+        l[i] = isfinite(s) ? half_down(s - half_up(h[i])) : (u16)0;
+    }
+    row += pair_at(c);
+    *(ushort4 *)row = make_ushort4(h[0], h[1], h[2], h[3]);
+    *(ushort4 *)(row + PAIR_RUN) = make_ushort4(l[0], l[1], l[2], l[3]);
 }
 __device__ __forceinline__ unsigned magnitude(float v) { return __float_as_uint(v) & 0x7fffffffu; }
 
@@ -102,16 +109,9 @@ __device__ __forceinline__ void split(const Job &j, int block) {
     for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o));
     const int e = plane_exp(m);
     if (lane == 0) j.e[r] = e;
-    u16 *hi = (u16 *)j.out + r * j.ldo, *lo = j.lo + r * j.ldo;
+    u16 *out = (u16 *)j.out + r * j.ldo;
 #pragma unroll 4
-    for (int c = lane * 4; c < j.ldo; c += 256) {
-        const f32x4 v = load4(in + c, j.cols - c);
-        u16 h[4], l[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) split_put(h, l, i, v[i], e);
-        *(ushort4 *)(hi + c) = make_ushort4(h[0], h[1], h[2], h[3]);
-        *(ushort4 *)(lo + c) = make_ushort4(l[0], l[1], l[2], l[3]);
-    }
+    for (int c = lane * 4; c < j.ldo / 2; c += 256) split_put(out, c, load4(in + c, j.cols - c), e);
 }
 
 // 64 x 64 tiles through LDS, which holds the tile transposed. E: u16 (copied)
@@ -150,18 +150,13 @@ __device__ __forceinline__ void turn(const Job &j, int block, unsigned char *lds
     __syncthreads();
     for (int i = tid; i < 64 * 16; i += 256) {
         const int c = i >> 4, r = (i & 15) * 4;
-        if (c0 + c >= j.cols || r0 + r >= j.ldo) continue;
+        if (c0 + c >= j.cols || r0 + r >= (F ? j.ldo / 2 : j.ldo)) continue;
         const E *t = tile + c * PITCH + r;
-        const int64_t at = (int64_t)(c0 + c) * j.ldo + r0 + r;
-        if constexpr (F) {
-            u16 h[4], l[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) split_put(h, l, k, t[k], es[c]);
-            *(ushort4 *)((u16 *)j.out + at) = make_ushort4(h[0], h[1], h[2], h[3]);
-            *(ushort4 *)(j.lo + at) = make_ushort4(l[0], l[1], l[2], l[3]);
-        } else {
-            *(ushort4 *)((u16 *)j.out + at) = make_ushort4(t[0], t[1], t[2], t[3]);
-        }
+        u16 *const out = (u16 *)j.out + (int64_t)(c0 + c) * j.ldo;
+        if constexpr (F)
+            split_put(out, r0 + r, f32x4{t[0], t[1], t[2], t[3]}, es[c]);
+        else
+            *(ushort4 *)(out + r0 + r) = make_ushort4(t[0], t[1], t[2], t[3]);
     }
     if (j.sum) {
         const int c = tid & 63, q = tid >> 6;
@@ -363,14 +358,14 @@ bool add_job(Jobs &all, const Job &in) {
             blocks = ((int64_t)j.rows * (j.ldo / (j.f32 ? 4 : 8)) + PAD_ITEMS - 1) / PAD_ITEMS;
             break;
         case JOB_SPLIT:
-            ok = ok && j.in && j.out && j.lo && j.e && j.rows > 0 && j.ldo >= j.cols && j.ldo % 4 == 0;
+            ok = ok && j.in && j.out && j.e && j.rows > 0 && j.ldo / 2 >= j.cols && j.ldo % (4 * PAIR_RUN) == 0;
             blocks = ((int64_t)j.rows + 3) / 4;
             break;
         case JOB_TURN:
-            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.rows && j.ldo % 4 == 0 &&
-                 (!j.f32 || (j.lo && j.e && j.max && j.parts > 0));
-            blocks = across * ((j.ldo + 63) / 64);
-            ok = ok && (!j.sum || (j.ldo + 63) / 64 == (j.rows + 63) / 64);
+            ok = ok && j.in && j.out && j.rows > 0 && j.ldo / (j.f32 ? 2 : 1) >= j.rows && j.ldo % (j.f32 ? 4 * PAIR_RUN : 4) == 0 &&
+                 (!j.f32 || (j.e && j.max && j.parts > 0));
+            blocks = across * ((j.ldo / (j.f32 ? 2 : 1) + 63) / 64);
+            ok = ok && (!j.sum || blocks == across * ((j.rows + 63) / 64));
             break;
         case JOB_COLMAX:
             ok = ok && j.in && j.max && j.rows > 0 && j.parts > 0 && j.f32;

@@ -63,16 +63,25 @@ template <typename V>
 __device__ __forceinline__ void store_at(void *base, uint32_t off, V v) {
     *(V *)((char *)base + off) = v;
 }
+// The same of planes (tiles begin at multiples of 32).
+__device__ __forceinline__ uint32_t offset_of(int m, int n, const Planes &p) {
+    return offset_of(m, p.pair ? pair_at(n) : n, p.ld, 2);
+}
+__device__ __forceinline__ u16 *at_tile(u16 *plane, const Tile &t, const Planes &p) {
+    return plane + (int64_t)t.z * p.z + (int64_t)t.m0 * p.ld + ((int64_t)t.n0 << p.pair);
+}
+__device__ __forceinline__ int width(const Planes &p) { return (int)(p.ld >> p.pair); }
 // Elements (m, n .. n + 3) of the tile of a matrix in planes; rows are padded
 // to 64, so 4 elements stay in a row, and rows beyond the last one read it.
 __device__ __forceinline__ void at4(const Planes &p, const Tile &t, int m, int n, int rows, f32x4 &hi, f32x4 &lo) {
     lo = f32x4{0.f, 0.f, 0.f, 0.f};
     if (t.inside) {
-        const uint32_t off = offset_of(m, n, p.ld, 2);
-        hi = half_up4(load_at<ushort4>(at_tile(p.hi, t, p.z, p.ld), off));
-        if (p.lo) lo = half_up4(load_at<ushort4>(at_tile(p.lo, t, p.z, p.ld), off));
+        const uint32_t off = offset_of(m, n, p);
+        hi = half_up4(load_at<ushort4>(at_tile(p.hi, t, p), off));
+        if (p.lo) lo = half_up4(load_at<ushort4>(at_tile(p.lo, t, p), off));
     } else {
-        const int64_t at = (int64_t)t.z * p.z + (int64_t)min(t.m0 + m, rows - 1) * p.ld + min(t.n0 + n, (int)p.ld - 4);
+        const int c = min(t.n0 + n, width(p) - 4);
+        const int64_t at = (int64_t)t.z * p.z + (int64_t)min(t.m0 + m, rows - 1) * p.ld + (p.pair ? pair_at(c) : c);
         hi = half_up4(*(const ushort4 *)(p.hi + at));
         if (p.lo) lo = half_up4(*(const ushort4 *)(p.lo + at));
     }
@@ -319,8 +328,8 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
             if (d && i >= 0 && i < 4 && t.m0 + m < a.M) d[t.z * o.diag_z + t.m0 + m] = i == 0 ? x[0] : i == 1 ? x[1] : i == 2 ? x[2] : x[3];
         }
         const uint4 q = pairs(x);
-        if (t.inside || (t.m0 + m < a.M && t.n0 + n < p.ld))
-            put_pairs(at_tile(p.hi, t, p.z, p.ld), p.lo ? at_tile(p.lo, t, p.z, p.ld) : nullptr, offset_of(m, n, p.ld, 2), q);
+        if (t.inside || (t.m0 + m < a.M && t.n0 + n < width(p)))
+            put_pairs(at_tile(p.hi, t, p), p.lo ? at_tile(p.lo, t, p) : nullptr, offset_of(m, n, p), q);
         return q;
     }
 }
@@ -345,7 +354,7 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
 template <int T>
 constexpr int mm_threads() { return T == 64 ? 256 : 512; }
 
-template <int T, int STAGES, int PHASES, bool F16, int EPI>
+template <int T, int STAGES, int PHASES, bool F16, bool PAIR, int EPI>
 __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2) void mm_kernel(const MmArgs a) {
     constexpr int NT = mm_threads<T>(), NW = NT / 64, WN = T == 256 ? 4 : 2;
     constexpr int TM = T * WN / NW, TN = T / WN, FM = TM / 16, FN = TN / 16;
@@ -361,7 +370,7 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
     const int split = blockIdx.y, z = blockIdx.z;
     const int m0 = tm * T, n0 = tn * T;
     const int nk = (a.K + BK - 1) / BK;
-    const int s0 = split * a.steps, mains = min(nk * a.nseg - s0, a.steps);
+    const int s0 = split * a.steps, mains = min(nk - s0, a.steps);
     // extension steps: the runs that overlap the tile's rows, in the last split
     int u = 0, ek = 0, exts = 0;
     if (EPI == EPI_ROWS && a.ext && split == a.splits - 1) {
@@ -383,16 +392,14 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         ob[i] = (uint32_t)((n - n0) * (uint32_t)a.ldb + ch) * 2u;
     }
     const int64_t za = (int64_t)z * a.za + (a.perm ? 0 : (int64_t)m0 * a.lda), zb = (int64_t)z * a.zb + (int64_t)n0 * a.ldb;
-    // the next step's operands: kept as running pointers, since a load of a
-    // segment's pointers in every step would hold it up
-    int seg = s0 / nk, seg_left = nk - (s0 - seg * nk), iss = 0;
-    const u16 *pa = (seg == 0 ? a.a[0] : seg == 1 ? a.a[1] : a.a[2]) + za + (s0 - seg * nk) * BK;
-    const u16 *pb = (seg == 0 ? a.b[0] : seg == 1 ? a.b[1] : a.b[2]) + zb + (s0 - seg * nk) * BK;
+    // the next step's operands
+    int iss = 0;
+    const u16 *pa = a.a + za + s0 * BK, *pb = a.b + zb + s0 * BK;
     // Requests the next step; past the last one, the last one again (into a
     // buffer whose reads are over), so that every step waits alike.
     auto issue = [&](unsigned char *stage) __attribute__((always_inline)) {
         const bool ext = EPI == EPI_ROWS && exts > 0 && iss >= mains;
-        const int kk = (s0 + min(iss, mains - 1)) * BK;   // (of one segment, where it is used)
+        const int kk = (s0 + min(iss, mains - 1)) * BK;
         if (EPI == EPI_ROWS && (ext || kk + BK > a.K)) {
             // rows of other runs, and chunks beyond a depth that is no
             // multiple of 64, are zeros
@@ -431,12 +438,6 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         if (iss < mains) {
             pa += BK;
             pb += BK;
-            if (EPI != EPI_ROWS && --seg_left == 0) {
-                ++seg;
-                seg_left = nk;
-                pa = (seg == 1 ? a.a[1] : a.a[2]) + za;
-                pb = (seg == 1 ? a.b[1] : a.b[2]) + zb;
-            }
         }
     };
     f32x4 acc[FM][FN];
@@ -462,17 +463,23 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         for (int j = 0; j < NB; ++j) f[j] = *(const H8 *)(s + rb + (PHASES == 1 && j >= FN ? h1 : h) + j % FN * 16 * ROW);
     };
     auto mul = [&](H8(&f)[NA], H8(&b)[NB], int row) __attribute__((always_inline)) {
+        // a whole step: both halves of the depth, or hi lo, lo hi and hi hi
+        constexpr int PRODUCTS = PHASES > 1 ? 1 : PAIR ? 3 : 2, ROWS = PHASES > 1 ? NA : FM;
 #pragma unroll
-        for (int i = 0; i < NA; ++i)
+        for (int q = 0; q < PRODUCTS; ++q) {
+            const int ha = PAIR ? q == 1 : q, hb = PAIR ? PHASES == 1 && q == 0 : q;
 #pragma unroll
-            for (int j = 0; j < FN; ++j) {
-                f32x4 &c = acc[row + i % FM][j];
-                const H8 &bj = b[PHASES == 1 && i >= FM ? FN + j : j];
-                if constexpr (F16)
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_f16(bj, f[i], c, 0, 0, 0);
-                else
-                    c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bj, f[i], c, 0, 0, 0);
-            }
+            for (int i = 0; i < ROWS; ++i)
+#pragma unroll
+                for (int j = 0; j < FN; ++j) {
+                    f32x4 &c = acc[row + i][j];
+                    const H8 &x = f[ha * FM + i], &y = b[hb * FN + j];
+                    if constexpr (F16)
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_f16(y, x, c, 0, 0, 0);
+                    else
+                        c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(y, x, c, 0, 0, 0);
+                }
+        }
         __builtin_amdgcn_sched_barrier(0);
     };
     // the loads of the step after `cur`'s have landed in every wave, and
@@ -485,9 +492,43 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    // one step; set: which fragments hold the whole step (PHASES == 1)
-    auto step = [&](unsigned char *cur, unsigned char *next, int set) __attribute__((always_inline)) {
+    // one step; set: which fragments hold the whole step (PHASES == 1), or
+    // b's hi (pairs)
+    auto paired = [&](unsigned char *cur, unsigned char *next, H8(&bh)[NB], H8(&bl)[NB]) __attribute__((always_inline)) {
         if constexpr (PHASES == 4) {
+            read_a(fa1, cur, h1, 0);
+            read_b(bl, cur, h1);
+            mul(fa0, bh, 0);
+            mul(fa0, bl, 0);
+            read_a(fa0, cur, h0, NA);
+            mul(fa1, bh, 0);
+            read_a(fa1, cur, h1, NA);
+            mul(fa0, bh, NA);
+            mul(fa0, bl, NA);
+            turn();
+            issue(cur);
+            read_a(fa0, next, h0, 0);
+            read_b(bl, next, h0);
+            mul(fa1, bh, NA);
+        } else {
+            read_a(fa1, cur, h1, 0);
+            read_b(bl, cur, h1);
+            mul(fa0, bh, 0);
+            mul(fa0, bl, 0);
+            turn();
+            issue(cur);
+            read_a(fa0, next, h0, 0);
+            read_b(bl, next, h0);
+            mul(fa1, bh, 0);
+        }
+    };
+    auto step = [&](unsigned char *cur, unsigned char *next, int set) __attribute__((always_inline)) {
+        if constexpr (PAIR && PHASES > 1) {
+            if (set)
+                paired(cur, next, fb1, fb0);
+            else
+                paired(cur, next, fb0, fb1);
+        } else if constexpr (PHASES == 4) {
             read_a(fa1, cur, h0, NA);
             mul(fa0, fb0, 0);
             read_a(fa0, cur, h1, 0);
@@ -523,7 +564,7 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
             }
         }
     };
-    static_assert(PHASES != 1 || STAGES % 2 == 0, "a turn of the ring is a turn of the fragments");
+    static_assert(STAGES % 2 == 0, "a turn of the ring is a turn of the fragments");
     unsigned char *const ring[4] = {st0, st1, st2, st3};
 #pragma unroll
     for (int i = 0; i < STAGES; ++i) issue(ring[i]);
@@ -602,8 +643,8 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         wait_lgkm0();
         asm volatile("" ::: "memory");
         const Planes &q = EPI == EPI_NEXT ? e.o.q : e.o.p;
-        u16 *const hi = q.hi + (int64_t)z * q.z + (int64_t)nb * q.ld + mb;
-        u16 *const lo = q.lo ? q.lo + (int64_t)z * q.z + (int64_t)nb * q.ld + mb : nullptr;
+        const Tile flip{z, nb, mb, tile.inside};
+        u16 *const hi = at_tile(q.hi, flip, q), *const lo = q.lo ? at_tile(q.lo, flip, q) : nullptr;
 #pragma unroll 1
         for (int i = 0; i < TN * RP / 256; ++i) {
             const int it = i * 64 + lane;
@@ -612,7 +653,7 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
 #pragma unroll
             for (int k = 0; k < 4; ++k)
                 (&v.x)[k] = *(const uint32_t *)(mine + (m + k) * TN * 4 + ((n >> 2) ^ swz(m + k)) * 16 + (n & 3) * 4);
-            if (tile.inside || (nb + n < e.N && mb + m < q.ld)) put_pairs(hi, lo, offset_of(n, m, q.ld, 2), v);
+            if (tile.inside || (nb + n < e.N && mb + m < width(q))) put_pairs(hi, lo, offset_of(n, m, q), v);
         }
     }
 }
@@ -652,11 +693,11 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
         for (int e = 0; e < 4; ++e) turn[m][n + e] = (&q.x)[e];
         __syncthreads();
         const Planes &t = EPI == EPI_NEXT ? a.o.q : a.o.p;
-        u16 *const hi = t.hi + (int64_t)z * t.z + (int64_t)n0 * t.ld + m0;
-        u16 *const lo = t.lo ? t.lo + (int64_t)z * t.z + (int64_t)n0 * t.ld + m0 : nullptr;
+        const Tile flip{z, n0, m0, tile.inside};
+        u16 *const hi = at_tile(t.hi, flip, t), *const lo = t.lo ? at_tile(t.lo, flip, t) : nullptr;
         // (thread: row m of the transpose, 4 of its columns from n on)
         const uint4 x = make_uint4(turn[n][m], turn[n + 1][m], turn[n + 2][m], turn[n + 3][m]);
-        if (n0 + m < a.N && m0 + n < t.ld) put_pairs(hi, lo, offset_of(m, n, t.ld, 2), x);
+        if (n0 + m < a.N && m0 + n < width(t)) put_pairs(hi, lo, offset_of(m, n, t), x);
     }
 }
 
@@ -666,22 +707,31 @@ int64_t tiles_of(const MmArgs &a, int T) {
     return a.sym ? tm * (tm + 1) / 2 : tm * tn;
 }
 
-template <int T, int STAGES, int PHASES, bool F16, int EPI>
+template <int T, int STAGES, int PHASES, bool F16, bool PAIR, int EPI>
 hipError_t go(const MmArgs &a, hipStream_t s) {
     const dim3 grid((unsigned)tiles_of(a, T), (unsigned)a.splits, (unsigned)a.batch);
     void *p[] = {const_cast<MmArgs *>(&a)};
-    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, STAGES, PHASES, F16, EPI>), grid,
+    hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, STAGES, PHASES, F16, PAIR, EPI>), grid,
                                    dim3(mm_threads<T>()), p, 0, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&mm_reduce_kernel<EPI>),
                            dim3((unsigned)tiles_of(a, 32), 1, (unsigned)a.batch), dim3(256), p, 0, s);
 }
 
-template <int EPI, bool F16>
+template <int EPI, bool F16, bool PAIR>
 hipError_t pick(const MmArgs &a, hipStream_t s) {
-        return a.tile == 256   ? go<256, 2, 4, F16, EPI>(a, s)
-           : a.tile == 128 ? go<128, 2, 2, F16, EPI>(a, s)
-                           : go<64, 4, 1, F16, EPI>(a, s);
+    return a.tile == 256   ? go<256, 2, 4, F16, PAIR, EPI>(a, s)
+           : a.tile == 128 ? go<128, 2, 2, F16, PAIR, EPI>(a, s)
+                           : go<64, 4, 1, F16, PAIR, EPI>(a, s);
+}
+// (float16) either layout, or pairs only
+template <int EPI>
+hipError_t any(const MmArgs &a, hipStream_t s) {
+    return a.pair ? pick<EPI, true, true>(a, s) : pick<EPI, true, false>(a, s);
+}
+template <int EPI>
+hipError_t pairs_only(const MmArgs &a, hipStream_t s) {
+    return a.pair ? pick<EPI, true, true>(a, s) : hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -700,11 +750,15 @@ double mm_plan(MmArgs &a) {
         int tile, slots;                        // workgroups that run at once
         double alone, full, fixed, fixed_part;  // microseconds; with partial sums out
     };
-    static const Form forms[] = {
+    static const Form single[] = {
         {256, 256, 1.65, 1.65, 28.0, 12.0}, {128, 512, 0.62, 0.95, 9.0, 7.0}, {64, 512, 0.21, 0.36, 5.5, 5.0}};
-    const int steps = (a.K + BK - 1) / BK * a.nseg;
+    static const Form pair[] = {
+        {256, 256, 2.35, 2.35, 28.0, 12.0}, {128, 512, 0.75, 1.25, 9.0, 7.0}, {64, 512, 0.27, 0.47, 5.5, 5.0}};
+    const Form *const forms = a.pair ? pair : single;
+    const int steps = (a.K + BK - 1) / BK;
     double best = 1e30;
-    for (const Form &f : forms) {
+    for (int i = 0; i < 3; ++i) {
+        const Form &f = forms[i];
         const int64_t tiles = tiles_of(a, f.tile) * a.batch;
         for (int want = 1; want <= 32 && want <= std::max(1, steps / 4); ++want) {
             const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
@@ -730,29 +784,27 @@ double mm_plan(MmArgs &a) {
 
 hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
     const int nk = (a.K + BK - 1) / BK;
-    if (a.M <= 0 || a.N <= 0 || a.K <= 0 || a.K % 8 || a.batch <= 0 || a.batch > 65535 || a.nseg < 1 || a.nseg > 3 ||
+    if (a.M <= 0 || a.N <= 0 || a.K <= 0 || a.K % 8 || a.batch <= 0 || a.batch > 65535 ||
         a.lda % 8 || a.ldb % 8 || a.lda > MM_MAX_LD || a.ldb > MM_MAX_LD ||
         (a.perm && a.perm_rows * a.lda > (1ll << 30)) || (a.tile != 64 && a.tile != 128 && a.tile != 256) || a.za % 8 || a.zb % 8 || a.lda < a.K || a.ldb < a.K || !a.zero || a.splits < 1 ||
-        a.steps < 1 || a.ext % BK || (int64_t)a.splits * a.steps < (int64_t)nk * a.nseg ||
-        (int64_t)(a.splits - 1) * a.steps >= (int64_t)nk * a.nseg)
+        a.steps < 1 || a.ext % BK || (int64_t)a.splits * a.steps < nk || (int64_t)(a.splits - 1) * a.steps >= nk)
         return hipErrorInvalidValue;
-    for (int i = 0; i < a.nseg; ++i)
-        if (!a.a[i] || !a.b[i] || (uintptr_t)a.a[i] % 16 || (uintptr_t)a.b[i] % 16) return hipErrorInvalidValue;
+    if (!a.a || !a.b || (uintptr_t)a.a % 16 || (uintptr_t)a.b % 16) return hipErrorInvalidValue;
     if (a.splits > 1 && (!a.partial || a.ldp % 4 || a.ldp < a.N)) return hipErrorInvalidValue;
-    if (a.ext && (!a.t || !a.bx || a.runs < 1 || !a.run_start || !a.first_run || a.batch != 1 || a.nseg != 1 || a.f16))
+    if (a.ext && (!a.t || !a.bx || a.runs < 1 || !a.run_start || !a.first_run || a.batch != 1))
         return hipErrorInvalidValue;
     if (a.sym && a.M != a.N) return hipErrorInvalidValue;
     if (a.epi != EPI_ROWS && (a.K % BK || a.ext)) return hipErrorInvalidValue;
     if ((int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64) > INT32_MAX / 256) return hipErrorInvalidValue;
     switch (a.epi) {
-        case EPI_ROWS: return a.f16 ? hipErrorInvalidValue : pick<EPI_ROWS, false>(a, s);
-        case EPI_SCALED: return pick<EPI_SCALED, true>(a, s);
-        case EPI_GRAM: return pick<EPI_GRAM, true>(a, s);
-        case EPI_POLY: return pick<EPI_POLY, true>(a, s);
-        case EPI_NEXT: return pick<EPI_NEXT, true>(a, s);
-        case EPI_ORTH: return pick<EPI_ORTH, true>(a, s);
-        case EPI_STEP: return pick<EPI_STEP, true>(a, s);
-        case EPI_MIX: return pick<EPI_MIX, true>(a, s);
+        case EPI_ROWS: return a.pair ? hipErrorInvalidValue : pick<EPI_ROWS, false, false>(a, s);
+        case EPI_SCALED: return pairs_only<EPI_SCALED>(a, s);
+        case EPI_GRAM: return any<EPI_GRAM>(a, s);
+        case EPI_POLY: return any<EPI_POLY>(a, s);
+        case EPI_NEXT: return any<EPI_NEXT>(a, s);
+        case EPI_ORTH: return any<EPI_ORTH>(a, s);
+        case EPI_STEP: return pairs_only<EPI_STEP>(a, s);
+        case EPI_MIX: return pairs_only<EPI_MIX>(a, s);
     }
     return hipErrorInvalidValue;
 }

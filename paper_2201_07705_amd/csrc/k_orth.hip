@@ -111,7 +111,8 @@ __global__ __launch_bounds__(256) void seed_kernel(const OrthArgs a) {
     const bool wide = a.rows <= a.cols;
     const Planes &p = wide ? a.x : a.xt, &q = wide ? a.xt : a.x;   // as the input lies, and transposed
     const int64_t base = (int64_t)z * a.rows * a.cols;
-    auto put4 = [](const Planes &p, int64_t at, f32x4 v) __attribute__((always_inline)) {
+    auto put4 = [](const Planes &p, int64_t row, int n, f32x4 v) __attribute__((always_inline)) {
+        const int64_t at = row + (p.pair ? pair_at(n) : n);
         const ushort4 h = make_ushort4(half_down(v[0]), half_down(v[1]), half_down(v[2]), half_down(v[3]));
         *(ushort4 *)(p.hi + at) = h;
         if (p.lo)
@@ -128,14 +129,14 @@ __global__ __launch_bounds__(256) void seed_kernel(const OrthArgs a) {
             v[k] = ldexpf(v[k], e);
             tile[y + 16 * i][x + k] = v[k];
         }
-        if (r < a.rows && c < p.ld) put4(p, z * p.z + r * p.ld + c, v);
+        if (r < a.rows && c < p.ld >> p.pair) put4(p, z * p.z + r * p.ld, c, v);
     }
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int c = c0 + y + 16 * i, r = r0 + x;
         const f32x4 v = {tile[x][y + 16 * i], tile[x + 1][y + 16 * i], tile[x + 2][y + 16 * i], tile[x + 3][y + 16 * i]};
-        if (c < a.cols && r < q.ld) put4(q, z * q.z + c * q.ld + r, v);
+        if (c < a.cols && r < q.ld >> q.pair) put4(q, z * q.z + c * q.ld, r, v);
     }
 }
 

@@ -26,11 +26,19 @@ enum MmEpi {
 };
 
 // 16-bit planes of a matrix: hi, and lo (the rest; null = not kept). Rows of
-// ld elements, z elements between the matrices of a batch.
+// ld elements, z elements between the matrices of a batch. Separate arrays,
+// or (pair) one whose rows alternate 32 elements of hi with the same 32 of
+// lo, which is then hi + 32: what a product of pairs reads together lies
+// together.
 struct Planes {
     u16 *hi, *lo;
     int64_t ld, z;
+    int pair;
 };
+constexpr int PAIR_RUN = 32;
+// Where element n of a row is in an array of pairs (4 elements from a
+// multiple of 4 on are consecutive in either layout).
+__host__ __device__ constexpr int pair_at(int n) { return 2 * n - (n & (PAIR_RUN - 1)); }
 
 struct MmOut {
     void *out;            // ROWS, SCALED, ORTH, STEP (w)
@@ -60,15 +68,15 @@ struct MmOut {
     float rate, decay;    // STEP
 };
 
-// C[m][n] = sum over segments and k of a[seg][row m][k] * b[seg][n][k].
-// Operands are rows of contiguous 16-bit elements; 16-byte aligned, ld a
-// multiple of 8; where K is not a multiple of 64 chunks of 8 beyond K
-// are read as zeros (K a multiple of 8).
+// C[m][n] = sum over k of a[row m][k] * b[n][k]. Operands are rows of
+// contiguous 16-bit elements (bf16 for EPI_ROWS, else float16); 16-byte
+// aligned, ld a multiple of 8; where K is not a multiple of 64 chunks of 8
+// beyond K are read as zeros (K a multiple of 8). pair: rows of pairs, K
+// counting both planes; the products hi hi, hi lo and lo hi are summed.
 struct MmArgs {
-    const u16 *a[3], *b[3];
+    const u16 *a, *b;
     int64_t lda, ldb, za, zb;
-    int nseg, M, N, K, batch;
-    int f16;              // 1: float16 operands, 0: bf16
+    int pair, M, N, K, batch;
     int epi;
     int sym;              // only tiles on and above the diagonal
     int tile;             // 64, 128 or 256 (mm_plan)
@@ -76,7 +84,7 @@ struct MmArgs {
     float *partial;       // [splits][batch][M][ldp] with splits > 1
     int64_t ldp;
     const u16 *zero;      // 16 zero bytes or more
-    const int *perm;      // row of a[seg] behind product row m, or null
+    const int *perm;      // row of a behind product row m, or null
     int64_t perm_rows;    // rows that it points into
     // low-rank extension of the depth (bf16): t [M][ext] rows against
     // bx [run][N][ext], where the row's run is the one holding m
@@ -176,11 +184,12 @@ enum JobKind {
     // out[r][c], c < ldo: rows (perm[r]) of `in` copied, zeros from cols on;
     // ldo whole 16-byte chunks
     JOB_PAD,
-    // float32 rows (perm[r]) as two float16 planes of in * 2^e, one exponent
-    // per row (its largest value lands in [2^14, 2^15)): out, lo, e
+    // float32 rows (perm[r]) as float16 pairs of in * 2^e, one exponent per
+    // row (its largest value lands in [2^14, 2^15)): out, e. ldo counts both
+    // planes, a multiple of 128
     JOB_SPLIT,
     // out[c][r], r < ldo: the transpose, zeros from rows on; float32 as
-    // planes with one exponent per output row, from the maxima of
+    // pairs (ldo as for SPLIT) with one exponent per output row, from the maxima of
     // JOB_COLMAX. sum: NULL, or [ceil(rows / 64)][cols] sums of 64 rows
     JOB_TURN,
     JOB_COLMAX,            // max [parts][cols]: largest magnitudes (as bits)
@@ -204,7 +213,6 @@ struct Job {
     int kind, blocks, f32, rows, cols, parts;
     const void *in;
     void *out;
-    u16 *lo;
     int *e;
     unsigned *max;
     float *sum;

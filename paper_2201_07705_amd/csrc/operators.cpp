@@ -366,19 +366,18 @@ Job job(int kind, const void *in, int64_t ldi, int rows, int cols, bool f32) {
     return j;
 }
 
-// A 16-bit copy of an operand: bf16 rows padded, float32 as planes.
+// A 16-bit copy of an operand: bf16 rows padded, float32 as pairs.
 struct Copy {
-    size_t o = 0, o_lo = 0, o_e = 0, o_max = 0;
+    size_t o = 0, o_e = 0, o_max = 0;
     int64_t ld = 0;
     int parts = 0;
 };
 // `rows` rows of `cols` in the copy
 Copy plan_copy(Call &c, int64_t rows, int64_t cols, bool f32, bool turned) {
     Copy p;
-    p.ld = op_round_up(cols, 64);
+    p.ld = op_round_up(cols, 64) * (f32 ? 2 : 1);
     p.o = c.lay.take(rows * p.ld, 2);
     if (f32) {
-        p.o_lo = c.lay.take(rows * p.ld, 2);
         p.o_e = c.lay.take(rows, 4);
         // column maxima by stretches of the input's rows
         p.parts = (int)std::min<int64_t>(32, (cols + 63) / 64);
@@ -392,7 +391,6 @@ bool add_copy(Call &c, const Copy &p, const void *in, int64_t ldi, int rows, int
               float *sum, Jobs &first, Jobs &second) {
     Job j = job(turned ? JOB_TURN : f32 ? JOB_SPLIT : JOB_PAD, in, ldi, turned ? cols : rows, turned ? rows : cols, f32);
     j.out = c.at<u16>(p.o);
-    j.lo = c.at<u16>(p.o_lo);
     j.e = c.at<int>(p.o_e);
     j.max = c.at<unsigned>(p.o_max);
     j.ldo = p.ld;
@@ -407,15 +405,10 @@ bool add_copy(Call &c, const Copy &p, const void *in, int64_t ldi, int rows, int
     return add_job(second, j);
 }
 
-// The operands of a product: bf16 one, float32 the three pairs of planes.
+// Copies as the operands of a product.
 void operands(Call &c, MmArgs &m, const Copy &a, const Copy &b) {
-    const u16 *ah = c.at<u16>(a.o), *al = c.at<u16>(a.o_lo), *bh = c.at<u16>(b.o), *bl = c.at<u16>(b.o_lo);
-    // the small products first
-    const u16 *as[3] = {ah, al, ah}, *bs[3] = {bl, bh, bh};
-    for (int i = 0; i < 3; ++i) {
-        m.a[i] = as[i];
-        m.b[i] = bs[i];
-    }
+    m.a = c.at<u16>(a.o);
+    m.b = c.at<u16>(b.o);
     m.lda = a.ld;
     m.ldb = b.ld;
     m.o.ea = c.at<int>(a.o_e);
@@ -453,12 +446,11 @@ int64_t plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
     m.M = b.rows;
     m.N = p.N;
     m.batch = 1;
-    m.nseg = f32 ? 3 : 1;
-    m.f16 = f32;
+    m.pair = f32;
     m.epi = f32 ? EPI_SCALED : EPI_ROWS;
     p.pad_in = f32 || !in_place(p.in, b.rows, p.ld_in, p.K);
     p.pad_w = f32 || p.w_t || !in_place(p.w, p.N, p.ld_w, p.K);
-    m.K = !f32 && p.K % 8 == 0 ? p.K : (int)op_round_up(p.K, 64);
+    m.K = f32 ? (int)(2 * op_round_up(p.K, 64)) : p.K % 8 == 0 ? p.K : (int)op_round_up(p.K, 64);
     mm_plan(m);
     if (p.pad_in) p.c_in = plan_copy(c, b.rows, p.K, f32, false);
     if (p.pad_w) p.c_w = plan_copy(c, p.N, p.K, f32, p.w_t);
@@ -496,8 +488,8 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, fl
         m.o.rp = rp;
         m.o.ldbx = op_round_up(p.N, 4);
     } else {
-        m.a[0] = p.pad_in ? c.at<u16>(p.c_in.o) : (const u16 *)p.in;
-        m.b[0] = p.pad_w ? c.at<u16>(p.c_w.o) : (const u16 *)p.w;
+        m.a = p.pad_in ? c.at<u16>(p.c_in.o) : (const u16 *)p.in;
+        m.b = p.pad_w ? c.at<u16>(p.c_w.o) : (const u16 *)p.w;
         m.lda = p.pad_in ? p.c_in.ld : p.ld_in;
         m.ldb = p.pad_w ? p.c_w.ld : p.ld_w;
         m.perm = p.pad_in ? nullptr : b.perm;   // copies are in the order of positions
@@ -751,10 +743,9 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     if (dw && !few) {
         w.M = (int)N;
         w.N = (int)K;
-        w.K = (int)op_round_up(M, 64);
+        w.K = (int)op_round_up(M, 64) * (f32 ? 2 : 1);
         w.batch = 1;
-        w.nseg = f32 ? 3 : 1;
-        w.f16 = f32;
+        w.pair = f32;
         w.epi = f32 ? EPI_SCALED : EPI_ROWS;
         mm_plan(w);
         c_dy = plan_copy(c, N, M, f32, true);
@@ -883,10 +874,6 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         if (gemel_status s = run_adapted(c, b, f32, p, c.at<float>(o_part))) return s;
     if (dw && !few) {
         operands(c, w, c_dy, c_x);
-        if (!f32) {
-            w.a[0] = c.at<u16>(c_dy.o);
-            w.b[0] = c.at<u16>(c_x.o);
-        }
         w.zero = (const u16 *)st->zero;
         w.partial = c.at<float>(o_part);
         w.o.out = dw;
@@ -949,8 +936,9 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     const int64_t each = 12 * np * mp + 20 * np * np;
     const int group = (int)std::max<int64_t>(1, std::min<int64_t>(all, (int64_t)(4ll << 30) / each));
     auto planes = [&](int64_t rows, int64_t ld, bool rest) {
-        Planes p{nullptr, nullptr, ld, rows * ld};
-        const size_t a = c.lay.take(group * rows * ld, 2), b = rest ? c.lay.take(group * rows * ld, 2) : 0;
+        if (lo) ld *= 2;   // pairs
+        Planes p{nullptr, nullptr, ld, rows * ld, lo};
+        const size_t a = c.lay.take(group * rows * ld, 2), b = rest && !lo ? c.lay.take(group * rows * ld, 2) : 0;
         p.hi = (u16 *)a;
         p.lo = (u16 *)b;
         return p;
@@ -965,10 +953,9 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     auto shape = [&](MmArgs &a, int M, int N, int64_t K, int epi, bool sym) {
         a.M = M;
         a.N = N;
-        a.K = (int)K;
+        a.K = (int)K * (lo ? 2 : 1);
         a.batch = group;
-        a.nseg = lo ? 3 : 1;
-        a.f16 = 1;
+        a.pair = lo;
         a.epi = epi;
         a.sym = sym;
         const double us = mm_plan(a);
@@ -994,7 +981,7 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     for (Planes *b : {&x, &t0, &t1, &s, &p, &t, &m0, &q}) {
         if (!b->ld) continue;
         b->hi = c.at<u16>((size_t)b->hi);
-        b->lo = b->lo ? c.at<u16>((size_t)b->lo) : nullptr;
+        b->lo = b->pair ? b->hi + PAIR_RUN : b->lo ? c.at<u16>((size_t)b->lo) : nullptr;
     }
     o.sums = c.at<double>(o_sums);
     o.lambda = c.at<float>(o_lambda);
@@ -1015,11 +1002,8 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         OPCHK(launch_seed(o, c.stream), "scaled update");
         // l * r of one batch, into a
         auto planes_of = [&](MmArgs &a, const Planes &l, const Planes &r) {
-            const u16 *al[3] = {l.hi, lo ? l.lo : nullptr, l.hi}, *bl[3] = {lo ? r.lo : r.hi, r.hi, r.hi};
-            for (int i = 0; i < 3; ++i) {
-                a.a[i] = al[i];
-                a.b[i] = bl[i];
-            }
+            a.a = l.hi;
+            a.b = r.hi;
             a.lda = l.ld;
             a.ldb = r.ld;
             a.za = l.z;
