@@ -739,21 +739,23 @@ hipError_t pairs_only(const MmArgs &a, hipStream_t s) {
 // Tile and depth splits, by the estimated time of the launch: the turns that
 // the compute units take, each a step's time for every step and a fixed part
 // for the pipeline's start and the epilogue; and, where the depth is split,
-// writing and reading the partial sums and the second launch. Measured steps
-// (microseconds, float16, workgroups on every compute unit): 64 x 64 tiles
-// 0.21 alone on a compute unit and 0.36 two at once, 128 x 128 0.62 and 0.95,
-// 256 x 256 1.65. A 512 x 512 result of depth 4608 takes 18.6 us unsplit and
-// 13.3 in 4 splits, a symmetric 4096 x 4096 one of depth 75264 1690 and 1210
-// us in 7 (its 136 tiles of 256 leave half of the 256 compute units idle).
+// writing and reading the partial sums and the second launch. The times are
+// a fit to 23 shapes from 128 x 128 x 8192 to 25088 x 4096 x 4096 at every
+// tile and up to 32 splits, within 9% of the measured ones; for each of these
+// shapes the tile and split chosen is the fastest one measured. What splits
+// are for: a symmetric 512 x 512 result of depth 4608 takes 16.3 us whole and
+// 10.2 in 4 splits, one of 4096 x 4096 and 25088 pairs 1322 and 1089 us in 7
+// (its 136 tiles of 256 leave half of the 256 compute units idle); 2048 x
+// 1000 of 1024 pairs is fastest whole (22.4 us).
 double mm_plan(MmArgs &a) {
     struct Form {
         int tile, slots;                        // workgroups that run at once
         double alone, full, fixed, fixed_part;  // microseconds; with partial sums out
     };
     static const Form single[] = {
-        {256, 256, 1.65, 1.65, 28.0, 12.0}, {128, 512, 0.62, 0.95, 9.0, 7.0}, {64, 512, 0.21, 0.36, 5.5, 5.0}};
+        {256, 256, 1.40, 1.40, 30.0, 6.5}, {128, 512, 0.48, 0.87, 12.3, 3.4}, {64, 512, 0.12, 0.36, 6.7, 2.5}};
     static const Form pair[] = {
-        {256, 256, 2.35, 2.35, 28.0, 12.0}, {128, 512, 0.75, 1.25, 9.0, 7.0}, {64, 512, 0.27, 0.47, 5.5, 5.0}};
+        {256, 256, 2.05, 2.05, 50.0, 7.0}, {128, 512, 0.56, 1.20, 12.5, 3.6}, {64, 512, 0.16, 0.44, 6.3, 2.0}};
     const Form *const forms = a.pair ? pair : single;
     const int steps = (a.K + BK - 1) / BK;
     double best = 1e30;
@@ -768,7 +770,7 @@ double mm_plan(MmArgs &a) {
             double us = (double)whole * (per * f.full + fixed);
             if (rest) us += per * (rest > 256 ? f.full : f.alone) + fixed;
             const double bytes = (double)splits * a.batch * a.M * op_round_up(a.N, 4) * (a.sym ? 2 : 4);
-            if (splits > 1) us += 5.0 + 2 * bytes / 5.5e6;
+            if (splits > 1) us += 4.8 + 0.13 * splits + 2 * bytes / 5.5e6;
             if (splits > 1 && bytes > 1e9) continue;
             if (us < best) {
                 best = us;

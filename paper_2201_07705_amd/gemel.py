@@ -536,10 +536,25 @@ class Context:
         rows, cols = t.shape
         return max(t.stride(0), cols) if rows > 1 else cols
 
-    def _stream(self, stream):
-        if stream is None:
-            stream = _torch().cuda.current_stream(self.device)
+    def _stream(self, stream, *tensors):
+        """The handle of the stream to work on. Where that is not the current
+        one the tensors are marked as used there, so that memory a caller
+        drops is not handed out again before the work is done."""
+        current = _torch().cuda.current_stream(self.device)
+        if stream is None or stream == current:
+            return current.cuda_stream
+        for t in tensors:
+            if t is not None:
+                t.record_stream(stream)
         return stream.cuda_stream
+
+    @staticmethod
+    def _empty(like, shape, dtype, stream):
+        """A result's tensor, from the memory of the stream that fills it."""
+        if stream is None:
+            return like.new_empty(shape, dtype=dtype)
+        with _torch().cuda.stream(stream):
+            return like.new_empty(shape, dtype=dtype)
 
     def _projection(self, batch, weight, a, b, bias):
         if batch._ctx is not self:
@@ -566,17 +581,21 @@ class Context:
         """y = x W^T + bias + scale * (x A^T) B^T, each row with its
         request's adapter: x [rows, n_in], weight [n_out, n_in], a
         [adapters, rank, n_in], b [adapters, n_out, rank] of the context's
-        type, bias float32. x, weight and out may have a row stride."""
+        type, bias float32. x, weight and out may have a row stride.
+
+        This and the operators below run on `stream` (None: the current
+        one), and make the tensors they return there."""
         p, n, k, dt = self._projection(batch, weight, a, b, bias)
         rows = batch.rows
         self._tensor("x", x, (rows, k), dt, contiguous=False)
         if out is None:
-            out = x.new_empty((rows, n))
+            out = self._empty(x, (rows, n), dt, stream)
         else:
             self._tensor("out", out, (rows, n), dt, contiguous=False)
         self._check(self._lib.gemel_adapt(
             self._h, batch.id, p, x.data_ptr(), self._stride(x),
-            out.data_ptr(), self._stride(out), self._stream(stream)))
+            out.data_ptr(), self._stride(out),
+            self._stream(stream, x, weight, a, b, bias, out)))
         return out
 
     def adapt_backward(self, batch, dy, x, weight, a=None, b=None,
@@ -603,7 +622,7 @@ class Context:
             want = dt if name == "x" else f32
             t = outputs.get(name) if outputs else None
             if t is None:
-                t = x.new_empty(shapes[name], dtype=want)
+                t = self._empty(x, shapes[name], want, stream)
             else:
                 self._tensor(f"outputs[{name!r}]", t, shapes[name], want,
                              contiguous=name != "x")
@@ -613,7 +632,7 @@ class Context:
             dy.data_ptr(), self._stride(dy), ptr.get("x"),
             self._stride(res["x"]) if "x" in res else 0, ptr.get("weight"),
             ptr.get("bias"), ptr.get("a"), ptr.get("b"),
-            self._stream(stream)))
+            self._stream(stream, x, dy, weight, a, b, *res.values())))
         return res
 
     @staticmethod
@@ -629,12 +648,12 @@ class Context:
         dt = self._torch_dtype()
         self._tensor("g", g, g.shape, dt)
         if out is None:
-            out = g.new_empty(g.shape)
+            out = self._empty(g, g.shape, dt, stream)
         else:
             self._tensor("out", out, g.shape, dt)
         self._check(self._lib.gemel_orthogonalize(
             self._h, count, rows, cols, g.data_ptr(), out.data_ptr(), steps,
-            self._stream(stream)))
+            self._stream(stream, g, out)))
         return out
 
     def muon_step(self, w, momentum_buffer, g, lr, momentum=0.95,
@@ -653,5 +672,6 @@ class Context:
             self._h, count, rows, cols, w.data_ptr(),
             momentum_buffer.data_ptr(), g.data_ptr(),
             None if copy is None else copy.data_ptr(), lr, momentum,
-            weight_decay, 1 if nesterov else 0, steps, self._stream(stream)))
+            weight_decay, 1 if nesterov else 0, steps,
+            self._stream(stream, w, momentum_buffer, g, copy)))
         return w

@@ -74,3 +74,33 @@ def test_muon_step(ctxs, rows, cols):  # noqa: F811
     assert ((m.to(f64) - m1).abs() <= 2.0 ** -22 * (1.95 * m1.abs() + g.abs())).all()
     assert (w.to(f64) - want).norm() <= rate * 2.0 ** -17 * o.norm() + 2.0 ** -22 * w0.norm()
     assert torch.equal(copy, w.bfloat16())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_operands_dropped_while_another_stream_works(ctxs, dtype):  # noqa: F811
+    """Operands that nobody holds after the call, and memory of the current
+    stream asked for and filled at once."""
+    import torch
+    ctx = ctxs[dtype]
+    s = problem(dtype, [300, 200], [1, 0], 2, 8, 1024, 512, 21)
+    b = batch_of(ctx, s)
+    want = ctx.adapt(b, s["x"], s["w"], s["a"], s["b"])
+    wide = ctx.adapt_backward(b, s["dy"], s["x"], s["w"], s["a"], s["b"])
+    o = ctx.orthogonalize(s["w"])
+    torch.cuda.synchronize()
+    st = torch.cuda.Stream()
+    outs = []
+    for _ in range(10):
+        copies = [s[q].clone() for q in ("x", "w", "a", "b", "dy")]
+        st.wait_stream(torch.cuda.current_stream())
+        outs.append((ctx.adapt(b, *copies[:4], stream=st),
+                     ctx.adapt_backward(b, copies[4], *copies[:4], stream=st),
+                     ctx.orthogonalize(copies[1], stream=st)))
+        shapes = [t.shape for t in copies]
+        del copies
+        for shape in shapes:
+            torch.full(shape, float("nan"), dtype=DT[dtype], device="cuda")
+    torch.cuda.synchronize()
+    for y, grads, q in outs:
+        assert torch.equal(y, want) and torch.equal(q, o)
+        assert all(torch.equal(grads[name], wide[name]) for name in wide)
