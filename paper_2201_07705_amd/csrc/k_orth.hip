@@ -221,33 +221,54 @@ __global__ __launch_bounds__(256) void thin_gram_kernel(const OrthArgs a) {
 
 // One workgroup per matrix: the products of symmetric polynomials of one
 // matrix commute and are symmetric, so tiles on and above the diagonal
-// suffice, and rows serve for columns.
+// suffice, and rows serve for columns. A wave for each of these tiles: what
+// takes time is the chain of some 20 products, and before it the latency of
+// reading the partial Gram matrices, which groups of 256 threads share.
 template <int NB>
-__global__ __launch_bounds__(256) void thin_poly_kernel(const OrthArgs a) {
-    constexpr int NP = 16 * NB, TILES = NB * (NB + 1) / 2, LD = NP + 2;
+constexpr int poly_threads() { return NB < 3 ? 256 : NB == 3 ? 512 : 1024; }
+template <int NB>
+__global__ __launch_bounds__(poly_threads<NB>()) void thin_poly_kernel(const OrthArgs a) {
+    constexpr int NP = 16 * NB, TILES = NB * (NB + 1) / 2, LD = NP + 2, NT = poly_threads<NB>(), GROUPS = NT / 256;
+    static_assert(GROUPS <= 4 && TILES * 256 <= NP * LD || GROUPS == 1, "a buffer for each group's sums");
     __shared__ double buf[4][NP * LD];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, g = lane >> 4, l16 = lane & 15;
     const int z = blockIdx.x;
     const double *part = a.gram + (int64_t)z * a.parts * NP * NP;
     double *s = buf[0], *p = buf[1], *q = buf[2], *t = buf[3];
-    for (int i = tid; i < NP * NP; i += 256) {
-        const int r = i / NP, c = i % NP;
-        if (r / 16 > c / 16) continue;
-        double v = 0.;
-        for (int k = 0; k < a.parts; ++k) v += part[(int64_t)k * NP * NP + i];
-        s[r * LD + c] = v;
-        if (r / 16 < c / 16) s[c * LD + r] = v;
-    }
+    const int group = tid >> 8, in = tid & 255;
+    // f(tile, element of S) over a thread's elements
+    auto elements = [&](auto &&f) __attribute__((always_inline)) {
+        int b = 0;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int j = i; j < NB; ++j, ++b) f(b, i * 16 + (in >> 4), j * 16 + (in & 15));
+    };
+    double v[TILES];
+    elements([&](int b, int r, int c) __attribute__((always_inline)) {
+        v[b] = 0.;
+#pragma unroll 8
+        for (int k = group; k < a.parts; k += GROUPS) v[b] += part[(int64_t)k * NP * NP + r * NP + c];
+        if (group) buf[group][b * 256 + in] = v[b];
+    });
+    __syncthreads();
+    if (group == 0)
+        elements([&](int b, int r, int c) __attribute__((always_inline)) {
+#pragma unroll
+            for (int k = 1; k < GROUPS; ++k) v[b] += buf[k][b * 256 + in];
+            s[r * LD + c] = v[b];
+            if (r / 16 < c / 16) s[c * LD + r] = v[b];
+        });
     __syncthreads();
     double trace = 0.;
     for (int i = 0; i < NP; ++i) trace += s[i * LD + i];
     __syncthreads();
     const double norm = sqrt(trace), inv = 1. / (norm + 1e-7);
-    for (int i = tid; i < NP * LD; i += 256) s[i] = s[i] * inv * inv;
+    for (int i = tid; i < NP * LD; i += NT) s[i] = s[i] * inv * inv;
     __syncthreads();
     // out(r, c, sum over k of x[r][k] y[c][k]) for both (r, c) and (c, r)
     auto product = [&](const double *x, const double *y, auto &&out) __attribute__((always_inline)) {
-        for (int b = wave; b < TILES; b += 4) {
+        for (int b = wave; b < TILES; b += NT / 64) {
             int i = 0, j = b;
             while (j >= NB - i) {
                 j -= NB - i;
@@ -286,7 +307,7 @@ __global__ __launch_bounds__(256) void thin_poly_kernel(const OrthArgs a) {
     }
     const int e = norm > 0. && isfinite(norm) ? -1 - ilogb(norm) : 0;
     const double scale = ldexp(inv, -e);
-    for (int i = tid; i < NP * NP; i += 256) a.q[(int64_t)z * NP * NP + i] = (float)(q[i / NP * LD + i % NP] * scale);
+    for (int i = tid; i < NP * NP; i += NT) a.q[(int64_t)z * NP * NP + i] = (float)(q[i / NP * LD + i % NP] * scale);
     if (tid == 0) a.e[z] = e;
 }
 
@@ -363,9 +384,9 @@ __global__ __launch_bounds__(256) void thin_apply_kernel(const OrthArgs a) {
     }
 }
 
-hipError_t launch(const void *fn, dim3 grid, const OrthArgs &a, hipStream_t s) {
+hipError_t launch(const void *fn, dim3 grid, const OrthArgs &a, hipStream_t s, int threads = 256) {
     void *p[] = {const_cast<OrthArgs *>(&a)};
-    return hipLaunchKernel(fn, grid, dim3(256), p, 0, s);
+    return hipLaunchKernel(fn, grid, dim3((unsigned)threads), p, 0, s);
 }
 bool valid(const OrthArgs &a) {
     return a.g && a.rows > 0 && a.cols > 0 && a.count > 0 && a.count <= 65535 && a.parts > 0 && a.steps >= 1 &&
@@ -415,7 +436,8 @@ hipError_t launch_thin_poly(const OrthArgs &a, hipStream_t s) {
     if (!valid_thin(a)) return hipErrorInvalidValue;
     return thin(a, [&](auto nb, bool) {
         constexpr int NB = decltype(nb)::value;
-        return launch(reinterpret_cast<const void *>(&thin_poly_kernel<NB>), dim3((unsigned)a.count), a, s);
+        return launch(reinterpret_cast<const void *>(&thin_poly_kernel<NB>), dim3((unsigned)a.count), a, s,
+                      poly_threads<NB>());
     });
 }
 
