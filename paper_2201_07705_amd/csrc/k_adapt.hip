@@ -166,9 +166,9 @@ __global__ __launch_bounds__(256) void shrink_sum_kernel(const Two<ShrinkArgs> a
     const ShrinkArgs &a = arg_of<ShrinkArgs>(blockIdx.y);
     const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, n = (int64_t)a.b.rows * a.rp;
     const int p = (int)(i / a.rp), q = (int)(i - (int64_t)p * a.rp);
-    if (a.slices < 2 || i >= n || p < a.b.run_start[0]) return;
-    int u = a.b.first_run[p >> 6];
-    while (a.b.run_start[u + 1] <= p) ++u;
+    if (a.slices < 2 || i >= n) return;
+    const int u = a.b.run_at[p];
+    if (u < 0) return;
     float t = 0.f;
 #pragma unroll 8
     for (int k = 0; k < a.slices; ++k) t += a.part[k * n + i];
@@ -317,7 +317,7 @@ __global__ __launch_bounds__(256) void outer_kernel(const Outers args) {
 
 bool tables(const BatchTables &b) {
     return b.perm && b.run_start && b.run_id && b.run_rank && b.run_scale && b.first_run && b.items && b.chunks &&
-           b.chunk_first && b.run_of && b.rows > 0 && b.runs > 0 && b.adapters > 0 && b.rank > 0;
+           b.chunk_first && b.run_of && b.run_at && b.rows > 0 && b.runs > 0 && b.adapters > 0 && b.rank > 0;
 }
 template <typename A>
 hipError_t launch(const void *fn, dim3 grid, int block, const A *a, int n, hipStream_t s) {

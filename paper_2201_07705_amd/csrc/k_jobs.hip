@@ -94,24 +94,46 @@ __device__ __forceinline__ void pad(const Job &j, int block) {
     }
 }
 
-// a wave per row
-__device__ __forceinline__ void split(const Job &j, int block) {
-    const int r = block * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+// f(column, 4 values) over a row's columns up to `end` (zeros from the last
+// on), from c on in steps; four loads in flight, no branch between them
+template <typename F>
+__device__ __forceinline__ void along(const float *in, int cols, int end, int c, int step, F &&f) {
+    for (; c + 3 * step + 4 <= cols; c += 4 * step) {
+        f32x4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = get_f32x4<f32x4>(in + c + k * step);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) f(c + k * step, v[k]);
+    }
+    for (; c < end; c += step) f(c, load4(in + c, cols - c));
+}
+
+// A workgroup per row (137 rows of 23605: 47 -> 12 us against a wave each), or
+// a wave for rows of up to SPLIT_WIDE.
+constexpr int SPLIT_WIDE = 1024;
+__device__ __forceinline__ void split(const Job &j, int block, unsigned char *lds) {
+    const bool wide = j.cols > SPLIT_WIDE;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = wide ? block : block * 4 + wave;
     if (r >= j.rows) return;
     const float *in = (const float *)j.in + (int64_t)(j.perm ? j.perm[r] : r) * j.ldi;
+    const int first = (wide ? (int)threadIdx.x : lane) * 4, step = wide ? 1024 : 256;
     unsigned m = 0;
-#pragma unroll 4
-    for (int c = lane * 4; c < j.cols; c += 256) {
-        const f32x4 v = load4(in + c, j.cols - c);
+    along(in, j.cols, j.cols, first, step, [&](int, f32x4 v) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) m = max(m, magnitude(v[i]));
-    }
+    });
     for (int o = 32; o; o >>= 1) m = max(m, (unsigned)__shfl_xor((int)m, o));
+    if (wide) {
+        unsigned *const part = (unsigned *)lds;
+        if (lane == 0) part[wave] = m;
+        __syncthreads();
+        m = max(max(part[0], part[1]), max(part[2], part[3]));
+    }
     const int e = plane_exp(m);
-    if (lane == 0) j.e[r] = e;
+    if (first == 0) j.e[r] = e;
     u16 *out = (u16 *)j.out + r * j.ldo;
-#pragma unroll 4
-    for (int c = lane * 4; c < j.ldo / 2; c += 256) split_put(out, c, load4(in + c, j.cols - c), e);
+    along(in, j.cols, (int)(j.ldo / 2), first, step,
+          [&](int c, f32x4 v) __attribute__((always_inline)) { split_put(out, c, v, e); });
 }
 
 // 64 x 64 tiles through LDS, which holds the tile transposed. E: u16 (copied)
@@ -124,21 +146,34 @@ __device__ __forceinline__ void turn(const Job &j, int block, unsigned char *lds
     float *const part = (float *)(lds + 64 * PITCH * sizeof(E) + 8);   // [4][64]
     const int tid = threadIdx.x, across = (j.cols + 63) / 64;
     const int r0 = block / across * 64, c0 = block % across * 64;
-    for (int i = tid; i < 64 * 64 / Q; i += 256) {
-        const int r = i / (64 / Q), c = i % (64 / Q) * Q;
-        union {
-            uint4 v;
-            E e[Q];
-        } x;
-        const E *in = (const E *)j.in + (int64_t)(r0 + r) * j.ldi + c0 + c;
-        if (r0 + r < j.rows && c0 + c + Q <= j.cols) {
-            x.v = get_16b(in);
-        } else {
+    union Chunk {
+        uint4 v;
+        E e[Q];
+    };
+    constexpr int N = 64 * 64 / Q / 256;   // chunks of a thread
+    Chunk x[N];
+    const bool whole = r0 + 64 <= j.rows && c0 + 64 <= j.cols;
+    if (whole) {
+        // (no branch between the loads)
 #pragma unroll
-            for (int k = 0; k < Q; ++k) x.e[k] = r0 + r < j.rows && c0 + c + k < j.cols ? in[k] : (E)0;
+        for (int i = 0; i < N; ++i) {
+            const int k = i * 256 + tid;
+            x[i].v = get_16b((const E *)j.in + (int64_t)(r0 + k / (64 / Q)) * j.ldi + c0 + k % (64 / Q) * Q);
         }
+    } else {
 #pragma unroll
-        for (int k = 0; k < Q; ++k) tile[(c + k) * PITCH + r] = x.e[k];
+        for (int i = 0; i < N; ++i) {
+            const int r = (i * 256 + tid) / (64 / Q), c = (i * 256 + tid) % (64 / Q) * Q;
+            const E *in = (const E *)j.in + (int64_t)(r0 + r) * j.ldi + c0 + c;
+#pragma unroll
+            for (int k = 0; k < Q; ++k) x[i].e[k] = r0 + r < j.rows && c0 + c + k < j.cols ? in[k] : (E)0;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const int r = (i * 256 + tid) / (64 / Q), c = (i * 256 + tid) % (64 / Q) * Q;
+#pragma unroll
+        for (int k = 0; k < Q; ++k) tile[(c + k) * PITCH + r] = x[i].e[k];
     }
     int *const es = (int *)(part + 256);
     if (F && tid < 64 && c0 + tid < j.cols) {
@@ -178,16 +213,33 @@ __device__ __forceinline__ void columns(const Job &j, int block, unsigned char *
     const int g = threadIdx.x >> 4, left = j.cols - c;
     const int r0 = (int)((int64_t)j.rows * p / j.parts), r1 = (int)((int64_t)j.rows * (p + 1) / j.parts);
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int r = r0 + g; r < r1; r += 16) {
-        f32x4 x = {0.f, 0.f, 0.f, 0.f};
-        if (left > 0) {
-            x = j.f32 ? load4((const float *)j.in + r * j.ldi + c, left) : up4((const u16 *)j.in + r * j.ldi + c, left);
-        }
+    auto add = [&](f32x4 x) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
             v[i] = MAX ? __uint_as_float(max(__float_as_uint(v[i]), magnitude(x[i]))) : v[i] + x[i];
+    };
+    const int in = left >= 4 ? 4 : left;
+    int r = r0 + g;
+    // (eight loads in flight, no branch between them)
+    if (in == 4 && j.f32) {
+        for (; r + 112 < r1; r += 128) {
+            f32x4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = get_f32x4<f32x4>((const float *)j.in + (r + 16 * k) * j.ldi + c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) add(x[k]);
+        }
+    } else if (in == 4) {
+        for (; r + 112 < r1; r += 128) {
+            ushort4 x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[k] = get_u16x4((const u16 *)j.in + (r + 16 * k) * j.ldi + c);
+#pragma unroll
+            for (int k = 0; k < 8; ++k) add(f32x4{bf_up(x[k].x), bf_up(x[k].y), bf_up(x[k].z), bf_up(x[k].w)});
+        }
     }
+    for (; r < r1 && in > 0; r += 16)
+        add(j.f32 ? load4((const float *)j.in + r * j.ldi + c, in) : up4((const u16 *)j.in + r * j.ldi + c, in));
     part[g * 16 + (threadIdx.x & 15)] = v;
     __syncthreads();
     if (g) return;
@@ -327,7 +379,7 @@ __global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
             else
                 pad<u16>(j, block);
             break;
-        case JOB_SPLIT: split(j, block); break;
+        case JOB_SPLIT: split(j, block, lds); break;
         case JOB_TURN:
             if (j.f32)
                 turn<float>(j, block, lds);
@@ -359,7 +411,7 @@ bool add_job(Jobs &all, const Job &in) {
             break;
         case JOB_SPLIT:
             ok = ok && j.in && j.out && j.e && j.rows > 0 && j.ldo / 2 >= j.cols && j.ldo % (4 * PAIR_RUN) == 0;
-            blocks = ((int64_t)j.rows + 3) / 4;
+            blocks = j.cols > SPLIT_WIDE ? j.rows : ((int64_t)j.rows + 3) / 4;
             break;
         case JOB_TURN:
             ok = ok && j.in && j.out && j.rows > 0 && j.ldo / (j.f32 ? 2 : 1) >= j.rows && j.ldo % (j.f32 ? 4 * PAIR_RUN : 4) == 0 &&

@@ -163,7 +163,9 @@ struct Near {
     f32x4 hi, lo;   // a matrix in planes (MIX: lo is the second matrix)
     f32x4 w;        // a diagonal, the weights, or the bias
     float d;        // POLY: the diagonal at m
-    int row, e;     // ROWS, SCALED: output row; SCALED: its exponent
+    int row;        // ROWS, SCALED: output row
+    int e, u;       // SCALED: its exponent, and its run or -1
+    int eb[4];      // SCALED: exponents of the columns
 };
 template <int EPI>
 __device__ __forceinline__ Near gather(const MmArgs &a, const Tile &t, int m, int n) {
@@ -172,11 +174,25 @@ __device__ __forceinline__ Near gather(const MmArgs &a, const Tile &t, int m, in
     if constexpr (EPI == EPI_ROWS || EPI == EPI_SCALED) {
         const int mc = min(t.m0 + m, a.M - 1);
         r.row = o.perm ? o.perm[mc] : mc;
-        if constexpr (EPI == EPI_SCALED) r.e = o.ea[mc];
         r.w = f32x4{0.f, 0.f, 0.f, 0.f};
-        if (o.bias)
+        if constexpr (EPI == EPI_SCALED) {
+            r.e = o.ea[mc];
+            r.u = a.runs > 0 ? o.run_at[mc] : -1;
+            if (t.inside) {
+                const uint4 x = get_16b(o.eb + t.n0 + n);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.eb[i] = (int)(&x.x)[i];
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) r.eb[i] = o.eb[min(t.n0 + n + i, a.N - 1)];
+            }
+        }
+        if (o.bias && t.inside) {
+            r.w = get_f32x4<f32x4>(o.bias + t.n0 + n);
+        } else if (o.bias) {
 #pragma unroll
             for (int i = 0; i < 4; ++i) r.w[i] = o.bias[min(t.n0 + n + i, a.N - 1)];
+        }
     } else if constexpr (EPI == EPI_POLY) {
         at4(o.s, t, m, n, a.M, r.hi, r.lo);
         if (o.sdiag) {
@@ -213,6 +229,39 @@ __device__ __forceinline__ Near gather(const MmArgs &a, const Tile &t, int m, in
     return r;
 }
 
+// SCALED: the low-rank part of G pieces (m, n .. n + 3), added to what
+// finish adds. No branch stands between the loads: rows without a run read
+// the first one's and drop it.
+template <int G>
+__device__ __forceinline__ void low_rank(const MmArgs &a, const Tile &t, const int (&m)[G], const int (&n)[G], Near (&near)[G]) {
+    const MmOut &o = a.o;
+    if (a.runs <= 0) return;
+    f32x4 sum[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) sum[g] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+    for (int r = 0; r < o.rank; r += 4) {   // (zeros from a run's rank on)
+        f32x4 x[G], b[G][4];
+#pragma unroll
+        for (int g = 0; g < G; ++g) {
+            x[g] = *(const f32x4 *)(o.t + (int64_t)min(t.m0 + m[g], a.M - 1) * o.rp + r);
+            const float *bx = o.bx + ((int64_t)max(near[g].u, 0) * o.rp + r) * o.ldbx + min((int64_t)t.n0 + n[g], o.ldbx - 4);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) b[g][i] = *(const f32x4 *)(bx + i * o.ldbx);
+        }
+#pragma unroll
+        for (int g = 0; g < G; ++g)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) sum[g] += x[g][i] * b[g][i];
+    }
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const f32x4 w = near[g].w + sum[g];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) near[g].w[i] = near[g].u < 0 ? near[g].w[i] : w[i];
+    }
+}
+
 // The epilogue of elements (m, n .. n + 3) of the tile. M and N are the
 // product's; planes are written up to their padded row lengths, with zeros
 // beyond M and N, because later products read them in steps of 64. Returns
@@ -235,23 +284,9 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
         const int64_t at = (int64_t)in.row * o.ld + t.n0 + n;
         if constexpr (EPI == EPI_SCALED) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -(in.e + o.eb[min(t.n0 + n + i, a.N - 1)]));
+            for (int i = 0; i < 4; ++i) v[i] = ldexpf(v[i], -(in.e + in.eb[i]));
         }
         v += in.w;
-        if constexpr (EPI == EPI_SCALED) {
-            const int p = t.m0 + m;
-            if (a.runs > 0 && p >= a.run_start[0]) {
-                int u = a.first_run[p >> 6];
-                while (a.run_start[u + 1] <= p) ++u;
-                const float *x = o.t + (int64_t)p * o.rp, *bx = o.bx + (int64_t)u * o.rp * o.ldbx + t.n0 + n;
-                // (zeros from the run's rank on, up to a multiple of 32)
-                for (int r = 0; r < o.run_rank[u]; r += 4) {
-                    const f32x4 x4 = *(const f32x4 *)(x + r);
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) v += x4[i] * *(const f32x4 *)(bx + (r + i) * o.ldbx);
-                }
-            }
-        }
         if (o.out_f32) {
             float *p = (float *)o.out + at;
             if (left > 3) {
@@ -614,7 +649,7 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
         const bool turned = (EPI == EPI_NEXT || ((EPI == EPI_GRAM || EPI == EPI_POLY || EPI == EPI_MIX) && e.sym && tn > tm)) &&
                             e.splits == 1;
         const Tile tile{z, mb, nb, mb + RP <= e.M && nb + TN <= e.N};
-        constexpr int ITEMS = RP * C / 64, GROUP = T == 256 ? (EPI == EPI_ROWS ? 1 : 2) : 4;   // (registers)
+        constexpr int ITEMS = RP * C / 64, GROUP = T == 256 ? (EPI == EPI_ROWS ? 1 : 2) : T == 128 && EPI == EPI_SCALED ? 2 : 4;   // (registers)
         static_assert(ITEMS % GROUP == 0, "whole groups");
 #pragma unroll 1
         for (int i0 = 0; i0 < ITEMS; i0 += GROUP) {
@@ -626,6 +661,16 @@ __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2)
                 v[i] = *(const f32x4 *)(mine + m * TN * 4 + (c ^ swz(m)) * 16);
                 if (e.splits == 1) near[i] = gather<EPI>(e, tile, m, c * 4);
             }
+            if constexpr (EPI == EPI_SCALED)
+                if (e.splits == 1) {
+                    int ms[GROUP], ns[GROUP];
+#pragma unroll
+                    for (int i = 0; i < GROUP; ++i) {
+                        ms[i] = ((i0 + i) * 64 + lane) / C;
+                        ns[i] = (lane & (C - 1)) * 4;
+                    }
+                    low_rank<GROUP>(e, tile, ms, ns, near);
+                }
 #pragma unroll
             for (int i = 0; i < GROUP; ++i) {
                 const int it = (i0 + i) * 64 + lane, m = it / C, c = it & (C - 1);
@@ -672,7 +717,11 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
     const bool turned = EPI == EPI_NEXT || (PLANES && a.sym && tn > tm);
     const int m = threadIdx.x >> 3, n = (threadIdx.x & 7) * 4;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    const Near near = gather<EPI>(a, tile, m, n);
+    Near near[1] = {gather<EPI>(a, tile, m, n)};
+    if constexpr (EPI == EPI_SCALED) {
+        const int ms[1] = {m}, ns[1] = {n};
+        low_rank<1>(a, tile, ms, ns, near);
+    }
     if (m0 + m < a.M && n0 + n < a.N) {
         const float *p = a.partial + ((int64_t)z * a.M + m0 + m) * a.ldp + n0 + n;
         const int64_t step = (int64_t)a.batch * a.M * a.ldp;
@@ -686,7 +735,7 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
         }
         for (; s < a.splits; ++s) v += *(const f32x4 *)(p + s * step);
     }
-    const uint4 q = finish<EPI>(a, tile, m, n, v, near);
+    const uint4 q = finish<EPI>(a, tile, m, n, v, near[0]);
     if constexpr (PLANES) {
         if (!turned) return;
 #pragma unroll
@@ -796,6 +845,10 @@ hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
     if (a.ext && (!a.t || !a.bx || a.runs < 1 || !a.run_start || !a.first_run || a.batch != 1))
         return hipErrorInvalidValue;
     if (a.sym && a.M != a.N) return hipErrorInvalidValue;
+    if (a.epi == EPI_SCALED && (!a.o.ea || !a.o.eb ||
+                                (a.runs > 0 && (!a.o.t || !a.o.bx || !a.o.run_at || a.o.rank % 4 || a.o.rank > a.o.rp ||
+                                                a.o.ldbx % 4 || a.o.ldbx < a.N))))
+        return hipErrorInvalidValue;
     if (a.epi != EPI_ROWS && (a.K % BK || a.ext)) return hipErrorInvalidValue;
     if ((int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64) > INT32_MAX / 256) return hipErrorInvalidValue;
     switch (a.epi) {

@@ -47,11 +47,12 @@ struct MmOut {
     const float *bias;    // [N] or null
     const int *perm;      // output row of product row m, or null
     const int *ea, *eb;   // SCALED
-    // SCALED: low-rank part, sum over r of t[m][r] * bx[run][r][n], rows of
-    // ldbx (a multiple of 4)
+    // SCALED: low-rank part, sum over r < rank of t[m][r] * bx[run][r][n]
+    // where the row has a run (run_at[m] >= 0); rank a multiple of 4, rows of
+    // bx ldbx apart, a multiple of 4
     const float *t, *bx;
-    const int *run_rank;
-    int rp;
+    const int *run_at;
+    int rp, rank;
     int64_t ldbx;
     Planes p, q;          // GRAM, POLY, MIX: p; NEXT: p = [m][n], q = [n][m]
     Planes s, s2;         // POLY, MIX: S; NEXT, ORTH, STEP: X as the product's rows lie
@@ -114,6 +115,7 @@ struct BatchTables {
     const int *chunks;     // [n_chunks][3]: run, first position, positions
     const int *chunk_first;// [runs + 1] chunks of a run
     const int *run_of;     // [adapters] run or -1
+    const int *run_at;     // [rows] run of position p or -1
     const int4 *row_info;  // [rows], batches of up to ROWS_MAX rows: position, run or -1, adapter, rank
     int rows, runs, adapters, rank, n_items, n_chunks;
 };

@@ -254,7 +254,10 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
         for (int p = 0; p < n; p += per_chunk)
             for (int v : {u, p0 + p, std::min(per_chunk, n - p)}) chunks.push_back(v);
     }
+    std::vector<int> run_at((size_t)rows, -1);
     run_start.push_back((int)rows);
+    for (size_t u = 0; u < run_id.size(); ++u)
+        std::fill(run_at.begin() + run_start[u], run_at.begin() + run_start[u + 1], (int)u);
     chunk_first.push_back((int)chunks.size() / 3);
     const int runs = (int)run_id.size();
     std::vector<int> first_run;
@@ -281,7 +284,7 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
                  o_scale = add(run_scale.data(), run_scale.size()), o_first = add(first_run.data(), first_run.size()),
                  o_items = add(items.data(), items.size()), o_chunks = add(chunks.data(), chunks.size()),
                  o_cf = add(chunk_first.data(), chunk_first.size()), o_of = add(run_of.data(), run_of.size()),
-                 o_info = add(info.data(), info.size());
+                 o_info = add(info.data(), info.size()), o_at = add(run_at.data(), run_at.size());
     DeviceScope scope(ctx->device);
     State *st = nullptr;
     if (gemel_status s = ready(ctx, &st)) return s;
@@ -303,6 +306,7 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
     t.chunks = d + o_chunks;
     t.chunk_first = d + o_cf;
     t.run_of = d + o_of;
+    t.run_at = d + o_at;
     t.row_info = (const int4 *)(d + o_info);
     t.rows = (int)rows;
     t.runs = runs;
@@ -484,8 +488,9 @@ gemel_status run_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, fl
         operands(c, m, p.c_in, p.c_w);
         m.o.t = p.t;
         m.o.bx = c.at<float>(p.o_bank);
-        m.o.run_rank = b.run_rank;
+        m.o.run_at = b.run_at;
         m.o.rp = rp;
+        m.o.rank = (int)op_round_up(b.rank, 4);
         m.o.ldbx = op_round_up(p.N, 4);
     } else {
         m.a = p.pad_in ? c.at<u16>(p.c_in.o) : (const u16 *)p.in;
