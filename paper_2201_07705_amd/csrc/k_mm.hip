@@ -383,9 +383,15 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
 // step (128) in hand; small ones take a whole one and four buffers, which is
 // what latency wants.
 //
-// What bounds it: the matrix cores at T = 256 (25088 x 4096 x 12288, float16:
-// 1262 TFLOP/s), the CU's 64 bytes a cycle from the L2 at T = 64 (half the
-// peak). 4096 x 4096 x 4096: T = 128 1243, T = 256 1190, T = 64 715 TFLOP/s.
+// Pairs: 32 columns of hi and of lo are a step, so that its three products
+// take four tiles through LDS where three plain steps of the same depth would
+// take six (2048 x 1000 of 1024 pairs 27.6 -> 22.4 us).
+//
+// What bounds it: the matrix cores at T = 256 and 128 (25088 x 4096 of 4096
+// pairs, with the update of X in both layouts: 2128 and 2113 us, 1195
+// TFLOP/s of float16 products), the CU's 64 bytes a cycle from the L2 at T =
+// 64 (2746 us). Below 512 tiles of 64 what a compute unit does alone counts:
+// 2048 x 1000 of 1024 pairs 22.4 us at T = 64, 33.2 at 128, 95.5 at 256.
 template <int T>
 constexpr int mm_threads() { return T == 64 ? 256 : 512; }
 

@@ -9,6 +9,11 @@
 // second adds the slices in order, multiplies the thin sums with the rows of
 // B that each output needs, and adds the bias. All sums are float32; float32
 // operands stay float32.
+//
+// 4096 -> 4096, every row its own adapter of rank 16, bf16: one row 11 us, 64
+// rows 16 us (3.4 TB/s of weights and adapters), of which two launches are 9;
+// as tiles of 64 rows, copies and thin products in launches of their own 28
+// and 97 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

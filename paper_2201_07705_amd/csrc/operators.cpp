@@ -19,6 +19,7 @@ using namespace gemel;
 namespace {
 
 constexpr int64_t MAX_ROWS = 1 << 22, MAX_DIM = 1 << 20, MAX_COUNT = 65535;
+constexpr int64_t NARROW = 64;   // outputs whose dW is summed without copies of x
 constexpr int MAX_RANK = 256, MAX_STEPS = ORTH_MAX_STEPS;
 
 struct DeviceScope {
@@ -648,6 +649,14 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     return run_adapted(c, b, f32, p, c.at<float>(o_part));
 }
 
+// Cuts a product over many positions into stretches: about three workgroups
+// on each compute unit, `groups` of them for each stretch.
+void stretches(OuterArgs &o, int64_t groups) {
+    const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(768 + groups - 1) / groups, (o.positions + 63) / 64, 64}));
+    o.per = (int)op_round_up((o.positions + want - 1) / want, 32);
+    o.n_chunks = (o.positions + o.per - 1) / o.per;
+}
+
 gemel_status zero_out(Call &c, float *p, int64_t n) {
     gemel_ctx *ctx = c.ctx;
     for (int64_t at = 0; p && at < n; at += 1 << 30)
@@ -695,8 +704,16 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     const int64_t Np = op_round_up(N, 64);
     const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
     // few rows: W is read as it lies for dx, and dW written as the product
-    // of a few columns of dy and rows of x, without copies of either
+    // of a few columns of dy and rows of x, without copies of either (bf16
+    // 4096 -> 4096, an adapter for each row: 1 row 90 -> 79 us, 64 rows 273 ->
+    // 151; float32 132 -> 80 and 250 -> 175)
     const bool few = M <= ROWS_MAX;
+    // few float32 outputs: dW in stretches of rows that read x as it lies,
+    // where the transposed pairs of x and the maxima for them would cost more
+    // than the product (16384 x 4096, 10 outputs 298 -> 64 us, 64 303 -> 114;
+    // 4096 x 512, 64 29 -> 18; at 100 outputs 512 x 4096 takes 26, not 23).
+    // bf16 copies are cheap, and the tiles faster: 64 outputs 87 us, not 113
+    const bool narrow = dw && !few && f32 && N <= NARROW, tiled = dw && !few && !narrow;
     // U = scale dy B and T = scale x A^T
     ShrinkArgs thin[2];
     const int n_thin = need_u + need_t;
@@ -722,11 +739,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         o.ld = op_round_up(K, 4);
         o.chunk = M * o.ld;
         o.positions = (int)N;
-        // stretches of W's rows: about three workgroups on each compute unit
-        const int64_t across = (K + (f32 ? 127 : 255)) / (f32 ? 128 : 256) * ((M + 31) / 32);
-        const int64_t want = std::max<int64_t>(1, std::min<int64_t>({(768 + across - 1) / across, (N + 63) / 64, 64}));
-        o.per = (int)op_round_up((N + want - 1) / want, 32);
-        o.n_chunks = (int)((N + o.per - 1) / o.per);
+        stretches(o, (K + (f32 ? 127 : 255)) / (f32 ? 128 : 256) * ((M + 31) / 32));
         part = o.n_chunks * o.chunk;
     } else if (dx) {
         p.in = dy;
@@ -745,7 +758,25 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // dW = dy^T x, on transposed copies of both
     MmArgs w{};
     Copy c_dy, c_x;
-    if (dw && !few) {
+    OuterArgs rows_dw{};
+    size_t o_dw = 0;   // (beside the other sums: one launch writes them all)
+    if (narrow) {
+        OuterArgs &o = rows_dw;
+        o.p = dy;
+        o.sp = lddy;
+        o.sr = 1;
+        o.q = x;
+        o.ldq = ldx;
+        o.p_f32 = o.q_f32 = f32;
+        o.R = (int)N;
+        o.C = (int)K;
+        o.ld = K;
+        o.chunk = N * K;
+        o.positions = (int)M;
+        stretches(o, (K + (f32 ? 127 : 255)) / (f32 ? 128 : 256) * ((N + 31) / 32));
+        if (o.n_chunks > 1) o_dw = c.lay.take(o.n_chunks * o.chunk, 4);
+    }
+    if (tiled) {
         w.M = (int)N;
         w.N = (int)K;
         w.K = (int)op_round_up(M, 64) * (f32 ? 2 : 1);
@@ -758,7 +789,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         part = std::max(part, partial_floats(w));
     }
     // column sums of dy: of 64 rows each where dy is transposed anyway
-    const int sums = (int)(dw ? (M + 63) / 64 : std::min<int64_t>(128, (M + 63) / 64));
+    const int sums = (int)(tiled ? (M + 63) / 64 : std::min<int64_t>(128, (M + 63) / 64));
     const size_t o_sum = c.lay.take(dbias && !few ? sums * N : 0, 4);
     const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * rp * K : 0, 4),
                  o_db = c.lay.take(db ? (int64_t)b.n_chunks * rp * N : 0, 4), o_part = c.lay.take(part, 4);
@@ -788,7 +819,19 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         rows_dx.out = c.at<float>(o_part);
         ok = ok && add_outer(outers, rows_dx);
     }
-    if (dw && !few) {
+    if (narrow) {
+        const bool joined = rows_dw.n_chunks > 1;
+        rows_dw.out = joined ? c.at<float>(o_dw) : dw;
+        ok = ok && add_outer(outers, rows_dw);
+        if (joined) {
+            Job j = job(JOB_COLADD, nullptr, 0, 0, (int)(N * K), true);
+            j.sum = rows_dw.out;
+            j.parts = rows_dw.n_chunks;
+            j.out = dw;
+            ok = ok && add_job(last, j);
+        }
+    }
+    if (tiled) {
         ok = ok && add_copy(c, c_dy, dy, lddy, (int)N, (int)M, f32, true, nullptr, sum, first, second);
         ok = ok && add_copy(c, c_x, x, ldx, (int)K, (int)M, f32, true, nullptr, nullptr, first, second);
     } else if (dbias) {
@@ -877,7 +920,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     if (n_thin) OPCHK(launch_shrink(thin, n_thin, stream), "thin products");
     if (dx && !few)
         if (gemel_status s = run_adapted(c, b, f32, p, c.at<float>(o_part))) return s;
-    if (dw && !few) {
+    if (tiled) {
         operands(c, w, c_dy, c_x);
         w.zero = (const u16 *)st->zero;
         w.partial = c.at<float>(o_part);
@@ -921,8 +964,8 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
 // which pairs can afford (2^-22 of S, spread over a whole row) and longer
 // chains could not (485 times after five).
 //
-// bf16 updates take one float16 product where float32 ones take three (hi hi,
-// hi lo, lo hi). What rounding would cost them is in a X: noise of 2^-12 of
+// bf16 updates take one float16 product of planes where float32 ones take
+// three of pairs (hi hi, hi lo, lo hi). What rounding would cost them is in a X: noise of 2^-12 of
 // X's large directions, spread over all small ones, would grow with these up
 // to 485 times. So X keeps its rest (lo) for that term, while M, S and X in M
 // X, whose rounding lands in the directions that are large already or is

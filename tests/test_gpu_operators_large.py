@@ -21,6 +21,8 @@ SHAPES = [
     ([4200], [0], 1, 48, 4104, 136),
     ([520, 1], [0, 1], 2, 16, 1, 3000),
     ([60], [0], 1, 7, 4999, 3),
+    ([3000, 71], [1, -1], 2, 8, 301, 41),           # few outputs, joined
+    ([65], [0], 1, 8, 130, 64),                     # few outputs, one stretch
 ]
 
 
