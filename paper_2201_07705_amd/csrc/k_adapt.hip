@@ -194,8 +194,13 @@ __device__ __forceinline__ void outer(const OuterArgs &a, int block, unsigned ch
     const int across = (a.C + COLS - 1) / COLS, down = (a.R + 31) / 32;
     const int bx = block % across, by = block / across % down, bz = block / (across * down);
     const int c0 = bx * COLS, r0 = by * 32;
-    const int p0 = a.chunks ? a.chunks[3 * bz + 1] : bz * a.per;
-    const int n = a.chunks ? a.chunks[3 * bz + 2] : min(a.per, a.positions - p0);
+    int p0 = bz * a.per, n = min(a.per, a.positions - p0);
+    if (a.chunks) {
+        const int ch = bz / a.sub, piece = bz - ch * a.sub;
+        const int all = a.chunks[3 * ch + 2], each = ((all + a.sub - 1) / a.sub + 31) / 32 * 32;
+        p0 = a.chunks[3 * ch + 1] + piece * each;
+        n = min(each, all - piece * each);
+    }
     constexpr int Q = 16 / E, LR = COLS / Q, NQ = 32 * LR / 256, NP = 32 * RB * 16 / 256;
     uint4 q[NQ];
     float p[NP];
@@ -367,6 +372,7 @@ hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
 bool add_outer(Outers &o, const OuterArgs &a) {
     if (o.n >= MAX_OUTER || !a.p || !a.q || !a.out || a.R < 1 || a.C < 1 || a.n_chunks < 1 || (a.sp != 1 && a.sr != 1) ||
         a.ld < a.C || (a.q_f32 && !a.p_f32) || (o.n && a.q_f32 != o.a[0].q_f32) ||
+        (a.chunks && (a.sub < 1 || a.n_chunks % a.sub)) ||
         (!a.chunks && (a.per < 1 || a.positions < 1 || (int64_t)a.n_chunks * a.per < a.positions ||
                        (int64_t)(a.n_chunks - 1) * a.per >= a.positions)))
         return false;

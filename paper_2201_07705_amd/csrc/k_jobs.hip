@@ -4,6 +4,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "op_args.h"
 #include "op_moves.h"
@@ -273,27 +274,53 @@ __device__ __forceinline__ void coladd(const Job &j, int block, unsigned char *l
         ((float *)j.out)[c] = part[threadIdx.x] + part[64 + threadIdx.x] + part[128 + threadIdx.x] + part[192 + threadIdx.x];
 }
 
-// 64 columns of a run per block
-__device__ __forceinline__ void pack(const Job &j, int block) {
-    const int across = ((int)(j.by_rank ? j.ldo : j.cols) + 63) / 64, u = block / across, c0 = block % across * 64;
-    const int rank = j.run_rank[u];
-    const int64_t in = (int64_t)j.run_id[u] * j.cols * j.R;
-    for (int i = threadIdx.x; i < 64 * j.rp; i += 256) {
-        // neighbours along the input's rows
-        const int r = j.in_rc ? i >> 6 : i % j.rp, c = c0 + (j.in_rc ? i & 63 : i / j.rp);
-        const bool there = r < rank && c < j.cols;
-        const int64_t at = in + (j.in_rc ? (int64_t)r * j.cols + c : (int64_t)c * j.R + r);
-        if (j.by_rank) {
-            if (c >= j.ldo) continue;
-            const int64_t to = ((int64_t)u * j.rp + r) * j.ldo + c;
-            if (j.f32)
-                ((float *)j.out)[to] = there ? ((const float *)j.in)[at] : 0.f;
-            else
-                ((u16 *)j.out)[to] = there ? ((const u16 *)j.in)[at] : (u16)0;
-        } else if (c < j.cols) {
-            u16 *out = (u16 *)j.out + ((int64_t)u * j.cols + c) * 2 * j.rp + r;
-            out[0] = out[j.rp] = there ? ((const u16 *)j.in)[at] : (u16)0;
+// 64 columns of a run per block, 32 rank indices at a time through LDS: both
+// the input and the output are moved along their own rows, whichever index
+// these have (40 adapters of 59 x 8385 to columns: 344 -> 40 us against
+// stores of single elements)
+__device__ __forceinline__ void pack(const Job &j, int block, unsigned char *lds) {
+    uint32_t *const tile = (uint32_t *)lds;   // [32][65]
+    const int width = j.by_rank ? (int)j.ldo : j.cols, across = (width + 63) / 64, u = block / across, c0 = block % across * 64;
+    const int rank = j.run_rank[u], tid = threadIdx.x;
+    // (a half of an adapter has at most 2^28 elements: 32-bit offsets)
+    const char *const in = (const char *)j.in + (int64_t)j.run_id[u] * j.cols * j.R * (j.f32 ? 4 : 2);
+    for (int r0 = 0; r0 < j.rp; r0 += 32) {
+        // (clamped, so that no branch stands between the loads)
+        uint32_t x[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = k * 256 + tid;
+            const int r = min(r0 + (j.in_rc ? i >> 6 : i & 31), rank - 1), c = min(c0 + (j.in_rc ? i & 63 : i >> 5), j.cols - 1);
+            const uint32_t at = j.in_rc ? (uint32_t)r * j.cols + c : (uint32_t)c * j.R + r;
+            x[k] = j.f32 ? *(const uint32_t *)(in + at * 4u) : *(const u16 *)(in + at * 2u);
         }
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const int i = k * 256 + tid, r = j.in_rc ? i >> 6 : i & 31, c = j.in_rc ? i & 63 : i >> 5;
+            tile[r * 65 + c] = r0 + r < rank && c0 + c < j.cols ? x[k] : 0u;
+        }
+        __syncthreads();
+        if (j.by_rank) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) {
+                const int r = (k * 256 + tid) >> 6, c = tid & 63;
+                if (c0 + c >= width) continue;
+                const int64_t to = ((int64_t)u * j.rp + r0 + r) * j.ldo + c0 + c;
+                if (j.f32)
+                    ((uint32_t *)j.out)[to] = tile[r * 65 + c];
+                else
+                    ((u16 *)j.out)[to] = (u16)tile[r * 65 + c];
+            }
+        } else if (c0 + (tid >> 2) < j.cols) {
+            const int c = tid >> 2, r = (tid & 3) * 8;
+            uint4 v;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) (&v.x)[k] = tile[(r + 2 * k) * 65 + c] | tile[(r + 2 * k + 1) * 65 + c] << 16;
+            u16 *out = (u16 *)j.out + ((int64_t)u * j.cols + c0 + c) * 2 * j.rp + r0 + r;
+            *(uint4 *)out = v;
+            *(uint4 *)(out + j.rp) = v;
+        }
+        __syncthreads();
     }
 }
 
@@ -302,20 +329,37 @@ __device__ __forceinline__ void chunks(const Job &j, int block, unsigned char *l
     float *const tile = (float *)lds;   // [32][65]
     const int across = (j.cols + CHUNK_COLS - 1) / CHUNK_COLS, ad = block / across, c0 = block % across * CHUNK_COLS;
     const int u = j.run_of[ad], rank = u < 0 ? 0 : j.run_rank[u];
-    const int k0 = u < 0 ? 0 : j.chunk_first[u], k1 = u < 0 ? 0 : j.chunk_first[u + 1];
+    const int k0 = u < 0 ? 0 : j.chunk_first[u] * j.sub, k1 = u < 0 ? 0 : j.chunk_first[u + 1] * j.sub;
     float *out = (float *)j.out + (int64_t)ad * j.R * j.cols;
+    const int tid = threadIdx.x, c = c0 + (tid & 63), cc = min(c, j.cols - 1);
     for (int r0 = 0; r0 < j.R; r0 += 32) {
-        for (int i = threadIdx.x; i < 32 * 64; i += 256) {
-            const int r = r0 + (i >> 6), c = c0 + (i & 63);
-            float v = 0.f;
-            if (r < rank && c < j.cols) {
+        // thread: rank indices r0 + tid / 64 + 4 q; all Q sums of a piece are
+        // asked for together
+        float v[8] = {};
+        auto add = [&](auto q_) __attribute__((always_inline)) {
+            constexpr int Q = decltype(q_)::value;
+            const float *p = j.sum + ((int64_t)k0 * j.rp + r0 + (tid >> 6)) * j.cols + cc;
 #pragma unroll 4
-                for (int k = k0; k < k1; ++k) v += j.sum[((int64_t)k * j.rp + r) * j.cols + c];
+            for (int k = k0; k < k1; ++k, p += (int64_t)j.rp * j.cols) {
+#pragma unroll
+                for (int q = 0; q < Q; ++q) v[q] += p[(int64_t)(4 * q) * j.cols];
             }
+        };
+        const int left = rank - r0;
+        if (left > 16)
+            add(std::integral_constant<int, 8>{});
+        else if (left > 4)
+            add(std::integral_constant<int, 4>{});
+        else if (left > 0)
+            add(std::integral_constant<int, 1>{});
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            const int i = (tid >> 6) + 4 * q, r = r0 + i;
+            const float x = r < rank && c < j.cols ? v[q] : 0.f;
             if (j.turned)
-                tile[(i >> 6) * 65 + (i & 63)] = v;
+                tile[i * 65 + (tid & 63)] = x;
             else if (r < j.R && c < j.cols)
-                out[(int64_t)r * j.cols + c] = v;
+                out[(int64_t)r * j.cols + c] = x;
         }
         if (!j.turned) continue;
         __syncthreads();
@@ -389,7 +433,7 @@ __global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
         case JOB_COLMAX: columns<true>(j, block, lds); break;
         case JOB_COLSUM: columns<false>(j, block, lds); break;
         case JOB_COLADD: coladd(j, block, lds); break;
-        case JOB_PACK: pack(j, block); break;
+        case JOB_PACK: pack(j, block, lds); break;
         case JOB_CHUNKS: chunks(j, block, lds); break;
         case JOB_ROWS: rows(j, block, lds); break;
     }
@@ -432,12 +476,12 @@ bool add_job(Jobs &all, const Job &in) {
             blocks = across;
             break;
         case JOB_PACK:
-            ok = ok && j.in && j.out && j.run_id && j.run_rank && j.R > 0 && j.rp >= j.R && j.n > 0 &&
+            ok = ok && j.in && j.out && j.run_id && j.run_rank && j.R > 0 && j.rp >= j.R && j.rp % 32 == 0 && j.n > 0 &&
                  (j.by_rank ? j.ldo >= j.cols : !j.f32);
             blocks = (j.by_rank ? (j.ldo + 63) / 64 : across) * j.n;
             break;
         case JOB_CHUNKS:
-            ok = ok && j.sum && j.out && j.run_of && j.run_rank && j.chunk_first && j.R > 0 && j.rp >= j.R && j.n > 0;
+            ok = ok && j.sum && j.sub > 0 && j.out && j.run_of && j.run_rank && j.chunk_first && j.R > 0 && j.rp >= j.R && j.n > 0;
             blocks = across * j.n;
             break;
         case JOB_ROWS:

@@ -117,7 +117,7 @@ struct BatchTables {
     const int *run_of;     // [adapters] run or -1
     const int *run_at;     // [rows] run of position p or -1
     const int4 *row_info;  // [rows], batches of up to ROWS_MAX rows: position, run or -1, adapter, rank
-    int rows, runs, adapters, rank, n_items, n_chunks;
+    int rows, runs, adapters, rank, n_items, n_chunks, per_chunk;   // per_chunk: most positions of a chunk
 };
 
 // y of up to ROWS_MAX rows. x and w in place: 16-byte aligned rows, K a
@@ -168,8 +168,11 @@ struct OuterArgs {
     const int *perm;       // or null
     float *out;
     int64_t ld, chunk;     // distance of rows, and of chunks
-    const int *chunks;     // [n_chunks][3]: .., first position, positions; null: `per` positions in each
-    int n_chunks, positions, per;
+    // [n_chunks / sub][3]: .., first position, positions, each of them in
+    // `sub` pieces of which the last ones may be empty; null: `per` positions
+    // in each
+    const int *chunks;
+    int n_chunks, sub, positions, per;
 };
 constexpr int MAX_OUTER = 4;
 struct Outers {
@@ -202,7 +205,7 @@ enum JobKind {
     // out[run][rp][ldo]. Rank indices from the run's rank on are zeros, and
     // so are columns beyond C
     JOB_PACK,
-    // out[adapter] = sum over its chunks of part [chunk][rp][C], as [R][C] or
+    // out[adapter] = sum over its chunks' pieces of part [piece][rp][C], as [R][C] or
     // (turned) [C][R]; zeros for adapters without rows, and from an
     // adapter's rank on
     JOB_CHUNKS,
@@ -221,6 +224,7 @@ struct Job {
     int64_t ldi, ldo;
     const int *perm;
     int in_rc, by_rank, turned, R, rp, n;   // PACK: n runs, CHUNKS: n adapters; columns in cols
+    int sub;               // CHUNKS: pieces of a chunk
     const int *run_id, *run_rank, *run_of, *chunk_first;
     const int4 *row_info;
     const float *t;

@@ -315,6 +315,7 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
     t.rank = max_rank;
     t.n_items = (int)items.size() / 3;
     t.n_chunks = (int)chunks.size() / 3;
+    t.per_chunk = per_chunk;
     st->batches[id] = std::move(b);
     *out_id = (int32_t)id;
     return GEMEL_OK;
@@ -791,8 +792,14 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // column sums of dy: of 64 rows each where dy is transposed anyway
     const int sums = (int)(tiled ? (M + 63) / 64 : std::min<int64_t>(128, (M + 63) / 64));
     const size_t o_sum = c.lay.take(dbias && !few ? sums * N : 0, 4);
-    const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * rp * K : 0, 4),
-                 o_db = c.lay.take(db ? (int64_t)b.n_chunks * rp * N : 0, 4), o_part = c.lay.take(part, 4);
+    // pieces of the adapters' chunks: where these have few columns, enough for
+    // three workgroups on each compute unit
+    auto pieces = [&](int64_t C) {
+        const int64_t groups = b.n_chunks * (rp / 32) * ((C + (f32 ? 127 : 255)) / (f32 ? 128 : 256));
+        return (int)std::max<int64_t>(1, std::min<int64_t>(768 / std::max<int64_t>(groups, 1), b.per_chunk / 64));
+    };
+    const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * pieces(K) * rp * K : 0, 4),
+                 o_db = c.lay.take(db ? (int64_t)b.n_chunks * pieces(N) * rp * N : 0, 4), o_part = c.lay.take(part, 4);
     if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
 
     Jobs first, second, last;
@@ -876,11 +883,13 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         o.ld = C;
         o.chunk = rp * C;
         o.chunks = b.chunks;
-        o.n_chunks = b.n_chunks;
+        o.sub = pieces(C);
+        o.n_chunks = b.n_chunks * o.sub;
         ok = ok && add_outer(outers, o);
         Job j = job(JOB_CHUNKS, nullptr, 0, 0, (int)C, true);
         j.sum = o.out;
         j.out = out;
+        j.sub = o.sub;
         j.turned = turned;
         j.R = b.rank;
         j.rp = rp;
