@@ -48,13 +48,15 @@ __device__ __forceinline__ const A &arg_of(int i) {
     return ((const Two<A> *)__builtin_amdgcn_kernarg_segment_ptr())->a[i];
 }
 
-// What becomes of a sum t (scaled) of position p and rank index q.
-__device__ __forceinline__ void put_thin(const ShrinkArgs &a, int64_t p, int q, float t) {
+// What becomes of a sum t (scaled) of position p and rank index q. An adapter
+// whose other half is not finite (bad) spoils its own rows, here, as that
+// half's copy holds zeros in those places.
+__device__ __forceinline__ void put_thin(const ShrinkArgs &a, int64_t p, int q, float t, int bad) {
     if (a.t) a.t[p * a.rp + q] = t;
     if (a.planes) {
         // bf16 pair: t to 16 bits, so that its product with B is as exact as
         // the main product's sums
-        const u16 h = bf_down(t);
+        const u16 h = bad ? (u16)0x7fc0 : bf_down(t);
         a.planes[p * 2 * a.rp + q] = h;
         a.planes[p * 2 * a.rp + a.rp + q] = bf_down(t - bf_up(h));
     }
@@ -145,7 +147,14 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
     for (int i = 0; i < 2; ++i)
 #pragma unroll
         for (int j = 0; j < RB; ++j) part[wave][i * RB + j][lane] = acc[i][j];
-    __syncthreads();
+    int bad = 0;
+    if (a.flags) {
+        for (int i = threadIdx.x; i < a.n_flags; i += 512) bad |= a.flags[(int64_t)u * a.n_flags + i];
+        bad = __syncthreads_or(bad);
+        if (a.slices > 1 && threadIdx.x == 0) a.bad[u] = bad;
+    } else {
+        __syncthreads();
+    }
     if (wave >= 2 * RB) return;
     f32x4 sum = part[0][wave][lane];
     for (int w = 1; w < 8; ++w) sum += part[w][wave][lane];
@@ -159,7 +168,7 @@ __global__ __launch_bounds__(512) void shrink_kernel(const Two<ShrinkArgs> args)
         if (a.slices > 1)
             a.part[((int64_t)slice * a.b.rows + p) * a.rp + q] = sum[e];
         else
-            put_thin(a, p, q, q < rank ? sum[e] * scale : 0.f);
+            put_thin(a, p, q, q < rank ? sum[e] * scale : 0.f, bad);
     }
 }
 
@@ -174,7 +183,7 @@ __global__ __launch_bounds__(256) void shrink_sum_kernel(const Two<ShrinkArgs> a
     float t = 0.f;
 #pragma unroll 8
     for (int k = 0; k < a.slices; ++k) t += a.part[k * n + i];
-    put_thin(a, p, q, q < a.b.run_rank[u] ? t * a.b.run_scale[u] : 0.f);
+    put_thin(a, p, q, q < a.b.run_rank[u] ? t * a.b.run_scale[u] : 0.f, a.flags ? a.bad[u] : 0);
 }
 
 // out[r][c] = sum over a chunk's positions of p(pos, r) q[row][c] for 32 r
@@ -357,7 +366,8 @@ hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
         if (!tables(a[i].b) || !a[i].x || !a[i].a || a[i].K <= 0 || a[i].rp % 32 || a[i].rp < a[i].b.rank ||
             a[i].b.n_items <= 0 || !(a[i].t || a[i].planes) || a[i].rp != a[0].rp || a[i].f32 != a[0].f32 ||
             a[i].b.items != a[0].b.items || a[i].slices < 1 || a[i].per < 1 || (int64_t)a[i].slices * a[i].per < a[i].K ||
-            (int64_t)(a[i].slices - 1) * a[i].per >= a[i].K || (a[i].slices > 1 && !a[i].part))
+            (int64_t)(a[i].slices - 1) * a[i].per >= a[i].K || (a[i].slices > 1 && !a[i].part) ||
+            (a[i].flags && (a[i].n_flags < 1 || (a[i].slices > 1 && !a[i].bad))))
             return hipErrorInvalidValue;
     const int slices = a[0].slices + (n > 1 ? a[1].slices : 0);
     const dim3 grid((unsigned)a[0].b.n_items, (unsigned)(a[0].rp / 32), (unsigned)slices);

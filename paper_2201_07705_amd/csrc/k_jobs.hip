@@ -284,6 +284,7 @@ __device__ __forceinline__ void pack(const Job &j, int block, unsigned char *lds
     const int rank = j.run_rank[u], tid = threadIdx.x;
     // (a half of an adapter has at most 2^28 elements: 32-bit offsets)
     const char *const in = (const char *)j.in + (int64_t)j.run_id[u] * j.cols * j.R * (j.f32 ? 4 : 2);
+    int bad = 0;
     for (int r0 = 0; r0 < j.rp; r0 += 32) {
         // (clamped, so that no branch stands between the loads)
         uint32_t x[8];
@@ -297,7 +298,10 @@ __device__ __forceinline__ void pack(const Job &j, int block, unsigned char *lds
 #pragma unroll
         for (int k = 0; k < 8; ++k) {
             const int i = k * 256 + tid, r = j.in_rc ? i >> 6 : i & 31, c = j.in_rc ? i & 63 : i >> 5;
-            tile[r * 65 + c] = r0 + r < rank && c0 + c < j.cols ? x[k] : 0u;
+            const bool there = r0 + r < rank && c0 + c < j.cols;
+            const bool spoilt = there && !j.by_rank && (x[k] & 0x7f80u) == 0x7f80u;
+            bad |= spoilt;
+            tile[r * 65 + c] = there && !spoilt ? x[k] : 0u;
         }
         __syncthreads();
         if (j.by_rank) {
@@ -322,6 +326,9 @@ __device__ __forceinline__ void pack(const Job &j, int block, unsigned char *lds
         }
         __syncthreads();
     }
+    if (j.by_rank) return;
+    bad = __syncthreads_or(bad);
+    if (tid == 0) j.flags[block] = bad;
 }
 
 // 64 columns of an adapter per block, 32 rank indices at a time
@@ -477,7 +484,7 @@ bool add_job(Jobs &all, const Job &in) {
             break;
         case JOB_PACK:
             ok = ok && j.in && j.out && j.run_id && j.run_rank && j.R > 0 && j.rp >= j.R && j.rp % 32 == 0 && j.n > 0 &&
-                 (j.by_rank ? j.ldo >= j.cols : !j.f32);
+                 (j.by_rank ? j.ldo >= j.cols : !j.f32 && j.flags);
             blocks = (j.by_rank ? (j.ldo + 63) / 64 : across) * j.n;
             break;
         case JOB_CHUNKS:

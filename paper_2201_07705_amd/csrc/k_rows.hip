@@ -305,9 +305,10 @@ hipError_t go(const RowsArgs &a, hipStream_t s) {
 
 // Slices of the depth: as many workgroups as run at once (three on a compute
 // unit with up to 32 rows, else two), and at least four steps in each; thin
-// products 2 KB of each row in a slice, which may take a third of those places
-// (all of them left 64 float32 rows of 64 adapters, 4096 -> 4096, one slice
-// and 93 us; counted as a quarter, 64 bf16 rows got 7 and took 18 us, not 16).
+// products 2 KB of each row in a slice, which may take half of those places,
+// of float32 a third. 64 rows of 64 adapters, 4096 -> 4096: float32 93 us
+// where they may take all (one slice is left), 50 for half, 44 for a third;
+// bf16 15.6 for half (4 slices), 17.8 for a third (5).
 void rows_plan(RowsArgs &a) {
     const int elem = a.f32 ? 4 : 2;
     a.all_steps = (int)(((int64_t)a.K * elem + ROW - 1) / ROW);
@@ -316,7 +317,7 @@ void rows_plan(RowsArgs &a) {
     a.thin_slices = (int)(((int64_t)a.K * elem + a.thin_bytes - 1) / a.thin_bytes);
     a.thin_blocks = a.b.runs ? a.b.n_items * a.rank_blocks * a.thin_slices : 0;
     const int tiles = (a.N + 63) / 64, slots = a.b.rows <= 32 ? 768 : 512;
-    const int want = std::max(1, std::min({(slots - std::min(a.thin_blocks, slots / 3)) / tiles, (a.all_steps + 3) / 4, 64}));
+    const int want = std::max(1, std::min({(slots - std::min(a.thin_blocks, slots / (a.f32 ? 3 : 2))) / tiles, (a.all_steps + 3) / 4, 64}));
     a.steps = (a.all_steps + want - 1) / want;
     a.slices = (a.all_steps + a.steps - 1) / a.steps;
     a.ldp = op_round_up(a.N, 4);

@@ -149,6 +149,11 @@ struct ShrinkArgs {
     int by_run, f32, K, rp;
     int slices, per;       // shrink_plan: the depth in slices of `per`
     float *part;           // [slices][rows][rp] with slices > 1
+    // null, or JOB_PACK's flags of the other half ([runs][n_flags]): planes of
+    // a run with any set are NaN; bad: [runs], with slices > 1
+    const int *flags;
+    int n_flags;
+    int *bad;
     u16 *planes;           // [rows][2 rp] hi | lo, or null
     float *t;              // [rows][rp]
     BatchTables b;
@@ -203,7 +208,9 @@ enum JobKind {
     // adapter halves per run, in [adapters][C][R] (or in_rc [R][C]):
     // out[run][C][2 rp] with each row's ranks twice (bf16), or by_rank:
     // out[run][rp][ldo]. Rank indices from the run's rank on are zeros, and
-    // so are columns beyond C
+    // so are columns beyond C. Not by_rank, values that are not finite become
+    // zeros too, and flags [runs][ceil(C / 64)] say where there were any: in
+    // the product rows of other runs meet them as factors of zero
     JOB_PACK,
     // out[adapter] = sum over its chunks' pieces of part [piece][rp][C], as [R][C] or
     // (turned) [C][R]; zeros for adapters without rows, and from an
@@ -225,6 +232,7 @@ struct Job {
     const int *perm;
     int in_rc, by_rank, turned, R, rp, n;   // PACK: n runs, CHUNKS: n adapters; columns in cols
     int sub;               // CHUNKS: pieces of a chunk
+    int *flags;            // PACK, not by_rank
     const int *run_id, *run_rank, *run_of, *chunk_first;
     const int4 *row_info;
     const float *t;

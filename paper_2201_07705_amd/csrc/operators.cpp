@@ -441,7 +441,7 @@ struct Adapted {
     // layout
     bool pad_in = false, pad_w = false;
     Copy c_in, c_w;
-    size_t o_bank = 0;
+    size_t o_bank = 0, o_flags = 0;
     MmArgs mm{};
 };
 
@@ -461,6 +461,7 @@ int64_t plan_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p) {
     if (p.pad_in) p.c_in = plan_copy(c, b.rows, p.K, f32, false);
     if (p.pad_w) p.c_w = plan_copy(c, p.N, p.K, f32, p.w_t);
     if (b.runs) p.o_bank = c.lay.take((int64_t)b.runs * op_round_up(p.N, 4) * rp, 4);
+    if (b.runs && !f32) p.o_flags = c.lay.take((int64_t)b.runs * ((p.N + 63) / 64 + 1), 4);   // flags, and one for each run
     return partial_floats(m);
 }
 
@@ -479,6 +480,7 @@ bool add_adapted(Call &c, const BatchTables &b, bool f32, Adapted &p, Jobs &firs
     k.ldo = op_round_up(p.N, 4);
     k.run_id = b.run_id;
     k.run_rank = b.run_rank;
+    if (!f32) k.flags = c.at<int>(p.o_flags);
     return add_job(second, k);
 }
 
@@ -543,6 +545,13 @@ ShrinkArgs shrink(const BatchTables &b, bool f32, const void *x, int64_t ldx, in
     s.b = b;
     shrink_plan(s, n);
     return s;
+}
+
+// The thin product takes over what JOB_PACK found in the other half.
+void spoil(Call &c, const Adapted &p, ShrinkArgs &s) {
+    s.n_flags = (p.N + 63) / 64;
+    s.flags = c.at<int>(p.o_flags);
+    s.bad = c.at<int>(p.o_flags) + (int64_t)s.b.runs * s.n_flags;
 }
 
 int64_t part_floats(const ShrinkArgs &s) { return s.slices > 1 ? (int64_t)s.slices * s.b.rows * s.rp : 0; }
@@ -644,6 +653,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
         (f32 ? (void *&)p.t : (void *&)p.planes) = c.at<void>(o_t);
         t.planes = p.planes;
         t.t = p.t;
+        if (!f32) spoil(c, p, t);
         t.part = c.at<float>(o_tp);
         OPCHK(launch_shrink(&t, 1, stream), "thin product");
     }
@@ -706,8 +716,8 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
     // few rows: W is read as it lies for dx, and dW written as the product
     // of a few columns of dy and rows of x, without copies of either (bf16
-    // 4096 -> 4096, an adapter for each row: 1 row 90 -> 79 us, 64 rows 273 ->
-    // 151; float32 132 -> 80 and 250 -> 175)
+    // 4096 -> 4096, an adapter for each row: 1 row 90 -> 79 us, 64 rows 275 ->
+    // 136; float32 132 -> 80 and 252 -> 150)
     const bool few = M <= ROWS_MAX;
     // few float32 outputs: dW in stretches of rows that read x as it lies,
     // where the transposed pairs of x and the maxima for them would cost more
@@ -923,6 +933,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         p.t = u;
         thin[0].a = c.at<char>(o_bt);
         thin[0].planes = dx ? p.planes : nullptr;
+        if (thin[0].planes) spoil(c, p, thin[0]);
         thin[0].t = u;
     }
     if (need_t) thin[need_u].t = t;

@@ -106,3 +106,30 @@ def test_operands_dropped_while_another_stream_works(ctxs, dtype):  # noqa: F811
     for y, grads, q in outs:
         assert torch.equal(y, want) and torch.equal(q, o)
         assert all(torch.equal(grads[name], wide[name]) for name in wide)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[5, 6, 4], [70, 80, 30], [40, 30, 7]])
+@pytest.mark.parametrize("k,n", [(96, 104), (9000, 200), (200, 9000)])
+def test_an_adapter_that_is_not_finite_spoils_its_own_rows(ctxs, dtype, rows, k, n):  # noqa: F811
+    """Requests of a spoilt adapter, a sound one and none, in one tile."""
+    import torch
+    ctx = ctxs[dtype]
+    s = problem(dtype, rows, [0, 1, -1], 2, 8, k, n, 31)
+    want = reference(s)
+    b = batch_of(ctx, s)
+    own, rest = slice(0, rows[0]), slice(rows[0], None)
+    for half, spoilt, at in (("b", float("nan"), (0, 3, 2)), ("b", float("inf"), (0, n - 1, 0)),
+                             ("a", float("nan"), (0, 5, k - 1)), ("a", float("-inf"), (0, 7, 1))):
+        t = dict(s, **{half: s[half].clone()})
+        t[half][at] = spoilt
+        y = ctx.adapt(b, s["x"], s["w"], t["a"], t["b"], bias=s["bias"])
+        close("y", y[rest], tuple(q[rest] for q in want["y"]))
+        assert not bool(torch.isfinite(y[own, at[1] if half == "b" else 0].float()).any())
+        got = ctx.adapt_backward(b, s["dy"], s["x"], s["w"], t["a"], t["b"])
+        close("x", got["x"][rest], tuple(q[rest] for q in want["x"]))
+        assert not bool(torch.isfinite(got["x"][own, at[2] if half == "a" else 0].float()).any())
+        for name in ("weight", "bias"):
+            close(name, got[name], want[name])
+        for name in ("a", "b"):
+            close(name, got[name][1:], tuple(q[1:] for q in want[name]))
