@@ -695,8 +695,8 @@ gemel_status gemel_profile(gemel_ctx *ctx, gemel_kernel_stat *stats,
  *  - While hip_stream is being captured into a graph a call is enqueued if
  *    an earlier call of the same sizes on that stream has grown the
  *    workspace, else it returns ESTATE. Replays of the graph use that
- *    workspace, so they are ordered after other work on the stream, and the
- *    graph is not replayed once a larger call on that stream has grown it.
+ *    workspace, so they are ordered after other work on the stream; a
+ *    workspace that was captured is kept when a larger call outgrows it.
  *  - Sums are float32 (norms float64), in an order that the sizes alone
  *    fix: the same call on the same data gives the same bits. float32
  *    contexts multiply float32 values as pairs of float16 (22 bits, each

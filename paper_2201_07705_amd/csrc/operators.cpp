@@ -59,6 +59,7 @@ struct Batch {
 struct Workspace {
     char *p = nullptr;
     size_t bytes = 0;
+    bool captured = false;   // a graph may hold its address
 };
 
 struct State : OperatorState {
@@ -68,6 +69,7 @@ struct State : OperatorState {
     void *pinned = nullptr;
     size_t pinned_bytes = 0;
     std::map<hipStream_t, Workspace> ws;
+    std::vector<char *> captured;   // outgrown workspaces that graphs may use
     std::vector<std::unique_ptr<Batch>> batches;
     // tables given back: `retired` ones may still be read by enqueued work
     std::vector<std::pair<void *, size_t>> spare, retired;
@@ -78,6 +80,7 @@ struct State : OperatorState {
         const bool ok = hipDeviceSynchronize() == hipSuccess;
         for (auto &w : ws)
             if (w.second.p) (void)hipFree(w.second.p);
+        for (char *p : captured) (void)hipFree(p);
         for (auto &b : batches)
             if (b && b->dev) (void)hipFree(b->dev);
         for (auto *v : {&spare, &retired})
@@ -86,6 +89,7 @@ struct State : OperatorState {
         if (pinned) (void)hipHostFree(pinned);
         if (side) (void)hipStreamDestroy(side);
         ws.clear();
+        captured.clear();
         batches.clear();
         spare.clear();
         retired.clear();
@@ -133,17 +137,18 @@ struct Layout {
 
 gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, size_t bytes, char **out) {
     Workspace &w = st.ws[stream];
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    if (stream) OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
     if (w.bytes < bytes) {
-        if (stream) {
-            hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
-            OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
-            if (cs != hipStreamCaptureStatusNone)
-                return fail(ctx, GEMEL_ESTATE, "the stream's workspace is too small to be captured: make the call once before");
-        }
+        if (cs != hipStreamCaptureStatusNone)
+            return fail(ctx, GEMEL_ESTATE, "the stream's workspace is too small to be captured: make the call once before");
         bytes = (size_t)op_round_up((int64_t)bytes, 2 << 20);
         if (w.p) {
             OPCHK(hipDeviceSynchronize(), "hipDeviceSynchronize");
-            (void)hipFree(w.p);
+            if (w.captured)
+                st.captured.push_back(w.p);
+            else
+                (void)hipFree(w.p);
             w = Workspace();
         }
         void *p = nullptr;
@@ -151,6 +156,7 @@ gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, size_t byt
         w.p = (char *)p;
         w.bytes = bytes;
     }
+    if (cs != hipStreamCaptureStatusNone) w.captured = true;
     *out = w.p;
     return GEMEL_OK;
 }

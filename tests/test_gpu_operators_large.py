@@ -133,3 +133,30 @@ def test_an_adapter_that_is_not_finite_spoils_its_own_rows(ctxs, dtype, rows, k,
             close(name, got[name], want[name])
         for name in ("a", "b"):
             close(name, got[name][1:], tuple(q[1:] for q in want[name]))
+
+
+def test_a_graph_outlives_its_workspace(ctxs):  # noqa: F811
+    """Replays after a larger call has grown the stream's workspace."""
+    import torch
+    ctx = ctxs["bf16"]
+    s = problem("bf16", [90, 45], [1, 0], 2, 8, 136, 104, 41)
+    big = problem("bf16", [4000], [0], 1, 8, 4096, 2048, 42)
+    b, bb = batch_of(ctx, s), batch_of(ctx, big)
+    want = ctx.adapt(b, s["x"], s["w"], s["a"], s["b"])
+    out = torch.zeros_like(want)
+    st = torch.cuda.Stream()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(st):
+        ctx.adapt(b, s["x"], s["w"], s["a"], s["b"])   # grows the workspace
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=st):
+        ctx.adapt(b, s["x"], s["w"], s["a"], s["b"], out=out)
+    with torch.cuda.stream(st):
+        ctx.adapt_backward(bb, big["dy"], big["x"], big["w"], big["a"], big["b"])
+    torch.cuda.synchronize()
+    for _ in range(3):
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want)
