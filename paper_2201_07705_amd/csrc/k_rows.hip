@@ -38,10 +38,18 @@ __device__ __forceinline__ void wait_vm() {
     static_assert(N >= 0 && N < 64, "vmcnt range");
     __builtin_amdgcn_s_waitcnt((N & 0xF) | ((N >> 4) << 14) | (0x7 << 4) | (0xF << 8));
 }
-__device__ __forceinline__ void barrier() {
+// The loads of a step have landed in every wave, and every wave has its last
+// fragments in registers: the buffer they came from may be refilled. (Their
+// products do not touch memory, so only the wait keeps the reads before the
+// barrier.)
+template <int N>
+__device__ __forceinline__ void turn() {
+    __builtin_amdgcn_s_waitcnt(0xF | (0x3 << 14) | (0x7 << 4));   // LDS reads
+    wait_vm<N>();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 }
 
 // The matrix-core product of two 16-byte chunks a lane holds: 8 bf16 (32
@@ -174,8 +182,7 @@ __global__ __launch_bounds__(256) void rows_kernel(const RowsArgs a) {
     for (int i = 0; i < RING - 1; ++i) issue(ring[i]);
     const int sw = (l16 >> 1) & 7;
     auto step = [&](const unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
-        wait_vm<(RING - 2) * LOADS>();
-        barrier();
+        turn<(RING - 2) * LOADS>();
         issue(next);
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
