@@ -2,8 +2,6 @@
 // adapters' own gradients, sums over rows.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-
 #include "op_args.h"
 #include "op_moves.h"
 
@@ -333,10 +331,6 @@ __global__ __launch_bounds__(256) void outer_kernel(const Outers args) {
         outer<F32, F32>(a, block, qs, ps);
 }
 
-bool tables(const BatchTables &b) {
-    return b.perm && b.run_start && b.run_id && b.run_rank && b.run_scale && b.first_run && b.items && b.chunks &&
-           b.chunk_first && b.run_of && b.run_at && b.rows > 0 && b.runs > 0 && b.adapters > 0 && b.rank > 0;
-}
 template <typename A>
 hipError_t launch(const void *fn, dim3 grid, int block, const A *a, int n, hipStream_t s) {
     Two<A> t{{a[0], a[n - 1]}};
@@ -346,29 +340,8 @@ hipError_t launch(const void *fn, dim3 grid, int block, const A *a, int n, hipSt
 
 }  // namespace
 
-// A workgroup takes 2 us for every 512 (float32) or 1024 columns, and adding
-// slices a launch of 5 us: the depth is cut where few workgroups would have
-// more than 8 us of it, into as many as the card holds at once.
-void shrink_plan(ShrinkArgs &a, int n) {
-    const int turn = a.f32 ? 512 : 1024, turns = (a.K + turn - 1) / turn;
-    const int64_t groups = (int64_t)a.b.n_items * (a.rp / 32) * n;
-    a.slices = 1;
-    a.per = a.K;
-    if (turns <= 4 || groups > 256) return;
-    const int want = (int)std::min<int64_t>(turns, 512 / std::max<int64_t>(1, groups));
-    a.per = (turns + want - 1) / want * turn;
-    a.slices = (a.K + a.per - 1) / a.per;
-}
-
 hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
-    if (n < 1 || n > 2) return hipErrorInvalidValue;
-    for (int i = 0; i < n; ++i)
-        if (!tables(a[i].b) || !a[i].x || !a[i].a || a[i].K <= 0 || a[i].rp % 32 || a[i].rp < a[i].b.rank ||
-            a[i].b.n_items <= 0 || !(a[i].t || a[i].planes) || a[i].rp != a[0].rp || a[i].f32 != a[0].f32 ||
-            a[i].b.items != a[0].b.items || a[i].slices < 1 || a[i].per < 1 || (int64_t)a[i].slices * a[i].per < a[i].K ||
-            (int64_t)(a[i].slices - 1) * a[i].per >= a[i].K || (a[i].slices > 1 && !a[i].part) ||
-            (a[i].flags && (a[i].n_flags < 1 || (a[i].slices > 1 && !a[i].bad))))
-            return hipErrorInvalidValue;
+    if (!shrink_valid(a, n)) return hipErrorInvalidValue;
     const int slices = a[0].slices + (n > 1 ? a[1].slices : 0);
     const dim3 grid((unsigned)a[0].b.n_items, (unsigned)(a[0].rp / 32), (unsigned)slices);
     const void *fn = a[0].f32 ? reinterpret_cast<const void *>(&shrink_kernel<true, 2>)
@@ -377,23 +350,6 @@ hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s) {
     if (e != hipSuccess || slices == n) return e;
     const dim3 all((unsigned)(((int64_t)a[0].b.rows * a[0].rp + 255) / 256), (unsigned)n);
     return launch(reinterpret_cast<const void *>(&shrink_sum_kernel), all, 256, a, n, s);
-}
-
-bool add_outer(Outers &o, const OuterArgs &a) {
-    if (o.n >= MAX_OUTER || !a.p || !a.q || !a.out || a.R < 1 || a.C < 1 || a.n_chunks < 1 || (a.sp != 1 && a.sr != 1) ||
-        a.ld < a.C || (a.q_f32 && !a.p_f32) || (o.n && a.q_f32 != o.a[0].q_f32) ||
-        (a.chunks && (a.sub < 1 || a.n_chunks % a.sub)) ||
-        (!a.chunks && (a.per < 1 || a.positions < 1 || (int64_t)a.n_chunks * a.per < a.positions ||
-                       (int64_t)(a.n_chunks - 1) * a.per >= a.positions)))
-        return false;
-    const int cols = a.q_f32 ? 128 : 256;
-    const int64_t blocks = (int64_t)((a.C + cols - 1) / cols) * ((a.R + 31) / 32) * a.n_chunks;
-    if (blocks + o.blocks > 0x7fffff00) return false;
-    o.a[o.n] = a;
-    o.first[o.n] = o.blocks;
-    o.blocks += (int)blocks;
-    o.first[++o.n] = o.blocks;
-    return true;
 }
 
 hipError_t launch_outer(const Outers &o, hipStream_t s) {

@@ -3,7 +3,6 @@
 // more than its work).
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "op_args.h"
@@ -66,7 +65,6 @@ __device__ __forceinline__ f32x4 up4(const u16 *p, int left) {
     return v;
 }
 
-constexpr int PAD_ITEMS = 1024;    // 16-byte chunks of a block of JOB_PAD
 constexpr int CHUNK_COLS = 64;     // columns of a block of JOB_CHUNKS
 
 // 16 bytes at a time; output rows are whole chunks of that
@@ -111,7 +109,6 @@ __device__ __forceinline__ void along(const float *in, int cols, int end, int c,
 
 // A workgroup per row (137 rows of 23605: 47 -> 12 us against a wave each), or
 // a wave for rows of up to SPLIT_WIDE.
-constexpr int SPLIT_WIDE = 1024;
 __device__ __forceinline__ void split(const Job &j, int block, unsigned char *lds) {
     const bool wide = j.cols > SPLIT_WIDE;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, r = wide ? block : block * 4 + wave;
@@ -447,64 +444,6 @@ __global__ __launch_bounds__(256) void jobs_kernel(const Jobs args) {
 }
 
 }  // namespace
-
-bool add_job(Jobs &all, const Job &in) {
-    if (all.n >= MAX_JOBS) return false;
-    Job &j = all.job[all.n];
-    j = in;
-    const int64_t across = ((int64_t)j.cols + 63) / 64;
-    int64_t blocks = 0;
-    bool ok = j.cols > 0;
-    switch (j.kind) {
-        case JOB_PAD:
-            ok = ok && j.in && j.out && j.rows > 0 && j.ldo >= j.cols && j.ldo % (j.f32 ? 4 : 8) == 0;
-            blocks = ((int64_t)j.rows * (j.ldo / (j.f32 ? 4 : 8)) + PAD_ITEMS - 1) / PAD_ITEMS;
-            break;
-        case JOB_SPLIT:
-            ok = ok && j.in && j.out && j.e && j.rows > 0 && j.ldo / 2 >= j.cols && j.ldo % (4 * PAIR_RUN) == 0;
-            blocks = j.cols > SPLIT_WIDE ? j.rows : ((int64_t)j.rows + 3) / 4;
-            break;
-        case JOB_TURN:
-            ok = ok && j.in && j.out && j.rows > 0 && j.ldo / (j.f32 ? 2 : 1) >= j.rows && j.ldo % (j.f32 ? 4 * PAIR_RUN : 4) == 0 &&
-                 (!j.f32 || (j.e && j.max && j.parts > 0));
-            blocks = across * ((j.ldo / (j.f32 ? 2 : 1) + 63) / 64);
-            ok = ok && (!j.sum || blocks == across * ((j.rows + 63) / 64));
-            break;
-        case JOB_COLMAX:
-            ok = ok && j.in && j.max && j.rows > 0 && j.parts > 0 && j.f32;
-            blocks = across * j.parts;
-            break;
-        case JOB_COLSUM:
-            ok = ok && j.in && j.sum && j.rows > 0 && j.parts > 0;
-            blocks = across * j.parts;
-            break;
-        case JOB_COLADD:
-            ok = ok && j.sum && j.out && j.parts > 0;
-            blocks = across;
-            break;
-        case JOB_PACK:
-            ok = ok && j.in && j.out && j.run_id && j.run_rank && j.R > 0 && j.rp >= j.R && j.rp % 32 == 0 && j.n > 0 &&
-                 (j.by_rank ? j.ldo >= j.cols : !j.f32 && j.flags);
-            blocks = (j.by_rank ? (j.ldo + 63) / 64 : across) * j.n;
-            break;
-        case JOB_CHUNKS:
-            ok = ok && j.sum && j.sub > 0 && j.out && j.run_of && j.run_rank && j.chunk_first && j.R > 0 && j.rp >= j.R && j.n > 0;
-            blocks = across * j.n;
-            break;
-        case JOB_ROWS:
-            ok = ok && j.sum && j.out && j.row_info && j.rows > 0 && j.rows <= ROWS_MAX && j.parts > 0 && j.ldi >= j.cols &&
-                 j.ldi % 4 == 0 && j.ldo >= j.cols && (!j.t || (j.in && j.R > 0 && j.R <= 256 && j.rp >= j.R));
-            blocks = (((int64_t)j.cols + 1023) / 1024) * j.rows;
-            break;
-        default: ok = false;
-    }
-    if (!ok || blocks < 1 || blocks + all.blocks > 0x7fffff00) return false;
-    j.blocks = (int)blocks;
-    all.first[all.n] = all.blocks;
-    all.blocks += j.blocks;
-    all.first[++all.n] = all.blocks;
-    return true;
-}
 
 hipError_t launch_jobs(const Jobs &j, hipStream_t s) {
     if (j.n == 0) return hipSuccess;

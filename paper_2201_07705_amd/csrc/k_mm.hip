@@ -2,7 +2,6 @@
 // A[m][k] * B[n][k], both operands rows of contiguous elements.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <climits>
 #include <type_traits>
 
@@ -18,7 +17,7 @@ typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int BK = 64;   // depth of a step: a 128-byte line of each row
+constexpr int BK = MM_BK;
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -756,21 +755,15 @@ __global__ __launch_bounds__(256) void mm_reduce_kernel(const MmArgs a) {
     }
 }
 
-int64_t tiles_of(const MmArgs &a, int T) {
-    const int64_t tm = T < 64 ? (a.M + 63) / 64 * (64 / T) : (a.M + T - 1) / T;
-    const int64_t tn = T < 64 ? (a.N + 63) / 64 * (64 / T) : (a.N + T - 1) / T;
-    return a.sym ? tm * (tm + 1) / 2 : tm * tn;
-}
-
 template <int T, int STAGES, int PHASES, bool F16, bool PAIR, int EPI>
 hipError_t go(const MmArgs &a, hipStream_t s) {
-    const dim3 grid((unsigned)tiles_of(a, T), (unsigned)a.splits, (unsigned)a.batch);
+    const dim3 grid((unsigned)mm_tiles(a, T), (unsigned)a.splits, (unsigned)a.batch);
     void *p[] = {const_cast<MmArgs *>(&a)};
     hipError_t e = hipLaunchKernel(reinterpret_cast<const void *>(&mm_kernel<T, STAGES, PHASES, F16, PAIR, EPI>), grid,
                                    dim3(mm_threads<T>()), p, 0, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return hipLaunchKernel(reinterpret_cast<const void *>(&mm_reduce_kernel<EPI>),
-                           dim3((unsigned)tiles_of(a, 32), 1, (unsigned)a.batch), dim3(256), p, 0, s);
+                           dim3((unsigned)mm_tiles(a, 32), 1, (unsigned)a.batch), dim3(256), p, 0, s);
 }
 
 template <int EPI, bool F16, bool PAIR>
@@ -791,72 +784,8 @@ hipError_t pairs_only(const MmArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Tile and depth splits, by the estimated time of the launch: the turns that
-// the compute units take, each a step's time for every step and a fixed part
-// for the pipeline's start and the epilogue; and, where the depth is split,
-// writing and reading the partial sums and the second launch. The times are
-// a fit to 23 shapes from 128 x 128 x 8192 to 25088 x 4096 x 4096 at every
-// tile and up to 32 splits, within 9% of the measured ones; for each of these
-// shapes the tile and split chosen is the fastest one measured. What splits
-// are for: a symmetric 512 x 512 result of depth 4608 takes 16.3 us whole and
-// 10.2 in 4 splits, one of 4096 x 4096 and 25088 pairs 1322 and 1089 us in 7
-// (its 136 tiles of 256 leave half of the 256 compute units idle); 2048 x
-// 1000 of 1024 pairs is fastest whole (22.4 us).
-double mm_plan(MmArgs &a) {
-    struct Form {
-        int tile, slots;                        // workgroups that run at once
-        double alone, full, fixed, fixed_part;  // microseconds; with partial sums out
-    };
-    static const Form single[] = {
-        {256, 256, 1.40, 1.40, 30.0, 6.5}, {128, 512, 0.48, 0.87, 12.3, 3.4}, {64, 512, 0.12, 0.36, 6.7, 2.5}};
-    static const Form pair[] = {
-        {256, 256, 2.05, 2.05, 50.0, 7.0}, {128, 512, 0.56, 1.20, 12.5, 3.6}, {64, 512, 0.16, 0.44, 6.3, 2.0}};
-    const Form *const forms = a.pair ? pair : single;
-    const int steps = (a.K + BK - 1) / BK;
-    double best = 1e30;
-    for (int i = 0; i < 3; ++i) {
-        const Form &f = forms[i];
-        const int64_t tiles = tiles_of(a, f.tile) * a.batch;
-        for (int want = 1; want <= 32 && want <= std::max(1, steps / 4); ++want) {
-            const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
-            if (splits != want) continue;
-            const int64_t groups = tiles * splits, whole = groups / f.slots, rest = groups % f.slots;
-            const double fixed = splits > 1 ? f.fixed_part : f.fixed;
-            double us = (double)whole * (per * f.full + fixed);
-            if (rest) us += per * (rest > 256 ? f.full : f.alone) + fixed;
-            const double bytes = (double)splits * a.batch * a.M * op_round_up(a.N, 4) * (a.sym ? 2 : 4);
-            if (splits > 1) us += 4.8 + 0.13 * splits + 2 * bytes / 5.5e6;
-            if (splits > 1 && bytes > 1e9) continue;
-            if (us < best) {
-                best = us;
-                a.tile = f.tile;
-                a.steps = per;
-                a.splits = splits;
-            }
-        }
-    }
-    a.ldp = op_round_up(a.N, 4);
-    return best;
-}
-
 hipError_t launch_mm(const MmArgs &a, hipStream_t s) {
-    const int nk = (a.K + BK - 1) / BK;
-    if (a.M <= 0 || a.N <= 0 || a.K <= 0 || a.K % 8 || a.batch <= 0 || a.batch > 65535 ||
-        a.lda % 8 || a.ldb % 8 || a.lda > MM_MAX_LD || a.ldb > MM_MAX_LD ||
-        (a.perm && a.perm_rows * a.lda > (1ll << 30)) || (a.tile != 64 && a.tile != 128 && a.tile != 256) || a.za % 8 || a.zb % 8 || a.lda < a.K || a.ldb < a.K || !a.zero || a.splits < 1 ||
-        a.steps < 1 || a.ext % BK || (int64_t)a.splits * a.steps < nk || (int64_t)(a.splits - 1) * a.steps >= nk)
-        return hipErrorInvalidValue;
-    if (!a.a || !a.b || (uintptr_t)a.a % 16 || (uintptr_t)a.b % 16) return hipErrorInvalidValue;
-    if (a.splits > 1 && (!a.partial || a.ldp % 4 || a.ldp < a.N)) return hipErrorInvalidValue;
-    if (a.ext && (!a.t || !a.bx || a.runs < 1 || !a.run_start || !a.first_run || a.batch != 1))
-        return hipErrorInvalidValue;
-    if (a.sym && a.M != a.N) return hipErrorInvalidValue;
-    if (a.epi == EPI_SCALED && (!a.o.ea || !a.o.eb ||
-                                (a.runs > 0 && (!a.o.t || !a.o.bx || !a.o.run_at || a.o.rank % 4 || a.o.rank > a.o.rp ||
-                                                a.o.ldbx % 4 || a.o.ldbx < a.N))))
-        return hipErrorInvalidValue;
-    if (a.epi != EPI_ROWS && (a.K % BK || a.ext)) return hipErrorInvalidValue;
-    if ((int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64) > INT32_MAX / 256) return hipErrorInvalidValue;
+    if (!mm_valid(a)) return hipErrorInvalidValue;
     switch (a.epi) {
         case EPI_ROWS: return a.pair ? hipErrorInvalidValue : pick<EPI_ROWS, false, false>(a, s);
         case EPI_SCALED: return pairs_only<EPI_SCALED>(a, s);

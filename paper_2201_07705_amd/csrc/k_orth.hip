@@ -393,13 +393,6 @@ hipError_t launch(const void *fn, dim3 grid, const OrthArgs &a, hipStream_t s, i
     void *p[] = {const_cast<OrthArgs *>(&a)};
     return hipLaunchKernel(fn, grid, dim3((unsigned)threads), p, 0, s);
 }
-bool valid(const OrthArgs &a) {
-    return a.g && a.rows > 0 && a.cols > 0 && a.count > 0 && a.count <= 65535 && a.parts > 0 && a.steps >= 1 &&
-           a.steps <= ORTH_MAX_STEPS && (!a.step || (a.m && a.f32));
-}
-bool valid_thin(const OrthArgs &a) {
-    return valid(a) && std::min(a.rows, a.cols) <= THIN_MAX && a.gram && a.q && a.e && a.out;
-}
 // f of the number of 16-row blocks, and whether the short axis is the rows
 template <typename F>
 hipError_t thin(const OrthArgs &a, F &&f) {
@@ -416,19 +409,18 @@ hipError_t thin(const OrthArgs &a, F &&f) {
 }  // namespace
 
 hipError_t launch_norm(const OrthArgs &a, hipStream_t s) {
-    if (!valid(a) || !a.sums) return hipErrorInvalidValue;
+    if (!orth_valid(a, false)) return hipErrorInvalidValue;
     return launch(reinterpret_cast<const void *>(&norm_kernel), dim3((unsigned)a.parts, (unsigned)a.count), a, s);
 }
 
 hipError_t launch_seed(const OrthArgs &a, hipStream_t s) {
-    const int64_t by = (a.rows + 63) / 64;
-    if (!valid(a) || !a.sums || !a.lambda || !a.x.hi || !a.xt.hi || by > 65535) return hipErrorInvalidValue;
+    if (!orth_valid(a, false)) return hipErrorInvalidValue;
     return launch(reinterpret_cast<const void *>(&seed_kernel),
-                  dim3((unsigned)((a.cols + 63) / 64), (unsigned)by, (unsigned)a.count), a, s);
+                  dim3((unsigned)((a.cols + 63) / 64), (unsigned)((a.rows + 63) / 64), (unsigned)a.count), a, s);
 }
 
 hipError_t launch_thin_gram(const OrthArgs &a, hipStream_t s) {
-    if (!valid_thin(a)) return hipErrorInvalidValue;
+    if (!orth_valid(a, true)) return hipErrorInvalidValue;
     return thin(a, [&](auto nb, bool wide) {
         constexpr int NB = decltype(nb)::value;
         return launch(wide ? reinterpret_cast<const void *>(&thin_gram_kernel<NB, true>)
@@ -438,7 +430,7 @@ hipError_t launch_thin_gram(const OrthArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_thin_poly(const OrthArgs &a, hipStream_t s) {
-    if (!valid_thin(a)) return hipErrorInvalidValue;
+    if (!orth_valid(a, true)) return hipErrorInvalidValue;
     return thin(a, [&](auto nb, bool) {
         constexpr int NB = decltype(nb)::value;
         return launch(reinterpret_cast<const void *>(&thin_poly_kernel<NB>), dim3((unsigned)a.count), a, s,
@@ -447,7 +439,7 @@ hipError_t launch_thin_poly(const OrthArgs &a, hipStream_t s) {
 }
 
 hipError_t launch_thin_apply(const OrthArgs &a, hipStream_t s) {
-    if (!valid_thin(a)) return hipErrorInvalidValue;
+    if (!orth_valid(a, true)) return hipErrorInvalidValue;
     return thin(a, [&](auto nb, bool wide) {
         constexpr int NB = decltype(nb)::value;
         return launch(wide ? reinterpret_cast<const void *>(&thin_apply_kernel<NB, true>)

@@ -16,7 +16,6 @@
 // and 97 us.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
 #include <type_traits>
 
 #include "op_args.h"
@@ -87,7 +86,7 @@ __device__ __forceinline__ uint4 chunk(const char *row, int at, int end) {
     return r.v;
 }
 
-constexpr int ROW = 128;   // bytes of a row in a step
+constexpr int ROW = ROWS_STEP;   // bytes of a row in a step
 constexpr int RING = 4;
 
 // Thin sums of item blockIdx / (rank blocks * slices): 4 waves share the slice.
@@ -310,34 +309,8 @@ hipError_t go(const RowsArgs &a, hipStream_t s) {
 
 }  // namespace
 
-// Slices of the depth: as many workgroups as run at once (three on a compute
-// unit with up to 32 rows, else two), and at least four steps in each; thin
-// products 2 KB of each row in a slice, which may take half of those places,
-// of float32 a third. 64 rows of 64 adapters, 4096 -> 4096: float32 93 us
-// where they may take all (one slice is left), 50 for half, 44 for a third;
-// bf16 15.6 for half (4 slices), 17.8 for a third (5).
-void rows_plan(RowsArgs &a) {
-    const int elem = a.f32 ? 4 : 2;
-    a.all_steps = (int)(((int64_t)a.K * elem + ROW - 1) / ROW);
-    a.rank_blocks = (a.b.rank + 15) / 16;
-    a.thin_bytes = 2048;
-    a.thin_slices = (int)(((int64_t)a.K * elem + a.thin_bytes - 1) / a.thin_bytes);
-    a.thin_blocks = a.b.runs ? a.b.n_items * a.rank_blocks * a.thin_slices : 0;
-    const int tiles = (a.N + 63) / 64, slots = a.b.rows <= 32 ? 768 : 512;
-    const int want = std::max(1, std::min({(slots - std::min(a.thin_blocks, slots / (a.f32 ? 3 : 2))) / tiles, (a.all_steps + 3) / 4, 64}));
-    a.steps = (a.all_steps + want - 1) / want;
-    a.slices = (a.all_steps + a.steps - 1) / a.steps;
-    a.ldp = op_round_up(a.N, 4);
-}
-
 hipError_t launch_rows(const RowsArgs &a, hipStream_t s) {
-    const int q = a.f32 ? 4 : 8;
-    if (!a.x || !a.w || !a.y || !a.partial || !a.zero || a.b.rows < 1 || a.b.rows > ROWS_MAX || a.N < 1 || a.K < 1 ||
-        a.slices < 1 || a.steps < 1 || (int64_t)(a.slices - 1) * a.steps >= a.all_steps ||
-        (int64_t)a.slices * a.steps < a.all_steps || (uintptr_t)a.x % 16 || (uintptr_t)a.w % 16 || a.ldx % q || a.ldw % q ||
-        a.K % q || a.ldx < a.K || a.ldw < a.K || a.k_bank > a.K || a.k_bank < 1 || a.ldp < a.N || a.ldp % 4 || (int64_t)a.K * (a.f32 ? 4 : 2) > (1 << 30) ||
-        (a.thin_blocks && (!a.a || !a.bank_b || !a.t || a.b.rank > 256)))
-        return hipErrorInvalidValue;
+    if (!rows_valid(a)) return hipErrorInvalidValue;
     return a.f32 ? go<true>(a, s) : go<false>(a, s);
 }
 

@@ -1,8 +1,8 @@
 // Argument blocks and launchers of the operators that serve and retrain
 // merged layers: adapted projections, their gradients, and orthogonalised
-// matrix updates. Each launcher checks on the host that its block matches
-// what the kernel and grid assume and returns hipErrorInvalidValue instead
-// of launching otherwise.
+// matrix updates. Each launcher checks on the host (op_plan.cpp) that its
+// block matches what the kernel and grid assume and returns
+// hipErrorInvalidValue instead of launching otherwise.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -98,7 +98,10 @@ struct MmArgs {
 // Longest rows: a tile's byte offsets fit 32 bits (and with a row table the
 // whole matrix's: perm_rows * lda up to 2^30 elements).
 constexpr int64_t MM_MAX_LD = 1 << 22;
+constexpr int MM_BK = 64;   // depth of a step: a 128-byte line of each row
 double mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape; the microseconds expected
+int64_t mm_tiles(const MmArgs &a, int T);   // T x T tiles of a result (32: the sum of splits)
+bool mm_valid(const MmArgs &a);
 hipError_t launch_mm(const MmArgs &a, hipStream_t s);
 
 constexpr int ROWS_MAX = 64;   // rows that launch_rows takes
@@ -138,7 +141,9 @@ struct RowsArgs {
     float *t;              // [thin_slices][rows][rank_blocks * 16]
     BatchTables b;
 };
+constexpr int ROWS_STEP = 128;   // bytes of a row in a step
 void rows_plan(RowsArgs &a);
+bool rows_valid(const RowsArgs &a);
 hipError_t launch_rows(const RowsArgs &a, hipStream_t s);
 
 // t[p][r] = scale * sum over k of x[perm[p]][k] * a[run][r][k]
@@ -159,6 +164,7 @@ struct ShrinkArgs {
     BatchTables b;
 };
 void shrink_plan(ShrinkArgs &a, int n);   // slices, per; n products go in one launch
+bool shrink_valid(const ShrinkArgs *a, int n);
 // One or two thin products (of one batch) in a launch (two, where the depth is cut).
 hipError_t launch_shrink(const ShrinkArgs *a, int n, hipStream_t s);
 
@@ -237,6 +243,8 @@ struct Job {
     const int4 *row_info;
     const float *t;
 };
+constexpr int PAD_ITEMS = 1024;    // 16-byte chunks of a block of JOB_PAD
+constexpr int SPLIT_WIDE = 1024;   // longest row that JOB_SPLIT gives to a wave
 constexpr int MAX_JOBS = 6;
 struct Jobs {
     int n = 0, blocks = 0;
@@ -273,6 +281,7 @@ struct OrthArgs {
     u16 *copy;
     float rate, decay;
 };
+bool orth_valid(const OrthArgs &a, bool thin);
 hipError_t launch_norm(const OrthArgs &a, hipStream_t s);   // momentum and squared sums
 hipError_t launch_seed(const OrthArgs &a, hipStream_t s);   // planes of the scaled update, lambda
 hipError_t launch_thin_gram(const OrthArgs &a, hipStream_t s);   // momentum and partial Gram matrices

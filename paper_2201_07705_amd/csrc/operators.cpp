@@ -11,6 +11,10 @@
 #include <utility>
 #include <vector>
 
+#ifdef __SANITIZE_ADDRESS__
+#include <sanitizer/asan_interface.h>
+#endif
+
 #include "internal.h"
 #include "op_args.h"
 
@@ -131,12 +135,27 @@ struct Layout {
     size_t take(int64_t n, size_t elem) {
         const size_t at = bytes;
         bytes += (size_t)op_round_up(n * (int64_t)elem, 256);
+#ifdef __SANITIZE_ADDRESS__
+        pieces.emplace_back(at, (size_t)n * elem);
+        bytes += 256;
+#endif
         return at;
     }
+#ifdef __SANITIZE_ADDRESS__
+    // CPU builds with AddressSanitizer: only the pieces themselves may be accessed
+    std::vector<std::pair<size_t, size_t>> pieces;
+    void fence(char *base, size_t all) const {
+        ASAN_POISON_MEMORY_REGION(base, all);
+        for (const auto &p : pieces) ASAN_UNPOISON_MEMORY_REGION(base + p.first, p.second);
+    }
+#else
+    void fence(char *, size_t) const {}
+#endif
 };
 
-gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, size_t bytes, char **out) {
+gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layout &lay, char **out) {
     Workspace &w = st.ws[stream];
+    size_t bytes = lay.bytes;
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
     if (stream) OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
     if (w.bytes < bytes) {
@@ -157,6 +176,7 @@ gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, size_t byt
         w.bytes = bytes;
     }
     if (cs != hipStreamCaptureStatusNone) w.captured = true;
+    lay.fence(w.p, w.bytes);
     *out = w.p;
     return GEMEL_OK;
 }
@@ -579,7 +599,7 @@ gemel_status adapt_rows(Call &c, const BatchTables &b, bool f32, const gemel_pro
     const size_t o_x = c.lay.take(copy_x ? b.rows * Kp : 0, e), o_w = c.lay.take(copy_w ? N * Kp : 0, e),
                  o_p = c.lay.take((int64_t)a.slices * b.rows * a.ldp, 4),
                  o_t = c.lay.take(a.thin_blocks ? (int64_t)a.thin_slices * b.rows * a.rank_blocks * 16 : 0, 4);
-    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return s;
+    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return s;
     a.x = x;
     a.ldx = ldx;
     a.w = proj->weight;
@@ -651,7 +671,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4),
                  o_tp = c.lay.take(b.runs ? part_floats(t) : 0, 4);
     const size_t o_part = c.lay.take(plan_adapted(c, b, f32, p), 4);
-    if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
+    if (gemel_status s = workspace(ctx, *st, stream, c.lay, &c.base)) return s;
     Jobs first, second;
     if (!add_adapted(c, b, f32, p, first, second)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
     OPCHK(launch_jobs(second, stream), "copies");
@@ -816,7 +836,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     };
     const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * pieces(K) * rp * K : 0, 4),
                  o_db = c.lay.take(db ? (int64_t)b.n_chunks * pieces(N) * rp * N : 0, 4), o_part = c.lay.take(part, 4);
-    if (gemel_status s = workspace(ctx, *st, stream, c.lay.bytes, &c.base)) return s;
+    if (gemel_status s = workspace(ctx, *st, stream, c.lay, &c.base)) return s;
 
     Jobs first, second, last;
     Outers outers;
@@ -970,7 +990,7 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
     o.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(m + 63) / 64, 64, (1024 + o.count - 1) / o.count}));
     const size_t og = c.lay.take((int64_t)o.count * o.parts * np * np, 8), oq = c.lay.take((int64_t)o.count * np * np, 4),
                  oe = c.lay.take(o.count, 4);
-    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return s;
+    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return s;
     o.gram = c.at<double>(og);
     o.q = c.at<float>(oq);
     o.e = c.at<int>(oe);
@@ -1053,7 +1073,7 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         q = planes(n, np, true);
     }
     const size_t o_part = c.lay.take(part, 4);
-    if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay.bytes, &c.base)) return e;
+    if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return e;
     for (Planes *b : {&x, &t0, &t1, &s, &p, &t, &m0, &q}) {
         if (!b->ld) continue;
         b->hi = c.at<u16>((size_t)b->hi);

@@ -1,0 +1,121 @@
+"""The operators' host code (request tables, workspaces, plans and argument
+blocks) compiled for the CPU with AddressSanitizer and driven through calls
+of many shapes. Every launch checks that each range its kernel would read or
+write may be accessed: operands and results are allocated to their last
+element, and the pieces of a workspace have gaps between them that may not
+be touched. No GPU is needed."""
+
+import json
+import os
+import random
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+STUB = os.path.join(ROOT, "tests", "opstub")
+HOST = os.path.join(ROOT, "tests", "hoststub")
+LIB = os.path.join(ROOT, "_build", "libgemel_ops.so")
+CSRC = os.path.join(ROOT, "paper_2201_07705_amd", "csrc")
+
+
+@pytest.fixture(scope="module")
+def opslib():
+    os.makedirs(os.path.dirname(LIB), exist_ok=True)
+    tmp = f"{LIB}.{os.getpid()}"
+    subprocess.check_call(
+        ["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address", "-fno-omit-frame-pointer",
+         "-fPIC", "-shared", f"-I{STUB}", f"-I{HOST}", f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}"]
+        + [os.path.join(CSRC, f"{f}.cpp") for f in ("registry", "plan", "batching", "operators", "op_plan")]
+        + [os.path.join(HOST, "hoststub.cpp"), os.path.join(STUB, "opstub.cpp"), "-o", tmp])
+    os.replace(tmp, LIB)
+    return LIB
+
+
+def drive(lib, calls):
+    asan = subprocess.check_output(["gcc", "-print-file-name=libasan.so"], text=True).strip()
+    env = dict(os.environ, LD_PRELOAD=asan, ASAN_OPTIONS="detect_leaks=0:allocator_may_return_null=1")
+    r = subprocess.run(["python", os.path.join(STUB, "drive.py"), lib, json.dumps(calls)],
+                       capture_output=True, text=True, env=env, timeout=600)
+    assert r.returncode == 0, r.stderr[-3000:]
+    return json.loads(r.stdout.strip().splitlines()[-1])
+
+
+def sound(lib, calls):
+    out = drive(lib, calls)
+    assert len(out["calls"]) == len(calls)
+    for c, o in zip(calls, out["calls"]):
+        assert o["status"] == 0, (c, o)
+    assert sum(o["launches"] for o in out["calls"]) > len(calls)
+    assert out["violations"] == 0, out["last"]
+
+
+def _log(rng, lo, hi):
+    import math
+    return max(lo, min(hi, round(math.exp(rng.uniform(math.log(lo), math.log(hi))))))
+
+
+def projection(rng, op, rows):
+    bank, rank = _log(rng, 1, 12), _log(rng, 1, 256)
+    n = rng.randint(1, min(rows, 9))
+    cuts = sorted(rng.randint(0, rows) for _ in range(n - 1))
+    n_rows = [b - a for a, b in zip([0] + cuts, cuts + [rows])]
+    c = {"op": op, "dtype": rng.choice(["bf16", "f32"]), "n_rows": n_rows,
+         "ids": [rng.randint(-1, bank - 1) for _ in n_rows], "bank": bank, "rank": rank,
+         "ranks": [rng.randint(1, rank) for _ in range(bank)],
+         "k": _log(rng, 1, 5000), "n": _log(rng, 1, 3000)}
+    if rng.random() < .5:
+        c["k"], c["n"] = 8 * ((c["k"] + 7) // 8), 8 * ((c["n"] + 7) // 8)
+    if rng.random() < .4:
+        c.update(pad=rng.randint(1, 9), shift=rng.randint(0, 3))
+    if op == "adapt_backward" and rng.random() < .4:
+        c["needs"] = [q for q in ("x", "weight", "bias", "a", "b") if rng.random() < .5] or ["x"]
+    return c
+
+
+@pytest.mark.parametrize("seed", range(6))
+def test_projections_stay_in_their_memory(opslib, seed):
+    rng = random.Random(seed)
+    calls = []
+    for op in ("adapt", "adapt_backward"):
+        for _ in range(25):
+            calls.append(projection(rng, op, _log(rng, 1, 64)))
+            calls.append(projection(rng, op, _log(rng, 65, 3000)))
+    sound(opslib, calls)
+
+
+def test_workspaces_of_small_calls_after_large_ones(opslib):
+    """The same workspace, laid out anew by every call."""
+    one = {"op": "adapt_backward", "dtype": "f32", "n_rows": [1200, 7], "ids": [0, 1], "bank": 2, "rank": 40,
+           "k": 1030, "n": 520}
+    calls = []
+    for rows in ([1200, 7], [3], [70], [0], [64], [65]):
+        for dtype in ("f32", "bf16"):
+            for op in ("adapt", "adapt_backward"):
+                calls.append(dict(one, op=op, dtype=dtype, n_rows=rows, ids=[0, 1][:len(rows)]))
+                # thin products and sums in slices
+                calls.append(dict(one, op=op, dtype=dtype, n_rows=rows, ids=[0, 1][:len(rows)], k=20001, n=70))
+                calls.append(dict(one, op=op, dtype=dtype, n_rows=rows, ids=[0, 1][:len(rows)], k=70, n=20001))
+    sound(opslib, calls)
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_matrices_stay_in_their_memory(opslib, seed):
+    rng = random.Random(100 + seed)
+    calls = []
+    for op in ("orthogonalize", "muon"):
+        for dtype in ("bf16", "f32"):
+            for _ in range(12):
+                rows, cols = _log(rng, 1, 1500), _log(rng, 1, 1500)
+                calls.append({"op": op, "dtype": dtype, "count": _log(rng, 1, 6), "rows": rows, "cols": cols,
+                              "steps": rng.randint(1, 8)})
+            # steps in pairs, odd and even, and batches of several groups
+            calls += [{"op": op, "dtype": dtype, "count": 2, "rows": 512, "cols": 4608, "steps": s} for s in (2, 4, 5)]
+            calls.append({"op": op, "dtype": dtype, "count": 140, "rows": 1100, "cols": 1030, "steps": 2})
+    sound(opslib, calls)
+
+
+def test_the_check_itself(opslib):
+    """Operands that begin one element before their memory are found out."""
+    c = {"op": "adapt", "dtype": "bf16", "n_rows": [90], "ids": [0], "bank": 1, "rank": 8, "k": 64, "n": 72}
+    assert drive(opslib, [dict(c, shift=-1)])["violations"] > 0
