@@ -392,7 +392,7 @@ __device__ __forceinline__ uint4 finish(const MmArgs &a, const Tile &t, int m, i
 // 64 (2746 us). Below 512 tiles of 64 what a compute unit does alone counts:
 // 2048 x 1000 of 1024 pairs 22.4 us at T = 64, 33.2 at 128, 95.5 at 256.
 template <int T>
-constexpr int mm_threads() { return T == 64 ? 256 : 512; }
+constexpr int mm_threads() { return mm_threads_of(T); }
 
 template <int T, int STAGES, int PHASES, bool F16, bool PAIR, int EPI>
 __global__ __launch_bounds__((mm_threads<T>()), T == 256 ? 1 : T == 128 ? 4 : 2) void mm_kernel(const MmArgs a) {

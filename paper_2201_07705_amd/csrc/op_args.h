@@ -11,6 +11,9 @@ namespace gemel {
 
 typedef unsigned short u16;
 
+// Threads of a grid along one axis (the runtime's limit).
+constexpr int64_t MAX_THREADS = 0xffffffffll;
+
 constexpr int64_t op_round_up(int64_t x, int64_t m) { return (x + m - 1) / m * m; }
 
 // What a product does with its sums v (float32) of element (m, n).
@@ -101,6 +104,8 @@ constexpr int64_t MM_MAX_LD = 1 << 22;
 constexpr int MM_BK = 64;   // depth of a step: a 128-byte line of each row
 double mm_plan(MmArgs &a);   // tile, splits, steps, ldp of a shape; the microseconds expected
 int64_t mm_tiles(const MmArgs &a, int T);   // T x T tiles of a result (32: the sum of splits)
+constexpr int mm_threads_of(int tile) { return tile == 64 ? 256 : 512; }
+bool mm_fits(const MmArgs &a);    // the sizes of a planned product, before it has operands
 bool mm_valid(const MmArgs &a);
 hipError_t launch_mm(const MmArgs &a, hipStream_t s);
 

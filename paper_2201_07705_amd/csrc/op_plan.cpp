@@ -2,7 +2,6 @@
 // slices from the sizes, and whether an argument block is one that its kernel
 // and grid can take. Plain host code, which CPU builds share.
 #include <algorithm>
-#include <climits>
 
 #include "op_args.h"
 
@@ -37,8 +36,9 @@ double mm_plan(MmArgs &a) {
     const Form *const forms = a.pair ? pair : single;
     const int steps = (a.K + MM_BK - 1) / MM_BK;
     double best = 1e30;
-    for (int i = 0; i < 3; ++i) {
+    for (int i = 0; i < 3; ++i) {   // (the 256 form first: there is always one)
         const Form &f = forms[i];
+        if (f.tile < 256 && mm_tiles(a, f.tile) * mm_threads_of(f.tile) > MAX_THREADS) continue;
         const int64_t tiles = mm_tiles(a, f.tile) * a.batch;
         for (int want = 1; want <= 32 && want <= std::max(1, steps / 4); ++want) {
             const int per = (steps + want - 1) / want, splits = (steps + per - 1) / per;
@@ -62,10 +62,15 @@ double mm_plan(MmArgs &a) {
     return best;
 }
 
+bool mm_fits(const MmArgs &a) {
+    return a.M > 0 && a.N > 0 && a.K > 0 && a.K <= MM_MAX_LD && a.batch > 0 && a.batch <= 65535 &&
+           mm_tiles(a, a.tile) * mm_threads_of(a.tile) <= MAX_THREADS &&
+           (a.splits <= 1 || mm_tiles(a, 32) * 256 <= MAX_THREADS);
+}
+
 bool mm_valid(const MmArgs &a) {
     const int nk = (a.K + MM_BK - 1) / MM_BK;
-    if (a.M <= 0 || a.N <= 0 || a.K <= 0 || a.K % 8 || a.batch <= 0 || a.batch > 65535 ||
-        a.lda % 8 || a.ldb % 8 || a.lda > MM_MAX_LD || a.ldb > MM_MAX_LD ||
+    if (a.K % 8 || a.lda % 8 || a.ldb % 8 || a.lda > MM_MAX_LD || a.ldb > MM_MAX_LD ||
         (a.perm && a.perm_rows * a.lda > (1ll << 30)) || (a.tile != 64 && a.tile != 128 && a.tile != 256) || a.za % 8 ||
         a.zb % 8 || a.lda < a.K || a.ldb < a.K || !a.zero || a.splits < 1 || a.steps < 1 ||
         a.ext % MM_BK || (int64_t)a.splits * a.steps < nk || (int64_t)(a.splits - 1) * a.steps >= nk)
@@ -80,8 +85,7 @@ bool mm_valid(const MmArgs &a) {
                                                 a.o.ldbx % 4 || a.o.ldbx < a.N))))
         return false;
     if (a.epi != EPI_ROWS && (a.K % MM_BK || a.ext)) return false;
-    if ((int64_t)((a.M + 63) / 64) * ((a.N + 63) / 64) > INT32_MAX / 256) return false;
-    return true;
+    return mm_fits(a);
 }
 
 // Slices of the depth: as many workgroups as run at once (three on a compute
@@ -156,7 +160,7 @@ bool add_outer(Outers &o, const OuterArgs &a) {
         return false;
     const int cols = a.q_f32 ? 128 : 256;
     const int64_t blocks = (int64_t)((a.C + cols - 1) / cols) * ((a.R + 31) / 32) * a.n_chunks;
-    if (blocks + o.blocks > 0x7fffff00) return false;
+    if ((blocks + o.blocks) * 256 > MAX_THREADS) return false;
     o.a[o.n] = a;
     o.first[o.n] = o.blocks;
     o.blocks += (int)blocks;
@@ -214,7 +218,7 @@ bool add_job(Jobs &all, const Job &in) {
             break;
         default: ok = false;
     }
-    if (!ok || blocks < 1 || blocks + all.blocks > 0x7fffff00) return false;
+    if (!ok || blocks < 1 || (blocks + all.blocks) * 256 > MAX_THREADS) return false;
     j.blocks = (int)blocks;
     all.first[all.n] = all.blocks;
     all.blocks += j.blocks;

@@ -671,6 +671,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     const size_t o_t = c.lay.take(b.runs ? (int64_t)b.rows * rp : 0, 4),
                  o_tp = c.lay.take(b.runs ? part_floats(t) : 0, 4);
     const size_t o_part = c.lay.take(plan_adapted(c, b, f32, p), 4);
+    if (!mm_fits(p.mm)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
     if (gemel_status s = workspace(ctx, *st, stream, c.lay, &c.base)) return s;
     Jobs first, second;
     if (!add_adapted(c, b, f32, p, first, second)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
@@ -728,15 +729,14 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     if (!dx && !dw && !dbias && !da && !db) return GEMEL_OK;
     DeviceScope scope(ctx->device);
     Call c{ctx, st, stream, {}, nullptr};
-    if (M == 0 || b.runs == 0) {
+    if (M == 0) {
         if (gemel_status s = zero_out(c, da, bank * K)) return s;
         if (gemel_status s = zero_out(c, db, bank * N)) return s;
-        da = db = nullptr;
-    }
-    if (M == 0) {
         if (gemel_status s = zero_out(c, dw, N * K)) return s;
         return zero_out(c, dbias, N);
     }
+    float *const no_da = b.runs ? nullptr : da, *const no_db = b.runs ? nullptr : db;   // zeros
+    if (!b.runs) da = db = nullptr;
     const int rp = (int)op_round_up(b.rank, 32);
     const int64_t Np = op_round_up(N, 64);
     const bool need_u = b.runs && (dx || da), need_t = b.runs && db;
@@ -749,8 +749,11 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // where the transposed pairs of x and the maxima for them would cost more
     // than the product (16384 x 4096, 10 outputs 298 -> 64 us, 64 303 -> 114;
     // 4096 x 512, 64 29 -> 18; at 100 outputs 512 x 4096 takes 26, not 23).
-    // bf16 copies are cheap, and the tiles faster: 64 outputs 87 us, not 113
-    const bool narrow = dw && !few && f32 && N <= NARROW, tiled = dw && !few && !narrow;
+    // bf16 copies are cheap, and the tiles faster: 64 outputs 87 us, not 113.
+    // So are dW of more than 2^21 float32 rows, whose transposed pairs would
+    // be longer than a product's rows can be
+    const bool narrow = dw && !few && f32 && (N <= NARROW || 2 * op_round_up(M, 64) > MM_MAX_LD),
+               tiled = dw && !few && !narrow;
     // U = scale dy B and T = scale x A^T
     ShrinkArgs thin[2];
     const int n_thin = need_u + need_t;
@@ -791,6 +794,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         p.out = dx;
         p.ld_out = lddx;
         part = plan_adapted(c, b, f32, p);
+        if (!mm_fits(p.mm)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
     }
     // dW = dy^T x, on transposed copies of both
     MmArgs w{};
@@ -821,6 +825,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         w.pair = f32;
         w.epi = f32 ? EPI_SCALED : EPI_ROWS;
         mm_plan(w);
+        if (!mm_fits(w)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
         c_dy = plan_copy(c, N, M, f32, true);
         c_x = plan_copy(c, K, M, f32, true);
         part = std::max(part, partial_floats(w));
@@ -951,6 +956,8 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     }
     if (!ok) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
 
+    if (gemel_status s = zero_out(c, no_da, bank * K)) return s;
+    if (gemel_status s = zero_out(c, no_db, bank * N)) return s;
     OPCHK(launch_jobs(first, stream), "column maxima");
     OPCHK(launch_jobs(second, stream), "copies");
     for (int i = 0; i < n_thin; ++i) thin[i].part = c.at<float>(o_thin[i]);
@@ -1073,6 +1080,8 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
         q = planes(n, np, true);
     }
     const size_t o_part = c.lay.take(part, 4);
+    for (const MmArgs *a : {&gram, &poly, &next, &last})
+        if (!mm_fits(*a)) return fail(ctx, GEMEL_EINVAL, "the matrices are too large");
     if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return e;
     for (Planes *b : {&x, &t0, &t1, &s, &p, &t, &m0, &q}) {
         if (!b->ld) continue;

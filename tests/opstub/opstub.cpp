@@ -315,3 +315,19 @@ hipError_t launch_thin_apply(const OrthArgs &a, hipStream_t) {
 }
 
 }  // namespace gemel
+
+extern "C" {
+// The grid (threads across) that a product of this shape would be launched
+// with, and 0 where its plan does not fit one.
+long long opstub_product_threads(int m, int n, int k, int batch, int pair, int sym) {
+    MmArgs a{};
+    a.M = m;
+    a.N = n;
+    a.K = k;
+    a.batch = batch;
+    a.pair = pair;
+    a.sym = sym;
+    mm_plan(a);
+    return mm_fits(a) ? mm_tiles(a, a.tile) * mm_threads_of(a.tile) : 0;
+}
+}

@@ -119,3 +119,28 @@ def test_the_check_itself(opslib):
     """Operands that begin one element before their memory are found out."""
     c = {"op": "adapt", "dtype": "bf16", "n_rows": [90], "ids": [0], "bank": 1, "rank": 8, "k": 64, "n": 72}
     assert drive(opslib, [dict(c, shift=-1)])["violations"] > 0
+
+
+def test_long_batches_of_float32(opslib):
+    """Rows beyond those that a transposed copy of pairs can hold, with few
+    and many outputs, and each gradient alone."""
+    rows = (1 << 21) + 1
+    c = {"op": "adapt_backward", "dtype": "f32", "n_rows": [rows - 5, 5], "ids": [0, 1], "bank": 2, "rank": 2,
+         "k": 4, "n": 65}
+    sound(opslib, [c, dict(c, needs=["weight"]), dict(c, k=130, n=3, needs=["weight", "bias"]),
+                   dict(c, dtype="bf16", needs=["weight"]), dict(c, op="adapt")])
+
+
+def test_products_of_any_size_have_a_grid(opslib):
+    """The largest batches with thousands of outputs, and every other shape
+    that memory could hold, fit the 2^32 threads of a grid."""
+    code = ("import ctypes, json, sys; L = ctypes.CDLL(sys.argv[1]); f = L.opstub_product_threads; "
+            "f.restype = ctypes.c_longlong; print(json.dumps([f(*c) for c in json.loads(sys.argv[2])]))")
+    shapes = [[1 << 22, 8256, 8, 1, 0, 0], [1 << 22, 16500, 4096, 1, 0, 0], [1 << 22, 33000, 64, 1, 1, 0],
+              [1 << 20, 130000, 64, 1, 0, 0], [1 << 22, 1, 8, 1, 0, 0], [64, 1 << 20, 1 << 20, 1, 0, 0],
+              [65, 1 << 20, 64, 1, 0, 0], [90000, 90000, 90112, 1, 0, 1], [4096, 25088, 8192, 1, 1, 0]]
+    asan = subprocess.check_output(["gcc", "-print-file-name=libasan.so"], text=True).strip()
+    r = subprocess.run(["python", "-c", code, opslib, json.dumps(shapes)], capture_output=True, text=True,
+                       env=dict(os.environ, LD_PRELOAD=asan, ASAN_OPTIONS="detect_leaks=0"))
+    threads = json.loads(r.stdout)
+    assert all(0 < t < 1 << 32 for t in threads), threads
