@@ -717,6 +717,9 @@ gemel_status gemel_profile(gemel_ctx *ctx, gemel_kernel_stat *stats,
  * The tables are on the device when the call returns (it waits for its own
  * copy, not for other work), so the batch serves calls on any stream, for
  * every projection that its requests go through. Not during capture.
+ * Tables given back are used again: once the work of their calls is over,
+ * or, where a call was captured into a graph, after a wait for the device
+ * (one for every 32 such batches).
  * *out_batch receives the batch's id.
  * Errors: EINVAL, ENOMEM, EDEVICE.
  */
@@ -727,8 +730,8 @@ gemel_status gemel_adapter_batch(gemel_ctx *ctx, const int32_t *adapter_ids,
                                  int32_t *out_batch);
 
 /* Give a batch's tables back. Work already enqueued with it still runs
- * (the memory is used again only after the device has been waited for);
- * graphs that hold its calls must not be replayed. Errors: EINVAL. */
+ * (the memory is used again only after that); graphs that hold its calls
+ * must not be replayed. Errors: EINVAL. */
 gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch);
 
 /*

@@ -57,6 +57,17 @@ struct Batch {
     BatchTables t{};
     void *dev = nullptr;
     size_t bytes = 0;
+    std::vector<hipStream_t> streams;   // that its calls ran on
+    bool captured = false;              // a graph may hold its addresses
+};
+
+// Tables given back that enqueued work may still read: until events, recorded
+// on the streams that their calls ran on, have passed.
+struct Retired {
+    void *dev;
+    size_t bytes;
+    std::vector<hipStream_t> streams;   // without an event yet
+    std::vector<hipEvent_t> events;
 };
 
 // A stretch of device memory that the kernels of one stream share.
@@ -75,8 +86,11 @@ struct State : OperatorState {
     std::map<hipStream_t, Workspace> ws;
     std::vector<char *> captured;   // outgrown workspaces that graphs may use
     std::vector<std::unique_ptr<Batch>> batches;
-    // tables given back: `retired` ones may still be read by enqueued work
-    std::vector<std::pair<void *, size_t>> spare, retired;
+    // tables given back: nobody reads `spare` ones; replays enqueued on unknown
+    // streams may still read `held` ones
+    std::vector<std::pair<void *, size_t>> spare, held;
+    std::vector<Retired> retired;
+    std::vector<hipEvent_t> events;   // not in use
 
     explicit State(int d) : device(d) {}
     bool release() override {
@@ -87,8 +101,13 @@ struct State : OperatorState {
         for (char *p : captured) (void)hipFree(p);
         for (auto &b : batches)
             if (b && b->dev) (void)hipFree(b->dev);
-        for (auto *v : {&spare, &retired})
+        for (auto *v : {&spare, &held})
             for (auto &b : *v) (void)hipFree(b.first);
+        for (auto &r : retired) {
+            (void)hipFree(r.dev);
+            for (hipEvent_t e : r.events) (void)hipEventDestroy(e);
+        }
+        for (hipEvent_t e : events) (void)hipEventDestroy(e);
         if (zero) (void)hipFree(zero);
         if (pinned) (void)hipHostFree(pinned);
         if (side) (void)hipStreamDestroy(side);
@@ -96,7 +115,9 @@ struct State : OperatorState {
         captured.clear();
         batches.clear();
         spare.clear();
+        held.clear();
         retired.clear();
+        events.clear();
         zero = pinned = nullptr;
         side = nullptr;
         return ok;
@@ -153,7 +174,9 @@ struct Layout {
 #endif
 };
 
-gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layout &lay, char **out) {
+// The call's pieces of its stream's workspace; `batch` (or null) is noted as
+// used on the stream.
+gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layout &lay, Batch *batch, char **out) {
     Workspace &w = st.ws[stream];
     size_t bytes = lay.bytes;
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
@@ -176,6 +199,10 @@ gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layo
         w.bytes = bytes;
     }
     if (cs != hipStreamCaptureStatusNone) w.captured = true;
+    if (batch && cs != hipStreamCaptureStatusNone)
+        batch->captured = true;
+    else if (batch && std::find(batch->streams.begin(), batch->streams.end(), stream) == batch->streams.end())
+        batch->streams.push_back(stream);
     lay.fence(w.p, w.bytes);
     *out = w.p;
     return GEMEL_OK;
@@ -201,6 +228,49 @@ gemel_status apart(gemel_ctx *ctx, const std::vector<Range> &r) {
     return GEMEL_OK;
 }
 
+// Makes tables whose calls are over spare. A stream that cannot be asked (it
+// was destroyed) leaves them to the next wait for the device.
+void reclaim(State &st) {
+    constexpr int LOOK = 8;   // unfinished ones that are asked for in a call
+    int busy = 0;
+    for (size_t i = 0; i < st.retired.size();) {
+        Retired &r = st.retired[i];
+        bool lost = false, done = true;
+        r.events.reserve(r.events.size() + r.streams.size());
+        st.events.reserve(st.events.size() + r.events.size() + r.streams.size() + 1);
+        while (!lost && !r.streams.empty()) {
+            hipEvent_t e = nullptr;
+            if (st.events.empty()) {
+                lost = hipEventCreateWithFlags(&e, hipEventDisableTiming) != hipSuccess;
+            } else {
+                e = st.events.back();
+                st.events.pop_back();
+            }
+            if (!lost && hipEventRecord(e, r.streams.back()) != hipSuccess) {
+                st.events.push_back(e);
+                lost = true;
+            }
+            if (lost) break;
+            r.events.push_back(e);
+            r.streams.pop_back();
+        }
+        for (size_t k = 0; !lost && done && busy < LOOK && k < r.events.size(); ++k) {
+            const hipError_t q = hipEventQuery(r.events[k]);
+            done = q == hipSuccess;
+            lost = !done && q != hipErrorNotReady;
+        }
+        if (lost) (void)hipGetLastError();
+        if (!lost && (!done || busy >= LOOK)) {
+            ++busy;
+            ++i;
+            continue;
+        }
+        (lost ? st.held : st.spare).push_back({r.dev, r.bytes});
+        st.events.insert(st.events.end(), r.events.begin(), r.events.end());
+        st.retired.erase(st.retired.begin() + (std::ptrdiff_t)i);
+    }
+}
+
 gemel_status upload(gemel_ctx *ctx, State &st, const std::vector<int32_t> &words, Batch &b) {
     size_t want = 64 << 10;
     while (want < words.size() * 4) want *= 2;
@@ -210,10 +280,14 @@ gemel_status upload(gemel_ctx *ctx, State &st, const std::vector<int32_t> &words
         return -1;
     };
     int at = fits();
-    if (at < 0 && st.retired.size() >= 32) {
+    if (at < 0) {
+        reclaim(st);
+        at = fits();
+    }
+    if (at < 0 && st.held.size() >= 32) {
         OPCHK(hipDeviceSynchronize(), "hipDeviceSynchronize");
-        st.spare.insert(st.spare.end(), st.retired.begin(), st.retired.end());
-        st.retired.clear();
+        st.spare.insert(st.spare.end(), st.held.begin(), st.held.end());
+        st.held.clear();
         at = fits();
     }
     if (at >= 0) {
@@ -319,7 +393,10 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
     size_t id = 0;
     while (id < st->batches.size() && st->batches[id]) ++id;
     if (id == st->batches.size()) st->batches.emplace_back();
+    // (giving back allocates nothing)
     st->retired.reserve(st->retired.size() + st->batches.size());
+    st->spare.reserve(st->spare.size() + st->batches.size());
+    st->held.reserve(st->held.size() + st->batches.size());
     if (gemel_status s = upload(ctx, *st, words, *b)) return s;
     const int *d = (const int *)b->dev;
     BatchTables &t = b->t;
@@ -361,6 +438,7 @@ struct Call {
     gemel_ctx *ctx;
     State *st;
     hipStream_t stream;
+    Batch *batch;
     Layout lay;
     char *base = nullptr;
     template <typename T>
@@ -368,6 +446,7 @@ struct Call {
         return (T *)(base + off);
     }
 };
+gemel_status workspace(Call &c) { return workspace(c.ctx, *c.st, c.stream, c.lay, c.batch, &c.base); }
 
 gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_projection *p) {
     if (!p) return fail(ctx, GEMEL_EINVAL, "proj is null");
@@ -599,7 +678,7 @@ gemel_status adapt_rows(Call &c, const BatchTables &b, bool f32, const gemel_pro
     const size_t o_x = c.lay.take(copy_x ? b.rows * Kp : 0, e), o_w = c.lay.take(copy_w ? N * Kp : 0, e),
                  o_p = c.lay.take((int64_t)a.slices * b.rows * a.ldp, 4),
                  o_t = c.lay.take(a.thin_blocks ? (int64_t)a.thin_slices * b.rows * a.rank_blocks * 16 : 0, 4);
-    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return s;
+    if (gemel_status s = workspace(c)) return s;
     a.x = x;
     a.ldx = ldx;
     a.w = proj->weight;
@@ -651,7 +730,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
                                      range("b", proj->b, bank * N * e, false)}))
         return s;
     DeviceScope scope(ctx->device);
-    Call c{ctx, st, stream, {}, nullptr};
+    Call c{ctx, st, stream, bt, {}, nullptr};
     if (b.rows <= ROWS_MAX) return adapt_rows(c, b, f32, proj, x, ldx, y, ldy);
     const int rp = (int)op_round_up(b.rank, 32);
     Adapted p{};
@@ -672,7 +751,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
                  o_tp = c.lay.take(b.runs ? part_floats(t) : 0, 4);
     const size_t o_part = c.lay.take(plan_adapted(c, b, f32, p), 4);
     if (!mm_fits(p.mm)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
-    if (gemel_status s = workspace(ctx, *st, stream, c.lay, &c.base)) return s;
+    if (gemel_status s = workspace(c)) return s;
     Jobs first, second;
     if (!add_adapted(c, b, f32, p, first, second)) return fail(ctx, GEMEL_EINVAL, "the projection is too large");
     OPCHK(launch_jobs(second, stream), "copies");
@@ -728,7 +807,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
         return s;
     if (!dx && !dw && !dbias && !da && !db) return GEMEL_OK;
     DeviceScope scope(ctx->device);
-    Call c{ctx, st, stream, {}, nullptr};
+    Call c{ctx, st, stream, bt, {}, nullptr};
     if (M == 0) {
         if (gemel_status s = zero_out(c, da, bank * K)) return s;
         if (gemel_status s = zero_out(c, db, bank * N)) return s;
@@ -841,7 +920,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     };
     const size_t o_da = c.lay.take(da ? (int64_t)b.n_chunks * pieces(K) * rp * K : 0, 4),
                  o_db = c.lay.take(db ? (int64_t)b.n_chunks * pieces(N) * rp * N : 0, 4), o_part = c.lay.take(part, 4);
-    if (gemel_status s = workspace(ctx, *st, stream, c.lay, &c.base)) return s;
+    if (gemel_status s = workspace(c)) return s;
 
     Jobs first, second, last;
     Outers outers;
@@ -997,7 +1076,7 @@ gemel_status orthogonal_thin(Call &c, OrthArgs o) {
     o.parts = (int)std::max<int64_t>(1, std::min<int64_t>({(m + 63) / 64, 64, (1024 + o.count - 1) / o.count}));
     const size_t og = c.lay.take((int64_t)o.count * o.parts * np * np, 8), oq = c.lay.take((int64_t)o.count * np * np, 4),
                  oe = c.lay.take(o.count, 4);
-    if (gemel_status s = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return s;
+    if (gemel_status s = workspace(c)) return s;
     o.gram = c.at<double>(og);
     o.q = c.at<float>(oq);
     o.e = c.at<int>(oe);
@@ -1082,7 +1161,7 @@ gemel_status orthogonal(Call &c, OrthArgs o) {
     const size_t o_part = c.lay.take(part, 4);
     for (const MmArgs *a : {&gram, &poly, &next, &last})
         if (!mm_fits(*a)) return fail(ctx, GEMEL_EINVAL, "the matrices are too large");
-    if (gemel_status e = workspace(ctx, *c.st, c.stream, c.lay, &c.base)) return e;
+    if (gemel_status e = workspace(c)) return e;
     for (Planes *b : {&x, &t0, &t1, &s, &p, &t, &m0, &q}) {
         if (!b->ld) continue;
         b->hi = c.at<u16>((size_t)b->hi);
@@ -1259,7 +1338,12 @@ gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch) {
         State *st;
         Batch *b;
         if (gemel_status s = get_batch(ctx, batch, &st, &b)) return s;
-        st->retired.push_back({b->dev, b->bytes});
+        if (b->captured)
+            st->held.push_back({b->dev, b->bytes});
+        else if (b->streams.empty())
+            st->spare.push_back({b->dev, b->bytes});
+        else
+            st->retired.push_back({b->dev, b->bytes, std::move(b->streams), {}});
         st->batches[(size_t)batch].reset();
         return GEMEL_OK;
     });
@@ -1294,7 +1378,7 @@ gemel_status gemel_orthogonalize(gemel_ctx *ctx, int32_t count, int32_t rows, in
         DeviceScope scope(ctx->device);
         State *st;
         if (gemel_status s = ready(ctx, &st)) return s;
-        Call c{ctx, st, (hipStream_t)hip_stream, {}, nullptr};
+        Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
         OrthArgs o{};
         o.g = g;
         o.f32 = ctx->dtype == GEMEL_F32;
@@ -1329,7 +1413,7 @@ gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows, int32_
         DeviceScope scope(ctx->device);
         State *st;
         if (gemel_status s = ready(ctx, &st)) return s;
-        Call c{ctx, st, (hipStream_t)hip_stream, {}, nullptr};
+        Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
         OrthArgs o{};
         o.g = g;
         o.m = momentum;

@@ -26,6 +26,7 @@ class Driver:
         L.hoststub_violations.restype = ctypes.c_long
         L.hoststub_set_capturing.argtypes = [ctypes.c_void_p]
         L.opstub_last.restype = ctypes.c_char_p
+        L.opstub_device_waits.restype = L.hoststub_allocs.restype = ctypes.c_long
         self.ctx = {}
         for dtype, code in (("f32", G.F32), ("bf16", G.BF16)):
             h = ctypes.c_void_p()
@@ -97,7 +98,41 @@ class Driver:
                                    c.get("steps", 5), None)
         return st, L.gemel_last_error(ctx)
 
+    def rounds(self, c):
+        """A server's rounds: each makes a batch, uses it on one of the
+        streams and gives it back, while events answer c["answer"]. The waits
+        for the device and the memory that only the batches took."""
+        L, ctx, out = self.L, self.ctx["bf16"], I32(-1)
+        streams = [None]
+        for _ in range(c["streams"] - 1):
+            s = ctypes.c_void_p()
+            assert L.hipStreamCreateWithFlags(ctypes.byref(s), 1) == 0
+            streams.append(s)
+        k, n = 16, 24
+        p = G.Projection(k, n, self.memory(n, k, k, 2), k, None, self.memory(8, k, k, 2), self.memory(n, 8, 8, 2))
+        x, y = self.memory(4, k, k, 2), self.memory(4, n, n, 2)
+        res = []
+        for answer in c["answers"]:
+            L.opstub_events_answer(answer)
+            waits, allocs = L.opstub_device_waits(), L.hoststub_allocs()
+            for i in range(c["rounds"]):
+                assert L.gemel_adapter_batch(ctx, (I32 * 1)(0), (I32 * 1)(4), 1, 1, 8, None, None,
+                                             ctypes.byref(out)) == G.OK
+                s = streams[i % len(streams)]
+                # (rounds of the first phase are not captured)
+                L.hoststub_set_capturing(s if c.get("capture") and res else None)
+                assert L.gemel_adapt(ctx, out.value, ctypes.byref(p), x, k, y, n, s) == G.OK
+                L.hoststub_set_capturing(None)
+                assert L.gemel_adapter_batch_free(ctx, out.value) == G.OK
+            res.append([L.opstub_device_waits() - waits, L.hoststub_allocs() - allocs])
+        L.opstub_events_answer(0)
+        return res
+
     def call(self, c):
+        if c["op"] == "rounds":
+            res = self.rounds(c)
+            self.drop()
+            return res
         ctx = self.ctx[c["dtype"]]
         before = self.L.opstub_launches()
         st, message = (self.projection if "k" in c else self.matrices)(c, ctx)

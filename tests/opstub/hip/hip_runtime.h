@@ -8,3 +8,9 @@
 struct int4 {
     int x, y, z, w;
 };
+
+// Waits for the device are counted, and events answer as the test says.
+#define hipErrorNotReady ((hipError_t)600)
+extern "C" hipError_t hipEventQuery(hipEvent_t e);
+extern "C" hipError_t opstub_device_synchronize();
+#define hipDeviceSynchronize opstub_device_synchronize

@@ -62,7 +62,19 @@ void touch_tables(const BatchTables &b) {
 }
 }  // namespace
 
+#undef hipDeviceSynchronize
+static long device_waits = 0;
+static hipError_t event_answer = hipSuccess;
+
 extern "C" {
+hipError_t hipEventQuery(hipEvent_t) { return event_answer; }
+hipError_t opstub_device_synchronize() {
+    ++device_waits;
+    return hipDeviceSynchronize();
+}
+long opstub_device_waits() { return device_waits; }
+// What every event answers from now on (0: passed, 600: not yet).
+void opstub_events_answer(int e) { event_answer = (hipError_t)e; }
 long opstub_violations() { return violations; }
 long opstub_launches() { return launches; }
 const char *opstub_last() { return last.c_str(); }
