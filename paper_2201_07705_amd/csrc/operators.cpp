@@ -208,22 +208,35 @@ gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layo
     return GEMEL_OK;
 }
 
-// Ranges of device memory that a call reads or writes.
+// Rows of device memory that a call reads or writes.
 struct Range {
     const char *what;
-    uintptr_t lo, hi;
+    uintptr_t lo, hi;        // from the first row to the end of the last
+    uintptr_t stride, width; // bytes (stride 0: one stretch)
     bool out;
 };
 Range range(const char *what, const void *p, int64_t bytes, bool out) {
-    return {what, (uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)bytes : 0), out};
+    return {what, (uintptr_t)p, (uintptr_t)p + (p ? (uintptr_t)bytes : 0), 0, 0, out};
 }
-int64_t span(int64_t rows, int64_t cols, int64_t stride, int64_t elem) {
-    return rows > 0 ? ((rows - 1) * stride + cols) * elem : 0;
+Range range(const char *what, const void *p, int64_t rows, int64_t cols, int64_t stride, int64_t elem, bool out) {
+    Range r = range(what, p, rows > 0 ? ((rows - 1) * stride + cols) * elem : 0, out);
+    r.stride = (uintptr_t)(stride * elem);
+    r.width = (uintptr_t)(cols * elem);
+    return r;
+}
+// Whether the rows of two ranges share bytes. Rows of one stride may lie side
+// by side, as columns of one wider matrix; of different strides their whole
+// spans count.
+bool overlap(const Range &a, const Range &b) {
+    if (a.lo >= b.hi || b.lo >= a.hi) return false;
+    if (!a.stride || a.stride != b.stride) return true;
+    const uintptr_t d = b.lo >= a.lo ? (b.lo - a.lo) % a.stride : (a.stride - (a.lo - b.lo) % a.stride) % a.stride;
+    return d < a.width || d + b.width > a.stride;
 }
 gemel_status apart(gemel_ctx *ctx, const std::vector<Range> &r) {
     for (size_t i = 0; i < r.size(); ++i)
         for (size_t j = 0; j < r.size(); ++j)
-            if (r[i].out && i != j && r[i].lo < r[j].hi && r[j].lo < r[i].hi)
+            if (r[i].out && i != j && overlap(r[i], r[j]))
                 return fail(ctx, GEMEL_EINVAL, std::string(r[i].what) + " overlaps " + r[j].what);
     return GEMEL_OK;
 }
@@ -723,9 +736,9 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     if (gemel_status s = check_rows(ctx, "x", x, ldx, K, e)) return s;
     if (gemel_status s = check_rows(ctx, "y", y, ldy, N, e)) return s;
     if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
-    if (gemel_status s = apart(ctx, {range("y", y, span(b.rows, N, ldy, e), true),
-                                     range("x", x, span(b.rows, K, ldx, e), false),
-                                     range("weight", proj->weight, span(N, K, proj->weight_stride, e), false),
+    if (gemel_status s = apart(ctx, {range("y", y, b.rows, N, ldy, e, true),
+                                     range("x", x, b.rows, K, ldx, e, false),
+                                     range("weight", proj->weight, N, K, proj->weight_stride, e, false),
                                      range("bias", proj->bias, N * 4, false), range("a", proj->a, bank * K * e, false),
                                      range("b", proj->b, bank * N * e, false)}))
         return s;
@@ -798,11 +811,11 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
             if (gemel_status s = check_rows(ctx, "dx", dx, lddx, K, e)) return s;
         if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
     }
-    if (gemel_status s = apart(ctx, {range("dx", dx, span(M, K, lddx, e), true), range("dweight", dw, N * K * 4, true),
+    if (gemel_status s = apart(ctx, {range("dx", dx, M, K, lddx, e, true), range("dweight", dw, N * K * 4, true),
                                      range("dbias", dbias, N * 4, true), range("da", da, bank * K * 4, true),
-                                     range("db", db, bank * N * 4, true), range("x", x, span(M, K, ldx, e), false),
-                                     range("dy", dy, span(M, N, lddy, e), false),
-                                     range("weight", proj->weight, span(N, K, proj->weight_stride, e), false),
+                                     range("db", db, bank * N * 4, true), range("x", x, M, K, ldx, e, false),
+                                     range("dy", dy, M, N, lddy, e, false),
+                                     range("weight", proj->weight, N, K, proj->weight_stride, e, false),
                                      range("a", proj->a, bank * K * e, false), range("b", proj->b, bank * N * e, false)}))
         return s;
     if (!dx && !dw && !dbias && !da && !db) return GEMEL_OK;

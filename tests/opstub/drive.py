@@ -66,8 +66,11 @@ class Driver:
                          self.memory(bank * n, rank, rank, e))
         x = self.memory(rows, k, k + pad, e, shift)
         if c["op"] == "adapt":
-            st = L.gemel_adapt(ctx, out.value, ctypes.byref(p), x, k + pad,
-                               self.memory(rows, n, n + pad, e, shift), n + pad, None)
+            if "beside" in c:   # y: columns of the matrix that x lies in
+                y, ldy = x + c["beside"] * e, k + pad + c.get("skew", 0)
+            else:
+                y, ldy = self.memory(rows, n, n + pad, e, shift), n + pad
+            st = L.gemel_adapt(ctx, out.value, ctypes.byref(p), x, k + pad, y, ldy, None)
         else:
             needs = c.get("needs", ["x", "weight", "bias", "a", "b"])
             shapes = {"weight": (n, k), "bias": (1, n), "a": (bank * rank, k),

@@ -161,3 +161,17 @@ def test_batches_given_back_wait_for_nothing(opslib):
     assert lost[0] == 3 and lost[1] <= 40
     (_, graph), = drive(opslib, [dict(rounds, streams=2, answers=[0, 0], rounds=130, capture=1)])["calls"]
     assert 1 <= graph[0] <= 2
+
+
+def test_columns_of_one_matrix_are_apart(opslib):
+    """x and y side by side in one matrix, in either order; refused where any
+    byte is shared."""
+    c = {"op": "adapt", "dtype": "bf16", "n_rows": [70], "ids": [0], "bank": 1, "rank": 4, "k": 24, "n": 16}
+    good = [dict(c, pad=16, beside=24), dict(c, pad=40, beside=30), dict(c, pad=40, beside=48),
+            dict(c, pad=40, beside=24 - 64 + 24), dict(c, pad=16, beside=-16), dict(c, n_rows=[1], beside=24)]
+    bad = [dict(c, pad=16, beside=b) for b in (23, 25, 0, -1, -15, -17, 40, 63)] + [dict(c, pad=16, beside=24, skew=1)]
+    out = drive(opslib, good + bad)["calls"]
+    for q, o in zip(good, out):
+        assert o["status"] == 0, (q, o)
+    for q, o in zip(bad, out[len(good):]):
+        assert o["status"] == -1 and "y overlaps x" in o["message"] and o["launches"] == 0, (q, o)
