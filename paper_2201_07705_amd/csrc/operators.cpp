@@ -461,6 +461,10 @@ struct Call {
 };
 gemel_status workspace(Call &c) { return workspace(c.ctx, *c.st, c.stream, c.lay, c.batch, &c.base); }
 
+gemel_status check_aligned(gemel_ctx *ctx, const char *what, const void *p, int64_t elem) {
+    if ((uintptr_t)p % (uintptr_t)elem) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is not aligned to its type");
+    return GEMEL_OK;
+}
 gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_projection *p) {
     if (!p) return fail(ctx, GEMEL_EINVAL, "proj is null");
     if (p->n_in < 1 || p->n_out < 1 || p->n_in > MAX_DIM || p->n_out > MAX_DIM)
@@ -468,13 +472,15 @@ gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_
     if (!p->weight) return fail(ctx, GEMEL_EINVAL, "weight is null");
     if (p->weight_stride < p->n_in) return fail(ctx, GEMEL_EINVAL, "weight_stride is smaller than n_in");
     if (t.runs > 0 && (!p->a || !p->b)) return fail(ctx, GEMEL_EINVAL, "the batch uses adapters: a and b must be given");
-    return GEMEL_OK;
+    const int64_t e = ctx->dtype == GEMEL_F32 ? 4 : 2;
+    if (gemel_status s = check_aligned(ctx, "bias", p->bias, 4)) return s;
+    if (gemel_status s = check_aligned(ctx, "a", p->a, e)) return s;
+    return check_aligned(ctx, "b", p->b, e);
 }
 gemel_status check_rows(gemel_ctx *ctx, const char *what, const void *p, int64_t stride, int64_t cols, int64_t elem) {
     if (!p) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is null");
     if (stride < cols || stride > INT32_MAX) return fail(ctx, GEMEL_EINVAL, std::string(what) + " has a bad row stride");
-    if ((uintptr_t)p % (uintptr_t)elem) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is not aligned to its type");
-    return GEMEL_OK;
+    return check_aligned(ctx, what, p, elem);
 }
 
 // ---- jobs around the products ----
@@ -811,6 +817,8 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
             if (gemel_status s = check_rows(ctx, "dx", dx, lddx, K, e)) return s;
         if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
     }
+    for (const auto &g : {std::make_pair("dweight", dw), {"dbias", dbias}, {"da", da}, {"db", db}})
+        if (gemel_status s = check_aligned(ctx, g.first, g.second, 4)) return s;
     if (gemel_status s = apart(ctx, {range("dx", dx, M, K, lddx, e, true), range("dweight", dw, N * K * 4, true),
                                      range("dbias", dbias, N * 4, true), range("da", da, bank * K * 4, true),
                                      range("db", db, bank * N * 4, true), range("x", x, M, K, ldx, e, false),

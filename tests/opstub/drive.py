@@ -64,6 +64,8 @@ class Driver:
         p = G.Projection(k, n, w, k + pad, self.memory(1, n, n, 4),
                          self.memory(bank * rank, k, k, e),
                          self.memory(bank * n, rank, rank, e))
+        off = c.get("off", {})   # bytes that a pointer is moved by
+        p.bias, p.a, p.b = p.bias + off.get("bias", 0), p.a + off.get("a", 0), p.b + off.get("b", 0)
         x = self.memory(rows, k, k + pad, e, shift)
         if c["op"] == "adapt":
             if "beside" in c:   # y: columns of the matrix that x lies in
@@ -75,7 +77,7 @@ class Driver:
             needs = c.get("needs", ["x", "weight", "bias", "a", "b"])
             shapes = {"weight": (n, k), "bias": (1, n), "a": (bank * rank, k),
                       "b": (bank * n, rank)}
-            g = {name: self.memory(r, q, q, 4) if name in needs else None
+            g = {name: self.memory(r, q, q, 4) + off.get("d" + name, 0) if name in needs else None
                  for name, (r, q) in shapes.items()}
             dx = self.memory(rows, k, k + pad, e, shift) if "x" in needs else None
             st = L.gemel_adapt_backward(

@@ -175,3 +175,18 @@ def test_columns_of_one_matrix_are_apart(opslib):
         assert o["status"] == 0, (q, o)
     for q, o in zip(bad, out[len(good):]):
         assert o["status"] == -1 and "y overlaps x" in o["message"] and o["launches"] == 0, (q, o)
+
+
+def test_pointers_that_are_not_aligned_are_refused(opslib):
+    calls, names = [], []
+    for dtype, e in (("bf16", 2), ("f32", 4)):
+        c = {"op": "adapt_backward", "dtype": dtype, "n_rows": [70], "ids": [0], "bank": 1, "rank": 4, "k": 24, "n": 16}
+        for name, size in (("bias", 4), ("a", e), ("b", e), ("dweight", 4), ("dbias", 4), ("da", 4), ("db", 4)):
+            for by in range(1, size):
+                calls.append(dict(c, off={name: by}))
+                names.append(name)
+                if name in ("bias", "a", "b"):
+                    calls.append(dict(c, op="adapt", off={name: by}))
+                    names.append(name)
+    for c, name, o in zip(calls, names, drive(opslib, calls)["calls"]):
+        assert o["status"] == -1 and o["launches"] == 0 and o["message"] == f"{name} is not aligned to its type", (c, o)
