@@ -473,7 +473,6 @@ gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_
     if (p->weight_stride < p->n_in) return fail(ctx, GEMEL_EINVAL, "weight_stride is smaller than n_in");
     if (t.runs > 0 && (!p->a || !p->b)) return fail(ctx, GEMEL_EINVAL, "the batch uses adapters: a and b must be given");
     const int64_t e = ctx->dtype == GEMEL_F32 ? 4 : 2;
-    if (gemel_status s = check_aligned(ctx, "bias", p->bias, 4)) return s;
     if (gemel_status s = check_aligned(ctx, "a", p->a, e)) return s;
     return check_aligned(ctx, "b", p->b, e);
 }
@@ -742,6 +741,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     if (gemel_status s = check_rows(ctx, "x", x, ldx, K, e)) return s;
     if (gemel_status s = check_rows(ctx, "y", y, ldy, N, e)) return s;
     if (gemel_status s = check_rows(ctx, "weight", proj->weight, proj->weight_stride, K, e)) return s;
+    if (gemel_status s = check_aligned(ctx, "bias", proj->bias, 4)) return s;
     if (gemel_status s = apart(ctx, {range("y", y, b.rows, N, ldy, e, true),
                                      range("x", x, b.rows, K, ldx, e, false),
                                      range("weight", proj->weight, N, K, proj->weight_stride, e, false),
