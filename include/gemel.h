@@ -740,8 +740,9 @@ gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch);
  *  bias    float32 [n_out] or NULL.
  *  a, b    the bank: a [n_adapters][max_rank][n_in] and
  *          b [n_adapters][n_out][max_rank], contiguous; both may be NULL
- *          for a batch none of whose rows uses an adapter. One that holds
- *          values that are not finite spoils the rows of its own requests
+ *          for a batch none of whose rows uses an adapter, and where of
+ *          the gradients only dweight and dbias are asked for. One that
+ *          holds values that are not finite spoils the rows of its own requests
  *          (in bf16 contexts all of a row) and no others.
  */
 typedef struct gemel_projection {

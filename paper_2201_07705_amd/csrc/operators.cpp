@@ -465,13 +465,13 @@ gemel_status check_aligned(gemel_ctx *ctx, const char *what, const void *p, int6
     if ((uintptr_t)p % (uintptr_t)elem) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is not aligned to its type");
     return GEMEL_OK;
 }
-gemel_status check_projection(gemel_ctx *ctx, const BatchTables &t, const gemel_projection *p) {
+gemel_status check_projection(gemel_ctx *ctx, const gemel_projection *p, bool adapters) {
     if (!p) return fail(ctx, GEMEL_EINVAL, "proj is null");
     if (p->n_in < 1 || p->n_out < 1 || p->n_in > MAX_DIM || p->n_out > MAX_DIM)
         return fail(ctx, GEMEL_EINVAL, "n_in and n_out must be in 1.." + std::to_string(MAX_DIM));
     if (!p->weight) return fail(ctx, GEMEL_EINVAL, "weight is null");
     if (p->weight_stride < p->n_in) return fail(ctx, GEMEL_EINVAL, "weight_stride is smaller than n_in");
-    if (t.runs > 0 && (!p->a || !p->b)) return fail(ctx, GEMEL_EINVAL, "the batch uses adapters: a and b must be given");
+    if (adapters && (!p->a || !p->b)) return fail(ctx, GEMEL_EINVAL, "the batch uses adapters: a and b must be given");
     const int64_t e = ctx->dtype == GEMEL_F32 ? 4 : 2;
     if (gemel_status s = check_aligned(ctx, "a", p->a, e)) return s;
     return check_aligned(ctx, "b", p->b, e);
@@ -734,7 +734,7 @@ gemel_status adapt(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, con
     Batch *bt;
     if (gemel_status s = get_batch(ctx, id, &st, &bt)) return s;
     const BatchTables &b = bt->t;
-    if (gemel_status s = check_projection(ctx, b, proj)) return s;
+    if (gemel_status s = check_projection(ctx, proj, b.runs > 0)) return s;
     if (b.rows == 0) return GEMEL_OK;
     const bool f32 = ctx->dtype == GEMEL_F32;
     const int64_t e = f32 ? 4 : 2, K = proj->n_in, N = proj->n_out, bank = (int64_t)b.adapters * b.rank;
@@ -807,7 +807,7 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     Batch *bt;
     if (gemel_status s = get_batch(ctx, id, &st, &bt)) return s;
     const BatchTables &b = bt->t;
-    if (gemel_status s = check_projection(ctx, b, proj)) return s;
+    if (gemel_status s = check_projection(ctx, proj, b.runs > 0 && (dx || da || db))) return s;
     const bool f32 = ctx->dtype == GEMEL_F32;
     const int64_t e = f32 ? 4 : 2, K = proj->n_in, N = proj->n_out, M = b.rows, bank = (int64_t)b.adapters * b.rank;
     if (M > 0) {

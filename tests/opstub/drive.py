@@ -64,8 +64,12 @@ class Driver:
         p = G.Projection(k, n, w, k + pad, self.memory(1, n, n, 4),
                          self.memory(bank * rank, k, k, e),
                          self.memory(bank * n, rank, rank, e))
+        if c.get("bare"):
+            p.a = p.b = None
         off = c.get("off", {})   # bytes that a pointer is moved by
-        p.bias, p.a, p.b = p.bias + off.get("bias", 0), p.a + off.get("a", 0), p.b + off.get("b", 0)
+        for name in off:
+            if not name.startswith("d"):
+                setattr(p, name, getattr(p, name) + off[name])
         x = self.memory(rows, k, k + pad, e, shift)
         if c["op"] == "adapt":
             if "beside" in c:   # y: columns of the matrix that x lies in

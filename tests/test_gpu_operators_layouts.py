@@ -44,3 +44,15 @@ def test_columns_of_one_matrix(ctxs, dtype, rows, k, n, gap):  # noqa: F811
     # one column shared
     with pytest.raises(G.GemelError, match="overlaps"):
         ctx.adapt(b, wide[:, :k], s["w"], s["a"], s["b"], out=wide[:, k - 1:k - 1 + n])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [[9, 30], [60, 70]])
+def test_shared_gradients_without_the_bank(ctxs, dtype, rows):  # noqa: F811
+    s = problem(dtype, rows, [1, 0], 2, 8, 72, 40, 52)
+    want = reference(s)
+    ctx, b = ctxs[dtype], batch_of(ctxs[dtype], s)
+    got = ctx.adapt_backward(b, s["dy"], s["x"], s["w"], needs=("weight", "bias"))
+    assert set(got) == {"weight", "bias"}
+    for name, t in got.items():
+        close(name, t, want[name])

@@ -193,3 +193,22 @@ def test_pointers_that_are_not_aligned_are_refused(opslib):
         assert o["status"] == -1 and o["launches"] == 0 and o["message"] == f"{name} is not aligned to its type", (c, o)
     # gradients do not read the bias
     assert drive(opslib, [dict(c, off={"bias": 1})])["calls"][0]["status"] == 0
+
+
+def test_the_shared_gradients_need_no_adapters(opslib):
+    """dweight and dbias of a batch with adapters, without the bank; what the
+    bank enters is refused without it."""
+    calls = []
+    for dtype in ("bf16", "f32"):
+        for rows in ([40], [90, 30]):
+            c = {"op": "adapt_backward", "dtype": dtype, "n_rows": rows, "ids": [0, 1][:len(rows)], "bank": 2,
+                 "rank": 4, "k": 24, "n": 16, "bare": 1}
+            calls += [dict(c, needs=["weight", "bias"]), dict(c, needs=["weight"]), dict(c, needs=["bias"])]
+            calls += [dict(c, needs=[q]) for q in ("x", "a", "b")] + [dict(c, op="adapt")]
+    out = drive(opslib, calls)
+    assert out["violations"] == 0
+    for q, o in zip(calls, out["calls"]):
+        if q["op"] == "adapt" or set(q["needs"]) & {"x", "a", "b"}:
+            assert o["status"] == -1 and o["launches"] == 0 and "a and b must be given" in o["message"], (q, o)
+        else:
+            assert o["status"] == 0, (q, o)
