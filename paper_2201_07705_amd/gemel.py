@@ -557,6 +557,13 @@ class Context:
         with _torch().cuda.stream(stream):
             return like.new_empty(shape, dtype=dtype)
 
+    @staticmethod
+    def _written(*tensors):
+        """Counts a change in place of tensors that a caller passed to be
+        written, so that autograd refuses graphs that had saved them."""
+        _torch().autograd.graph.increment_version(
+            [t for t in tensors if t is not None])
+
     def _projection(self, batch, weight, a, b, bias):
         if batch._ctx is not self:
             raise ValueError("the batch is closed or of another context")
@@ -585,19 +592,25 @@ class Context:
         type, bias float32. x, weight and out may have a row stride.
 
         This and the operators below run on `stream` (None: the current
-        one), and make the tensors they return there."""
+        one), and make the tensors they return there. Autograd does not
+        record them, whatever their operands require: results carry no
+        graph, and gradients are those of adapt_backward. Tensors passed to
+        be written count as changed in place."""
         p, n, k, dt = self._projection(batch, weight, a, b, bias)
         rows = batch.rows
         self._tensor("x", x, (rows, k), dt, contiguous=False)
-        if out is None:
-            out = self._empty(x, (rows, n), dt, stream)
+        y = out
+        if y is None:
+            y = self._empty(x, (rows, n), dt, stream)
         else:
-            self._tensor("out", out, (rows, n), dt, contiguous=False)
+            self._tensor("out", y, (rows, n), dt, contiguous=False)
         self._check(self._lib.gemel_adapt(
             self._h, batch.id, p, x.data_ptr(), self._stride(x),
-            out.data_ptr(), self._stride(out),
-            self._stream(stream, x, weight, a, b, bias, out)))
-        return out
+            y.data_ptr(), self._stride(y),
+            self._stream(stream, x, weight, a, b, bias, y)))
+        if out is not None:
+            self._written(out)
+        return y
 
     def adapt_backward(self, batch, dy, x, weight, a=None, b=None,
                        needs=("x", "weight", "bias", "a", "b"), outputs=None,
@@ -634,6 +647,8 @@ class Context:
             self._stride(res["x"]) if "x" in res else 0, ptr.get("weight"),
             ptr.get("bias"), ptr.get("a"), ptr.get("b"),
             self._stream(stream, x, dy, weight, a, b, *res.values())))
+        if outputs:
+            self._written(*(outputs.get(name) for name in res))
         return res
 
     @staticmethod
@@ -648,14 +663,17 @@ class Context:
         count, rows, cols = self._matrices(g)
         dt = self._torch_dtype()
         self._tensor("g", g, g.shape, dt)
-        if out is None:
-            out = self._empty(g, g.shape, dt, stream)
+        o = out
+        if o is None:
+            o = self._empty(g, g.shape, dt, stream)
         else:
-            self._tensor("out", out, g.shape, dt)
+            self._tensor("out", o, g.shape, dt)
         self._check(self._lib.gemel_orthogonalize(
-            self._h, count, rows, cols, g.data_ptr(), out.data_ptr(), steps,
-            self._stream(stream, g, out)))
-        return out
+            self._h, count, rows, cols, g.data_ptr(), o.data_ptr(), steps,
+            self._stream(stream, g, o)))
+        if out is not None:
+            self._written(out)
+        return o
 
     def muon_step(self, w, momentum_buffer, g, lr, momentum=0.95,
                   weight_decay=0.0, nesterov=True, steps=5, copy=None,
@@ -675,4 +693,5 @@ class Context:
             None if copy is None else copy.data_ptr(), lr, momentum,
             weight_decay, 1 if nesterov else 0, steps,
             self._stream(stream, w, momentum_buffer, g, copy)))
+        self._written(w, momentum_buffer, copy)
         return w
