@@ -285,6 +285,19 @@ def _torch():
     return _torch_module
 
 
+def _int32(name, v):
+    """v, which ctypes would cut to the C interface's int32 without a word."""
+    if not -(1 << 31) <= v < 1 << 31:
+        raise ValueError(f"{name} does not fit 32 bits: {v}")
+    return v
+
+
+def _int32s(name, values):
+    """An array of int32 (of at least one element)."""
+    return (ctypes.c_int32 * max(len(values), 1))(
+        *[_int32(name, v) for v in values])
+
+
 class AdapterBatch:
     """The requests of Context.adapter_batch: rows of the batch, the bank's
     sizes and the library's id. Give it back with close(), or drop it."""
@@ -494,17 +507,18 @@ class Context:
         of a bank of n_adapters adapters of up to `rank`; per adapter its
         rank (None: all `rank`) and scale (None: 1)."""
         n = len(adapter_ids)
+        _int32("n_adapters", n_adapters)
+        _int32("rank", rank)
         if len(n_rows) != n:
             raise ValueError("adapter_ids and n_rows differ in length")
         for what, v in (("ranks", ranks), ("scales", scales)):
             if v is not None and len(v) != n_adapters:
                 raise ValueError(f"{what} must have one entry per adapter")
-        i32 = ctypes.c_int32
-        out = i32(-1)
+        out = ctypes.c_int32(-1)
         self._check(self._lib.gemel_adapter_batch(
-            self._h, (i32 * max(n, 1))(*adapter_ids),
-            (i32 * max(n, 1))(*n_rows), n, n_adapters, rank,
-            None if ranks is None else (i32 * max(n_adapters, 1))(*ranks),
+            self._h, _int32s("adapter_ids", adapter_ids),
+            _int32s("n_rows", n_rows), n, n_adapters, rank,
+            None if ranks is None else _int32s("ranks", ranks),
             None if scales is None else
             (ctypes.c_float * max(n_adapters, 1))(*scales),
             ctypes.byref(out)))
@@ -571,6 +585,8 @@ class Context:
             raise ValueError("weight must be [n_out, n_in]")
         dt = self._torch_dtype()
         n, k = weight.shape
+        _int32("n_out", n)
+        _int32("n_in", k)
         self._tensor("weight", weight, (n, k), dt, contiguous=False)
         if (a is None) != (b is None):
             raise ValueError("a and b come together")
@@ -652,15 +668,19 @@ class Context:
         return res
 
     @staticmethod
-    def _matrices(t):
+    def _matrices(t, steps):
         if t.dim() not in (2, 3):
             raise ValueError("expected [rows, cols] or [count, rows, cols]")
-        return (1,) * (3 - t.dim()) + tuple(t.shape)
+        _int32("steps", steps)
+        shape = (1,) * (3 - t.dim()) + tuple(t.shape)
+        for name, v in zip(("count", "rows", "cols"), shape):
+            _int32(name, v)
+        return shape
 
     def orthogonalize(self, g, steps=5, out=None, stream=None):
         """Newton-Schulz orthogonalisation of [rows, cols] or [count, rows,
         cols] contiguous matrices of the context's type."""
-        count, rows, cols = self._matrices(g)
+        count, rows, cols = self._matrices(g, steps)
         dt = self._torch_dtype()
         self._tensor("g", g, g.shape, dt)
         o = out
@@ -681,7 +701,7 @@ class Context:
         """One optimiser step, in place, of float32 matrices w [rows, cols]
         or [count, rows, cols] with their momentum buffer and gradient; copy
         (bf16 contexts) receives the new w in bf16."""
-        count, rows, cols = self._matrices(w)
+        count, rows, cols = self._matrices(w, steps)
         for name, t in (("w", w), ("momentum_buffer", momentum_buffer),
                         ("g", g)):
             self._tensor(name, t, w.shape, _torch().float32)
