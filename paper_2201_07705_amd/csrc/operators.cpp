@@ -81,8 +81,9 @@ struct State : OperatorState {
     int device;
     void *zero = nullptr;        // 256 zero bytes
     hipStream_t side = nullptr;  // uploads of tables
-    void *pinned = nullptr;
+    void *pinned = nullptr;      // they are staged in
     size_t pinned_bytes = 0;
+    std::vector<void *> outgrown;   // staging memory before (to free it would wait for the device)
     std::map<hipStream_t, Workspace> ws;
     std::vector<char *> captured;   // outgrown workspaces that graphs may use
     std::vector<std::unique_ptr<Batch>> batches;
@@ -110,6 +111,7 @@ struct State : OperatorState {
         for (hipEvent_t e : events) (void)hipEventDestroy(e);
         if (zero) (void)hipFree(zero);
         if (pinned) (void)hipHostFree(pinned);
+        for (void *p : outgrown) (void)hipHostFree(p);
         if (side) (void)hipStreamDestroy(side);
         ws.clear();
         captured.clear();
@@ -118,6 +120,7 @@ struct State : OperatorState {
         held.clear();
         retired.clear();
         events.clear();
+        outgrown.clear();
         zero = pinned = nullptr;
         side = nullptr;
         return ok;
@@ -292,6 +295,7 @@ gemel_status upload(gemel_ctx *ctx, State &st, const std::vector<int32_t> &words
             if (st.spare[i].second == want) return (int)i;
         return -1;
     };
+    st.outgrown.reserve(st.outgrown.size() + 1);
     int at = fits();
     if (at < 0) {
         reclaim(st);
@@ -312,7 +316,7 @@ gemel_status upload(gemel_ctx *ctx, State &st, const std::vector<int32_t> &words
     b.bytes = want;
     hipError_t e = hipSuccess;
     if (st.pinned_bytes < want) {
-        if (st.pinned) (void)hipHostFree(st.pinned);
+        if (st.pinned) st.outgrown.push_back(st.pinned);
         st.pinned = nullptr;
         st.pinned_bytes = 0;
         e = hipHostMalloc(&st.pinned, want, hipHostMallocDefault);

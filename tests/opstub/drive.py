@@ -137,7 +137,19 @@ class Driver:
         L.opstub_events_answer(0)
         return res
 
+    def growing(self, c):
+        """Batches of ever more rows; the waits for the device."""
+        L, ctx, out = self.L, self.ctx["f32"], I32(-1)
+        waits = L.opstub_device_waits()
+        for rows in c["n_rows"]:
+            assert L.gemel_adapter_batch(ctx, (I32 * 1)(0), (I32 * 1)(rows), 1, 1, 8, None, None,
+                                         ctypes.byref(out)) == G.OK
+            assert L.gemel_adapter_batch_free(ctx, out.value) == G.OK
+        return L.opstub_device_waits() - waits
+
     def call(self, c):
+        if c["op"] == "growing":
+            return self.growing(c)
         if c["op"] == "rounds":
             res = self.rounds(c)
             self.drop()

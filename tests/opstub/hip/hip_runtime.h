@@ -13,4 +13,6 @@ struct int4 {
 #define hipErrorNotReady ((hipError_t)600)
 extern "C" hipError_t hipEventQuery(hipEvent_t e);
 extern "C" hipError_t opstub_device_synchronize();
+extern "C" hipError_t opstub_host_free(void *p);
 #define hipDeviceSynchronize opstub_device_synchronize
+#define hipHostFree opstub_host_free

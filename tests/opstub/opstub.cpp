@@ -63,6 +63,7 @@ void touch_tables(const BatchTables &b) {
 }  // namespace
 
 #undef hipDeviceSynchronize
+#undef hipHostFree
 static long device_waits = 0;
 static hipError_t event_answer = hipSuccess;
 
@@ -71,6 +72,11 @@ hipError_t hipEventQuery(hipEvent_t) { return event_answer; }
 hipError_t opstub_device_synchronize() {
     ++device_waits;
     return hipDeviceSynchronize();
+}
+// (which waits for the device too)
+hipError_t opstub_host_free(void *p) {
+    ++device_waits;
+    return hipHostFree(p);
 }
 long opstub_device_waits() { return device_waits; }
 // What every event answers from now on (0: passed, 600: not yet).

@@ -212,3 +212,9 @@ def test_the_shared_gradients_need_no_adapters(opslib):
             assert o["status"] == -1 and o["launches"] == 0 and "a and b must be given" in o["message"], (q, o)
         else:
             assert o["status"] == 0, (q, o)
+
+
+def test_larger_batches_wait_for_nothing(opslib):
+    """Neither new tables nor the memory that they are staged in."""
+    out = drive(opslib, [{"op": "growing", "n_rows": [1, 10000, 100, 40000, 1 << 20, 1 << 21, 5, 1 << 22]}])
+    assert out["calls"] == [0] and out["violations"] == 0
