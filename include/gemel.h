@@ -142,9 +142,11 @@ typedef struct gemel_group {
  * they are time-shared by swapping weights in from host memory over PCIe
  * (Section 3.2); the paper evaluates each workload under fixed caps on
  * that memory (Appendix A.3), which hbm_weight_budget stands for.
- *  dtype              GEMEL_F32 (float32 everywhere) or GEMEL_BF16 (bf16
- *                     weights and activations, float32 accumulation and
- *                     epilogue, float32 outputs).
+ *  dtype              GEMEL_F32 (float32 everywhere; large products of the
+ *                     operators that serve and retrain merged layers take
+ *                     its values as pairs of float16, see there) or
+ *                     GEMEL_BF16 (bf16 weights and activations, float32
+ *                     accumulation and epilogue, float32 outputs).
  *  hbm_weight_budget  bytes of device memory that weights may occupy
  *                     (resident copies plus the swap staging buffers);
  *                     0 = unlimited. Weights beyond the budget stay in
@@ -694,14 +696,29 @@ gemel_status gemel_profile(gemel_ctx *ctx, gemel_kernel_stat *stats,
  *    gemel_destroy; calls on different streams do not wait for each other.
  *  - While hip_stream is being captured into a graph a call is enqueued if
  *    an earlier call of the same sizes on that stream has grown the
- *    workspace, else it returns ESTATE. Replays of the graph use that
- *    workspace, so they are ordered after other work on the stream; a
- *    workspace that was captured is kept when a larger call outgrows it.
+ *    workspace, else it returns ESTATE. The graph then holds the workspace
+ *    of the stream that was captured, whichever stream it is replayed on:
+ *    the caller orders its replays after, and before, whatever else uses
+ *    that workspace (calls on the captured stream, other graphs captured
+ *    on it). Replays on the captured stream itself are so ordered; graphs
+ *    that are to run at the same time are captured on streams of their
+ *    own. A workspace that was captured is kept when a larger call outgrows
+ *    it.
  *  - Sums are float32 (norms float64), in an order that the sizes alone
- *    fix: the same call on the same data gives the same bits. float32
- *    contexts multiply float32 values as pairs of float16 (22 bits, each
- *    row scaled by a power of two); a row holding a value that is not
- *    finite gives results that are not finite.
+ *    fix: the same call on the same data gives the same bits. With other
+ *    rows beside it a row's result may differ in its last bits.
+ *  - float32 contexts multiply float32 values as pairs of float16 in the
+ *    products with W of more than 64 rows, in dweight (but for up to 64
+ *    rows, or up to 64 outputs, or more than 2^21 rows) and in matrices
+ *    with no axis of up to 64: a value is off by at most 2^-22 of itself or
+ *    2^-38 of the largest one of its row (for dweight: of its column of dy
+ *    or x), whichever is more, and 2^-22 of each product is dropped. Values
+ *    far below the largest of their row thus have fewer bits than float32:
+ *    22 down to 2^-16 of it, 14 at 2^-24. All else is multiplied unrounded.
+ *    A row holding a value that is not finite gives results that are not
+ *    finite.
+ *  - bf16 contexts keep x A^T (for y) and dy B (for dx) as pairs of bf16
+ *    (16 bits) in batches of more than 64 rows, else as float32.
  */
 
 /*

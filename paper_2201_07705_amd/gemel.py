@@ -608,10 +608,13 @@ class Context:
         type, bias float32. x, weight and out may have a row stride.
 
         This and the operators below run on `stream` (None: the current
-        one), and make the tensors they return there. Autograd does not
-        record them, whatever their operands require: results carry no
-        graph, and gradients are those of adapt_backward. Tensors passed to
-        be written count as changed in place."""
+        one), and make the tensors they return there. A captured call uses
+        the workspace of the stream that is captured (on which a call of the
+        same sizes has to come first) wherever its graph is replayed, so
+        replays and other users of that workspace must be ordered. Autograd
+        does not record the operators, whatever their operands require:
+        results carry no graph, and gradients are those of adapt_backward.
+        Tensors passed to be written count as changed in place."""
         p, n, k, dt = self._projection(batch, weight, a, b, bias)
         rows = batch.rows
         self._tensor("x", x, (rows, k), dt, contiguous=False)

@@ -85,3 +85,34 @@ def test_more_tiles_than_a_grid_of_the_smallest(ctxs):  # noqa: F811
     # every row was written: whole numbers, their sums over the outputs
     assert torch.equal(y.view(1024, -1, n)[:, 0].sum(1, dtype=torch.float32),
                        (x.view(1024, -1, k)[:, 0] @ w.T + s["bias"]).to(torch.bfloat16).sum(1, dtype=torch.float32))
+
+
+@pytest.mark.parametrize("small", [2.0 ** -10, 2.0 ** -20, 2.0 ** -24, 2.0 ** -30])
+def test_values_far_below_the_largest_of_their_row(ctxs, small):  # noqa: F811
+    """float32 gradients of one large row of dy among small ones, for inputs
+    that the large row has at zero: each operand is off by 2^-22 of itself or
+    2^-38 of the largest one that it is multiplied beside, a product by
+    2^-22, and a sum of 2048 by as many roundings of 2^-24."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    m, k, n = 2048, 256, 80
+    x = torch.randn(m, k, generator=gen, device="cuda")
+    dy = torch.randn(m, n, generator=gen, device="cuda") * small
+    dy[77] /= small
+    x[77, :128] = 0
+    w = torch.randn(n, k, generator=gen, device="cuda")
+    ctx = ctxs["f32"]
+    b = ctx.adapter_batch([-1], [m], 1, 1)
+    got = ctx.adapt_backward(b, dy, x, w, needs=("weight", "x"))
+    f64 = torch.float64
+
+    def off(t, axis):
+        t = t.to(f64).abs()
+        return torch.maximum(2.0 ** -22 * t, 2.0 ** -38 * t.amax(axis, keepdim=True))
+
+    dyd, xd, wd = dy.to(f64), x.to(f64), w.to(f64)
+    for name, p, q, ep, eq in (
+            ("weight", dyd.T, xd, off(dy, 0).T, off(x, 0)), ("x", dyd, wd, off(dy, 1), off(w, 0))):
+        mag = p.abs() @ q.abs()
+        bound = ep @ q.abs() + p.abs() @ eq + ep @ eq + (2.0 ** -22 + 2.0 ** -24 * (p.shape[1] + 8)) * mag
+        assert ((got[name].to(f64) - p.contiguous() @ q).abs() <= bound).all(), name

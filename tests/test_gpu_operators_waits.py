@@ -63,3 +63,37 @@ def test_new_batches_do_not_wait_for_other_work(ctxs):  # noqa: F811
     for y in outs:
         assert torch.equal(y, outs[0])
     close("y", outs[0], want)
+
+
+def test_graphs_of_streams_of_their_own_replay_together(ctxs):  # noqa: F811
+    """Each holds the workspace of the stream that it was captured on, so
+    their replays on other streams need no order."""
+    import torch
+    ctx = ctxs["bf16"]
+    work = []
+    for i in range(2):
+        s = problem("bf16", [700 + 50 * i, 90], [1, 0], 2, 16, 1032, 776, 60 + i)
+        b, st = batch_of(ctx, s), torch.cuda.Stream()
+        args = (s["x"], s["w"], s["a"], s["b"])
+        st.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(st):
+            want = [ctx.adapt(b, *args), ctx.adapt_backward(b, s["dy"], *args)["weight"]]
+        torch.cuda.synchronize()
+        outs = [torch.zeros_like(t) for t in want]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            ctx.adapt(b, *args, out=outs[0])
+            ctx.adapt_backward(b, s["dy"], *args, needs=("weight",), outputs={"weight": outs[1]})
+        work.append((graph, torch.cuda.Stream(), want, outs, (s, b)))
+    for _ in range(6):
+        for _, _, _, outs, _ in work:
+            for t in outs:
+                t.zero_()
+        torch.cuda.synchronize()
+        for graph, on, _, _, _ in work:
+            with torch.cuda.stream(on):
+                graph.replay()
+                graph.replay()
+        torch.cuda.synchronize()
+        for _, _, want, outs, _ in work:
+            assert all(torch.equal(p, q) for p, q in zip(want, outs))
