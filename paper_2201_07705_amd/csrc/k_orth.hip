@@ -157,7 +157,7 @@ __global__ __launch_bounds__(256) void seed_kernel(const OrthArgs a) {
 // ones than 64 would not have their polynomials in one workgroup's LDS.
 
 // Partial Gram matrices. A workgroup takes stretches of 64 positions of the
-// long axis through LDS ([n][64], row pitch 66 doubles' worth of banks), its
+// long axis through LDS ([n][64] floats, rows 68 apart), its
 // 4 waves 16 positions each, and adds the waves' sums at the end. Only tiles
 // on and above the diagonal are computed.
 template <int NB, bool WIDE>

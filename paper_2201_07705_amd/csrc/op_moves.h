@@ -23,6 +23,5 @@ __device__ __forceinline__ void put_f32x4(void *p, F4 v) {
     *(f32x4_any *)p = __builtin_bit_cast(f32x4_any, v);
 }
 __device__ __forceinline__ void put_u16x4(void *p, ushort4 v) { *(u16x4_any *)p = __builtin_bit_cast(u16x4_any, v); }
-__device__ __forceinline__ void put_16b(void *p, uint4 v) { *(u32x4_any *)p = __builtin_bit_cast(u32x4_any, v); }
 
 }  // namespace gemel
