@@ -8,6 +8,7 @@
 #include <memory>
 #include <new>
 #include <string>
+#include <thread>
 #include <utility>
 #include <vector>
 
@@ -58,7 +59,7 @@ struct Batch {
     void *dev = nullptr;
     size_t bytes = 0;
     std::vector<hipStream_t> streams;   // that its calls ran on
-    bool captured = false;              // a graph may hold its addresses
+    bool held = false;                  // a graph, or another thread's stream, may hold its addresses
 };
 
 // Tables given back that enqueued work may still read: until events, recorded
@@ -84,11 +85,11 @@ struct State : OperatorState {
     void *pinned = nullptr;      // they are staged in
     size_t pinned_bytes = 0;
     std::vector<void *> outgrown;   // staging memory before (to free it would wait for the device)
-    std::map<hipStream_t, Workspace> ws;
+    std::map<std::pair<hipStream_t, std::thread::id>, Workspace> ws;   // (each thread's own hipStreamPerThread)
     std::vector<char *> captured;   // outgrown workspaces that graphs may use
     std::vector<std::unique_ptr<Batch>> batches;
-    // tables given back: nobody reads `spare` ones; replays enqueued on unknown
-    // streams may still read `held` ones
+    // tables given back: nobody reads `spare` ones; work on streams that cannot
+    // be asked (replays of graphs) may still read `held` ones
     std::vector<std::pair<void *, size_t>> spare, held;
     std::vector<Retired> retired;
     std::vector<hipEvent_t> events;   // not in use
@@ -180,7 +181,10 @@ struct Layout {
 // The call's pieces of its stream's workspace; `batch` (or null) is noted as
 // used on the stream.
 gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layout &lay, Batch *batch, char **out) {
-    Workspace &w = st.ws[stream];
+    // one handle, a stream for each thread: another thread cannot ask for its
+    // work, which is waited for with the device
+    const bool per_thread = stream == hipStreamPerThread;
+    Workspace &w = st.ws[{stream, per_thread ? std::this_thread::get_id() : std::thread::id()}];
     size_t bytes = lay.bytes;
     hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
     if (stream) OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
@@ -202,8 +206,8 @@ gemel_status workspace(gemel_ctx *ctx, State &st, hipStream_t stream, const Layo
         w.bytes = bytes;
     }
     if (cs != hipStreamCaptureStatusNone) w.captured = true;
-    if (batch && cs != hipStreamCaptureStatusNone)
-        batch->captured = true;
+    if (batch && (cs != hipStreamCaptureStatusNone || per_thread))
+        batch->held = true;
     else if (batch && std::find(batch->streams.begin(), batch->streams.end(), stream) == batch->streams.end())
         batch->streams.push_back(stream);
     lay.fence(w.p, w.bytes);
@@ -1363,7 +1367,7 @@ gemel_status gemel_adapter_batch_free(gemel_ctx *ctx, int32_t batch) {
         State *st;
         Batch *b;
         if (gemel_status s = get_batch(ctx, batch, &st, &b)) return s;
-        if (b->captured)
+        if (b->held)
             st->held.push_back({b->dev, b->bytes});
         else if (b->streams.empty())
             st->spare.push_back({b->dev, b->bytes});

@@ -147,7 +147,43 @@ class Driver:
             assert L.gemel_adapter_batch_free(ctx, out.value) == G.OK
         return L.opstub_device_waits() - waits
 
+    def threads(self, c):
+        """Calls on hipStreamPerThread, one after the other, from threads of
+        their own that stay alive: the memory that each took, and the waits
+        for the device of batches that are given back."""
+        import threading
+        L, ctx, out = self.L, self.ctx["f32"], I32(-1)
+        w, x, y = self.memory(8, 8, 8, 4), self.memory(90, 8, 8, 4), self.memory(90, 8, 8, 4)
+        p = G.Projection(8, 8, w, 8, None, None, None)
+        took, end, turn = [], threading.Event(), threading.Event()
+
+        def one():
+            for _ in range(2):
+                assert L.gemel_adapter_batch(ctx, (I32 * 1)(-1), (I32 * 1)(90), 1, 1, 8, None, None,
+                                             ctypes.byref(out)) == G.OK
+                before = L.hoststub_allocs()
+                assert L.gemel_adapt(ctx, out.value, ctypes.byref(p), x, 8, y, 8, 2) == G.OK
+                took.append(L.hoststub_allocs() - before)
+                assert L.gemel_adapter_batch_free(ctx, out.value) == G.OK
+            turn.set()
+            end.wait()
+
+        alive = []
+        for _ in range(c["threads"]):
+            turn.clear()
+            alive.append(threading.Thread(target=one))
+            alive[-1].start()
+            turn.wait()
+        end.set()
+        for t in alive:
+            t.join()
+        return took
+
     def call(self, c):
+        if c["op"] == "threads":
+            res = self.threads(c)
+            self.drop()
+            return res
         if c["op"] == "growing":
             return self.growing(c)
         if c["op"] == "rounds":

@@ -5,6 +5,7 @@
 
 #define __host__
 #define __device__
+#define hipStreamPerThread ((hipStream_t)2)
 struct int4 {
     int x, y, z, w;
 };

@@ -218,3 +218,10 @@ def test_larger_batches_wait_for_nothing(opslib):
     """Neither new tables nor the memory that they are staged in."""
     out = drive(opslib, [{"op": "growing", "n_rows": [1, 10000, 100, 40000, 1 << 20, 1 << 21, 5, 1 << 22]}])
     assert out["calls"] == [0] and out["violations"] == 0
+
+
+def test_each_thread_has_its_own_per_thread_stream(opslib):
+    """hipStreamPerThread is one handle for many streams, which do not wait
+    for each other and so share no workspace."""
+    out = drive(opslib, [{"op": "threads", "threads": 3}])
+    assert out["calls"] == [[1, 0] * 3] and out["violations"] == 0
