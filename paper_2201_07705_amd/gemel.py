@@ -298,6 +298,16 @@ def _int32s(name, values):
         *[_int32(name, v) for v in values])
 
 
+def _current_stream(device):
+    """The handle of torch's current stream on the device. The entry that
+    gives the handle alone is not a public one; where it is missing a Stream
+    object is made for it (1 us of a call's 12)."""
+    raw = getattr(_torch()._C, "_cuda_getCurrentRawStream", None)
+    if raw is None:
+        return _torch().cuda.current_stream(device).cuda_stream
+    return raw(device)
+
+
 class AdapterBatch:
     """The requests of Context.adapter_batch: rows of the batch, the bank's
     sizes and the library's id. Give it back with close(), or drop it."""
@@ -554,8 +564,7 @@ class Context:
         """The handle of the stream to work on. Where that is not the current
         one the tensors are marked as used there, so that memory a caller
         drops is not handed out again before the work is done."""
-        # (the handle alone: making a Stream object takes 1 us of a call's 12)
-        current = _torch()._C._cuda_getCurrentRawStream(self.device)
+        current = _current_stream(self.device)
         if stream is None or stream.cuda_stream == current:
             return current
         for t in tensors:

@@ -97,3 +97,16 @@ def test_graphs_of_streams_of_their_own_replay_together(ctxs):  # noqa: F811
         torch.cuda.synchronize()
         for _, _, want, outs, _ in work:
             assert all(torch.equal(p, q) for p, q in zip(want, outs))
+
+
+def test_the_current_stream_without_the_private_entry(ctxs, monkeypatch):  # noqa: F811
+    import torch
+    from paper_2201_07705_amd import gemel as G
+    st = torch.cuda.Stream()
+    for on in (torch.cuda.current_stream(), st):
+        with torch.cuda.stream(on):
+            assert G._current_stream(0) == on.cuda_stream
+            with monkeypatch.context() as m:
+                m.delattr(torch._C, "_cuda_getCurrentRawStream", raising=False)
+                assert G._current_stream(0) == on.cuda_stream
+                ctxs["bf16"].orthogonalize(torch.ones(8, 8, device="cuda", dtype=torch.bfloat16))
