@@ -9,6 +9,7 @@ import json
 import os
 import random
 import subprocess
+from concurrent.futures import ThreadPoolExecutor
 
 import pytest
 
@@ -25,12 +26,16 @@ def opslib():
     tmp = f"{LIB}.{os.getpid()}"
     flags = ["g++", "-std=c++17", "-g", "-O1", "-fsanitize=address", "-fno-omit-frame-pointer", "-fPIC"]
     dirs = [f"-I{HOST}", f"-I{os.path.join(ROOT, 'include')}", f"-I{CSRC}"]
-    subprocess.check_call(flags + dirs + ["-c", os.path.join(HOST, "hoststub.cpp"), "-o", tmp + ".o"])
-    subprocess.check_call(
-        flags + ["-shared", f"-I{STUB}"] + dirs
-        + [os.path.join(CSRC, f"{f}.cpp") for f in ("registry", "plan", "batching", "operators", "op_plan")]
-        + [tmp + ".o", os.path.join(STUB, "opstub.cpp"), "-o", tmp])
-    os.remove(tmp + ".o")
+    sources = {os.path.join(HOST, "hoststub.cpp"): [], os.path.join(STUB, "opstub.cpp"): [f"-I{STUB}"]}
+    for name in ("registry", "plan", "batching", "operators", "op_plan"):
+        sources[os.path.join(CSRC, name + ".cpp")] = [f"-I{STUB}"]
+    objects = [f"{tmp}.{k}.o" for k in range(len(sources))]
+    with ThreadPoolExecutor(max_workers=8) as ex:
+        list(ex.map(subprocess.check_call, [flags + first + dirs + ["-c", src, "-o", obj]
+                                            for (src, first), obj in zip(sources.items(), objects)]))
+    subprocess.check_call(flags + ["-shared"] + objects + ["-o", tmp])
+    for obj in objects:
+        os.remove(obj)
     os.replace(tmp, LIB)
     return LIB
 
