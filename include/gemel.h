@@ -694,6 +694,7 @@ gemel_status gemel_profile(gemel_ctx *ctx, gemel_kernel_stat *stats,
  *    Calls on one stream share a workspace of the context, which grows to
  *    the largest call (growing synchronises the device) and is kept until
  *    gemel_destroy; calls on different streams do not wait for each other.
+ *    A stream is destroyed only when the work of its calls is over.
  *  - While hip_stream is being captured into a graph a call is enqueued if
  *    an earlier call of the same sizes on that stream has grown the
  *    workspace, else it returns ESTATE. The graph then holds the workspace
