@@ -858,8 +858,9 @@ gemel_status backward(gemel_ctx *ctx, int32_t id, const gemel_projection *proj, 
     // than the product (16384 x 4096, 10 outputs 298 -> 64 us, 64 303 -> 114;
     // 4096 x 512, 64 29 -> 18; at 100 outputs 512 x 4096 takes 26, not 23).
     // bf16 copies are cheap, and the tiles faster: 64 outputs 87 us, not 113.
-    // So are dW of more than 2^21 float32 rows, whose transposed pairs would
-    // be longer than a product's rows can be
+    // More than 2^21 float32 rows go the same way, whatever the outputs: their
+    // transposed pairs would be longer than a product's rows can be (256
+    // columns, 128 outputs: 2^21 rows as pairs 4.5 ms, 64 more rows 1.9)
     const bool narrow = dw && !few && f32 && (N <= NARROW || 2 * op_round_up(M, 64) > MM_MAX_LD),
                tiled = dw && !few && !narrow;
     // U = scale dy B and T = scale x A^T
