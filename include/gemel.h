@@ -835,6 +835,89 @@ gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows,
                              float weight_decay, int32_t nesterov,
                              int32_t steps, void *hip_stream);
 
+/*
+ * ---- Answers of merged models, and their distillation ----
+ *
+ * What a head's logits say, and how far they are from those of the model
+ * that was merged: the unmerged model's best answers (gemel_log_probs) are
+ * what a merged one is retrained against (gemel_distill and its gradient,
+ * whose dlogits is the dy of gemel_adapt_backward).
+ *
+ * The conventions of the calls above hold. Logits are float32 (as
+ * gemel_infer writes them) or bf16 (as gemel_adapt does) in every context:
+ * dtype says which. A class whose logit is -inf is not offered; softmaxes
+ * are those of logits / temperature (1e-6..1e6), summed in float32. A row
+ * that holds a NaN or +inf gives NaN and -1, and no other row is touched by
+ * it. Rows of more than 16384 (float32) or 32768 (bf16) classes may take a
+ * workspace. rows 0 is no error and touches nothing.
+ */
+
+/* Outputs of gemel_log_probs; each may be NULL (not computed). */
+typedef struct gemel_answers {
+    float *log_prob;        /* [rows] of the label: 0 where it is -1, -inf
+                               for a class not offered, NaN for a label
+                               outside -1..classes-1                      */
+    int32_t *rank;          /* [rows] classes with a larger logit, or an
+                               equal one and a lower index; -1 where the
+                               label is no class                          */
+    float *entropy;         /* [rows] 0 where no class is offered         */
+    float *log_sum;         /* [rows] log of the sum of exponentials      */
+    int32_t *top_indices;   /* [rows][top] the classes with the largest
+                               logits, of equal ones the lower index
+                               first; -1 beyond those offered             */
+    float *top_log_probs;   /* [rows][top] theirs; -inf beyond            */
+} gemel_answers;
+
+/*
+ * Answers of logits [rows][classes], rows logits_stride apart, 1 <= classes
+ * <= 2^20. labels: [rows] or NULL where neither log_prob nor rank is asked
+ * for. top in 0..64.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_log_probs(gemel_ctx *ctx, int32_t rows, int32_t classes,
+                             const void *logits, int64_t logits_stride,
+                             int32_t dtype, const int32_t *labels,
+                             int32_t top, float temperature,
+                             const gemel_answers *out, void *hip_stream);
+
+/*
+ * Loss of each row against its teacher's best logits: with q the softmax of
+ * values / temperature over the row's entries and p that of all of its
+ * logits / temperature,
+ *   loss[row] = temperature^2 * sum over entries of q (log q - log p).
+ *  indices, values  [rows][entries], contiguous, entries in 1..64: classes
+ *          and the teacher's logits or log probabilities (a shift of a row
+ *          changes nothing). An entry of class -1 or value -inf is not
+ *          there; entries of one class add up. A row without entries has
+ *          loss 0 and no gradient, whatever its logits hold.
+ * A class outside -1..classes-1, or a value of NaN or +inf, makes its row
+ * NaN; a class that the student does not offer makes its loss +inf.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_distill(gemel_ctx *ctx, int32_t rows, int32_t classes,
+                           const void *logits, int64_t logits_stride,
+                           int32_t dtype, const int32_t *indices,
+                           const float *values, int32_t entries,
+                           float temperature, float *loss, void *hip_stream);
+
+/*
+ * Gradient of the sum of dloss[row] * loss[row] with respect to the logits:
+ *   dlogits[row][c] = dloss[row] * temperature * (p_c - q of class c),
+ * in the logits' type, rows dlogits_stride apart. dloss: [rows] or NULL
+ * (all 1). loss: NULL, or [rows], written as gemel_distill does, from the
+ * same pass over the logits.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_distill_backward(gemel_ctx *ctx, int32_t rows,
+                                    int32_t classes, const float *dloss,
+                                    const void *logits,
+                                    int64_t logits_stride, int32_t dtype,
+                                    const int32_t *indices,
+                                    const float *values, int32_t entries,
+                                    float temperature, void *dlogits,
+                                    int64_t dlogits_stride, float *loss,
+                                    void *hip_stream);
+
 /* Description of the last error (see general conventions). */
 const char *gemel_last_error(const gemel_ctx *ctx);
 

@@ -1,0 +1,531 @@
+// Answers off rows of logits: log probability and rank of a label, entropy,
+// the best classes; and the loss of a student against a teacher's best logits
+// with its gradient.
+//
+// With c = log2(e) / T and t_i = (z_i - m) c, m the row's largest logit, every
+// result follows from S = sum 2^t_i and A = sum 2^t_i t_i:
+//   log sum = m / T + ln 2 log2 S,  log p_i = (z_i - m) / T - ln 2 log2 S,
+//   entropy = ln 2 (log2 S - A / S).
+//
+// A row is held in registers by a team of waves, each lane pieces of 16 bytes
+// of it, so that it is read once; rows that no team can hold are cut into
+// chunks whose sums and best classes a second launch joins.
+#include <hip/hip_runtime.h>
+
+#include "answer_args.h"
+#include "op_moves.h"
+
+namespace gemel {
+
+namespace {
+
+typedef unsigned short u16;
+typedef unsigned long long u64;
+constexpr float LN2 = 0.693147180559945309417f;
+
+__device__ __forceinline__ float infinity() { return __builtin_inff(); }
+__device__ __forceinline__ float quiet() { return __builtin_nanf(""); }
+
+// a, b, c: the largest; of a NaN and a number the number (fmaxf would first
+// bring every operand into canonical form)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
+
+// Reductions over a wave: rows of 16 lanes, then between them; every lane
+// gets the result.
+template <int CTRL, typename T>
+__device__ __forceinline__ T moved(T none, T v) {
+    return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, 0xf,
+                                                             0xf, false));
+}
+template <typename T, typename F>
+__device__ __forceinline__ T wave_reduce(T v, T none, F f) {
+    v = f(v, moved<0x111>(none, v));   // row_shr 1, 2, 4, 8
+    v = f(v, moved<0x112>(none, v));
+    v = f(v, moved<0x114>(none, v));
+    v = f(v, moved<0x118>(none, v));
+    v = f(v, moved<0x142>(none, v));   // row_bcast 15, 31
+    v = f(v, moved<0x143>(none, v));
+    return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 63));
+}
+__device__ __forceinline__ float wave_max(float v) {
+    return wave_reduce(v, -infinity(), [](float a, float b) { return max3(a, b, b); });
+}
+__device__ __forceinline__ float wave_sum(float v) {
+    return wave_reduce(v, 0.f, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ int wave_sum(int v) {
+    return wave_reduce(v, 0, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int wave_min(int v) {
+    return wave_reduce(v, 0x7fffffff, [](int a, int b) { return min(a, b); });
+}
+
+// What a team of W waves shares is written before and read after this.
+template <int W>
+__device__ __forceinline__ void team_sync() {
+    if constexpr (W == 1) {
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    } else {
+        __syncthreads();
+    }
+}
+
+// Classes [lo, hi) of a row in a team's registers: piece v of a lane begins
+// at class at(v). A piece that would pass the end is moved back to end there,
+// and what the piece before it holds already is -inf in it.
+template <bool F32, int W, int V>
+struct Held {
+    static constexpr int VEC = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
+    uint4 raw[V];
+    int lo, hi, tid;
+
+    __device__ __forceinline__ int first(int v) const { return lo + (v * W * 64 + tid) * VEC; }
+    __device__ __forceinline__ int at(int v) const { return hi - lo < VEC ? first(v) : min(first(v), hi - VEC); }
+    __device__ __forceinline__ float get(int v, int j) const {
+        if constexpr (F32)
+            return __uint_as_float((&raw[v].x)[j]);
+        else
+            return __uint_as_float(j & 1 ? (&raw[v].x)[j / 2] & 0xffff0000u : (&raw[v].x)[j / 2] << 16);
+    }
+    // The first n elements of piece v become -inf.
+    __device__ __forceinline__ void mask(int v, int n) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            uint32_t &x = (&raw[v].x)[i];
+            if constexpr (F32)
+                x = n > i ? 0xff800000u : x;
+            else
+                x = n > 2 * i + 1 ? 0xff80ff80u : n > 2 * i ? (x & 0xffff0000u) | 0xff80u : x;
+        }
+    }
+    // Before piece v is used: what was made of it earlier is made again, and
+    // nothing is made of it ahead (the compiler would keep every bf16 unpacked,
+    // or every exponential, in several times the registers). The sums or stores
+    // of the piece before are done first.
+    __device__ __forceinline__ void again(int v) {
+        asm volatile("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w)::"memory");
+    }
+    __device__ __forceinline__ void again(int v, float &s, float &a) {
+        asm volatile("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w), "+v"(s), "+v"(a));
+    }
+    __device__ __forceinline__ void load(const char *row, int lo_, int hi_, int tid_) {
+        lo = lo_;
+        hi = hi_;
+        tid = tid_;
+        if (hi - lo < VEC) {   // fewer classes than a piece
+#pragma unroll
+            for (int v = 0; v < V; ++v) mask(v, VEC);
+            if (tid == 0)
+#pragma unroll
+                for (int j = 0; j < VEC; ++j) {
+                    if (lo + j >= hi) continue;
+                    if constexpr (F32)
+                        (&raw[0].x)[j] = *(const uint32_t *)(row + (lo + j) * 4);
+                    else
+                        (&raw[0].x)[j / 2] = ((&raw[0].x)[j / 2] & (j & 1 ? 0xffffu : 0xffff0000u)) |
+                                             (uint32_t) * (const u16 *)(row + (lo + j) * 2) << (j & 1) * 16;
+                }
+            return;
+        }
+#pragma unroll
+        for (int v = 0; v < V; ++v) raw[v] = get_16b(row + (uint32_t)at(v) * SIZE);
+        const int wave0 = (tid & ~63) + 64;
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+            if (lo + (v * W * 64 + wave0) * VEC > hi) mask(v, first(v) - at(v));
+    }
+};
+
+__device__ __forceinline__ float logit(const Logits &l, const char *row, int i) {
+    return l.f32 ? *(const float *)(row + (int64_t)i * 4) : __uint_as_float((uint32_t) * (const u16 *)(row + (int64_t)i * 2) << 16);
+}
+
+// Sums of two parts of a row together.
+__device__ __forceinline__ Part joined(const Part &x, const Part &y, float c) {
+    Part p;
+    p.before = x.before + y.before;
+    // (NaN sums are not empty)
+    if (x.s == 0.f) return Part{y.m, y.s, y.a, p.before};
+    if (y.s == 0.f) return Part{x.m, x.s, x.a, p.before};
+    p.m = max3(x.m, y.m, y.m);
+    const float dx = (x.m - p.m) * c, dy = (y.m - p.m) * c;
+    const float fx = __builtin_amdgcn_exp2f(dx), fy = __builtin_amdgcn_exp2f(dy);
+    p.s = x.s * fx + y.s * fy;
+    // (what is 2^-127 of the other leaves nothing, however far it is away)
+    p.a = (fx > 0.f ? (x.a + dx * x.s) * fx : 0.f) + (fy > 0.f ? (y.a + dy * y.s) * fy : 0.f);
+    return p;
+}
+
+// Sums of the elements that a wave holds.
+template <bool F32, int W, int V>
+__device__ __forceinline__ Part wave_part(Held<F32, W, V> &h, float c) {
+    constexpr int VEC = Held<F32, W, V>::VEC;
+    float m = -infinity();
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) m = max3(m, h.get(v, j), h.get(v, j + 1));
+    m = wave_max(m);
+    const float ref = m == -infinity() ? 0.f : m;
+    float s = 0.f, a = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        h.again(v, s, a);
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float t = (h.get(v, j) - ref) * c;
+            const float e = __builtin_amdgcn_exp2f(t);
+            s += e;
+            // (0 times -inf, a masked class's, has to be nothing)
+            a = __builtin_fmaf(e, fmaxf(t, -1e30f), a);
+        }
+    }
+    return Part{m, wave_sum(s), wave_sum(a), 0};
+}
+
+// The team's sums from those of its waves, in every lane.
+template <int W>
+__device__ __forceinline__ Part team_part(Part p, Part *shared, int wave, float c) {
+    if constexpr (W == 1) return p;
+    if ((threadIdx.x & 63) == 0) shared[wave] = p;
+    __syncthreads();
+    Part sum = shared[0];
+#pragma unroll
+    for (int w = 1; w < W; ++w) sum = joined(sum, shared[w], c);
+    return sum;
+}
+
+struct Results {
+    bool lost;      // some logit is NaN or +inf
+    float log2_s;
+};
+__device__ __forceinline__ Results results(const Part &p) { return {!(p.s < infinity()), log2f(p.s)}; }
+__device__ __forceinline__ float log_prob(const Part &p, const Results &q, float z, float inv_t) {
+    if (q.lost) return quiet();
+    return z == -infinity() || p.s == 0.f ? -infinity() : (z - p.m) * inv_t - LN2 * q.log2_s;
+}
+// One row's outputs but for the list.
+__device__ __forceinline__ void put_row(const ScoreArgs &a, int row, const Part &p, int label, float z_label) {
+    const Results q = results(p);
+    if (a.entropy) {
+        const float h = LN2 * (q.log2_s - p.a / p.s);
+        a.entropy[row] = q.lost ? quiet() : p.s == 0.f || h < 0.f ? 0.f : h;
+    }
+    if (a.log_sum) a.log_sum[row] = q.lost ? quiet() : p.s == 0.f ? -infinity() : p.m * a.l.inv_t + LN2 * q.log2_s;
+    const bool in = label >= 0 && label < a.l.classes;
+    if (a.log_prob) a.log_prob[row] = label == -1 ? 0.f : in ? log_prob(p, q, z_label, a.l.inv_t) : quiet();
+    if (a.rank) a.rank[row] = in && !q.lost ? p.before : -1;
+}
+__device__ __forceinline__ void put_top(const ScoreArgs &a, int row, int i, const Part &p, const Results &q, float z, int index) {
+    const int64_t at = (int64_t)row * a.top + i;
+    if (a.top_index) a.top_index[at] = q.lost ? -1 : index;
+    if (a.top_log_prob) a.top_log_prob[at] = q.lost ? quiet() : index < 0 ? -infinity() : log_prob(p, q, z, a.l.inv_t);
+}
+
+struct Best {
+    float z;
+    int i;
+};
+
+template <bool F32, int W, int V>
+__global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const ScoreArgs a) {
+    constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W);
+    __shared__ Part parts[W];
+    __shared__ Best best[TEAMS][W];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int team = W == 1 ? wave : 0, w = W == 1 ? 0 : wave, tid = W == 1 ? lane : (int)threadIdx.x;
+    const int row = (int)blockIdx.x * TEAMS + team, chunk = blockIdx.y;
+    if (row >= a.l.rows) return;   // (a wave of its own: no barrier waits for it)
+    const int64_t unit = (int64_t)row * a.l.chunks + chunk;
+    const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * (F32 ? 4 : 2);
+    const int lo = chunk * a.l.chunk, hi = min(a.l.classes, lo + a.l.chunk);
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool in = label >= 0 && label < a.l.classes;
+    Held<F32, W, V> h;
+    h.load(z, lo, hi, tid);
+    const float z_label = in ? logit(a.l, z, label) : 0.f;
+    Part p = wave_part<F32, W, V>(h, a.l.c);
+    if (a.rank && in) {
+        int n = 0;
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int b = h.at(v), f = h.first(v);
+            h.again(v);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float x = h.get(v, j);
+                n += x > z_label || (x == z_label && b + j < label && b + j >= f);
+            }
+        }
+        p.before = wave_sum(n);
+    }
+    p = team_part<W>(p, parts, w, a.l.c);
+    const Results q = results(p);
+    if (tid == 0) {
+        if (a.l.chunks > 1)
+            a.part[unit] = p;
+        else
+            put_row(a, row, p, label, z_label);
+    }
+    // the best class behind the last one, `top` times
+    Best last{infinity(), -1};
+    for (int k = 0; k < a.top; ++k) {
+        Best b{-infinity(), -1};
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const int at = h.at(v);
+            h.again(v);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float x = h.get(v, j);
+                if (x > b.z && (x < last.z || (x == last.z && at + j > last.i))) b = Best{x, at + j};
+            }
+        }
+        const float most = wave_max(b.z);
+        b.i = wave_min(b.z == most && b.i >= 0 ? b.i : 0x7fffffff);
+        b.z = most;
+        if constexpr (W > 1) {
+            __syncthreads();
+            if (lane == 0) best[0][w] = b;
+            __syncthreads();
+            b = best[0][0];
+#pragma unroll
+            for (int i = 1; i < W; ++i) {
+                const Best o = best[0][i];
+                if (o.z > b.z || (o.z == b.z && o.i < b.i)) b = o;
+            }
+        }
+        if (b.z == -infinity()) b.i = -1;
+        if (b.i >= 0) last = b;
+        else last = Best{-infinity(), 0x7fffffff};
+        if (tid == 0) {
+            if (a.l.chunks > 1) {
+                a.list_value[unit * a.top + k] = b.z;
+                a.list_index[unit * a.top + k] = b.i;
+            } else {
+                put_top(a, row, k, p, q, b.z, b.i);
+            }
+        }
+    }
+}
+
+// A value and its class as one number: larger for what comes first.
+__device__ __forceinline__ u64 key_of(float z, int index) {
+    const uint32_t u = __float_as_uint(z + 0.f);   // (-0 is 0)
+    const uint32_t k = u & 0x80000000u ? ~u : u | 0x80000000u;
+    return index < 0 ? 0 : (u64)k << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ Best of_key(u64 key) {
+    const uint32_t k = (uint32_t)(key >> 32);
+    return key ? Best{__uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k), (int)~(uint32_t)key} : Best{-infinity(), -1};
+}
+
+// One row for each workgroup: the sums of its chunks, and the best of their
+// lists. Lists are sorted, so a class's place is what binary searches in the
+// others say.
+__global__ __launch_bounds__(256) void score_join_kernel(const ScoreArgs a) {
+    __shared__ u64 keys[ANSWER_MAX_CHUNKS * TOP_MAX];
+    const int row = blockIdx.x, tid = threadIdx.x, chunks = a.l.chunks, n = chunks * a.top;
+    const int64_t at = (int64_t)row * chunks;
+    Part p = a.part[at];
+    for (int i = 1; i < chunks; ++i) p = joined(p, a.part[at + i], a.l.c);
+    const Results q = results(p);
+    if (tid == 0) {
+        const int label = a.labels ? a.labels[row] : -1;
+        const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * (a.l.f32 ? 4 : 2);
+        put_row(a, row, p, label, label >= 0 && label < a.l.classes ? logit(a.l, z, label) : 0.f);
+    }
+    for (int i = tid; i < n; i += 256) keys[i] = key_of(a.list_value[at * a.top + i], a.list_index[at * a.top + i]);
+    __syncthreads();
+    int total = 0;
+    for (int i = tid; i < n; i += 256) {
+        const u64 key = keys[i];
+        if (!key) continue;
+        int place = 0;
+        for (int l = 0; l < chunks && place < a.top; ++l) {
+            int x = 0, y = a.top;   // entries of the list that come before
+            while (x < y) {
+                const int m = (x + y) >> 1;
+                if (keys[l * a.top + m] > key)
+                    x = m + 1;
+                else
+                    y = m;
+            }
+            place += x;
+        }
+        if (place < a.top) {
+            const Best b = of_key(key);
+            put_top(a, row, place, p, q, b.z, b.i);
+        }
+    }
+    // places that no class takes
+    for (int i = tid; i < n; i += 256) total += keys[i] != 0;
+    __shared__ int sums[4];
+    total = wave_sum(total);
+    if ((tid & 63) == 0) sums[tid >> 6] = total;
+    __syncthreads();
+    total = sums[0] + sums[1] + sums[2] + sums[3];
+    if (tid < a.top && tid >= total) put_top(a, row, tid, p, q, -infinity(), -1);
+}
+
+__device__ __forceinline__ uint32_t pack2(float a, float b) {
+    return (uint32_t)__builtin_bit_cast(u16, (__bf16)a) | (uint32_t)__builtin_bit_cast(u16, (__bf16)b) << 16;
+}
+
+// q = softmax of the teacher's entries v / T, p that of all of the student's
+// logits z / T: loss = T^2 sum q (log q - log p), and with respect to z
+//   dz = dloss T (p - q),
+// entries of one class added up. Every wave of a team keeps entry i in lane
+// i. What a lane writes for a class with an entry it overwrites itself, so
+// that the order of the two stores is that of the program.
+template <bool F32, int W, int V>
+__global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void distill_kernel(const DistillArgs a) {
+    constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W), SIZE = F32 ? 4 : 2;
+    __shared__ Part parts[W];
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+    const int team = W == 1 ? wave : 0, w = W == 1 ? 0 : wave, tid = W == 1 ? lane : (int)threadIdx.x;
+    const int row = (int)blockIdx.x * TEAMS + team, chunk = blockIdx.y;
+    if (row >= a.l.rows) return;
+    const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * SIZE;
+    const int lo = chunk * a.l.chunk, hi = min(a.l.classes, lo + a.l.chunk);
+    int index = -1;
+    float value = 0.f;
+    if (lane < a.k) {
+        index = a.index[(int64_t)row * a.k + lane];
+        value = a.value[(int64_t)row * a.k + lane];
+    }
+    const float weight = a.dloss ? a.dloss[row] : 1.f;
+    Held<F32, W, V> h;
+    h.load(z, lo, hi, tid);
+    const bool bad = __builtin_amdgcn_ballot_w64(index < -1 || index >= a.l.classes) != 0;
+    if (index >= a.l.classes) index = -1;
+    const bool entry = index >= 0;
+    const float z_entry = entry ? logit(a.l, z, index) : 0.f;
+    // the teacher's side; a value that is NaN or +inf makes the mass NaN
+    const float v = entry ? value * a.l.inv_t : -infinity();
+    const float v_most = wave_max(v);
+    const bool some = bad || __builtin_amdgcn_ballot_w64(!(v == -infinity())) != 0;
+    const float e = entry ? expf(v - (v_most == -infinity() ? 0.f : v_most)) : 0.f;
+    float mass = wave_sum(e);
+    if (bad) mass = quiet();
+    const float share = e / mass;
+    Part p;
+    if (a.l.chunks > 1) {
+        p = a.part[(int64_t)row * a.l.chunks];
+        for (int i = 1; i < a.l.chunks; ++i) p = joined(p, a.part[(int64_t)row * a.l.chunks + i], a.l.c);
+    } else {
+        p = team_part<W>(wave_part<F32, W, V>(h, a.l.c), parts, w, a.l.c);
+    }
+    const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
+    const float t_entry = (z_entry - p.m) * a.l.c;
+    if (a.loss && w == 0 && chunk == 0) {
+        const float log_q = v - v_most - logf(mass), log_p = (z_entry - p.m) * a.l.inv_t - LN2 * log2f(p.s);
+        const float sum = wave_sum(share > 0.f ? share * (log_q - log_p) : 0.f);
+        if (lane == 0) a.loss[row] = !some ? 0.f : lost ? quiet() : a.t * a.t * sum;
+    }
+    if (!a.dz) return;
+    char *const d = (char *)a.dz + (int64_t)row * a.ldd * SIZE;
+    auto put = [](char *d, int i, float g) __attribute__((always_inline)) {
+        if constexpr (F32)
+            *(float *)(d + (uint32_t)i * 4) = g;
+        else
+            *(u16 *)(d + (uint32_t)i * 2) = __builtin_bit_cast(u16, (__bf16)g);
+    };
+    // (a row without entries gives nothing, whatever it holds)
+    const float coef = !some ? 0.f : lost ? quiet() : weight * a.t, by = coef / p.s;
+    auto gradient = [&](float x) __attribute__((always_inline)) {
+        return some ? by * __builtin_amdgcn_exp2f((x - p.m) * a.l.c) : 0.f;
+    };
+#pragma unroll
+    for (int v = 0; v < V; ++v) {
+        h.again(v);
+        uint4 x;
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (&x.x)[j] = __float_as_uint(gradient(h.get(v, j)));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (&x.x)[j] = pack2(gradient(h.get(v, 2 * j)), gradient(h.get(v, 2 * j + 1)));
+        }
+        const int f = h.first(v);
+        if (f + VEC <= hi) *(u32x4_any *)(d + (uint32_t)f * SIZE) = __builtin_bit_cast(u32x4_any, x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    // the last classes, where they do not fill a piece
+    const int tail = lo + (hi - lo) / VEC * VEC;
+    if (tid == (hi - lo) / VEC % (W * 64))
+#pragma unroll 1
+        for (int i = tail; i < hi; ++i) put(d, i, gradient(logit(a.l, z, i)));
+    if (!some) return;
+    // this wave's classes with an entry
+    const int piece = entry ? (index - lo) / VEC % (W * 64) : -1;
+    u64 mine = __builtin_amdgcn_ballot_w64(entry && index >= lo && index < hi && piece >> 6 == w);
+    while (mine) {
+        const int i = __builtin_ctzll(mine);
+        mine &= mine - 1;
+        const int cls = __builtin_amdgcn_readlane(index, i), owner = __builtin_amdgcn_readlane(piece, i) & 63;
+        const float q = wave_sum(index == cls ? share : 0.f);
+        const float t = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(t_entry), i));
+        const float g = by * __builtin_amdgcn_exp2f(t) - coef * q;
+        if (lane == owner) put(d, cls, g);
+    }
+}
+
+template <typename A, typename K>
+hipError_t go(K kernel, const A &a, hipStream_t s) {
+    void *p[] = {const_cast<A *>(&a)};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)answer_groups(a.l), (unsigned)a.l.chunks),
+                           dim3(64 * a.l.waves * answer_teams(a.l.waves)), p, 0, s);
+}
+
+template <bool F32>
+hipError_t score_form(const ScoreArgs &a, hipStream_t s) {
+    switch (a.l.waves * 100 + a.l.vecs) {
+        case 101: return go(&score_kernel<F32, 1, 1>, a, s);
+        case 102: return go(&score_kernel<F32, 1, 2>, a, s);
+        case 104: return go(&score_kernel<F32, 1, 4>, a, s);
+        case 402: return go(&score_kernel<F32, 4, 2>, a, s);
+        case 404: return go(&score_kernel<F32, 4, 4>, a, s);
+        case 808: return go(&score_kernel<F32, 8, 8>, a, s);
+    }
+    return hipErrorInvalidValue;
+}
+template <bool F32>
+hipError_t distill_form(const DistillArgs &a, hipStream_t s) {
+    switch (a.l.waves * 100 + a.l.vecs) {
+        case 101: return go(&distill_kernel<F32, 1, 1>, a, s);
+        case 102: return go(&distill_kernel<F32, 1, 2>, a, s);
+        case 104: return go(&distill_kernel<F32, 1, 4>, a, s);
+        case 402: return go(&distill_kernel<F32, 4, 2>, a, s);
+        case 404: return go(&distill_kernel<F32, 4, 4>, a, s);
+        case 808: return go(&distill_kernel<F32, 8, 8>, a, s);
+        case 1608: return go(&distill_kernel<F32, 16, 8>, a, s);
+        case 1612: return go(&distill_kernel<F32, 16, 12>, a, s);
+    }
+    return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_score(const ScoreArgs &a, hipStream_t s) {
+    if (!score_valid(a)) return hipErrorInvalidValue;
+    return a.l.f32 ? score_form<true>(a, s) : score_form<false>(a, s);
+}
+
+hipError_t launch_score_join(const ScoreArgs &a, hipStream_t s) {
+    if (!score_valid(a) || a.l.chunks < 2 || a.l.rows * 256ll > 0xffffffffll) return hipErrorInvalidValue;
+    void *p[] = {const_cast<ScoreArgs *>(&a)};
+    return hipLaunchKernel(reinterpret_cast<const void *>(&score_join_kernel), dim3((unsigned)a.l.rows), dim3(256), p, 0, s);
+}
+
+hipError_t launch_distill(const DistillArgs &a, hipStream_t s) {
+    if (!distill_valid(a)) return hipErrorInvalidValue;
+    return a.l.f32 ? distill_form<true>(a, s) : distill_form<false>(a, s);
+}
+
+}  // namespace gemel

@@ -54,12 +54,15 @@ EXPORTED = ("gemel_create", "gemel_register_model", "gemel_merge",
             "gemel_model_outputs", "gemel_output_shape",
             "gemel_query", "gemel_set_option", "gemel_profile",
             "gemel_last_error", "gemel_destroy",
+            "gemel_log_probs", "gemel_distill", "gemel_distill_backward",
             "gemel_adapter_batch", "gemel_adapter_batch_free",
             "gemel_adapt", "gemel_adapt_backward", "gemel_orthogonalize",
             "gemel_muon_step")
 # Operators that serve and retrain merged layers: not part of CPU builds of
 # the planner alone.
 OPERATORS = EXPORTED[-6:]
+# Answers and distillation: builds of other operators alone lack them.
+ANSWERS = EXPORTED[-9:-6]
 
 _fp = ctypes.POINTER(ctypes.c_float)
 
@@ -94,6 +97,13 @@ class Projection(ctypes.Structure):
                 ("b", ctypes.c_void_p)]
 
 
+class Answers(ctypes.Structure):
+    _fields_ = [("log_prob", ctypes.c_void_p), ("rank", ctypes.c_void_p),
+                ("entropy", ctypes.c_void_p), ("log_sum", ctypes.c_void_p),
+                ("top_indices", ctypes.c_void_p),
+                ("top_log_probs", ctypes.c_void_p)]
+
+
 class KernelStat(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int32), ("launches", ctypes.c_int32),
                 ("flops", ctypes.c_double), ("bytes", ctypes.c_double),
@@ -125,7 +135,7 @@ def _hip_runtimes():
 def load(path):
     """Load another build of the same ABI (e.g. a CPU build of the host
     code used by the tests) with its C signatures declared. Such a build may
-    lack the operators of OPERATORS."""
+    lack the operators of OPERATORS and ANSWERS."""
     return _configure(ctypes.CDLL(path))
 
 
@@ -166,10 +176,12 @@ def _configure(L):
     L.gemel_last_error.restype = ctypes.c_char_p
     L.gemel_destroy.argtypes = [vp]
     for name in EXPORTED:
-        if name != "gemel_last_error" and name not in OPERATORS:
+        if name != "gemel_last_error" and name not in OPERATORS + ANSWERS:
             getattr(L, name).restype = ctypes.c_int32
     if hasattr(L, OPERATORS[0]):
         _configure_operators(L)
+    if hasattr(L, ANSWERS[0]):
+        _configure_answers(L)
     return L
 
 
@@ -187,6 +199,19 @@ def _configure_operators(L):
     L.gemel_muon_step.argtypes = [vp, i32, i32, i32, vp, vp, vp, vp, f32,
                                   f32, f32, i32, i32, vp]
     for name in OPERATORS:
+        getattr(L, name).restype = i32
+
+
+def _configure_answers(L):
+    vp, i32, i64 = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64
+    f32 = ctypes.c_float
+    L.gemel_log_probs.argtypes = [vp, i32, i32, vp, i64, i32, vp, i32, f32,
+                                  ctypes.POINTER(Answers), vp]
+    L.gemel_distill.argtypes = [vp, i32, i32, vp, i64, i32, vp, vp, i32, f32,
+                                vp, vp]
+    L.gemel_distill_backward.argtypes = [vp, i32, i32, vp, vp, i64, i32, vp,
+                                         vp, i32, f32, vp, i64, vp, vp]
+    for name in ANSWERS:
         getattr(L, name).restype = i32
 
 
@@ -727,3 +752,119 @@ class Context:
             self._stream(stream, w, momentum_buffer, g, copy)))
         self._written(w, momentum_buffer, copy)
         return w
+
+    # -- answers of merged models, and their distillation --
+    def _logits(self, logits):
+        """Rows, classes and type code of logits (bf16 or float32 in every
+        context), rows contiguous."""
+        torch = _torch()
+        if logits.dim() != 2:
+            raise ValueError("logits must be [rows, classes]")
+        if logits.dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError("logits must be float32 or bfloat16, are "
+                             f"{logits.dtype}")
+        rows, classes = logits.shape
+        _int32("rows", rows)
+        _int32("classes", classes)
+        self._tensor("logits", logits, (rows, classes), logits.dtype,
+                     contiguous=False)
+        return rows, classes, F32 if logits.dtype == torch.float32 else BF16
+
+    def log_probs(self, logits, labels=None, top=0, temperature=1.0,
+                  needs=None, outputs=None, stream=None):
+        """What logits [rows, classes] (bf16 or float32) answer, as a dict:
+        "log_prob" of each row's label and its "rank" (classes before it;
+        both with labels, int32 [rows], -1: none), "entropy", "log_sum", and
+        with top > 0 "top_indices" (int32, best first, of equal ones the
+        lower index) and "top_log_probs" [rows, top] of the softmax of
+        logits / temperature. Classes of -inf are not offered: -1 and -inf
+        stand where fewer than `top` are. needs: names of those wanted (None:
+        all); outputs: tensors to write, by name (others are made)."""
+        torch = _torch()
+        rows, classes, code = self._logits(logits)
+        _int32("top", top)
+        f32, i32 = torch.float32, torch.int32
+        kinds = {"entropy": ((rows,), f32), "log_sum": ((rows,), f32)}
+        if labels is not None:
+            self._tensor("labels", labels, (rows,), i32)
+            kinds.update(log_prob=((rows,), f32), rank=((rows,), i32))
+        if top > 0:
+            kinds.update(top_indices=((rows, top), i32),
+                         top_log_probs=((rows, top), f32))
+        res, a = {}, Answers()
+        for name in kinds if needs is None else needs:
+            if name not in kinds:
+                raise ValueError(f"no answer {name!r} (of these arguments)")
+            shape, dt = kinds[name]
+            t = outputs.get(name) if outputs else None
+            if t is None:
+                t = self._empty(logits, shape, dt, stream)
+            else:
+                self._tensor(f"outputs[{name!r}]", t, shape, dt)
+            res[name] = t
+            setattr(a, name, t.data_ptr())
+        self._check(self._lib.gemel_log_probs(
+            self._h, rows, classes, logits.data_ptr(), self._stride(logits),
+            code, None if labels is None else labels.data_ptr(), top,
+            temperature, a,
+            self._stream(stream, logits, labels, *res.values())))
+        if outputs:
+            self._written(*(outputs.get(name) for name in res))
+        return res
+
+    def _entries(self, logits, indices, values):
+        rows, classes, code = self._logits(logits)
+        if indices.dim() != 2:
+            raise ValueError("indices must be [rows, entries]")
+        k = indices.shape[1]
+        self._tensor("indices", indices, (rows, k), _torch().int32)
+        self._tensor("values", values, (rows, k), _torch().float32)
+        return rows, classes, code, k
+
+    def distill(self, logits, indices, values, temperature=1.0, out=None,
+                stream=None):
+        """Loss [rows] of logits [rows, classes] against a teacher's best
+        ones: temperature^2 * sum of q (log q - log p), q the softmax of
+        values / temperature over the row's entries (indices int32 and values
+        float32 [rows, entries], as the teacher's log_probs gives them; class
+        -1 or value -inf: no entry), p that of all logits / temperature."""
+        rows, classes, code, k = self._entries(logits, indices, values)
+        loss = out
+        if loss is None:
+            loss = self._empty(logits, (rows,), _torch().float32, stream)
+        else:
+            self._tensor("out", loss, (rows,), _torch().float32)
+        self._check(self._lib.gemel_distill(
+            self._h, rows, classes, logits.data_ptr(), self._stride(logits),
+            code, indices.data_ptr(), values.data_ptr(), k, temperature,
+            loss.data_ptr(),
+            self._stream(stream, logits, indices, values, loss)))
+        if out is not None:
+            self._written(out)
+        return loss
+
+    def distill_backward(self, dloss, logits, indices, values,
+                         temperature=1.0, loss=None, out=None, stream=None):
+        """Gradient of distill for dloss [rows] (None: all 1) with respect to
+        the logits, in their type. loss: a tensor [rows] that receives the
+        losses too, from the same pass."""
+        rows, classes, code, k = self._entries(logits, indices, values)
+        f32 = _torch().float32
+        for name, t in (("dloss", dloss), ("loss", loss)):
+            if t is not None:
+                self._tensor(name, t, (rows,), f32)
+        d = out
+        if d is None:
+            d = self._empty(logits, (rows, classes), logits.dtype, stream)
+        else:
+            self._tensor("out", d, (rows, classes), logits.dtype,
+                         contiguous=False)
+        self._check(self._lib.gemel_distill_backward(
+            self._h, rows, classes,
+            None if dloss is None else dloss.data_ptr(), logits.data_ptr(),
+            self._stride(logits), code, indices.data_ptr(),
+            values.data_ptr(), k, temperature, d.data_ptr(), self._stride(d),
+            None if loss is None else loss.data_ptr(),
+            self._stream(stream, dloss, logits, indices, values, d, loss)))
+        self._written(out, loss)
+        return d

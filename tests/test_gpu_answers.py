@@ -1,0 +1,378 @@
+"""Answers off logits and distillation on the GPU, against their definitions
+in 64 bits: types, odd numbers of classes, rows in one piece and in chunks,
+strides, masks, ties, values that are not finite, streams and graphs.
+
+Tolerances count roundings of 2^-24: a softmax's sum takes at most 128
+additions in a lane and 12 between lanes and parts, an exponential 2 and three
+for its argument (relative to that argument), a logarithm 2, and a bit of
+room: 300 for the logarithm of a sum, 4 for each unit of the distance of a
+logit from its row's largest. Denormal results may be flushed."""
+
+import math
+
+import pytest
+
+from paper_2201_07705_amd import gemel as G
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = G.Context(0, "bf16")
+    yield c
+    c.close()
+
+
+def half_step(dtype):
+    import torch
+    return torch.finfo(dtype).eps / 2
+
+
+def make(rows, classes, dtype, seed=0, pad=0, shift=0, spread=3.0):
+    """Logits with a few likely classes, as columns of a wider matrix."""
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    wide = torch.randn(rows, classes + pad + shift, device="cuda", generator=gen) * spread
+    z = wide.to(getattr(torch, dtype))[:, shift:shift + classes]
+    if classes > 1:
+        z[torch.arange(rows), torch.randint(classes, (rows,), device="cuda", generator=gen)] = 9.0
+    return z
+
+
+def answers64(z, labels, top, t=1.0):
+    import torch
+    raw = z.double()
+    x = raw / t
+    bad = (raw.isnan() | (raw == math.inf)).any(1)
+    empty = (raw == -math.inf).all(1) & ~bad
+    m = x.amax(1, keepdim=True)
+    m = torch.where(m.isfinite(), m, 0.0)
+    e = (x - m).exp()
+    s = e.sum(1, keepdim=True)
+    lp = x - m - s.log()
+    p = e / s
+    nan = torch.tensor(math.nan, device=z.device, dtype=torch.float64)
+    entropy = -torch.where(p > 0, p * lp, 0.0).sum(1)
+    out = {"entropy": torch.where(empty, 0.0, entropy), "log_sum": (m + s.log())[:, 0]}
+    classes = z.shape[1]
+    value, order = torch.sort(torch.where(raw.isnan(), -math.inf, raw), dim=1, descending=True, stable=True)
+    n = min(top, classes)
+    index = torch.full((z.shape[0], top), -1, device=z.device)
+    best = torch.full((z.shape[0], top), -math.inf, device=z.device, dtype=torch.float64)
+    offered = value[:, :n] > -math.inf
+    index[:, :n] = torch.where(offered, order[:, :n], -1)
+    best[:, :n] = torch.where(offered, lp.gather(1, order[:, :n]), -math.inf)
+    out["top_indices"] = torch.where(bad[:, None], -1, index)
+    out["top_log_probs"] = torch.where(bad[:, None], nan, best)
+    label = labels.long()
+    known = (label >= 0) & (label < classes)
+    at = torch.where(known, label, 0)[:, None]
+    mine = raw.gather(1, at)
+    ids = torch.arange(classes, device=z.device)
+    before = (raw > mine).sum(1) + ((raw == mine) & (ids < at)).sum(1)
+    out["rank"] = torch.where(known & ~bad, before, -1)
+    got = torch.where(empty | (mine[:, 0] == -math.inf), -math.inf, lp.gather(1, at)[:, 0])
+    out["log_prob"] = torch.where(label == -1, 0.0, torch.where(known & ~bad, got, nan))
+    out["entropy"] = torch.where(bad, nan, out["entropy"])
+    out["log_sum"] = torch.where(bad, nan, out["log_sum"])
+    return out
+
+
+def same(got, want, tol, what):
+    """Equal where the wanted value is not finite, else within tol."""
+    import torch
+    got, want = got.double(), want.double()
+    # (results are float32: what is beyond its range by half a step rounds to infinity)
+    beyond = torch.finfo(torch.float32).max * (1 + U)
+    want = torch.where(want.abs() >= beyond, torch.sign(want) * math.inf, want)
+    fin = want.isfinite()
+    eq = (got == want) | (got.isnan() & want.isnan())
+    off = torch.where(fin, (got - want).abs() - tol, torch.where(eq, -1.0, math.inf))
+    off = torch.where(off.isnan(), math.inf, off)
+    worst = off.max().item()
+    assert worst <= 0, f"{what}: off by {worst} more than allowed at {int(off.argmax())}"
+
+
+def check(ctx, z, labels, top, t=1.0, **kw):
+    import torch
+    got = ctx.log_probs(z, labels=labels, top=top, temperature=t, **kw)
+    want = answers64(z, labels, top, t)
+    assert set(got) == {"entropy", "log_sum", "log_prob", "rank"} | ({"top_indices", "top_log_probs"} if top else set())
+    n = math.log(z.shape[1]) + 1
+    for name in got:
+        if name in ("rank", "top_indices"):
+            assert got[name].dtype == torch.int32
+            assert torch.equal(got[name].long(), want[name].long()), name
+            continue
+        # (a log probability's size is its distance from the largest, log n aside)
+        size = torch.where(want[name].isfinite(), want[name].abs(), 0.0)
+        same(got[name], want[name], U * ((300 + 4 * size) * (n if name == "entropy" else 1) + 4 * n) + 1e-37, name)
+    return got
+
+
+WIDTHS = [1, 2, 3, 7, 8, 9, 63, 80, 255, 257, 511, 513, 1000, 1001, 1025, 2047, 2049, 4095, 4097, 8191, 8193, 16383,
+          16385, 32767, 32769, 65537, 100003]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS)
+def test_log_probs_of_any_width(ctx, classes, dtype):
+    import torch
+    rows = 5 if classes > 4000 else 37
+    z = make(rows, classes, dtype, seed=classes, pad=classes % 3, shift=classes % 5)
+    labels = torch.randint(-1, classes, (rows,), device="cuda", dtype=torch.int32)
+    check(ctx, z, labels, min(20, classes + 2))
+    check(ctx, z, labels, 1, t=0.7)
+    check(ctx, z, labels, 64, t=3.0)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", [3, 100, 1000, 5000, 40000])
+@pytest.mark.parametrize("kind", ["constant", "few values", "masked", "one offered", "lowest", "zeros of both signs", "ascending",
+                                  "descending", "huge", "one lane"])
+def test_ties_and_masks(ctx, kind, classes, dtype):
+    import torch
+    rows = 6
+    z = make(rows, classes, dtype, seed=3)
+    dt = z.dtype
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    if kind == "constant":
+        z = torch.full_like(z, 1.5)
+    elif kind == "few values":
+        z = torch.randint(3, (rows, classes), device="cuda", generator=gen).to(dt)
+    elif kind == "masked":
+        z[torch.rand(rows, classes, device="cuda", generator=gen) < 0.7] = -math.inf
+        z[1] = -math.inf
+        z[2, :classes // 2] = -math.inf
+    elif kind == "one offered":
+        z = torch.full_like(z, -math.inf)
+        z[torch.arange(rows), torch.arange(rows, device="cuda") * (classes - 1) // (rows - 1)] = -2.0
+    elif kind == "lowest":
+        z[:, ::2] = torch.finfo(dt).min
+        z[1] = torch.finfo(dt).min
+        z[2] = torch.finfo(dt).max / 2
+    elif kind == "zeros of both signs":
+        z = torch.where(torch.rand(rows, classes, device="cuda", generator=gen) < 0.5, 0.0, -0.0).to(dt)
+    elif kind in ("ascending", "descending"):
+        z = (torch.arange(classes, device="cuda") * (0.01 if kind == "ascending" else -0.01)).to(dt).expand(rows, -1).contiguous()
+    elif kind == "huge":
+        z = z * 1e9
+    elif kind == "one lane":
+        # the best classes all in pieces that one lane holds
+        z[:, :min(classes, 8)] = 30 + torch.arange(min(classes, 8), device="cuda").to(dt)
+    labels = torch.tensor([0, classes - 1, classes // 2, 1, -1, classes // 3], device="cuda", dtype=torch.int32)
+    for top in (1, 7, 64):
+        check(ctx, z, labels, top)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", [5, 1000, 3001, 40000])
+def test_rows_that_are_not_finite_stay_alone(ctx, classes, dtype):
+    import torch
+    z = make(9, classes, dtype, seed=8)
+    labels = torch.arange(9, device="cuda", dtype=torch.int32) % classes
+    clean = ctx.log_probs(z, labels=labels, top=5)
+    for where in (0, classes - 1, classes // 2):
+        x = z.clone()
+        x[2, where] = math.nan
+        x[4, where] = math.inf
+        x[6] = math.nan
+        got = check(ctx, x, labels, 5)
+        keep = [0, 1, 3, 5, 7, 8]
+        for name in got:
+            assert torch.equal(got[name][keep], clean[name][keep]), name
+
+
+def test_labels_that_are_no_class(ctx):
+    import torch
+    z = make(6, 100, "float32")
+    labels = torch.tensor([-1, 100, -2, 2 ** 31 - 1, -2 ** 31, 99], device="cuda", dtype=torch.int32)
+    check(ctx, z, labels, 0)
+
+
+def test_needs_and_outputs(ctx):
+    import torch
+    z = make(10, 333, "bfloat16")
+    labels = torch.zeros(10, device="cuda", dtype=torch.int32)
+    whole = ctx.log_probs(z, labels=labels, top=4)
+    for name in whole:
+        alone = ctx.log_probs(z, labels=labels, top=4, needs=(name,))
+        assert list(alone) == [name] and torch.equal(alone[name], whole[name])
+    out = {name: torch.full_like(v, 77) for name, v in whole.items()}
+    version = {name: v._version for name, v in out.items()}
+    got = ctx.log_probs(z, labels=labels, top=4, outputs=out)
+    for name in out:
+        assert got[name] is out[name] and torch.equal(out[name], whole[name]) and out[name]._version > version[name]
+    assert ctx.log_probs(z[:0], labels=labels[:0], top=4)["top_indices"].shape == (0, 4)
+
+
+def distill64(z, index, value, t, dloss):
+    import torch
+    x = z.double() / t
+    classes = z.shape[1]
+    used = (index >= 0) & (index < classes) & (value != -math.inf)
+    wrong = ((index < -1) | (index >= classes)).any(1)
+    v = torch.where(used, value.double() / t, -math.inf)
+    some = used.any(1) | wrong
+    vm = v.amax(1, keepdim=True)
+    e = torch.where(used, (v - torch.where(vm == -math.inf, 0.0, vm)).exp(), 0.0)
+    q = e / e.sum(1, keepdim=True)
+    lq = v - vm - e.sum(1, keepdim=True).log()
+    m = x.amax(1, keepdim=True)
+    m = torch.where(m == -math.inf, 0.0, m)
+    s = (x - m).exp().sum(1, keepdim=True)
+    lp = x - m - s.log()
+    p = (x - m).exp() / s
+    at = torch.where(used, index, 0).long()
+    mine = lp.gather(1, at)
+    loss = t * t * torch.where(q == 0, 0.0, q * (lq - mine)).sum(1)
+    share = torch.zeros_like(x).scatter_add(1, at, torch.where(used, q, 0.0))
+    g = (p - share) * (t * dloss.double()[:, None])
+    lost = some & (wrong | ~s[:, 0].isfinite() | (s[:, 0] == 0) | e.sum(1).isnan() | (vm[:, 0] == math.inf))
+    loss = torch.where(lost, math.nan, torch.where(some, loss, 0.0))
+    g = torch.where(lost[:, None], math.nan, torch.where(some[:, None], g, 0.0))
+    # what the tolerances depend on
+    far = torch.where(mine.isfinite() & used, (lq - mine).abs(), 0.0).amax(1)
+    span = torch.where(v.isfinite(), (v - vm).abs(), 0.0).amax(1) + torch.where(mine.isfinite(), mine.abs(), 0.0).amax(1)
+    # (nothing is allowed where the distance is infinite: p is 0 there)
+    dist = torch.where(x.isfinite() & m.isfinite(), (x - m).abs(), 0.0)
+    return loss, g, t * t * U * (400 + 8 * span + (100 + 4 * span) * far), \
+        (t * dloss.double().abs())[:, None] * U * ((300 + 4 * dist) * p.nan_to_num() + (100 + 4 * span[:, None]) * share.nan_to_num())
+
+
+def check_distill(ctx, z, index, value, t=1.0, dloss=None, out=None):
+    import torch
+    one = torch.ones(z.shape[0], device="cuda") if dloss is None else dloss
+    loss, g, loss_tol, g_tol = distill64(z, index, value, t, one)
+    got_loss = torch.full((z.shape[0],), 55.0, device="cuda")
+    got = ctx.distill_backward(dloss, z, index, value, temperature=t, loss=got_loss, out=out)
+    assert got.dtype == z.dtype and got.shape == z.shape
+    g_tol = g_tol + half_step(z.dtype) * (g.abs().nan_to_num() + g_tol) + 1e-37
+    same(got, g, g_tol, "dlogits")
+    same(got_loss, loss, loss_tol + 1e-37, "loss")
+    alone = ctx.distill(z, index, value, temperature=t)
+    same(alone, loss, loss_tol + 1e-37, "loss alone")
+    return got_loss, got
+
+
+def teacher(z, k, seed=1, noise=0.5):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = z.float() + noise * torch.randn(z.shape, device="cuda", generator=gen)
+    value, index = torch.topk(x, min(k, z.shape[1]), dim=1)
+    return index.int(), value
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS + [131072, 131073, 300001])
+def test_distill_of_any_width(ctx, classes, dtype):
+    import torch
+    rows = 3 if classes > 4000 else 33
+    z = make(rows, classes, dtype, seed=classes, pad=classes % 3, shift=classes % 5)
+    dloss = torch.rand(rows, device="cuda") - 0.3
+    for k, t in ((1, 1.0), (10, 2.0), (64, 0.8)):
+        index, value = teacher(z, k)
+        check_distill(ctx, z, index, value, t, dloss)
+    wide = torch.full((rows, classes + 9), 7.0, device="cuda", dtype=z.dtype)
+    check_distill(ctx, z, index, value, 1.0, None, out=wide[:, 4:4 + classes])
+    assert (wide[:, :4] == 7).all() and (wide[:, 4 + classes:] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", [6, 1000, 5000, 140001])
+def test_entries_of_every_kind(ctx, classes, dtype):
+    import torch
+    z = make(14, classes, dtype, seed=5)
+    index, value = teacher(z, 6)
+    inf = math.inf
+    index[1] = -1                          # no entry
+    value[2] = -inf                        # none that counts
+    index[3, 2:] = -1
+    index[4] = index[4, 0]                 # one class over and over
+    index[5, 3] = index[5, 1]
+    value[6, 1:] = -inf                    # one that counts
+    index[7, 0] = classes                  # no class
+    index[8, 5] = -2
+    value[9, 2] = math.nan
+    value[10, 2] = inf
+    z[11, index[11, 1].long()] = -inf      # not offered by the student
+    z[12, :] = -inf
+    z[13, ::2] = torch.finfo(z.dtype).min
+    loss, g = check_distill(ctx, z, index, value, 2.0)
+    assert loss[1] == 0 and loss[2] == 0 and not g[1:3].any() and loss[11] == inf
+    # a row without entries gives nothing, whatever it holds
+    z[1] = math.nan
+    z[2, 0] = inf
+    check_distill(ctx, z, index, value, 2.0)
+
+
+def test_gradient_against_differences(ctx):
+    """dlogits in float32 against symmetric differences of the loss in 64
+    bits: h^2 / 6 of the third derivative, below 4 / T^3, and 2^-53 of the loss over h."""
+    import torch
+    t, h = 2.0, 1e-4
+    z = make(3, 40, "float32", spread=1.0)
+    index, value = teacher(z, 7)
+    dloss = torch.tensor([0.5, -2.0, 1.0], device="cuda")
+    got = ctx.distill_backward(dloss, z, index, value, temperature=t).double()
+    zd = z.double()
+    for c in range(40):
+        step = torch.zeros_like(zd)
+        step[:, c] = h
+        diff = (distill64(zd + step, index, value, t, dloss)[0] - distill64(zd - step, index, value, t, dloss)[0]) / (2 * h)
+        tol = 2.0 * (t * t * 4 / t ** 3 * h * h / 6 + 100 * 2.0 ** -52 / h) + t * 2 * U * 800
+        assert ((diff * dloss.double() - got[:, c]).abs() <= tol).all()
+
+
+@pytest.mark.parametrize("classes,dtype", [(1000, "bfloat16"), (140001, "bfloat16"), (70000, "float32")])
+def test_another_stream_and_a_graph(ctx, classes, dtype):
+    """The same bits from another stream, and from a captured call replayed
+    over new inputs between eager work."""
+    import torch
+    z = make(7, classes, dtype)
+    labels = torch.arange(7, device="cuda", dtype=torch.int32)
+    index, value = teacher(z, 8)
+    dloss = torch.rand(7, device="cuda")
+    stream = torch.cuda.Stream()
+
+    def call(stream=None, outputs=None, loss=None, out=None):
+        a = ctx.log_probs(z, labels=labels, top=6, outputs=outputs, stream=stream)
+        loss = torch.empty(7, device="cuda") if loss is None else loss
+        return {**a, "loss": loss, "d": ctx.distill_backward(dloss, z, index, value, loss=loss, out=out, stream=stream)}
+
+    want = call()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        got = call(stream=stream)
+    stream.synchronize()
+    for name in want:
+        assert torch.equal(got[name], want[name]), name
+    graph = torch.cuda.CUDAGraph()
+    kept = {name: torch.zeros_like(v) for name, v in want.items()}
+    outputs = {name: kept[name] for name in kept if name not in ("loss", "d")}
+    with torch.cuda.graph(graph, stream=stream):
+        call(stream=torch.cuda.current_stream(), outputs=outputs, loss=kept["loss"], out=kept["d"])
+    for seed in range(4):
+        z.copy_(make(7, classes, dtype, seed=20 + seed))
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in want:
+            assert torch.equal(kept[name], want[name]), (seed, name)
+
+
+def test_a_wide_call_that_was_not_made_before_is_not_captured(ctx):
+    import torch
+    z = make(4, 200001, "float32")
+    stream = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        with pytest.raises(G.GemelError) as e:
+            ctx.log_probs(z, top=64, outputs={}, stream=torch.cuda.current_stream())
+        z.add_(0)
+    assert e.value.code == G.ESTATE
