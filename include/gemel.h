@@ -918,6 +918,67 @@ gemel_status gemel_distill_backward(gemel_ctx *ctx, int32_t rows,
                                     int64_t dlogits_stride, float *loss,
                                     void *hip_stream);
 
+/*
+ * ---- Merged layers in 4 bits ----
+ *
+ * A quarter of the memory of bf16 weights: blocks of 32 values of a row, each
+ * a 4-bit floating-point number, share a power of two (microscaling). The
+ * weights of a merged projection are quantised once and multiply rows as
+ * they are, or rows that are quantised too. The conventions of the calls
+ * above hold; rows 0 is no error and touches nothing.
+ */
+
+/*
+ * A matrix [rows][cols] (rows <= 2^22, 1 <= cols <= 2^20) as codes and scales.
+ *  codes   rows of P = 128 * ceil(cols / 256) bytes. Column c of a row is the
+ *          low (c even) or high half of byte c / 2: sign bit 8, and magnitude
+ *          0 .. 7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6. Columns beyond cols are zeros.
+ *  scales  [ceil(cols / 512)][rows][16] bytes: 2^(byte - 127), 255 for NaN.
+ *          Block b (columns 32 b .. 32 b + 31) of a row has byte 4 (b % 4) +
+ *          b % 16 / 4 of its 16 in group b / 16; blocks beyond cols have 0.
+ * Both are device memory aligned to 16 bytes.
+ */
+typedef struct gemel_mx {
+    int32_t rows, cols;
+    void *codes, *scales;
+} gemel_mx;
+
+/*
+ * Quantise x (out->rows by out->cols, of dtype GEMEL_F32 or GEMEL_BF16 in
+ * every context, rows x_stride apart) into the memory that out describes:
+ * a block's scale is 2^(floor(log2 of its largest magnitude) - 2), at least
+ * 2^-127, and each value becomes the nearest one there is, ties to the even
+ * code, at most 6 scales. A block that holds a value that is not finite is
+ * NaN.
+ * Errors: EINVAL, EDEVICE.
+ */
+gemel_status gemel_mx_quantize(gemel_ctx *ctx, const void *x,
+                               int64_t x_stride, int32_t dtype,
+                               const gemel_mx *out, void *hip_stream);
+
+/* The values that q's codes stand for, as dtype (exact, but for those beyond
+ * its range). Errors: EINVAL, EDEVICE. */
+gemel_status gemel_mx_dequantize(gemel_ctx *ctx, const gemel_mx *q, void *out,
+                                 int64_t out_stride, int32_t dtype,
+                                 void *hip_stream);
+
+/*
+ * y = x W^T + bias: weight [n_out][n_in] quantised, bias float32 [n_out] or
+ * NULL, y [rows][n_out] of the context's type, rows y_stride apart. The rows
+ * are either x [rows][n_in] of the context's type, multiplied unrounded, or
+ * xq [rows][n_in], quantised; the other one is NULL. Products are exact and
+ * sums float32, with the exceptions that x of float32 loses what is below
+ * 2^-126, and that a value of xq or weight is taken with its scale whatever
+ * it is (products below 2^-126 may be dropped). A row of x, or a block, that
+ * holds a value that is not finite gives rows, or columns, that are not
+ * finite.
+ * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
+ */
+gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x,
+                              int64_t x_stride, const gemel_mx *xq,
+                              const gemel_mx *weight, const float *bias,
+                              void *y, int64_t y_stride, void *hip_stream);
+
 /* Description of the last error (see general conventions). */
 const char *gemel_last_error(const gemel_ctx *ctx);
 

@@ -1,0 +1,205 @@
+// Products of rows that are not quantised (bf16, or float32 as three bf16
+// planes whose sum they are: every product is then exact and sums are
+// float32) with 4-bit weights, and of few quantised rows.
+//
+// Reading the weights bounds them: a lane loads the 32 codes of one block of
+// a weight row in one piece, and its registers are operands of the matrix
+// cores as soon as the hardware has made bf16 of them (8 codes are 4
+// conversions). The depth's order within 128 columns is the codes': lane
+// group g holds the block g, and the rows are read to match.
+#include <hip/hip_runtime.h>
+
+#include "mx_args.h"
+#include "mx_device.h"
+
+namespace gemel {
+
+namespace {
+
+typedef mx_f32x4 f32x4;
+enum { ACT_BF16, ACT_PLANES, ACT_MX };
+
+// Up to 16 rows: 16 outputs to a workgroup, whose waves take turns at the
+// groups of 512 columns. One launch: what counts is latency.
+template <int ACT>
+__global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
+    __shared__ f32x4 sums[16][64];
+    const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6));
+    const int N = a.w.rows, K = a.w.cols, groups = (K + MX_GROUP - 1) / MX_GROUP, n0 = blockIdx.x * 16;
+    const int64_t pitch = mx_pitch(K);
+    const int n = min(n0 + l16, N - 1), m = min(l16, a.M - 1);
+    const uint8_t *codes = a.w.codes + n * pitch + g * 16, *scales = a.w.scales + n * 16ll + g * 4;
+    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+    for (int kg = wave; kg < groups; kg += a.waves) {
+        const int parts = min(4, (int)(pitch / 64) - kg * 4);   // of 128 columns that are there
+        uint4 w[4];
+#pragma unroll
+        for (int s = 0; s < 4; ++s) w[s] = s < parts ? *(const uint4 *)(codes + kg * 256ll + s * 64) : uint4{0, 0, 0, 0};
+        const uint32_t sw = *(const uint32_t *)(scales + (int64_t)kg * N * 16);
+        if constexpr (ACT == ACT_MX) {
+            uint4 x[4];
+            const uint8_t *xc = a.q.codes + m * pitch + kg * 256ll + g * 16;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) x[s] = s < parts ? *(const uint4 *)(xc + s * 64) : uint4{0, 0, 0, 0};
+            const uint32_t sx = *(const uint32_t *)(a.q.scales + ((int64_t)kg * a.M + m) * 16 + g * 4);
+            // (of steps that are not there the scales are zeros, 2^-127)
+            acc = mx_mul<0>(__builtin_bit_cast(i32x4, w[0]), __builtin_bit_cast(i32x4, x[0]), acc, (int)sw, (int)sx);
+            acc = mx_mul<1>(__builtin_bit_cast(i32x4, w[1]), __builtin_bit_cast(i32x4, x[1]), acc, (int)sw, (int)sx);
+            acc = mx_mul<2>(__builtin_bit_cast(i32x4, w[2]), __builtin_bit_cast(i32x4, x[2]), acc, (int)sw, (int)sx);
+            acc = mx_mul<3>(__builtin_bit_cast(i32x4, w[3]), __builtin_bit_cast(i32x4, x[3]), acc, (int)sw, (int)sx);
+        } else {
+            constexpr int P = ACT == ACT_PLANES ? 3 : 1;
+            const int c0 = kg * MX_GROUP + g * 32;
+            auto mul = [&](int s, int i, const uint4 &x) __attribute__((always_inline)) {
+                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_bf16((&w[s].x)[i], mx_scale(sw >> s * 8 & 255)),
+                                                              __builtin_bit_cast(mx_bf16x8, x), acc, 0, 0, 0);
+            };
+#pragma unroll 1
+            for (int p = 0; p < P; ++p) {
+                const u16 *row = a.x + m * a.ldx + p * a.plane;
+                if ((kg + 1) * MX_GROUP <= K) {
+                    uint4 x[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) x[i] = get_16b(row + c0 + (i >> 2) * 128 + (i & 3) * 8);
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) mul(i >> 2, i & 3, x[i]);
+                } else {
+#pragma unroll
+                    for (int s = 0; s < 4; ++s) {
+                        if (s >= parts) break;
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) mul(s, i, mx_chunk(row, c0 + s * 128 + i * 8, K));
+                    }
+                }
+            }
+        }
+    }
+    sums[wave][lane] = acc;
+    __syncthreads();
+    if (wave) return;
+    for (int i = 1; i < a.waves; ++i) acc += sums[i][lane];
+    if (l16 < a.M && n0 + 4 * g < N)
+        mx_put(a.y, a.ldy, a.f32, l16, n0 + 4 * g, N, acc + mx_bias(a.bias, n0 + 4 * g, N));
+}
+
+// 16 MB rows and 256 outputs to a workgroup of 8 waves, 32 outputs to a wave,
+// over a slice of the depth. Steps of 128 columns of the rows pass through
+// two buffers of LDS (16-byte chunk c of row r at chunk c ^ r % 16: the
+// fragment reads of 16 rows fall on distinct banks), the next step's rows and
+// codes being loaded while this one is multiplied.
+template <int P, int MB>
+__global__ __launch_bounds__(512) void mx_rows_kernel(const MxRows a) {
+    constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = (CHUNKS + 511) / 512;
+    __shared__ uint4 st[2][CHUNKS];
+    const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int N = a.w.rows, K = a.w.cols, n0 = blockIdx.x * 256 + wave * 32, m0 = blockIdx.z * ROWS;
+    const int64_t pitch = mx_pitch(K);
+    const int step0 = (int)blockIdx.y * a.per * 4, steps = min((int)(pitch / 64) - step0, a.per * 4);
+    const uint8_t *codes[2], *scales[2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int n = min(n0 + j * 16 + l16, N - 1);
+        codes[j] = a.w.codes + n * pitch + g * 16;
+        scales[j] = a.w.scales + n * 16ll + g * 4;
+    }
+    uint4 x[LOADS], w[2], w_next[2];
+    uint32_t sw[2] = {0, 0}, sw_next[2] = {0, 0};
+    auto load = [&](int step) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int id = i * 512 + tid, p = id / (ROWS * 16), r = id / 16 % ROWS, c = step * 128 + (id & 15) * 8;
+            if (CHUNKS % 512 == 0 || id < CHUNKS)
+                x[i] = mx_chunk(a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx, c, K);
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w_next[j] = *(const uint4 *)(codes[j] + step * 64ll);
+            sw_next[j] = *(const uint32_t *)(scales[j] + (int64_t)(step >> 2) * N * 16);
+        }
+    };
+    auto store = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i) {
+            const int id = i * 512 + tid, r = id / 16;
+            if (CHUNKS % 512 == 0 || id < CHUNKS) st[buf][r * 16 + ((id & 15) ^ (r & 15))] = x[i];
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            w[j] = w_next[j];
+            sw[j] = sw_next[j];
+        }
+    };
+    f32x4 acc[2][MB];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) acc[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    load(step0);
+    for (int k = 0; k < steps; ++k) {
+        store(k & 1);
+        __syncthreads();
+        if (k + 1 < steps) load(step0 + k + 1);
+        const int s = (k & 3) * 8;   // (slices begin at whole groups)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mx_bf16x8 f[2];
+#pragma unroll
+            for (int j = 0; j < 2; ++j) f[j] = mx_bf16((&w[j].x)[i], mx_scale(sw[j] >> s & 255));
+#pragma unroll
+            for (int p = 0; p < P; ++p)
+#pragma unroll
+                for (int b = 0; b < MB; ++b) {
+                    const mx_bf16x8 v = __builtin_bit_cast(mx_bf16x8, st[k & 1][(p * ROWS + b * 16 + l16) * 16 + ((4 * g + i) ^ l16)]);
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) acc[j][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j], v, acc[j][b], 0, 0, 0);
+                }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const int n = n0 + j * 16 + 4 * g;
+        if (n >= N) continue;
+        const f32x4 bias = mx_bias(a.slices == 1 ? a.bias : nullptr, n, N);
+#pragma unroll
+        for (int b = 0; b < MB; ++b) {
+            const int m = m0 + b * 16 + l16;
+            if (m >= a.M) continue;
+            if (a.slices > 1)
+                *(f32x4 *)(a.part + ((int64_t)blockIdx.y * a.M + m) * a.ldp + n) = acc[j][b];
+            else
+                mx_put(a.y, a.ldy, a.f32, m, n, N, acc[j][b] + bias);
+        }
+    }
+}
+
+template <typename K>
+hipError_t go(K kernel, const MxRows &a, dim3 grid, int threads, hipStream_t s) {
+    void *p[] = {const_cast<MxRows *>(&a)};
+    return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3((unsigned)threads), p, 0, s);
+}
+template <int P>
+hipError_t many(const MxRows &a, hipStream_t s) {
+    const int mb = a.M <= 32 ? 2 : a.M <= 48 ? 3 : 4;
+    const dim3 grid((unsigned)((a.w.rows + 255) / 256), (unsigned)a.slices, (unsigned)((a.M + mb * 16 - 1) / (mb * 16)));
+    return mb == 2 ? go(&mx_rows_kernel<P, 2>, a, grid, 512, s) : mb == 3 ? go(&mx_rows_kernel<P, 3>, a, grid, 512, s)
+                                                                          : go(&mx_rows_kernel<P, 4>, a, grid, 512, s);
+}
+
+}  // namespace
+
+hipError_t launch_mx_rows(const MxRows &a, hipStream_t s) {
+    if (!mx_rows_valid(a)) return hipErrorInvalidValue;
+    if (a.M <= MX_FEW) {
+        const dim3 grid((unsigned)((a.w.rows + 15) / 16));
+        return a.q.codes      ? go(&mx_few_kernel<ACT_MX>, a, grid, a.waves * 64, s)
+               : a.planes > 1 ? go(&mx_few_kernel<ACT_PLANES>, a, grid, a.waves * 64, s)
+                              : go(&mx_few_kernel<ACT_BF16>, a, grid, a.waves * 64, s);
+    }
+    hipError_t e = a.planes > 1 ? many<3>(a, s) : many<1>(a, s);
+    if (e != hipSuccess || a.slices == 1) return e;
+    return launch_mx_sum(MxSum{a.part, a.ldp, a.slices, a.M, a.w.rows, a.bias, a.y, a.ldy, a.f32}, s);
+}
+
+}  // namespace gemel

@@ -1,0 +1,273 @@
+// The operators of matrices in microscaled 4-bit floating point: argument
+// checks, workspaces, and the order of their kernels.
+#include <climits>
+
+#include "mx_args.h"
+#include "op_call.h"
+
+using namespace gemel;
+using namespace gemel::op;
+
+namespace {
+
+constexpr int64_t MAX_ROWS = 1 << 22;
+constexpr int64_t PIECE = 1ll << 28;   // floats of partial sums of float32 rows that a pass takes
+
+gemel_status check_mx(gemel_ctx *ctx, const char *what, const gemel_mx *q, Mx *out) {
+    if (!q) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is null");
+    if (q->rows < 0 || q->rows > MAX_ROWS || q->cols < 1 || q->cols > MX_MAX_COLS)
+        return fail(ctx, GEMEL_EINVAL, std::string(what) + " must have 0.." + std::to_string(MAX_ROWS) + " rows of 1.." +
+                                           std::to_string(MX_MAX_COLS) + " columns");
+    *out = Mx{(uint8_t *)q->codes, (uint8_t *)q->scales, q->rows, q->cols};
+    if (q->rows == 0) return GEMEL_OK;
+    if (!q->codes || !q->scales) return fail(ctx, GEMEL_EINVAL, std::string(what) + ": codes or scales are null");
+    if ((uintptr_t)q->codes % 16 || (uintptr_t)q->scales % 16)
+        return fail(ctx, GEMEL_EINVAL, std::string(what) + ": codes and scales must be aligned to 16 bytes");
+    return GEMEL_OK;
+}
+Range codes_of(const Mx &q, bool out) { return range("codes", q.codes, q.rows * mx_pitch(q.cols), out); }
+Range scales_of(const Mx &q, bool out) { return range("scales", q.scales, q.rows * mx_groups(q.cols) * 16, out); }
+
+gemel_status check_type(gemel_ctx *ctx, int32_t dtype) {
+    return dtype == GEMEL_F32 || dtype == GEMEL_BF16 ? GEMEL_OK : fail(ctx, GEMEL_EINVAL, "unknown type of values");
+}
+
+// y of rows that are not quantised.
+struct Wide {
+    const void *x;
+    int64_t ldx;
+    int M;
+    Mx w;
+    const float *bias;
+    char *y;
+    int64_t ldy;
+    bool f32;
+};
+
+// Up to MX_ROWS rows: the weights are expanded in registers.
+gemel_status few_rows(Call &c, const Wide &p) {
+    gemel_ctx *ctx = c.ctx;
+    MxRows a{};
+    a.w = p.w;
+    a.x = (const u16 *)p.x;
+    a.ldx = p.ldx;
+    a.planes = 1;
+    a.M = p.M;
+    mx_rows_plan(a);
+    const int64_t ld = op_round_up(p.w.cols, 8);
+    const size_t o_x = c.lay.take(p.f32 ? 3 * p.M * ld : 0, 2),
+                 o_part = c.lay.take(a.slices > 1 ? (int64_t)a.slices * p.M * a.ldp : 0, 4);
+    if (c.lay.bytes)
+        if (gemel_status s = workspace(c)) return s;
+    if (p.f32) {
+        const MxPlanes split{(const float *)p.x, p.ldx, c.at<u16>(o_x), ld, p.M, p.w.cols};
+        OPCHK(launch_mx_planes(split, c.stream), "planes");
+        a.x = split.out;
+        a.ldx = ld;
+        a.plane = p.M * ld;
+        a.planes = 3;
+    }
+    a.bias = p.bias;
+    a.y = p.y;
+    a.ldy = p.ldy;
+    a.f32 = p.f32;
+    a.part = c.at<float>(o_part);
+    OPCHK(launch_mx_rows(a, c.stream), "product");
+    return GEMEL_OK;
+}
+
+// More rows: the weights are expanded to bf16 once and go through the bf16
+// product. float32 rows go as three bf16 planes below each other, whose
+// results are then added up, in pieces that bound the workspace.
+gemel_status many_rows(Call &c, const Wide &p) {
+    gemel_ctx *ctx = c.ctx;
+    const int64_t Kp = op_round_up(p.w.cols, 8), ldp = op_round_up(p.w.rows, 4);
+    const int each = p.f32 ? (int)std::min<int64_t>(p.M, std::max<int64_t>(MX_ROWS, PIECE / (3 * ldp))) : p.M;
+    const bool copy = !p.f32 && !in_place(p.x, p.M, p.ldx, p.w.cols);
+    MmArgs m{};
+    m.M = p.f32 ? 3 * each : p.M;
+    m.N = p.w.rows;
+    m.K = (int)Kp;
+    m.batch = 1;
+    m.epi = EPI_ROWS;
+    mm_plan(m);
+    int64_t partial = partial_floats(m);
+    const int rest = p.f32 ? p.M % each : 0;
+    MmArgs last = m;
+    if (rest) {
+        last.M = 3 * rest;
+        mm_plan(last);
+        partial = std::max(partial, partial_floats(last));
+    }
+    if (!mm_fits(m) || (rest && !mm_fits(last))) return fail(ctx, GEMEL_EINVAL, "the product is too large");
+    const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(p.f32 ? 3 * each * Kp : copy ? p.M * Kp : 0, 2),
+                 o_y = c.lay.take(p.f32 ? 3 * each * ldp : 0, 4), o_part = c.lay.take(partial, 4);
+    if (gemel_status s = workspace(c)) return s;
+    MxCast cast{};
+    cast.q = p.w;
+    cast.out = c.at<u16>(o_w);
+    cast.ld = Kp;
+    cast.out_cols = (int)Kp;
+    OPCHK(launch_mx_values(cast, c.stream), "weights");
+    for (int r = 0; r < p.M; r += each) {
+        MmArgs &a = p.M - r < each ? last : m;
+        const int rows = std::min(each, p.M - r);
+        a.a = (const u16 *)p.x;
+        a.lda = p.ldx;
+        if (p.f32) {
+            const MxPlanes split{(const float *)p.x + r * p.ldx, p.ldx, c.at<u16>(o_x), Kp, rows, p.w.cols};
+            OPCHK(launch_mx_planes(split, c.stream), "planes");
+        } else if (copy) {
+            Jobs jobs;
+            Job j{};
+            j.kind = JOB_PAD;
+            j.in = p.x;
+            j.ldi = p.ldx;
+            j.rows = p.M;
+            j.cols = p.w.cols;
+            j.out = c.at<u16>(o_x);
+            j.ldo = Kp;
+            if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
+            OPCHK(launch_jobs(jobs, c.stream), "copies");
+        }
+        if (p.f32 || copy) {
+            a.a = c.at<u16>(o_x);
+            a.lda = Kp;
+        }
+        a.b = (const u16 *)cast.out;
+        a.ldb = Kp;
+        a.zero = (const u16 *)c.st->zero;
+        a.partial = c.at<float>(o_part);
+        a.o.out = p.f32 ? c.at<void>(o_y) : p.y;
+        a.o.ld = p.f32 ? ldp : p.ldy;
+        a.o.out_f32 = p.f32;
+        a.o.bias = p.f32 ? nullptr : p.bias;
+        OPCHK(launch_mm(a, c.stream), "product");
+        if (p.f32)
+            OPCHK(launch_mx_sum(MxSum{c.at<float>(o_y), ldp, 3, rows, p.w.rows, p.bias, p.y + (int64_t)r * p.ldy * 4, p.ldy, 1}, c.stream),
+                  "sum of planes");
+    }
+    return GEMEL_OK;
+}
+
+gemel_status both_quantized(Call &c, const Mx &x, const Mx &w, const float *bias, void *y, int64_t ldy, bool f32) {
+    gemel_ctx *ctx = c.ctx;
+    if (x.rows <= MX_FEW) {
+        MxRows a{};
+        a.w = w;
+        a.q = x;
+        a.M = x.rows;
+        mx_rows_plan(a);
+        a.bias = bias;
+        a.y = y;
+        a.ldy = ldy;
+        a.f32 = f32;
+        OPCHK(launch_mx_rows(a, c.stream), "product");
+        return GEMEL_OK;
+    }
+    MxMm a{};
+    a.x = x;
+    a.w = w;
+    mx_mm_plan(a);
+    if (a.splits > 1) {
+        const size_t o_part = c.lay.take((int64_t)a.splits * x.rows * a.ldp, 4);
+        if (gemel_status s = workspace(c)) return s;
+        a.part = c.at<float>(o_part);
+    }
+    a.bias = bias;
+    a.y = y;
+    a.ldy = ldy;
+    a.f32 = f32;
+    OPCHK(launch_mx_mm(a, c.stream), "product");
+    return GEMEL_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+gemel_status gemel_mx_quantize(gemel_ctx *ctx, const void *x, int64_t x_stride, int32_t dtype, const gemel_mx *out,
+                               void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        MxCast a{};
+        if (gemel_status s = check_type(ctx, dtype)) return s;
+        if (gemel_status s = check_mx(ctx, "out", out, &a.q)) return s;
+        if (a.q.rows == 0) return GEMEL_OK;
+        const int64_t e = dtype == GEMEL_F32 ? 4 : 2;
+        if (gemel_status s = check_rows(ctx, "x", x, x_stride, a.q.cols, e)) return s;
+        if (gemel_status s = apart(ctx, {codes_of(a.q, true), scales_of(a.q, true),
+                                         range("x", x, a.q.rows, a.q.cols, x_stride, e, false)}))
+            return s;
+        DeviceScope scope(ctx->device);
+        State *st;
+        if (gemel_status s = ready(ctx, &st)) return s;
+        a.x = x;
+        a.ld = x_stride;
+        a.f32 = dtype == GEMEL_F32;
+        OPCHK(launch_mx_quantize(a, (hipStream_t)hip_stream), "quantisation");
+        return GEMEL_OK;
+    });
+}
+
+gemel_status gemel_mx_dequantize(gemel_ctx *ctx, const gemel_mx *q, void *out, int64_t out_stride, int32_t dtype,
+                                 void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        MxCast a{};
+        if (gemel_status s = check_type(ctx, dtype)) return s;
+        if (gemel_status s = check_mx(ctx, "q", q, &a.q)) return s;
+        if (a.q.rows == 0) return GEMEL_OK;
+        const int64_t e = dtype == GEMEL_F32 ? 4 : 2;
+        if (gemel_status s = check_rows(ctx, "out", out, out_stride, a.q.cols, e)) return s;
+        if (gemel_status s = apart(ctx, {range("out", out, a.q.rows, a.q.cols, out_stride, e, true), codes_of(a.q, false),
+                                         scales_of(a.q, false)}))
+            return s;
+        DeviceScope scope(ctx->device);
+        State *st;
+        if (gemel_status s = ready(ctx, &st)) return s;
+        a.out = out;
+        a.ld = out_stride;
+        a.f32 = dtype == GEMEL_F32;
+        a.out_cols = a.q.cols;
+        OPCHK(launch_mx_values(a, (hipStream_t)hip_stream), "values");
+        return GEMEL_OK;
+    });
+}
+
+gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x, int64_t x_stride, const gemel_mx *xq,
+                              const gemel_mx *weight, const float *bias, void *y, int64_t y_stride, void *hip_stream) {
+    if (!ctx) return GEMEL_EINVAL;
+    return guarded(ctx, [&]() -> gemel_status {
+        Mx q{}, w{};
+        if (gemel_status s = check_mx(ctx, "weight", weight, &w)) return s;
+        if (w.rows < 1) return fail(ctx, GEMEL_EINVAL, "weight has no rows");
+        if ((x != nullptr) == (xq != nullptr) && rows != 0) return fail(ctx, GEMEL_EINVAL, "either x or xq must be given");
+        if (rows < 0 || rows > MAX_ROWS) return fail(ctx, GEMEL_EINVAL, "rows must be in 0.." + std::to_string(MAX_ROWS));
+        if (xq) {
+            if (gemel_status s = check_mx(ctx, "xq", xq, &q)) return s;
+            if (q.rows != rows || q.cols != w.cols)
+                return fail(ctx, GEMEL_EINVAL, "xq must have `rows` rows of as many columns as weight");
+        }
+        if (rows == 0) return GEMEL_OK;
+        const bool f32 = ctx->dtype == GEMEL_F32;
+        const int64_t e = f32 ? 4 : 2;
+        if (x)
+            if (gemel_status s = check_rows(ctx, "x", x, x_stride, w.cols, e)) return s;
+        if (gemel_status s = check_rows(ctx, "y", y, y_stride, w.rows, e)) return s;
+        if (gemel_status s = check_aligned(ctx, "bias", bias, 4)) return s;
+        if (gemel_status s = apart(ctx, {range("y", y, rows, w.rows, y_stride, e, true),
+                                         range("x", x, rows, w.cols, x_stride, e, false), codes_of(q, false), scales_of(q, false),
+                                         codes_of(w, false), scales_of(w, false), range("bias", bias, w.rows * 4ll, false)}))
+            return s;
+        DeviceScope scope(ctx->device);
+        State *st;
+        if (gemel_status s = ready(ctx, &st)) return s;
+        Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
+        if (xq) return both_quantized(c, q, w, bias, y, y_stride, f32);
+        const Wide p{x, x_stride, rows, w, bias, (char *)y, y_stride, f32};
+        return rows <= MX_ROWS ? few_rows(c, p) : many_rows(c, p);
+    });
+}
+
+}  // extern "C"

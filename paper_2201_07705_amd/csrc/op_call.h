@@ -268,6 +268,14 @@ inline gemel_status check_rows(gemel_ctx *ctx, const char *what, const void *p, 
     return check_aligned(ctx, what, p, elem);
 }
 
+inline int64_t partial_floats(const MmArgs &a) {
+    return a.splits > 1 ? (int64_t)a.splits * a.batch * a.M * a.ldp : 0;
+}
+// Rows that a product reads where they are; others are copied first.
+inline bool in_place(const void *p, int64_t rows, int64_t ld, int64_t cols) {
+    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= MM_MAX_LD && rows * ld <= 1ll << 30;
+}
+
 // Runs f, with host allocation failures as a status.
 template <typename F>
 inline gemel_status guarded(gemel_ctx *ctx, F &&f) {

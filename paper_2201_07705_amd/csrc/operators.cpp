@@ -211,16 +211,6 @@ gemel_status make_batch(gemel_ctx *ctx, const int32_t *ids, const int32_t *n_row
     return GEMEL_OK;
 }
 
-// ---- products ----
-
-int64_t partial_floats(const MmArgs &a) {
-    return a.splits > 1 ? (int64_t)a.splits * a.batch * a.M * a.ldp : 0;
-}
-// Rows that a product reads where they are; others are copied first.
-bool in_place(const void *p, int64_t rows, int64_t ld, int64_t cols) {
-    return (uintptr_t)p % 16 == 0 && ld % 8 == 0 && cols % 8 == 0 && ld <= MM_MAX_LD && rows * ld <= 1ll << 30;
-}
-
 gemel_status check_projection(gemel_ctx *ctx, const gemel_projection *p, bool adapters) {
     if (!p) return fail(ctx, GEMEL_EINVAL, "proj is null");
     if (p->n_in < 1 || p->n_out < 1 || p->n_in > MAX_DIM || p->n_out > MAX_DIM)

@@ -55,14 +55,16 @@ EXPORTED = ("gemel_create", "gemel_register_model", "gemel_merge",
             "gemel_query", "gemel_set_option", "gemel_profile",
             "gemel_last_error", "gemel_destroy",
             "gemel_log_probs", "gemel_distill", "gemel_distill_backward",
+            "gemel_mx_quantize", "gemel_mx_dequantize", "gemel_mx_product",
             "gemel_adapter_batch", "gemel_adapter_batch_free",
             "gemel_adapt", "gemel_adapt_backward", "gemel_orthogonalize",
             "gemel_muon_step")
 # Operators that serve and retrain merged layers: not part of CPU builds of
 # the planner alone.
 OPERATORS = EXPORTED[-6:]
-# Answers and distillation: builds of other operators alone lack them.
-ANSWERS = EXPORTED[-9:-6]
+# Answers, distillation and 4-bit matrices: builds of the operators above
+# alone lack them.
+ANSWERS = EXPORTED[-12:-6]
 
 _fp = ctypes.POINTER(ctypes.c_float)
 
@@ -102,6 +104,11 @@ class Answers(ctypes.Structure):
                 ("entropy", ctypes.c_void_p), ("log_sum", ctypes.c_void_p),
                 ("top_indices", ctypes.c_void_p),
                 ("top_log_probs", ctypes.c_void_p)]
+
+
+class Mx(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("cols", ctypes.c_int32),
+                ("codes", ctypes.c_void_p), ("scales", ctypes.c_void_p)]
 
 
 class KernelStat(ctypes.Structure):
@@ -211,6 +218,10 @@ def _configure_answers(L):
                                 vp, vp]
     L.gemel_distill_backward.argtypes = [vp, i32, i32, vp, vp, i64, i32, vp,
                                          vp, i32, f32, vp, i64, vp, vp]
+    mx = ctypes.POINTER(Mx)
+    L.gemel_mx_quantize.argtypes = [vp, vp, i64, i32, mx, vp]
+    L.gemel_mx_dequantize.argtypes = [vp, mx, vp, i64, i32, vp]
+    L.gemel_mx_product.argtypes = [vp, i32, vp, i64, mx, mx, vp, vp, i64, vp]
     for name in ANSWERS:
         getattr(L, name).restype = i32
 
@@ -352,6 +363,25 @@ class AdapterBatch:
             self.close()
         except Exception:
             pass
+
+
+class MxMatrix:
+    """A matrix [rows, cols] in microscaled 4-bit floating point, as
+    Context.mx_quantize makes it: codes [rows, P] and scales [groups, rows,
+    16], both uint8 (include/gemel.h says which byte is which)."""
+
+    def __init__(self, codes, scales, rows, cols):
+        self.codes, self.scales = codes, scales
+        self.rows, self.cols = rows, cols
+
+    @staticmethod
+    def shapes(rows, cols):
+        """Shapes of codes and scales."""
+        return (rows, 128 * -(-cols // 256)), (-(-cols // 512), rows, 16)
+
+    @property
+    def nbytes(self):
+        return self.codes.numel() + self.scales.numel()
 
 
 class Context:
@@ -868,3 +898,103 @@ class Context:
             self._stream(stream, dloss, logits, indices, values, d, loss)))
         self._written(out, loss)
         return d
+
+    # -- merged layers in 4 bits --
+    def _mx(self, name, q):
+        """The C description of a quantised matrix, checked."""
+        if not isinstance(q, MxMatrix):
+            raise ValueError(f"{name} must be an MxMatrix")
+        _int32(name + " rows", q.rows)
+        _int32(name + " cols", q.cols)
+        u8 = _torch().uint8
+        codes, scales = MxMatrix.shapes(q.rows, q.cols)
+        self._tensor(name + ".codes", q.codes, codes, u8)
+        self._tensor(name + ".scales", q.scales, scales, u8)
+        return Mx(q.rows, q.cols, q.codes.data_ptr(), q.scales.data_ptr())
+
+    @staticmethod
+    def _value_type(name, dtype):
+        torch = _torch()
+        if dtype not in (torch.float32, torch.bfloat16):
+            raise ValueError(f"{name} must be float32 or bfloat16, is {dtype}")
+        return F32 if dtype == torch.float32 else BF16
+
+    def mx_quantize(self, x, out=None, stream=None):
+        """x [rows, cols] (bf16 or float32 in every context, rows may have a
+        stride) as an MxMatrix: blocks of 32 4-bit floating-point values of a
+        row that share a power of two. out: an MxMatrix of that size whose
+        memory is written."""
+        if x.dim() != 2:
+            raise ValueError("x must be [rows, cols]")
+        rows, cols = x.shape
+        code = self._value_type("x", x.dtype)
+        _int32("rows", rows)
+        _int32("cols", cols)
+        self._tensor("x", x, (rows, cols), x.dtype, contiguous=False)
+        q = out
+        if q is None:
+            u8 = _torch().uint8
+            codes, scales = MxMatrix.shapes(rows, cols)
+            q = MxMatrix(self._empty(x, codes, u8, stream),
+                         self._empty(x, scales, u8, stream), rows, cols)
+        elif (q.rows, q.cols) != (rows, cols):
+            raise ValueError(f"out is [{q.rows}, {q.cols}], x [{rows}, {cols}]")
+        self._check(self._lib.gemel_mx_quantize(
+            self._h, x.data_ptr(), self._stride(x), code, self._mx("out", q),
+            self._stream(stream, x, q.codes, q.scales)))
+        if out is not None:
+            self._written(q.codes, q.scales)
+        return q
+
+    def mx_dequantize(self, q, dtype=None, out=None, stream=None):
+        """The values [rows, cols] of an MxMatrix, in dtype (None: the
+        context's; bf16 or float32), exactly."""
+        c = self._mx("q", q)
+        dt = dtype or (out.dtype if out is not None else self._torch_dtype())
+        code = self._value_type("dtype", dt)
+        v = out
+        if v is None:
+            v = self._empty(q.codes, (q.rows, q.cols), dt, stream)
+        else:
+            self._tensor("out", v, (q.rows, q.cols), dt, contiguous=False)
+        self._check(self._lib.gemel_mx_dequantize(
+            self._h, c, v.data_ptr(), self._stride(v), code,
+            self._stream(stream, q.codes, q.scales, v)))
+        if out is not None:
+            self._written(out)
+        return v
+
+    def mx_product(self, x, weight, bias=None, out=None, stream=None):
+        """y = x W^T + bias with 4-bit weights: weight an MxMatrix [n_out,
+        n_in], bias float32, y [rows, n_out] of the context's type. x [rows,
+        n_in] is of the context's type and multiplied as it is, or an
+        MxMatrix: then both sides are 4 bits."""
+        w, dt = self._mx("weight", weight), self._torch_dtype()
+        n, k = weight.rows, weight.cols
+        if isinstance(x, MxMatrix):
+            rows, xq, base = x.rows, self._mx("x", x), x.codes
+            if x.cols != k:
+                raise ValueError(f"x has {x.cols} columns, weight {k}")
+            data, stride, used = None, 0, (x.codes, x.scales)
+        else:
+            if x.dim() != 2:
+                raise ValueError("x must be [rows, n_in]")
+            rows, xq, base = x.shape[0], None, x
+            _int32("rows", rows)
+            self._tensor("x", x, (rows, k), dt, contiguous=False)
+            data, stride, used = x.data_ptr(), self._stride(x), (x,)
+        if bias is not None:
+            self._tensor("bias", bias, (n,), _torch().float32)
+        y = out
+        if y is None:
+            y = self._empty(base, (rows, n), dt, stream)
+        else:
+            self._tensor("out", y, (rows, n), dt, contiguous=False)
+        self._check(self._lib.gemel_mx_product(
+            self._h, rows, data, stride, xq, w,
+            None if bias is None else bias.data_ptr(), y.data_ptr(),
+            self._stride(y),
+            self._stream(stream, *used, weight.codes, weight.scales, bias, y)))
+        if out is not None:
+            self._written(out)
+        return y

@@ -1,0 +1,322 @@
+"""Matrices in microscaled 4-bit floating point on the GPU: codes and scales
+against the definition bit by bit, and products against 64 bits, at every
+path's sizes, odd ones, strides, values that are not finite, streams and
+graphs."""
+
+import math
+
+import pytest
+
+from paper_2201_07705_amd import gemel as G
+
+pytestmark = pytest.mark.gpu
+
+MAGNITUDES = [0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0]
+U = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ctxs():
+    c = {d: G.Context(0, d) for d in ("bf16", "f32")}
+    yield c
+    for q in c.values():
+        q.close()
+
+
+def dtype_of(name):
+    import torch
+    return {"bf16": torch.bfloat16, "f32": torch.float32}[name]
+
+
+def power(e):
+    """2^e in float64, exactly."""
+    import torch
+    return ((e.long() + 1023) << 52).view(torch.float64)
+
+
+def blocks_of(x):
+    """x in blocks of 32, padded with zeros: [rows, blocks, 32] float64."""
+    import torch
+    rows, cols = x.shape
+    return torch.nn.functional.pad(x.double(), (0, -cols % 32)).view(rows, -1, 32)
+
+
+def encode64(x):
+    """Codes [rows, cols] and scale bytes [rows, blocks] by the definition."""
+    import torch
+    v = blocks_of(x)
+    most = v.abs().amax(2)
+    good = (v.abs() < math.inf).all(2)
+    m, e = torch.frexp(torch.where(good, most, 0.0))   # most = m 2^e, 0.5 <= m < 1
+    byte = torch.where(most > 0, (e - 1 - 2).clamp_min(-127), -127) + 127
+    a = (v / power(byte - 127)[:, :, None]).abs()
+    code = torch.zeros_like(a, dtype=torch.int64)
+    for i in range(7):
+        half = (MAGNITUDES[i] + MAGNITUDES[i + 1]) / 2
+        code += (a > half) | ((a == half) if i % 2 else torch.zeros_like(a, dtype=torch.bool))
+    code += 8 * torch.signbit(v)
+    return code.view(x.shape[0], -1)[:, :x.shape[1]], torch.where(good, byte, 255)
+
+
+def unpacked(q):
+    """Codes [rows, padded columns] and scale bytes [rows, blocks of all groups]."""
+    import torch
+    c = q.codes.long()
+    codes = torch.stack([c & 15, c >> 4], 2).view(q.rows, -1)
+    b = torch.arange(q.scales.shape[0] * 16, device=c.device)
+    return codes, q.scales.long().permute(1, 0, 2).reshape(q.rows, -1)[:, b // 16 * 16 + 4 * (b % 4) + b % 16 // 4]
+
+
+def values64(q):
+    import torch
+    codes, bytes_ = unpacked(q)
+    table = torch.tensor(MAGNITUDES + [-m for m in MAGNITUDES], dtype=torch.float64, device=codes.device)
+    scale = torch.where(bytes_ == 255, math.nan, power(bytes_ - 127))
+    blocks = codes.shape[1] // 32
+    return (table[codes].view(q.rows, blocks, 32) * scale[:, :blocks, None]).view(q.rows, -1)[:, :q.cols]
+
+
+def matrix(rows, cols, dtype, seed=0, pad=0, shift=0):
+    import torch
+    gen = torch.Generator(device="cuda").manual_seed(seed)
+    x = torch.randn(rows, cols + pad + shift, device="cuda", generator=gen)
+    x = x * torch.exp(2 * torch.randn(cols + pad + shift, device="cuda", generator=gen))
+    return x.to(dtype_of(dtype))[:, shift:shift + cols]
+
+
+def check_quantized(ctx, x):
+    import torch
+    q = ctx.mx_quantize(x)
+    codes, bytes_ = unpacked(q)
+    want_codes, want_bytes = encode64(x)
+    assert torch.equal(bytes_[:, :want_bytes.shape[1]], want_bytes)
+    assert not bytes_[:, want_bytes.shape[1]:].any() and not codes[:, q.cols:].any()
+    fine = (want_bytes != 255).repeat_interleave(32, dim=1)[:, :q.cols]
+    assert torch.equal(codes[:, :q.cols][fine], want_codes[fine])
+    want = values64(q)
+    for dt in (torch.float32, torch.bfloat16):
+        got = ctx.mx_dequantize(q, dtype=dt)
+        # (2^-128, half of the smallest scale, is a float32 and a bfloat16 like all the others)
+        assert got.dtype == dt and torch.equal(got.double().nan_to_num(nan=7e99), want.nan_to_num(nan=7e99))
+    return q
+
+
+COLS = [1, 7, 8, 9, 31, 32, 33, 127, 255, 256, 257, 300, 511, 512, 513, 769, 1000, 1537, 2048, 4100]
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("cols", COLS)
+def test_quantize_any_width(ctxs, cols, dtype):
+    for rows in (1, 3, 4, 5, 66):
+        check_quantized(ctxs["bf16"], matrix(rows, cols, dtype, seed=cols, pad=cols % 3, shift=cols % 2))
+    check_quantized(ctxs["f32"], matrix(17, cols, dtype, seed=cols))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_every_step_and_tie(ctxs, dtype):
+    """All halves and quarters of every code at scales over the whole range,
+    denormals, signs of zero, and blocks that are zero."""
+    import torch
+    dt = dtype_of(dtype)
+    steps = torch.arange(32, device="cuda").double() / 4          # 0 .. 7.75
+    rows = []
+    for e in range(-149, 128):
+        for shift in (0, 1e-6, -1e-6):
+            rows.append((steps * (1 + shift)).flip(0) * 2.0 ** e)
+            rows.append(-steps * (1 + shift) * 2.0 ** e)
+    x = torch.stack(rows)
+    x = x.where(x.abs() < 3e38, 1.0).to(dt)
+    check_quantized(ctxs["bf16"], x)
+    z = torch.zeros(3, 100, device="cuda", dtype=dt)
+    z[1] = -0.0
+    z[2, 40] = torch.finfo(dt).smallest_normal / 8
+    check_quantized(ctxs["bf16"], z)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_values_that_are_not_finite_spoil_their_block(ctxs, dtype):
+    import torch
+    x = matrix(9, 700, dtype)
+    x[1, 5] = math.nan
+    x[2, 699] = math.inf
+    x[3, 64] = -math.inf
+    x[4] = math.nan
+    x[5, 100] = torch.finfo(x.dtype).max
+    q = check_quantized(ctxs["bf16"], x)
+    bad = ctxs["bf16"].mx_dequantize(q).isnan().sum(1).tolist()
+    assert bad == [0, 32, 700 - 672, 32, 700, 0, 0, 0, 0]
+
+
+def test_out_and_strides(ctxs):
+    import torch
+    ctx = ctxs["bf16"]
+    x = matrix(20, 333, "f32")
+    q = ctx.mx_quantize(x)
+    r = G.MxMatrix(torch.full_like(q.codes, 9), torch.full_like(q.scales, 9), 20, 333)
+    version = r.codes._version
+    assert ctx.mx_quantize(x, out=r) is r and r.codes._version > version
+    assert torch.equal(r.codes, q.codes) and torch.equal(r.scales, q.scales)
+    wide = torch.full((20, 340), 5.0, device="cuda")
+    ctx.mx_dequantize(q, out=wide[:, 3:336])
+    assert torch.equal(wide[:, 3:336].double(), values64(q)) and (wide[:, :3] == 5).all() and (wide[:, 336:] == 5).all()
+    assert q.nbytes == 20 * 256 + 20 * 16
+    empty = ctx.mx_quantize(x[:0])
+    assert ctx.mx_dequantize(empty).shape == (0, 333) and ctx.mx_product(empty, q).shape == (0, 20)
+
+
+def product(dtype, acts, m, k, n, seed=0, pad=0, shift=0):
+    import torch
+    x = torch.relu(matrix(m, k, dtype, seed=seed, pad=pad, shift=shift))
+    if pad or shift:
+        y = torch.zeros(m, k + pad + shift, device="cuda", dtype=x.dtype)
+        y[:, shift:shift + k] = x
+        x = y[:, shift:shift + k]
+    gen = torch.Generator(device="cuda").manual_seed(seed + 1)
+    w = torch.randn(n, k, device="cuda", generator=gen) * torch.exp(torch.randn(n, 1, device="cuda", generator=gen))
+    return x, w, torch.randn(n, device="cuda", generator=gen)
+
+
+def check_product(ctx, x, wq, bias, acts, out=None):
+    """Sums of k products of exact factors and a bias: at most k / 4 + 70
+    additions follow each other (a lane's block, splits, waves), and each
+    matrix instruction may round a few times; 2^-24 of the sum of magnitudes
+    for each. The rounding of y itself."""
+    import torch
+    left = ctx.mx_quantize(x) if acts == "mx" else x
+    y = ctx.mx_product(left, wq, bias=bias, out=out)
+    xv, wv = values64(left) if acts == "mx" else x.double(), values64(wq)
+    want, size = xv @ wv.T, xv.abs() @ wv.abs().T
+    if bias is not None:
+        want, size = want + bias.double(), size + bias.double().abs()
+    tol = size * U * (wv.shape[1] / 4 + 70)
+    tol = tol + (want.abs() + tol) * torch.finfo(y.dtype).eps / 2 + 1e-37
+    assert y.dtype == x.dtype and y.shape == want.shape
+    off = ((y.double() - want).abs() - tol).max().item()
+    assert off <= 0, off
+    # (a typical error is far smaller: a lost term would show here)
+    scale = size.square().mean().sqrt().item()
+    typical = (y.double() - want).square().mean().sqrt().item()
+    assert typical <= scale * (torch.finfo(y.dtype).eps + 40 * U), (typical, scale)
+    return y
+
+
+ROWS = [1, 2, 15, 16, 17, 32, 33, 48, 49, 64, 65, 130, 256, 257, 300]
+SHAPES = [(16, 10), (33, 1), (100, 17), (256, 256), (257, 300), (512, 33), (513, 64), (1000, 1000), (1300, 513), (2048, 70),
+          (5000, 200)]
+
+
+@pytest.mark.parametrize("acts", ["float", "mx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k,n", SHAPES)
+def test_products(ctxs, k, n, dtype, acts):
+    ctx = ctxs[dtype]
+    for m in ROWS:
+        x, w, bias = product(dtype, acts, m, k, n, seed=m, pad=m % 3, shift=m % 2)
+        wq = ctx.mx_quantize(w)
+        check_product(ctx, x, wq, bias if m % 2 else None, acts)
+
+
+@pytest.mark.parametrize("acts", ["float", "mx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m,k,n", [(1, 25088, 4096), (37, 25088, 4096), (1000, 4096, 1000), (5000, 1024, 2100), (2500, 264, 4096),
+                                   (4500, 1000, 4000), (20000, 40, 33)])
+def test_large_products(ctxs, m, k, n, dtype, acts):
+    ctx = ctxs[dtype]
+    x, w, bias = product(dtype, acts, m, k, n)
+    check_product(ctx, x, ctx.mx_quantize(w), bias, acts)
+
+
+@pytest.mark.parametrize("acts", ["float", "mx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_products_into_columns_of_a_matrix(ctxs, dtype, acts):
+    import torch
+    ctx = ctxs[dtype]
+    for m in (3, 40, 300):
+        x, w, bias = product(dtype, acts, m, 200, 77, pad=5, shift=3)
+        wide = torch.full((m, 90), 3.0, device="cuda", dtype=dtype_of(dtype))
+        check_product(ctx, x, ctx.mx_quantize(w), bias, acts, out=wide[:, 7:84])
+        assert (wide[:, :7] == 3).all() and (wide[:, 84:] == 3).all()
+
+
+@pytest.mark.parametrize("acts", ["float", "mx"])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("m", [5, 40, 300])
+def test_what_is_not_finite_stays_in_its_rows_and_columns(ctxs, m, dtype, acts):
+    import torch
+    ctx = ctxs[dtype]
+    x, w, bias = product(dtype, acts, m, 600, 50)
+    clean = check_product(ctx, x, ctx.mx_quantize(w), bias, acts)
+    x, w = x.clone(), w.clone()
+    x[2, 599] = math.nan
+    x[4, 0] = math.inf
+    w[7, 300] = math.nan
+    y = ctx.mx_product(ctx.mx_quantize(x) if acts == "mx" else x, ctx.mx_quantize(w), bias=bias)
+    bad = torch.zeros(m, 50, dtype=torch.bool, device="cuda")
+    bad[[2, 4]] = True
+    bad[:, 7] = True
+    assert torch.equal(~y.isfinite(), bad) and torch.equal(y[~bad], clean[~bad])
+
+
+def test_scales_over_their_range(ctxs):
+    """Scales that multiply to an ordinary size, and 0 and 254 as they are."""
+    import torch
+    for dtype in ("bf16", "f32"):
+        ctx = ctxs[dtype]
+        for m in (4, 40):
+            x, w, _ = product(dtype, "mx", m, 96, 40)
+            x = x.float().clamp(0.01, 100) * 2.0 ** 100
+            w = w.clamp(-8, 8) * 2.0 ** -100
+            for acts in ("float", "mx"):
+                check_product(ctx, x.to(dtype_of(dtype)), ctx.mx_quantize(w), None, acts)
+    q = ctxs["f32"].mx_quantize(torch.ones(1, 64, device="cuda"))
+    q.scales[0, 0, 0], q.scales[0, 0, 4] = 0, 254
+    got = ctxs["f32"].mx_dequantize(q)
+    # (4 * 2^127 is beyond float32: infinity)
+    assert torch.equal(got, values64(q).float()) and got[0, 63] == math.inf and got[0, 0] == 2.0 ** -125
+
+
+@pytest.mark.parametrize("acts", ["float", "mx"])
+@pytest.mark.parametrize("m,k,n", [(1, 600, 100), (40, 1500, 300), (700, 520, 260)])
+def test_another_stream_and_a_graph(ctxs, m, k, n, acts):
+    import torch
+    ctx = ctxs["bf16"]
+    x, w, bias = product("bf16", acts, m, k, n)
+    stream = torch.cuda.Stream()
+    wq = ctx.mx_quantize(w)
+
+    def call(stream=None, xq=None, out=None):
+        left = ctx.mx_quantize(x, out=xq, stream=stream) if acts == "mx" else x
+        return ctx.mx_product(left, wq, bias=bias, out=out, stream=stream)
+
+    want = call()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        got = call(stream=stream)
+    stream.synchronize()
+    assert torch.equal(got, want)
+    xq, y = ctx.mx_quantize(x), torch.zeros_like(want)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(stream=torch.cuda.current_stream(), xq=xq, out=y)
+    for seed in range(4):
+        x.copy_(product("bf16", acts, m, k, n, seed=30 + seed)[0])
+        want = call()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want), seed
+
+
+def test_same_bits_again(ctxs):
+    import torch
+    for dtype in ("bf16", "f32"):
+        for acts in ("float", "mx"):
+            for m, k, n in ((1, 4096, 500), (50, 25088, 300), (600, 2048, 1000)):
+                ctx = ctxs[dtype]
+                x, w, bias = product(dtype, acts, m, k, n)
+                wq = ctx.mx_quantize(w)
+                left = ctx.mx_quantize(x) if acts == "mx" else x
+                first = ctx.mx_product(left, wq, bias=bias)
+                for _ in range(3):
+                    assert torch.equal(ctx.mx_product(left, wq, bias=bias), first)
