@@ -60,7 +60,7 @@ struct DistillArgs {
 struct AnswerForm {
     int waves, vecs;
 };
-constexpr int ANSWER_FORMS = 8;
+constexpr int ANSWER_FORMS = 9;
 extern const AnswerForm answer_forms[ANSWER_FORMS];
 constexpr int answer_vec(int f32) { return f32 ? 4 : 8; }   // classes of a piece
 // Rows that a workgroup holds at once

@@ -7,7 +7,7 @@
 
 namespace gemel {
 
-const AnswerForm answer_forms[ANSWER_FORMS] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 8}, {16, 8}, {16, 12}};
+const AnswerForm answer_forms[ANSWER_FORMS] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 8}, {16, 12}};
 
 namespace {
 void cut(Logits &l, const AnswerForm &f) {
@@ -25,9 +25,9 @@ bool form_of(const Logits &l) {
 
 // The smallest form that holds a row; wide rows in chunks.
 void score_plan(Logits &l, int) {
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < 7; ++i) {
         cut(l, answer_forms[i]);
-        if (l.chunks == 1) return;
+        if (l.chunks <= (i < 4 ? 1 : ANSWER_MAX_CHUNKS)) return;
     }
 }
 void distill_plan(Logits &l) {

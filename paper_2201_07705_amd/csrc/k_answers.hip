@@ -12,6 +12,8 @@
 // chunks whose sums and best classes a second launch joins.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "answer_args.h"
 #include "op_moves.h"
 
@@ -161,45 +163,60 @@ __device__ __forceinline__ Part joined(const Part &x, const Part &y, float c) {
     return p;
 }
 
-// Largest elements of a lane's groups, pairs of elements by turns.
+// Largest elements of a lane's groups: pieces, or parts of the only one or two.
 template <bool F32, int V>
 struct Groups {
-    static constexpr int PAIRS = V * (F32 ? 2 : 4), N = PAIRS < 4 ? PAIRS : 4;
+    static constexpr int SUB = V == 1 ? (F32 ? 2 : 4) : V == 2 ? 2 : 1, N = V * SUB, SIZE = (F32 ? 4 : 8) / SUB;
     float most[N];
 };
 
-// Sums of the elements that a wave holds.
-template <bool F32, int W, int V>
+// Sums of the elements that a wave holds (a: only with A).
+//
+// Where m c is of ordinary size t = z c - r, r being m c rounded, is one
+// operation instead of two; its sums are then those for m but for a factor of
+// 2^d, d = m c - r. (Elements that are far apart would lose bits there.)
+template <bool A, bool F32, int W, int V>
 __device__ __forceinline__ Part wave_part(Held<F32, W, V> &h, float c, Groups<F32, V> &most) {
-    constexpr int VEC = Held<F32, W, V>::VEC, N = Groups<F32, V>::N;
+    constexpr int VEC = Held<F32, W, V>::VEC;
+    using G = Groups<F32, V>;
+    float m = -infinity();
 #pragma unroll
-    for (int i = 0; i < N; ++i) most.most[i] = -infinity();
+    for (int g = 0; g < G::N; ++g) {
+        float &x = most.most[g];
+        x = -infinity();
 #pragma unroll
-    for (int v = 0; v < V; ++v)
-#pragma unroll
-        for (int j = 0; j < VEC; j += 2) {
-            float &m = most.most[(v * VEC + j) / 2 % N];
-            m = max3(m, h.get(v, j), h.get(v, j + 1));
+        for (int j = 0; j < G::SIZE; j += 2) {
+            const int v = g / G::SUB, k = g % G::SUB * G::SIZE + j;
+            x = max3(x, h.get(v, k), h.get(v, k + 1));
         }
-    float m = most.most[0];
-#pragma unroll
-    for (int i = 1; i < N; ++i) m = max3(m, most.most[i], most.most[i]);
-    m = wave_max(m);
-    const float ref = m == -infinity() ? 0.f : m;
-    float s = 0.f, a = 0.f;
-#pragma unroll
-    for (int v = 0; v < V; ++v) {
-        h.again(v, s, a);
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) {
-            const float t = (h.get(v, j) - ref) * c;
-            const float e = __builtin_amdgcn_exp2f(t);
-            s += e;
-            // (0 times -inf, a masked class's, has to be nothing)
-            a = __builtin_fmaf(e, fmaxf(t, -1e30f), a);
-        }
+        m = max3(m, x, x);
     }
-    return Part{m, wave_sum(s), wave_sum(a), 0};
+    m = wave_max(m);
+    const float ref = m == -infinity() ? 0.f : m, r = ref * c;
+    float s = 0.f, a = 0.f;
+    auto sums = [&](auto one) __attribute__((always_inline)) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            h.again(v, s, a);
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) {
+                const float t = decltype(one)::value ? __builtin_fmaf(h.get(v, j), c, -r) : (h.get(v, j) - ref) * c;
+                const float e = __builtin_amdgcn_exp2f(t);
+                s += e;
+                // (0 times -inf, a masked class's, has to be nothing)
+                if constexpr (A) a = __builtin_fmaf(e, fmaxf(t, -1e30f), a);
+            }
+        }
+    };
+    if (fabsf(r) < 0x1p16f) {
+        sums(std::true_type{});
+        const float d = __builtin_fmaf(ref, c, -r), f = __builtin_amdgcn_exp2f(-d);
+        a = (a - d * s) * f;
+        s *= f;
+    } else {
+        sums(std::false_type{});
+    }
+    return Part{m, wave_sum(s), A ? wave_sum(a) : 0.f, 0};
 }
 
 // The team's sums from those of its waves, in every lane.
@@ -212,6 +229,21 @@ __device__ __forceinline__ Part team_part(Part p, Part *shared, int wave, float 
 #pragma unroll
     for (int w = 1; w < W; ++w) sum = joined(sum, shared[w], c);
     return sum;
+}
+
+// A row's sums from those of its chunks, one to a lane, in every lane.
+__device__ __forceinline__ Part chunks_part(const Part *part, int chunks, float c) {
+    const int lane = threadIdx.x & 63;
+    Part p = part[min(lane, chunks - 1)];
+    const bool there = lane < chunks;
+    // (NaN sums stay, whatever their reference is; an empty chunk adds nothing)
+    const float m = wave_max(there ? p.m : -infinity()), d = p.s == 0.f ? 0.f : (p.m - m) * c, f = __builtin_amdgcn_exp2f(d);
+    Part q;
+    q.m = m;
+    q.s = wave_sum(there ? p.s * f : 0.f);
+    q.a = wave_sum(there && f > 0.f ? (p.a + d * p.s) * f : 0.f);
+    q.before = wave_sum(there ? p.before : 0);
+    return q;
 }
 
 struct Results {
@@ -263,26 +295,48 @@ __device__ __forceinline__ uint32_t ordered(float z) {
 }
 __device__ __forceinline__ float from_ordered(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
 
-// A value that at least `top` of the wave's elements reach, and few more: one
-// that about `top` of the largest elements of its lanes' groups reach, found
-// bit by bit (-inf where there are not as many groups).
-template <bool F32, int V>
-__device__ __forceinline__ float wave_reach(const Groups<F32, V> &most, int top) {
-    constexpr int N = Groups<F32, V>::N;
-    uint32_t k[N];
-#pragma unroll
-    for (int i = 0; i < N; ++i) k[i] = ordered(most.most[i]);
-    uint32_t reach = 0;
-#pragma unroll 1
-    for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
-        const uint32_t t = reach | bit;
+// The least value (in the order of `ordered`) that is known to be reached by
+// `top` of N values in each lane, and few more: between lo, which enough
+// reach, and hi, by halves.
+template <int N>
+__device__ __forceinline__ uint32_t reached(const uint32_t (&k)[N], uint32_t lo, uint32_t hi, int top) {
+    while (hi - lo > 1) {
+        const uint32_t t = lo + (hi - lo) / 2;
         int n = 0;
 #pragma unroll
         for (int i = 0; i < N; ++i) n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(k[i] >= t));
-        if (n >= top) reach = t;
-        if (n >= top && n <= top + (top >> 2)) break;
+        if (n >= top)
+            lo = t;
+        else
+            hi = t;
+        if (n >= top && n <= top + top / 4) break;
     }
-    return reach <= 0x7fffffu ? -infinity() : from_ordered(reach);
+    return lo;
+}
+// Values that at least `top` and `part` of the wave's elements reach, and few
+// more: ones that as many of its lanes' groups reach with their largest
+// (-inf where there are not as many).
+template <int N>
+__device__ __forceinline__ void wave_reach(const float (&most)[N], float m, int top, int part, float &all, float &some) {
+    uint32_t k[N], least = 0xffffffffu;
+    int n = 0;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        k[i] = ordered(most[i]);
+        const bool there = most[i] > -infinity();
+        least = min(least, there ? k[i] : 0xffffffffu);
+        n += __builtin_popcountll(__builtin_amdgcn_ballot_w64(there));
+    }
+    least = __builtin_bit_cast(uint32_t, wave_min(__builtin_bit_cast(int, least ^ 0x80000000u))) ^ 0x80000000u;
+    all = some = -infinity();
+    if (n < part) return;
+    const uint32_t hi = ordered(m) + 1;
+    uint32_t lo = least;
+    if (n >= top) {
+        lo = reached(k, lo, hi, top);
+        all = from_ordered(lo);
+    }
+    some = part < top ? from_ordered(reached(k, lo, hi, part)) : all;
 }
 
 // Entries of a wave's list of candidates for the best classes.
@@ -296,12 +350,12 @@ constexpr int CANDIDATES = 256;
 // 2048 rows of 100003 bf16 with their 20 best: searching 20 times takes 1480
 // us, candidates 278.
 template <bool F32, int W, int V>
-__global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const ScoreArgs a) {
+__global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_kernel(const ScoreArgs a) {
     constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W);
     __shared__ Part parts[W];
     __shared__ Best best[W];
     __shared__ u64 list[TEAMS * W][CANDIDATES];
-    __shared__ float reaches[W];
+    __shared__ float reaches[W], part_reaches[W];
     __shared__ int counts[W];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const int team = W == 1 ? wave : 0, w = W == 1 ? 0 : wave, tid = W == 1 ? lane : (int)threadIdx.x;
@@ -320,7 +374,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const Sc
     const bool here = a.rank && in && w == 0 && label >= lo && label < hi;
     const float near = here && piece + lane < label ? logit(a.l, z, piece + lane) : quiet();
     Groups<F32, V> most;
-    Part p = wave_part<F32, W, V>(h, a.l.c, most);
+    Part p = wave_part<true, F32, W, V>(h, a.l.c, most);
     if (a.rank && in) {
         int n = 0;
         if (z_label > -infinity()) {
@@ -347,9 +401,31 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const Sc
             p.before = wave_sum(n);
         }
     }
-    float reach = a.top ? wave_reach<F32, V>(most, a.top) : 0.f;
+    // what every wave's share of the best classes reaches is reached by `top`
+    // of the team's elements, and so is what `top` of a single wave's reach
+    float reach = 0.f, part_reach = 0.f;
+    if (a.top) {
+        const int part = (a.top + W - 1) / W;
+        using G = Groups<F32, V>;
+        if (a.top <= 24 || G::N == 1) {   // (with fewer lanes than that the bound is a good one)
+            float x[1] = {most.most[0]};
+#pragma unroll
+            for (int i = 1; i < G::N; ++i) x[0] = max3(x[0], most.most[i], most.most[i]);
+            wave_reach(x, p.m, a.top, part, reach, part_reach);
+        } else {
+            float x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = i < G::N ? most.most[i] : -infinity();
+#pragma unroll
+            for (int i = 4; i < G::N; ++i) x[i % 4] = max3(x[i % 4], most.most[i], most.most[i]);
+            wave_reach(x, p.m, a.top, part, reach, part_reach);
+        }
+    }
     if constexpr (W > 1)
-        if (lane == 0) reaches[w] = reach;
+        if (lane == 0) {
+            reaches[w] = reach;
+            part_reaches[w] = part_reach;
+        }
     p = team_part<W>(p, parts, w, a.l.c);   // (a barrier)
     const Results q = results(p);
     if (tid == 0) {
@@ -368,8 +444,13 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const Sc
         }
     };
     if constexpr (W > 1) {
+        part_reach = part_reaches[0];
 #pragma unroll
-        for (int i = 0; i < W; ++i) reach = max3(reach, reaches[i], reaches[i]);
+        for (int i = 0; i < W; ++i) {
+            reach = max3(reach, reaches[i], reaches[i]);
+            part_reach = fminf(part_reach, part_reaches[i]);
+        }
+        reach = max3(reach, part_reach, part_reach);
     }
     reach = max3(reach, -3.402823466e38f, -3.402823466e38f);   // (classes not offered are no candidates)
     u64 *const mine = list[team * W + w];
@@ -377,6 +458,11 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const Sc
     if (!q.lost) {   // (chunks: another one may be; the join sees to that)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
+            using G = Groups<F32, V>;
+            float m = most.most[v * G::SUB];
+#pragma unroll
+            for (int i = 1; i < G::SUB; ++i) m = max3(m, most.most[v * G::SUB + i], most.most[v * G::SUB + i]);
+            if (!__builtin_amdgcn_ballot_w64(m >= reach)) continue;
             const int at = h.at(v);
             h.again(v);
 #pragma unroll
@@ -418,6 +504,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void score_kernel(const Sc
             for (int l = 0; l < W; ++l) {
                 const u64 *const other = list[team * W + l];
                 const int m = W == 1 ? n : counts[l];
+#pragma unroll 4
                 for (int k = 0; k < m; ++k) before += other[k] > key;
             }
             if (before < a.top) put(before, of_key(key));
@@ -464,8 +551,7 @@ __global__ __launch_bounds__(256) void score_join_kernel(const ScoreArgs a) {
     __shared__ u64 keys[ANSWER_MAX_CHUNKS * TOP_MAX];
     const int row = blockIdx.x, tid = threadIdx.x, chunks = a.l.chunks, n = chunks * a.top;
     const int64_t at = (int64_t)row * chunks;
-    Part p = a.part[at];
-    for (int i = 1; i < chunks; ++i) p = joined(p, a.part[at + i], a.l.c);
+    const Part p = chunks_part(a.part + at, chunks, a.l.c);
     const Results q = results(p);
     if (tid == 0) {
         const int label = a.labels ? a.labels[row] : -1;
@@ -549,10 +635,9 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void distill_kernel(const 
     Part p;
     Groups<F32, V> most;
     if (a.l.chunks > 1) {
-        p = a.part[(int64_t)row * a.l.chunks];
-        for (int i = 1; i < a.l.chunks; ++i) p = joined(p, a.part[(int64_t)row * a.l.chunks + i], a.l.c);
+        p = chunks_part(a.part + (int64_t)row * a.l.chunks, a.l.chunks, a.l.c);
     } else {
-        p = team_part<W>(wave_part<F32, W, V>(h, a.l.c, most), parts, w, a.l.c);
+        p = team_part<W>(wave_part<false, F32, W, V>(h, a.l.c, most), parts, w, a.l.c);
     }
     const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
     const float t_entry = (z_entry - p.m) * a.l.c;
@@ -624,6 +709,7 @@ hipError_t score_form(const ScoreArgs &a, hipStream_t s) {
         case 104: return go(&score_kernel<F32, 1, 4>, a, s);
         case 402: return go(&score_kernel<F32, 4, 2>, a, s);
         case 404: return go(&score_kernel<F32, 4, 4>, a, s);
+        case 804: return go(&score_kernel<F32, 8, 4>, a, s);
         case 808: return go(&score_kernel<F32, 8, 8>, a, s);
     }
     return hipErrorInvalidValue;
@@ -636,6 +722,7 @@ hipError_t distill_form(const DistillArgs &a, hipStream_t s) {
         case 104: return go(&distill_kernel<F32, 1, 4>, a, s);
         case 402: return go(&distill_kernel<F32, 4, 2>, a, s);
         case 404: return go(&distill_kernel<F32, 4, 4>, a, s);
+        case 804: return go(&distill_kernel<F32, 8, 4>, a, s);
         case 808: return go(&distill_kernel<F32, 8, 8>, a, s);
         case 1608: return go(&distill_kernel<F32, 16, 8>, a, s);
         case 1612: return go(&distill_kernel<F32, 16, 12>, a, s);
