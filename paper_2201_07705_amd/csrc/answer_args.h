@@ -9,7 +9,7 @@
 namespace gemel {
 
 constexpr int TOP_MAX = 64;              // entries of a row: one for each lane of a wave
-constexpr int ANSWER_MAX_CHUNKS = 64;    // workgroups of a row
+constexpr int ANSWER_MAX_CHUNKS = 64;    // parts of a row: one for each lane of a wave
 
 // Rows of logits, and how they are cut: a team of `waves` waves holds `vecs`
 // pieces of 16 bytes in each lane, `chunk` classes of a row at most.
@@ -54,7 +54,8 @@ struct DistillArgs {
     float *loss;         // [rows] or null
     void *dz;            // or null
     int64_t ldd;
-    const Part *part;    // chunks > 1: sums of every chunk
+    const Part *part;    // chunks > 1: [rows][parts] sums of the row's parts
+    int parts;
 };
 
 struct AnswerForm {

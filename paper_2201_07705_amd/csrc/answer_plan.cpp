@@ -7,7 +7,7 @@
 
 namespace gemel {
 
-const AnswerForm answer_forms[ANSWER_FORMS] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 8}, {16, 12}};
+const AnswerForm answer_forms[ANSWER_FORMS] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 4}, {16, 9}};
 
 namespace {
 void cut(Logits &l, const AnswerForm &f) {
@@ -31,11 +31,11 @@ void score_plan(Logits &l, int) {
     }
 }
 void distill_plan(Logits &l) {
-    for (int i = 0; i < ANSWER_FORMS; ++i) {
+    for (int i : {0, 1, 2, 3, 4, 5, 7, 8}) {
         cut(l, answer_forms[i]);
         if (l.chunks == 1) return;
     }
-    score_plan(l, 0);
+    cut(l, answer_forms[4]);
 }
 
 int64_t answer_groups(const Logits &l) {
@@ -45,13 +45,14 @@ int64_t answer_groups(const Logits &l) {
 
 static bool logits_valid(const Logits &l) {
     return l.z && l.rows > 0 && l.classes > 0 && l.ld >= l.classes && form_of(l) && l.chunk > 0 &&
-           l.chunk <= l.waves * l.vecs * 64 * answer_vec(l.f32) && l.chunks >= 1 && l.chunks <= ANSWER_MAX_CHUNKS &&
+           l.chunk <= l.waves * l.vecs * 64 * answer_vec(l.f32) && l.chunks >= 1 && l.chunks <= 65535 &&
            (int64_t)l.chunk * l.chunks >= l.classes && (int64_t)l.chunk * (l.chunks - 1) < l.classes && l.c > 0 && l.inv_t > 0 &&
            (uintptr_t)l.z % (l.f32 ? 4 : 2) == 0 && answer_groups(l) * l.waves * answer_teams(l.waves) * 64 <= MAX_THREADS;
 }
 
 bool score_valid(const ScoreArgs &a) {
-    if (!logits_valid(a.l) || a.top < 0 || a.top > TOP_MAX || a.l.waves > 8) return false;
+    if (!logits_valid(a.l) || a.top < 0 || a.top > TOP_MAX || a.l.waves > 8 || a.l.chunks > ANSWER_MAX_CHUNKS)
+        return false;
     if (a.l.chunks > 1 && (!a.part || (a.top && (!a.list_value || !a.list_index)))) return false;
     return (a.log_prob || a.rank) ? a.labels != nullptr : true;
 }
@@ -59,7 +60,7 @@ bool score_valid(const ScoreArgs &a) {
 bool distill_valid(const DistillArgs &a) {
     return logits_valid(a.l) && a.k >= 1 && a.k <= TOP_MAX && a.index && a.value && (a.loss || a.dz) && a.t > 0 &&
            (!a.dz || (a.ldd >= a.l.classes && (uintptr_t)a.dz % (a.l.f32 ? 4 : 2) == 0)) &&
-           (a.l.chunks == 1 || a.part);
+           (a.l.chunks == 1 || (a.part && a.parts >= 1 && a.parts <= ANSWER_MAX_CHUNKS));
 }
 
 }  // namespace gemel

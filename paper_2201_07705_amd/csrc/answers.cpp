@@ -87,7 +87,9 @@ gemel_status distill(gemel_ctx *ctx, DistillArgs a, hipStream_t stream) {
         Call c{ctx, st, stream, nullptr, {}, nullptr};
         ScoreArgs sums{};
         sums.l = a.l;
-        const size_t o_part = c.lay.take((int64_t)a.l.rows * a.l.chunks, sizeof(Part));
+        score_plan(sums.l, 0);
+        a.parts = sums.l.chunks;
+        const size_t o_part = c.lay.take((int64_t)a.l.rows * a.parts, sizeof(Part));
         if (gemel_status s = workspace(c)) return s;
         a.part = sums.part = c.at<Part>(o_part);
         OPCHK(launch_score(sums, stream), "sums of wide rows");

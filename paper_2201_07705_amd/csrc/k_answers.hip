@@ -79,12 +79,14 @@ __device__ __forceinline__ void team_sync() {
 
 // Classes [lo, hi) of a row in a team's registers: piece v of a lane begins
 // at class at(v). A piece that would pass the end is moved back to end there,
-// and what the piece before it holds already is -inf in it.
-template <bool F32, int W, int V>
+// and what the piece before it holds already is -inf in it. The last L pieces
+// stay in LDS between their uses.
+template <bool F32, int W, int V, int L = 0>
 struct Held {
     static constexpr int VEC = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
     uint4 raw[V];
     int lo, hi, tid;
+    uint4 (*parked)[W * 64];
 
     __device__ __forceinline__ int first(int v) const { return lo + (v * W * 64 + tid) * VEC; }
     __device__ __forceinline__ int at(int v) const { return hi - lo < VEC ? first(v) : min(first(v), hi - VEC); }
@@ -110,9 +112,17 @@ struct Held {
     // or every exponential, in several times the registers). The sums or stores
     // of the piece before are done first.
     __device__ __forceinline__ void again(int v) {
+        if constexpr (L > 0)
+            if (v >= V - L) raw[v] = parked[v - (V - L)][tid];
         asm volatile("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w)::"memory");
     }
+    __device__ __forceinline__ void park(int v) {
+        if constexpr (L > 0)
+            if (v >= V - L) parked[v - (V - L)][tid] = raw[v];
+    }
     __device__ __forceinline__ void again(int v, float &s, float &a) {
+        if constexpr (L > 0)
+            if (v >= V - L) raw[v] = parked[v - (V - L)][tid];
         asm volatile("" : "+v"(raw[v].x), "+v"(raw[v].y), "+v"(raw[v].z), "+v"(raw[v].w), "+v"(s), "+v"(a));
     }
     __device__ __forceinline__ void load(const char *row, int lo_, int hi_, int tid_) {
@@ -175,10 +185,11 @@ struct Groups {
 // Where m c is of ordinary size t = z c - r, r being m c rounded, is one
 // operation instead of two; its sums are then those for m but for a factor of
 // 2^d, d = m c - r. (Elements that are far apart would lose bits there.)
-template <bool A, bool F32, int W, int V>
-__device__ __forceinline__ Part wave_part(Held<F32, W, V> &h, float c, Groups<F32, V> &most) {
+template <bool A, bool F32, int W, int V, int L>
+__device__ __forceinline__ Part wave_part(Held<F32, W, V, L> &h, float c, Groups<F32, V> &most) {
     constexpr int VEC = Held<F32, W, V>::VEC;
     using G = Groups<F32, V>;
+    static_assert(!L || G::SUB == 1, "parked pieces are groups");
     float m = -infinity();
 #pragma unroll
     for (int g = 0; g < G::N; ++g) {
@@ -190,6 +201,7 @@ __device__ __forceinline__ Part wave_part(Held<F32, W, V> &h, float c, Groups<F3
             x = max3(x, h.get(v, k), h.get(v, k + 1));
         }
         m = max3(m, x, x);
+        h.park(g);
     }
     m = wave_max(m);
     const float ref = m == -infinity() ? 0.f : m, r = ref * c;
@@ -374,7 +386,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_
     const bool here = a.rank && in && w == 0 && label >= lo && label < hi;
     const float near = here && piece + lane < label ? logit(a.l, z, piece + lane) : quiet();
     Groups<F32, V> most;
-    Part p = wave_part<true, F32, W, V>(h, a.l.c, most);
+    Part p = wave_part<true>(h, a.l.c, most);
     if (a.rank && in) {
         int n = 0;
         if (z_label > -infinity()) {
@@ -601,10 +613,11 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // entries of one class added up. Every wave of a team keeps entry i in lane
 // i. What a lane writes for a class with an entry it overwrites itself, so
 // that the order of the two stores is that of the program.
-template <bool F32, int W, int V>
-__global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void distill_kernel(const DistillArgs a) {
+template <bool F32, int W, int V, int L = 0>
+__global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(const DistillArgs a) {
     constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W), SIZE = F32 ? 4 : 2;
     __shared__ Part parts[W];
+    __shared__ uint4 parked[L ? L : 1][L ? W * 64 : 1];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
     const int team = W == 1 ? wave : 0, w = W == 1 ? 0 : wave, tid = W == 1 ? lane : (int)threadIdx.x;
     const int row = (int)blockIdx.x * TEAMS + team, chunk = blockIdx.y;
@@ -618,7 +631,8 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void distill_kernel(const 
         value = a.value[(int64_t)row * a.k + lane];
     }
     const float weight = a.dloss ? a.dloss[row] : 1.f;
-    Held<F32, W, V> h;
+    Held<F32, W, V, L> h;
+    if constexpr (L > 0) h.parked = parked;
     h.load(z, lo, hi, tid);
     const bool bad = __builtin_amdgcn_ballot_w64(index < -1 || index >= a.l.classes) != 0;
     if (index >= a.l.classes) index = -1;
@@ -635,9 +649,9 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64)) void distill_kernel(const 
     Part p;
     Groups<F32, V> most;
     if (a.l.chunks > 1) {
-        p = chunks_part(a.part + (int64_t)row * a.l.chunks, a.l.chunks, a.l.c);
+        p = chunks_part(a.part + (int64_t)row * a.parts, a.parts, a.l.c);
     } else {
-        p = team_part<W>(wave_part<false, F32, W, V>(h, a.l.c, most), parts, w, a.l.c);
+        p = team_part<W>(wave_part<false>(h, a.l.c, most), parts, w, a.l.c);
     }
     const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
     const float t_entry = (z_entry - p.m) * a.l.c;
@@ -723,9 +737,8 @@ hipError_t distill_form(const DistillArgs &a, hipStream_t s) {
         case 402: return go(&distill_kernel<F32, 4, 2>, a, s);
         case 404: return go(&distill_kernel<F32, 4, 4>, a, s);
         case 804: return go(&distill_kernel<F32, 8, 4>, a, s);
-        case 808: return go(&distill_kernel<F32, 8, 8>, a, s);
-        case 1608: return go(&distill_kernel<F32, 16, 8>, a, s);
-        case 1612: return go(&distill_kernel<F32, 16, 12>, a, s);
+        case 1604: return go(&distill_kernel<F32, 16, 4>, a, s);
+        case 1609: return go(&distill_kernel<F32, 16, 9, 4>, a, s);
     }
     return hipErrorInvalidValue;
 }

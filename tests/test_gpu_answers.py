@@ -267,7 +267,7 @@ def teacher(z, k, seed=1, noise=0.5):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("classes", WIDTHS + [131072, 131073, 300001])
+@pytest.mark.parametrize("classes", WIDTHS + [73728, 73729, 131072, 300001, 1 << 20])
 def test_distill_of_any_width(ctx, classes, dtype):
     import torch
     rows = 3 if classes > 4000 else 33
