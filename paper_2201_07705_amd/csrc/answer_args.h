@@ -11,8 +11,9 @@ namespace gemel {
 constexpr int TOP_MAX = 64;              // entries of a row: one for each lane of a wave
 constexpr int ANSWER_MAX_CHUNKS = 64;    // parts of a row: one for each lane of a wave
 
-// Rows of logits, and how they are cut: a team of `waves` waves holds `vecs`
-// pieces of 16 bytes in each lane, `chunk` classes of a row at most.
+// Rows of logits, and how they are cut: a team of `waves` waves (0: of 16
+// lanes) holds `vecs` pieces of 16 bytes in each lane, `chunk` classes of a
+// row at most.
 struct Logits {
     const void *z;
     int64_t ld;
@@ -61,11 +62,13 @@ struct DistillArgs {
 struct AnswerForm {
     int waves, vecs;
 };
-constexpr int ANSWER_FORMS = 9;
+constexpr int ANSWER_FORMS = 11;
 extern const AnswerForm answer_forms[ANSWER_FORMS];
 constexpr int answer_vec(int f32) { return f32 ? 4 : 8; }   // classes of a piece
 // Rows that a workgroup holds at once
-constexpr int answer_teams(int waves) { return waves == 1 ? 4 : 1; }
+constexpr int answer_teams(int waves) { return waves == 0 ? 16 : waves == 1 ? 4 : 1; }
+constexpr int answer_lanes(int waves) { return waves == 0 ? 16 : waves * 64; }   // of a team
+constexpr int answer_threads(int waves) { return answer_teams(waves) * answer_lanes(waves); }
 
 void score_plan(Logits &l, int top);
 void distill_plan(Logits &l);

@@ -7,13 +7,14 @@
 
 namespace gemel {
 
-const AnswerForm answer_forms[ANSWER_FORMS] = {{1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 4}, {16, 9}};
+const AnswerForm answer_forms[ANSWER_FORMS] = {
+    {0, 1}, {0, 2}, {1, 1}, {1, 2}, {1, 4}, {4, 2}, {4, 4}, {8, 4}, {8, 8}, {16, 4}, {16, 9}};
 
 namespace {
 void cut(Logits &l, const AnswerForm &f) {
     l.waves = f.waves;
     l.vecs = f.vecs;
-    l.chunk = f.waves * f.vecs * 64 * answer_vec(l.f32);
+    l.chunk = answer_lanes(f.waves) * f.vecs * answer_vec(l.f32);
     l.chunks = (l.classes + l.chunk - 1) / l.chunk;
 }
 bool form_of(const Logits &l) {
@@ -23,19 +24,20 @@ bool form_of(const Logits &l) {
 }
 }  // namespace
 
-// The smallest form that holds a row; wide rows in chunks.
-void score_plan(Logits &l, int) {
-    for (int i = 0; i < 7; ++i) {
+// The smallest form that holds a row (16 lanes search each of the best
+// classes in turn: only a few); wide rows in chunks.
+void score_plan(Logits &l, int top) {
+    for (int i = top <= 32 ? 0 : 2; i < 9; ++i) {
         cut(l, answer_forms[i]);
-        if (l.chunks <= (i < 4 ? 1 : ANSWER_MAX_CHUNKS)) return;
+        if (l.chunks <= (i < 6 ? 1 : ANSWER_MAX_CHUNKS)) return;
     }
 }
 void distill_plan(Logits &l) {
-    for (int i : {0, 1, 2, 3, 4, 5, 7, 8}) {
+    for (int i : {0, 1, 2, 3, 4, 5, 6, 7, 9, 10}) {
         cut(l, answer_forms[i]);
         if (l.chunks == 1) return;
     }
-    cut(l, answer_forms[4]);
+    cut(l, answer_forms[6]);
 }
 
 int64_t answer_groups(const Logits &l) {
@@ -45,9 +47,9 @@ int64_t answer_groups(const Logits &l) {
 
 static bool logits_valid(const Logits &l) {
     return l.z && l.rows > 0 && l.classes > 0 && l.ld >= l.classes && form_of(l) && l.chunk > 0 &&
-           l.chunk <= l.waves * l.vecs * 64 * answer_vec(l.f32) && l.chunks >= 1 && l.chunks <= 65535 &&
+           l.chunk <= answer_lanes(l.waves) * l.vecs * answer_vec(l.f32) && l.chunks >= 1 && l.chunks <= 65535 &&
            (int64_t)l.chunk * l.chunks >= l.classes && (int64_t)l.chunk * (l.chunks - 1) < l.classes && l.c > 0 && l.inv_t > 0 &&
-           (uintptr_t)l.z % (l.f32 ? 4 : 2) == 0 && answer_groups(l) * l.waves * answer_teams(l.waves) * 64 <= MAX_THREADS;
+           (uintptr_t)l.z % (l.f32 ? 4 : 2) == 0 && answer_groups(l) * answer_threads(l.waves) <= MAX_THREADS;
 }
 
 bool score_valid(const ScoreArgs &a) {

@@ -77,18 +77,18 @@ __device__ __forceinline__ void team_sync() {
     }
 }
 
-// Classes [lo, hi) of a row in a team's registers: piece v of a lane begins
+// Classes [lo, hi) of a row in the registers of T threads: piece v of a lane begins
 // at class at(v). A piece that would pass the end is moved back to end there,
 // and what the piece before it holds already is -inf in it. The last L pieces
 // stay in LDS between their uses.
-template <bool F32, int W, int V, int L = 0>
+template <bool F32, int T, int V, int L = 0>
 struct Held {
     static constexpr int VEC = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
     uint4 raw[V];
     int lo, hi, tid;
-    uint4 (*parked)[W * 64];
+    uint4 (*parked)[T];
 
-    __device__ __forceinline__ int first(int v) const { return lo + (v * W * 64 + tid) * VEC; }
+    __device__ __forceinline__ int first(int v) const { return lo + (v * T + tid) * VEC; }
     __device__ __forceinline__ int at(int v) const { return hi - lo < VEC ? first(v) : min(first(v), hi - VEC); }
     __device__ __forceinline__ float get(int v, int j) const {
         if constexpr (F32)
@@ -146,10 +146,10 @@ struct Held {
         }
 #pragma unroll
         for (int v = 0; v < V; ++v) raw[v] = get_16b(row + (uint32_t)at(v) * SIZE);
-        const int wave0 = (tid & ~63) + 64;
+        const int next = T < 64 ? T : (tid & ~63) + 64;
 #pragma unroll
         for (int v = 0; v < V; ++v)
-            if (lo + (v * W * 64 + wave0) * VEC > hi) mask(v, first(v) - at(v));
+            if (lo + (v * T + next) * VEC > hi) mask(v, first(v) - at(v));
     }
 };
 
@@ -185,9 +185,9 @@ struct Groups {
 // Where m c is of ordinary size t = z c - r, r being m c rounded, is one
 // operation instead of two; its sums are then those for m but for a factor of
 // 2^d, d = m c - r. (Elements that are far apart would lose bits there.)
-template <bool A, bool F32, int W, int V, int L>
-__device__ __forceinline__ Part wave_part(Held<F32, W, V, L> &h, float c, Groups<F32, V> &most) {
-    constexpr int VEC = Held<F32, W, V>::VEC;
+template <bool A, bool F32, int T, int V, int L>
+__device__ __forceinline__ Part wave_part(Held<F32, T, V, L> &h, float c, Groups<F32, V> &most) {
+    constexpr int VEC = Held<F32, T, V>::VEC;
     using G = Groups<F32, V>;
     static_assert(!L || G::SUB == 1, "parked pieces are groups");
     float m = -infinity();
@@ -363,7 +363,7 @@ constexpr int CANDIDATES = 256;
 // us, candidates 278.
 template <bool F32, int W, int V>
 __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_kernel(const ScoreArgs a) {
-    constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W);
+    constexpr int VEC = F32 ? 4 : 8, TEAMS = answer_teams(W);
     __shared__ Part parts[W];
     __shared__ Best best[W];
     __shared__ u64 list[TEAMS * W][CANDIDATES];
@@ -378,7 +378,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_
     const int lo = chunk * a.l.chunk, hi = min(a.l.classes, lo + a.l.chunk);
     const int label = a.labels ? a.labels[row] : -1;
     const bool in = label >= 0 && label < a.l.classes;
-    Held<F32, W, V> h;
+    Held<F32, W * 64, V> h;
     h.load(z, lo, hi, tid);
     const float z_label = in ? logit(a.l, z, label) : 0.f;
     // the classes before the label in its piece, one for each lane
@@ -419,7 +419,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_
     if (a.top) {
         const int part = (a.top + W - 1) / W;
         using G = Groups<F32, V>;
-        if (a.top <= 24 || G::N == 1) {   // (with fewer lanes than that the bound is a good one)
+        if (a.top <= 24 && hi - lo >= 4 * VEC * a.top) {   // (fine groups where lanes are few)
             float x[1] = {most.most[0]};
 #pragma unroll
             for (int i = 1; i < G::N; ++i) x[0] = max3(x[0], most.most[i], most.most[i]);
@@ -615,7 +615,7 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 // that the order of the two stores is that of the program.
 template <bool F32, int W, int V, int L = 0>
 __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(const DistillArgs a) {
-    constexpr int VEC = Held<F32, W, V>::VEC, TEAMS = answer_teams(W), SIZE = F32 ? 4 : 2;
+    constexpr int VEC = F32 ? 4 : 8, TEAMS = answer_teams(W), SIZE = F32 ? 4 : 2;
     __shared__ Part parts[W];
     __shared__ uint4 parked[L ? L : 1][L ? W * 64 : 1];
     const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
@@ -631,7 +631,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(con
         value = a.value[(int64_t)row * a.k + lane];
     }
     const float weight = a.dloss ? a.dloss[row] : 1.f;
-    Held<F32, W, V, L> h;
+    Held<F32, W * 64, V, L> h;
     if constexpr (L > 0) h.parked = parked;
     h.load(z, lo, hi, tid);
     const bool bad = __builtin_amdgcn_ballot_w64(index < -1 || index >= a.l.classes) != 0;
@@ -708,16 +708,229 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(con
     }
 }
 
+// ---- rows of few classes: 16 lanes to a row, 4 rows to a wave ----
+//
+// A wave to a row leaves most lanes idle and repeats what is done once for
+// each row: 97344 rows of 80 float32 classes, loss and gradient of 10 entries,
+// 60 us against 20.
+
+// Reductions over 16 lanes, by rotation: every lane gets the same bits.
+template <typename T, typename F>
+__device__ __forceinline__ T row_reduce(T v, F f) {
+    v = f(v, moved<0x128>(v, v));   // row_ror 8, 4, 2, 1
+    v = f(v, moved<0x124>(v, v));
+    v = f(v, moved<0x122>(v, v));
+    return f(v, moved<0x121>(v, v));
+}
+__device__ __forceinline__ float row_max(float v) {
+    return row_reduce(v, [](float a, float b) { return max3(a, b, b); });
+}
+__device__ __forceinline__ float row_sum(float v) {
+    return row_reduce(v, [](float a, float b) { return a + b; });
+}
+__device__ __forceinline__ int row_sum(int v) {
+    return row_reduce(v, [](int a, int b) { return a + b; });
+}
+__device__ __forceinline__ int row_min(int v) {
+    return row_reduce(v, [](int a, int b) { return min(a, b); });
+}
+
+// Sums of a row that 16 lanes hold.
+template <bool A, bool F32, int V>
+__device__ __forceinline__ Part row_part(const Held<F32, 16, V> &h, float c) {
+    constexpr int VEC = Held<F32, 16, V>::VEC;
+    float m = -infinity(), s = 0.f, a = 0.f;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < VEC; j += 2) m = max3(m, h.get(v, j), h.get(v, j + 1));
+    m = row_max(m);
+    const float ref = m == -infinity() ? 0.f : m;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const float t = (h.get(v, j) - ref) * c;
+            const float e = __builtin_amdgcn_exp2f(t);
+            s += e;
+            if constexpr (A) a = __builtin_fmaf(e, fmaxf(t, -1e30f), a);
+        }
+    return Part{m, row_sum(s), A ? row_sum(a) : 0.f, 0};
+}
+
+template <bool F32, int V>
+__global__ __launch_bounds__(256) void score_small_kernel(const ScoreArgs a) {
+    constexpr int VEC = F32 ? 4 : 8;
+    const int lane = threadIdx.x & 15, at_row = blockIdx.x * 16 + (threadIdx.x >> 4), row = min(at_row, a.l.rows - 1);
+    const bool there = at_row < a.l.rows;
+    const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * (F32 ? 4 : 2);
+    const int label = a.labels ? a.labels[row] : -1;
+    const bool in = label >= 0 && label < a.l.classes;
+    Held<F32, 16, V> h;
+    h.load(z, 0, a.l.classes, lane);
+    const float z_label = in ? logit(a.l, z, label) : 0.f;
+    Part p = row_part<true>(h, a.l.c);
+    float x[V * VEC];
+    int n = 0;
+#pragma unroll
+    for (int v = 0; v < V; ++v)
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) {
+            const int i = h.at(v) + j;
+            x[v * VEC + j] = h.get(v, j);
+            if (i < h.first(v) || i >= a.l.classes) continue;
+            n += x[v * VEC + j] > z_label || (x[v * VEC + j] == z_label && i < label);
+        }
+    p.before = row_sum(n);
+    const Results q = results(p);
+    if (lane == 0 && there) put_row(a, row, p, label, z_label);
+    for (int k = 0; k < a.top; ++k) {
+        Best b{-infinity(), 0x7fffffff};
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (x[v * VEC + j] > b.z) b = Best{x[v * VEC + j], h.at(v) + j};
+        const float top = row_max(b.z);
+        b.i = row_min(b.z == top ? b.i : 0x7fffffff);
+#pragma unroll
+        for (int v = 0; v < V; ++v)
+#pragma unroll
+            for (int j = 0; j < VEC; ++j)
+                if (h.at(v) + j == b.i) x[v * VEC + j] = -infinity();
+        if (lane == 0 && there) put_top(a, row, k, p, q, top, top == -infinity() ? -1 : b.i);
+    }
+}
+
+// E entries to a lane.
+template <bool F32, int V, int E>
+__global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a) {
+    constexpr int VEC = F32 ? 4 : 8, SIZE = F32 ? 4 : 2;
+    const int lane = threadIdx.x & 15, at_row = blockIdx.x * 16 + (threadIdx.x >> 4), row = min(at_row, a.l.rows - 1);
+    const bool there = at_row < a.l.rows;
+    const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * SIZE;
+    int index[E];
+    float v[E], z_entry[E], share[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        const bool here = i * 16 + lane < a.k;
+        const int64_t at = (int64_t)row * a.k + (here ? i * 16 + lane : 0);
+        index[i] = here ? a.index[at] : -1;
+        v[i] = a.value[at];
+    }
+    const float weight = a.dloss ? a.dloss[row] : 1.f;
+    Held<F32, 16, V> h;
+    h.load(z, 0, a.l.classes, lane);
+    int wrong = 0, some = 0;
+    float v_most = -infinity();
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        wrong |= index[i] < -1 || index[i] >= a.l.classes;
+        if (index[i] >= a.l.classes || index[i] < 0) index[i] = -1;
+        z_entry[i] = index[i] >= 0 ? logit(a.l, z, index[i]) : 0.f;
+        v[i] = index[i] >= 0 ? v[i] * a.l.inv_t : -infinity();
+        some |= !(v[i] == -infinity());
+        v_most = max3(v_most, v[i], v[i]);
+    }
+    wrong = row_sum(wrong);
+    some = row_sum(some | wrong);
+    v_most = row_max(v_most);
+    float mass = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        share[i] = index[i] >= 0 ? expf(v[i] - (v_most == -infinity() ? 0.f : v_most)) : 0.f;
+        mass += share[i];
+    }
+    mass = wrong ? quiet() : row_sum(mass);
+#pragma unroll
+    for (int i = 0; i < E; ++i) share[i] /= mass;
+    const Part p = row_part<false>(h, a.l.c);
+    const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
+    if (a.loss) {
+        const float log_mass = logf(mass), log_s = LN2 * log2f(p.s);
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < E; ++i) {
+            const float log_q = v[i] - v_most - log_mass, log_p = (z_entry[i] - p.m) * a.l.inv_t - log_s;
+            if (share[i] > 0.f) sum += share[i] * (log_q - log_p);
+        }
+        sum = row_sum(sum);
+        if (lane == 0 && there) a.loss[row] = !some ? 0.f : lost ? quiet() : a.t * a.t * sum;
+    }
+    if (!a.dz || !there) return;
+    char *const d = (char *)a.dz + (int64_t)row * a.ldd * SIZE;
+    const float coef = !some ? 0.f : lost ? quiet() : weight * a.t, by = coef / p.s;
+    auto gradient = [&](float x) __attribute__((always_inline)) {
+        return some ? by * __builtin_amdgcn_exp2f((x - p.m) * a.l.c) : 0.f;
+    };
+    auto put = [&](int i, float g) __attribute__((always_inline)) {
+        if constexpr (F32)
+            *(float *)(d + (uint32_t)i * 4) = g;
+        else
+            *(u16 *)(d + (uint32_t)i * 2) = __builtin_bit_cast(u16, (__bf16)g);
+    };
+#pragma unroll
+    for (int k = 0; k < V; ++k) {
+        uint4 x;
+        if constexpr (F32) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (&x.x)[j] = __float_as_uint(gradient(h.get(k, j)));
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) (&x.x)[j] = pack2(gradient(h.get(k, 2 * j)), gradient(h.get(k, 2 * j + 1)));
+        }
+        const int f = h.first(k);
+        if (f + VEC <= a.l.classes) *(u32x4_any *)(d + (uint32_t)f * SIZE) = __builtin_bit_cast(u32x4_any, x);
+    }
+    const int tail = a.l.classes / VEC * VEC + lane;
+    if (tail < a.l.classes) put(tail, gradient(logit(a.l, z, tail)));
+    if (!some) return;
+    // classes with an entry are written again, by the entry's lane, after the
+    // stores of the whole row (the wave's own, which stay in order); entries of
+    // one class write the same
+    float q[E];
+#pragma unroll
+    for (int i = 0; i < E; ++i) q[i] = 0.f;
+    auto add = [&](auto which, int i) __attribute__((always_inline)) {
+        constexpr int J = decltype(which)::value;   // (row_newbcast J)
+        const int cls = moved<0x150 + J>(0, index[i]);
+        const float s = moved<0x150 + J>(0.f, share[i]);
+#pragma unroll
+        for (int k = 0; k < E; ++k) q[k] += index[k] == cls ? s : 0.f;
+    };
+#pragma unroll
+    for (int i = 0; i < E; ++i) {
+        if (i * 16 >= a.k) break;
+#define ENTRY(J) \
+    if (i * 16 + J < a.k) add(std::integral_constant<int, J>{}, i)
+        ENTRY(0); ENTRY(1); ENTRY(2); ENTRY(3); ENTRY(4); ENTRY(5); ENTRY(6); ENTRY(7);
+        ENTRY(8); ENTRY(9); ENTRY(10); ENTRY(11); ENTRY(12); ENTRY(13); ENTRY(14); ENTRY(15);
+#undef ENTRY
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < E; ++i)
+        if (index[i] >= 0) put(index[i], by * __builtin_amdgcn_exp2f((z_entry[i] - p.m) * a.l.c) - coef * q[i]);
+}
+
 template <typename A, typename K>
 hipError_t go(K kernel, const A &a, hipStream_t s) {
     void *p[] = {const_cast<A *>(&a)};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), dim3((unsigned)answer_groups(a.l), (unsigned)a.l.chunks),
-                           dim3(64 * a.l.waves * answer_teams(a.l.waves)), p, 0, s);
+                           dim3((unsigned)answer_threads(a.l.waves)), p, 0, s);
+}
+
+template <bool F32, int V>
+hipError_t distill_small(const DistillArgs &a, hipStream_t s) {
+    return a.k <= 16 ? go(&distill_small_kernel<F32, V, 1>, a, s) : go(&distill_small_kernel<F32, V, 4>, a, s);
 }
 
 template <bool F32>
 hipError_t score_form(const ScoreArgs &a, hipStream_t s) {
     switch (a.l.waves * 100 + a.l.vecs) {
+        case 1: return go(&score_small_kernel<F32, 1>, a, s);
+        case 2: return go(&score_small_kernel<F32, 2>, a, s);
         case 101: return go(&score_kernel<F32, 1, 1>, a, s);
         case 102: return go(&score_kernel<F32, 1, 2>, a, s);
         case 104: return go(&score_kernel<F32, 1, 4>, a, s);
@@ -731,6 +944,8 @@ hipError_t score_form(const ScoreArgs &a, hipStream_t s) {
 template <bool F32>
 hipError_t distill_form(const DistillArgs &a, hipStream_t s) {
     switch (a.l.waves * 100 + a.l.vecs) {
+        case 1: return distill_small<F32, 1>(a, s);
+        case 2: return distill_small<F32, 2>(a, s);
         case 101: return go(&distill_kernel<F32, 1, 1>, a, s);
         case 102: return go(&distill_kernel<F32, 1, 2>, a, s);
         case 104: return go(&distill_kernel<F32, 1, 4>, a, s);
