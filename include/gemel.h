@@ -930,7 +930,7 @@ gemel_status gemel_distill_backward(gemel_ctx *ctx, int32_t rows,
 
 /*
  * A matrix [rows][cols] (rows <= 2^22, 1 <= cols <= 2^20) as codes and scales.
- *  codes   rows of P = 128 * ceil(cols / 256) bytes. Column c of a row is the
+ *  codes   rows of 256 * ceil(cols / 512) bytes. Column c of a row is the
  *          low (c even) or high half of byte c / 2: sign bit 8, and magnitude
  *          0 .. 7 for 0, 0.5, 1, 1.5, 2, 3, 4, 6. Columns beyond cols are zeros.
  *  scales  [ceil(cols / 512)][rows][16] bytes: 2^(byte - 127), 255 for NaN.

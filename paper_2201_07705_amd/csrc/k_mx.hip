@@ -123,7 +123,7 @@ __global__ __launch_bounds__(256) void mx_quantize_kernel(const MxCast a) {
             const uint32_t e = quad_max(v[r].exponent());
             const uint32_t byte = e == 255 ? 255u : max(e, 2u) - 2;
             const uint32_t codes = v[r].codes(e == 255 ? 1.f : scale_of(byte));
-            if (p.c < pitch * 2) *(uint32_t *)(a.q.codes + row * pitch + p.c / 2) = codes;
+            *(uint32_t *)(a.q.codes + row * pitch + p.c / 2) = codes;
             const int q = lane >> 2;
             if ((lane & 3) == 0)
                 a.q.scales[((int64_t)p.group * a.q.rows + row) * 16 + (q & 3) * 4 + (q >> 2)] = (uint8_t)byte;

@@ -15,7 +15,8 @@ namespace {
 typedef __attribute__((address_space(3))) unsigned char lds_u8;
 typedef mx_f32x4 f32x4;
 
-constexpr int ROW = MX_STEP / 2;   // bytes of a row in a step
+constexpr int ROW = MX_GROUP / 8;   // bytes of a row in a step (128 columns)
+constexpr int STAGES = 4;           // a turn of the buffers is a group of scales
 
 template <int N>
 __device__ __forceinline__ void wait_vm() {
@@ -33,20 +34,20 @@ __device__ __forceinline__ void fetch(const uint8_t *base, const uint32_t (&off)
 }
 
 // One T x T tile per workgroup: 8 waves of 128 x 64 (T = 256) or 32 x 64 (T =
-// 128), or 4 of 32 x 32 (T = 64). A step is 256 columns, 128 bytes of each
-// row, fetched by direct global-to-LDS loads into one of STAGES buffers; a
-// buffer is asked for again as soon as every wave has its last fragments in
-// registers. Slot p of a buffer holds row p / 8, 16-byte chunk (p % 8) ^ (row
-// / 2 % 8), so that the fragment reads of 16 rows fall on distinct banks. The
-// scales of two steps are one word of a lane, fetched with the first of them
-// behind the codes.
-template <int T, int STAGES, int PHASES>
+// 128), or 4 of 32 x 32 (T = 64). A step is 128 columns, 64 bytes of each row,
+// fetched by direct global-to-LDS loads into one of four buffers, three steps
+// ahead: a buffer is asked for again as soon as every wave has its last
+// fragments in registers. Slot p of a buffer holds row p / 4, 16-byte chunk
+// (p % 4) ^ (row / 2 % 4), so that the fragment reads of 16 rows fall on
+// distinct banks. The scales of four steps are one word of a lane, fetched
+// with the first of them.
+template <int T>
 __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2) void mx_mm_kernel(const MxMm a) {
     constexpr int NT = mx_threads_of(T), NW = NT / 64, WN = T == 256 ? 4 : 2;
     constexpr int TM = T * WN / NW, TN = T / WN, FM = TM / 16, FN = TN / 16;
-    constexpr int LOADS = T * 8 / NT, CODES = 2 * T * ROW, STAGE = CODES + 2 * T * 16;
-    __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE], st1[STAGE], st2[STAGES > 2 ? STAGE : 16],
-        st3[STAGES > 3 ? STAGE : 16];
+    constexpr int LOADS = T * 4 / NT, STAGE = 2 * T * ROW;
+    constexpr bool HALVES = T == 256;   // (no registers for all fragments of two steps)
+    __shared__ __attribute__((aligned(1024))) unsigned char st0[STAGE], st1[STAGE], st2[STAGE], st3[STAGE], sc[2 * T * 16];
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave - wm * WN, g = lane >> 4, l16 = lane & 15;
@@ -63,12 +64,12 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
     }
     const int m0 = tm * T, n0 = tn * T;
     const int64_t pitch = mx_pitch(a.w.cols);
-    const int s0 = (int)blockIdx.y * a.per * 2, total = min((int)(pitch / ROW) - s0, a.per * 2);
+    const int s0 = (int)blockIdx.y * a.per * 4, total = min((int)(pitch / ROW) - s0, a.per * STAGES);
 
     uint32_t oa[LOADS], ob[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int row = (i * NT + tid) >> 3, ch = ((tid & 7) ^ ((row >> 1) & 7)) * 16;
+        const int row = (i * NT + tid) >> 2, ch = ((tid & 3) ^ ((row >> 1) & 3)) * 16;
         oa[i] = (uint32_t)(min(m0 + row, M - 1) - m0) * (uint32_t)pitch + ch;
         ob[i] = (uint32_t)(min(n0 + row, N - 1) - n0) * (uint32_t)pitch + ch;
     }
@@ -78,23 +79,25 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
     constexpr int PARTS = T / 64;
     const int part = wave % (2 * PARTS), of_w = part >= PARTS, local = (part - of_w * PARTS) * 64 + lane;
     const int srows = of_w ? N : M;
-    const uint8_t *ps = (of_w ? a.w.scales : a.x.scales) + (int64_t)(s0 >> 1) * srows * 16;
+    const uint8_t *ps = (of_w ? a.w.scales : a.x.scales) + (int64_t)(s0 >> 2) * srows * 16;
     const uint32_t os = (uint32_t)min((of_w ? n0 : m0) + local, srows - 1) * 16u;
-    const int sslot = CODES + of_w * T * 16 + (part - of_w * PARTS) * 1024;
+    unsigned char *const sslot = sc + of_w * T * 16 + (part - of_w * PARTS) * 1024;
     int iss = 0;
-    // Requests the next step; past the last one, the last one again (into a
-    // buffer whose reads are over), so that every step waits alike.
-    auto issue = [&](unsigned char *stage, bool even) __attribute__((always_inline)) {
+    // Requests the next step, the P-th of its four; past the last one, the last
+    // one again (into a buffer whose reads are over), so that every step waits
+    // alike.
+    auto issue = [&](auto which, unsigned char *stage) __attribute__((always_inline)) {
+        constexpr int P = decltype(which)::value;
         fetch<LOADS, NW>(pa, oa, stage, wave);
         fetch<LOADS, NW>(pb, ob, stage + T * ROW, wave);
-        if (even) {
+        if constexpr (P == 0) {
             const __amdgpu_buffer_rsrc_t r = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t *>(ps), 0, -1, 0x00020000);
-            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8 *)(stage + sslot), 16, (int)os, 0, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (lds_u8 *)sslot, 16, (int)os, 0, 0, 0);
         }
         if (++iss < total) {
             pa += ROW;
             pb += ROW;
-            if (!even) ps += (int64_t)srows * 16;
+            if (P == 3) ps += (int64_t)srows * 16;
         }
     };
     f32x4 acc[FM][FN];
@@ -102,119 +105,87 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
     for (int i = 0; i < FM; ++i)
 #pragma unroll
         for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    constexpr int NA = PHASES == 4 ? FM / 2 : PHASES == 2 ? FM : 2 * FM, NB = PHASES == 1 ? 2 * FN : FN;
-    i32x4 fa0[NA], fa1[NA], fb0[NB], fb1[NB];
+    constexpr int NA = HALVES ? FM / 2 : FM;
+    i32x4 fa0[NA], fa1[NA], fb0[FN], fb1[FN];
     int sa[FM], sb[FN];
-    const int ra = (wm * TM + l16) * ROW, rb = T * ROW + (wn * TN + l16) * ROW;
-    const int h0 = (g ^ ((l16 >> 1) & 7)) * 16, h1 = ((4 + g) ^ ((l16 >> 1) & 7)) * 16;
-    auto read_a = [&](i32x4(&f)[NA], const unsigned char *s, int h, int row) __attribute__((always_inline)) {
+    const int h = (g ^ ((l16 >> 1) & 3)) * 16;
+    const int ra = (wm * TM + l16) * ROW + h, rb = T * ROW + (wn * TN + l16) * ROW + h;
+    auto read_a = [&](i32x4(&f)[NA], const unsigned char *s, int row) __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < NA; ++i) f[i] = *(const i32x4 *)(s + ra + (row + i) * 16 * ROW);
+    };
+    auto read_b = [&](i32x4(&f)[FN], const unsigned char *s) __attribute__((always_inline)) {
+#pragma unroll
+        for (int j = 0; j < FN; ++j) f[j] = *(const i32x4 *)(s + rb + j * 16 * ROW);
+    };
+    auto read_s = [&]() __attribute__((always_inline)) {
+#pragma unroll
+        for (int i = 0; i < FM; ++i) sa[i] = *(const int *)(sc + (wm * TM + i * 16 + l16) * 16 + g * 4);
+#pragma unroll
+        for (int j = 0; j < FN; ++j) sb[j] = *(const int *)(sc + T * 16 + (wn * TN + j * 16 + l16) * 16 + g * 4);
+    };
+    auto mul = [&](auto which, i32x4(&f)[NA], i32x4(&b)[FN], int row) __attribute__((always_inline)) {
+        constexpr int P = decltype(which)::value;
 #pragma unroll
         for (int i = 0; i < NA; ++i)
-            f[i] = *(const i32x4 *)(s + ra + (PHASES == 1 && i >= FM ? h1 : h) + (row + i % FM) * 16 * ROW);
-    };
-    auto read_b = [&](i32x4(&f)[NB], const unsigned char *s, int h) __attribute__((always_inline)) {
 #pragma unroll
-        for (int j = 0; j < NB; ++j) f[j] = *(const i32x4 *)(s + rb + (PHASES == 1 && j >= FN ? h1 : h) + j % FN * 16 * ROW);
-    };
-    auto read_s = [&](const unsigned char *s) __attribute__((always_inline)) {
-#pragma unroll
-        for (int i = 0; i < FM; ++i) sa[i] = *(const int *)(s + CODES + (wm * TM + i * 16 + l16) * 16 + g * 4);
-#pragma unroll
-        for (int j = 0; j < FN; ++j) sb[j] = *(const int *)(s + CODES + T * 16 + (wn * TN + j * 16 + l16) * 16 + g * 4);
-    };
-    // S: which 128 columns of the group (PHASES == 1: the first of two)
-    auto mul = [&](auto which, i32x4(&f)[NA], i32x4(&b)[NB], int row) __attribute__((always_inline)) {
-        constexpr int S = decltype(which)::value;
-        constexpr int ROWS = PHASES > 1 ? NA : FM;
-#pragma unroll
-        for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-            for (int j = 0; j < FN; ++j) acc[row + i][j] = mx_mul<S>(b[j], f[i], acc[row + i][j], sb[j], sa[row + i]);
-        if constexpr (PHASES == 1) {
-#pragma unroll
-            for (int i = 0; i < ROWS; ++i)
-#pragma unroll
-                for (int j = 0; j < FN; ++j) acc[i][j] = mx_mul<S + 1>(b[FN + j], f[FM + i], acc[i][j], sb[j], sa[i]);
-        }
+            for (int j = 0; j < FN; ++j) acc[row + i][j] = mx_mul<P>(b[j], f[i], acc[row + i][j], sb[j], sa[row + i]);
         __builtin_amdgcn_sched_barrier(0);
     };
-    // the loads of the step after `cur`'s have landed in every wave, and
-    // every wave has read the last of `cur` (with four stages, one of the two
-    // steps that are still on their way brings scales)
-    auto turn = [&]() __attribute__((always_inline)) {
+    // the loads of the step after `cur`'s, the P-th, have landed in every wave,
+    // and every wave has read the last of `cur`; two more steps are on their
+    // way, one of which may bring scales
+    auto turn = [&](auto which) __attribute__((always_inline)) {
+        constexpr int P = decltype(which)::value;
         wait_lgkm0();
-        wait_vm<(STAGES - 2) * 2 * LOADS + (STAGES > 2)>();
+        wait_vm<2 * 2 * LOADS + (P == 1 || P == 2)>();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_s_barrier();
         asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
-    auto step = [&](auto parity, unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
-        constexpr int ODD = decltype(parity)::value;
-        constexpr std::integral_constant<int, 2 * ODD> S0;
-        constexpr std::integral_constant<int, PHASES == 1 ? 2 * ODD : 2 * ODD + 1> S1;
-        if constexpr (PHASES == 4) {
-            read_a(fa1, cur, h0, NA);
-            mul(S0, fa0, fb0, 0);
-            read_a(fa0, cur, h1, 0);
-            read_b(fb1, cur, h1);
-            mul(S0, fa1, fb0, NA);
-            read_a(fa1, cur, h1, NA);
-            mul(S1, fa0, fb1, 0);
-            turn();
-            issue(cur, !ODD);
-            read_a(fa0, next, h0, 0);
-            read_b(fb0, next, h0);
-            mul(S1, fa1, fb1, NA);
-        } else if constexpr (PHASES == 2) {
-            read_a(fa1, cur, h1, 0);
-            read_b(fb1, cur, h1);
-            mul(S0, fa0, fb0, 0);
-            turn();
-            issue(cur, !ODD);
-            read_a(fa0, next, h0, 0);
-            read_b(fb0, next, h0);
-            mul(S1, fa1, fb1, 0);
+    auto step = [&](auto which, unsigned char *cur, unsigned char *next) __attribute__((always_inline)) {
+        constexpr int P = decltype(which)::value;
+        i32x4(&b)[FN] = P & 1 ? fb1 : fb0, (&b_next)[FN] = P & 1 ? fb0 : fb1;
+        if constexpr (HALVES) {
+            read_a(fa1, cur, NA);
+            mul(which, fa0, b, 0);
+            turn(which);
+            issue(which, cur);
+            read_a(fa0, next, 0);
+            read_b(b_next, next);
+            mul(which, fa1, b, NA);
         } else {
-            turn();
-            issue(cur, !ODD);
-            if (ODD) {
-                read_a(fa0, next, h0, 0);
-                read_b(fb0, next, h0);
-                mul(S0, fa1, fb1, 0);
-            } else {
-                read_a(fa1, next, h0, 0);
-                read_b(fb1, next, h0);
-                mul(S0, fa0, fb0, 0);
-            }
+            i32x4(&f)[NA] = P & 1 ? fa1 : fa0, (&f_next)[NA] = P & 1 ? fa0 : fa1;
+            turn(which);
+            issue(which, cur);
+            read_a(f_next, next, 0);
+            read_b(b_next, next);
+            mul(which, f, b, 0);
         }
-        if (ODD) read_s(next);
+        if constexpr (P == 3) read_s();
     };
-    static_assert(STAGES % 2 == 0, "a turn of the ring is a turn of the scales");
-    unsigned char *const ring[4] = {st0, st1, st2, st3};
-#pragma unroll
-    for (int i = 0; i < STAGES; ++i) issue(ring[i], i % 2 == 0);
-    wait_vm<(STAGES - 1) * 2 * LOADS + (STAGES > 2)>();
+    constexpr std::integral_constant<int, 0> P0;
+    constexpr std::integral_constant<int, 1> P1;
+    constexpr std::integral_constant<int, 2> P2;
+    constexpr std::integral_constant<int, 3> P3;
+    issue(P0, st0);
+    issue(P1, st1);
+    issue(P2, st2);
+    issue(P3, st3);
+    wait_vm<3 * 2 * LOADS>();
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     asm volatile("" ::: "memory");
-    read_a(fa0, st0, h0, 0);
-    read_b(fb0, st0, h0);
-    read_s(st0);
-    int left = total;
-    constexpr std::integral_constant<int, 0> EVEN;
-    constexpr std::integral_constant<int, 1> ODD;
-    for (; left >= STAGES; left -= STAGES) {
-#pragma unroll
-        for (int i = 0; i < STAGES; i += 2) {
-            step(EVEN, ring[i], ring[i + 1]);
-            step(ODD, ring[i + 1], ring[(i + 2) % STAGES]);
-        }
-    }
-    if (left > 0) step(EVEN, ring[0], ring[1]);
-    if constexpr (STAGES > 2) {
-        if (left > 1) step(ODD, ring[1], ring[2]);
-        if (left > 2) step(EVEN, ring[2], ring[3]);
+    read_a(fa0, st0, 0);
+    read_b(fb0, st0);
+    read_s();
+    // (rows of codes are whole groups of four steps)
+    for (int left = total; left > 0; left -= STAGES) {
+        step(P0, st0, st1);
+        step(P1, st1, st2);
+        step(P2, st2, st3);
+        step(P3, st3, st0);
     }
     wait_vm<0>();
     __builtin_amdgcn_sched_barrier(0);
@@ -223,8 +194,9 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
     // that whole rows of contiguous columns are written. 16-byte chunk c of row
     // m sits at chunk c ^ swz(m).
     constexpr int RP = TM < 64 ? TM : 64, C = TN / 4, SZ = RP * TN * 4;
-    static_assert(NW * SZ <= 2 * CODES && CODES % SZ == 0, "staging");
-    unsigned char *const mine = wave * SZ < CODES ? st0 + wave * SZ : st1 + (wave * SZ - CODES);
+    static_assert(NW * SZ <= 4 * STAGE && STAGE % SZ == 0, "staging");
+    const int buffer = wave * SZ / STAGE;
+    unsigned char *const mine = (buffer == 0 ? st0 : buffer == 1 ? st1 : buffer == 2 ? st2 : st3) + wave * SZ % STAGE;
     auto swz = [](int m) __attribute__((always_inline)) { return ((m & 3) * 4 + (m >> 2)) & (C - 1); };
     const int nb = n0 + wn * TN, n = nb + (lane & (C - 1)) * 4;
     const f32x4 bias = mx_bias(a.splits == 1 && n < N ? a.bias : nullptr, n, N);
@@ -255,10 +227,10 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
     }
 }
 
-template <int T, int STAGES, int PHASES>
+template <int T>
 hipError_t go(const MxMm &a, hipStream_t s) {
     void *p[] = {const_cast<MxMm *>(&a)};
-    return hipLaunchKernel(reinterpret_cast<const void *>(&mx_mm_kernel<T, STAGES, PHASES>),
+    return hipLaunchKernel(reinterpret_cast<const void *>(&mx_mm_kernel<T>),
                            dim3((unsigned)mx_mm_tiles(a), (unsigned)a.splits), dim3(mx_threads_of(T)), p, 0, s);
 }
 
@@ -266,7 +238,7 @@ hipError_t go(const MxMm &a, hipStream_t s) {
 
 hipError_t launch_mx_mm(const MxMm &a, hipStream_t s) {
     if (!mx_mm_valid(a)) return hipErrorInvalidValue;
-    hipError_t e = a.tile == 256 ? go<256, 2, 4>(a, s) : a.tile == 128 ? go<128, 2, 2>(a, s) : go<64, 4, 1>(a, s);
+    hipError_t e = a.tile == 256 ? go<256>(a, s) : a.tile == 128 ? go<128>(a, s) : go<64>(a, s);
     if (e != hipSuccess || a.splits == 1) return e;
     return launch_mx_sum(MxSum{a.part, a.ldp, a.splits, a.x.rows, a.w.rows, a.bias, a.y, a.ldy, a.f32}, s);
 }

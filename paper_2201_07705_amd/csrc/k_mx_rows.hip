@@ -32,18 +32,16 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
     const uint8_t *codes = a.w.codes + n * pitch + g * 16, *scales = a.w.scales + n * 16ll + g * 4;
     f32x4 acc = {0.f, 0.f, 0.f, 0.f};
     for (int kg = wave; kg < groups; kg += a.waves) {
-        const int parts = min(4, (int)(pitch / 64) - kg * 4);   // of 128 columns that are there
         uint4 w[4];
 #pragma unroll
-        for (int s = 0; s < 4; ++s) w[s] = s < parts ? *(const uint4 *)(codes + kg * 256ll + s * 64) : uint4{0, 0, 0, 0};
+        for (int s = 0; s < 4; ++s) w[s] = *(const uint4 *)(codes + kg * 256ll + s * 64);
         const uint32_t sw = *(const uint32_t *)(scales + (int64_t)kg * N * 16);
         if constexpr (ACT == ACT_MX) {
             uint4 x[4];
             const uint8_t *xc = a.q.codes + m * pitch + kg * 256ll + g * 16;
 #pragma unroll
-            for (int s = 0; s < 4; ++s) x[s] = s < parts ? *(const uint4 *)(xc + s * 64) : uint4{0, 0, 0, 0};
+            for (int s = 0; s < 4; ++s) x[s] = *(const uint4 *)(xc + s * 64);
             const uint32_t sx = *(const uint32_t *)(a.q.scales + ((int64_t)kg * a.M + m) * 16 + g * 4);
-            // (of steps that are not there the scales are zeros, 2^-127)
             acc = mx_mul<0>(__builtin_bit_cast(i32x4, w[0]), __builtin_bit_cast(i32x4, x[0]), acc, (int)sw, (int)sx);
             acc = mx_mul<1>(__builtin_bit_cast(i32x4, w[1]), __builtin_bit_cast(i32x4, x[1]), acc, (int)sw, (int)sx);
             acc = mx_mul<2>(__builtin_bit_cast(i32x4, w[2]), __builtin_bit_cast(i32x4, x[2]), acc, (int)sw, (int)sx);
@@ -51,26 +49,35 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
         } else {
             constexpr int P = ACT == ACT_PLANES ? 3 : 1;
             const int c0 = kg * MX_GROUP + g * 32;
+            const u16 *row = a.x + m * a.ldx;
             auto mul = [&](int s, int i, const uint4 &x) __attribute__((always_inline)) {
                 acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(mx_bf16((&w[s].x)[i], mx_scale(sw >> s * 8 & 255)),
                                                               __builtin_bit_cast(mx_bf16x8, x), acc, 0, 0, 0);
             };
+            if ((kg + 1) * MX_GROUP <= K) {
+                // (what fits the registers of 16 waves is in flight at once)
+                constexpr int AT_ONCE = P == 1 ? 16 : 8;
+#pragma unroll
+                for (int i0 = 0; i0 < 16; i0 += AT_ONCE) {
+                    uint4 x[P][AT_ONCE];
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                        for (int p = 0; p < P; ++p)
+                            x[p][i] = get_16b(row + p * a.plane + c0 + ((i0 + i) >> 2) * 128 + ((i0 + i) & 3) * 8);
+#pragma unroll
+                    for (int i = 0; i < AT_ONCE; ++i)
+#pragma unroll
+                        for (int p = 0; p < P; ++p) mul((i0 + i) >> 2, (i0 + i) & 3, x[p][i]);
+                }
+            } else {
+#pragma unroll
+                for (int s = 0; s < 4; ++s) {
+                    if (kg * MX_GROUP + s * 128 >= K) break;
 #pragma unroll 1
-            for (int p = 0; p < P; ++p) {
-                const u16 *row = a.x + m * a.ldx + p * a.plane;
-                if ((kg + 1) * MX_GROUP <= K) {
-                    uint4 x[16];
+                    for (int p = 0; p < P; ++p)
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) x[i] = get_16b(row + c0 + (i >> 2) * 128 + (i & 3) * 8);
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) mul(i >> 2, i & 3, x[i]);
-                } else {
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) {
-                        if (s >= parts) break;
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) mul(s, i, mx_chunk(row, c0 + s * 128 + i * 8, K));
-                    }
+                        for (int i = 0; i < 4; ++i) mul(s, i, mx_chunk(row + p * a.plane, c0 + s * 128 + i * 8, K));
                 }
             }
         }
@@ -83,82 +90,90 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
         mx_put(a.y, a.ldy, a.f32, l16, n0 + 4 * g, N, acc + mx_bias(a.bias, n0 + 4 * g, N));
 }
 
-// 16 MB rows and 256 outputs to a workgroup of 8 waves, 32 outputs to a wave,
-// over a slice of the depth. Steps of 128 columns of the rows pass through
-// two buffers of LDS (16-byte chunk c of row r at chunk c ^ r % 16: the
-// fragment reads of 16 rows fall on distinct banks), the next step's rows and
-// codes being loaded while this one is multiplied.
-template <int P, int MB>
-__global__ __launch_bounds__(512) void mx_rows_kernel(const MxRows a) {
+// 16 MB rows and 128 NB outputs to a workgroup of 8 waves, 16 NB outputs to a
+// wave, over a slice of the depth. Steps of 128 columns of the rows pass
+// through two buffers of LDS (16-byte chunk c of row r at chunk c ^ r % 16:
+// the fragment reads of 16 rows fall on distinct banks); rows and codes are
+// loaded two steps ahead. A fragment of the rows serves NB products: with NB
+// = 2 LDS is as busy as the matrix cores.
+template <int P, int MB, int NB>
+__global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
     constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = (CHUNKS + 511) / 512;
     __shared__ uint4 st[2][CHUNKS];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int N = a.w.rows, K = a.w.cols, n0 = blockIdx.x * 256 + wave * 32, m0 = blockIdx.z * ROWS;
+    const int N = a.w.rows, K = a.w.cols, n0 = blockIdx.x * 128 * NB + wave * 16 * NB, m0 = blockIdx.z * ROWS;
     const int64_t pitch = mx_pitch(K);
-    const int step0 = (int)blockIdx.y * a.per * 4, steps = min((int)(pitch / 64) - step0, a.per * 4);
-    const uint8_t *codes[2], *scales[2];
+    const int step0 = (int)blockIdx.y * a.per, steps = min((K + 127) / 128 - step0, a.per);
+    uint32_t codes[NB], scales[NB];   // (offsets: up to 2^20 outputs of 2^12 bytes of a group)
+    const uint8_t *const code0 = a.w.codes + (int64_t)min(n0, N - 1) * pitch, *const scale0 = a.w.scales + (int64_t)min(n0, N - 1) * 16;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const int n = min(n0 + j * 16 + l16, N - 1);
-        codes[j] = a.w.codes + n * pitch + g * 16;
-        scales[j] = a.w.scales + n * 16ll + g * 4;
+    for (int j = 0; j < NB; ++j) {
+        const int n = min(n0 + j * 16 + l16, N - 1) - min(n0, N - 1);
+        codes[j] = (uint32_t)n * (uint32_t)pitch + g * 16;
+        scales[j] = n * 16 + g * 4;
     }
-    uint4 x[LOADS], w[2], w_next[2];
-    uint32_t sw[2] = {0, 0}, sw_next[2] = {0, 0};
-    auto load = [&](int step) __attribute__((always_inline)) {
+    struct Ahead {
+        uint4 x[LOADS], w[NB];
+        uint32_t s[NB];
+    } ahead[2];
+    auto load = [&](Ahead &q, int step) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int id = i * 512 + tid, p = id / (ROWS * 16), r = id / 16 % ROWS, c = step * 128 + (id & 15) * 8;
             if (CHUNKS % 512 == 0 || id < CHUNKS)
-                x[i] = mx_chunk(a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx, c, K);
+                q.x[i] = mx_chunk(a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx, c, K);
         }
+        const uint8_t *const wc = code0 + step * 64ll, *const ws = scale0 + (int64_t)(step >> 2) * N * 16;
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            w_next[j] = *(const uint4 *)(codes[j] + step * 64ll);
-            sw_next[j] = *(const uint32_t *)(scales[j] + (int64_t)(step >> 2) * N * 16);
+        for (int j = 0; j < NB; ++j) {
+            q.w[j] = *(const uint4 *)(wc + codes[j]);
+            q.s[j] = *(const uint32_t *)(ws + scales[j]);
         }
     };
-    auto store = [&](int buf) __attribute__((always_inline)) {
+    f32x4 acc[NB][MB];
+#pragma unroll
+    for (int j = 0; j < NB; ++j)
+#pragma unroll
+        for (int b = 0; b < MB; ++b) acc[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto turn = [&](Ahead &q, uint4 *buf, int k) __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) {
             const int id = i * 512 + tid, r = id / 16;
-            if (CHUNKS % 512 == 0 || id < CHUNKS) st[buf][r * 16 + ((id & 15) ^ (r & 15))] = x[i];
+            if (CHUNKS % 512 == 0 || id < CHUNKS) buf[r * 16 + ((id & 15) ^ (r & 15))] = q.x[i];
         }
+        uint4 w[NB];
+        float scale[NB];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
-            w[j] = w_next[j];
-            sw[j] = sw_next[j];
+        for (int j = 0; j < NB; ++j) {
+            w[j] = q.w[j];
+            scale[j] = mx_scale(q.s[j] >> ((step0 + k) & 3) * 8 & 255);
         }
-    };
-    f32x4 acc[2][MB];
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-        for (int b = 0; b < MB; ++b) acc[j][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-    load(step0);
-    for (int k = 0; k < steps; ++k) {
-        store(k & 1);
         __syncthreads();
-        if (k + 1 < steps) load(step0 + k + 1);
-        const int s = (k & 3) * 8;   // (slices begin at whole groups)
+        if (k + 2 < steps) load(q, step0 + k + 2);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            mx_bf16x8 f[2];
+            mx_bf16x8 f[NB];
 #pragma unroll
-            for (int j = 0; j < 2; ++j) f[j] = mx_bf16((&w[j].x)[i], mx_scale(sw[j] >> s & 255));
+            for (int j = 0; j < NB; ++j) f[j] = mx_bf16((&w[j].x)[i], scale[j]);
 #pragma unroll
             for (int p = 0; p < P; ++p)
 #pragma unroll
                 for (int b = 0; b < MB; ++b) {
-                    const mx_bf16x8 v = __builtin_bit_cast(mx_bf16x8, st[k & 1][(p * ROWS + b * 16 + l16) * 16 + ((4 * g + i) ^ l16)]);
+                    const mx_bf16x8 v = __builtin_bit_cast(mx_bf16x8, buf[(p * ROWS + b * 16 + l16) * 16 + ((4 * g + i) ^ l16)]);
 #pragma unroll
-                    for (int j = 0; j < 2; ++j) acc[j][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j], v, acc[j][b], 0, 0, 0);
+                    for (int j = 0; j < NB; ++j) acc[j][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f[j], v, acc[j][b], 0, 0, 0);
                 }
         }
+    };
+    load(ahead[0], step0);
+    if (steps > 1) load(ahead[1], step0 + 1);
+    for (int k = 0; k < steps; k += 2) {
+        turn(ahead[0], st[0], k);
+        if (k + 1 < steps) turn(ahead[1], st[1], k + 1);
     }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
+    for (int j = 0; j < NB; ++j) {
         const int n = n0 + j * 16 + 4 * g;
         if (n >= N) continue;
         const f32x4 bias = mx_bias(a.slices == 1 ? a.bias : nullptr, n, N);
@@ -179,12 +194,12 @@ hipError_t go(K kernel, const MxRows &a, dim3 grid, int threads, hipStream_t s) 
     void *p[] = {const_cast<MxRows *>(&a)};
     return hipLaunchKernel(reinterpret_cast<const void *>(kernel), grid, dim3((unsigned)threads), p, 0, s);
 }
-template <int P>
+template <int P, int NB>
 hipError_t many(const MxRows &a, hipStream_t s) {
-    const int mb = a.M <= 32 ? 2 : a.M <= 48 ? 3 : 4;
-    const dim3 grid((unsigned)((a.w.rows + 255) / 256), (unsigned)a.slices, (unsigned)((a.M + mb * 16 - 1) / (mb * 16)));
-    return mb == 2 ? go(&mx_rows_kernel<P, 2>, a, grid, 512, s) : mb == 3 ? go(&mx_rows_kernel<P, 3>, a, grid, 512, s)
-                                                                          : go(&mx_rows_kernel<P, 4>, a, grid, 512, s);
+    const int mb = mx_row_blocks(a.M);
+    const dim3 grid((unsigned)((a.w.rows + 128 * NB - 1) / (128 * NB)), (unsigned)a.slices, (unsigned)((a.M + mb * 16 - 1) / (mb * 16)));
+    return mb == 2 ? go(&mx_rows_kernel<P, 2, NB>, a, grid, 512, s) : mb == 3 ? go(&mx_rows_kernel<P, 3, NB>, a, grid, 512, s)
+                                                                              : go(&mx_rows_kernel<P, 4, P == 3 ? 2 : NB>, a, grid, 512, s);
 }
 
 }  // namespace
@@ -197,7 +212,7 @@ hipError_t launch_mx_rows(const MxRows &a, hipStream_t s) {
                : a.planes > 1 ? go(&mx_few_kernel<ACT_PLANES>, a, grid, a.waves * 64, s)
                               : go(&mx_few_kernel<ACT_BF16>, a, grid, a.waves * 64, s);
     }
-    hipError_t e = a.planes > 1 ? many<3>(a, s) : many<1>(a, s);
+    hipError_t e = a.planes > 1 ? (a.wide ? many<3, 4>(a, s) : many<3, 2>(a, s)) : (a.wide ? many<1, 4>(a, s) : many<1, 2>(a, s));
     if (e != hipSuccess || a.slices == 1) return e;
     return launch_mx_sum(MxSum{a.part, a.ldp, a.slices, a.M, a.w.rows, a.bias, a.y, a.ldy, a.f32}, s);
 }

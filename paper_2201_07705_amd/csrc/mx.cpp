@@ -51,7 +51,7 @@ gemel_status few_rows(Call &c, const Wide &p) {
     a.w = p.w;
     a.x = (const u16 *)p.x;
     a.ldx = p.ldx;
-    a.planes = 1;
+    a.planes = p.f32 ? 3 : 1;
     a.M = p.M;
     mx_rows_plan(a);
     const int64_t ld = op_round_up(p.w.cols, 8);
@@ -65,7 +65,6 @@ gemel_status few_rows(Call &c, const Wide &p) {
         a.x = split.out;
         a.ldx = ld;
         a.plane = p.M * ld;
-        a.planes = 3;
     }
     a.bias = p.bias;
     a.y = p.y;
@@ -156,6 +155,7 @@ gemel_status both_quantized(Call &c, const Mx &x, const Mx &w, const float *bias
         MxRows a{};
         a.w = w;
         a.q = x;
+        a.planes = 1;
         a.M = x.rows;
         mx_rows_plan(a);
         a.bias = bias;

@@ -11,19 +11,19 @@ namespace gemel {
 typedef unsigned short u16;
 
 // Rows of 4-bit codes, two to a byte, and a scale byte for each block of 32
-// columns. Rows of codes are padded with zeros to 256 columns (128 bytes, what
-// a step of a product reads). Scales lie in groups of 512 columns, 16 bytes
-// for each row of the matrix: byte 4 g + s belongs to the block g of the
+// columns, in groups of 512 columns. Rows of codes are padded with zeros to
+// whole groups (256 bytes, four steps of a product). Scales lie group by
+// group, 16 bytes for each row of the matrix: byte 4 g + s belongs to the block g of the
 // group's s-th 128 columns, so that a lane of a product (which holds the
 // block g of every step) finds its scales of four steps in one word.
-constexpr int MX_BLOCK = 32, MX_STEP = 256, MX_GROUP = 512;
+constexpr int MX_BLOCK = 32, MX_GROUP = 512;
 struct Mx {
     uint8_t *codes;
     uint8_t *scales;
     int rows, cols;
 };
-constexpr int64_t mx_pitch(int64_t cols) { return (cols + MX_STEP - 1) / MX_STEP * (MX_STEP / 2); }
 constexpr int64_t mx_groups(int64_t cols) { return (cols + MX_GROUP - 1) / MX_GROUP; }
+constexpr int64_t mx_pitch(int64_t cols) { return mx_groups(cols) * (MX_GROUP / 2); }
 constexpr int64_t MX_MAX_COLS = 1 << 20;
 
 struct MxCast {
@@ -72,9 +72,10 @@ struct MxRows {
     int planes;           // 1 or 3
     Mx q;                 // instead of x: quantised rows (up to MX_FEW)
     int M;
-    // mx_rows_plan: waves of a workgroup; groups of 512 columns in a slice,
-    // and slices
-    int waves, per, slices;
+    // mx_rows_plan: up to MX_FEW rows, waves of a workgroup; else steps of 128
+    // columns in a slice, slices, and whether a workgroup takes 512 outputs
+    // instead of 256
+    int waves, per, slices, wide;
     const float *bias;
     void *y;
     int64_t ldy;
@@ -82,6 +83,7 @@ struct MxRows {
     float *part;          // slices > 1: [slices][M][ldp]
     int64_t ldp;
 };
+constexpr int mx_row_blocks(int M) { return M <= 32 ? 2 : M <= 48 ? 3 : 4; }   // 16 rows each, of a workgroup
 void mx_rows_plan(MxRows &a);
 bool mx_rows_valid(const MxRows &a);
 hipError_t launch_mx_rows(const MxRows &a, hipStream_t s);

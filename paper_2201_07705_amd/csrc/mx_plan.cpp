@@ -32,32 +32,35 @@ bool mx_sum_valid(const MxSum &a) {
 }
 
 // Up to MX_FEW rows: 16 outputs to a workgroup, whose waves (at most 16) have
-// a group of 512 columns or more each; no slices. Beyond: 256 outputs and 64
-// rows to a workgroup, slices until the card is full.
+// a group of 512 columns or more each; no slices. Beyond: slices until the
+// card is full, of at least 4 steps; 512 outputs to a workgroup where that
+// leaves enough of them.
 void mx_rows_plan(MxRows &a) {
-    const int groups = (int)mx_groups(a.w.cols);
     a.ldp = op_round_up(a.w.rows, 4);
+    a.per = a.slices = 1;
     if (a.M <= MX_FEW) {
-        a.waves = std::min(groups, 16);
-        a.per = (groups + a.waves - 1) / a.waves;   // (of a wave)
-        a.slices = 1;
+        a.waves = (int)std::min<int64_t>(mx_groups(a.w.cols), 16);
         return;
     }
     a.waves = 8;
-    const int64_t tiles = (int64_t)((a.w.rows + 255) / 256) * ((a.M + 63) / 64);
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(groups, 256 / tiles));
-    a.per = (groups + want - 1) / want;
-    a.slices = (groups + a.per - 1) / a.per;
+    const int steps = (a.w.cols + 127) / 128, rows = 16 * mx_row_blocks(a.M);
+    const int64_t down = (a.M + rows - 1) / rows;
+    a.wide = !(a.planes == 3 && rows == 64) && (a.w.rows + 511) / 512 * down * (steps / 4) >= 256;
+    const int n = a.wide ? 512 : 256;
+    const int64_t tiles = (a.w.rows + n - 1) / n * down;
+    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(steps / 4, 256 / tiles));
+    a.per = (steps + want - 1) / want;
+    a.slices = (steps + a.per - 1) / a.per;
 }
 
 bool mx_rows_valid(const MxRows &a) {
-    const int groups = (int)mx_groups(a.w.cols);
-    if (!mx_there(a.w) || a.M < 1 || !a.y || a.ldy < a.w.rows || a.per < 1 || a.slices < 1) return false;
+    const int steps = (a.w.cols + 127) / 128;
+    if (!mx_there(a.w) || a.M < 1 || !a.y || a.ldy < a.w.rows) return false;
     if (a.M <= MX_FEW) {
-        if (a.waves < 1 || a.waves > 16 || a.waves * a.per < groups || a.slices != 1) return false;
+        if (a.waves < 1 || a.waves > 16) return false;
     } else {
-        if (a.waves != 8 || a.slices * a.per < groups || (a.slices - 1) * a.per >= groups || a.slices > 65535 || a.q.codes ||
-            (a.M + 63) / 64 > 65535)
+        if (a.waves != 8 || a.slices < 1 || a.per < 1 || (int64_t)a.slices * a.per < steps || (int64_t)(a.slices - 1) * a.per >= steps ||
+            a.slices > 65535 || a.q.codes || a.M > 65535 * 16)
             return false;
         if (a.slices > 1 && (!a.part || a.ldp < a.w.rows || a.ldp % 4)) return false;
     }

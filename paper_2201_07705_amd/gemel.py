@@ -367,8 +367,8 @@ class AdapterBatch:
 
 class MxMatrix:
     """A matrix [rows, cols] in microscaled 4-bit floating point, as
-    Context.mx_quantize makes it: codes [rows, P] and scales [groups, rows,
-    16], both uint8 (include/gemel.h says which byte is which)."""
+    Context.mx_quantize makes it: codes [rows, 256 groups] and scales [groups,
+    rows, 16], both uint8 (include/gemel.h says which byte is which)."""
 
     def __init__(self, codes, scales, rows, cols):
         self.codes, self.scales = codes, scales
@@ -377,7 +377,8 @@ class MxMatrix:
     @staticmethod
     def shapes(rows, cols):
         """Shapes of codes and scales."""
-        return (rows, 128 * -(-cols // 256)), (-(-cols // 512), rows, 16)
+        groups = -(-cols // 512)
+        return (rows, 256 * groups), (groups, rows, 16)
 
     @property
     def nbytes(self):
