@@ -373,6 +373,7 @@ class MxMatrix:
     def __init__(self, codes, scales, rows, cols):
         self.codes, self.scales = codes, scales
         self.rows, self.cols = rows, cols
+        self._c = None   # the C description, once it was checked
 
     @staticmethod
     def shapes(rows, cols):
@@ -823,14 +824,20 @@ class Context:
             kinds.update(top_indices=((rows, top), i32),
                          top_log_probs=((rows, top), f32))
         res, a = {}, Answers()
+        if needs is None and not outputs:
+            # the numbers of a row are made together, as rows of one tensor
+            # (three tensors of their own take 2 us more)
+            flat = [name for name in kinds if kinds[name] == ((rows,), f32)]
+            made = self._empty(logits, (len(flat), rows), f32, stream)
+            res.update(zip(flat, made.unbind(0)))
         for name in kinds if needs is None else needs:
             if name not in kinds:
                 raise ValueError(f"no answer {name!r} (of these arguments)")
             shape, dt = kinds[name]
-            t = outputs.get(name) if outputs else None
+            t = outputs.get(name) if outputs else res.get(name)
             if t is None:
                 t = self._empty(logits, shape, dt, stream)
-            else:
+            elif outputs:
                 self._tensor(f"outputs[{name!r}]", t, shape, dt)
             res[name] = t
             setattr(a, name, t.data_ptr())
@@ -902,16 +909,22 @@ class Context:
 
     # -- merged layers in 4 bits --
     def _mx(self, name, q):
-        """The C description of a quantised matrix, checked."""
+        """The C description of a quantised matrix, checked (again where
+        anything in it is another one than the last time)."""
         if not isinstance(q, MxMatrix):
             raise ValueError(f"{name} must be an MxMatrix")
+        c, at = q._c, (self.device, q.rows, q.cols, q.codes.data_ptr(),
+                       q.scales.data_ptr())
+        if c is not None and c[0] == at:
+            return c[1]
         _int32(name + " rows", q.rows)
         _int32(name + " cols", q.cols)
         u8 = _torch().uint8
         codes, scales = MxMatrix.shapes(q.rows, q.cols)
         self._tensor(name + ".codes", q.codes, codes, u8)
         self._tensor(name + ".scales", q.scales, scales, u8)
-        return Mx(q.rows, q.cols, q.codes.data_ptr(), q.scales.data_ptr())
+        q._c = at, Mx(*at[1:])
+        return q._c[1]
 
     @staticmethod
     def _value_type(name, dtype):
@@ -938,6 +951,9 @@ class Context:
             codes, scales = MxMatrix.shapes(rows, cols)
             q = MxMatrix(self._empty(x, codes, u8, stream),
                          self._empty(x, scales, u8, stream), rows, cols)
+            at = (self.device, rows, cols, q.codes.data_ptr(),
+                  q.scales.data_ptr())
+            q._c = at, Mx(*at[1:])
         elif (q.rows, q.cols) != (rows, cols):
             raise ValueError(f"out is [{q.rows}, {q.cols}], x [{rows}, {cols}]")
         self._check(self._lib.gemel_mx_quantize(
