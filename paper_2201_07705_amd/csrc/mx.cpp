@@ -11,7 +11,7 @@ using namespace gemel::op;
 namespace {
 
 constexpr int64_t MAX_ROWS = 1 << 22;
-constexpr int64_t PIECE = 1ll << 28;   // floats of partial sums of float32 rows that a pass takes
+constexpr int64_t PIECE = 1ll << 27;   // values of float32 rows whose planes (6 bytes each) a pass holds, about
 
 gemel_status check_mx(gemel_ctx *ctx, const char *what, const gemel_mx *q, Mx *out) {
     if (!q) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is null");
@@ -44,63 +44,62 @@ struct Wide {
     bool f32;
 };
 
-// Up to MX_ROWS rows: the weights are expanded in registers.
-gemel_status few_rows(Call &c, const Wide &p) {
+// float32 rows, and up to MX_ROWS bf16 ones: the weights are expanded in
+// registers. Planes of float32 rows are made for a piece of the rows at a
+// time, which bounds the workspace.
+gemel_status in_registers(Call &c, const Wide &p) {
     gemel_ctx *ctx = c.ctx;
-    MxRows a{};
-    a.w = p.w;
-    a.x = (const u16 *)p.x;
-    a.ldx = p.ldx;
-    a.planes = p.f32 ? 3 : 1;
-    a.M = p.M;
-    mx_rows_plan(a);
     const int64_t ld = op_round_up(p.w.cols, 8);
-    const size_t o_x = c.lay.take(p.f32 ? 3 * p.M * ld : 0, 2),
-                 o_part = c.lay.take(a.slices > 1 ? (int64_t)a.slices * p.M * a.ldp : 0, 4);
+    const int each = p.f32 ? (int)std::min<int64_t>(p.M, std::max<int64_t>(1024, PIECE / ld / 64 * 64)) : p.M;
+    auto plan = [&](int rows) {
+        MxRows a{};
+        a.w = p.w;
+        a.planes = p.f32 ? 3 : 1;
+        a.M = rows;
+        mx_rows_plan(a);
+        return a;
+    };
+    const MxRows whole = plan(each), last = p.M % each ? plan(p.M % each) : whole;
+    auto partial = [](const MxRows &a) { return a.slices > 1 ? (int64_t)a.slices * a.M * a.ldp : 0; };
+    const size_t o_x = c.lay.take(p.f32 ? 3 * each * ld : 0, 2), o_part = c.lay.take(std::max(partial(whole), partial(last)), 4);
     if (c.lay.bytes)
         if (gemel_status s = workspace(c)) return s;
-    if (p.f32) {
-        const MxPlanes split{(const float *)p.x, p.ldx, c.at<u16>(o_x), ld, p.M, p.w.cols};
-        OPCHK(launch_mx_planes(split, c.stream), "planes");
-        a.x = split.out;
-        a.ldx = ld;
-        a.plane = p.M * ld;
+    for (int r = 0; r < p.M; r += each) {
+        MxRows a = p.M - r < each ? last : whole;
+        a.x = (const u16 *)p.x;
+        a.ldx = p.ldx;
+        if (p.f32) {
+            const MxPlanes split{(const float *)p.x + r * p.ldx, p.ldx, c.at<u16>(o_x), ld, a.M, p.w.cols};
+            OPCHK(launch_mx_planes(split, c.stream), "planes");
+            a.x = split.out;
+            a.ldx = ld;
+            a.plane = a.M * ld;
+        }
+        a.bias = p.bias;
+        a.y = p.y + (int64_t)r * p.ldy * (p.f32 ? 4 : 2);
+        a.ldy = p.ldy;
+        a.f32 = p.f32;
+        a.part = c.at<float>(o_part);
+        OPCHK(launch_mx_rows(a, c.stream), "product");
     }
-    a.bias = p.bias;
-    a.y = p.y;
-    a.ldy = p.ldy;
-    a.f32 = p.f32;
-    a.part = c.at<float>(o_part);
-    OPCHK(launch_mx_rows(a, c.stream), "product");
     return GEMEL_OK;
 }
 
-// More rows: the weights are expanded to bf16 once and go through the bf16
-// product. float32 rows go as three bf16 planes below each other, whose
-// results are then added up, in pieces that bound the workspace.
-gemel_status many_rows(Call &c, const Wide &p) {
+// More bf16 rows: the weights are expanded to bf16 once and go through the
+// bf16 product.
+gemel_status expanded(Call &c, const Wide &p) {
     gemel_ctx *ctx = c.ctx;
-    const int64_t Kp = op_round_up(p.w.cols, 8), ldp = op_round_up(p.w.rows, 4);
-    const int each = p.f32 ? (int)std::min<int64_t>(p.M, std::max<int64_t>(MX_ROWS, PIECE / (3 * ldp))) : p.M;
-    const bool copy = !p.f32 && !in_place(p.x, p.M, p.ldx, p.w.cols);
+    const int64_t Kp = op_round_up(p.w.cols, 8);
+    const bool copy = !in_place(p.x, p.M, p.ldx, p.w.cols);
     MmArgs m{};
-    m.M = p.f32 ? 3 * each : p.M;
+    m.M = p.M;
     m.N = p.w.rows;
     m.K = (int)Kp;
     m.batch = 1;
     m.epi = EPI_ROWS;
     mm_plan(m);
-    int64_t partial = partial_floats(m);
-    const int rest = p.f32 ? p.M % each : 0;
-    MmArgs last = m;
-    if (rest) {
-        last.M = 3 * rest;
-        mm_plan(last);
-        partial = std::max(partial, partial_floats(last));
-    }
-    if (!mm_fits(m) || (rest && !mm_fits(last))) return fail(ctx, GEMEL_EINVAL, "the product is too large");
-    const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(p.f32 ? 3 * each * Kp : copy ? p.M * Kp : 0, 2),
-                 o_y = c.lay.take(p.f32 ? 3 * each * ldp : 0, 4), o_part = c.lay.take(partial, 4);
+    if (!mm_fits(m)) return fail(ctx, GEMEL_EINVAL, "the product is too large");
+    const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(copy ? p.M * Kp : 0, 2), o_part = c.lay.take(partial_floats(m), 4);
     if (gemel_status s = workspace(c)) return s;
     MxCast cast{};
     cast.q = p.w;
@@ -108,44 +107,31 @@ gemel_status many_rows(Call &c, const Wide &p) {
     cast.ld = Kp;
     cast.out_cols = (int)Kp;
     OPCHK(launch_mx_values(cast, c.stream), "weights");
-    for (int r = 0; r < p.M; r += each) {
-        MmArgs &a = p.M - r < each ? last : m;
-        const int rows = std::min(each, p.M - r);
-        a.a = (const u16 *)p.x;
-        a.lda = p.ldx;
-        if (p.f32) {
-            const MxPlanes split{(const float *)p.x + r * p.ldx, p.ldx, c.at<u16>(o_x), Kp, rows, p.w.cols};
-            OPCHK(launch_mx_planes(split, c.stream), "planes");
-        } else if (copy) {
-            Jobs jobs;
-            Job j{};
-            j.kind = JOB_PAD;
-            j.in = p.x;
-            j.ldi = p.ldx;
-            j.rows = p.M;
-            j.cols = p.w.cols;
-            j.out = c.at<u16>(o_x);
-            j.ldo = Kp;
-            if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
-            OPCHK(launch_jobs(jobs, c.stream), "copies");
-        }
-        if (p.f32 || copy) {
-            a.a = c.at<u16>(o_x);
-            a.lda = Kp;
-        }
-        a.b = (const u16 *)cast.out;
-        a.ldb = Kp;
-        a.zero = (const u16 *)c.st->zero;
-        a.partial = c.at<float>(o_part);
-        a.o.out = p.f32 ? c.at<void>(o_y) : p.y;
-        a.o.ld = p.f32 ? ldp : p.ldy;
-        a.o.out_f32 = p.f32;
-        a.o.bias = p.f32 ? nullptr : p.bias;
-        OPCHK(launch_mm(a, c.stream), "product");
-        if (p.f32)
-            OPCHK(launch_mx_sum(MxSum{c.at<float>(o_y), ldp, 3, rows, p.w.rows, p.bias, p.y + (int64_t)r * p.ldy * 4, p.ldy, 1}, c.stream),
-                  "sum of planes");
+    m.a = (const u16 *)p.x;
+    m.lda = p.ldx;
+    if (copy) {
+        Jobs jobs;
+        Job j{};
+        j.kind = JOB_PAD;
+        j.in = p.x;
+        j.ldi = p.ldx;
+        j.rows = p.M;
+        j.cols = p.w.cols;
+        j.out = c.at<u16>(o_x);
+        j.ldo = Kp;
+        if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
+        OPCHK(launch_jobs(jobs, c.stream), "copies");
+        m.a = c.at<u16>(o_x);
+        m.lda = Kp;
     }
+    m.b = (const u16 *)cast.out;
+    m.ldb = Kp;
+    m.zero = (const u16 *)c.st->zero;
+    m.partial = c.at<float>(o_part);
+    m.o.out = p.y;
+    m.o.ld = p.ldy;
+    m.o.bias = p.bias;
+    OPCHK(launch_mm(m, c.stream), "product");
     return GEMEL_OK;
 }
 
@@ -266,7 +252,7 @@ gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x, int64
         Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
         if (xq) return both_quantized(c, q, w, bias, y, y_stride, f32);
         const Wide p{x, x_stride, rows, w, bias, (char *)y, y_stride, f32};
-        return rows <= MX_ROWS ? few_rows(c, p) : many_rows(c, p);
+        return f32 || rows <= MX_ROWS ? in_registers(c, p) : expanded(c, p);
     });
 }
 

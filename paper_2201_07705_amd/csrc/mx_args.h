@@ -64,7 +64,7 @@ hipError_t launch_mx_sum(const MxSum &a, hipStream_t s);
 // Rows that are not quantised against 4-bit weights w: bf16 rows, or three
 // planes of float32 ones. Up to MX_FEW rows the waves of a workgroup split
 // the depth; beyond that they split the outputs and share the rows in LDS.
-constexpr int MX_FEW = 16, MX_ROWS = 256;
+constexpr int MX_FEW = 16, MX_ROWS = 1024;   // MX_ROWS: of bf16; float32 rows always
 struct MxRows {
     Mx w;
     const u16 *x;
@@ -83,7 +83,11 @@ struct MxRows {
     float *part;          // slices > 1: [slices][M][ldp]
     int64_t ldp;
 };
-constexpr int mx_row_blocks(int M) { return M <= 32 ? 2 : M <= 48 ? 3 : 4; }   // 16 rows each, of a workgroup
+// 16 rows each, of a workgroup: as few as hold all rows, or 4 (3 where that
+// pads a tenth less)
+constexpr int mx_row_blocks(int M) {
+    return M <= 32 ? 2 : M <= 48 ? 3 : M <= 64 || 10 * ((M + 47) / 48 * 48) > 9 * ((M + 63) / 64 * 64) ? 4 : 3;
+}
 void mx_rows_plan(MxRows &a);
 bool mx_rows_valid(const MxRows &a);
 hipError_t launch_mx_rows(const MxRows &a, hipStream_t s);

@@ -125,16 +125,18 @@ def test_every_path_of_products(lib):
     f = dict(p, dtype="f32")
     q = dict(p, acts="mx")
     calls = [dict(p, rows=16), dict(f, rows=16), dict(q, rows=16), dict(p, rows=17), dict(f, rows=17), dict(q, rows=17),
-             dict(p, rows=256), dict(p, rows=257), dict(p, rows=257, k=1001), dict(f, rows=257), dict(q, rows=5000, n=4096),
+             dict(p, rows=1024), dict(p, rows=1025), dict(p, rows=1025, k=1001), dict(f, rows=1025), dict(q, rows=5000, n=4096),
              dict(p, rows=17, k=100), dict(q, rows=17, k=100)]
-    want = ["few", "planes few", "few", "rows", "planes rows", "mm", "rows", "values", "values", "values planes sum", "mm", "rows", "mm"]
+    want = ["few", "planes few", "few", "rows", "planes rows", "mm", "rows", "values", "values", "planes rows", "mm", "rows", "mm"]
     assert sound(lib, calls) == want
 
 
 def test_float32_rows_beyond_one_piece(lib):
-    """2^28 floats of partial sums bound a pass: pieces, the last one shorter."""
-    c = {"op": "product", "dtype": "f32", "acts": "float", "rows": 700, "k": 8, "n": 300000, "bias": 0}
-    assert sound(lib, [c]) == ["values planes sum planes sum planes sum"]
+    """2^27 values whose planes are held bound a pass: pieces, the last one
+    shorter, of few rows or the only one."""
+    c = {"op": "product", "dtype": "f32", "acts": "float", "k": 200000, "n": 10, "bias": 0}
+    want = {1024: "planes rows", 1025: "planes rows planes few", 2100: "planes rows planes rows planes rows"}
+    assert sound(lib, [dict(c, rows=r) for r in want]) == list(want.values())
 
 
 def test_the_check_itself(lib):

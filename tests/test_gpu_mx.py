@@ -219,7 +219,8 @@ def test_products(ctxs, k, n, dtype, acts):
 @pytest.mark.parametrize("acts", ["float", "mx"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("m,k,n", [(1, 25088, 4096), (37, 25088, 4096), (1000, 4096, 1000), (5000, 1024, 2100), (2500, 264, 4096),
-                                   (4500, 1000, 4000), (20000, 40, 33)])
+                                   (4500, 1000, 4000), (20000, 40, 33), (1024, 1000, 300),
+                                   (1025, 1001, 300), (1030, 140000, 20)])
 def test_large_products(ctxs, m, k, n, dtype, acts):
     ctx = ctxs[dtype]
     x, w, bias = product(dtype, acts, m, k, n)
