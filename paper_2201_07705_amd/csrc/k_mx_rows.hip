@@ -94,11 +94,12 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
 // wave, over a slice of the depth. Steps of 128 columns of the rows pass
 // through two buffers of LDS (16-byte chunk c of row r at chunk c ^ r % 16:
 // the fragment reads of 16 rows fall on distinct banks); rows and codes are
-// loaded two steps ahead. A fragment of the rows serves NB products: with NB
+// loaded one or two steps ahead. A fragment of the rows serves NB products: with NB
 // = 2 LDS is as busy as the matrix cores.
 template <int P, int MB, int NB>
 __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
     constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = (CHUNKS + 511) / 512;
+    constexpr int AHEAD = P == 3 && NB == 4 ? 1 : 2;   // steps (registers)
     __shared__ uint4 st[2][CHUNKS];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -116,13 +117,25 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
     struct Ahead {
         uint4 x[LOADS], w[NB];
         uint32_t s[NB];
-    } ahead[2];
-    auto load = [&](Ahead &q, int step) __attribute__((always_inline)) {
+    } ahead[AHEAD];
+    // (rows of x as the thread's chunks lie in them; no branch stands between
+    // the loads of a whole step)
+    const u16 *rows[LOADS];
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) {
-            const int id = i * 512 + tid, p = id / (ROWS * 16), r = id / 16 % ROWS, c = step * 128 + (id & 15) * 8;
-            if (CHUNKS % 512 == 0 || id < CHUNKS)
-                q.x[i] = mx_chunk(a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx, c, K);
+    for (int i = 0; i < LOADS; ++i) {
+        const int id = min(i * 512 + tid, CHUNKS - 1), p = id / (ROWS * 16), r = id / 16 % ROWS;
+        rows[i] = a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx + (id & 15) * 8;
+    }
+    auto load = [&](Ahead &q, int step) __attribute__((always_inline)) {
+        if ((step + 1) * 128 <= K) {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) q.x[i] = get_16b(rows[i] + step * 128);
+        } else {
+#pragma unroll
+            for (int i = 0; i < LOADS; ++i) {
+                const int c = (tid & 15) * 8;
+                q.x[i] = mx_chunk(rows[i] - c, step * 128 + c, K);
+            }
         }
         const uint8_t *const wc = code0 + step * 64ll, *const ws = scale0 + (int64_t)(step >> 2) * N * 16;
 #pragma unroll
@@ -150,7 +163,7 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
             scale[j] = mx_scale(q.s[j] >> ((step0 + k) & 3) * 8 & 255);
         }
         __syncthreads();
-        if (k + 2 < steps) load(q, step0 + k + 2);
+        if (k + AHEAD < steps) load(q, step0 + k + AHEAD);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             mx_bf16x8 f[NB];
@@ -167,10 +180,10 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
         }
     };
     load(ahead[0], step0);
-    if (steps > 1) load(ahead[1], step0 + 1);
+    if (AHEAD > 1 && steps > 1) load(ahead[AHEAD - 1], step0 + 1);
     for (int k = 0; k < steps; k += 2) {
         turn(ahead[0], st[0], k);
-        if (k + 1 < steps) turn(ahead[1], st[1], k + 1);
+        if (k + 1 < steps) turn(ahead[AHEAD - 1], st[1], k + 1);
     }
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -199,7 +212,7 @@ hipError_t many(const MxRows &a, hipStream_t s) {
     const int mb = mx_row_blocks(a.M);
     const dim3 grid((unsigned)((a.w.rows + 128 * NB - 1) / (128 * NB)), (unsigned)a.slices, (unsigned)((a.M + mb * 16 - 1) / (mb * 16)));
     return mb == 2 ? go(&mx_rows_kernel<P, 2, NB>, a, grid, 512, s) : mb == 3 ? go(&mx_rows_kernel<P, 3, NB>, a, grid, 512, s)
-                                                                              : go(&mx_rows_kernel<P, 4, P == 3 ? 2 : NB>, a, grid, 512, s);
+                                                                              : go(&mx_rows_kernel<P, 4, NB>, a, grid, 512, s);
 }
 
 }  // namespace

@@ -45,7 +45,7 @@ void mx_rows_plan(MxRows &a) {
     a.waves = 8;
     const int steps = (a.w.cols + 127) / 128, rows = 16 * mx_row_blocks(a.M);
     const int64_t down = (a.M + rows - 1) / rows;
-    a.wide = !(a.planes == 3 && rows == 64) && (a.w.rows + 511) / 512 * down * (steps / 4) >= 256;
+    a.wide = (a.w.rows + 511) / 512 * down * (steps / 4) >= 256;
     const int n = a.wide ? 512 : 256;
     const int64_t tiles = (a.w.rows + n - 1) / n * down;
     const int want = (int)std::max<int64_t>(1, std::min<int64_t>(steps / 4, 256 / tiles));
