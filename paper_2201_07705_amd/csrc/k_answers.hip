@@ -557,10 +557,12 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_
 }
 
 // One row for each workgroup: the sums of its chunks, and the best of their
-// lists. Lists are sorted, so a class's place is what binary searches in the
-// others say.
+// lists.
+constexpr int KEPT = 512;
+template <int N>   // entries of the lists
 __global__ __launch_bounds__(256) void score_join_kernel(const ScoreArgs a) {
-    __shared__ u64 keys[ANSWER_MAX_CHUNKS * TOP_MAX];
+    __shared__ u64 keys[N], kept[KEPT];
+    __shared__ int left;
     const int row = blockIdx.x, tid = threadIdx.x, chunks = a.l.chunks, n = chunks * a.top;
     const int64_t at = (int64_t)row * chunks;
     const Part p = chunks_part(a.part + at, chunks, a.l.c);
@@ -570,36 +572,61 @@ __global__ __launch_bounds__(256) void score_join_kernel(const ScoreArgs a) {
         const char *z = (const char *)a.l.z + (int64_t)row * a.l.ld * (a.l.f32 ? 4 : 2);
         put_row(a, row, p, label, label >= 0 && label < a.l.classes ? logit(a.l, z, label) : 0.f);
     }
+    if (tid == 0) left = 0;
     for (int i = tid; i < n; i += 256) keys[i] = key_of(a.list_value[at * a.top + i], a.list_index[at * a.top + i]);
     __syncthreads();
-    int total = 0;
+    // what the last entry of any list reaches is a bound on the row's last, and
+    // so is what every list's share of the best reaches: few are left, and each
+    // counts the ones before it (many only where few lists hold all of the best)
+    u64 least = 1, shares = ~0ull;
+    const int part = (a.top + chunks - 1) / chunks;
+    for (int l = 0; l < chunks && a.top; ++l) {
+        const u64 last = keys[l * a.top + a.top - 1], share = keys[l * a.top + part - 1];
+        least = last > least ? last : least;
+        shares = share < shares ? share : shares;
+    }
+    least = shares > least ? shares : least;
     for (int i = tid; i < n; i += 256) {
         const u64 key = keys[i];
-        if (!key) continue;
-        int place = 0;
-        for (int l = 0; l < chunks && place < a.top; ++l) {
-            int x = 0, y = a.top;   // entries of the list that come before
-            while (x < y) {
-                const int m = (x + y) >> 1;
-                if (keys[l * a.top + m] > key)
-                    x = m + 1;
-                else
-                    y = m;
-            }
-            place += x;
+        if (key < least) continue;
+        const int at = atomicAdd(&left, 1);
+        if (at < KEPT) kept[at] = key;
+    }
+    __syncthreads();
+    const int total = left;
+    auto place = [&](u64 key, int before) __attribute__((always_inline)) {
+        if (before >= a.top) return;
+        const Best b = of_key(key);
+        put_top(a, row, before, p, q, b.z, b.i);
+    };
+    if (total <= KEPT) {
+        for (int i = tid; i < total; i += 256) {
+            const u64 key = kept[i];
+            int before = 0;
+#pragma unroll 4
+            for (int k = 0; k < total; ++k) before += kept[k] > key;
+            place(key, before);
         }
-        if (place < a.top) {
-            const Best b = of_key(key);
-            put_top(a, row, place, p, q, b.z, b.i);
+    } else {
+        for (int i = tid; i < n; i += 256) {
+            const u64 key = keys[i];
+            if (key < least) continue;
+            int before = 0;
+            for (int l = 0; l < chunks && before < a.top; ++l) {
+                int x = 0, y = a.top;   // entries of the (sorted) list that come before
+                while (x < y) {
+                    const int m = (x + y) >> 1;
+                    if (keys[l * a.top + m] > key)
+                        x = m + 1;
+                    else
+                        y = m;
+                }
+                before += x;
+            }
+            place(key, before);
         }
     }
     // places that no class takes
-    for (int i = tid; i < n; i += 256) total += keys[i] != 0;
-    __shared__ int sums[4];
-    total = wave_sum(total);
-    if ((tid & 63) == 0) sums[tid >> 6] = total;
-    __syncthreads();
-    total = sums[0] + sums[1] + sums[2] + sums[3];
     if (tid < a.top && tid >= total) put_top(a, row, tid, p, q, -infinity(), -1);
 }
 
@@ -968,7 +995,9 @@ hipError_t launch_score(const ScoreArgs &a, hipStream_t s) {
 hipError_t launch_score_join(const ScoreArgs &a, hipStream_t s) {
     if (!score_valid(a) || a.l.chunks < 2 || a.l.rows * 256ll > 0xffffffffll) return hipErrorInvalidValue;
     void *p[] = {const_cast<ScoreArgs *>(&a)};
-    return hipLaunchKernel(reinterpret_cast<const void *>(&score_join_kernel), dim3((unsigned)a.l.rows), dim3(256), p, 0, s);
+    const void *kernel = a.l.chunks * a.top <= 1024 ? reinterpret_cast<const void *>(&score_join_kernel<1024>)
+                                                    : reinterpret_cast<const void *>(&score_join_kernel<ANSWER_MAX_CHUNKS * TOP_MAX>);
+    return hipLaunchKernel(kernel, dim3((unsigned)a.l.rows), dim3(256), p, 0, s);
 }
 
 hipError_t launch_distill(const DistillArgs &a, hipStream_t s) {

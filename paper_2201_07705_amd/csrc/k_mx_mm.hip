@@ -118,6 +118,8 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
 #pragma unroll
         for (int j = 0; j < FN; ++j) f[j] = *(const i32x4 *)(s + rb + j * 16 * ROW);
     };
+    // (reads are issued before the products that they are to pass behind)
+    auto behind = [&]() __attribute__((always_inline)) { __builtin_amdgcn_sched_barrier(0); };
     auto read_s = [&]() __attribute__((always_inline)) {
 #pragma unroll
         for (int i = 0; i < FM; ++i) sa[i] = *(const int *)(sc + (wm * TM + i * 16 + l16) * 16 + g * 4);
@@ -149,18 +151,21 @@ __global__ __launch_bounds__((mx_threads_of(T)), T == 256 ? 1 : T == 128 ? 4 : 2
         i32x4(&b)[FN] = P & 1 ? fb1 : fb0, (&b_next)[FN] = P & 1 ? fb0 : fb1;
         if constexpr (HALVES) {
             read_a(fa1, cur, NA);
+            behind();
             mul(which, fa0, b, 0);
             turn(which);
-            issue(which, cur);
             read_a(fa0, next, 0);
             read_b(b_next, next);
+            issue(which, cur);
+            behind();
             mul(which, fa1, b, NA);
         } else {
             i32x4(&f)[NA] = P & 1 ? fa1 : fa0, (&f_next)[NA] = P & 1 ? fa0 : fa1;
             turn(which);
-            issue(which, cur);
             read_a(f_next, next, 0);
             read_b(b_next, next);
+            issue(which, cur);
+            behind();
             mul(which, f, b, 0);
         }
         if constexpr (P == 3) read_s();

@@ -376,3 +376,21 @@ def test_a_wide_call_that_was_not_made_before_is_not_captured(ctx):
             ctx.log_probs(z, top=64, outputs={}, stream=torch.cuda.current_stream())
         z.add_(0)
     assert e.value.code == G.ESTATE
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_wide_rows_whose_best_lie_in_one_place(ctx, dtype):
+    """All of the best classes in one chunk of a row, in each chunk the same
+    ones, and rows with fewer classes offered than are asked for."""
+    import torch
+    classes = 300000
+    z = make(5, classes, dtype, seed=1, spread=0.5).clamp(max=3)
+    z[0, 777:900] = 20 + torch.arange(123, device="cuda").to(z.dtype) % 64 / 4
+    z[1] = -math.inf
+    z[1, ::20000] = 1.0
+    z[2] = 2.0
+    z[3] = (torch.arange(classes, device="cuda") % 97 == 5).to(z.dtype)
+    z[4] = (torch.arange(classes, device="cuda") % 8192 < 64).to(z.dtype) * 7
+    labels = torch.tensor([888, 40000, 5, classes - 1, 8192], device="cuda", dtype=torch.int32)
+    for top in (1, 20, 64):
+        check(ctx, z, labels, top)
