@@ -848,8 +848,10 @@ gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows,
  * dtype says which. A class whose logit is -inf is not offered; softmaxes
  * are those of logits / temperature (1e-6..1e6), summed in float32. A row
  * that holds a NaN or +inf gives NaN and -1, and no other row is touched by
- * it. Rows of more than 16384 (float32) or 32768 (bf16) classes may take a
- * workspace. rows 0 is no error and touches nothing.
+ * it. Calls with rows of more than 4096 (float32) or 8192 (bf16) classes may
+ * take a workspace; others can be captured without a call of their sizes
+ * before (but for a context's first one). rows 0 is no error and touches
+ * nothing.
  */
 
 /* Outputs of gemel_log_probs; each may be NULL (not computed). */

@@ -59,7 +59,7 @@ gemel_status log_probs(gemel_ctx *ctx, const Logits &l, const int32_t *labels, i
     score_plan(a.l, a.top);
     DeviceScope scope(ctx->device);
     State *st;
-    if (gemel_status s = ready(ctx, &st)) return s;
+    if (gemel_status s = ready(ctx, stream, &st)) return s;
     if (a.l.chunks == 1) {
         OPCHK(launch_score(a, stream), "log probabilities");
         return GEMEL_OK;
@@ -82,7 +82,7 @@ gemel_status distill(gemel_ctx *ctx, DistillArgs a, hipStream_t stream) {
     distill_plan(a.l);
     DeviceScope scope(ctx->device);
     State *st;
-    if (gemel_status s = ready(ctx, &st)) return s;
+    if (gemel_status s = ready(ctx, stream, &st)) return s;
     if (a.l.chunks > 1) {
         Call c{ctx, st, stream, nullptr, {}, nullptr};
         ScoreArgs sums{};

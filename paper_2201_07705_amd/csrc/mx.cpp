@@ -50,7 +50,7 @@ struct Wide {
 gemel_status in_registers(Call &c, const Wide &p) {
     gemel_ctx *ctx = c.ctx;
     const int64_t ld = op_round_up(p.w.cols, 8);
-    const int each = p.f32 ? (int)std::min<int64_t>(p.M, std::max<int64_t>(1024, PIECE / ld / 64 * 64)) : p.M;
+    const int each = p.f32 ? (int)std::min<int64_t>(p.M, std::max<int64_t>(1024, std::min(MX_MOST, PIECE / ld / 64 * 64))) : p.M;
     auto plan = [&](int rows) {
         MxRows a{};
         a.w = p.w;
@@ -187,7 +187,7 @@ gemel_status gemel_mx_quantize(gemel_ctx *ctx, const void *x, int64_t x_stride, 
             return s;
         DeviceScope scope(ctx->device);
         State *st;
-        if (gemel_status s = ready(ctx, &st)) return s;
+        if (gemel_status s = ready(ctx, (hipStream_t)hip_stream, &st)) return s;
         a.x = x;
         a.ld = x_stride;
         a.f32 = dtype == GEMEL_F32;
@@ -211,7 +211,7 @@ gemel_status gemel_mx_dequantize(gemel_ctx *ctx, const gemel_mx *q, void *out, i
             return s;
         DeviceScope scope(ctx->device);
         State *st;
-        if (gemel_status s = ready(ctx, &st)) return s;
+        if (gemel_status s = ready(ctx, (hipStream_t)hip_stream, &st)) return s;
         a.out = out;
         a.ld = out_stride;
         a.f32 = dtype == GEMEL_F32;
@@ -248,7 +248,7 @@ gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x, int64
             return s;
         DeviceScope scope(ctx->device);
         State *st;
-        if (gemel_status s = ready(ctx, &st)) return s;
+        if (gemel_status s = ready(ctx, (hipStream_t)hip_stream, &st)) return s;
         Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
         if (xq) return both_quantized(c, q, w, bias, y, y_stride, f32);
         const Wide p{x, x_stride, rows, w, bias, (char *)y, y_stride, f32};

@@ -65,6 +65,7 @@ hipError_t launch_mx_sum(const MxSum &a, hipStream_t s);
 // planes of float32 ones. Up to MX_FEW rows the waves of a workgroup split
 // the depth; beyond that they split the outputs and share the rows in LDS.
 constexpr int MX_FEW = 16, MX_ROWS = 1024;   // MX_ROWS: of bf16; float32 rows always
+constexpr int64_t MX_MOST = 1 << 19;         // rows of a launch
 struct MxRows {
     Mx w;
     const u16 *x;

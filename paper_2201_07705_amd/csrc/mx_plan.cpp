@@ -60,7 +60,7 @@ bool mx_rows_valid(const MxRows &a) {
         if (a.waves < 1 || a.waves > 16) return false;
     } else {
         if (a.waves != 8 || a.slices < 1 || a.per < 1 || (int64_t)a.slices * a.per < steps || (int64_t)(a.slices - 1) * a.per >= steps ||
-            a.slices > 65535 || a.q.codes || a.M > 65535 * 16)
+            a.slices > 65535 || a.q.codes || a.M > MX_MOST)
             return false;
         if (a.slices > 1 && (!a.part || a.ldp < a.w.rows || a.ldp % 4)) return false;
     }

@@ -148,6 +148,16 @@ inline gemel_status ready(gemel_ctx *ctx, State **out) {
     return GEMEL_OK;
 }
 
+// The same for a call on a stream: a context sets up nothing while that is
+// captured.
+inline gemel_status ready(gemel_ctx *ctx, hipStream_t stream, State **out) {
+    hipStreamCaptureStatus cs = hipStreamCaptureStatusNone;
+    if (!ctx->operators && stream) OPCHK(hipStreamIsCapturing(stream, &cs), "hipStreamIsCapturing");
+    if (cs != hipStreamCaptureStatusNone)
+        return fail(ctx, GEMEL_ESTATE, "the context's first call cannot be captured: make it once before");
+    return ready(ctx, out);
+}
+
 // Offsets of a call's buffers in its stream's workspace.
 struct Layout {
     size_t bytes = 0;

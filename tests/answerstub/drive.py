@@ -44,8 +44,27 @@ class Driver:
         return G.Mx(rows, cols, self.memory(*codes, codes[1], 1) + change[0] if change else self.memory(*codes, codes[1], 1),
                     self.memory(*scales, scales[1], 1) + (change[1] if change else 0))
 
+    def capture(self):
+        """A context's first call on a stream that is captured, and the same
+        call before and after another one."""
+        L, h, s = self.L, ctypes.c_void_p(), ctypes.c_void_p()
+        L.hoststub_set_capturing.argtypes = [ctypes.c_void_p]
+        assert L.gemel_create(ctypes.byref(h), 0, G.BF16, 0) == G.OK
+        assert L.hipStreamCreateWithFlags(ctypes.byref(s), 1) == 0
+        a = G.Answers(entropy=self.memory(4, 1, 1, 4))
+        narrow, wide = self.memory(4, 100, 100, 4), self.memory(4, 9000, 9000, 4)
+        res = []
+        for captured, z, n in ((1, narrow, 100), (0, narrow, 100), (1, narrow, 100), (1, wide, 9000), (0, wide, 9000), (1, wide, 9000)):
+            L.hoststub_set_capturing(s if captured else None)
+            res.append(L.gemel_log_probs(h, 4, n, z, n, G.F32, None, 0, 1.0, a, s))
+            L.hoststub_set_capturing(None)
+        assert L.gemel_destroy(h) == G.OK
+        return res
+
     def call(self, c):
         L, op = self.L, c["op"]
+        if op == "capture":
+            return self.capture()
         ctx = self.ctx[c.get("ctx", "bf16")]
         e = 4 if c["dtype"] == "f32" else 2
         code = G.F32 if c["dtype"] == "f32" else G.BF16

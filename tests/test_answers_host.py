@@ -139,6 +139,17 @@ def test_float32_rows_beyond_one_piece(lib):
     assert sound(lib, [dict(c, rows=r) for r in want]) == list(want.values())
 
 
+def test_many_short_float32_rows(lib):
+    c = {"op": "product", "dtype": "f32", "acts": "float", "k": 3, "n": 2, "bias": 0}
+    assert sound(lib, [dict(c, rows=(1 << 19) + 1), dict(c, rows=1 << 19)]) == ["planes rows planes few", "planes rows"]
+
+
+def test_what_may_be_captured(lib):
+    """Neither a context's first call nor one that its stream's workspace is
+    too small for; nothing else needs a call before."""
+    assert drive(lib, [{"op": "capture"}])["calls"] == [[-7, 0, 0, -7, 0, 0]]
+
+
 def test_the_check_itself(lib):
     """Operands that begin one element before their memory are found out."""
     for c in ({"op": "log_probs", "dtype": "bf16", "rows": 5, "classes": 100, "k": 3, "off": {"logits": -2}},
