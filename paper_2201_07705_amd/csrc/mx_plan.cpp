@@ -34,7 +34,9 @@ bool mx_sum_valid(const MxSum &a) {
 // Up to MX_FEW rows: 16 outputs to a workgroup, whose waves (at most 16) have
 // a group of 512 columns or more each; no slices. Beyond: slices until the
 // card is full, of at least 4 steps; 512 outputs to a workgroup where that
-// leaves enough of them.
+// leaves enough of them (37 rows 4096 -> 4096, whose 32 steps fill few
+// workgroups: 18.5 us with 512, 13.7 with 256; float32 25088 -> 4096 42 and
+// 47). 16 rows 4096 -> 4096 7.7 us, 17 rows 11.5.
 void mx_rows_plan(MxRows &a) {
     a.ldp = op_round_up(a.w.rows, 4);
     a.per = a.slices = 1;
@@ -73,7 +75,8 @@ int64_t mx_mm_tiles(const MxMm &a) {
 }
 
 // The largest tile that still fills the card, cut over the depth where even
-// small ones do not.
+// small ones do not. 4096 -> 4096: 4096 rows in tiles of 256 41 us (3360
+// TFLOP/s), 2048 in tiles of 128 26 (2630).
 void mx_mm_plan(MxMm &a) {
     const int groups = (int)mx_groups(a.w.cols);
     a.splits = 1;
