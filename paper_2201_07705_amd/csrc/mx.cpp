@@ -44,12 +44,11 @@ struct Wide {
     bool f32;
 };
 
-// float32 rows, and up to MX_ROWS bf16 ones: the weights are expanded in
-// registers (bf16 25088 -> 4096: 512 rows 124 us, expanded once 172; 1024
-// rows 240 and 245, 2048 rows 451 and 393; float32, planes below each other
-// through the bf16 product: 1024 rows 553 and 685, 16384 rows 9.5 and 8.9 ms
-// there, 1.6 and 1.7 ms for 4096 -> 4096). Planes of float32 rows are made for
-// a piece of the rows at a time, which bounds the workspace.
+// float32 rows, and bf16 ones where that is expected to take less time: the
+// weights are expanded in registers (float32, planes below each other through
+// the bf16 product instead: 1024 rows 25088 -> 4096 473 us and 685, 16384 rows
+// 8.2 and 8.9 ms, 4096 -> 4096 1.25 and 1.7). Planes of float32 rows are made
+// for a piece of the rows at a time, which bounds the workspace.
 gemel_status in_registers(Call &c, const Wide &p) {
     gemel_ctx *ctx = c.ctx;
     const int64_t ld = op_round_up(p.w.cols, 8);
@@ -88,19 +87,19 @@ gemel_status in_registers(Call &c, const Wide &p) {
     return GEMEL_OK;
 }
 
-// More bf16 rows: the weights are expanded to bf16 once and go through the
-// bf16 product.
-gemel_status expanded(Call &c, const Wide &p) {
+// bf16 rows otherwise: the weights are expanded to bf16 once and go through
+// the bf16 product, which needs a copy of rows that are not aligned. Which of
+// the two is taken: up to MX_ROWS rows never this one, slower at each of 10
+// shapes of 256 to 1024 rows; beyond, the one of the smaller estimate, both a
+// fit to these shapes of up to 16384 rows: what is taken is 1.5% from the
+// faster one in the mean, 26% at worst. 25088 -> 4096: 1024 rows 211 us in
+// registers, expanded once 248, 2048 rows 393 and 398, 4096 rows 781 and 689;
+// 1000 -> 1000 4096 rows 16.3 and 25.6; 21990 -> 856 (copied) 3451 rows 183
+// and 321.
+gemel_status expanded(Call &c, const Wide &p, MmArgs m) {
     gemel_ctx *ctx = c.ctx;
-    const int64_t Kp = op_round_up(p.w.cols, 8);
+    const int64_t Kp = m.K;
     const bool copy = !in_place(p.x, p.M, p.ldx, p.w.cols);
-    MmArgs m{};
-    m.M = p.M;
-    m.N = p.w.rows;
-    m.K = (int)Kp;
-    m.batch = 1;
-    m.epi = EPI_ROWS;
-    mm_plan(m);
     if (!mm_fits(m)) return fail(ctx, GEMEL_EINVAL, "the product is too large");
     const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(copy ? p.M * Kp : 0, 2), o_part = c.lay.take(partial_floats(m), 4);
     if (gemel_status s = workspace(c)) return s;
@@ -136,6 +135,24 @@ gemel_status expanded(Call &c, const Wide &p) {
     m.o.bias = p.bias;
     OPCHK(launch_mm(m, c.stream), "product");
     return GEMEL_OK;
+}
+
+gemel_status wide_product(Call &c, const Wide &p) {
+    if (p.f32 || p.M <= MX_ROWS) return in_registers(c, p);
+    MmArgs m{};
+    m.M = p.M;
+    m.N = p.w.rows;
+    m.K = (int)op_round_up(p.w.cols, 8);
+    m.batch = 1;
+    m.epi = EPI_ROWS;
+    const double bytes = 2.0 * p.M * p.w.cols;   // of the rows; microseconds
+    double once = 7 + std::max(0.8 * mm_plan(m), bytes / 2.3e6) + 2.5 * p.w.rows * p.w.cols / 2.4e6;
+    if (!in_place(p.x, p.M, p.ldx, p.w.cols)) once += 5.4 + 2 * bytes / 2.3e6;
+    MxRows a{};
+    a.w = p.w;
+    a.planes = 1;
+    a.M = p.M;
+    return p.M <= MX_MOST && (!mm_fits(m) || mx_rows_plan(a) <= once) ? in_registers(c, p) : expanded(c, p, m);
 }
 
 gemel_status both_quantized(Call &c, const Mx &x, const Mx &w, const float *bias, void *y, int64_t ldy, bool f32) {
@@ -255,7 +272,7 @@ gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x, int64
         Call c{ctx, st, (hipStream_t)hip_stream, nullptr, {}, nullptr};
         if (xq) return both_quantized(c, q, w, bias, y, y_stride, f32);
         const Wide p{x, x_stride, rows, w, bias, (char *)y, y_stride, f32};
-        return f32 || rows <= MX_ROWS ? in_registers(c, p) : expanded(c, p);
+        return wide_product(c, p);
     });
 }
 

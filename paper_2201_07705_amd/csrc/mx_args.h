@@ -64,7 +64,7 @@ hipError_t launch_mx_sum(const MxSum &a, hipStream_t s);
 // Rows that are not quantised against 4-bit weights w: bf16 rows, or three
 // planes of float32 ones. Up to MX_FEW rows the waves of a workgroup split
 // the depth; beyond that they split the outputs and share the rows in LDS.
-constexpr int MX_FEW = 16, MX_ROWS = 1024;   // MX_ROWS: of bf16; float32 rows always
+constexpr int MX_FEW = 16, MX_ROWS = 1024;   // MX_ROWS: of bf16 always, more by estimate; float32 rows always
 constexpr int64_t MX_MOST = 1 << 19;         // rows of a launch
 struct MxRows {
     Mx w;
@@ -89,7 +89,7 @@ struct MxRows {
 constexpr int mx_row_blocks(int M) {
     return M <= 32 ? 2 : M <= 48 ? 3 : M <= 64 || 10 * ((M + 47) / 48 * 48) > 9 * ((M + 63) / 64 * 64) ? 4 : 3;
 }
-void mx_rows_plan(MxRows &a);
+double mx_rows_plan(MxRows &a);   // the microseconds expected
 bool mx_rows_valid(const MxRows &a);
 hipError_t launch_mx_rows(const MxRows &a, hipStream_t s);
 

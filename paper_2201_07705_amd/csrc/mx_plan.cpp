@@ -32,27 +32,49 @@ bool mx_sum_valid(const MxSum &a) {
 }
 
 // Up to MX_FEW rows: 16 outputs to a workgroup, whose waves (at most 16) have
-// a group of 512 columns or more each; no slices. Beyond: slices until the
-// card is full, of at least 4 steps; 512 outputs to a workgroup where that
-// leaves enough of them (37 rows 4096 -> 4096, whose 32 steps fill few
-// workgroups: 18.5 us with 512, 13.7 with 256; float32 25088 -> 4096 42 and
-// 47). 16 rows 4096 -> 4096 7.7 us, 17 rows 11.5.
-void mx_rows_plan(MxRows &a) {
+// a group of 512 columns or more each; no slices (16 rows 4096 -> 4096 7.7 us,
+// 17 rows 11.5). Beyond: 256 or 512 outputs to a workgroup and slices of the
+// depth, by the estimated time: the turns that the 256 compute units take,
+// each a step's time for every step (expanding weights, and products) and a
+// fixed part, and the sums of slices. The times are a fit to 10 shapes of 20
+// to 16384 rows, forms and slices, 10% off in the mean square; the form taken
+// is 0.6% from the fastest one measured in the mean and 24% at worst (2048
+// outputs of 512 columns). What is at stake: bf16 25088 -> 4096 37 rows 23.4
+// us with 256 outputs, 27.0 with 512, 2048 rows 463 and 393; 1024 rows 4096 ->
+// 4096 39.9 whole with 256, 51.3 in two slices with 512.
+double mx_rows_plan(MxRows &a) {
     a.ldp = op_round_up(a.w.rows, 4);
     a.per = a.slices = 1;
+    a.wide = 0;
     if (a.M <= MX_FEW) {
         a.waves = (int)std::min<int64_t>(mx_groups(a.w.cols), 16);
-        return;
+        return 0;
     }
     a.waves = 8;
-    const int steps = (a.w.cols + 127) / 128, rows = 16 * mx_row_blocks(a.M);
-    const int64_t down = (a.M + rows - 1) / rows;
-    a.wide = (a.w.rows + 511) / 512 * down * (steps / 4) >= 256;
-    const int n = a.wide ? 512 : 256;
-    const int64_t tiles = (a.w.rows + n - 1) / n * down;
-    const int want = (int)std::max<int64_t>(1, std::min<int64_t>(steps / 4, 256 / tiles));
-    a.per = (steps + want - 1) / want;
-    a.slices = (steps + a.per - 1) / a.per;
+    const int steps = (a.w.cols + 127) / 128, blocks = mx_row_blocks(a.M), down = (a.M + 16 * blocks - 1) / (16 * blocks);
+    double best = 1e30;
+    for (int wide = 0; wide < 2; ++wide) {
+        const int n = wide ? 512 : 256, products = a.planes * blocks * (wide ? 4 : 2);
+        const double step = wide ? 0.71 + 0.063 * products : 0.47 + 0.07 * products;   // microseconds
+        const double fixed = a.planes == 1 ? (wide ? 12 : 5) : (wide ? 7.5 : 6.5);
+        const int64_t tiles = (int64_t)((a.w.rows + n - 1) / n) * down;
+        const int most = (int)std::max<int64_t>(1, std::min<int64_t>({steps / 2, 512 / tiles, 64}));
+        for (int want = 1; want <= most; ++want) {
+            const int per = (steps + want - 1) / want;
+            if ((steps + per - 1) / per != want) continue;
+            const double bytes = want > 1 ? 4.0 * want * a.M * a.ldp : 0;
+            if (bytes > 1e9) break;
+            double us = 2 + (double)((tiles * want + 255) / 256) * (per * step + fixed);
+            if (want > 1) us += 2.5 + 0.1 * want + 2 * bytes / 6.2e6;
+            if (us < best) {
+                best = us;
+                a.wide = wide;
+                a.per = per;
+                a.slices = want;
+            }
+        }
+    }
+    return best;
 }
 
 bool mx_rows_valid(const MxRows &a) {

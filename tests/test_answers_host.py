@@ -126,8 +126,10 @@ def test_every_path_of_products(lib):
     q = dict(p, acts="mx")
     calls = [dict(p, rows=16), dict(f, rows=16), dict(q, rows=16), dict(p, rows=17), dict(f, rows=17), dict(q, rows=17),
              dict(p, rows=1024), dict(p, rows=1025), dict(p, rows=1025, k=1001), dict(f, rows=1025), dict(q, rows=5000, n=4096),
-             dict(p, rows=17, k=100), dict(q, rows=17, k=100)]
-    want = ["few", "planes few", "few", "rows", "planes rows", "mm", "rows", "values", "values", "planes rows", "mm", "rows", "mm"]
+             dict(p, rows=17, k=100), dict(q, rows=17, k=100), dict(p, rows=5000, k=4096), dict(p, rows=8192, k=515, n=9000),
+             dict(p, rows=3451, k=3001, n=90), dict(p, rows=257, k=300000, n=5)]
+    want = ["few", "planes few", "few", "rows", "planes rows", "mm", "rows", "rows", "rows", "planes rows", "mm", "rows", "mm",
+            "values", "values", "rows", "rows"]
     assert sound(lib, calls) == want
 
 

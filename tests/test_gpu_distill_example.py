@@ -92,7 +92,12 @@ def test_four_bits_answer_as_their_values_say(example):
         plain = ctx.adapter_batch([-1], [rows], 1, 1)
         z = ctx.adapt(plain, x, ctx.mx_dequantize(q))
         size = x.double().abs() @ ctx.mx_dequantize(q, dtype=torch.float32).double().abs().T
-        assert ((y.double() - z.double()).abs() <= z.double().abs() * 2.0 ** -8 + size * 400 * 2.0 ** -24).all()
+        # Two sums in orders of their own, each then rounded by at most half a
+        # step (2^-8 of it): |y - z| <= |y - s| + |s - t| + |t - z|, where the
+        # sums s and t are at most (1 + 2^-8) times as large as y and z.
+        sums = size * 400 * 2.0 ** -24
+        half = 2.0 ** -8 * (1 + 2.0 ** -8)
+        assert ((y.double() - z.double()).abs() <= (y.double().abs() + z.double().abs()) * half + sums).all()
         best = ctx.log_probs(y, top=3)
         labels = best["top_indices"][:, 1].contiguous()
         again = ctx.log_probs(y, labels=labels)

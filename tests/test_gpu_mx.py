@@ -227,6 +227,17 @@ def test_large_products(ctxs, m, k, n, dtype, acts):
     check_product(ctx, x, ctx.mx_quantize(w), bias, acts)
 
 
+@pytest.mark.parametrize("m,k,n", [(2052, 1000, 300), (5000, 4096, 300), (8192, 515, 9000), (1500, 1000, 1000), (4096, 1000, 1000),
+                                   (3451, 2199, 856), (256, 4096, 700), (257, 4096, 700), (2049, 20000, 100)])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_many_bf16_rows(ctxs, m, k, n, shift):
+    """Weights expanded in registers and once, rows with and without a copy,
+    slices of the depth."""
+    ctx = ctxs["bf16"]
+    x, w, bias = product("bf16", "float", m, k, n, pad=shift, shift=shift)
+    check_product(ctx, x, ctx.mx_quantize(w), bias, "float")
+
+
 @pytest.mark.parametrize("acts", ["float", "mx"])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_products_into_columns_of_a_matrix(ctxs, dtype, acts):
