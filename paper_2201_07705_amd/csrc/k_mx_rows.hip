@@ -101,7 +101,7 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
 // 4096 in 510 us; NB = 4 473, 1330 TFLOP/s of bf16 products).
 template <int P, int MB, int NB>
 __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
-    constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = (CHUNKS + 511) / 512;
+    constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = mx_piece_loads(P * ROWS);
     constexpr int AHEAD = P == 3 && NB == 4 ? 1 : 2;   // steps (registers)
     __shared__ uint4 st[2][CHUNKS];
     const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -121,24 +121,22 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
         uint4 x[LOADS], w[NB];
         uint32_t s[NB];
     } ahead[AHEAD];
-    // (rows of x as the thread's chunks lie in them; no branch stands between
+    // (where the thread's pieces begin in their rows; no branch stands between
     // the loads of a whole step)
-    const u16 *rows[LOADS];
+    const u16 *pieces[LOADS];
+    const int col = mx_piece_col(tid);
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-        const int id = min(i * 512 + tid, CHUNKS - 1), p = id / (ROWS * 16), r = id / 16 % ROWS;
-        rows[i] = a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx + (id & 15) * 8;
+        const int row = mx_piece_row(i, tid, P * ROWS), p = row / ROWS, r = row % ROWS;
+        pieces[i] = a.x + p * a.plane + (int64_t)min(m0 + r, a.M - 1) * a.ldx + col;
     }
     auto load = [&](Ahead &q, int step) __attribute__((always_inline)) {
         if ((step + 1) * 128 <= K) {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) q.x[i] = get_16b(rows[i] + step * 128);
+            for (int i = 0; i < LOADS; ++i) q.x[i] = get_16b(pieces[i] + step * 128);
         } else {
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) {
-                const int c = (tid & 15) * 8;
-                q.x[i] = mx_chunk(rows[i] - c, step * 128 + c, K);
-            }
+            for (int i = 0; i < LOADS; ++i) q.x[i] = mx_chunk(pieces[i] - col, step * 128 + col, K);
         }
         const uint8_t *const wc = code0 + step * 64ll, *const ws = scale0 + (int64_t)(step >> 2) * N * 16;
 #pragma unroll

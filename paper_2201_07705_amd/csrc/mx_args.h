@@ -89,6 +89,20 @@ struct MxRows {
 constexpr int mx_row_blocks(int M) {
     return M <= 32 ? 2 : M <= 48 ? 3 : M <= 64 || 10 * ((M + 47) / 48 * 48) > 9 * ((M + 63) / 64 * 64) ? 4 : 3;
 }
+// Beyond MX_FEW rows: the rows of a workgroup (of every plane, below each
+// other) pass through LDS in steps of 128 columns, in pieces of 8: load i of
+// thread t of 512 brings the piece at columns mx_piece_col(t) of the step, of
+// row mx_piece_row(i, t, rows). Where rows are no multiple of 32, threads that
+// are left over load the last row once more.
+constexpr int MX_PIECE_THREADS = 512;
+constexpr int mx_piece_loads(int rows) { return (rows * 16 + MX_PIECE_THREADS - 1) / MX_PIECE_THREADS; }
+constexpr int mx_piece_col(int thread) { return thread % 16 * 8; }
+constexpr int mx_piece_row(int i, int thread, int rows) {
+    const int row = (i * MX_PIECE_THREADS + thread) / 16;
+    return row < rows ? row : rows - 1;
+}
+// Columns of the piece at column c that there are.
+constexpr int mx_piece_cols(int c, int cols) { return c + 8 <= cols ? 8 : c < cols ? cols - c : 0; }
 double mx_rows_plan(MxRows &a);   // the microseconds expected
 bool mx_rows_valid(const MxRows &a);
 hipError_t launch_mx_rows(const MxRows &a, hipStream_t s);

@@ -77,11 +77,12 @@ __device__ __forceinline__ mx_f32x4 mx_bias(const float *bias, int n, int N) {
 
 // 16 bytes of bf16 from element c of a row of `cols`, zeros from there on.
 __device__ __forceinline__ uint4 mx_chunk(const u16 *row, int c, int cols) {
-    if (c + 8 <= cols) return get_16b(row + c);
+    const int there = mx_piece_cols(c, cols);
+    if (there == 8) return get_16b(row + c);
     uint4 v = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < 8; ++j)
-        if (c + j < cols) (&v.x)[j / 2] |= (uint32_t)row[c + j] << (j & 1) * 16;
+        if (j < there) (&v.x)[j / 2] |= (uint32_t)row[c + j] << (j & 1) * 16;
     return v;
 }
 

@@ -126,9 +126,26 @@ hipError_t launch_mx_sum(const MxSum &a, hipStream_t) {
     touch_rows("y", a.y, a.rows, a.cols, a.ldy, a.f32 ? 4 : 2);
     return hipSuccess;
 }
+// What the threads of mx_rows_kernel read of x: the pieces of a whole step and
+// of the last one, with the kernel's own map (the whole steps between them
+// end before the columns do).
+static void touch_pieces(const MxRows &a) {
+    const int rows = 16 * mx_row_blocks(a.M), all = a.planes * rows, last = (a.w.cols - 1) / 128;
+    for (int m0 = 0; m0 < a.M; m0 += rows)
+        for (int i = 0; i < mx_piece_loads(all); ++i)
+            for (int t = 0; t < MX_PIECE_THREADS; ++t) {
+                const int row = mx_piece_row(i, t, all), m = m0 + row % rows < a.M ? m0 + row % rows : a.M - 1;
+                const u16 *p = a.x + row / rows * a.plane + m * a.ldx;
+                for (int step : {0, last}) {
+                    const int c = step * 128 + mx_piece_col(t);
+                    touch("a piece of x", p + c, mx_piece_cols(c, a.w.cols) * 2);
+                }
+            }
+}
 hipError_t launch_mx_rows(const MxRows &a, hipStream_t) {
     BEGIN(a.M <= MX_FEW ? "few" : "rows", mx_rows_valid(a));
     touch_mx("w", a.w);
+    if (a.M > MX_FEW) touch_pieces(a);
     if (a.q.codes)
         touch_mx("q", a.q);
     else
