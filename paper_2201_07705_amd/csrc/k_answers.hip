@@ -672,11 +672,13 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(con
     if (index >= a.l.classes) index = -1;
     const bool entry = index >= 0;
     const float z_entry = entry ? logit(a.l, z, index) : 0.f;
-    // the teacher's side; a value that is NaN or +inf makes the mass NaN
-    const float v = entry ? value * a.l.inv_t : -infinity();
-    const float v_most = wave_max(v);
+    // the teacher's side, like the student's the distance from the largest
+    // value first, then scaled (finite values do not overflow); a value that is
+    // NaN or +inf makes the mass NaN
+    const float v = entry ? value : -infinity();
+    const float v_most = wave_max(v), far = (v - (v_most == -infinity() ? 0.f : v_most)) * a.l.inv_t;
     const bool some = bad || __builtin_amdgcn_ballot_w64(!(v == -infinity())) != 0;
-    const float e = entry ? expf(v - (v_most == -infinity() ? 0.f : v_most)) : 0.f;
+    const float e = entry ? expf(far) : 0.f;
     float mass = wave_sum(e);
     if (bad) mass = quiet();
     const float share = e / mass;
@@ -690,7 +692,7 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(con
     const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
     const float t_entry = (z_entry - p.m) * a.l.c;
     if (a.loss && w == 0 && chunk == 0) {
-        const float log_q = v - v_most - logf(mass), log_p = (z_entry - p.m) * a.l.inv_t - LN2 * log2f(p.s);
+        const float log_q = far - logf(mass), log_p = (z_entry - p.m) * a.l.inv_t - LN2 * log2f(p.s);
         const float sum = wave_sum(share > 0.f ? share * (log_q - log_p) : 0.f);
         if (lane == 0) a.loss[row] = !some ? 0.f : lost ? quiet() : a.t * a.t * sum;
     }
@@ -862,7 +864,7 @@ __global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a)
         wrong |= index[i] < -1 || index[i] >= a.l.classes;
         if (index[i] >= a.l.classes || index[i] < 0) index[i] = -1;
         z_entry[i] = index[i] >= 0 ? logit(a.l, z, index[i]) : 0.f;
-        v[i] = index[i] >= 0 ? v[i] * a.l.inv_t : -infinity();
+        if (index[i] < 0) v[i] = -infinity();
         some |= !(v[i] == -infinity());
         v_most = max3(v_most, v[i], v[i]);
     }
@@ -872,7 +874,9 @@ __global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a)
     float mass = 0.f;
 #pragma unroll
     for (int i = 0; i < E; ++i) {
-        share[i] = index[i] >= 0 ? expf(v[i] - (v_most == -infinity() ? 0.f : v_most)) : 0.f;
+        // (the distance first, then scaled: finite values do not overflow)
+        v[i] = (v[i] - (v_most == -infinity() ? 0.f : v_most)) * a.l.inv_t;
+        share[i] = index[i] >= 0 ? expf(v[i]) : 0.f;
         mass += share[i];
     }
     mass = wrong ? quiet() : row_sum(mass);
@@ -885,7 +889,7 @@ __global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a)
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < E; ++i) {
-            const float log_q = v[i] - v_most - log_mass, log_p = (z_entry[i] - p.m) * a.l.inv_t - log_s;
+            const float log_q = v[i] - log_mass, log_p = (z_entry[i] - p.m) * a.l.inv_t - log_s;
             if (share[i] > 0.f) sum += share[i] * (log_q - log_p);
         }
         sum = row_sum(sum);

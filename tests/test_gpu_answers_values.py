@@ -1,0 +1,71 @@
+"""Distillation against teachers' values of any size: only the distances of a
+row's values from each other count, and the type's lowest and largest ones
+are values like others, at every temperature."""
+
+import math
+
+import pytest
+
+from paper_2201_07705_amd import gemel as G
+from test_gpu_answers import make, teacher
+
+pytestmark = pytest.mark.gpu
+
+WIDTHS = [20, 100, 1000, 9000, 80000]
+
+
+@pytest.fixture(scope="module")
+def ctx():
+    c = G.Context(0, "bf16")
+    yield c
+    c.close()
+
+
+def both(ctx, z, index, value, t):
+    """Loss and gradient; the loss alone is the same."""
+    import torch
+    loss = torch.full((z.shape[0],), 55.0, device="cuda")
+    d = ctx.distill_backward(None, z, index, value, temperature=t, loss=loss)
+    assert torch.equal(ctx.distill(z, index, value, temperature=t), loss)
+    return loss, d
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS)
+@pytest.mark.parametrize("k", [5, 20])
+def test_a_shift_of_the_values_changes_nothing(ctx, classes, k, dtype):
+    """Multiples of 1/16 and of the shift are exact in float32, and so are
+    their distances: the same bits."""
+    import torch
+    z = make(7, classes, dtype, seed=classes)
+    index, value = teacher(z, k)
+    value = (value * 16).round() / 16
+    for t in (0.7, 1.0, 1.5):
+        loss, d = both(ctx, z, index, value, t)
+        assert loss.isfinite().all() and d.isfinite().all()
+        for shift in (-16384.0, 4096.0, 16384.0):
+            loss2, d2 = both(ctx, z, index, value + shift, t)
+            assert torch.equal(loss2, loss) and torch.equal(d2, d), (t, shift)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS)
+@pytest.mark.parametrize("k", [5, 20])
+def test_lowest_and_largest_values(ctx, classes, k, dtype):
+    """Rows of one value are those of zeros, whatever the value; behind a
+    value that is far above them others are as good as not there."""
+    import torch
+    z = make(6, classes, dtype, seed=classes)
+    index, value = teacher(z, k)
+    most = torch.finfo(torch.float32).max
+    value[0], value[1], value[2] = -most, most, 0.0
+    value[3], value[4], value[5] = -most, 0.0, -most
+    value[3, 2], value[4, 2], value[5, 2] = 0.0, most, most
+    same = torch.zeros_like(value)
+    same[3:] = -math.inf
+    same[3:, 2] = 0.0
+    for t in (0.1, 0.5, 1.0, 3.0):
+        loss, d = both(ctx, z, index, value, t)
+        want, d_want = both(ctx, z, index, same, t)
+        assert want.isfinite().all() and want.abs().min() > 0 and d_want.abs().amax(1).min() > 0
+        assert torch.equal(loss, want) and torch.equal(d, d_want), t
