@@ -258,6 +258,18 @@ __device__ __forceinline__ Part chunks_part(const Part *part, int chunks, float 
     return q;
 }
 
+// Half the distance of a and b: that of finite ones is finite.
+__device__ __forceinline__ float half_of(float a, float b) { return 0.5f * a - 0.5f * b; }
+
+// Loss of a row, which is 2 T times the sum of these over its entries: the
+// share q of an entry times half of T (log q - log p), with half the
+// distances of the teacher's value and of the logit from their row's largest,
+// and half of T (ln mass - ln S). (Divided by T instead, distances would
+// overflow in losses that do not.)
+__device__ __forceinline__ float loss_part(float share, float half_v, float half_z, float half_sums) {
+    return share > 0.f ? share * (half_v - half_z - half_sums) : 0.f;
+}
+
 struct Results {
     bool lost;      // some logit is NaN or +inf
     float log2_s;
@@ -265,7 +277,7 @@ struct Results {
 __device__ __forceinline__ Results results(const Part &p) { return {!(p.s < infinity()), log2f(p.s)}; }
 __device__ __forceinline__ float log_prob(const Part &p, const Results &q, float z, float inv_t) {
     if (q.lost) return quiet();
-    return z == -infinity() || p.s == 0.f ? -infinity() : (z - p.m) * inv_t - LN2 * q.log2_s;
+    return z == -infinity() || p.s == 0.f ? -infinity() : half_of(z, p.m) * (2.f * inv_t) - LN2 * q.log2_s;
 }
 // One row's outputs but for the list.
 __device__ __forceinline__ void put_row(const ScoreArgs &a, int row, const Part &p, int label, float z_label) {
@@ -692,9 +704,9 @@ __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(con
     const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
     const float t_entry = (z_entry - p.m) * a.l.c;
     if (a.loss && w == 0 && chunk == 0) {
-        const float log_q = far - logf(mass), log_p = (z_entry - p.m) * a.l.inv_t - LN2 * log2f(p.s);
-        const float sum = wave_sum(share > 0.f ? share * (log_q - log_p) : 0.f);
-        if (lane == 0) a.loss[row] = !some ? 0.f : lost ? quiet() : a.t * a.t * sum;
+        const float half_sums = 0.5f * a.t * (logf(mass) - LN2 * log2f(p.s));
+        const float sum = wave_sum(loss_part(share, half_of(v, v_most), half_of(z_entry, p.m), half_sums));
+        if (lane == 0) a.loss[row] = !some ? 0.f : lost ? quiet() : 2.f * a.t * sum;
     }
     if (!a.dz) return;
     char *const d = (char *)a.dz + (int64_t)row * a.ldd * SIZE;
@@ -875,8 +887,8 @@ __global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a)
 #pragma unroll
     for (int i = 0; i < E; ++i) {
         // (the distance first, then scaled: finite values do not overflow)
-        v[i] = (v[i] - (v_most == -infinity() ? 0.f : v_most)) * a.l.inv_t;
-        share[i] = index[i] >= 0 ? expf(v[i]) : 0.f;
+        const float far = (v[i] - (v_most == -infinity() ? 0.f : v_most)) * a.l.inv_t;
+        share[i] = index[i] >= 0 ? expf(far) : 0.f;
         mass += share[i];
     }
     mass = wrong ? quiet() : row_sum(mass);
@@ -885,15 +897,12 @@ __global__ __launch_bounds__(256) void distill_small_kernel(const DistillArgs a)
     const Part p = row_part<false>(h, a.l.c);
     const bool lost = !(p.s < infinity()) || p.s == 0.f || mass != mass;
     if (a.loss) {
-        const float log_mass = logf(mass), log_s = LN2 * log2f(p.s);
+        const float half_sums = 0.5f * a.t * (logf(mass) - LN2 * log2f(p.s));
         float sum = 0.f;
 #pragma unroll
-        for (int i = 0; i < E; ++i) {
-            const float log_q = v[i] - log_mass, log_p = (z_entry[i] - p.m) * a.l.inv_t - log_s;
-            if (share[i] > 0.f) sum += share[i] * (log_q - log_p);
-        }
+        for (int i = 0; i < E; ++i) sum += loss_part(share[i], half_of(v[i], v_most), half_of(z_entry[i], p.m), half_sums);
         sum = row_sum(sum);
-        if (lane == 0 && there) a.loss[row] = !some ? 0.f : lost ? quiet() : a.t * a.t * sum;
+        if (lane == 0 && there) a.loss[row] = !some ? 0.f : lost ? quiet() : 2.f * a.t * sum;
     }
     if (!a.dz || !there) return;
     char *const d = (char *)a.dz + (int64_t)row * a.ldd * SIZE;

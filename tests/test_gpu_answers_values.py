@@ -69,3 +69,57 @@ def test_lowest_and_largest_values(ctx, classes, k, dtype):
         want, d_want = both(ctx, z, index, same, t)
         assert want.isfinite().all() and want.abs().min() > 0 and d_want.abs().amax(1).min() > 0
         assert torch.equal(loss, want) and torch.equal(d, d_want), t
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS)
+@pytest.mark.parametrize("k", [5, 20])
+def test_a_student_of_lowest_logits_has_a_finite_loss(ctx, classes, k, dtype):
+    """Where the student's logit of the only entry lies D below its largest
+    one, far from all others, the loss is T^2 (D / T + ln S), S at most the
+    classes: T D is within 2^-24 of it, and infinite only where that is beyond
+    float32. (Three products and a difference, 2^-24 each, and the share's
+    1 + 2^-22.)"""
+    import torch
+    z = make(4, classes, dtype, seed=classes)
+    most = torch.finfo(z.dtype).max
+    index, value = teacher(z, k)
+    value[:, 1:] = -math.inf
+    rows, entry = torch.arange(4, device="cuda"), index[:, 0].long()
+    z[rows, entry] = -most
+    z[1, (entry[1] + 1) % classes] = most
+    z[3, (entry[3] + 1) % classes] = most / 2
+    x = z.double()
+    apart = x.amax(1) - x[rows, entry]
+    for t in (0.1, 0.3, 0.45, 0.7, 1.0, 2.0):
+        loss, d = both(ctx, z, index, value, t)
+        want = t * apart
+        fits = want <= torch.finfo(torch.float32).max
+        assert (t < 0.5) == bool(fits.all())
+        assert ((loss.double() - want).abs()[fits] <= 10 * 2.0 ** -24 * want[fits]).all(), t
+        assert (loss[~fits] == math.inf).all() and d.isfinite().all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("classes", WIDTHS)
+def test_log_probabilities_as_far_as_float32_reaches(ctx, classes, dtype):
+    """-(D / T) - ln S, as above, of labels and best classes: -inf only
+    beyond float32."""
+    import torch
+    z = make(4, classes, dtype, seed=classes)
+    most = torch.finfo(z.dtype).max
+    z[:, 3], z[:, 1] = -most, most
+    z[2, 1], z[3] = most / 4, -math.inf
+    z[3, 3], z[3, 1] = -most, most
+    labels = torch.full((4,), 3, device="cuda", dtype=torch.int32)
+    x = z.double()
+    for t in (0.5, 1.0, 2.5, 4.0, 1000.0):
+        got = ctx.log_probs(z, labels=labels, top=2, temperature=t)
+        want = -(x.amax(1) - x[:, 3]) / t
+        fits = want.abs() <= torch.finfo(torch.float32).max
+        assert (t > 2) == bool(fits.all())
+        for v in (got["log_prob"], got["top_log_probs"][3:4, 1]):
+            w, f = want[-len(v):], fits[-len(v):]
+            assert ((v.double() - w).abs()[f] <= 10 * 2.0 ** -24 * w.abs()[f]).all(), t
+            assert (v[~f] == -math.inf).all()
+        assert got["top_indices"][3].tolist() == [1, 3] and (got["rank"][:3] == classes - 1).all()
