@@ -371,9 +371,32 @@ class MxMatrix:
     rows, 16], both uint8 (include/gemel.h says which byte is which)."""
 
     def __init__(self, codes, scales, rows, cols):
-        self.codes, self.scales = codes, scales
+        self._codes, self._scales = codes, scales
         self.rows, self.cols = rows, cols
         self._c = None   # the C description, once it was checked
+
+    @property
+    def codes(self):
+        return self._codes
+
+    @codes.setter
+    def codes(self, t):
+        self._codes, self._c = t, None   # (another tensor is checked anew)
+
+    @property
+    def scales(self):
+        return self._scales
+
+    @scales.setter
+    def scales(self, t):
+        self._scales, self._c = t, None
+
+    def _key(self, device):
+        """What a description holds for: tensors can be given other memory or
+        another shape in place."""
+        a, b = self._codes, self._scales
+        return (device, self.rows, self.cols, a.data_ptr(), b.data_ptr(),
+                a.shape, b.shape, a.is_contiguous(), b.is_contiguous())
 
     @staticmethod
     def shapes(rows, cols):
@@ -913,8 +936,7 @@ class Context:
         anything in it is another one than the last time)."""
         if not isinstance(q, MxMatrix):
             raise ValueError(f"{name} must be an MxMatrix")
-        c, at = q._c, (self.device, q.rows, q.cols, q.codes.data_ptr(),
-                       q.scales.data_ptr())
+        c, at = q._c, q._key(self.device)
         if c is not None and c[0] == at:
             return c[1]
         _int32(name + " rows", q.rows)
@@ -923,7 +945,7 @@ class Context:
         codes, scales = MxMatrix.shapes(q.rows, q.cols)
         self._tensor(name + ".codes", q.codes, codes, u8)
         self._tensor(name + ".scales", q.scales, scales, u8)
-        q._c = at, Mx(*at[1:])
+        q._c = at, Mx(*at[1:5])
         return q._c[1]
 
     @staticmethod
@@ -951,9 +973,8 @@ class Context:
             codes, scales = MxMatrix.shapes(rows, cols)
             q = MxMatrix(self._empty(x, codes, u8, stream),
                          self._empty(x, scales, u8, stream), rows, cols)
-            at = (self.device, rows, cols, q.codes.data_ptr(),
-                  q.scales.data_ptr())
-            q._c = at, Mx(*at[1:])
+            at = q._key(self.device)
+            q._c = at, Mx(*at[1:5])
         elif (q.rows, q.cols) != (rows, cols):
             raise ValueError(f"out is [{q.rows}, {q.cols}], x [{rows}, {cols}]")
         self._check(self._lib.gemel_mx_quantize(
