@@ -834,7 +834,8 @@ class Context:
         lower index) and "top_log_probs" [rows, top] of the softmax of
         logits / temperature. Classes of -inf are not offered: -1 and -inf
         stand where fewer than `top` are. needs: names of those wanted (None:
-        all); outputs: tensors to write, by name (others are made)."""
+        all); outputs: tensors to write, by name (others are made; a name
+        that is none of these answers is refused)."""
         torch = _torch()
         rows, classes, code = self._logits(logits)
         _int32("top", top)
@@ -846,6 +847,10 @@ class Context:
         if top > 0:
             kinds.update(top_indices=((rows, top), i32),
                          top_log_probs=((rows, top), f32))
+        for name in outputs or ():
+            if name not in kinds:
+                raise ValueError(f"outputs: no answer {name!r} (of these "
+                                 "arguments)")
         res, a = {}, Answers()
         if needs is None and not outputs:
             # the numbers of a row are made together, as rows of one tensor
