@@ -12,6 +12,7 @@ namespace {
 
 constexpr int64_t MAX_ROWS = 1 << 22;
 constexpr int64_t PIECE = 1ll << 27;   // values of float32 rows whose planes (6 bytes each) a pass holds, about
+constexpr int64_t COPIES = 1ll << 30;  // values of copied bf16 rows that a pass holds
 
 gemel_status check_mx(gemel_ctx *ctx, const char *what, const gemel_mx *q, Mx *out) {
     if (!q) return fail(ctx, GEMEL_EINVAL, std::string(what) + " is null");
@@ -87,8 +88,15 @@ gemel_status in_registers(Call &c, const Wide &p) {
     return GEMEL_OK;
 }
 
+// Rows that the bf16 product reads where they are (without a row table it
+// takes any number of them).
+bool in_place(const Wide &p) {
+    return (uintptr_t)p.x % 16 == 0 && p.ldx % 8 == 0 && p.w.cols % 8 == 0 && p.ldx <= MM_MAX_LD;
+}
+
 // bf16 rows otherwise: the weights are expanded to bf16 once and go through
-// the bf16 product, which needs a copy of rows that are not aligned. Which of
+// the bf16 product, which needs a copy of rows that are not aligned, of as many
+// at a time as bound the workspace. Which of
 // the two is taken: up to MX_ROWS rows never this one, slower at each of 10
 // shapes of 256 to 1024 rows; beyond, the one of the smaller estimate, both a
 // fit to these shapes of up to 16384 rows: what is taken is 1.5% from the
@@ -99,9 +107,11 @@ gemel_status in_registers(Call &c, const Wide &p) {
 gemel_status expanded(Call &c, const Wide &p, MmArgs m) {
     gemel_ctx *ctx = c.ctx;
     const int64_t Kp = m.K;
-    const bool copy = !in_place(p.x, p.M, p.ldx, p.w.cols);
+    const bool copy = !in_place(p);
+    const int each = copy ? (int)std::min<int64_t>(p.M, std::max<int64_t>(1024, COPIES / Kp / 256 * 256)) : p.M;
     if (!mm_fits(m)) return fail(ctx, GEMEL_EINVAL, "the product is too large");
-    const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(copy ? p.M * Kp : 0, 2), o_part = c.lay.take(partial_floats(m), 4);
+    m.M = each;   // (tiles and splits stay those of all rows)
+    const size_t o_w = c.lay.take(p.w.rows * Kp, 2), o_x = c.lay.take(copy ? each * Kp : 0, 2), o_part = c.lay.take(partial_floats(m), 4);
     if (gemel_status s = workspace(c)) return s;
     MxCast cast{};
     cast.q = p.w;
@@ -109,31 +119,34 @@ gemel_status expanded(Call &c, const Wide &p, MmArgs m) {
     cast.ld = Kp;
     cast.out_cols = (int)Kp;
     OPCHK(launch_mx_values(cast, c.stream), "weights");
-    m.a = (const u16 *)p.x;
-    m.lda = p.ldx;
-    if (copy) {
-        Jobs jobs;
-        Job j{};
-        j.kind = JOB_PAD;
-        j.in = p.x;
-        j.ldi = p.ldx;
-        j.rows = p.M;
-        j.cols = p.w.cols;
-        j.out = c.at<u16>(o_x);
-        j.ldo = Kp;
-        if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
-        OPCHK(launch_jobs(jobs, c.stream), "copies");
-        m.a = c.at<u16>(o_x);
-        m.lda = Kp;
-    }
     m.b = (const u16 *)cast.out;
     m.ldb = Kp;
     m.zero = (const u16 *)c.st->zero;
     m.partial = c.at<float>(o_part);
-    m.o.out = p.y;
     m.o.ld = p.ldy;
     m.o.bias = p.bias;
-    OPCHK(launch_mm(m, c.stream), "product");
+    for (int r = 0; r < p.M; r += each) {
+        m.M = std::min(each, p.M - r);
+        m.a = (const u16 *)p.x + r * p.ldx;
+        m.lda = p.ldx;
+        if (copy) {
+            Jobs jobs;
+            Job j{};
+            j.kind = JOB_PAD;
+            j.in = m.a;
+            j.ldi = p.ldx;
+            j.rows = m.M;
+            j.cols = p.w.cols;
+            j.out = c.at<u16>(o_x);
+            j.ldo = Kp;
+            if (!add_job(jobs, j)) return fail(ctx, GEMEL_EINVAL, "x is too large");
+            OPCHK(launch_jobs(jobs, c.stream), "copies");
+            m.a = c.at<u16>(o_x);
+            m.lda = Kp;
+        }
+        m.o.out = (u16 *)p.y + r * p.ldy;
+        OPCHK(launch_mm(m, c.stream), "product");
+    }
     return GEMEL_OK;
 }
 
@@ -147,7 +160,7 @@ gemel_status wide_product(Call &c, const Wide &p) {
     m.epi = EPI_ROWS;
     const double bytes = 2.0 * p.M * p.w.cols;   // of the rows; microseconds
     double once = 7 + std::max(0.8 * mm_plan(m), bytes / 2.3e6) + 2.5 * p.w.rows * p.w.cols / 2.4e6;
-    if (!in_place(p.x, p.M, p.ldx, p.w.cols)) once += 5.4 + 2 * bytes / 2.3e6;
+    if (!in_place(p)) once += 5.4 + 2 * bytes / 2.3e6;
     MxRows a{};
     a.w = p.w;
     a.planes = 1;

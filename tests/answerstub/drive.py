@@ -20,7 +20,7 @@ class Driver:
         self.L = L = G.load(path)
         L.hipMalloc.argtypes = [ctypes.POINTER(ctypes.c_void_p), ctypes.c_size_t]
         L.hipFree.argtypes = [ctypes.c_void_p]
-        for name in ("answerstub_violations", "opstub_violations", "hoststub_violations"):
+        for name in ("answerstub_violations", "opstub_violations", "hoststub_violations", "opstub_launches"):
             getattr(L, name).restype = ctypes.c_long
         L.answerstub_names.restype = L.answerstub_last.restype = ctypes.c_char_p
         self.ctx = {}
@@ -69,6 +69,7 @@ class Driver:
         e = 4 if c["dtype"] == "f32" else 2
         code = G.F32 if c["dtype"] == "f32" else G.BF16
         rows, pad, shift = c["rows"], c.get("pad", 0), c.get("shift", 0)
+        others = L.opstub_launches()   # (copies and bf16 products, among them)
         off = c.get("off", {})   # bytes that a pointer is moved by
 
         def mem(name, r, q):
@@ -112,7 +113,7 @@ class Driver:
             L.hipFree(p)
         self.held = []
         return {"status": st, "message": (L.gemel_last_error(ctx) or b"").decode() if st else "",
-                "kernels": L.answerstub_names().decode()}
+                "kernels": L.answerstub_names().decode(), "others": L.opstub_launches() - others}
 
 
 def main():
