@@ -24,6 +24,13 @@ bool form_of(const Logits &l) {
 }
 }  // namespace
 
+int64_t answer_groups(const Logits &l) {
+    const int teams = answer_teams(l.waves);
+    return ((int64_t)l.rows + teams - 1) / teams;
+}
+
+static bool threads_fit(const Logits &l) { return answer_groups(l) * answer_threads(l.waves) <= MAX_THREADS; }
+
 // The smallest form that holds a row (16 lanes search each of the best
 // classes in turn: only a few; 65536 rows of 80 classes, 16 lanes against a
 // wave: 5 best 17 and 48 us, 20 best 46 and 92, 64 best in a wave 74); wide
@@ -39,25 +46,21 @@ void score_plan(Logits &l, int top) {
 // The smallest form that holds a row; rows beyond the largest in chunks of
 // its own after a pass for their sums (2048 rows of 100003 bf16 287 us, of
 // which the sums take 100; held in one workgroup's registers, 16 waves of 16
-// pieces spill).
+// pieces spill). So are 2^22 rows that would take 16 waves each, more threads
+// than a launch has.
 void distill_plan(Logits &l) {
     for (int i : {0, 1, 2, 3, 4, 5, 6, 7, 9, 10}) {
         cut(l, answer_forms[i]);
-        if (l.chunks == 1) return;
+        if (l.chunks == 1 && threads_fit(l)) return;
     }
     cut(l, answer_forms[6]);
-}
-
-int64_t answer_groups(const Logits &l) {
-    const int teams = answer_teams(l.waves);
-    return ((int64_t)l.rows + teams - 1) / teams;
 }
 
 static bool logits_valid(const Logits &l) {
     return l.z && l.rows > 0 && l.classes > 0 && l.ld >= l.classes && form_of(l) && l.chunk > 0 &&
            l.chunk <= answer_lanes(l.waves) * l.vecs * answer_vec(l.f32) && l.chunks >= 1 && l.chunks <= 65535 &&
            (int64_t)l.chunk * l.chunks >= l.classes && (int64_t)l.chunk * (l.chunks - 1) < l.classes && l.c > 0 && l.inv_t > 0 &&
-           (uintptr_t)l.z % (l.f32 ? 4 : 2) == 0 && answer_groups(l) * answer_threads(l.waves) <= MAX_THREADS;
+           (uintptr_t)l.z % (l.f32 ? 4 : 2) == 0 && threads_fit(l);
 }
 
 bool score_valid(const ScoreArgs &a) {
