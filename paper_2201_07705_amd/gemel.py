@@ -948,8 +948,8 @@ class Context:
         _int32(name + " cols", q.cols)
         u8 = _torch().uint8
         codes, scales = MxMatrix.shapes(q.rows, q.cols)
-        self._tensor(name + ".codes", q.codes, codes, u8)
-        self._tensor(name + ".scales", q.scales, scales, u8)
+        self._tensor(name + ".codes", q._codes, codes, u8)
+        self._tensor(name + ".scales", q._scales, scales, u8)
         q._c = at, Mx(*at[1:5])
         return q._c[1]
 
@@ -980,11 +980,15 @@ class Context:
                          self._empty(x, scales, u8, stream), rows, cols)
             at = q._key(self.device)
             q._c = at, Mx(*at[1:5])
-        elif (q.rows, q.cols) != (rows, cols):
-            raise ValueError(f"out is [{q.rows}, {q.cols}], x [{rows}, {cols}]")
+            c = q._c[1]
+        else:
+            if (q.rows, q.cols) != (rows, cols):
+                raise ValueError(f"out is [{q.rows}, {q.cols}], "
+                                 f"x [{rows}, {cols}]")
+            c = self._mx("out", q)
         self._check(self._lib.gemel_mx_quantize(
-            self._h, x.data_ptr(), self._stride(x), code, self._mx("out", q),
-            self._stream(stream, x, q.codes, q.scales)))
+            self._h, x.data_ptr(), self._stride(x), code, c,
+            self._stream(stream, x, q._codes, q._scales)))
         if out is not None:
             self._written(q.codes, q.scales)
         return q
@@ -995,14 +999,15 @@ class Context:
         c = self._mx("q", q)
         dt = dtype or (out.dtype if out is not None else self._torch_dtype())
         code = self._value_type("dtype", dt)
-        v = out
+        v, ldv = out, q.cols
         if v is None:
             v = self._empty(q.codes, (q.rows, q.cols), dt, stream)
         else:
             self._tensor("out", v, (q.rows, q.cols), dt, contiguous=False)
+            ldv = self._stride(v)
         self._check(self._lib.gemel_mx_dequantize(
-            self._h, c, v.data_ptr(), self._stride(v), code,
-            self._stream(stream, q.codes, q.scales, v)))
+            self._h, c, v.data_ptr(), ldv, code,
+            self._stream(stream, q._codes, q._scales, v)))
         if out is not None:
             self._written(out)
         return v
@@ -1018,7 +1023,7 @@ class Context:
             rows, xq, base = x.rows, self._mx("x", x), x.codes
             if x.cols != k:
                 raise ValueError(f"x has {x.cols} columns, weight {k}")
-            data, stride, used = None, 0, (x.codes, x.scales)
+            data, stride, used = None, 0, (x._codes, x._scales)
         else:
             if x.dim() != 2:
                 raise ValueError("x must be [rows, n_in]")
@@ -1028,16 +1033,16 @@ class Context:
             data, stride, used = x.data_ptr(), self._stride(x), (x,)
         if bias is not None:
             self._tensor("bias", bias, (n,), _torch().float32)
-        y = out
+        y, ldy = out, n
         if y is None:
             y = self._empty(base, (rows, n), dt, stream)
         else:
             self._tensor("out", y, (rows, n), dt, contiguous=False)
+            ldy = self._stride(y)
         self._check(self._lib.gemel_mx_product(
             self._h, rows, data, stride, xq, w,
-            None if bias is None else bias.data_ptr(), y.data_ptr(),
-            self._stride(y),
-            self._stream(stream, *used, weight.codes, weight.scales, bias, y)))
+            None if bias is None else bias.data_ptr(), y.data_ptr(), ldy,
+            self._stream(stream, *used, weight._codes, weight._scales, bias, y)))
         if out is not None:
             self._written(out)
         return y
