@@ -11,7 +11,7 @@ model needs for itself:
     distill_backward  how far its logits are from the teachers' best, and the gradient
     adapt_backward    gradients of the weights, the bias and all adapters
     muon_step         orthogonalised momentum updates
-    mx_quantize       the float32 weights as 4-bit ones, a quarter of the bf16 copy's memory
+    mx_quantize       the float32 weights as 4-bit ones
     mx_product        frames through them
     log_probs         and what they answer
 

@@ -850,8 +850,8 @@ gemel_status gemel_muon_step(gemel_ctx *ctx, int32_t count, int32_t rows,
  * that holds a NaN or +inf gives NaN and -1, and no other row is touched by
  * it. Calls with rows of more than 4096 (float32) or 8192 (bf16) classes may
  * take a workspace; others can be captured without a call of their sizes
- * before (but for a context's first one). rows 0 is no error and touches
- * nothing.
+ * before (but for a context's first one). rows is at most 2^22; 0 is no error
+ * and touches nothing.
  */
 
 /* Outputs of gemel_log_probs; each may be NULL (not computed). */
@@ -893,7 +893,9 @@ gemel_status gemel_log_probs(gemel_ctx *ctx, int32_t rows, int32_t classes,
  *          there; entries of one class add up. A row without entries has
  *          loss 0 and no gradient, whatever its logits hold.
  * A class outside -1..classes-1, or a value of NaN or +inf, makes its row
- * NaN; a class that the student does not offer makes its loss +inf.
+ * NaN, and so do entries of a row whose logits offer no class; a class that
+ * the student does not offer beside others makes its loss +inf. The lowest
+ * finite values are values like others at every temperature.
  * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
  */
 gemel_status gemel_distill(gemel_ctx *ctx, int32_t rows, int32_t classes,
@@ -923,11 +925,14 @@ gemel_status gemel_distill_backward(gemel_ctx *ctx, int32_t rows,
 /*
  * ---- Merged layers in 4 bits ----
  *
- * A quarter of the memory of bf16 weights: blocks of 32 values of a row, each
- * a 4-bit floating-point number, share a power of two (microscaling). The
+ * Blocks of 32 values of a row, each a 4-bit floating-point number, share a
+ * power of two (microscaling). A row takes 272 bytes for every 512 columns
+ * begun: 0.27 of bf16 where it is whole groups of 512, more where it is
+ * short (576 columns 0.47, 256 columns 0.53; 64 columns twice bf16). The
  * weights of a merged projection are quantised once and multiply rows as
- * they are, or rows that are quantised too. The conventions of the calls
- * above hold; rows 0 is no error and touches nothing.
+ * they are, or rows that are quantised too; the caller holds them, and
+ * gemel_infer and its weight budget do not use them. The conventions of the
+ * calls above hold; rows 0 is no error and touches nothing.
  */
 
 /*
@@ -971,9 +976,12 @@ gemel_status gemel_mx_dequantize(gemel_ctx *ctx, const gemel_mx *q, void *out,
  * xq [rows][n_in], quantised; the other one is NULL. Products are exact and
  * sums float32, with the exceptions that x of float32 loses what is below
  * 2^-126, and that a value of xq or weight is taken with its scale whatever
- * it is (products below 2^-126 may be dropped). A row of x, or a block, that
- * holds a value that is not finite gives rows, or columns, that are not
- * finite.
+ * it is (products below 2^-126 may be dropped). Weights of 2^128 and more
+ * (scale bytes 253 and 254, which gemel_mx_quantize does not write) overflow
+ * against x. A row of x, or a block, that holds a value that is not finite
+ * gives rows, or columns, that are not finite. rows is at most 2^22. The
+ * order of sums of more than 1024 bf16 rows of x depends, beside the sizes,
+ * on whether x and its rows are aligned to 16 bytes.
  * Errors: EINVAL, ENOMEM, EDEVICE, ESTATE.
  */
 gemel_status gemel_mx_product(gemel_ctx *ctx, int32_t rows, const void *x,

@@ -35,8 +35,8 @@ static bool threads_fit(const Logits &l) { return answer_groups(l) * answer_thre
 // classes in turn: only a few; 65536 rows of 80 classes, 16 lanes against a
 // wave: 5 best 17 and 48 us, 20 best 46 and 92, 64 best in a wave 74); wide
 // rows in chunks of 4 waves of 4 pieces (2048 rows of 100003 bf16, 20 best:
-// 157 us; of 2 pieces 248, of 8 in 4 waves 159, of 4 and 8 in 8 waves 209 and
-// 226), larger ones only where there would be more than 64.
+// 147 us; of 2 pieces 205, of 4 and 8 pieces in 8 waves 200 and 218), larger
+// ones only where there would be more than 64.
 void score_plan(Logits &l, int top) {
     for (int i = top <= 32 ? 0 : 2; i < 9; ++i) {
         cut(l, answer_forms[i]);
@@ -45,7 +45,7 @@ void score_plan(Logits &l, int top) {
 }
 // The smallest form that holds a row; rows beyond the largest in chunks of
 // its own after a pass for their sums (2048 rows of 100003 bf16 287 us, of
-// which the sums take 100; held in one workgroup's registers, 16 waves of 16
+// which the sums take 95; held in one workgroup's registers, 16 waves of 16
 // pieces spill). So are 2^22 rows that would take 16 waves each, more threads
 // than a launch has.
 void distill_plan(Logits &l) {

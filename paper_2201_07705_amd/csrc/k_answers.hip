@@ -376,7 +376,7 @@ constexpr int CANDIDATES = 256;
 // with 64; short rows, those that a row needs once. 2048 rows of 100003 bf16
 // with their 20 best: searched one after the other 1480 us, as candidates 278,
 // in chunks of 4 waves instead of 8 with twice the elements 147 (the sums alone
-// 96, reading 80); 16384 rows of 1001 with 5: 34 and 18 us.
+// 95, reading 80); 16384 rows of 1001 with 5: 34 and 18 us.
 template <bool F32, int W, int V>
 __global__ __launch_bounds__((W == 1 ? 256 : W * 64), V < 8 ? 8 : 4) void score_kernel(const ScoreArgs a) {
     constexpr int VEC = F32 ? 4 : 8, TEAMS = answer_teams(W);
@@ -655,9 +655,9 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
 //   dz = dloss T (p - q),
 // entries of one class added up. Every wave of a team keeps entry i in lane
 // i. What bounds it: reading and writing, which overlap only between the
-// workgroups of a compute unit: 4096 rows of 65537 bf16 take 330 us where one
-// fits (all pieces in registers), 243 where two do (4 of 9 pieces in LDS);
-// a copy of as many bytes 211. What a lane writes for a class with an entry it overwrites itself, so
+// workgroups of a compute unit: 4096 rows of 65537 bf16 take 302 us where one
+// fits (all pieces in registers), 245 where two do (4 of 9 pieces in LDS);
+// a copy of as many bytes 201. What a lane writes for a class with an entry it overwrites itself, so
 // that the order of the two stores is that of the program.
 template <bool F32, int W, int V, int L = 0>
 __global__ __launch_bounds__((W == 1 ? 256 : W * 64), 8) void distill_kernel(const DistillArgs a) {

@@ -8,7 +8,7 @@
 // columns to a lane, with all loads in flight before the first is used; the
 // 4 lanes of a block agree on its scale by two lane moves, and the conversion
 // to 4 bits is the hardware's (it divides by the scale and rounds as above).
-// 4096 x 25088 float32 in 86 us (5.4 TB/s), its values again in 88 (117 for
+// 4096 x 25088 float32 in 86 us (5.4 TB/s), its values again in 88 (116 for
 // the first while the values of the call before are still written back);
 // 16384 x 4096 bf16 in 34.
 #include <hip/hip_runtime.h>

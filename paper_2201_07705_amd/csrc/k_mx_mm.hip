@@ -43,10 +43,10 @@ __device__ __forceinline__ void fetch(const uint8_t *base, const uint32_t (&off)
 // with the first of them.
 //
 // 16384 rows 4096 -> 4096 158 us (3480 TFLOP/s), 8192^3 270 to 281 (4000).
-// What bounds it: the matrix instructions with the LDS reads that feed them,
-// at a clock that falls to 2.0 GHz (matrix cores busy 42% of all cycles, LDS
-// 27%). Trials without the fetches take 135 us, without the stores of the
-// results 153, without the barriers 157. Two stages of 256 columns instead of
+// What bounds it is not one unit: the matrix cores are busy 42% of all cycles,
+// LDS 27%, at a clock that falls to 2.0 GHz; with one workgroup, two waves to
+// a SIMD, they wait for each other. Trials without the fetches take 135 us,
+// without the stores of the results 153, without the barriers 157. Two stages of 256 columns instead of
 // four of 128, or fragments read before instead of among the products, took
 // the same.
 template <int T>

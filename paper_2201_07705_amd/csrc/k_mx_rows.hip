@@ -98,7 +98,7 @@ __global__ __launch_bounds__(1024) void mx_few_kernel(const MxRows a) {
 // the fragment reads of 16 rows fall on distinct banks); rows and codes are
 // loaded one or two steps ahead. A fragment of the rows serves NB products:
 // with NB = 2 LDS is as busy as the matrix cores (1024 float32 rows 25088 ->
-// 4096 in 510 us; NB = 4 473, 1330 TFLOP/s of bf16 products).
+// 4096 in 510 us; NB = 4 469, 1350 TFLOP/s of bf16 products).
 template <int P, int MB, int NB>
 __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
     constexpr int ROWS = 16 * MB, CHUNKS = P * ROWS * 16, LOADS = mx_piece_loads(P * ROWS);
@@ -109,7 +109,7 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
     const int N = a.w.rows, K = a.w.cols, n0 = blockIdx.x * 128 * NB + wave * 16 * NB, m0 = blockIdx.z * ROWS;
     const int64_t pitch = mx_pitch(K);
     const int step0 = (int)blockIdx.y * a.per, steps = min((K + 127) / 128 - step0, a.per);
-    uint32_t codes[NB], scales[NB];   // (offsets: up to 2^20 outputs of 2^12 bytes of a group)
+    uint32_t codes[NB], scales[NB];   // (from the wave's first output: up to 63 rows of 2^19 bytes)
     const uint8_t *const code0 = a.w.codes + (int64_t)min(n0, N - 1) * pitch, *const scale0 = a.w.scales + (int64_t)min(n0, N - 1) * 16;
 #pragma unroll
     for (int j = 0; j < NB; ++j) {
@@ -167,8 +167,8 @@ __global__ __launch_bounds__(512, 2) void mx_rows_kernel(const MxRows a) {
         if (k + AHEAD < steps) load(q, step0 + k + AHEAD);
         // Fragments of the rows, the one of piece i, plane p, block b being the
         // (i P + p) MB + b-th: read AHEAD_READS before they are used, so that the
-        // matrix cores do not wait for LDS (1024 rows 25088 -> 4096 bf16 210 us,
-        // read where they are used 237; float32 473 and 498; 3 and 6 ahead
+        // matrix cores do not wait for LDS (1024 rows 25088 -> 4096 bf16 209 us,
+        // read where they are used 237; float32 469 and 498; 3 and 6 ahead
         // instead of 2 and 4 within 1.5%, with 4 to 8 registers more).
         constexpr int READS = 4 * P * MB, AHEAD_READS = NB == 4 ? 2 : 4, RING = AHEAD_READS + 1;
         mx_bf16x8 v[RING], f[NB];

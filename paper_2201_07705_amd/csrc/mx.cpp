@@ -47,7 +47,7 @@ struct Wide {
 
 // float32 rows, and bf16 ones where that is expected to take less time: the
 // weights are expanded in registers (float32, planes below each other through
-// the bf16 product instead: 1024 rows 25088 -> 4096 473 us and 685, 16384 rows
+// the bf16 product instead: 1024 rows 25088 -> 4096 469 us and 685, 16384 rows
 // 8.2 and 8.9 ms, 4096 -> 4096 1.25 and 1.7). Planes of float32 rows are made
 // for a piece of the rows at a time, which bounds the workspace.
 gemel_status in_registers(Call &c, const Wide &p) {
@@ -100,7 +100,7 @@ bool in_place(const Wide &p) {
 // the two is taken: up to MX_ROWS rows never this one, slower at each of 10
 // shapes of 256 to 1024 rows; beyond, the one of the smaller estimate, both a
 // fit to these shapes of up to 16384 rows: what is taken is 1.5% from the
-// faster one in the mean, 26% at worst. 25088 -> 4096: 1024 rows 211 us in
+// faster one in the mean, 26% at worst. 25088 -> 4096: 1024 rows 209 us in
 // registers, expanded once 248, 2048 rows 393 and 398, 4096 rows 781 and 689;
 // 1000 -> 1000 4096 rows 16.3 and 25.6; 21990 -> 856 (copied) 3451 rows 183
 // and 321.

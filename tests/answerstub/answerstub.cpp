@@ -1,6 +1,8 @@
 // CPU stand-in for the kernels of answers, distillation and 4-bit matrices,
-// beside that of ../opstub: every launch checks that each range its kernel
-// would read or write is one that may be accessed.
+// beside that of ../opstub: every launch checks that its operands and results
+// are, as wholes, ranges that may be accessed. The addresses that threads form
+// inside of them are the kernels' own; they are enumerated for the rows of x of
+// mx_rows_kernel alone (touch_pieces here, and pieces.cpp).
 #include <sanitizer/asan_interface.h>
 
 #include <cstdio>

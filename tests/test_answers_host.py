@@ -1,9 +1,10 @@
 """The host code of answers, distillation and 4-bit matrices (checks, plans,
 workspaces, argument blocks) compiled for the CPU with AddressSanitizer and
-driven through calls of many shapes. Every launch checks that each range its
-kernel would read or write may be accessed: operands and results are
-allocated to their last byte, and the pieces of a workspace have gaps between
-them that may not be touched. No GPU is needed."""
+driven through calls of many shapes. Every launch checks that its operands and
+results may be accessed as wholes: they are allocated to their last byte, and
+the pieces of a workspace have gaps between them that may not be touched. What
+a kernel's threads address within them is not looked at, but for the rows of
+products with more than 16 of them. No GPU is needed."""
 
 import json
 import os
